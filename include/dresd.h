@@ -258,6 +258,121 @@ dresd_status dresd_retrieve_quantised(dresd_store *store, const void *queries, c
                                       int32_t *out_tokens, void *stream);
 
 /*
+ * Paged key/value cache of the language model that verifies the drafts, and its attention.
+ * Batch verification (Section 3.6) runs the language model on the n x L draft matrix behind
+ * the tokens it has already read; the keys and values of those tokens are kept here, so that
+ * a step computes only its new tokens.  Per step and layer a caller appends the new tokens'
+ * keys and values, attends, and -- once dresd_drafts_accept() has chosen a draft -- keeps the
+ * accepted tokens and drops the rest by counting on from them.
+ *
+ * The cache is PAGED: the tokens of a sequence lie in pages of `page_size` tokens anywhere in
+ * the pool, found through a table.  Keys and values have arrays of their own:
+ *
+ *   k_pages, v_pages  device, [layers][num_pages][kv_heads][page_size][head_dim] row-major,
+ *                     16-byte aligned, in `dtype` -- or one byte per element when the
+ *                     cache is 8-bit (k_exps / v_exps not NULL)
+ *   k_exps, v_exps    device, uint8 [layers][num_pages][kv_heads][page_size], or both NULL
+ *   dtype             DRESD_F16 or DRESD_BF16: the type of queries, keys and values handed in
+ *                     and out
+ *   head_dim          64 or 128;  page_size 16, 32, 64 or 128
+ *
+ * 8-bit rows (one token, one head) are held in E4M3 with one power-of-two scale:
+ *     e       = the least integer with max_j |x_j| <= 448 2^e, but at least -24 (fp16) or
+ *               -126 (bf16); 0 for a row of zeros.  Magnitudes above 61440 (fp16) or
+ *               1.875 2^127 (bf16), infinities included, count as that bound.
+ *     code_j  = e4m3(x_j 2^-e), rounded to nearest even;  exponent byte = e + 127
+ *     value_j = code_j 2^e, which `dtype` represents exactly
+ * A row that holds a NaN gives unspecified values.
+ *
+ * All arrays are BORROWED.  dresd_kv_create() allocates the workspace of the attention on the
+ * current device (about 50 MB) and launches nothing.  A cache is bound to its device and may be used
+ * from one stream at a time; the calls below are asynchronous on `stream`, allocate nothing
+ * and can be captured into a CUDA graph.
+ */
+typedef struct dresd_kv dresd_kv; /* opaque handle */
+
+dresd_status dresd_kv_create(void *k_pages, void *v_pages, uint8_t *k_exps, uint8_t *v_exps, int layers,
+                             int64_t num_pages, int kv_heads, int page_size, int head_dim, dresd_dtype dtype,
+                             dresd_kv **out_kv);
+void dresd_kv_destroy(dresd_kv *kv); /* frees the workspace only; NULL is allowed */
+
+/*
+ * A batch of chunks: sequence b has ctx[b] tokens in the cache and start[b+1] - start[b] new
+ * ones, rows start[b] .. of the dense tensors.  New token i has position ctx[b] + i and
+ * lies in page page_table[b][position / page_size].  All arrays are device memory and read
+ * when the kernels run.  Nothing here is checked on the host; the kernels take a start[]
+ * entry outside 0 .. rows as the nearer bound, a negative ctx as 0, and tokens whose page
+ * number is outside 0 .. num_pages - 1 or beyond the table are not written, read as zeros, and
+ * give unspecified attention results (but no access outside the arrays).
+ *   rows       rows of the dense tensors (start[B])
+ *   max_chunk  the longest chunk, or 0 if unknown (then rows is taken): only the choice of
+ *              kernel depends on it
+ */
+typedef struct {
+    const int32_t *page_table; /* [B][table_width] */
+    const int32_t *ctx;        /* [B]     */
+    const int32_t *start;      /* [B + 1] */
+    int32_t B, table_width, rows, max_chunk;
+} dresd_kv_batch;
+
+/*
+ * dresd_kv_append   writes the keys and values of a chunk into the cache (quantising them on
+ *                   the way when it is 8-bit).  k, v: device, [rows][kv_heads][head_dim] with
+ *                   the distances `k_row`, `k_head` (in elements) between rows and heads -- slices of a
+ *                   joint projection need no copy; addresses and distances multiples of
+ *                   16 bytes.
+ * dresd_kv_read     the mirror image: positions ctx[b] .. of every sequence, brought back in
+ *                   `dtype`: out_k, out_v device, dense [rows][kv_heads][head_dim].
+ */
+dresd_status dresd_kv_append(dresd_kv *kv, int layer, const dresd_kv_batch *batch, const void *k, int64_t k_row,
+                             int64_t k_head, const void *v, int64_t v_row, int64_t v_head, void *stream);
+dresd_status dresd_kv_read(dresd_kv *kv, int layer, const dresd_kv_batch *batch, void *out_k, void *out_v,
+                           void *stream);
+
+/*
+ * Attention of the new tokens over the cache (which holds them already):
+ *     out[t][h] = sum_j softmax_j(scale q[t][h] . k_j) v_j,   j over the positions t sees,
+ * keys and values of head h / (heads / kv_heads).  Token i of a chunk sees every position before the
+ * chunk, and of the chunk the tokens 0 .. i (mask NULL) or those whose bit is set.
+ *
+ *   q          device, [rows][heads][head_dim] in `dtype`, distances q_row / q_head in elements as above;
+ *              heads a multiple of kv_heads, at most 64 per kv head
+ *   mask       device, [rows][mask_words]: bit j % 32 of word j / 32 of row t = 1: t sees token j of its
+ *              own chunk (bits beyond the chunk are ignored, missing words count as 0).  A chunk of a
+ *              sequence's last token and its n drafts of L tokens sets, for token
+ *              1 + r L + t, the bits 0 and 1 + r L .. 1 + r L + t.
+ *   out        device, dense [rows][heads][head_dim] in `dtype`
+ *   out_lse    device, fp32 [rows][heads], or NULL: ln sum_j exp(scale q.k_j)
+ *
+ * Products of 16-bit numbers, sums, maxima and exponentials in fp32; the weights of the second
+ * product are rounded to `dtype` once.  A token that sees nothing gets zeros and -infinity.
+ * Keys and values that a token does not see take no part whatever they hold, NaN included;
+ * so do the unused places of a page.  Non-finite values that it does see give
+ * non-finite results.  The order of summation depends on the lengths only.
+ */
+dresd_status dresd_kv_attend(dresd_kv *kv, int layer, const dresd_kv_batch *batch, const void *q, int64_t q_row,
+                             int64_t q_head, int heads, float scale, const uint32_t *mask, int mask_words, void *out,
+                             float *out_lse, void *stream);
+
+/*
+ * After dresd_drafts_accept(): the chunk of sequence b was its last token and n drafts of L tokens, and
+ * draft best[b] was accepted with length[b] tokens, the last of them the model's own (not yet in the
+ * cache).  Moves the accepted draft's tokens in ALL layers from places 1 + best L + t of the
+ * chunk to places 1 + t, t < length - 1, so that the sequence goes on with
+ * ctx[b] + length[b] tokens.  best < 0 (none was valid) moves nothing; best 0 is in place
+ * already.  batch: page_table, ctx, B and table_width are used.
+ *   best, length   device, int32 [B]: out_best, out_len of dresd_drafts_accept()
+ */
+dresd_status dresd_kv_keep_draft(dresd_kv *kv, const dresd_kv_batch *batch, const int32_t *best, const int32_t *length,
+                                 int n, int L, void *stream);
+
+/* dresd_store_status() for a cache: waits for its last stream, reports and clears its status word. */
+dresd_status dresd_kv_status(dresd_kv *kv);
+
+/* Kernels enqueued by the cache's last call. */
+int dresd_kv_last_launches(const dresd_kv *kv);
+
+/*
  * Process-wide switches (not part of the paper; for measurement and tests).
  *   "build_keys_pairs"  1 (default): dresd_build_keys runs on CTA pairs -- clusters of two
  *                       CTAs, one tensor-core instruction spanning both SMs, each CTA staging

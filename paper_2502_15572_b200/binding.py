@@ -34,7 +34,16 @@ EXPORTS = (
     "dresd_merge_shards", "dresd_build_keys", "dresd_fit_zscore", "dresd_set_global_option", "dresd_quantise_keys", "dresd_store_attach_quantised",
     "dresd_retrieve_quantised", "dresd_store_index_first_tokens", "dresd_merge_shards_packed",
     "dresd_noalloc_status", "dresd_debug_build", "dresd_store_debug_selftest",
+    "dresd_kv_create", "dresd_kv_destroy", "dresd_kv_append", "dresd_kv_read", "dresd_kv_attend",
+    "dresd_kv_keep_draft", "dresd_kv_status", "dresd_kv_last_launches",
 )
+
+
+class dresd_kv_batch(ctypes.Structure):
+    """The C struct: device addresses of a batch of chunks, and its sizes."""
+    _fields_ = [("page_table", ctypes.c_void_p), ("ctx", ctypes.c_void_p), ("start", ctypes.c_void_p),
+                ("B", ctypes.c_int32), ("table_width", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("max_chunk", ctypes.c_int32)]
 
 
 class DresdError(RuntimeError):
@@ -117,6 +126,23 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.dresd_debug_build.argtypes = []
     lib.dresd_store_debug_selftest.restype = i32
     lib.dresd_store_debug_selftest.argtypes = [vp, vp]
+    batch = c.POINTER(dresd_kv_batch)
+    lib.dresd_kv_create.restype = i32
+    lib.dresd_kv_create.argtypes = [vp, vp, vp, vp, i32, i64, i32, i32, i32, i32, c.POINTER(vp)]
+    lib.dresd_kv_destroy.restype = None
+    lib.dresd_kv_destroy.argtypes = [vp]
+    lib.dresd_kv_append.restype = i32
+    lib.dresd_kv_append.argtypes = [vp, i32, batch, vp, i64, i64, vp, i64, i64, vp]
+    lib.dresd_kv_read.restype = i32
+    lib.dresd_kv_read.argtypes = [vp, i32, batch, vp, vp, vp]
+    lib.dresd_kv_attend.restype = i32
+    lib.dresd_kv_attend.argtypes = [vp, i32, batch, vp, i64, i64, i32, f32, vp, i32, vp, vp, vp]
+    lib.dresd_kv_keep_draft.restype = i32
+    lib.dresd_kv_keep_draft.argtypes = [vp, batch, vp, vp, i32, i32, vp]
+    lib.dresd_kv_status.restype = i32
+    lib.dresd_kv_status.argtypes = [vp]
+    lib.dresd_kv_last_launches.restype = i32
+    lib.dresd_kv_last_launches.argtypes = [vp]
     if path is None:
         _lib = lib
     return lib
@@ -285,6 +311,46 @@ def dresd_noalloc_status(stream: int = 0) -> None:
     _check(load().dresd_noalloc_status(stream))
 
 
+def dresd_kv_create(k_pages_ptr: int, v_pages_ptr: int, k_exps_ptr, v_exps_ptr, layers: int, num_pages: int,
+                    kv_heads: int, page_size: int, head_dim: int, dtype: int) -> int:
+    h = ctypes.c_void_p()
+    _check(load().dresd_kv_create(k_pages_ptr, v_pages_ptr, k_exps_ptr, v_exps_ptr, layers, num_pages, kv_heads,
+                                  page_size, head_dim, dtype, ctypes.byref(h)))
+    return h.value
+
+
+def dresd_kv_append(kv: int, layer: int, batch: dresd_kv_batch, k_ptr: int, k_row: int, k_head: int, v_ptr: int,
+                    v_row: int, v_head: int, stream: int = 0) -> None:
+    _check(load().dresd_kv_append(kv, layer, batch, k_ptr, k_row, k_head, v_ptr, v_row, v_head, stream))
+
+
+def dresd_kv_read(kv: int, layer: int, batch: dresd_kv_batch, out_k_ptr: int, out_v_ptr: int, stream: int = 0) -> None:
+    _check(load().dresd_kv_read(kv, layer, batch, out_k_ptr, out_v_ptr, stream))
+
+
+def dresd_kv_attend(kv: int, layer: int, batch: dresd_kv_batch, q_ptr: int, q_row: int, q_head: int, heads: int,
+                    scale: float, mask_ptr, mask_words: int, out_ptr: int, out_lse_ptr, stream: int = 0) -> None:
+    _check(load().dresd_kv_attend(kv, layer, batch, q_ptr, q_row, q_head, heads, scale, mask_ptr, mask_words, out_ptr,
+                                  out_lse_ptr, stream))
+
+
+def dresd_kv_keep_draft(kv: int, batch: dresd_kv_batch, best_ptr: int, length_ptr: int, n: int, L: int,
+                        stream: int = 0) -> None:
+    _check(load().dresd_kv_keep_draft(kv, batch, best_ptr, length_ptr, n, L, stream))
+
+
+def dresd_kv_status(kv: int) -> None:
+    _check(load().dresd_kv_status(kv))
+
+
+def dresd_kv_last_launches(kv: int) -> int:
+    return int(load().dresd_kv_last_launches(kv))
+
+
+def dresd_kv_destroy(kv: int) -> None:
+    load().dresd_kv_destroy(kv)
+
+
 # ---- torch convenience ----------------------------------------------------------
 def _torch():
     import torch
@@ -435,6 +501,151 @@ class Store:
     def close(self):
         if getattr(self, "handle", None):
             dresd_store_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def draft_mask(n: int, L: int, device="cuda"):
+    """Visibility bits of a chunk that is a sequence's last token and its n drafts of L tokens, int32
+    [1 + n L][words]: every token sees the first one and its own draft up to itself."""
+    import numpy as np
+    size = 1 + n * L
+    seen = np.zeros((size, (size + 31) // 32 * 32), dtype=np.uint8)
+    seen[:, 0] = 1
+    for r in range(n):
+        at = 1 + r * L
+        seen[at:at + L, at:at + L] = np.tri(L, dtype=np.uint8)
+    words = np.packbits(seen, axis=1, bitorder="little").view("<i4")
+    return _torch().from_numpy(np.ascontiguousarray(words)).to(device)
+
+
+class KvBatch:
+    """A batch of chunks (``dresd_kv_batch``): int32 CUDA tensors, borrowed; their contents are read when a call runs."""
+
+    def __init__(self, page_table, ctx, start, rows: int, max_chunk: int = 0):
+        torch = _torch()
+        for name, t, dims in (("page_table", page_table, 2), ("ctx", ctx, 1), ("start", start, 1)):
+            if not t.is_cuda or t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous():
+                raise DresdError(-1, f"{name} must be a contiguous int32 CUDA tensor with {dims} dimension(s)")
+        B, width = page_table.shape
+        if ctx.shape[0] != B or start.shape[0] != B + 1:
+            raise DresdError(-1, f"ctx has {ctx.shape[0]} and start {start.shape[0]} entries for {B} sequences")
+        self.page_table, self.ctx, self.start = page_table, ctx, start          # keep alive
+        self.B, self.rows, self.max_chunk = B, rows, max_chunk
+        self.c = dresd_kv_batch(page_table.data_ptr(), ctx.data_ptr(), start.data_ptr(), B, width, rows, max_chunk)
+
+
+class KvCache:
+    """A paged key/value cache on the current CUDA device; tensors passed in are borrowed.
+
+    k_pages, v_pages: [layers][num_pages][kv_heads][page_size][head_dim] in `dtype`, or uint8 with
+    k_exps, v_exps: uint8 [layers][num_pages][kv_heads][page_size] (8-bit rows)."""
+
+    def __init__(self, k_pages, v_pages, dtype: str, k_exps=None, v_exps=None):
+        torch = _torch()
+        if dtype not in ("f16", "bf16"):
+            raise DresdError(-2, f"the cache holds f16, bf16 or 8-bit rows, not {dtype}")
+        self.torch_dtype = {"f16": torch.float16, "bf16": torch.bfloat16}[dtype]
+        if (k_exps is None) != (v_exps is None):
+            raise DresdError(-1, "k_exps and v_exps go together")
+        held = self.torch_dtype if k_exps is None else torch.uint8
+        for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+            if not t.is_cuda or t.dtype != held or t.dim() != 5 or not t.is_contiguous():
+                raise DresdError(-1, f"{name} must be a contiguous {held} CUDA tensor with 5 dimensions")
+        if v_pages.shape != k_pages.shape:
+            raise DresdError(-1, "k_pages and v_pages must have the same shape")
+        for name, t in (("k_exps", k_exps), ("v_exps", v_exps)):
+            if t is not None and (not t.is_cuda or t.dtype != torch.uint8 or t.shape != k_pages.shape[:4] or
+                                  not t.is_contiguous()):
+                raise DresdError(-1, f"{name} must be a contiguous uint8 CUDA tensor of shape {tuple(k_pages.shape[:4])}")
+        self.dtype = dtype
+        self.k_pages, self.v_pages, self.k_exps, self.v_exps = k_pages, v_pages, k_exps, v_exps   # keep alive
+        self.layers, self.num_pages, self.kv_heads, self.page_size, self.head_dim = k_pages.shape
+        ptr = lambda t: None if t is None else t.data_ptr()
+        self.handle = dresd_kv_create(k_pages.data_ptr(), v_pages.data_ptr(), ptr(k_exps), ptr(v_exps), self.layers,
+                                      self.num_pages, self.kv_heads, self.page_size, self.head_dim, DTYPE_CODE[dtype])
+
+    def _rows(self, name, t, batch, heads=None):
+        """Distances of rows and heads of a [rows][heads][head_dim] tensor."""
+        if t.dtype != self.torch_dtype or not t.is_cuda or t.dim() != 3:
+            raise DresdError(-1, f"{name} must be a {self.torch_dtype} CUDA tensor with 3 dimensions")
+        if t.shape[0] != batch.rows or t.shape[2] != self.head_dim or (heads is not None and t.shape[1] != heads):
+            raise DresdError(-1, f"{name} has shape {tuple(t.shape)}")
+        row, head, last = t.stride()
+        if last != 1:
+            raise DresdError(-1, f"{name}: the elements of a head must be adjacent")
+        return row, head
+
+    def append(self, layer: int, k, v, batch: KvBatch, stream=None):
+        """Writes the chunks' keys and values, [rows][kv_heads][head_dim] (slices of a joint projection are fine)."""
+        k_row, k_head = self._rows("k", k, batch, self.kv_heads)
+        v_row, v_head = self._rows("v", v, batch, self.kv_heads)
+        s = (stream or _torch().cuda.current_stream()).cuda_stream
+        dresd_kv_append(self.handle, layer, batch.c, k.data_ptr(), k_row, k_head, v.data_ptr(), v_row, v_head, s)
+
+    def read(self, layer: int, batch: KvBatch, out=None, stream=None):
+        """Returns ``(k, v)``, dense [rows][kv_heads][head_dim], of the positions ctx[b] .. of every sequence."""
+        torch = _torch()
+        shape = (batch.rows, self.kv_heads, self.head_dim)
+        if out is None:
+            out = (torch.empty(shape, dtype=self.torch_dtype, device=self.k_pages.device),
+                   torch.empty(shape, dtype=self.torch_dtype, device=self.k_pages.device))
+        k, v = out
+        for name, t in (("out k", k), ("out v", v)):
+            if t.shape != shape or t.dtype != self.torch_dtype or not t.is_cuda or not t.is_contiguous():
+                raise DresdError(-1, f"{name} must be a contiguous {self.torch_dtype} CUDA tensor of shape {shape}")
+        s = (stream or torch.cuda.current_stream()).cuda_stream
+        dresd_kv_read(self.handle, layer, batch.c, k.data_ptr(), v.data_ptr(), s)
+        return k, v
+
+    def attend(self, layer: int, q, batch: KvBatch, scale: float | None = None, mask=None, out=None, lse=None, stream=None):
+        """Attention of the chunks' tokens, q [rows][heads][head_dim], over the cache; returns `out`, dense like q.
+        scale: 1 / sqrt(head_dim) if not given.  mask: int32 [rows][words], None = causal (see draft_mask).
+        lse: fp32 [rows][heads] to be filled, optional."""
+        torch = _torch()
+        q_row, q_head = self._rows("q", q, batch)
+        rows, heads, d = q.shape
+        if out is None:
+            out = torch.empty((rows, heads, d), dtype=self.torch_dtype, device=q.device)
+        elif out.shape != q.shape or out.dtype != q.dtype or not out.is_cuda or not out.is_contiguous():
+            raise DresdError(-1, f"out must be a contiguous {q.dtype} CUDA tensor of shape {tuple(q.shape)}")
+        if lse is not None and (lse.shape != (rows, heads) or lse.dtype != torch.float32 or not lse.is_cuda or
+                                not lse.is_contiguous()):
+            raise DresdError(-1, f"lse must be a contiguous float32 CUDA tensor of shape {(rows, heads)}")
+        mask_ptr, words = None, 0
+        if mask is not None:
+            if mask.dtype != torch.int32 or not mask.is_cuda or mask.dim() != 2 or mask.shape[0] != rows or not mask.is_contiguous():
+                raise DresdError(-1, f"mask must be a contiguous int32 CUDA tensor of {rows} rows")
+            mask_ptr, words = mask.data_ptr(), mask.shape[1]
+        s = (stream or torch.cuda.current_stream()).cuda_stream
+        dresd_kv_attend(self.handle, layer, batch.c, q.data_ptr(), q_row, q_head, heads,
+                        d ** -0.5 if scale is None else scale, mask_ptr, words, out.data_ptr(),
+                        None if lse is None else lse.data_ptr(), s)
+        return out
+
+    def keep_draft(self, batch: KvBatch, best, length, n: int, L: int, stream=None):
+        """Moves the accepted drafts' tokens into place in every layer (best, length: of dresd_drafts_accept)."""
+        torch = _torch()
+        for name, t in (("best", best), ("length", length)):
+            if t.dtype != torch.int32 or not t.is_cuda or t.shape != (batch.B,) or not t.is_contiguous():
+                raise DresdError(-1, f"{name} must be a contiguous int32 CUDA tensor of {batch.B} entries")
+        s = (stream or torch.cuda.current_stream()).cuda_stream
+        dresd_kv_keep_draft(self.handle, batch.c, best.data_ptr(), length.data_ptr(), n, L, s)
+
+    def status(self):
+        dresd_kv_status(self.handle)
+
+    def last_launches(self) -> int:
+        return dresd_kv_last_launches(self.handle)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            dresd_kv_destroy(self.handle)
             self.handle = None
 
     def __del__(self):

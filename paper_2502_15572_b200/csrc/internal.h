@@ -180,6 +180,41 @@ cudaError_t launch_merge_rerank(const unsigned long long *cand, int lists, int B
                                 const int32_t *want_first, const int32_t *next_tokens, int stored_len, int draft_len,
                                 int32_t *out_ids, float *out_scores, int32_t *out_tokens, cudaStream_t stream);
 
+// ---- K10 / K11: paged key/value cache and the attention over it ----
+struct KvArgs {
+    void *k, *v;                // [layers][num_pages][heads][page][d], 16-bit or E4M3 codes
+    uint8_t *k_exps, *v_exps;   // [layers][num_pages][heads][page] biased exponents, null = 16-bit cache
+    int layers, heads, page_shift, d, dtype, num_pages;
+    int layer;                  // layer of the call
+    const int32_t *table, *ctx, *start;
+    int B, width, rows;
+    int *status;
+};
+cudaError_t launch_kv_append(const KvArgs &a, const void *k, long long k_row, long long k_head, const void *v,
+                             long long v_row, long long v_head, cudaStream_t stream);
+cudaError_t launch_kv_read(const KvArgs &a, void *out_k, void *out_v, cudaStream_t stream);
+cudaError_t launch_kv_keep_draft(const KvArgs &a, const int32_t *best, const int32_t *length, int n, int L,
+                                 cudaStream_t stream);
+
+struct AttendArgs {
+    KvArgs kv;
+    const void *q;
+    long long q_row, q_head;    // distances in elements
+    int group;                  // query heads per key/value head
+    float scale_log2;           // scale x log2(e)
+    const uint32_t *mask;       // [rows][mask_words] or null = causal
+    int mask_words;
+    void *out;                  // [rows][heads * group][d]
+    float *lse;                 // [rows][heads * group] or null
+    float *part;                // partial results: see kv_plan.cuh
+    unsigned int *tickets;      // one per CTA, all zero between calls
+    int max_rows;               // rows of the longest chunk x group
+};
+// Workspace of the attention kernels (floats of `part`, tickets) on a device with `sms` SMs.
+size_t attend_part_floats(int sms, int d);
+int attend_max_ctas(int sms);
+cudaError_t launch_attend_mma(const AttendArgs &a, int sms, cudaStream_t stream);
+
 // Debug build only: one thread fails check 7 on purpose (no access is attempted), to show the reporting path.
 cudaError_t launch_debug_selftest(int *status, cudaStream_t stream);
 

@@ -1,0 +1,229 @@
+// K10 -- the paged key/value cache: writing (and quantising) new tokens, reading positions back, and moving
+// the accepted draft's tokens into place.
+//
+// All three move every byte once and compute next to nothing, so they are bound by HBM (and, on a few
+// hundred tokens, by the launch and the chain start[] -> ctx[] -> table -> data).  A lane handles 16 bytes
+// of a 16-bit row (8 elements), so a row of d = 128 is one half-warp and the quantiser's
+// maximum is four shuffles; a thread takes the same piece of kHeads heads of a token, whose loads
+// are independent and whose page is looked up once.
+#include "kv_plan.cuh"
+
+namespace dresd {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kHeads = 4;        // heads per thread
+
+// Page and offset of a dense row's token; false when the table does not reach it or names no page of the pool.
+__device__ __forceinline__ bool place_of(const KvArgs &a, int row, int &page, int &off)
+{
+    int lo = 0, hi = a.B;                                  // last b with start[b] <= row
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (__ldg(a.start + mid) <= row) lo = mid;
+        else hi = mid;
+    }
+    const int first = max(__ldg(a.start + lo), 0);
+    if (row < first || row >= __ldg(a.start + lo + 1)) return false;
+    const long long p = (long long)max(__ldg(a.ctx + lo), 0) + (row - first);
+    const long long i = p >> a.page_shift;
+    if (i >= a.width) return false;
+    page = __ldg(a.table + (long long)lo * a.width + i);
+    off = (int)(p & ((1 << a.page_shift) - 1));
+    return page >= 0 && page < a.num_pages;
+}
+
+template <typename T, bool Q8, int D>
+__global__ void __launch_bounds__(kThreads)
+append_kernel(const KvArgs a, const T *__restrict__ k, long long k_row, long long k_head, const T *__restrict__ v,
+              long long v_row, long long v_head)
+{
+    constexpr int kLanes = D / 8;                          // threads per row
+    const int groups = (a.heads + kHeads - 1) / kHeads;
+    const long long unit = ((long long)blockIdx.x * kThreads + threadIdx.x) / kLanes;
+    const int piece = threadIdx.x % kLanes;
+    if (unit >= (long long)a.rows * groups) return;        // whole sub-warps leave together
+    const int row = (int)(unit / groups), h0 = (int)(unit % groups) * kHeads;
+    const bool is_v = blockIdx.y != 0;
+    const T *src = is_v ? v + row * v_row : k + row * k_row;
+    const long long step = is_v ? v_head : k_head;
+    uint4 x[kHeads];
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i)
+        if (h0 + i < a.heads) x[i] = __ldg(reinterpret_cast<const uint4 *>(src + (h0 + i) * step + piece * 8));
+    int page, off;
+    if (!place_of(a, row, page, off)) return;
+    const unsigned lanes = kLanes == 32 ? 0xFFFFFFFFu : ((1u << kLanes) - 1) << (threadIdx.x % 32 / kLanes * kLanes);
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+        if (h0 + i >= a.heads) break;
+        const long long r = kv_row(a, a.layer, page, h0 + i, off);
+        if constexpr (!Q8) {
+            reinterpret_cast<uint4 *>(is_v ? a.v : a.k)[r * kLanes + piece] = x[i];
+        } else {
+            const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+            float f[8], amax = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 p = unpack2<T>(w[j]);
+                f[2 * j] = p.x;
+                f[2 * j + 1] = p.y;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (fabsf(f[j]) > KvType<T>::kBound) f[j] = copysignf(KvType<T>::kBound, f[j]);
+                amax = fmaxf(amax, fabsf(f[j]));
+            }
+#pragma unroll
+            for (int o = kLanes / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(lanes, amax, o));
+            const int e = kv_exponent(amax, KvType<T>::kMinExp);
+            const float s = pow2f(-e);                     // the product is exact: one rounding, to E4M3
+            uint32_t c[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                c[j] = to_e4m3(f[4 * j] * s) | to_e4m3(f[4 * j + 1] * s) << 8 | to_e4m3(f[4 * j + 2] * s) << 16 |
+                       to_e4m3(f[4 * j + 3] * s) << 24;
+            reinterpret_cast<uint2 *>(is_v ? a.v : a.k)[r * kLanes + piece] = make_uint2(c[0], c[1]);
+            if (piece == 0) (is_v ? a.v_exps : a.k_exps)[r] = (uint8_t)(e + 127);
+        }
+    }
+}
+
+template <typename T, bool Q8, int D>
+__global__ void __launch_bounds__(kThreads) read_kernel(const KvArgs a, T *__restrict__ out_k, T *__restrict__ out_v)
+{
+    constexpr int kLanes = D / 8;
+    const int groups = (a.heads + kHeads - 1) / kHeads;
+    const long long unit = ((long long)blockIdx.x * kThreads + threadIdx.x) / kLanes;
+    const int piece = threadIdx.x % kLanes;
+    if (unit >= (long long)a.rows * groups) return;
+    const int row = (int)(unit / groups), h0 = (int)(unit % groups) * kHeads;
+    const bool is_v = blockIdx.y != 0;
+    uint4 *dst = reinterpret_cast<uint4 *>(is_v ? out_v : out_k) + ((long long)row * a.heads + h0) * kLanes + piece;
+    int page = 0, off = 0;
+    const bool there = place_of(a, row, page, off);
+    const void *cache = is_v ? a.v : a.k;
+    if constexpr (!Q8) {
+        uint4 x[kHeads];
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+            x[i] = make_uint4(0, 0, 0, 0);
+            if (there && h0 + i < a.heads)
+                x[i] = reinterpret_cast<const uint4 *>(cache)[kv_row(a, a.layer, page, h0 + i, off) * kLanes + piece];
+        }
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i)
+            if (h0 + i < a.heads) dst[i * kLanes] = x[i];
+    } else {
+        const uint8_t *exps = is_v ? a.v_exps : a.k_exps;
+        uint2 x[kHeads];
+        int e[kHeads];
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+            x[i] = make_uint2(0, 0);
+            e[i] = 127;
+            if (there && h0 + i < a.heads) {
+                const long long r = kv_row(a, a.layer, page, h0 + i, off);
+                x[i] = reinterpret_cast<const uint2 *>(cache)[r * kLanes + piece];
+                e[i] = exps[r];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+            if (h0 + i >= a.heads) break;
+            const float s = __uint_as_float(max((uint32_t)e[i], 1u) << 23);      // stored bytes are 1 .. 247
+            const uint32_t w[2] = {x[i].x, x[i].y};
+            uint32_t o[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t two = w[j >> 1] >> (16 * (j & 1));
+                o[j] = pack2<T>(from_e4m3(two & 0xFF) * s, from_e4m3(two >> 8 & 0xFF) * s);
+            }
+            dst[i * kLanes] = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+    }
+}
+
+// One thread per 16 bytes of a moved row.  Sources lie behind every destination (1 + best L + t >= 1 + L >
+// 1 + t'), so the rows move independently of each other.
+__global__ void __launch_bounds__(kThreads)
+keep_kernel(const KvArgs a, const int32_t *__restrict__ best, const int32_t *__restrict__ length, int n, int L,
+            int pieces)
+{
+    const int b = blockIdx.y, r = best[b], kept = min(length[b] - 1, L);
+    if (r < 1 || r >= n) return;
+    const int ctx = max(a.ctx[b], 0);
+    const bool is_v = blockIdx.z != 0;
+    uint4 *cache = static_cast<uint4 *>(is_v ? a.v : a.k);
+    uint8_t *exps = is_v ? a.v_exps : a.k_exps;
+    const long long per_row = (long long)L * pieces, all = per_row * a.heads * a.layers;
+    for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < all; i += (long long)gridDim.x * kThreads) {
+        const int piece = (int)(i % pieces), t = (int)(i / pieces % L);
+        if (t >= kept) continue;
+        const int head = (int)(i / per_row % a.heads), layer = (int)(i / per_row / a.heads);
+        const long long to = (long long)ctx + 1 + t, from = to + (long long)r * L;
+        if ((from >> a.page_shift) >= a.width) continue;
+        const int in_page = (1 << a.page_shift) - 1;
+        const int pf = __ldg(a.table + (long long)b * a.width + (from >> a.page_shift));
+        const int pt = __ldg(a.table + (long long)b * a.width + (to >> a.page_shift));
+        if (pf < 0 || pf >= a.num_pages || pt < 0 || pt >= a.num_pages) continue;
+        const long long rf = kv_row(a, layer, pf, head, (int)(from & in_page)), rto = kv_row(a, layer, pt, head, (int)(to & in_page));
+        cache[rto * pieces + piece] = cache[rf * pieces + piece];
+        if (exps && piece == 0) exps[rto] = exps[rf];
+    }
+}
+
+template <typename F>
+cudaError_t by_type(const KvArgs &a, F &&f)
+{
+    const bool q8 = a.k_exps != nullptr;
+    if (a.dtype == kF16) {
+        __half *t = nullptr;
+        if (a.d == 64) return q8 ? f(t, std::true_type{}, std::integral_constant<int, 64>{}) : f(t, std::false_type{}, std::integral_constant<int, 64>{});
+        return q8 ? f(t, std::true_type{}, std::integral_constant<int, 128>{}) : f(t, std::false_type{}, std::integral_constant<int, 128>{});
+    }
+    __nv_bfloat16 *t = nullptr;
+    if (a.d == 64) return q8 ? f(t, std::true_type{}, std::integral_constant<int, 64>{}) : f(t, std::false_type{}, std::integral_constant<int, 64>{});
+    return q8 ? f(t, std::true_type{}, std::integral_constant<int, 128>{}) : f(t, std::false_type{}, std::integral_constant<int, 128>{});
+}
+
+dim3 row_grid(const KvArgs &a)
+{
+    const long long units = (long long)a.rows * ((a.heads + kHeads - 1) / kHeads);
+    return dim3((unsigned)((units * (a.d / 8) + kThreads - 1) / kThreads), 2);
+}
+
+}  // namespace
+
+cudaError_t launch_kv_append(const KvArgs &a, const void *k, long long k_row, long long k_head, const void *v,
+                             long long v_row, long long v_head, cudaStream_t stream)
+{
+    return by_type(a, [&](auto *t, auto q8, auto d) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        append_kernel<T, decltype(q8)::value, decltype(d)::value><<<row_grid(a), kThreads, 0, stream>>>(
+            a, static_cast<const T *>(k), k_row, k_head, static_cast<const T *>(v), v_row, v_head);
+        return cudaGetLastError();
+    });
+}
+
+cudaError_t launch_kv_read(const KvArgs &a, void *out_k, void *out_v, cudaStream_t stream)
+{
+    return by_type(a, [&](auto *t, auto q8, auto d) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        read_kernel<T, decltype(q8)::value, decltype(d)::value><<<row_grid(a), kThreads, 0, stream>>>(
+            a, static_cast<T *>(out_k), static_cast<T *>(out_v));
+        return cudaGetLastError();
+    });
+}
+
+cudaError_t launch_kv_keep_draft(const KvArgs &a, const int32_t *best, const int32_t *length, int n, int L,
+                                 cudaStream_t stream)
+{
+    const int pieces = a.d * (a.k_exps ? 1 : 2) / 16;
+    const long long all = (long long)L * pieces * a.heads * a.layers;
+    const long long blocks = (all + kThreads - 1) / kThreads;
+    keep_kernel<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096), a.B, 2), kThreads, 0, stream>>>(a, best, length, n, L, pieces);
+    return cudaGetLastError();
+}
+
+}  // namespace dresd

@@ -1,0 +1,210 @@
+// Shared by the kernels of the paged key/value cache: element conversions, addresses, and the
+// division of the attention's work over the CTAs.
+#pragma once
+
+#include "common.cuh"
+#include "internal.h"
+
+namespace dresd {
+
+// ---- 8-bit rows: E4M3 codes with one power-of-two scale per (token, head) --------------------
+template <typename T> struct KvType;
+template <> struct KvType<__half> {
+    static constexpr int kMinExp = -24;                  // 2^-24 is the finest step of fp16: a smaller scale gains nothing
+    static constexpr float kBound = 61440.f;             // 240 x 2^8: the largest value that is finite after rounding
+};
+template <> struct KvType<__nv_bfloat16> {
+    static constexpr int kMinExp = -126;
+    static constexpr float kBound = 3.1901471898837980e38f;   // 1.875 x 2^127
+};
+
+// Least e with amax <= 448 2^e (448 = 1.75 x 2^8), from the bits of amax; 0 for amax = 0.
+__device__ __forceinline__ int kv_exponent(float amax, int min_exp)
+{
+    const uint32_t u = __float_as_uint(amax);
+    const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return u == 0 ? 0 : max(e, min_exp);
+}
+__device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+
+template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t w);
+template <> __device__ __forceinline__ float2 unpack2<__half>(uint32_t w)
+{
+    return __half22float2(*reinterpret_cast<const __half2 *>(&w));
+}
+template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t w)
+{
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi)
+{
+    __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<uint32_t *>(&h);
+}
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi)
+{
+    __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t *>(&h);
+}
+
+// ---- a batch of chunks -------------------------------------------------------------------------
+struct Chunk {
+    int row0, len;      // rows of the dense tensors
+    int ctx, total;     // positions before the chunk; positions in all that the table reaches
+};
+__device__ __forceinline__ Chunk kv_chunk(const KvArgs &a, int b)
+{
+    Chunk c;
+    c.row0 = min(max(a.start[b], 0), a.rows);
+    c.len = min(max(a.start[b + 1], c.row0), a.rows) - c.row0;
+    c.ctx = max(a.ctx[b], 0);
+    c.total = (int)min((long long)c.ctx + c.len, (long long)a.width << a.page_shift);
+    return c;
+}
+// Row of (layer, page, head, offset) in the cache arrays; page numbers outside the pool count as `bad`.
+__device__ __forceinline__ long long kv_row(const KvArgs &a, int layer, int page, int head, int off)
+{
+    return (((((long long)layer * a.num_pages + page) * a.heads + head) << a.page_shift) + off);
+}
+
+// ---- division of the attention's work -----------------------------------------------------------
+// An ITEM is a tile of kRows rows (row r of a chunk is head r % group of token r / group) of one sequence
+// and key/value head; its cost is the number of kTile-position tiles that its rows see (at least
+// one, so that every row is written).  The items in the order (sequence, row tile, head) form one
+// line of W tiles, and CTA i of n takes tiles i W / n .. (i + 1) W / n - 1 of it, whatever the
+// lengths: the CTAs finish together however ragged the batch is.  A CTA therefore works on the tail
+// of one item, some whole items and the head of another.  Parts of an item are joined by the CTA that
+// finishes it last, in the order of the CTAs, so results do not depend on timing.
+struct Segment {
+    int b, rt, head;        // the item
+    int kt0, kt1;           // its tiles that this CTA takes
+    int n_kt;               // its tiles in all
+    int c0, c1;             // CTAs that share it
+    int slot;               // slot of this CTA's part (0: it is the CTA's first segment, 1: a later one)
+    int slot0;              // slot of c0's part; those of c0 + 1 .. c1 are 0
+};
+
+template <int kRows, int kTile>
+struct KvPlan {
+    const AttendArgs &a;
+    long long W, lo, hi, u;     // tiles in all; this CTA's; next tile
+    int n, cta;
+    int b, rt, head, kt;        // item of tile u, and its place there
+    bool first;
+    Chunk c;
+
+    __device__ __forceinline__ KvPlan(const AttendArgs &a_) : a(a_) {}
+
+    __device__ __forceinline__ int row_tiles(const Chunk &k) const { return (k.len * a.group + kRows - 1) / kRows; }
+    __device__ __forceinline__ int tiles(const Chunk &k, int r) const
+    {
+        int seen = k.total;
+        if (!a.mask) seen = min(seen, k.ctx + min(k.len - 1, ((r + 1) * kRows - 1) / a.group) + 1);
+        return max(1, (seen + kTile - 1) / kTile);
+    }
+    __device__ __forceinline__ long long cost(int bb) const
+    {
+        const Chunk k = kv_chunk(a.kv, bb);
+        const int nr = row_tiles(k);
+        long long t = 0;
+        if (a.mask) t = (long long)nr * tiles(k, 0);
+        else
+            for (int r = 0; r < nr; ++r) t += tiles(k, r);
+        return t * a.kv.heads;
+    }
+
+    // Called by all 32 lanes of a warp; false = nothing to do.  Small problems are not spread over more
+    // CTAs than give each `least` tiles.
+    __device__ bool start(int lane, int least)
+    {
+        const int B = a.kv.B;
+        cta = blockIdx.x;
+        long long mine = 0;
+        for (int b0 = 0; b0 < B; b0 += 32) mine += b0 + lane < B ? cost(b0 + lane) : 0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
+        W = mine;
+        n = (int)min((long long)gridDim.x, (W + least - 1) / least);
+        if (cta >= n) return false;
+        lo = u = W * cta / n;
+        hi = W * (cta + 1) / n;
+        // the sequence that tile `lo` belongs to
+        long long before = 0;
+        b = 0;
+        for (int b0 = 0; b0 < B; b0 += 32) {
+            const long long own = b0 + lane < B ? cost(b0 + lane) : 0;
+            long long incl = own;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+                if (lane >= o) incl += x;
+            }
+            const unsigned m = __ballot_sync(0xFFFFFFFFu, before + incl > lo);
+            if (m) {
+                const int l = __ffs(m) - 1;
+                b = b0 + l;
+                before += __shfl_sync(0xFFFFFFFFu, incl - own, l);
+                break;
+            }
+            before += __shfl_sync(0xFFFFFFFFu, incl, 31);
+        }
+        c = kv_chunk(a.kv, b);
+        long long rest = lo - before;
+        for (rt = 0;; ++rt) {
+            const long long t = (long long)tiles(c, rt) * a.kv.heads;
+            if (rest < t) break;
+            rest -= t;
+        }
+        const int nk = tiles(c, rt);
+        head = (int)(rest / nk);
+        kt = (int)(rest % nk);
+        first = true;
+        return true;
+    }
+    __device__ __forceinline__ int owner(long long t) const { return (int)(((t + 1) * n - 1) / W); }
+
+    // The next segment; false when the CTA has done its share.  Uniform over the CTA.
+    __device__ bool next(Segment &s)
+    {
+        if (u >= hi) return false;
+        s.n_kt = tiles(c, rt);
+        s.b = b;
+        s.rt = rt;
+        s.head = head;
+        s.kt0 = kt;
+        s.kt1 = (int)min((long long)s.n_kt, kt + (hi - u));
+        const long long item = u - kt;
+        s.c0 = owner(item);
+        s.c1 = owner(item + s.n_kt - 1);
+        s.slot = first ? 0 : 1;
+        s.slot0 = W * s.c0 / n == item ? 0 : 1;
+        first = false;
+        u += s.kt1 - s.kt0;
+        kt = s.kt1;
+        return true;
+    }
+    // Moves on to the next item (call after the segment's work, when its chunk is no longer needed).
+    __device__ void advance()
+    {
+        if (u >= hi || kt < tiles(c, rt)) return;
+        kt = 0;
+        if (++head < a.kv.heads) return;
+        head = 0;
+        if (++rt < row_tiles(c)) return;
+        rt = 0;
+        do {
+            ++b;
+            c = kv_chunk(a.kv, b);
+        } while (c.len == 0);            // ends: u < hi means that a later sequence has tiles
+    }
+};
+
+// Parts of shared items: per CTA two slots of `rows` x (d + 2) floats: the sums, then the rows' maxima, then the
+// rows' weight sums.
+__device__ __forceinline__ float *part_slot(const AttendArgs &a, int cta, int slot, int rows)
+{
+    return a.part + ((size_t)cta * 2 + slot) * rows * (a.kv.d + 2);
+}
+
+}  // namespace dresd
