@@ -369,6 +369,17 @@ dresd_status dresd_kv_keep_draft(dresd_kv *kv, const dresd_kv_batch *batch, cons
 /* dresd_store_status() for a cache: waits for its last stream, reports and clears its status word. */
 dresd_status dresd_kv_status(dresd_kv *kv);
 
+/*
+ * For tests and measurements (set between calls).
+ *   "attend_path"  0 = automatic (by rows per key/value head), 1 = the mma.sync kernel, 2 = the tcgen05 kernel
+ *                  (which a scale that is not positive never takes)
+ *   "wait_ms"      bound of the device-side waits in milliseconds (0 = default, about 2 s)
+ *   "debug_lose_stage"  test hook: in the next calls the first CTA of the tcgen05 kernel never receives its
+ *                  tile (value-1), so its waits run out and dresd_kv_status() reports DRESD_ERR_TIMEOUT; 0 = off
+ * Unknown names return DRESD_ERR_INVALID.
+ */
+dresd_status dresd_kv_set_option(dresd_kv *kv, const char *name, int value);
+
 /* Kernels enqueued by the cache's last call. */
 int dresd_kv_last_launches(const dresd_kv *kv);
 

@@ -35,7 +35,7 @@ EXPORTS = (
     "dresd_retrieve_quantised", "dresd_store_index_first_tokens", "dresd_merge_shards_packed",
     "dresd_noalloc_status", "dresd_debug_build", "dresd_store_debug_selftest",
     "dresd_kv_create", "dresd_kv_destroy", "dresd_kv_append", "dresd_kv_read", "dresd_kv_attend",
-    "dresd_kv_keep_draft", "dresd_kv_status", "dresd_kv_last_launches",
+    "dresd_kv_keep_draft", "dresd_kv_status", "dresd_kv_set_option", "dresd_kv_last_launches",
 )
 
 
@@ -141,6 +141,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.dresd_kv_keep_draft.argtypes = [vp, batch, vp, vp, i32, i32, vp]
     lib.dresd_kv_status.restype = i32
     lib.dresd_kv_status.argtypes = [vp]
+    lib.dresd_kv_set_option.restype = i32
+    lib.dresd_kv_set_option.argtypes = [vp, c.c_char_p, i32]
     lib.dresd_kv_last_launches.restype = i32
     lib.dresd_kv_last_launches.argtypes = [vp]
     if path is None:
@@ -341,6 +343,10 @@ def dresd_kv_keep_draft(kv: int, batch: dresd_kv_batch, best_ptr: int, length_pt
 
 def dresd_kv_status(kv: int) -> None:
     _check(load().dresd_kv_status(kv))
+
+
+def dresd_kv_set_option(kv: int, name: str, value: int) -> None:
+    _check(load().dresd_kv_set_option(kv, name.encode(), value))
 
 
 def dresd_kv_last_launches(kv: int) -> int:
@@ -636,6 +642,9 @@ class KvCache:
                 raise DresdError(-1, f"{name} must be a contiguous int32 CUDA tensor of {batch.B} entries")
         s = (stream or torch.cuda.current_stream()).cuda_stream
         dresd_kv_keep_draft(self.handle, batch.c, best.data_ptr(), length.data_ptr(), n, L, s)
+
+    def set_option(self, name: str, value: int):
+        dresd_kv_set_option(self.handle, name, value)
 
     def status(self):
         dresd_kv_status(self.handle)

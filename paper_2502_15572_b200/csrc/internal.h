@@ -209,11 +209,18 @@ struct AttendArgs {
     float *part;                // partial results: see kv_plan.cuh
     unsigned int *tickets;      // one per CTA, all zero between calls
     int max_rows;               // rows of the longest chunk x group
+    long long wait_cycles;      // bound of every device-side wait in cycles, 0 = default
+    int lose_stage;             // test hook: CTA 0 never receives tile (value - 1); 0 = off
 };
-// Workspace of the attention kernels (floats of `part`, tickets) on a device with `sms` SMs.
-size_t attend_part_floats(int sms, int d);
-int attend_max_ctas(int sms);
+// Few rows per key/value head (at most 16) or a scale that is not positive: mma.sync, straight from registers.
+int attend_mma_max_ctas(int sms);                         // tickets
+size_t attend_mma_part_floats(int sms, int d);            // floats of `part`
 cudaError_t launch_attend_mma(const AttendArgs &a, int sms, cudaStream_t stream);
+// More rows: tcgen05.  Tensor maps: k, v over the cache's rows [layers x pages x heads x page][d] (boxes of 64 elements
+// x page rows; 8-bit: d bytes x page rows), q over [rows][heads][d] (boxes of 64 elements x group x 128 / group).
+size_t attend_umma_part_floats(int sms, int d);
+cudaError_t launch_attend_umma(const CUtensorMap &q_map, const CUtensorMap &k_map, const CUtensorMap &v_map,
+                               const AttendArgs &a, int sms, cudaStream_t stream);
 
 // Debug build only: one thread fails check 7 on purpose (no access is attempted), to show the reporting path.
 cudaError_t launch_debug_selftest(int *status, cudaStream_t stream);

@@ -50,35 +50,12 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x)
     return y;
 }
 
-// Two E4M3 codes in bytes 1 and 3 of `w` (the others 0) as a pair of T, times the pair `scale`.  fp16: the hardware
-// conversion.  bf16: the code's bits moved to bf16's exponent and mantissa are its value x 2^-120 (the biases
-// differ by 120, E4M3's subnormals fall among the normal numbers' steps), so `scale` carries 2^120.
-template <typename T> __device__ __forceinline__ uint32_t codes_to_pair(uint32_t w, uint32_t scale);
-template <> __device__ __forceinline__ uint32_t codes_to_pair<__half>(uint32_t w, uint32_t scale)
+// Parts of shared items: per CTA two slots of `rows` x (d + 2) floats: the sums, then the rows' maxima, then the
+// rows' weight sums.
+__device__ __forceinline__ float *part_slot(const AttendArgs &a, int cta, int slot, int rows)
 {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)__byte_perm(w, 0, 0x0031), __NV_E4M3);
-    const __half2 r = __hmul2(*reinterpret_cast<const __half2 *>(&h), *reinterpret_cast<const __half2 *>(&scale));
-    return *reinterpret_cast<const uint32_t *>(&r);
+    return a.part + ((size_t)cta * 2 + slot) * rows * (a.kv.d + 2);
 }
-template <> __device__ __forceinline__ uint32_t codes_to_pair<__nv_bfloat16>(uint32_t w, uint32_t scale)
-{
-    const uint32_t b = (w & 0x80008000u) | ((w >> 4) & 0x07F007F0u);
-    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&b), *reinterpret_cast<const __nv_bfloat162 *>(&scale));
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
-// What codes_to_pair() multiplies by for exponent byte `eb`, as the bits of one T.  bf16: 2^(e + 120) is representable up
-// to e = 7; larger ones (values beyond 57344) are finished by a second product with big_scale().
-template <typename T> __device__ __forceinline__ uint32_t scale_bits(int eb);
-template <> __device__ __forceinline__ uint32_t scale_bits<__half>(int eb)
-{
-    const int e = eb - 127;                               // -24 .. 8
-    return e >= -14 ? (uint32_t)(min(e, 15) + 15) << 10 : 1u << max(e + 24, 0);
-}
-template <> __device__ __forceinline__ uint32_t scale_bits<__nv_bfloat16>(int eb)
-{
-    return (uint32_t)(min(eb, 134) + 120) << 7;
-}
-__device__ __forceinline__ uint32_t big_scale(int eb) { return (uint32_t)(127 + max(eb - 134, 0)) << 7; }
 
 template <int kBytes> struct Piece;                       // a lane's load
 template <> struct Piece<16> { using type = uint4; };
@@ -105,10 +82,10 @@ attend_mma_kernel(const AttendArgs a, int least)
     __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
     __shared__ unsigned s_ticket;
 
-    KvPlan<kRows, kTile> plan(a);
-    if (!plan.start(lane, least)) return;
+    KvPlan<FewRows<kRows, kTile>> plan;
+    if (!plan.start(a, lane, least)) return;
     Segment seg;
-    while (plan.next(seg)) {
+    while (plan.next(a, seg)) {
         const Chunk ch = plan.c;
         const int heads = a.kv.heads * a.group;
         const int rows = min(kRows, ch.len * a.group - seg.rt * kRows);     // valid rows of the tile
@@ -454,7 +431,7 @@ attend_mma_kernel(const AttendArgs a, int least)
             }
         }
         __syncthreads();                                    // s_o is written again by the next segment
-        plan.advance();
+        plan.advance(a);
     }
 }
 
@@ -469,7 +446,7 @@ cudaError_t launch(const AttendArgs &a, int sms, cudaStream_t stream)
         occupancy = n;
     }
     int grid = sms * occupancy;
-    if (grid > attend_max_ctas(sms)) grid = attend_max_ctas(sms);
+    if (grid > attend_mma_max_ctas(sms)) grid = attend_mma_max_ctas(sms);
     attend_mma_kernel<T, Q8, D, NT><<<grid, kThreads, 0, stream>>>(a, 2);
     return cudaGetLastError();
 }
@@ -483,8 +460,8 @@ cudaError_t by_shape(const AttendArgs &a, int sms, cudaStream_t stream)
 
 }  // namespace
 
-int attend_max_ctas(int sms) { return 8 * sms; }
-size_t attend_part_floats(int sms, int d) { return (size_t)attend_max_ctas(sms) * 2 * 16 * (d + 2); }
+int attend_mma_max_ctas(int sms) { return 8 * sms; }
+size_t attend_mma_part_floats(int sms, int d) { return (size_t)attend_mma_max_ctas(sms) * 2 * 16 * (d + 2); }
 
 cudaError_t launch_attend_mma(const AttendArgs &a, int sms, cudaStream_t stream)
 {

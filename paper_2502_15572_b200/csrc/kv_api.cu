@@ -1,7 +1,9 @@
 // C ABI of the paged key/value cache (the dresd_kv_* calls of include/dresd.h): handle, argument
-// validation, workspace.  The kernels are in k10_kv_cache.cu and k11_attend_mma.cu.
+// validation, tensor maps, workspace.  The kernels are in k10_kv_cache.cu, k11_attend_mma.cu and
+// k12_attend_umma.cu.
 #include <cstdarg>
 #include <cstdio>
+#include <cstring>
 #include <new>
 
 #include "../../include/dresd.h"
@@ -40,6 +42,38 @@ bool is_device_ptr(const void *p)
     }
     return at.type == cudaMemoryTypeDevice || at.type == cudaMemoryTypeManaged;
 }
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_tiled_fn()
+{
+    static EncodeTiledFn fn = nullptr;
+    if (!fn) {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(p);
+    }
+    return fn;
+}
+
+// 16-bit elements in boxes of one 128-byte swizzle row, or bytes in boxes of whole rows; zeros beyond the ends.
+bool encode(CUtensorMap *map, const void *base, int dtype, int rank, const cuuint64_t *dims, const cuuint64_t *strides,
+            const cuuint32_t *box)
+{
+    const cuuint32_t ones[3] = {1, 1, 1};
+    EncodeTiledFn fn = encode_tiled_fn();
+    return fn && fn(map,
+                    dtype == kE4M3  ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                    : dtype == kF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                    : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                    rank, const_cast<void *>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    dtype == kE4M3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 }  // namespace
@@ -47,9 +81,11 @@ bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0;
 struct dresd_kv {
     uint32_t magic;
     int device, sms;
+    CUtensorMap k_map, v_map;    // over the cache's rows
     KvArgs args;                 // arrays and geometry; the batch's part is filled in per call
     float *part;                 // parts of shared items (see kv_plan.cuh)
     unsigned int *tickets;
+    int opt_path, opt_wait_ms, opt_lose_stage;
     cudaStream_t last_stream;
     int last_launches;
 };
@@ -98,13 +134,14 @@ dresd_status check_call(dresd_kv *kv, int layer, const dresd_kv_batch *b, bool w
     return DRESD_OK;
 }
 
-// Rows of `heads` heads at the given distances: 16-byte loads, and the last one's address within 2^62.
-dresd_status check_rows(const char *name, const void *p, long long row, long long head, int heads, int d)
+// Rows of `heads` heads at the given distances: 16-byte loads.
+dresd_status check_rows(const char *name, const void *p, int rows, long long row, long long head, int heads, int d)
 {
     if (!is_device_ptr(p) || !aligned16(p)) return fail(DRESD_ERR_INVALID, "%s must be a 16-byte aligned device pointer", name);
     if (row < 0 || head < 0 || row % 8 != 0 || head % 8 != 0)
         return fail(DRESD_ERR_INVALID, "%s: the distances of rows and heads must be multiples of 8 elements", name);
-    if (heads > 1 && head < d) return fail(DRESD_ERR_INVALID, "%s: heads of %d elements overlap at a distance of %lld", name, d, head);
+    if ((heads > 1 && (head < d || head >= 1LL << 38)) || (rows > 1 && (row < d || row >= 1LL << 38)))
+        return fail(DRESD_ERR_INVALID, "%s: distances of %lld (rows) and %lld (heads) elements for heads of %d", name, row, head, d);
     return DRESD_OK;
 }
 
@@ -153,8 +190,17 @@ dresd_status dresd_kv_create(void *k_pages, void *v_pages, uint8_t *k_exps, uint
         free_kv(kv);
         return fail_cuda(e, "device query");
     }
-    const size_t tickets = sizeof(unsigned int) * (size_t)attend_max_ctas(kv->sms);
-    if (cudaMalloc(&kv->part, sizeof(float) * attend_part_floats(kv->sms, head_dim)) != cudaSuccess ||
+    const size_t tickets = sizeof(unsigned int) * (size_t)attend_mma_max_ctas(kv->sms);
+    const size_t few = attend_mma_part_floats(kv->sms, head_dim), many = attend_umma_part_floats(kv->sms, head_dim);
+    const cuuint64_t dims[2] = {(cuuint64_t)head_dim, (cuuint64_t)layers * num_pages * kv_heads * page_size};
+    const cuuint64_t strides[1] = {(cuuint64_t)head_dim * (k_exps ? 1 : 2)};
+    const cuuint32_t box[2] = {(cuuint32_t)(k_exps ? head_dim : 64), (cuuint32_t)page_size};
+    if (!encode(&kv->k_map, k_pages, k_exps ? kE4M3 : a.dtype, 2, dims, strides, box) ||
+        !encode(&kv->v_map, v_pages, k_exps ? kE4M3 : a.dtype, 2, dims, strides, box)) {
+        free_kv(kv);
+        return fail(DRESD_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+    }
+    if (cudaMalloc(&kv->part, sizeof(float) * (few > many ? few : many)) != cudaSuccess ||
         cudaMalloc(&kv->tickets, tickets) != cudaSuccess || cudaMalloc(&a.status, sizeof(int)) != cudaSuccess) {
         cudaGetLastError();
         free_kv(kv);
@@ -184,8 +230,8 @@ dresd_status dresd_kv_append(dresd_kv *kv, int layer, const dresd_kv_batch *batc
     if (st != DRESD_OK) return st;
     kv->last_launches = 0;
     if (a.B == 0 || a.rows == 0) return DRESD_OK;
-    if ((st = check_rows("k", k, k_row, k_head, a.heads, a.d)) != DRESD_OK) return st;
-    if ((st = check_rows("v", v, v_row, v_head, a.heads, a.d)) != DRESD_OK) return st;
+    if ((st = check_rows("k", k, a.rows, k_row, k_head, a.heads, a.d)) != DRESD_OK) return st;
+    if ((st = check_rows("v", v, a.rows, v_row, v_head, a.heads, a.d)) != DRESD_OK) return st;
     kv->last_stream = static_cast<cudaStream_t>(stream);
     const cudaError_t e = launch_kv_append(a, k, k_row, k_head, v, v_row, v_head, kv->last_stream);
     if (e != cudaSuccess) return fail_cuda(e, "kv_append launch");
@@ -226,7 +272,7 @@ dresd_status dresd_kv_attend(dresd_kv *kv, int layer, const dresd_kv_batch *batc
         return fail(DRESD_ERR_UNSUPPORTED, "rows x heads per key/value head exceed 2^31 - 1025");
     kv->last_launches = 0;
     if (a.kv.B == 0 || a.kv.rows == 0) return DRESD_OK;
-    if ((st = check_rows("q", q, q_row, q_head, heads, a.kv.d)) != DRESD_OK) return st;
+    if ((st = check_rows("q", q, a.kv.rows, q_row, q_head, heads, a.kv.d)) != DRESD_OK) return st;
     if (!is_device_ptr(out) || !aligned16(out) || (out_lse && !is_device_ptr(out_lse)))
         return fail(DRESD_ERR_INVALID, "out must be a 16-byte aligned device pointer, out_lse a device pointer or NULL");
     if (mask && !is_device_ptr(mask)) return fail(DRESD_ERR_INVALID, "mask must be a device pointer");
@@ -242,8 +288,25 @@ dresd_status dresd_kv_attend(dresd_kv *kv, int layer, const dresd_kv_batch *batc
     a.part = kv->part;
     a.tickets = kv->tickets;
     a.max_rows = (batch->max_chunk > 0 ? batch->max_chunk : batch->rows) * a.group;
+    a.wait_cycles = (long long)kv->opt_wait_ms * 2000000LL;        // ~2 GHz
+    a.lose_stage = kv->opt_lose_stage;
     kv->last_stream = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = launch_attend_mma(a, kv->sms, kv->last_stream);
+    cudaError_t e;
+    // Up to 16 rows per key/value head the registers of mma.sync hold them.  The other kernel masks before it scales, which
+    // needs a positive scale.
+    const bool many = kv->opt_path == 0 ? a.max_rows > 16 : kv->opt_path == 2;
+    if (many && scale > 0.f) {
+        CUtensorMap q_map;
+        const cuuint64_t dims[3] = {(cuuint64_t)a.kv.d, (cuuint64_t)heads, (cuuint64_t)a.kv.rows};
+        // the distance of a dimension with one entry is never used, but has to be a valid one
+        const cuuint64_t strides[2] = {heads > 1 ? (cuuint64_t)q_head * 2 : (cuuint64_t)a.kv.d * 2,
+                                       a.kv.rows > 1 ? (cuuint64_t)q_row * 2 : (cuuint64_t)heads * a.kv.d * 2};
+        const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)(128 / a.group)};
+        if (!encode(&q_map, q, a.kv.dtype, 3, dims, strides, box)) return fail(DRESD_ERR_CUDA, "cuTensorMapEncodeTiled failed for q");
+        e = launch_attend_umma(q_map, kv->k_map, kv->v_map, a, kv->sms, kv->last_stream);
+    } else {
+        e = launch_attend_mma(a, kv->sms, kv->last_stream);
+    }
     if (e != cudaSuccess) return fail_cuda(e, "kv_attend launch");
     kv->last_launches = 1;
     return DRESD_OK;
@@ -279,11 +342,32 @@ dresd_status dresd_kv_status(dresd_kv *kv)
     if (word == 0) return DRESD_OK;
     e = cudaMemset(kv->args.status, 0, sizeof(int));
     // a kernel that gave up may have left tickets behind
-    if (e == cudaSuccess) e = cudaMemset(kv->tickets, 0, sizeof(unsigned int) * (size_t)attend_max_ctas(kv->sms));
+    if (e == cudaSuccess) e = cudaMemset(kv->tickets, 0, sizeof(unsigned int) * (size_t)attend_mma_max_ctas(kv->sms));
     if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
     if (e != cudaSuccess) return fail_cuda(e, "status reset");
     if (word <= -1000) return fail(DRESD_ERR_INTERNAL, "bounds check %d failed inside a kernel", -1000 - word);
     return fail(DRESD_ERR_TIMEOUT, "a device-side wait expired");
+}
+
+dresd_status dresd_kv_set_option(dresd_kv *kv, const char *name, int value)
+{
+    if (!valid(kv) || !name) return fail(DRESD_ERR_INVALID, "cache handle or option name is NULL");
+    if (strcmp(name, "attend_path") == 0) {
+        if (value < 0 || value > 2) return fail(DRESD_ERR_INVALID, "attend_path = %d outside 0..2", value);
+        kv->opt_path = value;
+        return DRESD_OK;
+    }
+    if (strcmp(name, "wait_ms") == 0) {
+        if (value < 0 || value > 60000) return fail(DRESD_ERR_INVALID, "wait_ms = %d outside 0..60000", value);
+        kv->opt_wait_ms = value;
+        return DRESD_OK;
+    }
+    if (strcmp(name, "debug_lose_stage") == 0) {
+        if (value < 0) return fail(DRESD_ERR_INVALID, "debug_lose_stage = %d is negative", value);
+        kv->opt_lose_stage = value;
+        return DRESD_OK;
+    }
+    return fail(DRESD_ERR_INVALID, "unknown option '%s'", name);
 }
 
 int dresd_kv_last_launches(const dresd_kv *kv) { return valid(kv) ? kv->last_launches : 0; }

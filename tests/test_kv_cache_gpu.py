@@ -160,12 +160,12 @@ def check_attend(case, q, scale=None, seen=None, mask=None, lse=True, q_view=Non
         tol = u * V[..., None] + u * np.abs(want) + ((2 * (ds + 2.0 ** -21) + n * 2.0 ** -24) * V)[..., None] + 2.0 ** -24
         fin = np.isfinite(want)
         assert np.array_equal(np.isfinite(got[s:e]), fin), f"sequence {b}: non-finite places differ"
-        err = np.abs(got[s:e] - want)[fin] - tol[fin]
+        err = np.abs(got[s:e][fin] - want[fin]) - tol[fin]
         assert err.max(initial=-1) <= 0, f"sequence {b}: {err.max()} beyond the tolerance"
         if got_lse is not None:
             some = vis.any(1)
             assert np.all(np.isneginf(got_lse[s:e][~some])) and np.all(got[s:e][~some] == 0)
-            off = np.abs(got_lse[s:e] - wlse)[some] - (ds + 2.0 ** -20 + 2.0 ** -23 * np.abs(wlse))[some]
+            off = np.abs(got_lse[s:e][some] - wlse[some]) - (ds[some] + 2.0 ** -20 + 2.0 ** -23 * np.abs(wlse[some]))
             assert off.max(initial=-1) <= 0, f"sequence {b}: lse {off.max()} beyond the tolerance"
     return got
 
@@ -307,6 +307,46 @@ def test_large_scores_and_types_lowest_values():
     q = case.queries(2)
     q[:, :, 0] = q[:, :, 0].abs() + 1
     check_attend(case, q)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("path", [1, 2])
+@pytest.mark.parametrize("dtype,d,page,quantised", [("f16", 64, 32, False), ("bf16", 128, 16, False), ("bf16", 64, 128, True), ("f16", 128, 64, True)])
+def test_either_kernel_takes_any_batch(path, dtype, d, page, quantised):
+    """Both kernels on single tokens, short and long chunks in one batch; more rows than the largest row tile."""
+    ctx, chunk = [0, 130, 1000, 17, 255, 60], [1, 1, 3, 0, 300, 129]
+    case = Case(dtype, d, page, 2, ctx, chunk, quantised, seed=60)
+    case.cache.set_option("attend_path", path)
+    check_attend(case, case.queries(6))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [0.0, -0.25, 3.0])
+def test_scales(scale):
+    case = Case("f16", 64, 16, 2, [50, 9], [40, 33], seed=61)
+    check_attend(case, case.queries(4, amp=0.5), scale=scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("quantised", [False, True])
+@pytest.mark.parametrize("stage", [1, 2, 7])
+def test_a_wait_that_runs_out_is_reported(quantised, stage):
+    """The first CTA never receives one of its tiles: the call ends, the status says so, the next call is right again."""
+    case = Case("bf16", 128, 32, 4, [30000, 200], [40, 64], quantised, seed=62)
+    q = case.queries(8)
+    first = case.cache.attend(0, q, case.batch)
+    case.cache.set_option("wait_ms", 20)
+    case.cache.set_option("debug_lose_stage", stage)
+    case.cache.attend(0, q, case.batch)
+    with pytest.raises(binding.DresdError) as e:
+        case.cache.status()
+    assert e.value.status == -5
+    case.cache.set_option("debug_lose_stage", 0)
+    case.cache.set_option("wait_ms", 0)
+    assert torch.equal(case.cache.attend(0, q, case.batch), first)
+    case.cache.status()
+    with pytest.raises(binding.DresdError):
+        case.cache.set_option("no_such_option", 1)
 
 
 @pytest.mark.gpu
