@@ -271,7 +271,7 @@ dresd_status dresd_retrieve_quantised(dresd_store *store, const void *queries, c
  *   k_pages, v_pages  device, [layers][num_pages][kv_heads][page_size][head_dim] row-major,
  *                     16-byte aligned, in `dtype` -- or one byte per element when the
  *                     cache is 8-bit (k_exps / v_exps not NULL)
- *   k_exps, v_exps    device, uint8 [layers][num_pages][kv_heads][page_size], or both NULL
+ *   k_exps, v_exps    device, uint8 [layers][num_pages][kv_heads][page_size], 16-byte aligned, or both NULL
  *   dtype             DRESD_F16 or DRESD_BF16: the type of queries, keys and values handed in
  *                     and out
  *   head_dim          64 or 128;  page_size 16, 32, 64 or 128

@@ -358,9 +358,15 @@ def dresd_kv_destroy(kv: int) -> None:
 
 
 # ---- torch convenience ----------------------------------------------------------
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def to_device(array, dtype: str, device="cuda"):
@@ -516,6 +522,13 @@ class Store:
             pass
 
 
+def _raw_stream(device_index: int, stream) -> int:
+    """cudaStream_t of `stream`, or of the device's current stream."""
+    if stream is not None:
+        return stream.cuda_stream
+    return _torch()._C._cuda_getCurrentRawStream(device_index)
+
+
 def draft_mask(n: int, L: int, device="cuda"):
     """Visibility bits of a chunk that is a sequence's last token and its n drafts of L tokens, int32
     [1 + n L][words]: every token sees the first one and its own draft up to itself."""
@@ -572,16 +585,18 @@ class KvCache:
         self.dtype = dtype
         self.k_pages, self.v_pages, self.k_exps, self.v_exps = k_pages, v_pages, k_exps, v_exps   # keep alive
         self.layers, self.num_pages, self.kv_heads, self.page_size, self.head_dim = k_pages.shape
+        self.device_index = k_pages.device.index
         ptr = lambda t: None if t is None else t.data_ptr()
         self.handle = dresd_kv_create(k_pages.data_ptr(), v_pages.data_ptr(), ptr(k_exps), ptr(v_exps), self.layers,
                                       self.num_pages, self.kv_heads, self.page_size, self.head_dim, DTYPE_CODE[dtype])
 
     def _rows(self, name, t, batch, heads=None):
         """Distances of rows and heads of a [rows][heads][head_dim] tensor."""
-        if t.dtype != self.torch_dtype or not t.is_cuda or t.dim() != 3:
+        shape = t.shape
+        if t.dtype != self.torch_dtype or not t.is_cuda or len(shape) != 3:
             raise DresdError(-1, f"{name} must be a {self.torch_dtype} CUDA tensor with 3 dimensions")
-        if t.shape[0] != batch.rows or t.shape[2] != self.head_dim or (heads is not None and t.shape[1] != heads):
-            raise DresdError(-1, f"{name} has shape {tuple(t.shape)}")
+        if shape[0] != batch.rows or shape[2] != self.head_dim or (heads is not None and shape[1] != heads):
+            raise DresdError(-1, f"{name} has shape {tuple(shape)}")
         row, head, last = t.stride()
         if last != 1:
             raise DresdError(-1, f"{name}: the elements of a head must be adjacent")
@@ -591,22 +606,21 @@ class KvCache:
         """Writes the chunks' keys and values, [rows][kv_heads][head_dim] (slices of a joint projection are fine)."""
         k_row, k_head = self._rows("k", k, batch, self.kv_heads)
         v_row, v_head = self._rows("v", v, batch, self.kv_heads)
-        s = (stream or _torch().cuda.current_stream()).cuda_stream
-        dresd_kv_append(self.handle, layer, batch.c, k.data_ptr(), k_row, k_head, v.data_ptr(), v_row, v_head, s)
+        dresd_kv_append(self.handle, layer, batch.c, k.data_ptr(), k_row, k_head, v.data_ptr(), v_row, v_head,
+                        _raw_stream(self.device_index, stream))
 
     def read(self, layer: int, batch: KvBatch, out=None, stream=None):
         """Returns ``(k, v)``, dense [rows][kv_heads][head_dim], of the positions ctx[b] .. of every sequence."""
         torch = _torch()
         shape = (batch.rows, self.kv_heads, self.head_dim)
         if out is None:
-            out = (torch.empty(shape, dtype=self.torch_dtype, device=self.k_pages.device),
-                   torch.empty(shape, dtype=self.torch_dtype, device=self.k_pages.device))
-        k, v = out
-        for name, t in (("out k", k), ("out v", v)):
-            if t.shape != shape or t.dtype != self.torch_dtype or not t.is_cuda or not t.is_contiguous():
-                raise DresdError(-1, f"{name} must be a contiguous {self.torch_dtype} CUDA tensor of shape {shape}")
-        s = (stream or torch.cuda.current_stream()).cuda_stream
-        dresd_kv_read(self.handle, layer, batch.c, k.data_ptr(), v.data_ptr(), s)
+            k, v = torch.empty((2, *shape), dtype=self.torch_dtype, device=self.k_pages.device).unbind(0)
+        else:
+            k, v = out
+            for name, t in (("out k", k), ("out v", v)):
+                if t.shape != shape or t.dtype != self.torch_dtype or not t.is_cuda or not t.is_contiguous():
+                    raise DresdError(-1, f"{name} must be a contiguous {self.torch_dtype} CUDA tensor of shape {shape}")
+        dresd_kv_read(self.handle, layer, batch.c, k.data_ptr(), v.data_ptr(), _raw_stream(self.device_index, stream))
         return k, v
 
     def attend(self, layer: int, q, batch: KvBatch, scale: float | None = None, mask=None, out=None, lse=None, stream=None):
@@ -617,7 +631,7 @@ class KvCache:
         q_row, q_head = self._rows("q", q, batch)
         rows, heads, d = q.shape
         if out is None:
-            out = torch.empty((rows, heads, d), dtype=self.torch_dtype, device=q.device)
+            out = torch.empty((rows, heads, d), dtype=self.torch_dtype, device=self.k_pages.device)
         elif out.shape != q.shape or out.dtype != q.dtype or not out.is_cuda or not out.is_contiguous():
             raise DresdError(-1, f"out must be a contiguous {q.dtype} CUDA tensor of shape {tuple(q.shape)}")
         if lse is not None and (lse.shape != (rows, heads) or lse.dtype != torch.float32 or not lse.is_cuda or
@@ -628,20 +642,19 @@ class KvCache:
             if mask.dtype != torch.int32 or not mask.is_cuda or mask.dim() != 2 or mask.shape[0] != rows or not mask.is_contiguous():
                 raise DresdError(-1, f"mask must be a contiguous int32 CUDA tensor of {rows} rows")
             mask_ptr, words = mask.data_ptr(), mask.shape[1]
-        s = (stream or torch.cuda.current_stream()).cuda_stream
         dresd_kv_attend(self.handle, layer, batch.c, q.data_ptr(), q_row, q_head, heads,
                         d ** -0.5 if scale is None else scale, mask_ptr, words, out.data_ptr(),
-                        None if lse is None else lse.data_ptr(), s)
+                        None if lse is None else lse.data_ptr(), _raw_stream(self.device_index, stream))
         return out
 
     def keep_draft(self, batch: KvBatch, best, length, n: int, L: int, stream=None):
         """Moves the accepted drafts' tokens into place in every layer (best, length: of dresd_drafts_accept)."""
-        torch = _torch()
+        int32 = _torch().int32
         for name, t in (("best", best), ("length", length)):
-            if t.dtype != torch.int32 or not t.is_cuda or t.shape != (batch.B,) or not t.is_contiguous():
+            if t.dtype != int32 or not t.is_cuda or t.shape != (batch.B,) or not t.is_contiguous():
                 raise DresdError(-1, f"{name} must be a contiguous int32 CUDA tensor of {batch.B} entries")
-        s = (stream or torch.cuda.current_stream()).cuda_stream
-        dresd_kv_keep_draft(self.handle, batch.c, best.data_ptr(), length.data_ptr(), n, L, s)
+        dresd_kv_keep_draft(self.handle, batch.c, best.data_ptr(), length.data_ptr(), n, L,
+                            _raw_stream(self.device_index, stream))
 
     def set_option(self, name: str, value: int):
         dresd_kv_set_option(self.handle, name, value)

@@ -196,6 +196,21 @@ cudaError_t launch_kv_read(const KvArgs &a, void *out_k, void *out_v, cudaStream
 cudaError_t launch_kv_keep_draft(const KvArgs &a, const int32_t *best, const int32_t *length, int n, int L,
                                  cudaStream_t stream);
 
+// Division by a number that the host knows: q = (umulhi(n, m) + n) >> s for n < 2^31 (Granlund and Montgomery 1994).
+struct FastDiv {
+    uint32_t d, m, s;
+    FastDiv() : d(1), m(1), s(0) {}
+    explicit FastDiv(uint32_t d_) : d(d_), s(0)
+    {
+        while ((1u << s) < d) ++s;
+        m = (uint32_t)(((1ull << 32) * ((1ull << s) - d)) / d + 1);
+    }
+#ifdef __CUDACC__
+    __device__ __forceinline__ int div(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> s); }
+    __device__ __forceinline__ int ceil(int n) const { return div(n + (int)d - 1); }
+#endif
+};
+
 struct AttendArgs {
     KvArgs kv;
     const void *q;
@@ -208,7 +223,11 @@ struct AttendArgs {
     float *lse;                 // [rows][heads * group] or null
     float *part;                // partial results: see kv_plan.cuh
     unsigned int *tickets;      // one per CTA, all zero between calls
-    int max_rows;               // rows of the longest chunk x group
+    int max_chunk;              // the longest chunk (only the choice of kernel depends on it)
+    FastDiv by_group;           // group
+    FastDiv by_rows;            // rows (few rows) or tokens (many) of a row tile
+    FastDiv by_unit;            // positions (few rows) or 128-position tiles (many) of a unit of work
+    int ctas;                   // CTAs of a worker: 1, or a cluster (see kv_plan.cuh)
     long long wait_cycles;      // bound of every device-side wait in cycles, 0 = default
     int lose_stage;             // test hook: CTA 0 never receives tile (value - 1); 0 = off
 };

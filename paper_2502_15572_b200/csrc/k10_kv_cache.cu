@@ -13,6 +13,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kHeads = 4;        // heads per thread
+constexpr int kKeepBlocks = 4096;
 
 // Page and offset of a dense row's token; false when the table does not reach it or names no page of the pool.
 __device__ __forceinline__ bool place_of(const KvArgs &a, int row, int &page, int &off)
@@ -31,6 +32,17 @@ __device__ __forceinline__ bool place_of(const KvArgs &a, int row, int &page, in
     page = __ldg(a.table + (long long)lo * a.width + i);
     off = (int)(p & ((1 << a.page_shift) - 1));
     return page >= 0 && page < a.num_pages;
+}
+
+// Magnitudes above the bound become the bound; NaN stays one.
+template <typename T>
+__device__ __forceinline__ uint32_t bounded(uint32_t two)
+{
+    constexpr uint32_t kInf = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
+    uint32_t lo = two & 0xFFFFu, hi = two >> 16;
+    if (lo > KvType<T>::kBoundBits && lo <= kInf) lo = KvType<T>::kBoundBits;
+    if (hi > KvType<T>::kBoundBits && hi <= kInf) hi = KvType<T>::kBoundBits;
+    return lo | hi << 16;
 }
 
 template <typename T, bool Q8, int D>
@@ -53,6 +65,7 @@ append_kernel(const KvArgs a, const T *__restrict__ k, long long k_row, long lon
         if (h0 + i < a.heads) x[i] = __ldg(reinterpret_cast<const uint4 *>(src + (h0 + i) * step + piece * 8));
     int page, off;
     if (!place_of(a, row, page, off)) return;
+    constexpr uint32_t kMag = 0x7FFF7FFFu;
     const unsigned lanes = kLanes == 32 ? 0xFFFFFFFFu : ((1u << kLanes) - 1) << (threadIdx.x % 32 / kLanes * kLanes);
 #pragma unroll
     for (int i = 0; i < kHeads; ++i) {
@@ -61,29 +74,28 @@ append_kernel(const KvArgs a, const T *__restrict__ k, long long k_row, long lon
         if constexpr (!Q8) {
             reinterpret_cast<uint4 *>(is_v ? a.v : a.k)[r * kLanes + piece] = x[i];
         } else {
-            const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-            float f[8], amax = 0.f;
+            uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+            // magnitudes of either type order like their bits, two at a time
+            uint32_t big = __vmaxu2(__vmaxu2(w[0] & kMag, w[1] & kMag), __vmaxu2(w[2] & kMag, w[3] & kMag));
+#pragma unroll
+            for (int o = kLanes / 2; o > 0; o >>= 1) big = __vmaxu2(big, __shfl_xor_sync(lanes, big, o));
+            big = max(big & 0xFFFFu, big >> 16);
+            if (big > KvType<T>::kBoundBits) {             // the same for every lane of the row
+                big = KvType<T>::kBoundBits;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = (w[j] & ~kMag) | bounded<T>(w[j] & kMag);
+            }
+            const int e = kv_exponent(unpack2<T>(big).x, KvType<T>::kMinExp);
+            const float s = pow2f(-e);                     // the product is exact: one rounding, to E4M3
+            uint32_t c[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float2 p = unpack2<T>(w[j]);
-                f[2 * j] = p.x;
-                f[2 * j + 1] = p.y;
+                float2 p = unpack2<T>(w[j]);
+                p.x *= s;
+                p.y *= s;
+                c[j] = __nv_cvt_float2_to_fp8x2(p, __NV_SATFINITE, __NV_E4M3);
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (fabsf(f[j]) > KvType<T>::kBound) f[j] = copysignf(KvType<T>::kBound, f[j]);
-                amax = fmaxf(amax, fabsf(f[j]));
-            }
-#pragma unroll
-            for (int o = kLanes / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(lanes, amax, o));
-            const int e = kv_exponent(amax, KvType<T>::kMinExp);
-            const float s = pow2f(-e);                     // the product is exact: one rounding, to E4M3
-            uint32_t c[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                c[j] = to_e4m3(f[4 * j] * s) | to_e4m3(f[4 * j + 1] * s) << 8 | to_e4m3(f[4 * j + 2] * s) << 16 |
-                       to_e4m3(f[4 * j + 3] * s) << 24;
-            reinterpret_cast<uint2 *>(is_v ? a.v : a.k)[r * kLanes + piece] = make_uint2(c[0], c[1]);
+            reinterpret_cast<uint2 *>(is_v ? a.v : a.k)[r * kLanes + piece] = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
             if (piece == 0) (is_v ? a.v_exps : a.k_exps)[r] = (uint8_t)(e + 127);
         }
     }
@@ -151,19 +163,18 @@ keep_kernel(const KvArgs a, const int32_t *__restrict__ best, const int32_t *__r
             int pieces)
 {
     const int b = blockIdx.y, r = best[b], kept = min(length[b] - 1, L);
-    if (r < 1 || r >= n) return;
+    if (r < 1 || r >= n || kept < 1) return;
     const int ctx = max(a.ctx[b], 0);
     const bool is_v = blockIdx.z != 0;
     uint4 *cache = static_cast<uint4 *>(is_v ? a.v : a.k);
     uint8_t *exps = is_v ? a.v_exps : a.k_exps;
-    const long long per_row = (long long)L * pieces, all = per_row * a.heads * a.layers;
-    for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < all; i += (long long)gridDim.x * kThreads) {
-        const int piece = (int)(i % pieces), t = (int)(i / pieces % L);
-        if (t >= kept) continue;
-        const int head = (int)(i / per_row % a.heads), layer = (int)(i / per_row / a.heads);
+    const int in_page = (1 << a.page_shift) - 1;
+    const unsigned per_row = (unsigned)kept * pieces, all = per_row * a.heads * a.layers;
+    for (unsigned i = blockIdx.x * kThreads + threadIdx.x; i < all; i += gridDim.x * kThreads) {
+        const unsigned lh = i / per_row, x = i - lh * per_row, t = x / pieces, piece = x - t * pieces;
+        const unsigned layer = lh / a.heads, head = lh - layer * a.heads;
         const long long to = (long long)ctx + 1 + t, from = to + (long long)r * L;
         if ((from >> a.page_shift) >= a.width) continue;
-        const int in_page = (1 << a.page_shift) - 1;
         const int pf = __ldg(a.table + (long long)b * a.width + (from >> a.page_shift));
         const int pt = __ldg(a.table + (long long)b * a.width + (to >> a.page_shift));
         if (pf < 0 || pf >= a.num_pages || pt < 0 || pt >= a.num_pages) continue;
@@ -220,9 +231,10 @@ cudaError_t launch_kv_keep_draft(const KvArgs &a, const int32_t *best, const int
                                  cudaStream_t stream)
 {
     const int pieces = a.d * (a.k_exps ? 1 : 2) / 16;
-    const long long all = (long long)L * pieces * a.heads * a.layers;
+    const long long all = (long long)L * pieces * a.heads * a.layers;       // below 2^31, checked by the caller
     const long long blocks = (all + kThreads - 1) / kThreads;
-    keep_kernel<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096), a.B, 2), kThreads, 0, stream>>>(a, best, length, n, L, pieces);
+    const int most = kKeepBlocks / a.B > 16 ? kKeepBlocks / a.B : 16;
+    keep_kernel<<<dim3((unsigned)(blocks < most ? blocks : most), a.B, 2), kThreads, 0, stream>>>(a, best, length, n, L, pieces);
     return cudaGetLastError();
 }
 

@@ -66,7 +66,7 @@ __device__ __forceinline__ uint32_t word(const uint2 &v, int i) { return i == 0 
 // NT: tiles of 8 rows.
 template <typename T, bool Q8, int D, int NT>
 __global__ void __launch_bounds__(kThreads)
-attend_mma_kernel(const AttendArgs a, int least)
+attend_mma_kernel(const __grid_constant__ AttendArgs a, int least)
 {
     constexpr int kRows = 8 * NT;
     constexpr int kRowBytes = Q8 ? D : 2 * D;             // one key or value
@@ -82,8 +82,8 @@ attend_mma_kernel(const AttendArgs a, int least)
     __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
     __shared__ unsigned s_ticket;
 
-    KvPlan<FewRows<kRows, kTile>> plan;
-    if (!plan.start(a, lane, least)) return;
+    KvPlan<FewRows> plan;
+    if (!plan.start(a, lane, blockIdx.x, gridDim.x, least)) return;
     Segment seg;
     while (plan.next(a, seg)) {
         const Chunk ch = plan.c;
@@ -95,8 +95,8 @@ attend_mma_kernel(const AttendArgs a, int least)
         for (int nt = 0; nt < NT; ++nt) {
             const int r = seg.rt * kRows + nt * 8 + g;
             const bool ok = nt * 8 + g < rows;
-            const T *src = static_cast<const T *>(a.q) + (long long)(ch.row0 + (ok ? r / a.group : 0)) * a.q_row +
-                           (seg.head * a.group + (ok ? r % a.group : 0)) * a.q_head;
+            const T *src = static_cast<const T *>(a.q) + (long long)(ch.row0 + (ok ? a.by_group.div(r) : 0)) * a.q_row +
+                           (seg.head * a.group + (ok ? (r - a.by_group.div(r) * a.group) : 0)) * a.q_head;
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) {
                 // 16-bit keys: piece 4 i + c.  8-bit keys: a key's piece is 16 elements, two of the query's.
@@ -115,7 +115,7 @@ attend_mma_kernel(const AttendArgs a, int least)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int r = min(nt * 8 + 2 * c + i, rows - 1);
-                const int tok = (seg.rt * kRows + r) / a.group;
+                const int tok = a.by_group.div(seg.rt * kRows + r);
                 limit[nt][i] = a.mask ? ch.total : min(ch.total, ch.ctx + tok + 1);
                 bits[nt][i] = a.mask ? a.mask + (long long)(ch.row0 + tok) * a.mask_words : nullptr;
             }
@@ -363,7 +363,7 @@ attend_mma_kernel(const AttendArgs a, int least)
             }
         __syncthreads();
         const bool shared_item = seg.c0 != seg.c1;
-        float *part = part_slot(a, plan.cta, seg.slot, kRows);
+        float *part = part_slot(a, blockIdx.x, seg.slot, kRows);
         // a thread takes 4 elements of a row
         for (int x = tid; x < rows * (D / 4); x += kThreads) {
             const int r = x / (D / 4), e = x % (D / 4) * 4;
@@ -389,7 +389,7 @@ attend_mma_kernel(const AttendArgs a, int least)
             } else {
                 const float inv = ll > 0.f ? 1.f / ll : ll == 0.f ? 0.f : ll;      // a NaN sum stays one
                 const int rr = seg.rt * kRows + r;
-                const long long at = (long long)(ch.row0 + rr / a.group) * heads + seg.head * a.group + rr % a.group;
+                const long long at = (long long)(ch.row0 + a.by_group.div(rr)) * heads + seg.head * a.group + (rr - a.by_group.div(rr) * a.group);
                 *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + at * D + e) =
                     make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
                 if (a.lse && e == 0) a.lse[at] = (base + log2f(ll)) * 0.69314718055994531f;
@@ -423,7 +423,7 @@ attend_mma_kernel(const AttendArgs a, int least)
                     const float base = mm > -INFINITY ? mm : 0.f;
                     const float inv = ll > 0.f ? 1.f / ll : ll == 0.f ? 0.f : ll;
                     const int rr = seg.rt * kRows + r;
-                    const long long at = (long long)(ch.row0 + rr / a.group) * heads + seg.head * a.group + rr % a.group;
+                    const long long at = (long long)(ch.row0 + a.by_group.div(rr)) * heads + seg.head * a.group + (rr - a.by_group.div(rr) * a.group);
                     *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + at * D + e) =
                         make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
                     if (a.lse && e == 0) a.lse[at] = (base + log2f(ll)) * 0.69314718055994531f;
@@ -453,7 +453,7 @@ cudaError_t launch(const AttendArgs &a, int sms, cudaStream_t stream)
 template <typename T, bool Q8>
 cudaError_t by_shape(const AttendArgs &a, int sms, cudaStream_t stream)
 {
-    const bool one = a.max_rows <= 8;
+    const bool one = (long long)a.max_chunk * a.group <= 8;
     if (a.kv.d == 64) return one ? launch<T, Q8, 64, 1>(a, sms, stream) : launch<T, Q8, 64, 2>(a, sms, stream);
     return one ? launch<T, Q8, 128, 1>(a, sms, stream) : launch<T, Q8, 128, 2>(a, sms, stream);
 }
@@ -463,8 +463,11 @@ cudaError_t by_shape(const AttendArgs &a, int sms, cudaStream_t stream)
 int attend_mma_max_ctas(int sms) { return 8 * sms; }
 size_t attend_mma_part_floats(int sms, int d) { return (size_t)attend_mma_max_ctas(sms) * 2 * 16 * (d + 2); }
 
-cudaError_t launch_attend_mma(const AttendArgs &a, int sms, cudaStream_t stream)
+cudaError_t launch_attend_mma(const AttendArgs &args, int sms, cudaStream_t stream)
 {
+    AttendArgs a = args;
+    a.by_unit = FastDiv(kTile);
+    a.by_rows = FastDiv((long long)a.max_chunk * a.group <= 8 ? 8 : 16);
     const bool q8 = a.kv.k_exps != nullptr;
     if (a.kv.dtype == kF16) return q8 ? by_shape<__half, true>(a, sms, stream) : by_shape<__half, false>(a, sms, stream);
     return q8 ? by_shape<__nv_bfloat16, true>(a, sms, stream) : by_shape<__nv_bfloat16, false>(a, sms, stream);

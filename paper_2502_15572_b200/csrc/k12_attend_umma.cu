@@ -10,18 +10,27 @@
 //     P_w = 2^(scale S_w - m)        a thread owns a row: no shuffles; 16 bits, back to TMEM
 //     O_w += P_w V         P from TMEM, V as stored ([position][d] is the MN-major operand)
 //
+// When there are fewer items than CTAs, clusters of up to eight CTAs share an item: the 2 x ctas streams take every
+// (2 x ctas)-th tile, and each CTA adds up its share of the sums over distributed shared memory.
+//
 // Items of more than 128 rows give the streams two row tiles and every loaded tile of positions to both; items of
 // up to 128 rows give both streams the same rows and every second tile each, and join them at the end.  Rows of a group of heads are
 // packed: 128 / group tokens x group heads are one row tile, which one TMA box of the queries fetches.
 //
 // Roles: warp 0 loads tiles (a lane per page and slab, so that small pages are issued side by side), warp 1 issues the products,
-// warp 2 loads queries, warp 3 looks after values nobody may see (below), warps 4-7 and 8-11 are the streams' softmax;
-// with an 8-bit cache warps 12-15 turn codes into 16-bit tiles.  The maximum is raised only when a score passes it by 2^8, so O
-// is rarely rescaled; by then the stream's products have ended, because its next S is issued behind them.
+// warp 2 works out the CTA's segments and loads their queries, warp 3 clears values behind a sequence's end, warps 4-7 and
+// 8-11 are the streams' softmax; with an 8-bit cache warps 12-15 turn codes into 16-bit tiles.
 //
-// 0 x NaN is NaN, so a place that a row does not see must not reach the second product: places behind the sequence's end
-// are cleared in shared memory, and non-finite values of the chunk itself are taken out there and put back at the end as
-// what they make of a result, NaN, for the rows and elements that see them.
+// The chain scores -> weights -> second product -> next scores of a stream is what bounds a long call (its S, P and O fill
+// TMEM, so a stream has one tile in the works), hence: the maximum in independent chains of three-input maxima, taken
+// while the second half of the scores is still on its way; the maximum only raised when a score passes it by 2^8, so that O
+// is rarely rescaled (by then the stream's products have ended, its next S is issued behind them); every fourth
+// exponential on the FMA pipes (the MUFU unit takes 8 cycles a warp); and the second product begins when half of
+// the weights are stored.
+//
+// 0 x NaN is NaN, so what a row does not see must not reach the second product as a non-finite number.  Places behind the
+// sequence's end are cleared in shared memory.  Values of the chunk itself are not looked at unless a sum comes out
+// non-finite; then repair() adds up the row again without the ones it does not see.
 #include "kv_plan.cuh"
 
 namespace dresd {
@@ -30,6 +39,7 @@ namespace {
 constexpr int kTile = 128;                                 // rows of a row tile, positions of a tile
 constexpr int kSlabBytes = kTile * 128;                    // 64 elements of every row of a tile
 constexpr float kSlack = 8.f;
+constexpr int kMaxCluster = 8;
 
 template <bool Q8, int D>
 struct Geometry {
@@ -40,72 +50,81 @@ struct Geometry {
     static constexpr int kRawBytes = kTile * D;
     static constexpr int kThreads = Q8 ? 512 : 384;
     static constexpr int kBig = 2 * kTileBytes + kStages * kTileBytes + kRaw * kRawBytes;
-    static constexpr int kSmall = 2048 + 1024;             // maxima and sums of both streams; barriers and plan
+    static constexpr int kSmall = 2048 + (D == 64 ? 2048 : 1024);             // maxima and sums of both streams; barriers, plan, exponents
 };
 constexpr int kSmemBytes = 232448;                         // all of an SM's shared memory (one CTA per SM, by TMEM too)
-constexpr int kMaxStages = 10, kMaxRaw = 8;
 
 // Row tiles of one or two streams.
 struct ManyRows {
-    static __device__ __forceinline__ int per_tile(const AttendArgs &a) { return kTile / a.group; }     // tokens of a stream
-    static __device__ __forceinline__ int row_tiles(const AttendArgs &a, const Chunk &k)
-    {
-        const int t = 2 * per_tile(a);
-        return (k.len + t - 1) / t;
-    }
+    static __device__ __forceinline__ int per_tile(const AttendArgs &a) { return (int)a.by_rows.d >> 1; }     // tokens of a stream
+    static __device__ __forceinline__ int row_tiles(const AttendArgs &a, const Chunk &k) { return a.by_rows.ceil(k.len); }
     static __device__ __forceinline__ int tokens(const AttendArgs &a, const Chunk &k, int r)
     {
-        const int t = 2 * per_tile(a);
-        return min(t, k.len - r * t);
+        return min((int)a.by_rows.d, k.len - r * (int)a.by_rows.d);
     }
     static __device__ __forceinline__ bool one_tile(const AttendArgs &a, const Chunk &k, int r) { return tokens(a, k, r) <= per_tile(a); }
     // position tiles that the item's rows see
     static __device__ __forceinline__ int tiles(const AttendArgs &a, const Chunk &k, int r)
     {
         int seen = k.total;
-        if (!a.mask) seen = min(seen, k.ctx + r * 2 * per_tile(a) + tokens(a, k, r));
+        if (!a.mask) seen = min(seen, k.ctx + r * (int)a.by_rows.d + tokens(a, k, r));
         return max(1, (seen + kTile - 1) / kTile);
     }
-    // a unit keeps both streams busy for one tile: one tile of positions for two row tiles, two for one
+    // a unit keeps all streams busy for one tile: one tile of positions for two row tiles, one for each stream for one
     static __device__ __forceinline__ int units(const AttendArgs &a, const Chunk &k, int r)
     {
         const int t = tiles(a, k, r);
-        return one_tile(a, k, r) ? (t + 1) / 2 : t;
+        return one_tile(a, k, r) ? a.by_unit.ceil(t) : t;
     }
 };
 
+// What every role knows of a segment, worked out once by warp 2 and handed over in shared memory.
+struct Job {
+    Segment seg;
+    Chunk c;
+    int more;            // 0: there are no more segments
+    int one;             // both streams (of every CTA of a cluster) on the same rows
+    int t0, step;        // this CTA's tile j is t0 + j, or of one: t0 + j / 2 x step + j % 2
+    int nt;              // its tiles
+    int n[2];            // tiles of the streams
+    __device__ __forceinline__ void set(const AttendArgs &a, int rank)
+    {
+        more = 1;
+        one = ManyRows::one_tile(a, c, seg.rt);
+        const int all = ManyRows::tiles(a, c, seg.rt);
+        if (one) {
+            step = 2 * a.ctas;
+            t0 = step * seg.kt0 + 2 * rank;
+            const int end = min(step * seg.kt1, all);
+            n[0] = a.by_unit.ceil(max(0, end - t0));
+            n[1] = a.by_unit.ceil(max(0, end - t0 - 1));
+            nt = n[0] + n[1];
+        } else {
+            step = 2;
+            t0 = seg.kt0;
+            n[0] = n[1] = nt = seg.kt1 - seg.kt0;
+        }
+    }
+    __device__ __forceinline__ int tile(int j) const { return t0 + (one ? (j >> 1) * step + (j & 1) : j); }
+    // Place of value tile j in the order in which tiles are loaded and consumed: K0 V0 K1 V1 ... for two row tiles,
+    // K0 K1 V0 K2 V1 K3 ... for one.
+    __device__ __forceinline__ int v_place(int j) const { return one ? (j == nt - 1 ? 2 * nt - 1 : 2 + 2 * j) : 2 * j + 1; }
+    // the last value tile holds places behind the end
+    __device__ __forceinline__ bool ragged() const { return nt > 0 && (tile(nt - 1) + 1) * kTile > c.total; }
+};
+
+template <int kStages, int kRaw>
 struct Shared {
-    uint64_t full[kMaxStages], empty[kMaxStages], v_ok[kMaxStages];
-    uint64_t raw_full[kMaxRaw], raw_empty[kMaxRaw];
-    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2];
+    uint64_t full[kStages], empty[kStages];
+    uint64_t raw_full[kRaw ? kRaw : 1], raw_empty[kRaw ? kRaw : 1];
+    uint64_t q_full[2], q_empty[2], s_full[2], p_half[2], p_full[2], o_full[2];
+    uint64_t cleared[2];                                   // ragged value tile of this segment, of the next
+    uint64_t job_full[2], job_empty[2];
+    uint64_t ready, taken;                                 // cluster: every CTA's sums are in place / have been read
+    alignas(16) uint8_t exps[kRaw ? kRaw : 1][kTile];      // exponents of the 8-bit tiles (bulk copies: 16-byte aligned)
+    Job job[2];
     uint32_t tmem;
     unsigned ticket;
-    int bad;                                               // a value of some chunk was not finite
-    // the softmax warps' place in the plan lives here, not in their registers, which the scores need
-    KvPlan<ManyRows> plan;
-    Segment seg;
-    int more;
-};
-static_assert(sizeof(Shared) <= 1024, "barriers and plan");
-
-// What every role knows of a segment.
-struct Work {
-    bool one;            // both streams on the same rows
-    int t0, nt;          // first position tile, tiles
-    int n[2];            // tiles of the streams
-    __device__ __forceinline__ Work(const AttendArgs &a, const Chunk &c, const Segment &s)
-    {
-        one = ManyRows::one_tile(a, c, s.rt);
-        const int all = ManyRows::tiles(a, c, s.rt);
-        t0 = one ? 2 * s.kt0 : s.kt0;
-        nt = (one ? min(2 * s.kt1, all) : s.kt1) - t0;
-        n[0] = one ? (nt + 1) / 2 : nt;
-        n[1] = one ? nt / 2 : nt;
-    }
-    // Places of key tile j and value tile j in the order in which tiles are loaded and consumed:
-    // K0 V0 K1 V1 ... for two row tiles, K0 K1 V0 K2 V1 K3 ... for one.
-    __device__ __forceinline__ int k_place(int j) const { return one ? (j < 2 ? j : 2 * j - 1) : 2 * j; }
-    __device__ __forceinline__ int v_place(int j) const { return one ? (j == nt - 1 ? 2 * nt - 1 : 2 + 2 * j) : 2 * j + 1; }
 };
 
 __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, int x, int y, int z, uint64_t *bar)
@@ -114,6 +133,43 @@ __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, i
         "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
         ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
         : "memory");
+}
+// Plain bulk copy; 16-byte aligned, a multiple of 16 bytes.
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+                 "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+// Distributed shared memory: the same place in CTA `rank` of the cluster.
+__device__ __forceinline__ float ld_cluster(const float *p, uint32_t rank)
+{
+    float x;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(mapa_rank(smem_u32(p), rank)) : "memory");
+    return x;
+}
+__device__ __forceinline__ float4 ld_cluster(const float4 *p, uint32_t rank)
+{
+    float4 x;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(mapa_rank(smem_u32(p), rank)) : "memory");
+    return x;
+}
+// Bounded wait on a barrier that other CTAs of the cluster arrive on.
+__device__ __forceinline__ bool mbar_wait_cluster(uint64_t *bar, uint32_t parity, long long limit)
+{
+    const long long t0 = clock64();
+    while (true) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(smem_u32(bar)), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if (clock64() - t0 > limit) return false;
+    }
 }
 // First operand from TMEM.
 __device__ __forceinline__ void umma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
@@ -140,6 +196,16 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t *r)
           "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(taddr));
 }
+// Waits for the loads, and tells the compiler that these 32 registers come with it.
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t *r)
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+                   "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+                   "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+                 :: "memory");
+}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
 {
     asm volatile(
@@ -159,6 +225,30 @@ __device__ __forceinline__ void set_registers()
     if constexpr (kMore) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCount));
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCount));
 }
+// Barrier and "all of them".
+__device__ __forceinline__ bool bar_and(int id, int threads, bool x)
+{
+    int r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.s32 q, %3, 0;\n\t"
+        "bar.red.and.pred p, %1, %2, q;\n\t"
+        "selp.s32 %0, 1, 0, p;\n\t}"
+        : "=r"(r)
+        : "r"(id), "r"(threads), "r"((int)x)
+        : "memory");
+    return r != 0;
+}
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xFFFFFFFF;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r != 0;
+}
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
@@ -166,25 +256,116 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// Parts of shared items: two slots per CTA; sums as [d / 4][256 rows] float4 (a warp's rows side by side), maxima,
-// weight sums, and whether a value was not finite.
+// Parts of shared items: two slots per CTA; sums as [d / 4][256 rows] float4 (a warp's rows side by side), maxima and
+// weight sums.
 constexpr int kPartRows = 2 * kTile;
-__host__ __device__ constexpr size_t part_floats(int d) { return (size_t)kPartRows * (d + 2) + 32; }
+__host__ __device__ constexpr size_t part_floats(int d) { return (size_t)kPartRows * (d + 2); }
 
-// The rows of the chunk's own tokens that (row's token, j) ...: does token `tok` of the chunk see its place j?
-__device__ __forceinline__ bool sees(const AttendArgs &a, const Chunk &c, int tok, int j)
+// Packed pairs of floats.
+__device__ __forceinline__ uint64_t pair(float lo, float hi)
 {
-    if (c.ctx + j >= c.total) return false;
-    if (!a.mask) return j <= tok;
-    return (j >> 5) < a.mask_words && (a.mask[(long long)(c.row0 + tok) * a.mask_words + (j >> 5)] >> (j & 31) & 1);
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// 2^x of a pair on the FMA pipes: x = n + f with n the nearest whole number (x + 1.5 x 2^23 holds n in its low bits), 2^f by a
+// polynomial of degree 5 on [-1/2, 1/2] (least squares at Chebyshev points, reweighted towards the smallest largest relative
+// error; 2^-22.1 in fp32 arithmetic over the interval), 2^n from n's bits.  NaN stays NaN; below 2^-126 the result
+// stays at about 2^-126.
+__device__ __forceinline__ uint64_t ex2_fma(uint64_t x)
+{
+    float lo, hi;
+    unpair(x, lo, hi);
+    x = pair(max_nan(lo, -126.f), max_nan(hi, -126.f));
+    const float kRound = 12582912.f + 127.f;               // low bits of the sum: n + 127
+    const uint64_t t = add2(x, pair(kRound, kRound));
+    const uint64_t f = add2(x, mul2(add2(t, pair(-kRound, -kRound)), pair(-1.f, -1.f)));
+    uint64_t p = pair(0.0013276466634124517f, 0.0013276466634124517f);
+    p = fma2(p, f, pair(0.009675540961325169f, 0.009675540961325169f));
+    p = fma2(p, f, pair(0.05550713464617729f, 0.05550713464617729f));
+    p = fma2(p, f, pair(0.24022120237350464f, 0.24022120237350464f));
+    p = fma2(p, f, pair(0.6931469440460205f, 0.6931469440460205f));
+    p = fma2(p, f, pair(1.0000001192092896f, 1.0000001192092896f));
+    unpair(t, lo, hi);
+    return mul2(p, pair(__uint_as_float(__float_as_uint(lo) << 23), __uint_as_float(__float_as_uint(hi) << 23)));
+}
+
+// Sums of stream `st` for row `row` and elements d .. d + 31 of a segment, added up one position after the other without what the
+// row does not see -- called when the tensor cores' sum is not finite.  Leaves `x` alone if the chunk's own values are
+// finite (then the non-finite ones are seen by every row).
+template <typename T, int D>
+__device__ __noinline__ void repair(const AttendArgs &a, const Job &job, int st, int row, int tok, float m, int d, float *x)
+{
+    const Chunk &c = job.c;
+    tok = min(tok, c.len - 1);
+    const int head = job.seg.head, heads = a.group, in_page = (1 << a.kv.page_shift) - 1;
+    const T *q = static_cast<const T *>(a.q) + (long long)(c.row0 + tok) * a.q_row + (long long)(head * heads + row - a.by_group.div(row) * heads) * a.q_head;
+    auto row_of = [&](int p) {
+        const int page = a.kv.table[(long long)job.seg.b * a.kv.width + (p >> a.kv.page_shift)];
+        return kv_row(a.kv, a.kv.layer, page < 0 || page >= a.kv.num_pages ? 0 : page, head, p & in_page);
+    };
+    float y[32] = {};
+    bool odd = false;
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int j = 0; j < job.n[st]; ++j) {
+            const int p0 = job.tile(job.one ? 2 * j + st : j) * kTile;
+            for (int p = max(p0, pass ? 0 : c.ctx); p < min(p0 + kTile, c.total); ++p) {
+                const long long r = row_of(p);
+                const T *k = static_cast<const T *>(a.kv.k) + r * D, *v = static_cast<const T *>(a.kv.v) + r * D + d;
+                if (pass == 0) {
+                    for (int e = 0; e < 32; ++e) odd |= !isfinite(unpack2<T>(reinterpret_cast<const uint16_t *>(v)[e]).x);
+                    continue;
+                }
+                const int t = p - c.ctx;
+                if (t >= 0 && !(a.mask ? (t >> 5) < a.mask_words && (a.mask[(long long)(c.row0 + tok) * a.mask_words + (t >> 5)] >> (t & 31) & 1) : t <= tok)) continue;
+                float s = 0.f;
+                for (int e = 0; e < D; e += 2) {
+                    const float2 kk = unpack2<T>(*reinterpret_cast<const uint32_t *>(k + e)), qq = unpack2<T>(*reinterpret_cast<const uint32_t *>(q + e));
+                    s = fmaf(kk.x, qq.x, s);
+                    s = fmaf(kk.y, qq.y, s);
+                }
+                const float w = unpack2<T>(pack2<T>(ex2((s - m) * a.scale_log2), 0.f)).x;
+                for (int e = 0; e < 32; ++e) y[e] += w * unpack2<T>(reinterpret_cast<const uint16_t *>(v)[e]).x;
+            }
+        }
+        if (pass == 0 && !odd) return;
+    }
+    for (int e = 0; e < 32; ++e) x[e] = y[e];
 }
 
 template <typename T, bool Q8, int D>
 __global__ void __launch_bounds__(Geometry<Q8, D>::kThreads, 1)
 attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
-                   const __grid_constant__ CUtensorMap v_map, const AttendArgs a)
+                   const __grid_constant__ CUtensorMap v_map, const __grid_constant__ AttendArgs a)
 {
     using Geo = Geometry<Q8, D>;
+    using Sh = Shared<Geo::kStages, Geo::kRaw>;
+    static_assert(2048 + sizeof(Sh) <= Geo::kSmall, "shared memory");
     constexpr int kStages = Geo::kStages, kSlabs = Geo::kSlabs, kTileBytes = Geo::kTileBytes;
     extern __shared__ uint8_t smem_raw[];
     const int pad = (int)(-smem_u32(smem_raw) & 1023u);
@@ -193,19 +374,19 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     uint8_t *raws = stages + kStages * kTileBytes;
     float *s_m = reinterpret_cast<float *>(raws + Geo::kRaw * Geo::kRawBytes);       // [2][128]
     float *s_l = s_m + 2 * kTile;                                                     // [2][128]
-    Shared &sh = *reinterpret_cast<Shared *>(s_l + 2 * kTile);
+    Sh &sh = *reinterpret_cast<Sh *>(s_l + 2 * kTile);
     if (pad + Geo::kBig + Geo::kSmall > kSmemBytes) {       // shared memory never starts there
         if (threadIdx.x == 0) report_timeout(a.kv.status);
         return;
     }
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long wl = a.wait_cycles > 0 ? a.wait_cycles : kWaitCycles;
+    const int rank = a.ctas > 1 ? (int)cluster_ctarank() : 0;
 
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
             mbar_init(&sh.full[s], Q8 ? 4 : 1);
             mbar_init(&sh.empty[s], 1);
-            mbar_init(&sh.v_ok[s], 1);
         }
         for (int s = 0; s < Geo::kRaw; ++s) {
             mbar_init(&sh.raw_full[s], 1);
@@ -213,30 +394,48 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         }
         for (int w = 0; w < 2; ++w) {
             mbar_init(&sh.q_full[w], 1);
-            mbar_init(&sh.q_empty[w], 1);
+            mbar_init(&sh.q_empty[w], w == 0 && a.ctas > 1 ? 2 : 1);      // cluster: the sums pass through its place
             mbar_init(&sh.s_full[w], 1);
+            mbar_init(&sh.p_half[w], 4);
             mbar_init(&sh.p_full[w], 4);
             mbar_init(&sh.o_full[w], 1);
+            mbar_init(&sh.cleared[w], 1);
+            mbar_init(&sh.job_full[w], 1);
+            mbar_init(&sh.job_empty[w], Q8 ? 2 + 8 + 4 : 3 + 8);          // a warp each: loads, products, (clearing,) softmax, (conversion)
         }
-        sh.bad = sh.more = 0;
+        mbar_init(&sh.ready, a.ctas);
+        mbar_init(&sh.taken, a.ctas);
         mbar_fence_init();
+        tma_prefetch_desc(&q_map);
+        tma_prefetch_desc(&k_map);
+        tma_prefetch_desc(&v_map);
     }
     if (warp == 3) {
         tmem_alloc(&sh.tmem, 512);
         tmem_relinquish();
     }
-    KvPlan<ManyRows> plan;
-    const bool busy = plan.start(a, lane, 1);                  // the same for the whole CTA
-    if (tid == 0) sh.plan = plan;
     tc_fence_before();
-    __syncthreads();
+    __syncwarp();
+    if (a.ctas > 1) cluster_sync_all();                     // the neighbours' barriers are set up
+    else __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sh.tmem;                          // S0, S1 at 0, 128; O0, O1 at 256, 256 + D
-    Segment seg;
+    pdl_wait();                                             // what follows reads what earlier kernels wrote
+    pdl_launch_dependents();
 
-    if (!busy) {
-        // nothing to do: fall through to the end
-    } else if (warp < 4) {
+    // Segment number `i` of this CTA, when warp 2 has worked it out; false = a wait ran out.
+    auto job_of = [&](int i) { return mbar_wait(&sh.job_full[i & 1], (i >> 1) & 1, wl); };
+    // The calling warp is done with it.
+    auto job_done = [&](int i) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.job_empty[i & 1]);
+    };
+
+    if (warp < 4) {
+        KvPlan<ManyRows> plan;
+        bool more = false;
+        // (before the registers are given up: it calls functions that are compiled apart)
+        if (warp == 2) more = plan.start(a, lane, blockIdx.x / a.ctas, gridDim.x / a.ctas, 1);     // the same for the whole cluster
         set_registers<false, Q8 ? 64 : 88>();
         if (warp == 0) {
             // ---- tiles of keys and values: 16-bit ones straight into the stages, 8-bit ones into the raw ring
@@ -245,189 +444,219 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             constexpr int kParts = Q8 ? 1 : kSlabs;              // copies per page
             uint8_t *ring = Q8 ? raws : stages;
             uint64_t *full = Q8 ? sh.raw_full : sh.full, *empty = Q8 ? sh.raw_empty : sh.empty;
-            if (lane == 0) {
-                tma_prefetch_desc(&k_map);
-                tma_prefetch_desc(&v_map);
-            }
             const int per = kTile >> a.kv.page_shift;            // pages per tile
+            const int pg = lane / kParts, part = lane % kParts;
             const int beyond = (int)min((long long)a.kv.layers * a.kv.num_pages * a.kv.heads << a.kv.page_shift, 2147483647LL);
-            int it = 0, issued = 0;
+            int issued = 0;
             bool ok = true;
-            while (ok && plan.next(a, seg)) {
-                const Chunk c = plan.c;
-                const Work w(a, c, seg);
-                // page of this lane's copy of tile t, as a row of the maps (out of range: zeros are loaded)
-                auto row_of = [&](int t) {
-                    const int p = t * kTile + ((lane / kParts) << a.kv.page_shift);
+            for (int i = 0; ok; ++i) {
+                if (!job_of(i)) { ok = false; break; }
+                const Job &w = sh.job[i & 1];
+                if (!w.more) break;
+                const int total = w.c.total, head = w.seg.head;
+                const int32_t *table = a.kv.table + (long long)w.seg.b * a.kv.width;
+                // page of this lane's copy of this CTA's tile j, as a row of the maps (out of range: zeros are loaded)
+                auto row_of = [&](int j) {
+                    const int p = w.tile(j) * kTile + (pg << a.kv.page_shift);
                     int page = -1;
-                    if (lane < per * kParts && p < c.total)
-                        page = __ldg(a.kv.table + (long long)seg.b * a.kv.width + (p >> a.kv.page_shift));
+                    if (j < w.nt && pg < per && p < total) page = __ldg(table + (p >> a.kv.page_shift));
                     if (page < 0 || page >= a.kv.num_pages) return beyond;
-                    return (int)kv_row(a.kv, a.kv.layer, page, seg.head, 0);
+                    return (int)kv_row(a.kv, a.kv.layer, page, head, 0);
                 };
-                auto load = [&](const CUtensorMap *map, int row) {
-                    const int s = it % kRing;
-                    if (it >= kRing && !mbar_wait(&empty[s], ((it / kRing) - 1) & 1, wl)) ok = false;
+                auto load = [&](bool is_v, int row) {
+                    const int s = issued % kRing;
+                    if (issued >= kRing && !mbar_wait(&empty[s], ((issued / kRing) - 1) & 1, wl)) ok = false;
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     if (!ok) return;
-                    if (lane == 0) mbar_arrive_expect_tx(&full[s], (uint32_t)kBytes);
+                    if (lane == 0) mbar_arrive_expect_tx(&full[s], (uint32_t)(kBytes + (Q8 ? kTile : 0)));
                     __syncwarp();
-                    if (lane < per * kParts && !(a.lose_stage > 0 && blockIdx.x == 0 && it == a.lose_stage - 1)) {
-                        const int pg = lane / kParts, part = lane % kParts;
+                    if (pg < per && !(a.lose_stage > 0 && blockIdx.x == 0 && issued == a.lose_stage - 1)) {
                         uint8_t *dst = ring + (size_t)s * kBytes + part * kSlabBytes + ((size_t)pg << a.kv.page_shift) * (Q8 ? D : 128);
-                        tma_load_2d(dst, map, part * 64, row, &full[s]);
+                        tma_load_2d(dst, is_v ? &v_map : &k_map, part * 64, row, &full[s]);
+                        // the page's exponents; zeros have any
+                        if constexpr (Q8)
+                            bulk_load(sh.exps[s] + (pg << a.kv.page_shift), (is_v ? a.kv.v_exps : a.kv.k_exps) + (row < beyond ? row : 0),
+                                      1u << a.kv.page_shift, &full[s]);
                     }
-                    ++it;
-                    issued = it;
+                    ++issued;
                 };
-                const int ahead = w.one ? 2 : 1;
-                int r0 = row_of(w.t0), r1 = w.nt > 1 ? row_of(w.t0 + 1) : beyond;    // of value tiles j, j + 1
-                load(&k_map, r0);
-                if (ahead == 2 && w.nt > 1) load(&k_map, r1);
-                for (int j = 0; j < w.nt && ok; ++j) {
-                    const int r2 = j + 2 < w.nt ? row_of(w.t0 + j + 2) : beyond;
-                    load(&v_map, r0);
-                    if (ok && j + ahead < w.nt) load(&k_map, ahead == 2 ? r2 : r1);
+                const int ahead = w.one ? 2 : 1, nt = w.nt;
+                int r0 = row_of(0), r1 = row_of(1);          // of value tiles j, j + 1
+#pragma unroll 1
+                for (int x = 0; x < min(ahead, nt) && ok; ++x) load(false, x ? r1 : r0);
+#pragma unroll 1
+                for (int j = 0; j < nt && ok; ++j) {
+                    const int r2 = row_of(j + 2);
+                    load(true, r0);
+                    if (ok && j + ahead < nt) load(false, ahead == 2 ? r2 : r1);
                     r0 = r1;
                     r1 = r2;
                 }
-                plan.advance(a);
+                job_done(i);
             }
             if (!ok && lane == 0) report_timeout(a.kv.status);
             // no copy may be in flight when the CTA ends
-            for (int i = max(0, issued - kRing); i < issued; ++i)
-                if (!mbar_wait(&full[i % kRing], (i / kRing) & 1, wl)) {
+            for (int x = max(0, issued - kRing); x < issued; ++x)
+                if (!mbar_wait(&full[x % kRing], (x / kRing) & 1, wl)) {
                     if (lane == 0) report_timeout(a.kv.status);
                     break;
                 }
         } else if (warp == 1) {
-            // ---- products
-            if (lane == 0) {
-                constexpr uint32_t kFmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
-                constexpr uint32_t kCommon = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((uint32_t)(kTile >> 4) << 24);
-                constexpr uint32_t kIdescS = kCommon | ((uint32_t)(kTile >> 3) << 17);
-                constexpr uint32_t kIdescO = kCommon | ((uint32_t)(D >> 3) << 17) | (1u << 16);       // second operand MN-major
-                int base = 0;                                    // tiles consumed by earlier segments
-                int steps[2] = {0, 0}, q_uses[2] = {0, 0};
-                bool ok = true;
-                while (ok && plan.next(a, seg)) {
-                    const Work w(a, plan.c, seg);
-                    auto scores = [&](int st, int j) {
-                        const int i = base + w.k_place(w.one ? 2 * j + st : j), s = i % kStages;
-                        if (!mbar_wait(&sh.full[s], (i / kStages) & 1, wl)) return false;
-                        tc_fence_after();
-                        const uint32_t qa = smem_u32(q_s) + (w.one ? 0 : st * kTileBytes), ka = smem_u32(stages) + s * kTileBytes;
+            // ---- products.  The whole warp walks through the loop and one lane issues: what the instructions take must be known
+            // to be the same for all lanes (hence the shuffles), or every operand is moved to the uniform registers by itself,
+            // at 100 cycles and more an instruction against the 64 that it runs.
+            constexpr uint32_t kFmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+            constexpr uint32_t kCommon = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((uint32_t)(kTile >> 4) << 24);
+            constexpr uint32_t kIdescS = kCommon | ((uint32_t)(kTile >> 3) << 17);
+            constexpr uint32_t kIdescO = kCommon | ((uint32_t)(D >> 3) << 17) | (1u << 16);       // second operand MN-major
+            auto uniform = [](int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); };
+            const uint32_t t0 = uniform(tmem);
+            const uint64_t q_desc = make_desc(smem_u32(q_s)), k_desc = make_desc(smem_u32(stages)), v_desc = make_desc_mn(smem_u32(stages));
+            const bool issuer = elect_one();
+            int base = 0;                                    // tiles consumed by earlier segments
+            int steps0 = 0, steps1 = 0, uses0 = 0, uses1 = 0, clears0 = 0, clears1 = 0;
+            bool ok = true;
+            for (int i = 0; ok; ++i) {
+                if (!__all_sync(0xFFFFFFFFu, job_of(i))) { ok = false; break; }
+                const Job &w = sh.job[i & 1];
+                if (!uniform(w.more)) break;
+                const bool one = uniform(w.one) != 0, ragged = !Q8 && uniform(w.ragged()) != 0;
+                const int nt = uniform(w.nt), n0 = uniform(w.n[0]), n1 = uniform(w.n[1]);
+                auto wait = [&](uint64_t *bar, int parity) {
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity & 1, wl));
+                    tc_fence_after();
+                    return ok;
+                };
+                auto k_place = [&](int j) { return one ? (j < 2 ? j : 2 * j - 1) : 2 * j; };
+                auto v_place = [&](int j) { return one ? (j == nt - 1 ? 2 * nt - 1 : 2 + 2 * j) : 2 * j + 1; };
+                auto scores = [&](auto st_, int j) {
+                    constexpr int st = decltype(st_)::value;
+                    const int x = base + k_place(one ? 2 * j + st : j), s = x % kStages;
+                    if (!wait(&sh.full[s], x / kStages)) return;
+                    const uint64_t qd = q_desc + (one ? 0 : st * (kTileBytes >> 4)), kd = k_desc + s * (kTileBytes >> 4);
+                    const bool last = one ? 2 * j + st == nt - 1 : j == nt - 1;
+                    if (issuer) {
 #pragma unroll
                         for (int k = 0; k < D / 16; ++k)
-                            umma_f16(tmem + st * kTile, make_desc(qa + (k >> 2) * kSlabBytes) + 2 * (k & 3),
-                                     make_desc(ka + (k >> 2) * kSlabBytes) + 2 * (k & 3), kIdescS, k != 0);
+                            umma_f16(t0 + st * kTile, qd + ((k >> 2) * (kSlabBytes >> 4) + 2 * (k & 3)), kd + ((k >> 2) * (kSlabBytes >> 4) + 2 * (k & 3)),
+                                     kIdescS, k != 0);
                         tc_commit(&sh.s_full[st]);
-                        if (w.one || st == 1) tc_commit(&sh.empty[s]);
-                        if (w.one ? 2 * j + st == w.nt - 1 : j == w.nt - 1) tc_commit(&sh.q_empty[w.one ? 0 : st]);
-                        return true;
-                    };
-                    for (int st = 0; st < (w.one ? 1 : 2) && ok; ++st) {
-                        ok = mbar_wait(&sh.q_full[st], q_uses[st] & 1, wl);
-                        ++q_uses[st];
+                        if (one || st == 1) tc_commit(&sh.empty[s]);
+                        if (last) tc_commit(&sh.q_empty[one ? 0 : st]);
                     }
-                    for (int st = 0; st < 2 && ok; ++st)
-                        if (w.n[st] > 0) ok = scores(st, 0);
-                    for (int j = 0; j < w.n[0] && ok; ++j)
-                        for (int st = 0; st < 2 && ok; ++st) {
-                            if (j >= w.n[st]) continue;
-                            const int i = base + w.v_place(w.one ? 2 * j + st : j), s = i % kStages;
-                            ok = mbar_wait(Q8 ? &sh.full[s] : &sh.v_ok[s], (i / kStages) & 1, wl) && mbar_wait(&sh.p_full[st], steps[st] & 1, wl);
-                            if (!ok) break;
-                            ++steps[st];
-                            tc_fence_after();
-                            const uint32_t va = smem_u32(stages) + s * kTileBytes;
+                    __syncwarp();
+                };
+                auto sums = [&](auto st_, int j, int &steps) {
+                    constexpr int st = decltype(st_)::value;
+                    const int vj = one ? 2 * j + st : j, x = base + v_place(vj), s = x % kStages;
+                    if (!wait(&sh.full[s], x / kStages)) return;
+                    if (ragged && vj == nt - 1 && (one || st == 0)) {
+                        if (!wait(&sh.cleared[i & 1], i & 1 ? clears1 : clears0)) return;
+                        if (i & 1) ++clears1;
+                        else ++clears0;
+                    }
+                    const uint64_t vd = v_desc + s * (kTileBytes >> 4);
+                    const uint32_t o = t0 + 256 + st * D, p = t0 + st * kTile;
+                    if (!wait(&sh.p_half[st], steps)) return;
+                    if (issuer) {
+                        if (j == 0) umma_f16_ta(o, p, vd, kIdescO, 0);
+                        else umma_f16_ta(o, p, vd, kIdescO, 1);
 #pragma unroll
-                            for (int k = 0; k < kTile / 16; ++k)
-                                umma_f16_ta(tmem + 256 + st * D, tmem + st * kTile + 8 * k, make_desc_mn(va) + 128 * k, kIdescO, (j | k) != 0);
-                            if (w.one || st == 1) tc_commit(&sh.empty[s]);
-                            if (j == w.n[st] - 1) tc_commit(&sh.o_full[st]);
-                            else ok = scores(st, j + 1);
-                        }
-                    base += 2 * w.nt;
-                    plan.advance(a);
+                        for (int k = 1; k < kTile / 32; ++k) umma_f16_ta(o, p + 8 * k, vd + 128 * k, kIdescO, 1);
+                    }
+                    __syncwarp();
+                    if (!wait(&sh.p_full[st], steps)) return;
+                    ++steps;
+                    if (issuer) {
+#pragma unroll
+                        for (int k = kTile / 32; k < kTile / 16; ++k) umma_f16_ta(o, p + 8 * k, vd + 128 * k, kIdescO, 1);
+                        if (one || st == 1) tc_commit(&sh.empty[s]);
+                        if (j == (st ? n1 : n0) - 1) tc_commit(&sh.o_full[st]);
+                    }
+                    __syncwarp();
+                };
+                const std::integral_constant<int, 0> s0{};
+                const std::integral_constant<int, 1> s1{};
+                wait(&sh.q_full[0], uses0++);
+                if (ok && !one) wait(&sh.q_full[1], uses1++);
+                if (nt == 0 && ok && issuer) tc_commit(&sh.q_empty[0]);        // a cluster with fewer tiles than streams
+                if (ok && n0 > 0) scores(s0, 0);
+                if (ok && n1 > 0) scores(s1, 0);
+#pragma unroll 1
+                for (int j = 0; j < n0 && ok; ++j) {
+                    sums(s0, j, steps0);
+                    if (ok && j + 1 < n0) scores(s0, j + 1);
+                    if (!ok || j >= n1) continue;
+                    sums(s1, j, steps1);
+                    if (ok && j + 1 < n1) scores(s1, j + 1);
                 }
-                if (!ok) report_timeout(a.kv.status);
+                base += 2 * nt;
+                job_done(i);
             }
+            if (!ok && lane == 0) report_timeout(a.kv.status);
         } else if (warp == 2) {
-            // ---- queries
+            // ---- the plan, and queries
             if (lane == 0) {
-                tma_prefetch_desc(&q_map);
                 const int tokens = ManyRows::per_tile(a);
                 const uint32_t bytes = (uint32_t)(tokens * a.group * 128 * kSlabs);
-                int uses[2] = {0, 0}, last[2] = {-1, -1};
+                int uses0 = 0, uses1 = 0;
                 bool ok = true;
-                while (ok && plan.next(a, seg)) {
-                    const Work w(a, plan.c, seg);
-                    for (int st = 0; st < (w.one ? 1 : 2) && ok; ++st) {
-                        if (uses[st] > 0) ok = mbar_wait(&sh.q_empty[st], (uses[st] - 1) & 1, wl);
+#pragma unroll 1
+                for (int i = 0; ok; ++i) {
+                    if (i >= 2 && !mbar_wait(&sh.job_empty[i & 1], ((i >> 1) - 1) & 1, wl)) { ok = false; break; }
+                    Job &w = sh.job[i & 1];
+                    if (more) more = plan.next(a, w.seg);
+                    w.more = 0;
+                    if (more) {
+                        w.c = plan.c;
+                        w.set(a, rank);
+                    }
+                    mbar_arrive(&sh.job_full[i & 1]);
+                    if (!more) break;
+                    const int tiles = w.one ? 1 : 2, y = w.seg.head * a.group, z = plan.c.row0 + 2 * w.seg.rt * tokens;
+                    plan.advance(a);
+#pragma unroll 1
+                    for (int st = 0; st < tiles && ok; ++st) {
+                        int &uses = st ? uses1 : uses0;
+                        if (uses > 0) ok = mbar_wait(&sh.q_empty[st], (uses - 1) & 1, wl);
                         if (!ok) break;
                         mbar_arrive_expect_tx(&sh.q_full[st], bytes);
+#pragma unroll
                         for (int p = 0; p < kSlabs; ++p)
-                            tma_load_3d(q_s + st * kTileBytes + p * kSlabBytes, &q_map, p * 64, seg.head * a.group,
-                                        plan.c.row0 + (2 * seg.rt + st) * tokens, &sh.q_full[st]);
-                        last[st] = uses[st]++;
+                            tma_load_3d(q_s + st * kTileBytes + p * kSlabBytes, &q_map, p * 64, y, z + st * tokens, &sh.q_full[st]);
+                        ++uses;
                     }
-                    plan.advance(a);
                 }
                 if (!ok) report_timeout(a.kv.status);
-                for (int st = 0; st < 2; ++st)
-                    if (last[st] >= 0 && !mbar_wait(&sh.q_full[st], last[st] & 1, wl)) report_timeout(a.kv.status);
+                // no copy may be in flight when the CTA ends
+                if (uses0 > 0 && !mbar_wait(&sh.q_full[0], (uses0 - 1) & 1, wl)) report_timeout(a.kv.status);
+                if (uses1 > 0 && !mbar_wait(&sh.q_full[1], (uses1 - 1) & 1, wl)) report_timeout(a.kv.status);
             }
-        } else if (warp == 3) {
-            // ---- values nobody may see (16-bit cache; the conversion does it for codes)
+        } else {
+            // ---- values behind the end (16-bit cache; the conversion does it for codes)
             if constexpr (!Q8) {
-                constexpr uint32_t kInf = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
                 int base = 0;
                 bool ok = true;
-                while (ok && plan.next(a, seg)) {
-                    const Chunk c = plan.c;
-                    const Work w(a, c, seg);
-                    for (int x = 0, vj = 0; x < 2 * w.nt && ok; ++x) {
-                        const int i = base + x, s = i % kStages;
-                        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&sh.full[s], (i / kStages) & 1, wl));
+                for (int i = 0; ok; ++i) {
+                    if (!job_of(i)) { ok = false; break; }
+                    const Job &w = sh.job[i & 1];
+                    if (!w.more) break;
+                    if (w.ragged()) {
+                        const int x = base + w.v_place(w.nt - 1), s = x % kStages;
+                        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&sh.full[s], (x / kStages) & 1, wl));
                         if (!ok) break;
-                        if (x == w.v_place(vj)) {
-                            const int p0 = (w.t0 + vj) * kTile;
-                            ++vj;
-                            if (p0 + kTile > c.ctx) {
-                                const int end = min(max(c.total - p0, 0), kTile);             // rows in use
-                                uint4 *tile = reinterpret_cast<uint4 *>(stages + (size_t)s * kTileBytes);
-                                for (int y = lane; y < kSlabs * (kTile - end) * 8; y += 32) {
-                                    const int rows = kTile - end;
-                                    tile[(y / (rows * 8)) * (kTile * 8) + end * 8 + y % (rows * 8)] = make_uint4(0, 0, 0, 0);
-                                }
-                                const int from = max(c.ctx - p0, 0), n = max(end - from, 0);
-                                bool odd = false;
-#pragma unroll 4
-                                for (int y = lane; y < kSlabs * n * 8; y += 32) {
-                                    const uint4 v = tile[(y / (n * 8)) * (kTile * 8) + from * 8 + y % (n * 8)];
-                                    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+                        const int end = max(w.c.total - w.tile(w.nt - 1) * kTile, 0), rows = kTile - end;
+                        uint8_t *tile = stages + (size_t)s * kTileBytes + end * 128;
+#pragma unroll 1
+                        for (int y = lane; y < rows * 8; y += 32)
 #pragma unroll
-                                    for (int k = 0; k < 4; ++k) odd |= (u[k] & kInf) == kInf || (u[k] >> 16 & kInf) == kInf;
-                                }
-                                if (__any_sync(0xFFFFFFFFu, odd)) {
-                                    for (int y = lane; y < kSlabs * n * 8; y += 32) {
-                                        uint32_t *u = reinterpret_cast<uint32_t *>(&tile[(y / (n * 8)) * (kTile * 8) + from * 8 + y % (n * 8)]);
-                                        for (int k = 0; k < 4; ++k) {
-                                            if ((u[k] & kInf) == kInf) u[k] &= 0xFFFF0000u;
-                                            if ((u[k] >> 16 & kInf) == kInf) u[k] &= 0x0000FFFFu;
-                                        }
-                                    }
-                                    *reinterpret_cast<volatile int *>(&sh.bad) = 1;
-                                }
-                                fence_async_smem();
-                                __syncwarp();
-                            }
-                        }
-                        if (lane == 0) mbar_arrive(&sh.v_ok[s]);
+                            for (int p = 0; p < kSlabs; ++p) *reinterpret_cast<uint4 *>(tile + p * kSlabBytes + y * 16) = make_uint4(0, 0, 0, 0);
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sh.cleared[i & 1]);
                     }
                     base += 2 * w.nt;
-                    plan.advance(a);
+                    job_done(i);
                 }
                 if (!ok && lane == 0) report_timeout(a.kv.status);
             }
@@ -439,31 +668,28 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         const int row = tid & 127;                           // TMEM lane
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;    // (warp % 4) x 32 lanes, in the address's upper half
         const uint32_t ts = tmem + lanes + st * kTile, to = tmem + lanes + 256 + st * D;
-        const int per = ManyRows::per_tile(a);
-        const int heads = a.kv.heads * a.group;
+        const int row_tok = a.by_group.div(row);
         const float scale = a.scale_log2;
-        int steps = 0, items[2] = {0, 0};
+        int steps = 0, items0 = 0, items1 = 0, joins = 0;
         bool dead = false;
-        while (true) {
-            bar_sync(1, 256);                                // the last segment's readers are done (O, s_m, s_l too)
-            if (tid == 128) {
-                if (sh.more) sh.plan.advance(a);
-                sh.more = sh.plan.next(a, sh.seg);
+        for (int i = 0;; ++i) {
+            if (!bar_and(1, 256, job_of(i))) {               // all softmax warps go on, or none (they meet at barriers)
+                report_timeout(a.kv.status);
+                break;
             }
-            bar_sync(1, 256);
-            if (!sh.more) break;
-            const Work w(a, sh.plan.c, sh.seg);
-            const Segment &seg = sh.seg;
-            const Chunk &c = sh.plan.c;
-            const int first_tok = (2 * seg.rt + (w.one ? 0 : st)) * per;
-            const int tok = first_tok + row / a.group;       // of this row; may lie behind the chunk
-            const bool valid = row < per * a.group && tok < c.len;
+            const Job &w = sh.job[i & 1];
+            if (!w.more) break;
+            const Chunk &c = w.c;
+            const Segment &seg = w.seg;
+            const int n_mine = w.n[st];
+            const int first_tok = (2 * seg.rt + (w.one ? 0 : st)) * ManyRows::per_tile(a);
+            const int tok = first_tok + row_tok;              // of this row; may lie behind the chunk
             const int limit = a.mask ? c.total : min(c.total, c.ctx + min(tok, c.len - 1) + 1);
             const int all_seen = min(c.total, a.mask ? c.ctx : c.ctx + min(first_tok, c.len - 1) + 1);    // by every row
-            const uint32_t *mask = a.mask ? a.mask + (long long)(c.row0 + min(tok, c.len - 1)) * a.mask_words : nullptr;
             float m = -INFINITY, l = 0.f;
-            for (int j = 0; j < w.n[st]; ++j) {
-                const int p0 = (w.t0 + (w.one ? 2 * j + st : j)) * kTile;
+#pragma unroll 1
+            for (int j = 0; j < n_mine; ++j) {
+                const int p0 = w.tile(w.one ? 2 * j + st : j) * kTile;
                 if (!dead && !mbar_wait(&sh.s_full[st], steps & 1, wl)) {
                     report_timeout(a.kv.status);
                     dead = true;
@@ -472,32 +698,48 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 ++steps;
                 tc_fence_after();
                 float s[kTile];
+                uint32_t *su = reinterpret_cast<uint32_t *>(s);
+                const bool masked = p0 + kTile > all_seen;
+                tmem_ld32(ts, su);
+                tmem_ld32(ts + 32, su + 32);
+                tmem_ld_wait_for(su);
+                tmem_ld_wait_for(su + 32);
+                tmem_ld32(ts + 64, su + 64);
+                tmem_ld32(ts + 96, su + 96);
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int k = 0; k < kTile; k += 32) tmem_ld32(ts + k, reinterpret_cast<uint32_t *>(s) + k);
-                tmem_ld_wait();
-                if (p0 + kTile > all_seen) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int p = p0 + 32 * k;
-                        const int n = min(max(limit - p, 0), 32);
-                        uint32_t see = n == 32 ? 0xFFFFFFFFu : (1u << n) - 1u;
-                        if (a.mask && p + 32 > c.ctx) {
-                            const int j0 = p - c.ctx;         // place in the chunk of bit 0; context below 0
-                            const int w0 = j0 >> 5;           // floor
-                            const uint32_t lo = w0 >= 0 && w0 < a.mask_words ? mask[w0] : w0 < 0 ? 0xFFFFFFFFu : 0u;
-                            const uint32_t hi = w0 + 1 >= 0 && w0 + 1 < a.mask_words ? mask[w0 + 1] : 0u;
-                            see &= __funnelshift_r(lo, hi, j0 & 31);
-                        }
-#pragma unroll
-                        for (int x = 0; x < 32; ++x)
-                            if (!(see >> x & 1)) s[32 * k + x] = -INFINITY;
+                for (int h = 0; h < 2; ++h) {
+                    if (h == 1) {
+                        tmem_ld_wait_for(su + 64);
+                        tmem_ld_wait_for(su + 96);
                     }
-                }
-                float mx = s[0];
+                    if (masked) {
 #pragma unroll
-                for (int k = 1; k < kTile; ++k) mx = fmaxf(mx, s[k]);
-                if (__any_sync(0xFFFFFFFFu, (mx - m) * scale > kSlack)) {     // -inf - -inf is NaN: no
-                    const float mn = fmaxf(m, mx);
+                        for (int k = 2 * h; k < 2 * h + 2; ++k) {
+                            const int p = p0 + 32 * k;
+                            const int n = min(max(limit - p, 0), 32);
+                            uint32_t see = n == 32 ? 0xFFFFFFFFu : (1u << n) - 1u;
+                            if (a.mask && p + 32 > c.ctx) {
+                                const uint32_t *mask = a.mask + (long long)(c.row0 + min(tok, c.len - 1)) * a.mask_words;
+                                const int j0 = p - c.ctx;         // place in the chunk of bit 0; context below 0
+                                const int w0 = j0 >> 5;           // floor; -1 at the least
+                                const uint32_t lo = w0 < 0 ? 0xFFFFFFFFu : w0 < a.mask_words ? mask[w0] : 0u;
+                                const uint32_t hi = w0 + 1 < a.mask_words ? mask[w0 + 1] : 0u;
+                                see &= __funnelshift_r(lo, hi, j0 & 31);
+                            }
+#pragma unroll
+                            for (int x = 0; x < 32; ++x)
+                                if (!(see >> x & 1)) s[32 * k + x] = -INFINITY;
+                        }
+                    }
+#pragma unroll
+                    for (int k = 64 * h; k < 64 * h + 64; k += 8)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) mx[x] = fmaxf(fmaxf(mx[x], s[k + 2 * x]), s[k + 2 * x + 1]);
+                }
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                if (__any_sync(0xFFFFFFFFu, (top - m) * scale > kSlack)) {     // -inf - -inf is NaN: no
+                    const float mn = fmaxf(m, top);
                     if (j > 0) {
                         const float f = mn > -INFINITY ? ex2((m - mn) * scale) : 1.f;
                         l *= f;
@@ -514,43 +756,82 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     m = mn;
                 }
                 const float base = m > -INFINITY ? m * scale : 0.f;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c0 = 0; c0 < kTile; c0 += 32) {       // in pieces, so that scores leave the registers as weights come
+                const uint64_t scale2 = pair(scale, scale), base2 = pair(-base, -base);
+                uint64_t sum0 = 0, sum1 = 0;
+                // weights of 32 scores at a time, packed and stored over scores that have been read
+                auto weights = [&](int c0, bool fma) {
                     uint32_t p[16];
 #pragma unroll
                     for (int k = 0; k < 32; k += 2) {
-                        const float x = ex2(fmaf(s[c0 + k], scale, -base)), y = ex2(fmaf(s[c0 + k + 1], scale, -base));
-                        sum[k / 2 % 2 * 2] += x;
-                        sum[k / 2 % 2 * 2 + 1] += y;
-                        p[k / 2] = pack2<T>(x, y);
+                        uint64_t x = fma2(pair(s[c0 + k], s[c0 + k + 1]), scale2, base2);
+                        float lo, hi;
+                        if (fma && (k & 6) == 6) {
+                            x = ex2_fma(x);
+                            unpair(x, lo, hi);
+                        } else {
+                            unpair(x, lo, hi);
+                            lo = ex2(lo);
+                            hi = ex2(hi);
+                            x = pair(lo, hi);
+                        }
+                        if (k & 2) sum1 = add2(sum1, x);
+                        else sum0 = add2(sum0, x);
+                        p[k / 2] = pack2<T>(lo, hi);
                     }
                     tmem_st16(ts + c0 / 2, p);
+                };
+                auto stored = [&](uint64_t *bar) {
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar);
+                };
+                if (masked) {                                 // -infinity has to give 0 exactly
+                    weights(0, false);
+                    weights(32, false);
+                    stored(&sh.p_half[st]);
+                    weights(64, false);
+                    weights(96, false);
+                } else {
+                    weights(0, true);
+                    weights(32, true);
+                    stored(&sh.p_half[st]);
+                    weights(64, true);
+                    weights(96, true);
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.p_full[st]);
+                float a0, a1;
+                unpair(add2(sum0, sum1), a0, a1);
+                l += a0 + a1;
+                stored(&sh.p_full[st]);
             }
             // ---- the segment's result
+            const bool valid = row < ManyRows::per_tile(a) * a.group && tok < c.len;
+            const int heads = a.kv.heads * a.group;
             s_m[st * kTile + row] = m;
             s_l[st * kTile + row] = l;
-            for (int x = 0; x < 2; ++x)
-                if (w.n[x] > 0) {
-                    if ((w.one || x == st) && !dead && !mbar_wait(&sh.o_full[x], items[x] & 1, wl)) {
-                        report_timeout(a.kv.status);
-                        dead = true;
-                    }
-                    ++items[x];
+            if (w.n[0] > 0) {
+                if ((w.one || st == 0) && !dead && !mbar_wait(&sh.o_full[0], items0 & 1, wl)) {
+                    report_timeout(a.kv.status);
+                    dead = true;
                 }
+                ++items0;
+            }
+            if (w.n[1] > 0) {
+                if ((w.one || st == 1) && !dead && !mbar_wait(&sh.o_full[1], items1 & 1, wl)) {
+                    report_timeout(a.kv.status);
+                    dead = true;
+                }
+                ++items1;
+            }
             dead = __any_sync(0xFFFFFFFFu, dead);
             tc_fence_after();
             bar_sync(1, 256);
-            // rows and elements of this thread: two row tiles: row 128 st + row, all elements; one: row `row`, half of them,
-            // from both streams
-            const int d0 = w.one ? st * (D / 2) : 0, d1 = w.one ? d0 + D / 2 : D;
+            // A thread has a row and some OCTETS of its elements, o0, o0 + o_step, ...: with two row tiles its stream's row and
+            // all octets; with one, half of the octets from both streams, or in a cluster its CTA's share of them.
+            const bool joined = w.one && a.ctas > 1;
             const int prow = w.one ? row : st * kTile + row;
+            const int o0 = joined ? 2 * rank + st : w.one ? st * (D / 16) : 0;
+            const int o_step = joined ? 2 * a.ctas : 1, o_end = w.one && !joined ? o0 + D / 16 : D / 8;
             float f0 = 1.f, f1 = 0.f;
             if (w.one) {
                 const float ma = s_m[row], mb = s_m[kTile + row];
@@ -560,19 +841,25 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 l = f0 * s_l[row] + f1 * s_l[kTile + row];
             }
             const bool split = seg.c0 != seg.c1;
-            const long long at = (long long)(c.row0 + tok) * heads + seg.head * a.group + row % a.group;
-            bool bad = *reinterpret_cast<volatile int *>(&sh.bad) != 0;
-            auto put = [&](int d, const float *x, float inv) {       // 32 elements of the result
-                if (!valid) return;
-                uint4 *dst = reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + at * D + d);
-#pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    dst[v] = make_uint4(pack2<T>(x[8 * v] * inv, x[8 * v + 1] * inv), pack2<T>(x[8 * v + 2] * inv, x[8 * v + 3] * inv),
-                                        pack2<T>(x[8 * v + 4] * inv, x[8 * v + 5] * inv), pack2<T>(x[8 * v + 6] * inv, x[8 * v + 7] * inv));
-            };
-            float *slots = a.part;
-            float *part = slots + ((size_t)blockIdx.x * 2 + seg.slot) * part_floats(D);
+            const long long at = (long long)(c.row0 + tok) * heads + seg.head * a.group + row - row_tok * a.group;
+            const bool own = (w.tile(max(w.nt - 1, 0)) + 1) * kTile > c.ctx;      // the chunk's own tokens are among the positions
+            float *part = a.part + ((size_t)blockIdx.x * 2 + seg.slot) * part_floats(D);
             float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;       // a NaN sum stays one
+            auto put = [&](int o, const float *x) {            // an octet of the result
+                if (valid)
+                    reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + at * D)[o] =
+                        make_uint4(pack2<T>(x[0] * inv, x[1] * inv), pack2<T>(x[2] * inv, x[3] * inv), pack2<T>(x[4] * inv, x[5] * inv),
+                                   pack2<T>(x[6] * inv, x[7] * inv));
+            };
+            auto put_part = [&](int o, const float *x) {
+                if (!valid) return;
+                float4 *dst = reinterpret_cast<float4 *>(part) + (size_t)(2 * o) * kPartRows + prow;
+                __stcg(dst, make_float4(x[0], x[1], x[2], x[3]));
+                __stcg(dst + kPartRows, make_float4(x[4], x[5], x[6], x[7]));
+            };
+            // sums of this CTA: 32 elements at a time from TMEM to the result, the part, or (cluster) shared memory
+            float4 *sums = reinterpret_cast<float4 *>(q_s);    // [D / 4][128 rows], where the queries were
+            const int d0 = w.one ? st * (D / 2) : 0, d1 = w.one ? d0 + D / 2 : D;
 #pragma unroll 1
             for (int d = d0; d < d1; d += 32) {
                 uint32_t r[32];
@@ -581,64 +868,150 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 tmem_ld_wait();
 #pragma unroll
                 for (int k = 0; k < 32; ++k) x[k] = __uint_as_float(r[k]);
+                auto check = [&](int of, float *x) {           // sums of stream `of`
+                    if constexpr (!Q8) {
+                        float odd = 0.f;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) odd = fmaf(x[k], 0.f, odd);
+                        if (own && valid && odd != 0.f) {      // NaN
+                            float y[32];
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) y[k] = x[k];
+                            repair<T, D>(a, w, of, row, tok, s_m[of * kTile + row], d, y);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) x[k] = y[k];
+                        }
+                    }
+                };
+                if (w.n[w.one ? 0 : st] > 0) check(w.one ? 0 : st, x);
                 if (w.one) {
 #pragma unroll
                     for (int k = 0; k < 32; ++k) x[k] = f0 > 0.f || f0 != f0 ? f0 * x[k] : 0.f;
                     if (w.n[1] > 0) {
                         tmem_ld32(tmem + lanes + 256 + D + d, r);
                         tmem_ld_wait();
+                        float z[32];
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) x[k] += f1 > 0.f || f1 != f1 ? f1 * __uint_as_float(r[k]) : 0.f;
+                        for (int k = 0; k < 32; ++k) z[k] = __uint_as_float(r[k]);
+                        check(1, z);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) x[k] += f1 > 0.f || f1 != f1 ? f1 * z[k] : 0.f;
                     }
                 }
-                if (!split) put(d, x, inv);
-                else if (valid) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        __stcg(reinterpret_cast<float4 *>(part) + (size_t)(d / 4 + k) * kPartRows + prow,
-                               make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]));
+                for (int k = 0; k < 4; ++k) {
+                    if (joined) {
+                        sums[(d / 4 + 2 * k) * kTile + row] = make_float4(x[8 * k], x[8 * k + 1], x[8 * k + 2], x[8 * k + 3]);
+                        sums[(d / 4 + 2 * k + 1) * kTile + row] = make_float4(x[8 * k + 4], x[8 * k + 5], x[8 * k + 6], x[8 * k + 7]);
+                    } else if (split) {
+                        put_part(d / 8 + k, x + 8 * k);
+                    } else {
+                        put(d / 8 + k, x + 8 * k);
+                    }
                 }
             }
+            if (joined) {
+                bar_sync(1, 256);
+                if (tid - 128 < a.ctas) mbar_arrive_cluster(mapa_rank(smem_u32(&sh.ready), tid - 128));
+                if (!dead && !mbar_wait_cluster(&sh.ready, joins & 1, wl)) {
+                    report_timeout(a.kv.status);
+                    dead = true;
+                }
+                // all loads of a kind before the first use: a remote load takes long, many take little longer
+                float ma[kMaxCluster], mb[kMaxCluster], f[kMaxCluster], g[kMaxCluster];
+#pragma unroll
+                for (int x = 0; x < kMaxCluster; ++x) {
+                    ma[x] = mb[x] = -INFINITY;
+                    f[x] = g[x] = 0.f;
+                    if (x < a.ctas) {
+                        ma[x] = ld_cluster(s_m + row, x);
+                        mb[x] = ld_cluster(s_m + kTile + row, x);
+                        f[x] = ld_cluster(s_l + row, x);
+                        g[x] = ld_cluster(s_l + kTile + row, x);
+                    }
+                }
+                m = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < kMaxCluster; ++x) m = fmaxf(m, fmaxf(ma[x], mb[x]));
+                l = 0.f;
+#pragma unroll
+                for (int x = 0; x < kMaxCluster; ++x) {
+                    const bool any = x < a.ctas && m > -INFINITY;
+                    if (any) l += ex2((ma[x] - m) * scale) * f[x] + ex2((mb[x] - m) * scale) * g[x];
+                    f[x] = any ? ex2((fmaxf(ma[x], mb[x]) - m) * scale) : 0.f;
+                }
+                inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+#pragma unroll 1
+                for (int o = o0; o < o_end; o += o_step) {
+                    float4 y[kMaxCluster], z[kMaxCluster];
+#pragma unroll
+                    for (int x = 0; x < kMaxCluster; ++x)
+                        if (x < a.ctas) {
+                            y[x] = ld_cluster(sums + 2 * o * kTile + row, x);
+                            z[x] = ld_cluster(sums + (2 * o + 1) * kTile + row, x);
+                        }
+                    float x8[8] = {};
+#pragma unroll
+                    for (int x = 0; x < kMaxCluster; ++x)
+                        if (x < a.ctas && (f[x] > 0.f || f[x] != f[x])) {
+                            x8[0] += f[x] * y[x].x, x8[1] += f[x] * y[x].y, x8[2] += f[x] * y[x].z, x8[3] += f[x] * y[x].w;
+                            x8[4] += f[x] * z[x].x, x8[5] += f[x] * z[x].y, x8[6] += f[x] * z[x].z, x8[7] += f[x] * z[x].w;
+                        }
+                    if (split) put_part(o, x8);
+                    else put(o, x8);
+                }
+                fence_async_smem();                           // the next queries come to the same place
+                bar_sync(1, 256);
+                if (tid - 128 < a.ctas) mbar_arrive_cluster(mapa_rank(smem_u32(&sh.taken), tid - 128));
+                if (!dead && !mbar_wait_cluster(&sh.taken, joins & 1, wl)) {
+                    report_timeout(a.kv.status);
+                    dead = true;
+                }
+                dead = __any_sync(0xFFFFFFFFu, dead);
+                ++joins;
+            }
+            if (a.ctas > 1 && tid == 128) mbar_arrive(&sh.q_empty[0]);
             bool done = !split;
             if (split) {
-                if (d0 == 0) {
+                if (o0 == (joined ? 2 * rank : 0)) {
                     __stcg(part + kPartRows * D + prow, m);
                     __stcg(part + kPartRows * (D + 1) + prow, l);
                 }
-                if (tid == 128) __stcg(part + kPartRows * (D + 2), bad ? 1.f : 0.f);
                 __threadfence();
                 bar_sync(1, 256);
-                if (tid == 128) sh.ticket = atomicAdd(a.tickets + seg.c0, 1u);
+                // CTAs of the same rank join the same octets
+                if (tid == 128) sh.ticket = atomicAdd(a.tickets + seg.c0 * a.ctas + rank, 1u);
                 bar_sync(1, 256);
                 done = *reinterpret_cast<volatile unsigned *>(&sh.ticket) == (unsigned)(seg.c1 - seg.c0);
-                if (done) {                                       // the last of the item's CTAs: join the parts in order
+                if (done) {                                       // the last of the item's workers: join the parts in order
                     __threadfence();
-                    if (tid == 128) a.tickets[seg.c0] = 0;
+                    if (tid == 128) a.tickets[seg.c0 * a.ctas + rank] = 0;
+                    auto part_of = [&](int i) {
+                        return a.part + ((size_t)(i * a.ctas + rank) * 2 + (i == seg.c0 ? seg.slot0 : 0)) * part_floats(D);
+                    };
                     m = -INFINITY;
-                    for (int i = seg.c0; i <= seg.c1; ++i) {
-                        const float *ps = slots + ((size_t)i * 2 + (i == seg.c0 ? seg.slot0 : 0)) * part_floats(D);
-                        m = fmaxf(m, __ldcg(ps + kPartRows * D + prow));
-                        bad |= __ldcg(ps + kPartRows * (D + 2)) != 0.f;
-                    }
+                    for (int i = seg.c0; i <= seg.c1; ++i) m = fmaxf(m, __ldcg(part_of(i) + kPartRows * D + prow));
                     l = 0.f;
                     for (int i = seg.c0; i <= seg.c1; ++i) {
-                        const float *ps = slots + ((size_t)i * 2 + (i == seg.c0 ? seg.slot0 : 0)) * part_floats(D);
+                        const float *ps = part_of(i);
                         const float f = m > -INFINITY ? ex2((__ldcg(ps + kPartRows * D + prow) - m) * scale) : 0.f;
                         l += f * __ldcg(ps + kPartRows * (D + 1) + prow);
                     }
                     inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
 #pragma unroll 1
-                    for (int d = d0; d < d1; d += 32) {
-                        float x[32];
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) x[k] = 0.f;
+                    for (int o = o0; o < o_end; o += 4 * o_step) {           // four octets at a time
+                        float x[32] = {};
+#pragma unroll 2
                         for (int i = seg.c0; i <= seg.c1; ++i) {
-                            const float *ps = slots + ((size_t)i * 2 + (i == seg.c0 ? seg.slot0 : 0)) * part_floats(D);
+                            const float *ps = part_of(i);
                             const float f = m > -INFINITY ? ex2((__ldcg(ps + kPartRows * D + prow) - m) * scale) : 0.f;
                             float4 y[8];
 #pragma unroll
-                            for (int k = 0; k < 8; ++k)
-                                y[k] = valid ? __ldcg(reinterpret_cast<const float4 *>(ps) + (size_t)(d / 4 + k) * kPartRows + prow) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            for (int k = 0; k < 8; ++k) {
+                                const int oo = o + (k >> 1) * o_step;
+                                y[k] = valid && oo < o_end ? __ldcg(reinterpret_cast<const float4 *>(ps) + (size_t)(2 * oo + (k & 1)) * kPartRows + prow)
+                                                           : make_float4(0.f, 0.f, 0.f, 0.f);
+                            }
                             if (f > 0.f || f != f) {
 #pragma unroll
                                 for (int k = 0; k < 8; ++k) {
@@ -649,28 +1022,16 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                                 }
                             }
                         }
-                        put(d, x, inv);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (o + k * o_step < o_end) put(o + k * o_step, x + 8 * k);
                     }
                 }
             }
-            if (done && valid) {
-                if (a.lse && d0 == 0) a.lse[at] = (m > -INFINITY ? m * scale + log2f(l) : -INFINITY) * 0.69314718055994531f;
-                if constexpr (!Q8) {
-                    if (bad)
-                        for (int t = 0; t < c.len; ++t) {
-                            if (!sees(a, c, tok, t)) continue;
-                            const int p = c.ctx + t;
-                            int page = a.kv.table[(long long)seg.b * a.kv.width + (p >> a.kv.page_shift)];
-                            if (page < 0 || page >= a.kv.num_pages) continue;
-                            const T *v = static_cast<const T *>(a.kv.v) + kv_row(a.kv, a.kv.layer, page, seg.head, p & ((1 << a.kv.page_shift) - 1)) * D;
-                            for (int d = d0; d < d1; ++d) {
-                                const float x = unpack2<T>(*reinterpret_cast<const uint16_t *>(v + d)).x;
-                                if (!isfinite(x)) reinterpret_cast<uint16_t *>(a.out)[at * D + d] = 0x7FFF;     // NaN in both types
-                            }
-                        }
-                }
-            }
+            if (done && valid && a.lse && o0 == 0) a.lse[at] = (m > -INFINITY ? m * scale + log2f(l) : -INFINITY) * 0.69314718055994531f;
             tc_fence_before();
+            bar_sync(1, 256);                                // all have read O, s_m and s_l
+            job_done(i);
         }
     } else {
         // ---- 8-bit tiles -> 16-bit tiles (128 threads)
@@ -678,29 +1039,19 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             set_registers<false, 64>();
             constexpr int kPieces = D / 16;                  // 16-byte pieces of a position
             const int t = tid & 127;
-            int i = 0;                                       // tiles done
+            int done = 0;                                    // tiles
             bool ok = true;
-            while (ok && plan.next(a, seg)) {
-                const Chunk c = plan.c;
-                const Work w(a, c, seg);
-                for (int x = 0, kj = 0, vj = 0; x < 2 * w.nt && ok; ++x, ++i) {
+            for (int i = 0; ok; ++i) {
+                if (!job_of(i)) { ok = false; break; }
+                const Job &w = sh.job[i & 1];
+                if (!w.more) break;
+                const Chunk c = w.c;
+                for (int x = 0, kj = 0, vj = 0; x < 2 * w.nt && ok; ++x, ++done) {
                     const bool is_v = x == w.v_place(vj);
-                    const int p0 = (w.t0 + (is_v ? vj++ : kj++)) * kTile;
-                    // exponents of the positions this thread converts: t / kPieces + n x 128 / kPieces
-                    int eb[kPieces];
-#pragma unroll
-                    for (int n = 0; n < kPieces; ++n) {
-                        const int p = p0 + t / kPieces + n * (kTile / kPieces);
-                        eb[n] = -1;
-                        if (p < c.total) {
-                            const int page = __ldg(a.kv.table + (long long)seg.b * a.kv.width + (p >> a.kv.page_shift));
-                            if (page >= 0 && page < a.kv.num_pages)
-                                eb[n] = (is_v ? a.kv.v_exps : a.kv.k_exps)[kv_row(a.kv, a.kv.layer, page, seg.head, p & ((1 << a.kv.page_shift) - 1))];
-                        }
-                    }
-                    const int rs = i % Geo::kRaw, s = i % kStages;
-                    bool got = mbar_wait(&sh.raw_full[rs], (i / Geo::kRaw) & 1, wl);
-                    if (i >= kStages) got = got && mbar_wait(&sh.empty[s], ((i / kStages) - 1) & 1, wl);
+                    const int p0 = w.tile(is_v ? vj++ : kj++) * kTile;
+                    const int rs = done % Geo::kRaw, s = done % kStages;
+                    bool got = mbar_wait(&sh.raw_full[rs], (done / Geo::kRaw) & 1, wl);
+                    if (done >= kStages) got = got && mbar_wait(&sh.empty[s], ((done / kStages) - 1) & 1, wl);
                     ok = __all_sync(0xFFFFFFFFu, got);
                     if (!ok) break;
                     const uint8_t *raw = raws + (size_t)rs * Geo::kRawBytes;
@@ -711,10 +1062,10 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         const int pos = t / kPieces + n * (kTile / kPieces), piece = t % kPieces;
                         const uint4 r = *reinterpret_cast<const uint4 *>(raw + pos * D + piece * 16);
                         uint32_t u[4] = {r.x, r.y, r.z, r.w};
-                        const int e = max(eb[n], 0);
+                        const int e = sh.exps[rs][pos];
                         if (!clean) {                          // unused places and the code of NaN count as 0
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) u[k] = eb[n] < 0 ? 0u : u[k] & ~__vcmpeq4(u[k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                            for (int k = 0; k < 4; ++k) u[k] = p0 + pos >= c.total ? 0u : u[k] & ~__vcmpeq4(u[k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
                         }
                         const uint32_t sc = scale_bits<T>(e) * 0x10001u;
                         uint32_t o[8];
@@ -747,13 +1098,15 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         mbar_arrive(&sh.raw_empty[rs]);
                     }
                 }
-                plan.advance(a);
+                job_done(i);
             }
             if (!ok && lane == 0) report_timeout(a.kv.status);
         }
     }
     tc_fence_before();
-    __syncthreads();
+    __syncwarp();
+    if (a.ctas > 1) cluster_sync_all();                     // nobody leaves while a neighbour may read its shared memory
+    else __syncthreads();
     if (warp == 3) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
@@ -767,8 +1120,32 @@ cudaError_t launch(const CUtensorMap &q_map, const CUtensorMap &k_map, const CUt
     static_assert(Geometry<Q8, D>::kBig + Geometry<Q8, D>::kSmall <= kSmemBytes, "shared memory");
     const cudaError_t e = cudaFuncSetAttribute(attend_umma_kernel<T, Q8, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
     if (e != cudaSuccess) return e;
-    attend_umma_kernel<T, Q8, D><<<sms, Geometry<Q8, D>::kThreads, kSmemBytes, stream>>>(q_map, k_map, v_map, a);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = a.ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(sms / a.ctas * a.ctas);
+    cfg.blockDim = dim3(Geometry<Q8, D>::kThreads);
+    cfg.dynamicSmemBytes = kSmemBytes;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.ctas > 1 ? 2 : 1;
+    if (a.ctas > 1) {
+        // how many clusters the device holds at once (its SMs come in groups, which a cluster does not cross); the
+        // same on every device of this build
+        static int held[kMaxCluster + 1] = {};
+        if (held[a.ctas] == 0) {
+            int n = 0;
+            const cudaError_t eo = cudaOccupancyMaxActiveClusters(&n, attend_umma_kernel<T, Q8, D>, &cfg);
+            if (eo != cudaSuccess) return eo;
+            held[a.ctas] = n > 0 ? n : 1;
+        }
+        if ((int)cfg.gridDim.x > held[a.ctas] * a.ctas) cfg.gridDim.x = held[a.ctas] * a.ctas;
+    }
+    return cudaLaunchKernelEx(&cfg, attend_umma_kernel<T, Q8, D>, q_map, k_map, v_map, a);
 }
 
 }  // namespace
@@ -776,8 +1153,17 @@ cudaError_t launch(const CUtensorMap &q_map, const CUtensorMap &k_map, const CUt
 size_t attend_umma_part_floats(int sms, int d) { return (size_t)sms * 2 * part_floats(d); }
 
 cudaError_t launch_attend_umma(const CUtensorMap &q_map, const CUtensorMap &k_map, const CUtensorMap &v_map,
-                               const AttendArgs &a, int sms, cudaStream_t stream)
+                               const AttendArgs &args, int sms, cudaStream_t stream)
 {
+    AttendArgs a = args;
+    // One row tile per sequence and head, and fewer of them than half the SMs: clusters share them.  No more CTAs than give
+    // every stream a tile of the longest sequence that the table can hold.
+    const long long items = (long long)a.kv.B * a.kv.heads, tiles = (((long long)a.kv.width << a.kv.page_shift) + kTile - 1) / kTile;
+    long long ctas = a.max_chunk <= kTile / a.group ? sms / items : 1;
+    if (ctas > (tiles + 1) / 2) ctas = (tiles + 1) / 2;
+    a.ctas = (int)(ctas < 1 ? 1 : ctas > kMaxCluster ? kMaxCluster : ctas);
+    a.by_rows = FastDiv(2 * (kTile / a.group));
+    a.by_unit = FastDiv(2 * a.ctas);
     const bool q8 = a.kv.k_exps != nullptr;
     if (a.kv.dtype == kF16) {
         if (a.kv.d == 64) return q8 ? launch<__half, true, 64>(q_map, k_map, v_map, a, sms, stream) : launch<__half, false, 64>(q_map, k_map, v_map, a, sms, stream);

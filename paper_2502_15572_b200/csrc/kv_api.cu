@@ -116,8 +116,8 @@ dresd_status check_call(dresd_kv *kv, int layer, const dresd_kv_batch *b, bool w
     if (b->B < 0) return fail(DRESD_ERR_INVALID, "B = %d is negative", b->B);
     if (b->B > kMaxKvBatch) return fail(DRESD_ERR_UNSUPPORTED, "B = %d exceeds %d", b->B, kMaxKvBatch);
     if (b->table_width < 1) return fail(DRESD_ERR_INVALID, "table_width = %d must be positive", b->table_width);
-    if (((long long)b->table_width << kv->args.page_shift) > 2147483647LL)
-        return fail(DRESD_ERR_UNSUPPORTED, "table_width = %d reaches beyond 2^31 - 1 positions", b->table_width);
+    if (((long long)b->table_width << kv->args.page_shift) > 2147483647LL - 4096)
+        return fail(DRESD_ERR_UNSUPPORTED, "table_width = %d reaches beyond 2^31 - 4097 positions", b->table_width);
     if (whole && (b->rows < 0 || b->max_chunk < 0 || b->max_chunk > b->rows))
         return fail(DRESD_ERR_INVALID, "rows = %d / max_chunk = %d", b->rows, b->max_chunk);
     *out = kv->args;
@@ -168,6 +168,7 @@ dresd_status dresd_kv_create(void *k_pages, void *v_pages, uint8_t *k_exps, uint
     if (num_pages > 2147483647LL / page_size / kv_heads / layers)
         return fail(DRESD_ERR_UNSUPPORTED, "the cache has more than 2^31 - 1 rows");
     if (!aligned16(k_pages) || !aligned16(v_pages)) return fail(DRESD_ERR_INVALID, "pages not 16-byte aligned");
+    if (k_exps && (!aligned16(k_exps) || !aligned16(v_exps))) return fail(DRESD_ERR_INVALID, "exponents not 16-byte aligned");
     if (!is_device_ptr(k_pages) || !is_device_ptr(v_pages) || (k_exps && (!is_device_ptr(k_exps) || !is_device_ptr(v_exps))))
         return fail(DRESD_ERR_INVALID, "k_pages/v_pages/k_exps/v_exps must be device pointers");
     dresd_kv *kv = new (std::nothrow) dresd_kv();
@@ -280,6 +281,7 @@ dresd_status dresd_kv_attend(dresd_kv *kv, int layer, const dresd_kv_batch *batc
     a.q_row = q_row;
     a.q_head = q_head;
     a.group = heads / a.kv.heads;
+    a.by_group = FastDiv(a.group);
     a.scale_log2 = scale * 1.4426950408889634f;
     a.mask = mask;
     a.mask_words = mask_words;
@@ -287,14 +289,14 @@ dresd_status dresd_kv_attend(dresd_kv *kv, int layer, const dresd_kv_batch *batc
     a.lse = out_lse;
     a.part = kv->part;
     a.tickets = kv->tickets;
-    a.max_rows = (batch->max_chunk > 0 ? batch->max_chunk : batch->rows) * a.group;
+    a.max_chunk = batch->max_chunk > 0 ? batch->max_chunk : batch->rows;
     a.wait_cycles = (long long)kv->opt_wait_ms * 2000000LL;        // ~2 GHz
     a.lose_stage = kv->opt_lose_stage;
     kv->last_stream = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     // Up to 16 rows per key/value head the registers of mma.sync hold them.  The other kernel masks before it scales, which
     // needs a positive scale.
-    const bool many = kv->opt_path == 0 ? a.max_rows > 16 : kv->opt_path == 2;
+    const bool many = kv->opt_path == 0 ? (long long)a.max_chunk * a.group > 16 : kv->opt_path == 2;
     if (many && scale > 0.f) {
         CUtensorMap q_map;
         const cuuint64_t dims[3] = {(cuuint64_t)a.kv.d, (cuuint64_t)heads, (cuuint64_t)a.kv.rows};
@@ -321,6 +323,8 @@ dresd_status dresd_kv_keep_draft(dresd_kv *kv, const dresd_kv_batch *batch, cons
     if (n < 1 || L < 1) return fail(DRESD_ERR_INVALID, "bad n/L");
     if (n > DRESD_MAX_TOP_N) return fail(DRESD_ERR_UNSUPPORTED, "n = %d exceeds DRESD_MAX_TOP_N", n);
     if (L > 65536) return fail(DRESD_ERR_UNSUPPORTED, "L = %d exceeds 65536", L);
+    if ((long long)L * a.heads * a.layers * a.d / 8 > 2147483647LL)
+        return fail(DRESD_ERR_UNSUPPORTED, "L = %d drafts' rows of %d layers exceed 2^31 - 1 pieces", L, a.layers);
     kv->last_launches = 0;
     if (a.B == 0) return DRESD_OK;
     if (!is_device_ptr(best) || !is_device_ptr(length)) return fail(DRESD_ERR_INVALID, "best/length must be device pointers");
