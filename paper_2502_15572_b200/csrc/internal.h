@@ -222,7 +222,7 @@ struct AttendArgs {
     void *out;                  // [rows][heads * group][d]
     float *lse;                 // [rows][heads * group] or null
     float *part;                // partial results: see kv_plan.cuh
-    unsigned int *tickets;      // one per CTA, all zero between calls
+    unsigned int *tickets;      // one per SM, all zero between calls
     int max_chunk;              // the longest chunk (only the choice of kernel depends on it)
     FastDiv by_group;           // group
     FastDiv by_rows;            // rows (few rows) or tokens (many) of a row tile
@@ -231,10 +231,10 @@ struct AttendArgs {
     long long wait_cycles;      // bound of every device-side wait in cycles, 0 = default
     int lose_stage;             // test hook: CTA 0 never receives tile (value - 1); 0 = off
 };
-// Few rows per key/value head (at most 16) or a scale that is not positive: mma.sync, straight from registers.
-int attend_mma_max_ctas(int sms);                         // tickets
+// Few rows per key/value head (at most 16) or a scale that is not positive: mma.sync.
+// Tensor maps over the cache's rows: boxes of 16 rows x 64 elements (8-bit: x d bytes), swizzled.
 size_t attend_mma_part_floats(int sms, int d);            // floats of `part`
-cudaError_t launch_attend_mma(const AttendArgs &a, int sms, cudaStream_t stream);
+cudaError_t launch_attend_mma(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttendArgs &a, int sms, cudaStream_t stream);
 // More rows: tcgen05.  Tensor maps: k, v over the cache's rows [layers x pages x heads x page][d] (boxes of 64 elements
 // x page rows; 8-bit: d bytes x page rows), q over [rows][heads][d] (boxes of 64 elements x group x 128 / group).
 size_t attend_umma_part_floats(int sms, int d);

@@ -3,14 +3,15 @@
 //     s_rj = scale q_r . k_j,   out_r = sum_j 2^(s_rj - m_r) v_j / sum_j 2^(s_rj - m_r)      (scale holds log2 e)
 //
 // in one pass over the cache with the running maximum m, weight sum l and weighted sum o of every row.  Every
-// key and value is read once and meets a handful of rows, so the bound is HBM and the aim is many loads in flight
-// with nothing between them and the arithmetic: a warp takes 16 positions at a time STRAIGHT INTO REGISTERS in the
-// fragment layout of mma.sync m16n8k16 -- no shared memory, no barrier, no transposition:
+// key and value is read once and meets a handful of rows, so the bound is HBM: what counts is many bytes in flight with
+// nothing between them and the arithmetic.  Each warp has a ring of tiles of 16 positions of its own, filled by TMA and
+// emptied by itself: it needs no barrier with other warps, and a tile is asked for again as soon as its last word is in
+// registers.  Tiles of the next segment follow those of the present one without a gap.
 //
-//   S^T = K Q^T   keys as the M = 16 operand, rows as N = 8.  The k index of the instruction may run over the
-//                 elements of a row in any order that keys and queries share; it is laid out so that a lane's
+//   S^T = K Q^T   mma.sync m16n8k16 with keys as the M = 16 operand and rows as N = 8.  The k index of the instruction may
+//                 run over the elements of a row in any order that keys and queries share; it is laid out so that a lane's
 //                 fragments are whole 16-byte pieces of a key.
-//   O^T = V^T P^T elements as M, rows as N, positions as K.  A lane loads 16-byte pieces of four values; pairs of
+//   O^T = V^T P^T elements as M, rows as N, positions as K.  A lane reads 16-byte pieces of four values; pairs of
 //                 positions are joined with byte permutes (for E4M3 before the conversion, which takes two codes at
 //                 once).  P^T is S^T's own fragment turned by movmatrix.
 //
@@ -18,17 +19,20 @@
 // beyond 8 and the accumulators take half the registers.  8-bit codes become 16-bit numbers exactly; the keys' scale is
 // applied to the score, the values' to the value, both powers of two.
 //
-// Work is divided as kv_plan.cuh says; the four warps of a CTA take 16 positions each of every 64-position tile and are
-// joined through shared memory at the end of a segment.  The maximum is only raised when a score passes it by 2^8
+// Which position is which row of the instruction is free as well: row g is position g ^ (g odd ? 4 : 0), which together
+// with the 128-byte swizzle of the copies makes the reads of keys and of values free of bank conflicts.
+//
+// Work is divided as kv_plan.cuh says; the warps of a CTA (and the CTAs of a cluster) take every
+// (warps x CTAs)-th tile of a segment and are joined at its end.  The maximum is only raised when a score passes it by 2^8
 // (weights stay far inside the range of either type), which saves the shuffles of the maximum on most tiles.
 #include "kv_plan.cuh"
 
 namespace dresd {
 namespace {
 
-constexpr int kWarps = 4;
+constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
-constexpr int kTile = kWarps * 16;
+constexpr int kTile = 16;
 constexpr float kSlack = 8.f;           // log2 of the largest weight before the maximum is raised
 
 template <typename T>
@@ -49,6 +53,40 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x)
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
+// Position of instruction row g (0 .. 7) within its eight.
+__device__ __forceinline__ int place(int g) { return g ^ ((g & 1) << 2); }
+
+template <bool Q8, int D, int NT>
+struct Geometry {
+    static constexpr int kRows = 8 * NT;
+    static constexpr int kRowBytes = Q8 ? D : 2 * D;      // one key or value
+    static constexpr int kSlabs = kRowBytes > 128 ? kRowBytes / 128 : 1;
+    static constexpr int kHalf = kTile * kRowBytes;       // keys (or values) of a tile
+    static constexpr int kStage = 2 * kHalf;
+    // bytes in flight: 192 KB an SM, less where the join's buffer or the exponents need the room
+    static constexpr int kStages = (NT == 2 ? 16384 : Q8 ? 20480 : 24576) / kStage;
+    static constexpr int kJoinRow = D + 4;                // floats of a row of a warp's sums
+};
+
+struct Job {
+    Segment seg;
+    Chunk c;
+    int more;
+    int t0, t1;             // tiles of the segment (all warps')
+};
+template <bool Q8, int D, int NT>
+struct Shared {
+    using Geo = Geometry<Q8, D, NT>;
+    alignas(1024) uint8_t ring[kWarps][Geo::kStages][Geo::kStage];
+    alignas(16) float o[kWarps][Geo::kRows][Geo::kJoinRow];          // the warps' sums; then, in a cluster, the CTA's as float4
+    alignas(16) uint8_t exps[Q8 ? kWarps : 1][Geo::kStages][2][kTile];
+    float m[kWarps][Geo::kRows], l[kWarps][Geo::kRows];
+    float cm[Geo::kRows], cl[Geo::kRows];                            // the CTA's
+    uint64_t full[kWarps][Geo::kStages];
+    uint64_t ready, taken;
+    Job job[4];
+    unsigned ticket;
+};
 
 // Parts of shared items: per CTA two slots of `rows` x (d + 2) floats: the sums, then the rows' maxima, then the
 // rows' weight sums.
@@ -65,100 +103,205 @@ __device__ __forceinline__ uint32_t word(const uint2 &v, int i) { return i == 0 
 
 // NT: tiles of 8 rows.
 template <typename T, bool Q8, int D, int NT>
-__global__ void __launch_bounds__(kThreads)
-attend_mma_kernel(const __grid_constant__ AttendArgs a, int least)
+__global__ void __launch_bounds__(kThreads, 1)
+attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                  const __grid_constant__ AttendArgs a)
 {
-    constexpr int kRows = 8 * NT;
-    constexpr int kRowBytes = Q8 ? D : 2 * D;             // one key or value
+    using Geo = Geometry<Q8, D, NT>;
+    constexpr int kRows = Geo::kRows, kRowBytes = Geo::kRowBytes, kStages = Geo::kStages;
     constexpr int kKeyPieces = kRowBytes / 64;            // 16-byte pieces of a key per lane (4 lanes share a key)
     constexpr int kSteps = D / 16;                        // k-steps of the first product, M-tiles of the second
     constexpr int kValBytes = kRowBytes >= 128 ? 16 : 8;  // a lane's piece of a value (8 lanes share a value)
     constexpr int kValPieces = kRowBytes / 8 / kValBytes;
     constexpr int kValElems = kValBytes / (Q8 ? 1 : 2);   // elements in it
+    constexpr int kOwn = (kRows * D / 4 + kThreads - 1) / kThreads;       // float4 of a thread in a join
     using VPiece = typename Piece<kValBytes>::type;
+    using Sh = Shared<Q8, D, NT>;
 
+    extern __shared__ uint8_t smem_raw[];
+    Sh &sh = *reinterpret_cast<Sh *>(smem_raw);
+    if (smem_u32(smem_raw) & 1023u) {                       // shared memory never starts there
+        if (threadIdx.x == 0) report_timeout(a.kv.status);
+        return;
+    }
+    float4 *sums = reinterpret_cast<float4 *>(sh.o);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
-    __shared__ float s_o[kWarps][kRows][D + 4];
-    __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
-    __shared__ unsigned s_ticket;
+    const long long wl = a.wait_cycles > 0 ? a.wait_cycles : kWaitCycles;
+    const int rank = a.ctas > 1 ? (int)cluster_ctarank() : 0;
+    const int step = kWarps * a.ctas;                      // a warp takes every step-th tile
 
+    if (lane == 0) {
+        for (int s = 0; s < kStages; ++s) mbar_init(&sh.full[warp][s], 1);
+        if (warp == 0) {
+            mbar_init(&sh.ready, a.ctas);
+            mbar_init(&sh.taken, a.ctas);
+            tma_prefetch_desc(&k_map);
+            tma_prefetch_desc(&v_map);
+        }
+        mbar_fence_init();
+    }
+    pdl_wait();                                             // what follows reads what earlier kernels wrote
+    pdl_launch_dependents();
+
+    // Warp 0 works out the segments, one ahead of the present one.
     KvPlan<FewRows> plan;
-    if (!plan.start(a, lane, blockIdx.x, gridDim.x, least)) return;
-    Segment seg;
-    while (plan.next(a, seg)) {
-        const Chunk ch = plan.c;
-        const int heads = a.kv.heads * a.group;
+    bool more = false;
+    auto publish = [&](int i) {
+        Job &w = sh.job[i & 3];
+        if (more) more = plan.next(a, w.seg);
+        w.more = more;
+        if (!more) return;
+        w.c = plan.c;
+        int seen = plan.c.total;
+        if (!a.mask) seen = min(seen, plan.c.ctx + min(plan.c.len - 1, a.by_group.div((w.seg.rt + 1) * kRows - 1)) + 1);
+        w.t0 = w.seg.kt0 * step;
+        w.t1 = min(w.seg.kt1 * step, (seen + kTile - 1) / kTile);
+        plan.advance(a);
+    };
+    if (warp == 0) {
+        more = plan.start(a, lane, blockIdx.x / a.ctas, gridDim.x / a.ctas);       // the same for the whole cluster
+        if (lane == 0) {
+            publish(0);
+            publish(1);
+        }
+    }
+    if (a.ctas > 1) cluster_sync_all();                     // the neighbours' barriers are set up
+    else __syncthreads();
+
+    // ---- the ring.  The fetching side is up to kStages tiles ahead of the using side, in the next segment if need be.
+    const int beyond = (int)min((long long)a.kv.layers * a.kv.num_pages * a.kv.heads << a.kv.page_shift, 2147483647LL);
+    int fetched = 0, f_job = 0, f_tile = -1;               // the last tile that next_row() gave of segment f_job
+    auto row_of = [&](const Job &w, int tile) {             // row of the tile's positions in the maps; beyond the end: zeros
+        const int p = tile * kTile;
+        if (p >= w.c.total) return beyond;
+        const int page = __ldg(a.kv.table + (long long)w.seg.b * a.kv.width + (p >> a.kv.page_shift));
+        if (page < 0 || page >= a.kv.num_pages) return beyond;
+        return (int)kv_row(a.kv, a.kv.layer, page, w.seg.head, p & ((1 << a.kv.page_shift) - 1));
+    };
+    // Row of the next tile to fetch, -1 = none known yet (up to the segment after `i`).
+    auto next_row = [&](int i) {
+        for (; f_job <= i + 1; ++f_job, f_tile = -1) {
+            const Job &w = sh.job[f_job & 3];
+            if (!w.more) break;
+            f_tile = f_tile < 0 ? w.t0 + rank * kWarps + warp : f_tile + step;
+            if (f_tile < w.t1) return row_of(w, f_tile);
+        }
+        return -1;
+    };
+    auto fetch = [&](int row) {                             // lane 0
+        const int s = fetched % kStages;
+        uint64_t *bar = &sh.full[warp][s];
+        uint8_t *dst = sh.ring[warp][s];
+        mbar_arrive_expect_tx(bar, (uint32_t)(Geo::kStage + (Q8 ? 2 * kTile : 0)));
+        if (a.lose_stage > 0 && blockIdx.x == 0 && warp == 0 && fetched == a.lose_stage - 1) return;
+#pragma unroll
+        for (int p = 0; p < Geo::kSlabs; ++p) {
+            tma_load_2d(dst + p * kTile * 128, &k_map, p * 64, row, bar);
+            tma_load_2d(dst + Geo::kHalf + p * kTile * 128, &v_map, p * 64, row, bar);
+        }
+        if constexpr (Q8) {
+            const int e = row < beyond ? row : 0;           // zeros have any exponents
+            bulk_load(sh.exps[warp][s][0], a.kv.k_exps + e, kTile, bar);
+            bulk_load(sh.exps[warp][s][1], a.kv.v_exps + e, kTile, bar);
+        }
+    };
+    int pending = next_row(0);                              // row of the next tile to fetch
+    for (int s = 0; s < kStages && pending >= 0; ++s) {
+        if (lane == 0) fetch(pending);
+        ++fetched;
+        pending = next_row(0);
+    }
+
+    int used = 0, joins = 0;
+    bool dead = false;
+    for (int i = 0;; ++i) {
+        const Job &w = sh.job[i & 3];
+        if (!w.more) break;
+        const Segment &seg = w.seg;
+        const Chunk ch = w.c;
+        if (pending < 0) pending = next_row(i);             // the segment after this one has become known
+        while (fetched - used < kStages && pending >= 0) {
+            if (lane == 0) fetch(pending);
+            ++fetched;
+            pending = next_row(i);
+        }
         const int rows = min(kRows, ch.len * a.group - seg.rt * kRows);     // valid rows of the tile
         // ---- the queries, as the B operand: lane (g, c) holds row g's pieces
         uint32_t q[NT][kSteps][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int r = seg.rt * kRows + nt * 8 + g;
+            const int r = seg.rt * kRows + nt * 8 + g, tok = a.by_group.div(r);
             const bool ok = nt * 8 + g < rows;
-            const T *src = static_cast<const T *>(a.q) + (long long)(ch.row0 + (ok ? a.by_group.div(r) : 0)) * a.q_row +
-                           (seg.head * a.group + (ok ? (r - a.by_group.div(r) * a.group) : 0)) * a.q_head;
+            const T *src = static_cast<const T *>(a.q) + (long long)(ch.row0 + (ok ? tok : 0)) * a.q_row +
+                           (seg.head * a.group + (ok ? r - tok * a.group : 0)) * a.q_head;
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                // 16-bit keys: piece 4 i + c.  8-bit keys: a key's piece is 16 elements, two of the query's.
-                const int at = Q8 ? (i / 2 * 4 + c) * 16 + i % 2 * 8 : (i * 4 + c) * 8;
-                const uint4 x = ok ? __ldg(reinterpret_cast<const uint4 *>(src + at)) : make_uint4(0, 0, 0, 0);
-                q[nt][2 * i][0] = x.x;
-                q[nt][2 * i][1] = x.y;
-                q[nt][2 * i + 1][0] = x.z;
-                q[nt][2 * i + 1][1] = x.w;
+            for (int x = 0; x < D / 32; ++x) {
+                // 16-bit keys: piece 4 x + c.  8-bit keys: a key's piece is 16 elements, two of the query's.
+                const int at = Q8 ? (x / 2 * 4 + c) * 16 + x % 2 * 8 : (x * 4 + c) * 8;
+                const uint4 v = ok ? __ldg(reinterpret_cast<const uint4 *>(src + at)) : make_uint4(0, 0, 0, 0);
+                q[nt][2 * x][0] = v.x;
+                q[nt][2 * x][1] = v.y;
+                q[nt][2 * x + 1][0] = v.z;
+                q[nt][2 * x + 1][1] = v.w;
             }
         }
-        int limit[NT][2];                                  // causal: positions that rows 2c, 2c + 1 see
-        const uint32_t *bits[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = min(nt * 8 + 2 * c + i, rows - 1);
-                const int tok = a.by_group.div(seg.rt * kRows + r);
-                limit[nt][i] = a.mask ? ch.total : min(ch.total, ch.ctx + tok + 1);
-                bits[nt][i] = a.mask ? a.mask + (long long)(ch.row0 + tok) * a.mask_words : nullptr;
-            }
         float o[NT][kSteps][4] = {};
         float m[NT][2], l[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) m[nt][0] = m[nt][1] = -INFINITY, l[nt][0] = l[nt][1] = 0.f;
 
-        for (int kt = seg.kt0; kt < seg.kt1; ++kt) {
-            const int p0 = kt * kTile + warp * 16;
-            if (p0 >= ch.total) break;                     // positions grow: nothing further for this warp
-            int page = __ldg(a.kv.table + (long long)seg.b * a.kv.width + (p0 >> a.kv.page_shift));
-            if (page < 0 || page >= a.kv.num_pages) page = 0;
-            // the pool has at least one page, and 16 positions from a multiple of 16 lie in one page
-            const long long row = kv_row(a.kv, a.kv.layer, page, seg.head, p0 & ((1 << a.kv.page_shift) - 1));
+#pragma unroll 1
+        for (int t = w.t0 + rank * kWarps + warp; t < w.t1; t += step) {
+            const int p0 = t * kTile, s = used % kStages;
+            if (!dead && !mbar_wait(&sh.full[warp][s], (used / kStages) & 1, wl)) {
+                report_timeout(a.kv.status);
+                dead = true;
+            }
+            dead = __any_sync(0xFFFFFFFFu, dead);
+            const uint8_t *ks = sh.ring[warp][s], *vs_ = ks + Geo::kHalf;
+            // ---- S^T = K Q^T; lane (g, c): keys place(g) (+ 8)
+            float sc[NT][4] = {};
             uint4 kx[2][kKeyPieces];
             VPiece vx[4][kValPieces];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int i = 0; i < kKeyPieces; ++i)
-                    kx[j][i] = __ldcs(reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(a.kv.k) + (row + j * 8 + g) * kRowBytes) + i * 4 + c);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < kValPieces; ++i)
-                    vx[j][i] = __ldcs(reinterpret_cast<const VPiece *>(static_cast<const uint8_t *>(a.kv.v) +
-                                                                     (row + (j & 1) + (j >> 1) * 8 + 2 * c) * kRowBytes) + i * 8 + g);
             int ke[2] = {127, 127}, ve[4] = {127, 127, 127, 127};
-            if constexpr (Q8) {
-                ke[0] = a.kv.k_exps[row + g];
-                ke[1] = a.kv.k_exps[row + 8 + g];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) ve[j] = a.kv.v_exps[row + (j & 1) + (j >> 1) * 8 + 2 * c];
+            for (int j = 0; j < 2; ++j) {
+                const int r = 8 * j + place(g);
+#pragma unroll
+                for (int x = 0; x < kKeyPieces; ++x) {
+                    const int ch16 = 4 * x + c;            // 16-byte piece of the row
+                    const int at = kRowBytes == 64 ? r * 64 + ((ch16 ^ ((r >> 1) & 3)) << 4)
+                                                   : (ch16 >> 3) * (kTile * 128) + r * 128 + (((ch16 & 7) ^ (r & 7)) << 4);
+                    kx[j][x] = *reinterpret_cast<const uint4 *>(ks + at);
+                }
+                if constexpr (Q8) ke[j] = sh.exps[warp][s][0][r];
             }
-            // ---- S^T = K Q^T
-            float s[NT][4] = {};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {                  // values of positions place(2 c), place(2 c + 1) (+ 8)
+                const int r = (j >> 1) * 8 + place(2 * c + (j & 1));
+#pragma unroll
+                for (int x = 0; x < kValPieces; ++x) {
+                    if constexpr (kRowBytes == 64) {
+                        vx[j][x] = *reinterpret_cast<const VPiece *>(vs_ + r * 64 + (((g >> 1) ^ ((r >> 1) & 3)) << 4) + (g & 1) * 8);
+                    } else {
+                        vx[j][x] = *reinterpret_cast<const VPiece *>(vs_ + x * (kTile * 128) + r * 128 + ((g ^ (r & 7)) << 4));
+                    }
+                }
+                if constexpr (Q8) ve[j] = sh.exps[warp][s][1][r];
+            }
+            ++used;
+            __syncwarp();                                  // the tile is in registers: ask for the next one
+            if (pending >= 0) {
+                if (lane == 0) fetch(pending);
+                ++fetched;
+                pending = next_row(i);
+            }
             if constexpr (!Q8) {
 #pragma unroll
                 for (int st = 0; st < kSteps; ++st)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
-                        mma16816<T>(s[nt], word(kx[0][st / 2], st % 2 * 2), word(kx[1][st / 2], st % 2 * 2),
+                        mma16816<T>(sc[nt], word(kx[0][st / 2], st % 2 * 2), word(kx[1][st / 2], st % 2 * 2),
                                     word(kx[0][st / 2], st % 2 * 2 + 1), word(kx[1][st / 2], st % 2 * 2 + 1), q[nt][st][0], q[nt][st][1]);
             } else {
                 const uint32_t one = scale_bits<T>(127) * 0x10001u;
@@ -166,68 +309,67 @@ attend_mma_kernel(const __grid_constant__ AttendArgs a, int least)
                 for (int st = 0; st < kSteps; ++st) {
                     uint32_t f[2][2];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const uint32_t w = word(kx[j][st / 4], st % 4);
-                        f[j][0] = codes_to_pair<T>(__byte_perm(w, 0, 0x1404), one);
-                        f[j][1] = codes_to_pair<T>(__byte_perm(w, 0, 0x3424), one);
-                    }
+                    for (int j = 0; j < 2; ++j) codes_to_pairs<T>(word(kx[j][st / 4], st % 4), one, f[j][0], f[j][1]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
-                        mma16816<T>(s[nt], f[0][0], f[1][0], f[0][1], f[1][1], q[nt][st][0], q[nt][st][1]);
+                        mma16816<T>(sc[nt], f[0][0], f[1][0], f[0][1], f[1][1], q[nt][st][0], q[nt][st][1]);
                 }
             }
-            // ---- scale, mask.  s[nt][2 j + i]: key g + 8 j, row 2 c + i
-            const bool all_seen = p0 + 16 <= ch.ctx && p0 + 16 <= ch.total;
+            // ---- scale, mask.  sc[nt][2 j + x]: key place(g) + 8 j, row 2 c + x
+            const bool all_seen = p0 + kTile <= ch.ctx && p0 + kTile <= ch.total;
             const float sk[2] = {Q8 ? a.scale_log2 * pow2f(min(ke[0], 253) - 127) : a.scale_log2,
                                  Q8 ? a.scale_log2 * pow2f(min(ke[1], 253) - 127) : a.scale_log2};
             bool over = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int x = 0; x < 2; ++x)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        float x = s[nt][2 * j + i] * sk[j];
+                        float y = sc[nt][2 * j + x] * sk[j];
                         if (!all_seen) {
-                            const int p = p0 + 8 * j + g, t = p - ch.ctx;
-                            bool seen = p < limit[nt][i];
-                            if (a.mask && t >= 0 && seen) seen = (t >> 5) < a.mask_words && (bits[nt][i][t >> 5] >> (t & 31) & 1);
-                            if (!seen) x = -INFINITY;
+                            const int r = min(nt * 8 + 2 * c + x, rows - 1), tok = a.by_group.div(seg.rt * kRows + r);
+                            const int p = p0 + 8 * j + place(g), e = p - ch.ctx;
+                            bool seen = p < ch.total;
+                            if (seen && e >= 0)
+                                seen = a.mask ? (e >> 5) < a.mask_words && (a.mask[(long long)(ch.row0 + tok) * a.mask_words + (e >> 5)] >> (e & 31) & 1)
+                                              : e <= tok;
+                            if (!seen) y = -INFINITY;
                         }
-                        s[nt][2 * j + i] = x;
-                        over |= x > m[nt][i] + kSlack;
+                        sc[nt][2 * j + x] = y;
+                        over |= y > m[nt][x] + kSlack;
                     }
             if (__any_sync(0xFFFFFFFFu, over)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float x = fmaxf(fmaxf(s[nt][i], s[nt][2 + i]), m[nt][i]);
+                    for (int x = 0; x < 2; ++x) {
+                        float y = fmaxf(fmaxf(sc[nt][x], sc[nt][2 + x]), m[nt][x]);
 #pragma unroll
-                        for (int sh = 4; sh < 32; sh <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, sh));
-                        const float f = x > -INFINITY ? exp2f(m[nt][i] - x) : 1.f;
-                        m[nt][i] = x;
-                        l[nt][i] *= f;
+                        for (int sh_ = 4; sh_ < 32; sh_ <<= 1) y = fmaxf(y, __shfl_xor_sync(0xFFFFFFFFu, y, sh_));
+                        const float f = y > -INFINITY ? ex2(m[nt][x] - y) : 1.f;
+                        m[nt][x] = y;
+                        l[nt][x] *= f;
 #pragma unroll
                         for (int st = 0; st < kSteps; ++st) {
-                            o[nt][st][i] *= f;
-                            o[nt][st][2 + i] *= f;
+                            o[nt][st][x] *= f;
+                            o[nt][st][2 + x] *= f;
                         }
                     }
             }
-            // ---- weights, and P^T as the B operand: lane (g, c) holds row g, positions 2 c, 2 c + 1 (+ 8)
+            // ---- weights, and P^T as the B operand: lane (g, c) holds row g, positions of rows 2 c, 2 c + 1 (+ 8)
             uint32_t p[NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float base = m[nt][i] > -INFINITY ? m[nt][i] : 0.f;
+                for (int x = 0; x < 2; ++x) {
+                    const float base = m[nt][x] > -INFINITY ? m[nt][x] : 0.f;
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) s[nt][2 * j + i] = exp2f(s[nt][2 * j + i] - base);
-                    l[nt][i] += s[nt][i] + s[nt][2 + i];
+                    for (int j = 0; j < 2; ++j) sc[nt][2 * j + x] = ex2(sc[nt][2 * j + x] - base);
+                    l[nt][x] += sc[nt][x] + sc[nt][2 + x];
                 }
 #pragma unroll
-                for (int j = 0; j < 2; ++j) p[nt][j] = turn8x8(pack2<T>(s[nt][2 * j], s[nt][2 * j + 1]));
+                for (int j = 0; j < 2; ++j) p[nt][j] = turn8x8(pack2<T>(sc[nt][2 * j], sc[nt][2 * j + 1]));
             }
             // ---- O^T += V^T P^T
             uint32_t vs[2] = {0, 0}, vb[2] = {0, 0};
@@ -246,18 +388,18 @@ attend_mma_kernel(const __grid_constant__ AttendArgs a, int least)
                 // are cleared, and non-finite values of the chunk itself are taken out here and added row by row.
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (p0 + (j & 1) + (j >> 1) * 8 + 2 * c >= ch.total) {
+                    if (p0 + (j >> 1) * 8 + place(2 * c + (j & 1)) >= ch.total) {
 #pragma unroll
-                        for (int i = 0; i < kValPieces; ++i) vx[j][i] = VPiece{};
+                        for (int x = 0; x < kValPieces; ++x) vx[j][x] = VPiece{};
                     }
                 if constexpr (Q8) {                        // the code of NaN counts as 0
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
 #pragma unroll
-                        for (int i = 0; i < kValPieces; ++i) {
-                            uint32_t *x = reinterpret_cast<uint32_t *>(&vx[j][i]);
+                        for (int x = 0; x < kValPieces; ++x) {
+                            uint32_t *u = reinterpret_cast<uint32_t *>(&vx[j][x]);
 #pragma unroll
-                            for (int w = 0; w < kValBytes / 4; ++w) x[w] &= ~__vcmpeq4(x[w] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                            for (int k = 0; k < kValBytes / 4; ++k) u[k] &= ~__vcmpeq4(u[k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
                         }
                 } else {
                     constexpr uint32_t kInf = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
@@ -265,44 +407,48 @@ attend_mma_kernel(const __grid_constant__ AttendArgs a, int least)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
 #pragma unroll
-                        for (int i = 0; i < kValPieces; ++i)
+                        for (int x = 0; x < kValPieces; ++x)
 #pragma unroll
-                            for (int w = 0; w < kValBytes / 4; ++w) {
-                                const uint32_t x = word(vx[j][i], w);
-                                odd |= (x & kInf) == kInf || (x >> 16 & kInf) == kInf;
+                            for (int k = 0; k < kValBytes / 4; ++k) {
+                                const uint32_t u = word(vx[j][x], k);
+                                odd |= (u & kInf) == kInf || (u >> 16 & kInf) == kInf;
                             }
                     if (__any_sync(0xFFFFFFFFu, odd)) {
-                        for (int k = 0; k < 16 && p0 + k < ch.total; ++k) {
-                            const T *vrow = static_cast<const T *>(a.kv.v) + (row + k) * D;
-                            float w[NT][2];                // weights of rows 2 c, 2 c + 1 at position k
+#pragma unroll 1
+                        for (int k = 0; k < kTile && p0 + k < ch.total; ++k) {
+                            const int page = __ldg(a.kv.table + (long long)seg.b * a.kv.width + (p0 >> a.kv.page_shift));
+                            if (page < 0 || page >= a.kv.num_pages) break;
+                            const T *vrow = static_cast<const T *>(a.kv.v) +
+                                            kv_row(a.kv, a.kv.layer, page, seg.head, (p0 + k) & ((1 << a.kv.page_shift) - 1)) * D;
+                            float wgt[NT][2];              // weights of rows 2 c, 2 c + 1 at position k; it is row place(k) of its eight
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                                for (int i = 0; i < 2; ++i)
-                                    w[nt][i] = __shfl_sync(0xFFFFFFFFu, k < 8 ? s[nt][i] : s[nt][2 + i], (k & 7) * 4 + c);
+                                for (int x = 0; x < 2; ++x)
+                                    wgt[nt][x] = __shfl_sync(0xFFFFFFFFu, k < 8 ? sc[nt][x] : sc[nt][2 + x], place(k & 7) * 4 + c);
 #pragma unroll
                             for (int st = 0; st < kSteps; ++st)
 #pragma unroll
                                 for (int h = 0; h < 2; ++h) {
                                     const int e = 2 * st + h;
-                                    const float x = unpack2<T>(*reinterpret_cast<const uint16_t *>(vrow + e / kValElems * 8 * kValElems + g * kValElems + e % kValElems)).x;
-                                    if (isfinite(x)) continue;
+                                    const float y = unpack2<T>(reinterpret_cast<const uint16_t *>(vrow)[e / kValElems * 8 * kValElems + g * kValElems + e % kValElems]).x;
+                                    if (isfinite(y)) continue;
 #pragma unroll
                                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                                        for (int i = 0; i < 2; ++i)
-                                            if (w[nt][i] > 0.f) o[nt][st][2 * h + i] += w[nt][i] * x;
+                                        for (int x = 0; x < 2; ++x)
+                                            if (wgt[nt][x] > 0.f) o[nt][st][2 * h + x] += wgt[nt][x] * y;
                                 }
                         }
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
 #pragma unroll
-                            for (int i = 0; i < kValPieces; ++i) {
-                                uint32_t *x = reinterpret_cast<uint32_t *>(&vx[j][i]);
+                            for (int x = 0; x < kValPieces; ++x) {
+                                uint32_t *u = reinterpret_cast<uint32_t *>(&vx[j][x]);
 #pragma unroll
-                                for (int w = 0; w < kValBytes / 4; ++w) {
-                                    if ((x[w] & kInf) == kInf) x[w] &= 0xFFFF0000u;
-                                    if ((x[w] >> 16 & kInf) == kInf) x[w] &= 0x0000FFFFu;
+                                for (int k = 0; k < kValBytes / 4; ++k) {
+                                    if ((u[k] & kInf) == kInf) u[k] &= 0xFFFF0000u;
+                                    if ((u[k] >> 16 & kInf) == kInf) u[k] &= 0x0000FFFFu;
                                 }
                             }
                     }
@@ -312,22 +458,18 @@ attend_mma_kernel(const __grid_constant__ AttendArgs a, int least)
 #pragma unroll
             for (int st = 0; st < kSteps; ++st) {
                 constexpr int kPer = kValElems / 2;        // M-tiles per piece
-                const int i = st / kPer, e = st % kPer;    // e: pair of elements within the piece
+                const int x = st / kPer, e = st % kPer;    // e: pair of elements within the piece
                 uint32_t f[2][2];                          // [pair of positions][element e0, e1]
-                if constexpr (!Q8) {
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const uint32_t lo = word(vx[2 * j][i], e), hi = word(vx[2 * j + 1][i], e);
+                for (int j = 0; j < 2; ++j) {
+                    if constexpr (!Q8) {
+                        const uint32_t lo = word(vx[2 * j][x], e), hi = word(vx[2 * j + 1][x], e);
                         f[j][0] = __byte_perm(lo, hi, 0x5410);
                         f[j][1] = __byte_perm(lo, hi, 0x7632);
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const uint32_t lo = word(vx[2 * j][i], e / 2) >> (16 * (e & 1)), hi = word(vx[2 * j + 1][i], e / 2) >> (16 * (e & 1));
-                        const uint32_t w = __byte_perm(lo, hi, 0x5140);       // codes: e0 of both positions, e1 of both
-                        f[j][0] = codes_to_pair<T>(__byte_perm(w, 0, 0x1404), vs[j]);
-                        f[j][1] = codes_to_pair<T>(__byte_perm(w, 0, 0x3424), vs[j]);
+                    } else {
+                        const uint32_t lo = word(vx[2 * j][x], e / 2), hi = word(vx[2 * j + 1][x], e / 2);
+                        // codes: e0 of both positions, e1 of both
+                        codes_to_pairs<T>(__byte_perm(lo, hi, e & 1 ? 0x7362 : 0x5140), vs[j], f[j][0], f[j][1]);
                         if constexpr (std::is_same<T, __nv_bfloat16>::value)
                             if (big)
 #pragma unroll
@@ -341,136 +483,205 @@ attend_mma_kernel(const __grid_constant__ AttendArgs a, int least)
                 for (int nt = 0; nt < NT; ++nt) mma16816<T>(o[nt][st], f[0][0], f[0][1], f[1][0], f[1][1], p[nt][0], p[nt][1]);
             }
         }
-        // ---- join the four warps
+        // ---- join the warps
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int x = 0; x < 2; ++x) {
 #pragma unroll
-                for (int sh = 4; sh < 32; sh <<= 1) l[nt][i] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][i], sh);
-                const int r = nt * 8 + 2 * c + i;
+                for (int sh_ = 4; sh_ < 32; sh_ <<= 1) l[nt][x] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][x], sh_);
+                const int r = nt * 8 + 2 * c + x;
                 if (g == 0) {
-                    s_m[warp][r] = m[nt][i];
-                    s_l[warp][r] = l[nt][i];
+                    sh.m[warp][r] = m[nt][x];
+                    sh.l[warp][r] = l[nt][x];
                 }
 #pragma unroll
-                for (int st = 0; st < kSteps; ++st)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int e = 2 * st + h;
-                        s_o[warp][r][e / kValElems * 8 * kValElems + g * kValElems + e % kValElems] = o[nt][st][2 * h + i];
-                    }
+                for (int st = 0; st < kSteps; st += 2) {   // elements 2 st .. 2 st + 3 of the lane's piece are neighbours
+                    const int e = 2 * st;
+                    *reinterpret_cast<float4 *>(&sh.o[warp][r][e / kValElems * 8 * kValElems + g * kValElems + e % kValElems]) =
+                        make_float4(o[nt][st][x], o[nt][st][2 + x], o[nt][st + 1][x], o[nt][st + 1][2 + x]);
+                }
             }
         __syncthreads();
-        const bool shared_item = seg.c0 != seg.c1;
+        if (warp == 0 && lane == 0) publish(i + 2);
+        const int heads = a.kv.heads * a.group;
+        const bool split = seg.c0 != seg.c1;
         float *part = part_slot(a, blockIdx.x, seg.slot, kRows);
-        // a thread takes 4 elements of a row
-        for (int x = tid; x < rows * (D / 4); x += kThreads) {
+        auto finish = [&](int r, int e, const float4 &acc, float mm, float ll) {       // four elements of a row's result
+            const float inv = ll > 0.f ? 1.f / ll : ll == 0.f ? 0.f : ll;              // a NaN sum stays one
+            const int rr = seg.rt * kRows + r, tok = a.by_group.div(rr);
+            const long long at = (long long)(ch.row0 + tok) * heads + seg.head * a.group + rr - tok * a.group;
+            *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + at * D + e) =
+                make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
+            if (a.lse && e == 0) a.lse[at] = ((mm > -INFINITY ? mm : 0.f) + log2f(ll)) * 0.69314718055994531f;
+        };
+        auto add = [](float4 &acc, float f, const float4 &y) {                         // what has no weight may be anything
+            if (f > 0.f || f != f) acc.x += f * y.x, acc.y += f * y.y, acc.z += f * y.z, acc.w += f * y.w;
+        };
+        auto put = [&](int x, const float4 &acc, float mm, float ll) {                 // float4 x of the sums
             const int r = x / (D / 4), e = x % (D / 4) * 4;
-            float mm = s_m[0][r];
-#pragma unroll
-            for (int w = 1; w < kWarps; ++w) mm = fmaxf(mm, s_m[w][r]);
-            const float base = mm > -INFINITY ? mm : 0.f;
-            float ll = 0.f;
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float f = exp2f(s_m[w][r] - base);
-                ll += f * s_l[w][r];
-                const float4 y = *reinterpret_cast<const float4 *>(&s_o[w][r][e]);
-                if (f > 0.f) acc.x += f * y.x, acc.y += f * y.y, acc.z += f * y.z, acc.w += f * y.w;
-            }
-            if (shared_item) {
-                __stcg(reinterpret_cast<float4 *>(part + r * D + e), acc);
-                if (e == 0) {
+            if (r >= rows) return;
+            if (!split) {
+                finish(r, e, acc, mm, ll);
+            } else {
+                __stcg(reinterpret_cast<float4 *>(part) + x, acc);
+                if (e == 0 || a.ctas > 1) {                                            // of a cluster every CTA needs them
                     __stcg(part + kRows * D + r, mm);
                     __stcg(part + kRows * D + kRows + r, ll);
                 }
+            }
+        };
+        float4 own[kOwn];
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+            const int x = tid + k * kThreads, r = x / (D / 4), e = x % (D / 4) * 4;
+            if (x >= kRows * (D / 4)) break;
+            float mm = sh.m[0][r];
+#pragma unroll
+            for (int y = 1; y < kWarps; ++y) mm = fmaxf(mm, sh.m[y][r]);
+            float ll = 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int y = 0; y < kWarps; ++y) {
+                const float f = mm > -INFINITY ? ex2(sh.m[y][r] - mm) : 0.f;
+                ll += f * sh.l[y][r];
+                add(acc, f, *reinterpret_cast<const float4 *>(&sh.o[y][r][e]));
+            }
+            if (a.ctas == 1) {
+                put(x, acc, mm, ll);
             } else {
-                const float inv = ll > 0.f ? 1.f / ll : ll == 0.f ? 0.f : ll;      // a NaN sum stays one
-                const int rr = seg.rt * kRows + r;
-                const long long at = (long long)(ch.row0 + a.by_group.div(rr)) * heads + seg.head * a.group + (rr - a.by_group.div(rr) * a.group);
-                *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + at * D + e) =
-                    make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
-                if (a.lse && e == 0) a.lse[at] = (base + log2f(ll)) * 0.69314718055994531f;
+                own[k] = acc;
+                if (e == 0) sh.cm[r] = mm, sh.cl[r] = ll;
             }
         }
-        if (shared_item) {
+        if (a.ctas > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k)
+                if (tid + k * kThreads < kRows * (D / 4)) sums[tid + k * kThreads] = own[k];
+            __syncthreads();
+            if (tid < a.ctas) mbar_arrive_cluster(mapa_rank(smem_u32(&sh.ready), tid));
+            if (!dead && !mbar_wait_cluster(&sh.ready, joins & 1, wl)) {
+                report_timeout(a.kv.status);
+                dead = true;
+            }
+#pragma unroll 1
+            for (int y = tid * a.ctas + rank; y < kRows * (D / 4); y += kThreads * a.ctas) {
+                const int r = y / (D / 4);
+                // all remote loads before the first use
+                float pm[kMaxCluster], pl[kMaxCluster];
+                float4 ps[kMaxCluster];
+#pragma unroll
+                for (int x = 0; x < kMaxCluster; ++x) {
+                    pm[x] = -INFINITY;
+                    if (x < a.ctas) {
+                        pm[x] = ld_cluster(sh.cm + r, x);
+                        pl[x] = ld_cluster(sh.cl + r, x);
+                        ps[x] = ld_cluster(sums + y, x);
+                    }
+                }
+                float mm = pm[0];
+#pragma unroll
+                for (int x = 1; x < kMaxCluster; ++x) mm = fmaxf(mm, pm[x]);
+                float ll = 0.f;
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int x = 0; x < kMaxCluster; ++x)
+                    if (x < a.ctas && mm > -INFINITY) {
+                        const float f = ex2(pm[x] - mm);
+                        ll += f * pl[x];
+                        add(acc, f, ps[x]);
+                    }
+                put(y, acc, mm, ll);
+            }
+            __syncthreads();
+            if (tid < a.ctas) mbar_arrive_cluster(mapa_rank(smem_u32(&sh.taken), tid));
+            if (!dead && !mbar_wait_cluster(&sh.taken, joins & 1, wl)) {
+                report_timeout(a.kv.status);
+                dead = true;
+            }
+            dead = __any_sync(0xFFFFFFFFu, dead);
+            ++joins;
+        }
+        if (split) {
             __threadfence();
             __syncthreads();
-            if (tid == 0) s_ticket = atomicAdd(a.tickets + seg.c0, 1u);
+            if (tid == 0) sh.ticket = atomicAdd(a.tickets + seg.c0 * a.ctas + rank, 1u);
             __syncthreads();
-            if (s_ticket == (unsigned)(seg.c1 - seg.c0)) {                       // the last of them: join the parts
+            if (sh.ticket == (unsigned)(seg.c1 - seg.c0)) {                      // the last of them: join the parts in order
                 __threadfence();
-                if (tid == 0) a.tickets[seg.c0] = 0;
-                for (int x = tid; x < rows * (D / 4); x += kThreads) {
+                if (tid == 0) a.tickets[seg.c0 * a.ctas + rank] = 0;
+#pragma unroll 1
+                for (int x = tid * a.ctas + rank; x < rows * (D / 4); x += kThreads * a.ctas) {
                     const int r = x / (D / 4), e = x % (D / 4) * 4;
                     float mm = -INFINITY, ll = 0.f;
                     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int i = seg.c0; i <= seg.c1; ++i) {
-                        const float *ps = part_slot(a, i, i == seg.c0 ? seg.slot0 : 0, kRows);
+#pragma unroll 4
+                    for (int y = seg.c0; y <= seg.c1; ++y) {
+                        const float *ps = part_slot(a, y * a.ctas + rank, y == seg.c0 ? seg.slot0 : 0, kRows);
                         const float pm = __ldcg(ps + kRows * D + r), pl = __ldcg(ps + kRows * D + kRows + r);
-                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(ps + r * D + e));
-                        const float nm = fmaxf(mm, pm), base = nm > -INFINITY ? nm : 0.f;
-                        const float f0 = exp2f(mm - base), f1 = exp2f(pm - base);
+                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(ps) + x);
+                        const float nm = fmaxf(mm, pm);
+                        const float f0 = nm > -INFINITY ? ex2(mm - nm) : 0.f, f1 = nm > -INFINITY ? ex2(pm - nm) : 0.f;
                         ll = f0 * ll + f1 * pl;
-                        acc.x = f0 * acc.x + (f1 > 0.f ? f1 * y.x : 0.f);
-                        acc.y = f0 * acc.y + (f1 > 0.f ? f1 * y.y : 0.f);
-                        acc.z = f0 * acc.z + (f1 > 0.f ? f1 * y.z : 0.f);
-                        acc.w = f0 * acc.w + (f1 > 0.f ? f1 * y.w : 0.f);
+                        acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
+                        add(acc, f1, v);
                         mm = nm;
                     }
-                    const float base = mm > -INFINITY ? mm : 0.f;
-                    const float inv = ll > 0.f ? 1.f / ll : ll == 0.f ? 0.f : ll;
-                    const int rr = seg.rt * kRows + r;
-                    const long long at = (long long)(ch.row0 + a.by_group.div(rr)) * heads + seg.head * a.group + (rr - a.by_group.div(rr) * a.group);
-                    *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + at * D + e) =
-                        make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
-                    if (a.lse && e == 0) a.lse[at] = (base + log2f(ll)) * 0.69314718055994531f;
+                    finish(r, e, acc, mm, ll);
                 }
             }
         }
-        __syncthreads();                                    // s_o is written again by the next segment
-        plan.advance(a);
+        __syncthreads();                                    // the join's buffers are written again; job i + 2 is known
     }
+    // no copy may be in flight when the CTA ends: all fetched tiles have been used unless a wait ran out
+    for (; used < fetched; ++used)
+        if (!mbar_wait(&sh.full[warp][used % kStages], (used / kStages) & 1, wl)) {
+            if (lane == 0) report_timeout(a.kv.status);
+            break;
+        }
+    __syncwarp();
+    if (a.ctas > 1) cluster_sync_all();                     // nobody leaves while a neighbour may read its shared memory
 }
 
 template <typename T, bool Q8, int D, int NT>
-cudaError_t launch(const AttendArgs &a, int sms, cudaStream_t stream)
+cudaError_t launch(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttendArgs &a, int sms, cudaStream_t stream)
 {
-    static int occupancy = 0;                               // same for every device of this build (sm_100a)
-    if (occupancy == 0) {
-        int n = 0;
-        cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, attend_mma_kernel<T, Q8, D, NT>, kThreads, 0);
-        if (e != cudaSuccess) return e;
-        occupancy = n;
-    }
-    int grid = sms * occupancy;
-    if (grid > attend_mma_max_ctas(sms)) grid = attend_mma_max_ctas(sms);
-    attend_mma_kernel<T, Q8, D, NT><<<grid, kThreads, 0, stream>>>(a, 2);
-    return cudaGetLastError();
+    constexpr int kSmem = (int)sizeof(Shared<Q8, D, NT>);
+    static_assert(kSmem <= 232448, "shared memory");
+    auto kernel = attend_mma_kernel<T, Q8, D, NT>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    return launch_workers(kernel, kThreads, kSmem, a.ctas, sms, stream, k_map, v_map, a);
 }
 template <typename T, bool Q8>
-cudaError_t by_shape(const AttendArgs &a, int sms, cudaStream_t stream)
+cudaError_t by_shape(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttendArgs &a, int sms, cudaStream_t stream)
 {
-    const bool one = (long long)a.max_chunk * a.group <= 8;
-    if (a.kv.d == 64) return one ? launch<T, Q8, 64, 1>(a, sms, stream) : launch<T, Q8, 64, 2>(a, sms, stream);
-    return one ? launch<T, Q8, 128, 1>(a, sms, stream) : launch<T, Q8, 128, 2>(a, sms, stream);
+    if (a.kv.d == 64)
+        return a.by_rows.d == 8 ? launch<T, Q8, 64, 1>(k_map, v_map, a, sms, stream) : launch<T, Q8, 64, 2>(k_map, v_map, a, sms, stream);
+    return a.by_rows.d == 8 ? launch<T, Q8, 128, 1>(k_map, v_map, a, sms, stream) : launch<T, Q8, 128, 2>(k_map, v_map, a, sms, stream);
 }
 
 }  // namespace
 
-int attend_mma_max_ctas(int sms) { return 8 * sms; }
-size_t attend_mma_part_floats(int sms, int d) { return (size_t)attend_mma_max_ctas(sms) * 2 * 16 * (d + 2); }
+size_t attend_mma_part_floats(int sms, int d) { return (size_t)sms * 2 * 16 * (d + 2); }
 
-cudaError_t launch_attend_mma(const AttendArgs &args, int sms, cudaStream_t stream)
+cudaError_t launch_attend_mma(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttendArgs &args, int sms, cudaStream_t stream)
 {
     AttendArgs a = args;
-    a.by_unit = FastDiv(kTile);
-    a.by_rows = FastDiv((long long)a.max_chunk * a.group <= 8 ? 8 : 16);
+    // One tile of 8 rows if the longest chunk fits it, otherwise of 16.
+    const long long rows = (long long)a.max_chunk * a.group;
+    a.by_rows = FastDiv(rows <= 8 ? 8 : 16);
+    // Fewer items than half the SMs: clusters share them.  No more CTAs than give every warp a tile of the longest sequence
+    // that the table can hold.
+    const long long items = (long long)a.kv.B * a.kv.heads * ((rows + 15) / 16), positions = (long long)a.kv.width << a.kv.page_shift;
+    long long ctas = sms / items;
+    if (ctas > (positions + kWarps * kTile - 1) / (kWarps * kTile)) ctas = (positions + kWarps * kTile - 1) / (kWarps * kTile);
+    a.ctas = (int)(ctas < 1 ? 1 : ctas > kMaxCluster ? kMaxCluster : ctas);
+    a.by_unit = FastDiv(kWarps * kTile * a.ctas);
     const bool q8 = a.kv.k_exps != nullptr;
-    if (a.kv.dtype == kF16) return q8 ? by_shape<__half, true>(a, sms, stream) : by_shape<__half, false>(a, sms, stream);
-    return q8 ? by_shape<__nv_bfloat16, true>(a, sms, stream) : by_shape<__nv_bfloat16, false>(a, sms, stream);
+    if (a.kv.dtype == kF16) return q8 ? by_shape<__half, true>(k_map, v_map, a, sms, stream) : by_shape<__half, false>(k_map, v_map, a, sms, stream);
+    return q8 ? by_shape<__nv_bfloat16, true>(k_map, v_map, a, sms, stream) : by_shape<__nv_bfloat16, false>(k_map, v_map, a, sms, stream);
 }
 
 }  // namespace dresd

@@ -39,7 +39,6 @@ namespace {
 constexpr int kTile = 128;                                 // rows of a row tile, positions of a tile
 constexpr int kSlabBytes = kTile * 128;                    // 64 elements of every row of a tile
 constexpr float kSlack = 8.f;
-constexpr int kMaxCluster = 8;
 
 template <bool Q8, int D>
 struct Geometry {
@@ -134,43 +133,6 @@ __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, i
         ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
         : "memory");
 }
-// Plain bulk copy; 16-byte aligned, a multiple of 16 bytes.
-__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
-                 "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar))
-                 : "memory");
-}
-// Distributed shared memory: the same place in CTA `rank` of the cluster.
-__device__ __forceinline__ float ld_cluster(const float *p, uint32_t rank)
-{
-    float x;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(mapa_rank(smem_u32(p), rank)) : "memory");
-    return x;
-}
-__device__ __forceinline__ float4 ld_cluster(const float4 *p, uint32_t rank)
-{
-    float4 x;
-    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(mapa_rank(smem_u32(p), rank)) : "memory");
-    return x;
-}
-// Bounded wait on a barrier that other CTAs of the cluster arrive on.
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t *bar, uint32_t parity, long long limit)
-{
-    const long long t0 = clock64();
-    while (true) {
-        uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok)
-            : "r"(smem_u32(bar)), "r"(parity)
-            : "memory");
-        if (ok) return true;
-        if (clock64() - t0 > limit) return false;
-    }
-}
 // First operand from TMEM.
 __device__ __forceinline__ void umma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
 {
@@ -215,8 +177,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
         : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 // A warpgroup's registers per thread.  The warpgroups' shares together are what the CTA was launched with: 512 x 128
 // (8-bit: 64 + 192 + 192 + 64 a thread of each) or 384 x 168 (88 + 208 + 208).
 template <bool kMore, int kCount>
@@ -249,13 +209,6 @@ __device__ __forceinline__ bool elect_one()
         : "=r"(r));
     return r != 0;
 }
-__device__ __forceinline__ float ex2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 // Parts of shared items: two slots per CTA; sums as [d / 4][256 rows] float4 (a warp's rows side by side), maxima and
 // weight sums.
 constexpr int kPartRows = 2 * kTile;
@@ -434,8 +387,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     if (warp < 4) {
         KvPlan<ManyRows> plan;
         bool more = false;
-        // (before the registers are given up: it calls functions that are compiled apart)
-        if (warp == 2) more = plan.start(a, lane, blockIdx.x / a.ctas, gridDim.x / a.ctas, 1);     // the same for the whole cluster
+        if (warp == 2) more = plan.start(a, lane, blockIdx.x / a.ctas, gridDim.x / a.ctas);     // the same for the whole cluster
         set_registers<false, Q8 ? 64 : 88>();
         if (warp == 0) {
             // ---- tiles of keys and values: 16-bit ones straight into the stages, 8-bit ones into the raw ring
@@ -1071,8 +1023,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         uint32_t o[8];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            o[2 * k] = codes_to_pair<T>(__byte_perm(u[k], 0, 0x1404), sc);
-                            o[2 * k + 1] = codes_to_pair<T>(__byte_perm(u[k], 0, 0x3424), sc);
+                            codes_to_pairs<T>(u[k], sc, o[2 * k], o[2 * k + 1]);
                         }
                         if constexpr (std::is_same<T, __nv_bfloat16>::value) {
                             if (e > 134) {
@@ -1120,32 +1071,7 @@ cudaError_t launch(const CUtensorMap &q_map, const CUtensorMap &k_map, const CUt
     static_assert(Geometry<Q8, D>::kBig + Geometry<Q8, D>::kSmall <= kSmemBytes, "shared memory");
     const cudaError_t e = cudaFuncSetAttribute(attend_umma_kernel<T, Q8, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = a.ctas;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.gridDim = dim3(sms / a.ctas * a.ctas);
-    cfg.blockDim = dim3(Geometry<Q8, D>::kThreads);
-    cfg.dynamicSmemBytes = kSmemBytes;
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = a.ctas > 1 ? 2 : 1;
-    if (a.ctas > 1) {
-        // how many clusters the device holds at once (its SMs come in groups, which a cluster does not cross); the
-        // same on every device of this build
-        static int held[kMaxCluster + 1] = {};
-        if (held[a.ctas] == 0) {
-            int n = 0;
-            const cudaError_t eo = cudaOccupancyMaxActiveClusters(&n, attend_umma_kernel<T, Q8, D>, &cfg);
-            if (eo != cudaSuccess) return eo;
-            held[a.ctas] = n > 0 ? n : 1;
-        }
-        if ((int)cfg.gridDim.x > held[a.ctas] * a.ctas) cfg.gridDim.x = held[a.ctas] * a.ctas;
-    }
-    return cudaLaunchKernelEx(&cfg, attend_umma_kernel<T, Q8, D>, q_map, k_map, v_map, a);
+    return launch_workers(attend_umma_kernel<T, Q8, D>, Geometry<Q8, D>::kThreads, kSmemBytes, a.ctas, sms, stream, q_map, k_map, v_map, a);
 }
 
 }  // namespace

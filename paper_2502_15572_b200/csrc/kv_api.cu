@@ -59,9 +59,9 @@ EncodeTiledFn encode_tiled_fn()
     return fn;
 }
 
-// 16-bit elements in boxes of one 128-byte swizzle row, or bytes in boxes of whole rows; zeros beyond the ends.
+// Zeros beyond the ends.
 bool encode(CUtensorMap *map, const void *base, int dtype, int rank, const cuuint64_t *dims, const cuuint64_t *strides,
-            const cuuint32_t *box)
+            const cuuint32_t *box, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B)
 {
     const cuuint32_t ones[3] = {1, 1, 1};
     EncodeTiledFn fn = encode_tiled_fn();
@@ -70,8 +70,7 @@ bool encode(CUtensorMap *map, const void *base, int dtype, int rank, const cuuin
                     : dtype == kF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
                                     : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
                     rank, const_cast<void *>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                    dtype == kE4M3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
-                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                    swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -81,7 +80,8 @@ bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0;
 struct dresd_kv {
     uint32_t magic;
     int device, sms;
-    CUtensorMap k_map, v_map;    // over the cache's rows
+    CUtensorMap k_map, v_map;    // over the cache's rows, boxes of a page (tcgen05 kernel)
+    CUtensorMap k16_map, v16_map;    // boxes of 16 rows (mma.sync kernel)
     KvArgs args;                 // arrays and geometry; the batch's part is filled in per call
     float *part;                 // parts of shared items (see kv_plan.cuh)
     unsigned int *tickets;
@@ -191,13 +191,17 @@ dresd_status dresd_kv_create(void *k_pages, void *v_pages, uint8_t *k_exps, uint
         free_kv(kv);
         return fail_cuda(e, "device query");
     }
-    const size_t tickets = sizeof(unsigned int) * (size_t)attend_mma_max_ctas(kv->sms);
+    const size_t tickets = sizeof(unsigned int) * (size_t)kv->sms;
     const size_t few = attend_mma_part_floats(kv->sms, head_dim), many = attend_umma_part_floats(kv->sms, head_dim);
     const cuuint64_t dims[2] = {(cuuint64_t)head_dim, (cuuint64_t)layers * num_pages * kv_heads * page_size};
     const cuuint64_t strides[1] = {(cuuint64_t)head_dim * (k_exps ? 1 : 2)};
     const cuuint32_t box[2] = {(cuuint32_t)(k_exps ? head_dim : 64), (cuuint32_t)page_size};
-    if (!encode(&kv->k_map, k_pages, k_exps ? kE4M3 : a.dtype, 2, dims, strides, box) ||
-        !encode(&kv->v_map, v_pages, k_exps ? kE4M3 : a.dtype, 2, dims, strides, box)) {
+    const cuuint32_t box16[2] = {box[0], 16};
+    const int held = k_exps ? kE4M3 : a.dtype;
+    const CUtensorMapSwizzle none = k_exps ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;
+    const CUtensorMapSwizzle row = k_exps && head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
+    if (!encode(&kv->k_map, k_pages, held, 2, dims, strides, box, none) || !encode(&kv->v_map, v_pages, held, 2, dims, strides, box, none) ||
+        !encode(&kv->k16_map, k_pages, held, 2, dims, strides, box16, row) || !encode(&kv->v16_map, v_pages, held, 2, dims, strides, box16, row)) {
         free_kv(kv);
         return fail(DRESD_ERR_CUDA, "cuTensorMapEncodeTiled failed");
     }
@@ -307,7 +311,7 @@ dresd_status dresd_kv_attend(dresd_kv *kv, int layer, const dresd_kv_batch *batc
         if (!encode(&q_map, q, a.kv.dtype, 3, dims, strides, box)) return fail(DRESD_ERR_CUDA, "cuTensorMapEncodeTiled failed for q");
         e = launch_attend_umma(q_map, kv->k_map, kv->v_map, a, kv->sms, kv->last_stream);
     } else {
-        e = launch_attend_mma(a, kv->sms, kv->last_stream);
+        e = launch_attend_mma(kv->k16_map, kv->v16_map, a, kv->sms, kv->last_stream);
     }
     if (e != cudaSuccess) return fail_cuda(e, "kv_attend launch");
     kv->last_launches = 1;
@@ -346,7 +350,7 @@ dresd_status dresd_kv_status(dresd_kv *kv)
     if (word == 0) return DRESD_OK;
     e = cudaMemset(kv->args.status, 0, sizeof(int));
     // a kernel that gave up may have left tickets behind
-    if (e == cudaSuccess) e = cudaMemset(kv->tickets, 0, sizeof(unsigned int) * (size_t)attend_mma_max_ctas(kv->sms));
+    if (e == cudaSuccess) e = cudaMemset(kv->tickets, 0, sizeof(unsigned int) * (size_t)kv->sms);
     if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
     if (e != cudaSuccess) return fail_cuda(e, "status reset");
     if (word <= -1000) return fail(DRESD_ERR_INTERNAL, "bounds check %d failed inside a kernel", -1000 - word);

@@ -64,6 +64,22 @@ template <> __device__ __forceinline__ uint32_t codes_to_pair<__nv_bfloat16>(uin
     const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&b), *reinterpret_cast<const __nv_bfloat162 *>(&scale));
     return *reinterpret_cast<const uint32_t *>(&r);
 }
+// The four codes of a word as two pairs.
+template <typename T>
+__device__ __forceinline__ void codes_to_pairs(uint32_t w, uint32_t scale, uint32_t &lo, uint32_t &hi)
+{
+    if constexpr (std::is_same<T, __half>::value) {
+        const __half2 s = *reinterpret_cast<const __half2 *>(&scale);
+        const __half2_raw x = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3);
+        const __half2_raw y = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
+        const __half2 p = __hmul2(*reinterpret_cast<const __half2 *>(&x), s), q = __hmul2(*reinterpret_cast<const __half2 *>(&y), s);
+        lo = *reinterpret_cast<const uint32_t *>(&p);
+        hi = *reinterpret_cast<const uint32_t *>(&q);
+    } else {
+        lo = codes_to_pair<T>(__byte_perm(w, 0, 0x1404), scale);
+        hi = codes_to_pair<T>(__byte_perm(w, 0, 0x3424), scale);
+    }
+}
 // What codes_to_pair() multiplies by for exponent byte `eb`, as the bits of one T.  bf16: 2^(e + 120) is representable up
 // to e = 7; larger ones (values beyond 57344) are finished by a second product with big_scale().
 template <typename T> __device__ __forceinline__ uint32_t scale_bits(int eb);
@@ -99,18 +115,66 @@ __device__ __forceinline__ long long kv_row(const KvArgs &a, int layer, int page
     return (((((long long)layer * a.num_pages + page) * a.heads + head) << a.page_shift) + off);
 }
 
+// ---- shared memory of the CTA and its cluster ------------------------------------------------------
+constexpr int kMaxCluster = 8;
+
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+// Plain bulk copy; 16-byte aligned, a multiple of 16 bytes.
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+                 "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+// Distributed shared memory: the same place in CTA `rank` of the cluster.
+__device__ __forceinline__ float ld_cluster(const float *p, uint32_t rank)
+{
+    float x;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(mapa_rank(smem_u32(p), rank)) : "memory");
+    return x;
+}
+__device__ __forceinline__ float4 ld_cluster(const float4 *p, uint32_t rank)
+{
+    float4 x;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(mapa_rank(smem_u32(p), rank)) : "memory");
+    return x;
+}
+// Bounded wait on a barrier that other CTAs of the cluster arrive on.
+__device__ __forceinline__ bool mbar_wait_cluster(uint64_t *bar, uint32_t parity, long long limit)
+{
+    const long long t0 = clock64();
+    while (true) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(smem_u32(bar)), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if (clock64() - t0 > limit) return false;
+    }
+}
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // ---- division of the attention's work -----------------------------------------------------------
 // An ITEM is a tile of rows of one sequence and key/value head (row r of a chunk is head r % group of token r / group);
 // its cost is the number of UNITS of positions that its rows see (at least one, so that every row is written).  How many
 // rows and positions that is, a kernel's Shape says.  A WORKER is a CTA, or a cluster of CTAs that split every unit among
 // them and join their results through shared memory.  Worker i of n gets
 //
-//   few items: a piece of ONE item.  Every item is cut into pieces of at most L units, L the least for which there are
-//       workers for all pieces, if that is within an eighth and four units of an even share W / n: nobody starts a second
-//       item, whose fixed cost (queries, join) is several units.
-//   otherwise: units i W / n .. (i + 1) W / n - 1 of all W units in the order (sequence, row tile, head), so that the
-//       workers finish together however ragged the batch is; a worker has the tail of one item, some whole items and
-//       the head of another.
+//   few items: a piece of ONE item.  With n / items workers for each, items are cut into pieces of at most L units, if L is
+//       within an eighth and four units of an even share W / n: nobody starts a second item, whose fixed cost (queries,
+//       join) is several units.
+//   otherwise: an even share of all W units in the order (sequence, row tile, head), so that the workers finish together
+//       however ragged the batch is; a worker has the tail of one item, some whole items and the head of another.
 //
 // Parts of an item are joined by the worker that finishes it last, in the order of the workers, so results do not depend
 // on timing.
@@ -133,9 +197,16 @@ struct FewRows {
     }
 };
 
+// Quotients of numbers that nearly always fit 32 bits.
+__device__ __forceinline__ long long quotient(long long a, long long b)
+{
+    return ((unsigned long long)(a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 template <typename Shape>
 struct KvPlan {
-    long long W, hi, u;         // many items: units in all; end of this worker's; next unit
+    long long W, hi, u;         // units in all; end of this worker's; next unit
+    long long even, more;       // the first `more` workers have even + 1 units, the others even
     int n;                      // workers (0: a piece each)
     int b, rt, head, kt;        // item of unit u, and its place there
     int pieces, piece;          // of the item, and this worker's
@@ -143,96 +214,111 @@ struct KvPlan {
     bool first;
     Chunk c;
 
-    // Pieces of at most L units of one head of sequence bb (L = 1: its units).  One copy of this code serves every pass
-    // below: a kernel starts with a cold instruction cache, where straight-line copies cost more than the arithmetic.
-    static __device__ __noinline__ unsigned pieces_of(const AttendArgs &a, int bb, unsigned L, unsigned *items)
+    // Units of sequence bb for one head in pieces of at most L (L = 1: the units), its largest item, its row tiles.
+    static __device__ __forceinline__ unsigned pieces_of(const AttendArgs &a, const Chunk &k, unsigned L, unsigned *most, unsigned *items)
     {
-        const Chunk k = kv_chunk(a.kv, bb);
         const int nr = Shape::row_tiles(a, k);
-        unsigned p = 0;
+        unsigned p = 0, m = 0;
 #pragma unroll 1
         for (int r = 0; r < nr; ++r) {
             const unsigned u = Shape::units(a, k, r);
             p += L == 1 ? u : (u + L - 1) / L;
+            m = max(m, u);
         }
+        *most = m;
         *items = nr;
         return p;
     }
-    // Sum over the sequences of pieces_of, or (find >= 0) the sequence that piece `find` belongs to and the pieces before it.
-    static __device__ __noinline__ long long scan(const AttendArgs &a, int lane, unsigned L, long long find, int *b, long long *out)
+    __device__ __forceinline__ long long begin(int i) const { return i * even + min((long long)i, more); }
+    __device__ __forceinline__ int owner(long long t) const
     {
-        long long before = 0, items = 0;
+        const long long big = more * (even + 1);
+        return (int)(t < big ? quotient(t, even + 1) : more + quotient(t - big, even));
+    }
+
+    // Called by all 32 lanes of a warp of worker `me` of `count`; false = nothing to do.
+    __device__ bool start(const AttendArgs &a, int lane, int me, int count)
+    {
+        const int B = a.kv.B;
+        // units, items and the largest item
+        W = 0;
+        unsigned items = 0, most = 0;
+        Chunk k;
 #pragma unroll 1
-        for (int b0 = 0; b0 < a.kv.B; b0 += 32) {
-            unsigned n = 0;
-            const long long own = b0 + lane < a.kv.B ? (long long)pieces_of(a, b0 + lane, L, &n) * a.kv.heads : 0;
+        for (int b0 = 0; b0 < B; b0 += 32) {
+            unsigned m = 0, i = 0, p = 0;
+            if (b0 + lane < B) {
+                k = kv_chunk(a.kv, b0 + lane);
+                p = pieces_of(a, k, 1, &m, &i);
+            }
+            const unsigned lo = __reduce_add_sync(0xFFFFFFFFu, p & 0xFFFFu), up = __reduce_add_sync(0xFFFFFFFFu, p >> 16);
+            W += lo + ((long long)up << 16);
+            items += __reduce_add_sync(0xFFFFFFFFu, i);
+            most = max(most, __reduce_max_sync(0xFFFFFFFFu, m));
+        }
+        W *= a.kv.heads;
+        first = true;
+        if (W == 0) return false;
+        const unsigned each = (long long)items * a.kv.heads <= count ? (unsigned)count / (items * a.kv.heads) : 0;
+        n = (int)min((long long)count, W);
+        even = quotient(W, n);
+        more = W - even * n;
+        unsigned L = each ? (most + each - 1) / each : 0;
+        long long find = me;
+        if (each && L <= even + 1 + even / 8 + 4) {
+            n = 0;
+        } else {
+            L = 1;
+            if (me >= n) return false;
+            find = u = begin(me);
+            hi = begin(me + 1);
+        }
+        // the sequence that piece or unit `find` belongs to, and what comes before it
+        long long before = 0;
+        bool found = false;
+#pragma unroll 1
+        for (int b0 = 0; b0 < B; b0 += 32) {
+            unsigned m, i;
+            long long own = 0;
+            if (b0 + lane < B) {
+                if (B > 32) k = kv_chunk(a.kv, b0 + lane);
+                own = (long long)pieces_of(a, k, L, &m, &i) * a.kv.heads;
+            }
             long long incl = own;
-            items += n;
-#pragma unroll 1
+#pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const long long x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
                 if (lane >= o) incl += x;
             }
-            const unsigned m = find >= 0 ? __ballot_sync(0xFFFFFFFFu, before + incl > find) : 0;
-            if (m) {
-                const int l = __ffs(m) - 1;
-                *b = b0 + l;
-                *out = before + __shfl_sync(0xFFFFFFFFu, incl - own, l);
-                return 1;
+            const unsigned hit = __ballot_sync(0xFFFFFFFFu, before + incl > find);
+            if (hit) {
+                const int l = __ffs(hit) - 1;
+                b = b0 + l;
+                before += __shfl_sync(0xFFFFFFFFu, incl - own, l);
+                c.row0 = __shfl_sync(0xFFFFFFFFu, k.row0, l);
+                c.len = __shfl_sync(0xFFFFFFFFu, k.len, l);
+                c.ctx = __shfl_sync(0xFFFFFFFFu, k.ctx, l);
+                c.total = __shfl_sync(0xFFFFFFFFu, k.total, l);
+                found = true;
+                break;
             }
             before += __shfl_sync(0xFFFFFFFFu, incl, 31);
         }
-        if (find >= 0) return 0;
-#pragma unroll 1
-        for (int o = 16; o > 0; o >>= 1) items += __shfl_xor_sync(0xFFFFFFFFu, items, o);
-        *out = items * a.kv.heads;
-        return before;
-    }
-
-    // Called by all 32 lanes of a warp of worker `me` of `count`; false = nothing to do.  No piece is
-    // smaller than `least` units unless its item is.
-    __device__ bool start(const AttendArgs &a, int lane, int me, int count, int least)
-    {
-        long long items, before;
-        W = scan(a, lane, 1, -1, &b, &items);
-        first = true;
-        if (W == 0) return false;
-        n = (int)min((long long)count, (W + least - 1) / least);
-        const long long even = max((W + count - 1) / count, (long long)least), most = even + even / 8 + 4;
-        unsigned L = 1;
-        long long find;
-        bool each = false;
-#pragma unroll 1
-        for (long long LL = even; items <= count && LL <= most && !each; LL += (LL + 15) / 16) {
-            long long ignored;
-            L = (unsigned)LL;
-            each = scan(a, lane, L, -1, &b, &ignored) <= count;
-        }
-        if (each) {
-            n = 0;
-            find = me;
-        } else {
-            if (me >= n) return false;
-            L = 1;
-            find = u = W * me / n;
-            hi = W * (me + 1) / n;
-        }
-        if (!scan(a, lane, L, find, &b, &before)) return false;
-        c = kv_chunk(a.kv, b);
+        if (!found) return false;
         long long rest = find - before;
 #pragma unroll 1
         for (rt = 0;; ++rt) {
-            pieces = (int)(((unsigned)Shape::units(a, c, rt) + L - 1) / L);
+            const unsigned units = Shape::units(a, c, rt);
+            pieces = (int)(L == 1 ? units : (units + L - 1) / L);
             const long long t = (long long)pieces * a.kv.heads;
             if (rest < t) break;
             rest -= t;
         }
-        head = (int)(rest / pieces);
-        kt = piece = (int)(rest % pieces);
+        head = (int)quotient(rest, pieces);
+        kt = piece = (int)(rest - (long long)head * pieces);
         c0 = me - piece;
         return true;
     }
-    __device__ __forceinline__ int owner(long long t) const { return (int)(((t + 1) * n - 1) / W); }
 
     // The next segment; false when the worker has done its share.  Uniform over the worker.
     __device__ bool next(const AttendArgs &a, Segment &s)
@@ -245,8 +331,8 @@ struct KvPlan {
         s.slot = first ? 0 : 1;
         first = false;
         if (n == 0) {
-            s.kt0 = (int)((long long)units * piece / pieces);
-            s.kt1 = (int)((long long)units * (piece + 1) / pieces);
+            s.kt0 = (int)quotient((long long)units * piece, pieces);
+            s.kt1 = (int)quotient((long long)units * (piece + 1), pieces);
             s.c0 = c0;
             s.c1 = c0 + pieces - 1;
             s.slot0 = 0;
@@ -257,7 +343,7 @@ struct KvPlan {
         const long long item = u - kt;
         s.c0 = owner(item);
         s.c1 = owner(item + units - 1);
-        s.slot0 = W * s.c0 / n == item ? 0 : 1;
+        s.slot0 = begin(s.c0) == item ? 0 : 1;
         u += s.kt1 - s.kt0;
         kt = s.kt1;
         return true;
@@ -277,5 +363,36 @@ struct KvPlan {
         } while (c.len == 0);            // ends: u < hi means that a later sequence has units
     }
 };
+
+// A persistent kernel of one CTA per SM, as clusters of `ctas`, no more of them than the device holds at once (its SMs
+// come in groups, which a cluster does not cross).
+template <typename... KArgs, typename... Args>
+cudaError_t launch_workers(void (*kernel)(KArgs...), int threads, int smem, int ctas, int sms, cudaStream_t stream, const Args &...args)
+{
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(sms / ctas * ctas);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = ctas > 1 ? 2 : 1;
+    if (ctas > 1) {
+        static int held[kMaxCluster + 1] = {};              // per kernel type; every kernel of a type fills an SM
+        if (held[ctas] == 0) {
+            int n = 0;
+            const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+            if (e != cudaSuccess) return e;
+            held[ctas] = n > 0 ? n : 1;
+        }
+        if ((int)cfg.gridDim.x > held[ctas] * ctas) cfg.gridDim.x = held[ctas] * ctas;
+    }
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 
 }  // namespace dresd
