@@ -16,8 +16,13 @@
 //                 once).  P^T is S^T's own fragment turned by movmatrix.
 //
 // 16-row tiles of queries would leave M half empty at the usual 1 to 8 rows per head; with rows as N nothing is padded
-// beyond 8 and the accumulators take half the registers.  8-bit codes become 16-bit numbers exactly; the keys' scale is
-// applied to the score, the values' to the value, both powers of two.
+// beyond 8 and the accumulators take half the registers.
+//
+// 8-bit caches are multiplied in fp16, whatever the type of the queries, because the hardware turns E4M3 codes into fp16
+// numbers (exactly) in one instruction per two.  A bf16 query row is multiplied by the power of two that brings its
+// largest element to 2^14 .. 2^15: every element down to 2^-31 of it stays exact, the rest is off by 2^-40 of it.  The keys'
+// scale is applied to the score; the values' to the weight, relative to the largest exponent so far, and the
+// sums are brought back at the end.
 //
 // Which position is which row of the instruction is free as well: row g is position g ^ (g odd ? 4 : 0), which together
 // with the 128-byte swizzle of the copies makes the reads of keys and of values free of bank conflicts.
@@ -114,6 +119,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     constexpr int kValBytes = kRowBytes >= 128 ? 16 : 8;  // a lane's piece of a value (8 lanes share a value)
     constexpr int kValPieces = kRowBytes / 8 / kValBytes;
     constexpr int kValElems = kValBytes / (Q8 ? 1 : 2);   // elements in it
+    using M = std::conditional_t<Q8, __half, T>;            // type of the products
     constexpr int kOwn = (kRows * D / 4 + kThreads - 1) / kThreads;       // float4 of a thread in a join
     using VPiece = typename Piece<kValBytes>::type;
     using Sh = Shared<Q8, D, NT>;
@@ -170,26 +176,31 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 
     // ---- the ring.  The fetching side is up to kStages tiles ahead of the using side, in the next segment if need be.
     const int beyond = (int)min((long long)a.kv.layers * a.kv.num_pages * a.kv.heads << a.kv.page_shift, 2147483647LL);
-    int fetched = 0, f_job = 0, f_tile = -1;               // the last tile that next_row() gave of segment f_job
-    auto row_of = [&](const Job &w, int tile) {             // row of the tile's positions in the maps; beyond the end: zeros
-        const int p = tile * kTile;
-        if (p >= w.c.total) return beyond;
-        const int page = __ldg(a.kv.table + (long long)w.seg.b * a.kv.width + (p >> a.kv.page_shift));
-        if (page < 0 || page >= a.kv.num_pages) return beyond;
-        return (int)kv_row(a.kv, a.kv.layer, page, w.seg.head, p & ((1 << a.kv.page_shift) - 1));
-    };
-    // Row of the next tile to fetch, -1 = none known yet (up to the segment after `i`).
-    auto next_row = [&](int i) {
+    int fetched = 0, f_job = 0, f_tile = -1;               // the last tile that was looked up, of segment f_job
+    // The next tile: its place in the pool but for the page, whose number (loaded here, used when the copy is issued) may be
+    // anything.  pending = false: none known yet (up to the segment after `i`).
+    bool pending = false;
+    int page = 0, head = 0, off = 0;
+    auto look_ahead = [&](int i) {
+        pending = false;
         for (; f_job <= i + 1; ++f_job, f_tile = -1) {
             const Job &w = sh.job[f_job & 3];
-            if (!w.more) break;
+            if (!w.more) return;
             f_tile = f_tile < 0 ? w.t0 + rank * kWarps + warp : f_tile + step;
-            if (f_tile < w.t1) return row_of(w, f_tile);
+            if (f_tile >= w.t1) continue;
+            const int p = f_tile * kTile;
+            pending = true;
+            head = w.seg.head;
+            off = p & ((1 << a.kv.page_shift) - 1);
+            page = -1;
+            if (p < w.c.total) page = __ldg(a.kv.table + (long long)w.seg.b * a.kv.width + (p >> a.kv.page_shift));
+            return;
         }
-        return -1;
     };
-    auto fetch = [&](int row) {                             // lane 0
+    auto fetch = [&] {                                      // lane 0
         const int s = fetched % kStages;
+        // beyond the end or outside the pool: zeros are loaded
+        const int row = (unsigned)page < (unsigned)a.kv.num_pages ? (int)kv_row(a.kv, a.kv.layer, page, head, off) : beyond;
         uint64_t *bar = &sh.full[warp][s];
         uint8_t *dst = sh.ring[warp][s];
         mbar_arrive_expect_tx(bar, (uint32_t)(Geo::kStage + (Q8 ? 2 * kTile : 0)));
@@ -205,11 +216,11 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             bulk_load(sh.exps[warp][s][1], a.kv.v_exps + e, kTile, bar);
         }
     };
-    int pending = next_row(0);                              // row of the next tile to fetch
-    for (int s = 0; s < kStages && pending >= 0; ++s) {
-        if (lane == 0) fetch(pending);
+    look_ahead(0);
+    while (fetched < kStages && pending) {
+        if (lane == 0) fetch();
         ++fetched;
-        pending = next_row(0);
+        look_ahead(0);
     }
 
     int used = 0, joins = 0;
@@ -219,11 +230,11 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         if (!w.more) break;
         const Segment &seg = w.seg;
         const Chunk ch = w.c;
-        if (pending < 0) pending = next_row(i);             // the segment after this one has become known
-        while (fetched - used < kStages && pending >= 0) {
-            if (lane == 0) fetch(pending);
+        if (!pending) look_ahead(i);                        // the segment after this one has become known
+        while (fetched - used < kStages && pending) {
+            if (lane == 0) fetch();
             ++fetched;
-            pending = next_row(i);
+            look_ahead(i);
         }
         const int rows = min(kRows, ch.len * a.group - seg.rt * kRows);     // valid rows of the tile
         // ---- the queries, as the B operand: lane (g, c) holds row g's pieces
@@ -245,6 +256,35 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 q[nt][2 * x + 1][1] = v.w;
             }
         }
+        float q_scale[NT][2];                               // 8-bit: of rows 2 c, 2 c + 1
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            int e = 0;
+            if constexpr (Q8 && std::is_same<T, __nv_bfloat16>::value) {
+                uint32_t big = 0;
+#pragma unroll
+                for (int st = 0; st < kSteps; ++st) big = __vmaxu2(big, __vmaxu2(q[nt][st][0] & 0x7FFF7FFFu, q[nt][st][1] & 0x7FFF7FFFu));
+                big = max(big & 0xFFFFu, big >> 16);
+                big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
+                big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
+                // 2^e in two factors, as e may be beyond a single number's range
+                e = big ? min(14 + 127 - (int)(big >> 7), 200) : 0;
+                const float f0 = pow2f(e / 2), f1 = pow2f(e - e / 2);
+#pragma unroll
+                for (int st = 0; st < kSteps; ++st)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const float2 v = unpack2<T>(q[nt][st][x]);
+                        q[nt][st][x] = pack2<__half>(v.x * f0 * f1, v.y * f0 * f1);
+                    }
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {                   // row r's scale is with the lanes 4 r .. 4 r + 3
+                const int er = __shfl_sync(0xFFFFFFFFu, e, 4 * (2 * c + x));
+                q_scale[nt][x] = a.scale_log2 * pow2f(-(er / 2)) * pow2f(-(er - er / 2));
+            }
+        }
+        int v_exp = -127;                                   // 8-bit: the sums are held relative to 2^v_exp
         float o[NT][kSteps][4] = {};
         float m[NT][2], l[NT][2];
 #pragma unroll
@@ -263,7 +303,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             float sc[NT][4] = {};
             uint4 kx[2][kKeyPieces];
             VPiece vx[4][kValPieces];
-            int ke[2] = {127, 127}, ve[4] = {127, 127, 127, 127};
+            int ke[2] = {127, 127}, ve[2] = {127, 127};
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int r = 8 * j + place(g);
@@ -274,7 +314,10 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                                                    : (ch16 >> 3) * (kTile * 128) + r * 128 + (((ch16 & 7) ^ (r & 7)) << 4);
                     kx[j][x] = *reinterpret_cast<const uint4 *>(ks + at);
                 }
-                if constexpr (Q8) ke[j] = sh.exps[warp][s][0][r];
+                if constexpr (Q8) {
+                    ke[j] = min((int)sh.exps[warp][s][0][r], 253);
+                    ve[j] = min((int)sh.exps[warp][s][1][r], 253);
+                }
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {                  // values of positions place(2 c), place(2 c + 1) (+ 8)
@@ -287,14 +330,13 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         vx[j][x] = *reinterpret_cast<const VPiece *>(vs_ + x * (kTile * 128) + r * 128 + ((g ^ (r & 7)) << 4));
                     }
                 }
-                if constexpr (Q8) ve[j] = sh.exps[warp][s][1][r];
             }
             ++used;
             __syncwarp();                                  // the tile is in registers: ask for the next one
-            if (pending >= 0) {
-                if (lane == 0) fetch(pending);
+            if (pending) {
+                if (lane == 0) fetch();
                 ++fetched;
-                pending = next_row(i);
+                look_ahead(i);
             }
             if constexpr (!Q8) {
 #pragma unroll
@@ -304,29 +346,36 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         mma16816<T>(sc[nt], word(kx[0][st / 2], st % 2 * 2), word(kx[1][st / 2], st % 2 * 2),
                                     word(kx[0][st / 2], st % 2 * 2 + 1), word(kx[1][st / 2], st % 2 * 2 + 1), q[nt][st][0], q[nt][st][1]);
             } else {
-                const uint32_t one = scale_bits<T>(127) * 0x10001u;
 #pragma unroll
                 for (int st = 0; st < kSteps; ++st) {
                     uint32_t f[2][2];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) codes_to_pairs<T>(word(kx[j][st / 4], st % 4), one, f[j][0], f[j][1]);
+                    for (int j = 0; j < 2; ++j) codes_to_halves(word(kx[j][st / 4], st % 4), f[j][0], f[j][1]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
-                        mma16816<T>(sc[nt], f[0][0], f[1][0], f[0][1], f[1][1], q[nt][st][0], q[nt][st][1]);
+                        mma16816<M>(sc[nt], f[0][0], f[1][0], f[0][1], f[1][1], q[nt][st][0], q[nt][st][1]);
                 }
             }
             // ---- scale, mask.  sc[nt][2 j + x]: key place(g) + 8 j, row 2 c + x
             const bool all_seen = p0 + kTile <= ch.ctx && p0 + kTile <= ch.total;
-            const float sk[2] = {Q8 ? a.scale_log2 * pow2f(min(ke[0], 253) - 127) : a.scale_log2,
-                                 Q8 ? a.scale_log2 * pow2f(min(ke[1], 253) - 127) : a.scale_log2};
+            const float sk[2] = {pow2f(ke[0] - 127), pow2f(ke[1] - 127)};
             bool over = false;
+            if constexpr (Q8) {
+                if (!all_seen) {                           // places that are not in use have any exponent
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        if (p0 + 8 * j + place(g) >= ch.total) ve[j] = 1;
+                }
+                over = max(ve[0], ve[1]) - 127 > v_exp;
+            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        float y = sc[nt][2 * j + x] * sk[j];
+                        float y = sc[nt][2 * j + x] * q_scale[nt][x];
+                        if constexpr (Q8) y *= sk[j];
                         if (!all_seen) {
                             const int r = min(nt * 8 + 2 * c + x, rows - 1), tok = a.by_group.div(seg.rt * kRows + r);
                             const int p = p0 + 8 * j + place(g), e = p - ch.ctx;
@@ -340,6 +389,12 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         over |= y > m[nt][x] + kSlack;
                     }
             if (__any_sync(0xFFFFFFFFu, over)) {
+                float fe = 1.f;
+                if constexpr (Q8) {
+                    const int e = max(v_exp, __reduce_max_sync(0xFFFFFFFFu, max(ve[0], ve[1])) - 127);
+                    fe = pow2f(max(v_exp - e, -126));
+                    v_exp = e;
+                }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -352,8 +407,8 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         l[nt][x] *= f;
 #pragma unroll
                         for (int st = 0; st < kSteps; ++st) {
-                            o[nt][st][x] *= f;
-                            o[nt][st][2 + x] *= f;
+                            o[nt][st][x] *= f * fe;
+                            o[nt][st][2 + x] *= f * fe;
                         }
                     }
             }
@@ -369,20 +424,12 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     l[nt][x] += sc[nt][x] + sc[nt][2 + x];
                 }
 #pragma unroll
-                for (int j = 0; j < 2; ++j) p[nt][j] = turn8x8(pack2<T>(sc[nt][2 * j], sc[nt][2 * j + 1]));
-            }
-            // ---- O^T += V^T P^T
-            uint32_t vs[2] = {0, 0}, vb[2] = {0, 0};
-            bool big = false;
-            if constexpr (Q8) {
-                vs[0] = scale_bits<T>(ve[0]) | scale_bits<T>(ve[1]) << 16;
-                vs[1] = scale_bits<T>(ve[2]) | scale_bits<T>(ve[3]) << 16;
-                if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-                    big = max(max(ve[0], ve[1]), max(ve[2], ve[3])) > 134;
-                    vb[0] = big_scale(ve[0]) | big_scale(ve[1]) << 16;
-                    vb[1] = big_scale(ve[2]) | big_scale(ve[3]) << 16;
+                for (int j = 0; j < 2; ++j) {
+                    const float f = Q8 ? pow2f(max(ve[j] - 127 - v_exp, -126)) : 1.f;
+                    p[nt][j] = turn8x8(Q8 ? pack2<M>(sc[nt][2 * j] * f, sc[nt][2 * j + 1] * f) : pack2<M>(sc[nt][2 * j], sc[nt][2 * j + 1]));
                 }
             }
+            // ---- O^T += V^T P^T
             if (!all_seen) {
                 // Positions that some row does not see may hold anything, and 0 x NaN is NaN: unused positions
                 // are cleared, and non-finite values of the chunk itself are taken out here and added row by row.
@@ -469,18 +516,11 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     } else {
                         const uint32_t lo = word(vx[2 * j][x], e / 2), hi = word(vx[2 * j + 1][x], e / 2);
                         // codes: e0 of both positions, e1 of both
-                        codes_to_pairs<T>(__byte_perm(lo, hi, e & 1 ? 0x7362 : 0x5140), vs[j], f[j][0], f[j][1]);
-                        if constexpr (std::is_same<T, __nv_bfloat16>::value)
-                            if (big)
-#pragma unroll
-                                for (int h = 0; h < 2; ++h) {
-                                    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<__nv_bfloat162 *>(&f[j][h]), *reinterpret_cast<__nv_bfloat162 *>(&vb[j]));
-                                    f[j][h] = *reinterpret_cast<const uint32_t *>(&r);
-                                }
+                        codes_to_halves(__byte_perm(lo, hi, e & 1 ? 0x7362 : 0x5140), f[j][0], f[j][1]);
                     }
                 }
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma16816<T>(o[nt][st], f[0][0], f[0][1], f[1][0], f[1][1], p[nt][0], p[nt][1]);
+                for (int nt = 0; nt < NT; ++nt) mma16816<M>(o[nt][st], f[0][0], f[0][1], f[1][0], f[1][1], p[nt][0], p[nt][1]);
             }
         }
         // ---- join the warps
@@ -498,8 +538,9 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll
                 for (int st = 0; st < kSteps; st += 2) {   // elements 2 st .. 2 st + 3 of the lane's piece are neighbours
                     const int e = 2 * st;
+                    const float f = Q8 ? pow2f(max(v_exp, -126)) : 1.f;
                     *reinterpret_cast<float4 *>(&sh.o[warp][r][e / kValElems * 8 * kValElems + g * kValElems + e % kValElems]) =
-                        make_float4(o[nt][st][x], o[nt][st][2 + x], o[nt][st + 1][x], o[nt][st + 1][2 + x]);
+                        make_float4(o[nt][st][x] * f, o[nt][st][2 + x] * f, o[nt][st + 1][x] * f, o[nt][st + 1][2 + x] * f);
                 }
             }
         __syncthreads();
@@ -677,6 +718,9 @@ cudaError_t launch_attend_mma(const CUtensorMap &k_map, const CUtensorMap &v_map
     const long long items = (long long)a.kv.B * a.kv.heads * ((rows + 15) / 16), positions = (long long)a.kv.width << a.kv.page_shift;
     long long ctas = sms / items;
     if (ctas > (positions + kWarps * kTile - 1) / (kWarps * kTile)) ctas = (positions + kWarps * kTile - 1) / (kWarps * kTile);
+    // Clusters leave SMs idle (of 148, clusters of 8 use at most 128 or so) but save the join through global memory, about 3 us:
+    // not where a CTA's share of the cache may take longer than some 20 us (1 MB).
+    if (items * positions * 2 * a.kv.d * (a.kv.k_exps ? 1 : 2) / sms > 1 << 20) ctas = 1;
     a.ctas = (int)(ctas < 1 ? 1 : ctas > kMaxCluster ? kMaxCluster : ctas);
     a.by_unit = FastDiv(kWarps * kTile * a.ctas);
     const bool q8 = a.kv.k_exps != nullptr;

@@ -64,7 +64,15 @@ template <> __device__ __forceinline__ uint32_t codes_to_pair<__nv_bfloat16>(uin
     const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&b), *reinterpret_cast<const __nv_bfloat162 *>(&scale));
     return *reinterpret_cast<const uint32_t *>(&r);
 }
-// The four codes of a word as two pairs.
+// The four codes of a word as two pairs of fp16.
+__device__ __forceinline__ void codes_to_halves(uint32_t w, uint32_t &lo, uint32_t &hi)
+{
+    const __half2_raw x = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3);
+    const __half2_raw y = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
+    lo = *reinterpret_cast<const uint32_t *>(&x);
+    hi = *reinterpret_cast<const uint32_t *>(&y);
+}
+// The four codes of a word as two pairs, scaled.
 template <typename T>
 __device__ __forceinline__ void codes_to_pairs(uint32_t w, uint32_t scale, uint32_t &lo, uint32_t &hi)
 {
