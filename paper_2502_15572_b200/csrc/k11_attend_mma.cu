@@ -35,8 +35,6 @@
 namespace dresd {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = kWarps * 32;
 constexpr int kTile = 16;
 constexpr float kSlack = 8.f;           // log2 of the largest weight before the maximum is raised
 
@@ -68,9 +66,12 @@ struct Geometry {
     static constexpr int kSlabs = kRowBytes > 128 ? kRowBytes / 128 : 1;
     static constexpr int kHalf = kTile * kRowBytes;       // keys (or values) of a tile
     static constexpr int kStage = 2 * kHalf;
-    // bytes in flight: 192 KB an SM, less where the join's buffer or the exponents need the room
-    static constexpr int kStages = (NT == 2 ? 16384 : Q8 ? 20480 : 24576) / kStage;
+    // A tile takes a warp about as long whatever its bytes: smaller tiles need more warps to keep HBM busy.
+    static constexpr int kWarps = kStage <= 4096 && NT == 1 ? 16 : 8;
+    static constexpr int kThreads = kWarps * 32;
+    static constexpr int kStages = 131072 / (kWarps * kStage);       // 128 KB in flight an SM
     static constexpr int kJoinRow = D + 4;                // floats of a row of a warp's sums
+    static constexpr int kSums = kRows * D / 4;           // float4 of a CTA's sums
 };
 
 struct Job {
@@ -82,12 +83,14 @@ struct Job {
 template <bool Q8, int D, int NT>
 struct Shared {
     using Geo = Geometry<Q8, D, NT>;
-    alignas(1024) uint8_t ring[kWarps][Geo::kStages][Geo::kStage];
-    alignas(16) float o[kWarps][Geo::kRows][Geo::kJoinRow];          // the warps' sums; then, in a cluster, the CTA's as float4
-    alignas(16) uint8_t exps[Q8 ? kWarps : 1][Geo::kStages][2][kTile];
-    float m[kWarps][Geo::kRows], l[kWarps][Geo::kRows];
-    float cm[Geo::kRows], cl[Geo::kRows];                            // the CTA's
-    uint64_t full[kWarps][Geo::kStages];
+    alignas(1024) uint8_t ring[Geo::kWarps][Geo::kStages][Geo::kStage];
+    alignas(16) float o[Geo::kWarps][Geo::kRows][Geo::kJoinRow];     // the warps' sums
+    // cluster: what the CTAs send: sums, maximum and weight sum of float4 number n x ctas + rank, from CTA f at [f x per + n]
+    alignas(16) float4 sent[Geo::kSums + kMaxCluster];
+    alignas(16) float2 sent_ml[Geo::kSums + kMaxCluster];
+    alignas(16) uint8_t exps[Q8 ? Geo::kWarps : 1][Geo::kStages][2][kTile];
+    float m[Geo::kWarps][Geo::kRows], l[Geo::kWarps][Geo::kRows];
+    uint64_t full[Geo::kWarps][Geo::kStages];
     uint64_t ready, taken;
     Job job[4];
     unsigned ticket;
@@ -108,19 +111,18 @@ __device__ __forceinline__ uint32_t word(const uint2 &v, int i) { return i == 0 
 
 // NT: tiles of 8 rows.
 template <typename T, bool Q8, int D, int NT>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Geometry<Q8, D, NT>::kThreads, 1)
 attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                   const __grid_constant__ AttendArgs a)
 {
     using Geo = Geometry<Q8, D, NT>;
-    constexpr int kRows = Geo::kRows, kRowBytes = Geo::kRowBytes, kStages = Geo::kStages;
+    constexpr int kRows = Geo::kRows, kRowBytes = Geo::kRowBytes, kStages = Geo::kStages, kWarps = Geo::kWarps, kThreads = Geo::kThreads;
     constexpr int kKeyPieces = kRowBytes / 64;            // 16-byte pieces of a key per lane (4 lanes share a key)
     constexpr int kSteps = D / 16;                        // k-steps of the first product, M-tiles of the second
     constexpr int kValBytes = kRowBytes >= 128 ? 16 : 8;  // a lane's piece of a value (8 lanes share a value)
     constexpr int kValPieces = kRowBytes / 8 / kValBytes;
     constexpr int kValElems = kValBytes / (Q8 ? 1 : 2);   // elements in it
     using M = std::conditional_t<Q8, __half, T>;            // type of the products
-    constexpr int kOwn = (kRows * D / 4 + kThreads - 1) / kThreads;       // float4 of a thread in a join
     using VPiece = typename Piece<kValBytes>::type;
     using Sh = Shared<Q8, D, NT>;
 
@@ -130,7 +132,6 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         if (threadIdx.x == 0) report_timeout(a.kv.status);
         return;
     }
-    float4 *sums = reinterpret_cast<float4 *>(sh.o);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     const long long wl = a.wait_cycles > 0 ? a.wait_cycles : kWaitCycles;
     const int rank = a.ctas > 1 ? (int)cluster_ctarank() : 0;
@@ -139,7 +140,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     if (lane == 0) {
         for (int s = 0; s < kStages; ++s) mbar_init(&sh.full[warp][s], 1);
         if (warp == 0) {
-            mbar_init(&sh.ready, a.ctas);
+            mbar_init(&sh.ready, 1);
             mbar_init(&sh.taken, a.ctas);
             tma_prefetch_desc(&k_map);
             tma_prefetch_desc(&v_map);
@@ -176,31 +177,38 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 
     // ---- the ring.  The fetching side is up to kStages tiles ahead of the using side, in the next segment if need be.
     const int beyond = (int)min((long long)a.kv.layers * a.kv.num_pages * a.kv.heads << a.kv.page_shift, 2147483647LL);
-    int fetched = 0, f_job = 0, f_tile = -1;               // the last tile that was looked up, of segment f_job
+    int fetched = 0, f_job = -1, f_tile = -step;           // the last tile that was looked up, of segment f_job
     // The next tile: its place in the pool but for the page, whose number (loaded here, used when the copy is issued) may be
     // anything.  pending = false: none known yet (up to the segment after `i`).
     bool pending = false;
-    int page = 0, head = 0, off = 0;
+    int page = 0, off = 0;
+    int f_end = 0, f_total = 0, f_head = 0;                // of segment f_job
+    const int32_t *f_table = nullptr;
+    const int layer_pages = a.kv.layer * a.kv.num_pages, in_page = (1 << a.kv.page_shift) - 1;
     auto look_ahead = [&](int i) {
-        pending = false;
-        for (; f_job <= i + 1; ++f_job, f_tile = -1) {
-            const Job &w = sh.job[f_job & 3];
+        f_tile += step;
+        while (f_tile >= f_end) {                          // on to the next segment
+            pending = false;
+            if (f_job >= i + 1) return;
+            const Job &w = sh.job[(f_job + 1) & 3];
             if (!w.more) return;
-            f_tile = f_tile < 0 ? w.t0 + rank * kWarps + warp : f_tile + step;
-            if (f_tile >= w.t1) continue;
-            const int p = f_tile * kTile;
-            pending = true;
-            head = w.seg.head;
-            off = p & ((1 << a.kv.page_shift) - 1);
-            page = -1;
-            if (p < w.c.total) page = __ldg(a.kv.table + (long long)w.seg.b * a.kv.width + (p >> a.kv.page_shift));
-            return;
+            ++f_job;
+            f_tile = w.t0 + rank * kWarps + warp;
+            f_end = w.t1;
+            f_total = w.c.total;
+            f_head = w.seg.head;
+            f_table = a.kv.table + (long long)w.seg.b * a.kv.width;
         }
+        const int p = f_tile * kTile;
+        pending = true;
+        off = p & in_page;
+        page = -1;
+        if (p < f_total) page = __ldg(f_table + (p >> a.kv.page_shift));
     };
     auto fetch = [&] {                                      // lane 0
         const int s = fetched % kStages;
-        // beyond the end or outside the pool: zeros are loaded
-        const int row = (unsigned)page < (unsigned)a.kv.num_pages ? (int)kv_row(a.kv, a.kv.layer, page, head, off) : beyond;
+        // beyond the end or outside the pool: zeros are loaded.  (The pool has fewer than 2^31 rows.)
+        const int row = (unsigned)page < (unsigned)a.kv.num_pages ? (((layer_pages + page) * a.kv.heads + f_head) << a.kv.page_shift) + off : beyond;
         uint64_t *bar = &sh.full[warp][s];
         uint8_t *dst = sh.ring[warp][s];
         mbar_arrive_expect_tx(bar, (uint32_t)(Geo::kStage + (Q8 ? 2 * kTile : 0)));
@@ -572,11 +580,18 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 }
             }
         };
-        float4 own[kOwn];
-#pragma unroll
-        for (int k = 0; k < kOwn; ++k) {
-            const int x = tid + k * kThreads, r = x / (D / 4), e = x % (D / 4) * 4;
-            if (x >= kRows * (D / 4)) break;
+        const int per = (Geo::kSums + a.ctas - 1) / a.ctas;                            // float4 of a CTA of a cluster
+        if (a.ctas > 1) {
+            if (tid == 0) mbar_arrive_expect_tx(&sh.ready, (uint32_t)(a.ctas * ((Geo::kSums - rank + a.ctas - 1) / a.ctas) * 24));
+            // what was sent the last time has been read
+            if (joins > 0 && !dead && !mbar_wait_cluster(&sh.taken, (joins - 1) & 1, wl)) {
+                report_timeout(a.kv.status);
+                dead = true;
+            }
+        }
+#pragma unroll 1
+        for (int x = tid; x < Geo::kSums; x += kThreads) {
+            const int r = x / (D / 4), e = x % (D / 4) * 4;
             float mm = sh.m[0][r];
 #pragma unroll
             for (int y = 1; y < kWarps; ++y) mm = fmaxf(mm, sh.m[y][r]);
@@ -590,57 +605,32 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             }
             if (a.ctas == 1) {
                 put(x, acc, mm, ll);
-            } else {
-                own[k] = acc;
-                if (e == 0) sh.cm[r] = mm, sh.cl[r] = ll;
+            } else {                                                                   // to the CTA that adds up number x
+                const int to = x % a.ctas, at = rank * per + x / a.ctas;
+                st_async(&sh.sent[at], acc, &sh.ready, to);
+                st_async(&sh.sent_ml[at], make_float2(mm, ll), &sh.ready, to);
             }
         }
         if (a.ctas > 1) {
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < kOwn; ++k)
-                if (tid + k * kThreads < kRows * (D / 4)) sums[tid + k * kThreads] = own[k];
-            __syncthreads();
-            if (tid < a.ctas) mbar_arrive_cluster(mapa_rank(smem_u32(&sh.ready), tid));
             if (!dead && !mbar_wait_cluster(&sh.ready, joins & 1, wl)) {
                 report_timeout(a.kv.status);
                 dead = true;
             }
 #pragma unroll 1
-            for (int y = tid * a.ctas + rank; y < kRows * (D / 4); y += kThreads * a.ctas) {
-                const int r = y / (D / 4);
-                // all remote loads before the first use
-                float pm[kMaxCluster], pl[kMaxCluster];
-                float4 ps[kMaxCluster];
-#pragma unroll
-                for (int x = 0; x < kMaxCluster; ++x) {
-                    pm[x] = -INFINITY;
-                    if (x < a.ctas) {
-                        pm[x] = ld_cluster(sh.cm + r, x);
-                        pl[x] = ld_cluster(sh.cl + r, x);
-                        ps[x] = ld_cluster(sums + y, x);
-                    }
-                }
-                float mm = pm[0];
-#pragma unroll
-                for (int x = 1; x < kMaxCluster; ++x) mm = fmaxf(mm, pm[x]);
-                float ll = 0.f;
+            for (int y = tid; y * a.ctas + rank < Geo::kSums; y += kThreads) {
+                float mm = -INFINITY, ll = 0.f;
                 float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int x = 0; x < kMaxCluster; ++x)
-                    if (x < a.ctas && mm > -INFINITY) {
-                        const float f = ex2(pm[x] - mm);
-                        ll += f * pl[x];
-                        add(acc, f, ps[x]);
-                    }
-                put(y, acc, mm, ll);
+                for (int x = 0; x < a.ctas; ++x) mm = fmaxf(mm, sh.sent_ml[x * per + y].x);
+                for (int x = 0; x < a.ctas; ++x) {
+                    const float2 p = sh.sent_ml[x * per + y];
+                    const float f = mm > -INFINITY ? ex2(p.x - mm) : 0.f;
+                    ll += f * p.y;
+                    add(acc, f, sh.sent[x * per + y]);
+                }
+                put(y * a.ctas + rank, acc, mm, ll);
             }
             __syncthreads();
             if (tid < a.ctas) mbar_arrive_cluster(mapa_rank(smem_u32(&sh.taken), tid));
-            if (!dead && !mbar_wait_cluster(&sh.taken, joins & 1, wl)) {
-                report_timeout(a.kv.status);
-                dead = true;
-            }
             dead = __any_sync(0xFFFFFFFFu, dead);
             ++joins;
         }
@@ -686,14 +676,27 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 }
 
 template <typename T, bool Q8, int D, int NT>
-cudaError_t launch(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttendArgs &a, int sms, cudaStream_t stream)
+cudaError_t launch(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttendArgs &args, int sms, cudaStream_t stream)
 {
+    using Geo = Geometry<Q8, D, NT>;
     constexpr int kSmem = (int)sizeof(Shared<Q8, D, NT>);
     static_assert(kSmem <= 232448, "shared memory");
+    AttendArgs a = args;
+    // Fewer items than half the SMs: clusters share them.  No more CTAs than give every warp a tile of the longest sequence
+    // that the table can hold.
+    const long long items = (long long)a.kv.B * a.kv.heads * (((long long)a.max_chunk * a.group + Geo::kRows - 1) / Geo::kRows);
+    const long long positions = (long long)a.kv.width << a.kv.page_shift, tile = Geo::kWarps * kTile;
+    long long ctas = sms / items;
+    if (ctas > (positions + tile - 1) / tile) ctas = (positions + tile - 1) / tile;
+    // Clusters leave SMs idle (of 148, clusters of 8 use at most 128 or so) but save the join through global memory, about 3 us:
+    // not where a CTA's share of the cache may take longer than some 20 us (1 MB).
+    if (items * positions * 2 * Geo::kRowBytes / sms > 1 << 20) ctas = 1;
+    a.ctas = (int)(ctas < 1 ? 1 : ctas > kMaxCluster ? kMaxCluster : ctas);
+    a.by_unit = FastDiv((uint32_t)tile * a.ctas);
     auto kernel = attend_mma_kernel<T, Q8, D, NT>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
-    return launch_workers(kernel, kThreads, kSmem, a.ctas, sms, stream, k_map, v_map, a);
+    return launch_workers(kernel, Geo::kThreads, kSmem, a.ctas, sms, stream, k_map, v_map, a);
 }
 template <typename T, bool Q8>
 cudaError_t by_shape(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttendArgs &a, int sms, cudaStream_t stream)
@@ -710,19 +713,7 @@ size_t attend_mma_part_floats(int sms, int d) { return (size_t)sms * 2 * 16 * (d
 cudaError_t launch_attend_mma(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttendArgs &args, int sms, cudaStream_t stream)
 {
     AttendArgs a = args;
-    // One tile of 8 rows if the longest chunk fits it, otherwise of 16.
-    const long long rows = (long long)a.max_chunk * a.group;
-    a.by_rows = FastDiv(rows <= 8 ? 8 : 16);
-    // Fewer items than half the SMs: clusters share them.  No more CTAs than give every warp a tile of the longest sequence
-    // that the table can hold.
-    const long long items = (long long)a.kv.B * a.kv.heads * ((rows + 15) / 16), positions = (long long)a.kv.width << a.kv.page_shift;
-    long long ctas = sms / items;
-    if (ctas > (positions + kWarps * kTile - 1) / (kWarps * kTile)) ctas = (positions + kWarps * kTile - 1) / (kWarps * kTile);
-    // Clusters leave SMs idle (of 148, clusters of 8 use at most 128 or so) but save the join through global memory, about 3 us:
-    // not where a CTA's share of the cache may take longer than some 20 us (1 MB).
-    if (items * positions * 2 * a.kv.d * (a.kv.k_exps ? 1 : 2) / sms > 1 << 20) ctas = 1;
-    a.ctas = (int)(ctas < 1 ? 1 : ctas > kMaxCluster ? kMaxCluster : ctas);
-    a.by_unit = FastDiv(kWarps * kTile * a.ctas);
+    a.by_rows = FastDiv((long long)a.max_chunk * a.group <= 8 ? 8 : 16);       // a row tile
     const bool q8 = a.kv.k_exps != nullptr;
     if (a.kv.dtype == kF16) return q8 ? by_shape<__half, true>(k_map, v_map, a, sms, stream) : by_shape<__half, false>(k_map, v_map, a, sms, stream);
     return q8 ? by_shape<__nv_bfloat16, true>(k_map, v_map, a, sms, stream) : by_shape<__nv_bfloat16, false>(k_map, v_map, a, sms, stream);

@@ -148,6 +148,19 @@ __device__ __forceinline__ float4 ld_cluster(const float4 *p, uint32_t rank)
     asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(mapa_rank(smem_u32(p), rank)) : "memory");
     return x;
 }
+// Sends to CTA `rank` of the cluster; its barrier (at the same place as `bar` here) counts the bytes when they have arrived.
+__device__ __forceinline__ void st_async(float4 *p, const float4 &x, uint64_t *bar, uint32_t rank)
+{
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(mapa_rank(smem_u32(p), rank)),
+                 "f"(x.x), "f"(x.y), "f"(x.z), "f"(x.w), "r"(mapa_rank(smem_u32(bar), rank))
+                 : "memory");
+}
+__device__ __forceinline__ void st_async(float2 *p, const float2 &x, uint64_t *bar, uint32_t rank)
+{
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(mapa_rank(smem_u32(p), rank)),
+                 "f"(x.x), "f"(x.y), "r"(mapa_rank(smem_u32(bar), rank))
+                 : "memory");
+}
 // Bounded wait on a barrier that other CTAs of the cluster arrive on.
 __device__ __forceinline__ bool mbar_wait_cluster(uint64_t *bar, uint32_t parity, long long limit)
 {
@@ -218,6 +231,7 @@ struct KvPlan {
     int n;                      // workers (0: a piece each)
     int b, rt, head, kt;        // item of unit u, and its place there
     int pieces, piece;          // of the item, and this worker's
+    unsigned L;                 // units of a piece
     int c0;
     bool first;
     Chunk c;
@@ -244,8 +258,8 @@ struct KvPlan {
         return (int)(t < big ? quotient(t, even + 1) : more + quotient(t - big, even));
     }
 
-    // Called by all 32 lanes of a warp of worker `me` of `count`; false = nothing to do.
-    __device__ bool start(const AttendArgs &a, int lane, int me, int count)
+    // Any number of sequences and units.
+    __device__ __noinline__ bool start_any(const AttendArgs &a, int lane, int me, int count)
     {
         const int B = a.kv.B;
         // units, items and the largest item
@@ -271,7 +285,7 @@ struct KvPlan {
         n = (int)min((long long)count, W);
         even = quotient(W, n);
         more = W - even * n;
-        unsigned L = each ? (most + each - 1) / each : 0;
+        L = each ? (most + each - 1) / each : 0;
         long long find = me;
         if (each && L <= even + 1 + even / 8 + 4) {
             n = 0;
@@ -328,6 +342,76 @@ struct KvPlan {
         return true;
     }
 
+    // Called by all 32 lanes of a warp of worker `me` of `count`; false = nothing to do.  Up to 32 sequences with fewer
+    // than 2^24 units in all, a lane has one and everything fits 32 bits: a small call's time is latency, this included.
+    __device__ bool start(const AttendArgs &a, int lane, int me, int count)
+    {
+        const int B = a.kv.B, H = a.kv.heads;
+        Chunk k{0, 0, 0, 0};
+        unsigned nr = 0, own = 0, most = 0;
+        if (lane < B) {
+            k = kv_chunk(a.kv, lane);
+            own = pieces_of(a, k, 1, &most, &nr);
+        }
+        most = __reduce_max_sync(0xFFFFFFFFu, most);
+        const unsigned rows = __reduce_max_sync(0xFFFFFFFFu, nr);
+        if (B > 32 || (long long)rows * most * H >= 1 << 19) return start_any(a, lane, me, count);
+        const unsigned w = __reduce_add_sync(0xFFFFFFFFu, own) * H, items = __reduce_add_sync(0xFFFFFFFFu, nr) * H;
+        W = w;
+        first = true;
+        if (w == 0) return false;
+        unsigned find = me;
+        L = 0;
+        if (items <= (unsigned)count) {
+            const unsigned each = (unsigned)count / items;
+            L = (most + each - 1) / each;
+        }
+        if (L > 0 && L * count <= w + w / 8 + 5 * count) {
+            n = 0;
+            if (rows == 1) {
+                own = L == 1 ? own : (own + L - 1) / L;
+            } else {
+                unsigned m, i;
+                own = lane < B ? pieces_of(a, k, L, &m, &i) : 0;
+            }
+        } else {
+            L = 1;
+            n = min(count, (int)w);
+            if (me >= n) return false;
+            even = w / n;
+            more = w - (unsigned)even * n;
+            u = begin(me);
+            hi = begin(me + 1);
+            find = (unsigned)u;
+        }
+        own *= H;
+        unsigned incl = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        const unsigned hit = __ballot_sync(0xFFFFFFFFu, incl > find);
+        if (!hit) return false;
+        b = __ffs(hit) - 1;
+        unsigned rest = find - __shfl_sync(0xFFFFFFFFu, incl - own, b);
+        c.row0 = __shfl_sync(0xFFFFFFFFu, k.row0, b);
+        c.len = __shfl_sync(0xFFFFFFFFu, k.len, b);
+        c.ctx = __shfl_sync(0xFFFFFFFFu, k.ctx, b);
+        c.total = __shfl_sync(0xFFFFFFFFu, k.total, b);
+#pragma unroll 1
+        for (rt = 0;; ++rt) {
+            const unsigned units = Shape::units(a, c, rt);
+            pieces = (int)(L == 1 ? units : (units + L - 1) / L);
+            if (rest < (unsigned)pieces * H) break;
+            rest -= pieces * H;
+        }
+        head = pieces == 1 ? (int)rest : (int)(rest / (unsigned)pieces);
+        kt = piece = (int)(rest - (unsigned)head * pieces);
+        c0 = me - piece;
+        return true;
+    }
+
     // The next segment; false when the worker has done its share.  Uniform over the worker.
     __device__ bool next(const AttendArgs &a, Segment &s)
     {
@@ -339,8 +423,8 @@ struct KvPlan {
         s.slot = first ? 0 : 1;
         first = false;
         if (n == 0) {
-            s.kt0 = (int)quotient((long long)units * piece, pieces);
-            s.kt1 = (int)quotient((long long)units * (piece + 1), pieces);
+            s.kt0 = piece * (int)L;
+            s.kt1 = min(units, s.kt0 + (int)L);
             s.c0 = c0;
             s.c1 = c0 + pieces - 1;
             s.slot0 = 0;
