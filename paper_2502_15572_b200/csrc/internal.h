@@ -222,17 +222,21 @@ struct AttendArgs {
     void *out;                  // [rows][heads * group][d]
     float *lse;                 // [rows][heads * group] or null
     float *part;                // partial results: see kv_plan.cuh
-    unsigned int *tickets;      // one per SM, all zero between calls
+    unsigned int *tickets;      // one per worker, all zero between calls
     int max_chunk;              // the longest chunk (only the choice of kernel depends on it)
     FastDiv by_group;           // group
     FastDiv by_rows;            // rows (few rows) or tokens (many) of a row tile
     FastDiv by_unit;            // positions (few rows) or 128-position tiles (many) of a unit of work
     int ctas;                   // CTAs of a worker: 1, or a cluster (see kv_plan.cuh)
+    int groups;                 // workers of a CTA (few rows; then ctas is 1)
+    int fixed;                  // what an item costs besides its units, in units
+    int small;                  // the plan's numbers fit 32 bits
     long long wait_cycles;      // bound of every device-side wait in cycles, 0 = default
     int lose_stage;             // test hook: CTA 0 never receives tile (value - 1); 0 = off
 };
 // Few rows per key/value head (at most 16) or a scale that is not positive: mma.sync.
 // Tensor maps over the cache's rows: boxes of 16 rows x 64 elements (8-bit: x d bytes), swizzled.
+size_t attend_mma_workers(int sms);                       // tickets
 size_t attend_mma_part_floats(int sms, int d);            // floats of `part`
 cudaError_t launch_attend_mma(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttendArgs &a, int sms, cudaStream_t stream);
 // More rows: tcgen05.  Tensor maps: k, v over the cache's rows [layers x pages x heads x page][d] (boxes of 64 elements

@@ -27,8 +27,9 @@
 // Which position is which row of the instruction is free as well: row g is position g ^ (g odd ? 4 : 0), which together
 // with the 128-byte swizzle of the copies makes the reads of keys and of values free of bank conflicts.
 //
-// Work is divided as kv_plan.cuh says; the warps of a CTA (and the CTAs of a cluster) take every
-// (warps x CTAs)-th tile of a segment and are joined at its end.  The maximum is only raised when a score passes it by 2^8
+// Work is divided as kv_plan.cuh says.  With few items a worker is a CTA or a cluster; with more items than SMs it is a group of
+// four warps, so that what a segment costs besides its tiles (queries, join) is hidden behind the tiles of the
+// other groups.  The warps of a worker take every (warps)-th tile of a segment and are joined at its end.  The maximum is only raised when a score passes it by 2^8
 // (weights stay far inside the range of either type), which saves the shuffles of the maximum on most tiles.
 #include "kv_plan.cuh"
 
@@ -36,6 +37,8 @@ namespace dresd {
 namespace {
 
 constexpr int kTile = 16;
+constexpr int kGroup = 4;                // warps of a group
+constexpr int kFixed = 4;
 constexpr float kSlack = 8.f;           // log2 of the largest weight before the maximum is raised
 
 template <typename T>
@@ -92,15 +95,15 @@ struct Shared {
     float m[Geo::kWarps][Geo::kRows], l[Geo::kWarps][Geo::kRows];
     uint64_t full[Geo::kWarps][Geo::kStages];
     uint64_t ready, taken;
-    Job job[4];
-    unsigned ticket;
+    Job job[Geo::kWarps / kGroup][4];
+    unsigned ticket[Geo::kWarps / kGroup];
 };
 
-// Parts of shared items: per CTA two slots of `rows` x (d + 2) floats: the sums, then the rows' maxima, then the
+// Parts of shared items: per group (or CTA) two slots of `rows` x (d + 2) floats: the sums, then the rows' maxima, then the
 // rows' weight sums.
-__device__ __forceinline__ float *part_slot(const AttendArgs &a, int cta, int slot, int rows)
+__device__ __forceinline__ float *part_slot(const AttendArgs &a, int worker, int slot, int rows)
 {
-    return a.part + ((size_t)cta * 2 + slot) * rows * (a.kv.d + 2);
+    return a.part + ((size_t)worker * 2 + slot) * rows * (a.kv.d + 2);
 }
 
 template <int kBytes> struct Piece;                       // a lane's load
@@ -135,7 +138,14 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     const long long wl = a.wait_cycles > 0 ? a.wait_cycles : kWaitCycles;
     const int rank = a.ctas > 1 ? (int)cluster_ctarank() : 0;
-    const int step = kWarps * a.ctas;                      // a warp takes every step-th tile
+    const bool grouped = a.groups > 1;                     // then not in clusters
+    const int g_warps = grouped ? kGroup : kWarps, group = warp / g_warps, first_warp = group * g_warps;
+    const int g_tid = tid - first_warp * 32, g_threads = g_warps * 32;
+    const int worker = grouped ? blockIdx.x * a.groups + group : blockIdx.x;       // of a cluster each CTA has its own parts
+    const int step = g_warps * a.ctas;                     // a warp takes every step-th tile
+    const int mine = rank * kWarps + warp - first_warp;    // starting here
+    Job *jobs = sh.job[group];
+    auto sync = [&] { bar_sync(1 + group, g_threads); };
 
     if (lane == 0) {
         for (int s = 0; s < kStages; ++s) mbar_init(&sh.full[warp][s], 1);
@@ -150,23 +160,22 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     pdl_wait();                                             // what follows reads what earlier kernels wrote
     pdl_launch_dependents();
 
-    // Warp 0 works out the segments, one ahead of the present one.
+    // The worker's first warp works out the segments, one ahead of the present one.
     KvPlan<FewRows> plan;
     bool more = false;
     auto publish = [&](int i) {
-        Job &w = sh.job[i & 3];
+        Job &w = jobs[i & 3];
         if (more) more = plan.next(a, w.seg);
         w.more = more;
         if (!more) return;
         w.c = plan.c;
-        int seen = plan.c.total;
-        if (!a.mask) seen = min(seen, plan.c.ctx + min(plan.c.len - 1, a.by_group.div((w.seg.rt + 1) * kRows - 1)) + 1);
+        const int seen = FewRows::seen(a, plan.c, w.seg.rt);
         w.t0 = w.seg.kt0 * step;
         w.t1 = min(w.seg.kt1 * step, (seen + kTile - 1) / kTile);
-        plan.advance(a);
     };
-    if (warp == 0) {
-        more = plan.start(a, lane, blockIdx.x / a.ctas, gridDim.x / a.ctas);       // the same for the whole cluster
+    if (warp == first_warp) {
+        more = grouped ? plan.start(a, lane, worker, gridDim.x * a.groups)
+                       : plan.start(a, lane, blockIdx.x / a.ctas, gridDim.x / a.ctas);         // the same for the whole cluster
         if (lane == 0) {
             publish(0);
             publish(1);
@@ -190,10 +199,10 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         while (f_tile >= f_end) {                          // on to the next segment
             pending = false;
             if (f_job >= i + 1) return;
-            const Job &w = sh.job[(f_job + 1) & 3];
+            const Job &w = jobs[(f_job + 1) & 3];
             if (!w.more) return;
             ++f_job;
-            f_tile = w.t0 + rank * kWarps + warp;
+            f_tile = w.t0 + mine;
             f_end = w.t1;
             f_total = w.c.total;
             f_head = w.seg.head;
@@ -234,7 +243,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     int used = 0, joins = 0;
     bool dead = false;
     for (int i = 0;; ++i) {
-        const Job &w = sh.job[i & 3];
+        const Job &w = jobs[i & 3];
         if (!w.more) break;
         const Segment &seg = w.seg;
         const Chunk ch = w.c;
@@ -299,7 +308,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         for (int nt = 0; nt < NT; ++nt) m[nt][0] = m[nt][1] = -INFINITY, l[nt][0] = l[nt][1] = 0.f;
 
 #pragma unroll 1
-        for (int t = w.t0 + rank * kWarps + warp; t < w.t1; t += step) {
+        for (int t = w.t0 + mine; t < w.t1; t += step) {
             const int p0 = t * kTile, s = used % kStages;
             if (!dead && !mbar_wait(&sh.full[warp][s], (used / kStages) & 1, wl)) {
                 report_timeout(a.kv.status);
@@ -310,7 +319,6 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             // ---- S^T = K Q^T; lane (g, c): keys place(g) (+ 8)
             float sc[NT][4] = {};
             uint4 kx[2][kKeyPieces];
-            VPiece vx[4][kValPieces];
             int ke[2] = {127, 127}, ve[2] = {127, 127};
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -326,25 +334,6 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     ke[j] = min((int)sh.exps[warp][s][0][r], 253);
                     ve[j] = min((int)sh.exps[warp][s][1][r], 253);
                 }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {                  // values of positions place(2 c), place(2 c + 1) (+ 8)
-                const int r = (j >> 1) * 8 + place(2 * c + (j & 1));
-#pragma unroll
-                for (int x = 0; x < kValPieces; ++x) {
-                    if constexpr (kRowBytes == 64) {
-                        vx[j][x] = *reinterpret_cast<const VPiece *>(vs_ + r * 64 + (((g >> 1) ^ ((r >> 1) & 3)) << 4) + (g & 1) * 8);
-                    } else {
-                        vx[j][x] = *reinterpret_cast<const VPiece *>(vs_ + x * (kTile * 128) + r * 128 + ((g ^ (r & 7)) << 4));
-                    }
-                }
-            }
-            ++used;
-            __syncwarp();                                  // the tile is in registers: ask for the next one
-            if (pending) {
-                if (lane == 0) fetch();
-                ++fetched;
-                look_ahead(i);
             }
             if constexpr (!Q8) {
 #pragma unroll
@@ -363,6 +352,26 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     for (int nt = 0; nt < NT; ++nt)
                         mma16816<M>(sc[nt], f[0][0], f[1][0], f[0][1], f[1][1], q[nt][st][0], q[nt][st][1]);
                 }
+            }
+            VPiece vx[4][kValPieces];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {                  // values of positions place(2 c), place(2 c + 1) (+ 8)
+                const int r = (j >> 1) * 8 + place(2 * c + (j & 1));
+#pragma unroll
+                for (int x = 0; x < kValPieces; ++x) {
+                    if constexpr (kRowBytes == 64) {
+                        vx[j][x] = *reinterpret_cast<const VPiece *>(vs_ + r * 64 + (((g >> 1) ^ ((r >> 1) & 3)) << 4) + (g & 1) * 8);
+                    } else {
+                        vx[j][x] = *reinterpret_cast<const VPiece *>(vs_ + x * (kTile * 128) + r * 128 + ((g ^ (r & 7)) << 4));
+                    }
+                }
+            }
+            ++used;
+            __syncwarp();                                  // the tile is in registers: ask for the next one
+            if (pending) {
+                if (lane == 0) fetch();
+                ++fetched;
+                look_ahead(i);
             }
             // ---- scale, mask.  sc[nt][2 j + x]: key place(g) + 8 j, row 2 c + x
             const bool all_seen = p0 + kTile <= ch.ctx && p0 + kTile <= ch.total;
@@ -551,11 +560,11 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         make_float4(o[nt][st][x] * f, o[nt][st][2 + x] * f, o[nt][st + 1][x] * f, o[nt][st + 1][2 + x] * f);
                 }
             }
-        __syncthreads();
-        if (warp == 0 && lane == 0) publish(i + 2);
+        sync();
+        if (g_tid == 0) publish(i + 2);
         const int heads = a.kv.heads * a.group;
         const bool split = seg.c0 != seg.c1;
-        float *part = part_slot(a, blockIdx.x, seg.slot, kRows);
+        float *part = part_slot(a, worker, seg.slot, kRows);
         auto finish = [&](int r, int e, const float4 &acc, float mm, float ll) {       // four elements of a row's result
             const float inv = ll > 0.f ? 1.f / ll : ll == 0.f ? 0.f : ll;              // a NaN sum stays one
             const int rr = seg.rt * kRows + r, tok = a.by_group.div(rr);
@@ -590,15 +599,15 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             }
         }
 #pragma unroll 1
-        for (int x = tid; x < Geo::kSums; x += kThreads) {
+        for (int x = g_tid; x < Geo::kSums; x += g_threads) {
             const int r = x / (D / 4), e = x % (D / 4) * 4;
-            float mm = sh.m[0][r];
-#pragma unroll
-            for (int y = 1; y < kWarps; ++y) mm = fmaxf(mm, sh.m[y][r]);
+            float mm = -INFINITY;
+#pragma unroll 4
+            for (int y = first_warp; y < first_warp + g_warps; ++y) mm = fmaxf(mm, sh.m[y][r]);
             float ll = 0.f;
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int y = 0; y < kWarps; ++y) {
+#pragma unroll 4
+            for (int y = first_warp; y < first_warp + g_warps; ++y) {
                 const float f = mm > -INFINITY ? ex2(sh.m[y][r] - mm) : 0.f;
                 ll += f * sh.l[y][r];
                 add(acc, f, *reinterpret_cast<const float4 *>(&sh.o[y][r][e]));
@@ -636,14 +645,14 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         }
         if (split) {
             __threadfence();
-            __syncthreads();
-            if (tid == 0) sh.ticket = atomicAdd(a.tickets + seg.c0 * a.ctas + rank, 1u);
-            __syncthreads();
-            if (sh.ticket == (unsigned)(seg.c1 - seg.c0)) {                      // the last of them: join the parts in order
+            sync();
+            if (g_tid == 0) sh.ticket[group] = atomicAdd(a.tickets + seg.c0 * a.ctas + rank, 1u);
+            sync();
+            if (sh.ticket[group] == (unsigned)(seg.c1 - seg.c0)) {                      // the last of them: join the parts in order
                 __threadfence();
-                if (tid == 0) a.tickets[seg.c0 * a.ctas + rank] = 0;
+                if (g_tid == 0) a.tickets[seg.c0 * a.ctas + rank] = 0;
 #pragma unroll 1
-                for (int x = tid * a.ctas + rank; x < rows * (D / 4); x += kThreads * a.ctas) {
+                for (int x = g_tid * a.ctas + rank; x < rows * (D / 4); x += g_threads * a.ctas) {
                     const int r = x / (D / 4), e = x % (D / 4) * 4;
                     float mm = -INFINITY, ll = 0.f;
                     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -663,7 +672,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 }
             }
         }
-        __syncthreads();                                    // the join's buffers are written again; job i + 2 is known
+        sync();                                             // the join's buffers are written again; job i + 2 is known
     }
     // no copy may be in flight when the CTA ends: all fetched tiles have been used unless a wait ran out
     for (; used < fetched; ++used)
@@ -692,7 +701,13 @@ cudaError_t launch(const CUtensorMap &k_map, const CUtensorMap &v_map, const Att
     // not where a CTA's share of the cache may take longer than some 20 us (1 MB).
     if (items * positions * 2 * Geo::kRowBytes / sms > 1 << 20) ctas = 1;
     a.ctas = (int)(ctas < 1 ? 1 : ctas > kMaxCluster ? kMaxCluster : ctas);
-    a.by_unit = FastDiv((uint32_t)tile * a.ctas);
+    // More items than SMs: a CTA's groups work on items of their own.
+    a.groups = items > sms ? Geo::kWarps / kGroup : 1;
+    const int unit = (int)tile * a.ctas / a.groups;
+    a.by_unit = FastDiv(unit);
+    // Queries and join of a segment take about as long as four tiles of a warp.
+    a.fixed = kFixed;
+    a.small = a.kv.heads * (a.kv.B + (long long)a.kv.rows * a.group / Geo::kRows + 1) * (positions / unit + 1 + a.fixed) < 1LL << 30;
     auto kernel = attend_mma_kernel<T, Q8, D, NT>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
@@ -708,7 +723,8 @@ cudaError_t by_shape(const CUtensorMap &k_map, const CUtensorMap &v_map, const A
 
 }  // namespace
 
-size_t attend_mma_part_floats(int sms, int d) { return (size_t)sms * 2 * 16 * (d + 2); }
+size_t attend_mma_workers(int sms) { return (size_t)sms * 16 / kGroup; }
+size_t attend_mma_part_floats(int sms, int d) { return attend_mma_workers(sms) * 2 * 16 * (d + 2); }
 
 cudaError_t launch_attend_mma(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttendArgs &args, int sms, cudaStream_t stream)
 {

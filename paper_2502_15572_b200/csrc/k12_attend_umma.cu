@@ -39,6 +39,7 @@ namespace {
 constexpr int kTile = 128;                                 // rows of a row tile, positions of a tile
 constexpr int kSlabBytes = kTile * 128;                    // 64 elements of every row of a tile
 constexpr float kSlack = 8.f;
+constexpr int kFixed = 2;                                  // queries and join of a segment take about as long as two tiles
 
 template <bool Q8, int D>
 struct Geometry {
@@ -566,8 +567,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     mbar_arrive(&sh.job_full[i & 1]);
                     if (!more) break;
                     const int tiles = w.one ? 1 : 2, y = w.seg.head * a.group, z = plan.c.row0 + 2 * w.seg.rt * tokens;
-                    plan.advance(a);
-#pragma unroll 1
+            #pragma unroll 1
                     for (int st = 0; st < tiles && ok; ++st) {
                         int &uses = st ? uses1 : uses0;
                         if (uses > 0) ok = mbar_wait(&sh.q_empty[st], (uses - 1) & 1, wl);
@@ -1090,6 +1090,9 @@ cudaError_t launch_attend_umma(const CUtensorMap &q_map, const CUtensorMap &k_ma
     a.ctas = (int)(ctas < 1 ? 1 : ctas > kMaxCluster ? kMaxCluster : ctas);
     a.by_rows = FastDiv(2 * (kTile / a.group));
     a.by_unit = FastDiv(2 * a.ctas);
+    a.groups = 1;
+    a.fixed = kFixed;
+    a.small = a.kv.heads * (a.kv.B + (long long)a.kv.rows * a.group / kTile + 1) * (tiles + 1 + a.fixed) < 1LL << 30;
     const bool q8 = a.kv.k_exps != nullptr;
     if (a.kv.dtype == kF16) {
         if (a.kv.d == 64) return q8 ? launch<__half, true, 64>(q_map, k_map, v_map, a, sms, stream) : launch<__half, false, 64>(q_map, k_map, v_map, a, sms, stream);

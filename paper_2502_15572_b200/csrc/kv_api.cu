@@ -191,7 +191,7 @@ dresd_status dresd_kv_create(void *k_pages, void *v_pages, uint8_t *k_exps, uint
         free_kv(kv);
         return fail_cuda(e, "device query");
     }
-    const size_t tickets = sizeof(unsigned int) * (size_t)kv->sms;
+    const size_t tickets = sizeof(unsigned int) * attend_mma_workers(kv->sms);
     const size_t few = attend_mma_part_floats(kv->sms, head_dim), many = attend_umma_part_floats(kv->sms, head_dim);
     const cuuint64_t dims[2] = {(cuuint64_t)head_dim, (cuuint64_t)layers * num_pages * kv_heads * page_size};
     const cuuint64_t strides[1] = {(cuuint64_t)head_dim * (k_exps ? 1 : 2)};
@@ -350,7 +350,7 @@ dresd_status dresd_kv_status(dresd_kv *kv)
     if (word == 0) return DRESD_OK;
     e = cudaMemset(kv->args.status, 0, sizeof(int));
     // a kernel that gave up may have left tickets behind
-    if (e == cudaSuccess) e = cudaMemset(kv->tickets, 0, sizeof(unsigned int) * (size_t)kv->sms);
+    if (e == cudaSuccess) e = cudaMemset(kv->tickets, 0, sizeof(unsigned int) * attend_mma_workers(kv->sms));
     if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
     if (e != cudaSuccess) return fail_cuda(e, "status reset");
     if (word <= -1000) return fail(DRESD_ERR_INTERNAL, "bounds check %d failed inside a kernel", -1000 - word);

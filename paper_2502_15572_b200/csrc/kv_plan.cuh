@@ -192,10 +192,11 @@ __device__ __forceinline__ float ex2(float x)
 // them and join their results through shared memory.  Worker i of n gets
 //
 //   few items: a piece of ONE item.  With n / items workers for each, items are cut into pieces of at most L units, if L is
-//       within an eighth and four units of an even share W / n: nobody starts a second item, whose fixed cost (queries,
+//       within an eighth and five units of an even share W / n: nobody starts a second item, whose fixed cost (queries,
 //       join) is several units.
-//   otherwise: an even share of all W units in the order (sequence, row tile, head), so that the workers finish together
-//       however ragged the batch is; a worker has the tail of one item, some whole items and the head of another.
+//   otherwise: an even share of a line of all items in the order (sequence, row tile, head), so that the workers finish
+//       together however ragged the batch is; a worker has the tail of one item, some whole items and the head of another.
+//       An item is as long as its units and `fixed` places before them, which stand for that fixed cost.
 //
 // Parts of an item are joined by the worker that finishes it last, in the order of the workers, so results do not depend
 // on timing.
@@ -210,33 +211,26 @@ struct Segment {
 // Shape of the kernel for few rows: tiles of by_rows.d rows, units of by_unit.d positions.
 struct FewRows {
     static __device__ __forceinline__ int row_tiles(const AttendArgs &a, const Chunk &k) { return a.by_rows.ceil(k.len * a.group); }
-    static __device__ __forceinline__ int units(const AttendArgs &a, const Chunk &k, int r)
+    static __device__ __forceinline__ int seen(const AttendArgs &a, const Chunk &k, int r)         // positions
     {
-        int seen = k.total;
-        if (!a.mask) seen = min(seen, k.ctx + min(k.len - 1, a.by_group.div((r + 1) * (int)a.by_rows.d - 1)) + 1);
-        return max(1, a.by_unit.ceil(seen));
+        return a.mask ? k.total : min(k.total, k.ctx + min(k.len - 1, a.by_group.div((r + 1) * (int)a.by_rows.d - 1)) + 1);
     }
+    static __device__ __forceinline__ int units(const AttendArgs &a, const Chunk &k, int r) { return max(1, a.by_unit.ceil(seen(a, k, r))); }
 };
-
-// Quotients of numbers that nearly always fit 32 bits.
-__device__ __forceinline__ long long quotient(long long a, long long b)
-{
-    return ((unsigned long long)(a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
-}
 
 template <typename Shape>
 struct KvPlan {
-    long long W, hi, u;         // units in all; end of this worker's; next unit
-    long long even, more;       // the first `more` workers have even + 1 units, the others even
+    long long hi, u;            // end of this worker's part of the line; its next place
+    long long even, more;       // the first `more` workers have even + 1 places, the others even
     int n;                      // workers (0: a piece each)
-    int b, rt, head, kt;        // item of unit u, and its place there
+    int b, rt, head, kt;        // item of place u, and the place in it
     int pieces, piece;          // of the item, and this worker's
     unsigned L;                 // units of a piece
     int c0;
     bool first;
     Chunk c;
 
-    // Units of sequence bb for one head in pieces of at most L (L = 1: the units), its largest item, its row tiles.
+    // Units of a sequence for one head in pieces of at most L, its largest item, its row tiles.
     static __device__ __forceinline__ unsigned pieces_of(const AttendArgs &a, const Chunk &k, unsigned L, unsigned *most, unsigned *items)
     {
         const int nr = Shape::row_tiles(a, k);
@@ -252,162 +246,104 @@ struct KvPlan {
         return p;
     }
     __device__ __forceinline__ long long begin(int i) const { return i * even + min((long long)i, more); }
+    static __device__ __forceinline__ long long quotient(long long x, long long y)      // nearly always in 32 bits
+    {
+        return ((unsigned long long)(x | y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
+    }
     __device__ __forceinline__ int owner(long long t) const
     {
         const long long big = more * (even + 1);
         return (int)(t < big ? quotient(t, even + 1) : more + quotient(t - big, even));
     }
-
-    // Any number of sequences and units.
-    __device__ __noinline__ bool start_any(const AttendArgs &a, int lane, int me, int count)
+    static __device__ __forceinline__ unsigned add_lanes(unsigned x) { return __reduce_add_sync(0xFFFFFFFFu, x); }
+    static __device__ __forceinline__ long long add_lanes(long long x)
     {
-        const int B = a.kv.B;
-        // units, items and the largest item
-        W = 0;
-        unsigned items = 0, most = 0;
-        Chunk k;
 #pragma unroll 1
-        for (int b0 = 0; b0 < B; b0 += 32) {
-            unsigned m = 0, i = 0, p = 0;
-            if (b0 + lane < B) {
-                k = kv_chunk(a.kv, b0 + lane);
-                p = pieces_of(a, k, 1, &m, &i);
-            }
-            const unsigned lo = __reduce_add_sync(0xFFFFFFFFu, p & 0xFFFFu), up = __reduce_add_sync(0xFFFFFFFFu, p >> 16);
-            W += lo + ((long long)up << 16);
-            items += __reduce_add_sync(0xFFFFFFFFu, i);
-            most = max(most, __reduce_max_sync(0xFFFFFFFFu, m));
-        }
-        W *= a.kv.heads;
-        first = true;
-        if (W == 0) return false;
-        const unsigned each = (long long)items * a.kv.heads <= count ? (unsigned)count / (items * a.kv.heads) : 0;
-        n = (int)min((long long)count, W);
-        even = quotient(W, n);
-        more = W - even * n;
-        L = each ? (most + each - 1) / each : 0;
-        long long find = me;
-        if (each && L <= even + 1 + even / 8 + 4) {
-            n = 0;
-        } else {
-            L = 1;
-            if (me >= n) return false;
-            find = u = begin(me);
-            hi = begin(me + 1);
-        }
-        // the sequence that piece or unit `find` belongs to, and what comes before it
-        long long before = 0;
-        bool found = false;
-#pragma unroll 1
-        for (int b0 = 0; b0 < B; b0 += 32) {
-            unsigned m, i;
-            long long own = 0;
-            if (b0 + lane < B) {
-                if (B > 32) k = kv_chunk(a.kv, b0 + lane);
-                own = (long long)pieces_of(a, k, L, &m, &i) * a.kv.heads;
-            }
-            long long incl = own;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-                if (lane >= o) incl += x;
-            }
-            const unsigned hit = __ballot_sync(0xFFFFFFFFu, before + incl > find);
-            if (hit) {
-                const int l = __ffs(hit) - 1;
-                b = b0 + l;
-                before += __shfl_sync(0xFFFFFFFFu, incl - own, l);
-                c.row0 = __shfl_sync(0xFFFFFFFFu, k.row0, l);
-                c.len = __shfl_sync(0xFFFFFFFFu, k.len, l);
-                c.ctx = __shfl_sync(0xFFFFFFFFu, k.ctx, l);
-                c.total = __shfl_sync(0xFFFFFFFFu, k.total, l);
-                found = true;
-                break;
-            }
-            before += __shfl_sync(0xFFFFFFFFu, incl, 31);
-        }
-        if (!found) return false;
-        long long rest = find - before;
-#pragma unroll 1
-        for (rt = 0;; ++rt) {
-            const unsigned units = Shape::units(a, c, rt);
-            pieces = (int)(L == 1 ? units : (units + L - 1) / L);
-            const long long t = (long long)pieces * a.kv.heads;
-            if (rest < t) break;
-            rest -= t;
-        }
-        head = (int)quotient(rest, pieces);
-        kt = piece = (int)(rest - (long long)head * pieces);
-        c0 = me - piece;
-        return true;
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+        return x;
     }
 
-    // Called by all 32 lanes of a warp of worker `me` of `count`; false = nothing to do.  Up to 32 sequences with fewer
-    // than 2^24 units in all, a lane has one and everything fits 32 bits: a small call's time is latency, this included.
-    __device__ bool start(const AttendArgs &a, int lane, int me, int count)
+    // Called by all 32 lanes of a warp of worker `me` of `count`; false = nothing to do.  A small call's time is latency, this
+    // included: one pass over the lengths, and 32 bits where the host knows that they are enough.
+    __device__ __forceinline__ bool start(const AttendArgs &a, int lane, int me, int count)
     {
-        const int B = a.kv.B, H = a.kv.heads;
-        Chunk k{0, 0, 0, 0};
-        unsigned nr = 0, own = 0, most = 0;
-        if (lane < B) {
-            k = kv_chunk(a.kv, lane);
-            own = pieces_of(a, k, 1, &most, &nr);
+        return a.small ? start_as<unsigned>(a, lane, me, count) : start_as<long long>(a, lane, me, count);
+    }
+    template <typename Int>
+    __device__ bool start_as(const AttendArgs &a, int lane, int me, int count)
+    {
+        // a lane adds up B / 32 sequences in a row
+        const int per = (a.kv.B + 31) >> 5, H = a.kv.heads, b0 = lane * per, b1 = min(b0 + per, a.kv.B);
+        unsigned most = 0, nr = 0;
+        Int own = 0;
+#pragma unroll 1
+        for (int bb = b0; bb < b1; ++bb) {
+            unsigned m, i;
+            own += pieces_of(a, kv_chunk(a.kv, bb), 1, &m, &i);
+            most = max(most, m);
+            nr += i;
         }
         most = __reduce_max_sync(0xFFFFFFFFu, most);
-        const unsigned rows = __reduce_max_sync(0xFFFFFFFFu, nr);
-        if (B > 32 || (long long)rows * most * H >= 1 << 19) return start_any(a, lane, me, count);
-        const unsigned w = __reduce_add_sync(0xFFFFFFFFu, own) * H, items = __reduce_add_sync(0xFFFFFFFFu, nr) * H;
-        W = w;
+        const Int items = (Int)__reduce_add_sync(0xFFFFFFFFu, nr) * H, W = add_lanes(own) * H;
         first = true;
-        if (w == 0) return false;
-        unsigned find = me;
+        if (W == 0) return false;
+        Int find = me;
         L = 0;
-        if (items <= (unsigned)count) {
-            const unsigned each = (unsigned)count / items;
-            L = (most + each - 1) / each;
+        if (items <= (Int)count) {
+            const unsigned each = (unsigned)count / (unsigned)items;
+            L = each == 1 ? most : (most + each - 1) / each;
         }
-        if (L > 0 && L * count <= w + w / 8 + 5 * count) {
+        if (L > 0 && (Int)L * count <= W + W / 8 + 5 * count) {
             n = 0;
-            if (rows == 1) {
-                own = L == 1 ? own : (own + L - 1) / L;
-            } else {
-                unsigned m, i;
-                own = lane < B ? pieces_of(a, k, L, &m, &i) : 0;
+            if (L > 1) {
+                own = 0;
+#pragma unroll 1
+                for (int bb = b0; bb < b1; ++bb) {
+                    unsigned m, i;
+                    own += pieces_of(a, kv_chunk(a.kv, bb), L, &m, &i);
+                }
             }
         } else {
             L = 1;
-            n = min(count, (int)w);
+            own += (Int)nr * a.fixed;
+            const Int line = W + items * a.fixed;
+            n = (int)min((Int)count, line);
             if (me >= n) return false;
-            even = w / n;
-            more = w - (unsigned)even * n;
+            even = line / n;
+            more = line - (Int)even * n;
             u = begin(me);
             hi = begin(me + 1);
-            find = (unsigned)u;
+            find = (Int)u;
         }
         own *= H;
-        unsigned incl = own;
+        Int incl = own;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const unsigned x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            const Int x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
             if (lane >= o) incl += x;
         }
         const unsigned hit = __ballot_sync(0xFFFFFFFFu, incl > find);
         if (!hit) return false;
-        b = __ffs(hit) - 1;
-        unsigned rest = find - __shfl_sync(0xFFFFFFFFu, incl - own, b);
-        c.row0 = __shfl_sync(0xFFFFFFFFu, k.row0, b);
-        c.len = __shfl_sync(0xFFFFFFFFu, k.len, b);
-        c.ctx = __shfl_sync(0xFFFFFFFFu, k.ctx, b);
-        c.total = __shfl_sync(0xFFFFFFFFu, k.total, b);
+        const int l = __ffs(hit) - 1;
+        Int rest = find - __shfl_sync(0xFFFFFFFFu, incl - own, l);
+        b = l * per;
+        c = kv_chunk(a.kv, b);
+        rt = 0;
 #pragma unroll 1
-        for (rt = 0;; ++rt) {
+        while (true) {                                      // ends: the lane has more pieces than `rest`
+            if (rt == Shape::row_tiles(a, c)) {
+                c = kv_chunk(a.kv, ++b);
+                rt = 0;
+                continue;
+            }
             const unsigned units = Shape::units(a, c, rt);
-            pieces = (int)(L == 1 ? units : (units + L - 1) / L);
-            if (rest < (unsigned)pieces * H) break;
-            rest -= pieces * H;
+            pieces = n ? (int)units + a.fixed : (int)(L == 1 ? units : (units + L - 1) / L);
+            if (rest < (Int)pieces * H) break;
+            rest -= (Int)pieces * H;
+            ++rt;
         }
-        head = pieces == 1 ? (int)rest : (int)(rest / (unsigned)pieces);
-        kt = piece = (int)(rest - (unsigned)head * pieces);
+        head = pieces == 1 ? (int)rest : (int)(rest / (Int)pieces);
+        kt = piece = (int)(rest - (Int)head * pieces);
         c0 = me - piece;
         return true;
     }
@@ -415,44 +351,52 @@ struct KvPlan {
     // The next segment; false when the worker has done its share.  Uniform over the worker.
     __device__ bool next(const AttendArgs &a, Segment &s)
     {
-        if (n == 0 ? !first : u >= hi) return false;
-        const int units = Shape::units(a, c, rt);
-        s.b = b;
-        s.rt = rt;
-        s.head = head;
-        s.slot = first ? 0 : 1;
-        first = false;
         if (n == 0) {
+            if (!first) return false;
+            first = false;
+            s.b = b;
+            s.rt = rt;
+            s.head = head;
             s.kt0 = piece * (int)L;
-            s.kt1 = min(units, s.kt0 + (int)L);
+            s.kt1 = min(Shape::units(a, c, rt), s.kt0 + (int)L);
             s.c0 = c0;
             s.c1 = c0 + pieces - 1;
-            s.slot0 = 0;
+            s.slot = s.slot0 = 0;
             return true;
         }
-        s.kt0 = kt;
-        s.kt1 = (int)min((long long)units, kt + (hi - u));
-        const long long item = u - kt;
-        s.c0 = owner(item);
-        s.c1 = owner(item + units - 1);
-        s.slot0 = begin(s.c0) == item ? 0 : 1;
-        u += s.kt1 - s.kt0;
-        kt = s.kt1;
-        return true;
-    }
-    // Moves on to the next item (call after the segment's work, when its chunk is no longer needed).
-    __device__ void advance(const AttendArgs &a)
-    {
-        if (n == 0 || u >= hi || kt < Shape::units(a, c, rt)) return;
-        kt = 0;
-        if (++head < a.kv.heads) return;
-        head = 0;
-        if (++rt < Shape::row_tiles(a, c)) return;
-        rt = 0;
-        do {
-            ++b;
-            c = kv_chunk(a.kv, b);
-        } while (c.len == 0);            // ends: u < hi means that a later sequence has units
+#pragma unroll 1
+        while (u < hi) {
+            const int size = Shape::units(a, c, rt) + a.fixed;
+            if (kt == size) {                                // on to the next item (there is one: u < hi)
+                kt = 0;
+                if (++head < a.kv.heads) continue;
+                head = 0;
+                ++rt;
+#pragma unroll 1
+                while (rt >= Shape::row_tiles(a, c)) {
+                    c = kv_chunk(a.kv, ++b);
+                    rt = 0;
+                }
+                continue;
+            }
+            const long long item = u - kt;
+            const int end = (int)min((long long)size, kt + (hi - u));
+            s.kt0 = max(kt - a.fixed, 0);
+            s.kt1 = end - a.fixed;
+            u += end - kt;
+            kt = end;
+            if (s.kt1 <= s.kt0) continue;                    // the fixed part alone: its units are the next worker's
+            s.b = b;
+            s.rt = rt;
+            s.head = head;
+            s.c0 = owner(item + a.fixed);
+            s.c1 = owner(item + size - 1);
+            s.slot = first ? 0 : 1;
+            s.slot0 = begin(s.c0) >= item ? 0 : 1;
+            first = false;
+            return true;
+        }
+        return false;
     }
 };
 
