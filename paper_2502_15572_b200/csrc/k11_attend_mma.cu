@@ -28,7 +28,7 @@
 // with the 128-byte swizzle of the copies makes the reads of keys and of values free of bank conflicts.
 //
 // Work is divided as kv_plan.cuh says.  With few items a worker is a CTA or a cluster; with more items than SMs it is a group of
-// four warps, so that what a segment costs besides its tiles (queries, join) is hidden behind the tiles of the
+// four warps or fewer, so that what a segment costs besides its tiles (queries, join) is hidden behind the tiles of the
 // other groups.  The warps of a worker take every (warps)-th tile of a segment and are joined at its end.  The maximum is only raised when a score passes it by 2^8
 // (weights stay far inside the range of either type), which saves the shuffles of the maximum on most tiles.
 #include "kv_plan.cuh"
@@ -37,7 +37,6 @@ namespace dresd {
 namespace {
 
 constexpr int kTile = 16;
-constexpr int kGroup = 4;                // warps of a group
 constexpr int kFixed = 4;
 constexpr float kSlack = 8.f;           // log2 of the largest weight before the maximum is raised
 
@@ -95,8 +94,8 @@ struct Shared {
     float m[Geo::kWarps][Geo::kRows], l[Geo::kWarps][Geo::kRows];
     uint64_t full[Geo::kWarps][Geo::kStages];
     uint64_t ready, taken;
-    Job job[Geo::kWarps / kGroup][4];
-    unsigned ticket[Geo::kWarps / kGroup];
+    Job job[Geo::kWarps][4];                                         // of a worker
+    unsigned ticket[Geo::kWarps];
 };
 
 // Parts of shared items: per group (or CTA) two slots of `rows` x (d + 2) floats: the sums, then the rows' maxima, then the
@@ -139,13 +138,16 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     const long long wl = a.wait_cycles > 0 ? a.wait_cycles : kWaitCycles;
     const int rank = a.ctas > 1 ? (int)cluster_ctarank() : 0;
     const bool grouped = a.groups > 1;                     // then not in clusters
-    const int g_warps = grouped ? kGroup : kWarps, group = warp / g_warps, first_warp = group * g_warps;
+    const int g_warps = kWarps / a.groups, group = warp / g_warps, first_warp = group * g_warps;
     const int g_tid = tid - first_warp * 32, g_threads = g_warps * 32;
     const int worker = grouped ? blockIdx.x * a.groups + group : blockIdx.x;       // of a cluster each CTA has its own parts
     const int step = g_warps * a.ctas;                     // a warp takes every step-th tile
     const int mine = rank * kWarps + warp - first_warp;    // starting here
     Job *jobs = sh.job[group];
-    auto sync = [&] { bar_sync(1 + group, g_threads); };
+    auto sync = [&] {
+        if (g_warps == 1) __syncwarp();
+        else bar_sync(1 + group, g_threads);
+    };
 
     if (lane == 0) {
         for (int s = 0; s < kStages; ++s) mbar_init(&sh.full[warp][s], 1);
@@ -701,8 +703,12 @@ cudaError_t launch(const CUtensorMap &k_map, const CUtensorMap &v_map, const Att
     // not where a CTA's share of the cache may take longer than some 20 us (1 MB).
     if (items * positions * 2 * Geo::kRowBytes / sms > 1 << 20) ctas = 1;
     a.ctas = (int)(ctas < 1 ? 1 : ctas > kMaxCluster ? kMaxCluster : ctas);
-    // More items than SMs: a CTA's groups work on items of their own.
-    a.groups = items > sms ? Geo::kWarps / kGroup : 1;
+    // More items than SMs: a CTA's groups work on items of their own.  Small groups only where no sequence is long, because the
+    // last worker on an item joins its parts alone.
+    const int group = items >= (long long)sms * Geo::kWarps && positions <= 2048       ? 1
+                      : items >= (long long)sms * Geo::kWarps / 2 && positions <= 8192 ? 2
+                                                                                       : 4;
+    a.groups = items > sms ? Geo::kWarps / group : 1;
     const int unit = (int)tile * a.ctas / a.groups;
     a.by_unit = FastDiv(unit);
     // Queries and join of a segment take about as long as four tiles of a warp.
@@ -723,8 +729,8 @@ cudaError_t by_shape(const CUtensorMap &k_map, const CUtensorMap &v_map, const A
 
 }  // namespace
 
-size_t attend_mma_workers(int sms) { return (size_t)sms * 16 / kGroup; }
-size_t attend_mma_part_floats(int sms, int d) { return attend_mma_workers(sms) * 2 * 16 * (d + 2); }
+size_t attend_mma_workers(int sms) { return (size_t)sms * 16; }        // 16 warps with 8 rows, or 8 with 16
+size_t attend_mma_part_floats(int sms, int d) { return attend_mma_workers(sms) * 2 * 8 * (d + 2); }
 
 cudaError_t launch_attend_mma(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttendArgs &args, int sms, cudaStream_t stream)
 {
