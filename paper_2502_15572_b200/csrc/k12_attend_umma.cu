@@ -7,7 +7,7 @@
 // tensor cores work on one stream while the other's warps take exponentials:
 //
 //     S_w = Q_w K^T        128 rows x 128 positions, operands in shared memory (128-byte swizzle, K-major)
-//     P_w = 2^(scale S_w - m)        a thread owns a row: no shuffles; 16 bits, back to TMEM
+//     P_w = 2^(scale S_w - m)        two threads own a row, 64 positions each: no shuffles; 16 bits, back to TMEM
 //     O_w += P_w V         P from TMEM, V as stored ([position][d] is the MN-major operand)
 //
 // When there are fewer items than CTAs, clusters of up to eight CTAs share an item: the 2 x ctas streams take every
@@ -17,16 +17,19 @@
 // up to 128 rows give both streams the same rows and every second tile each, and join them at the end.  Rows of a group of heads are
 // packed: 128 / group tokens x group heads are one row tile, which one TMA box of the queries fetches.
 //
-// Roles: warp 0 loads tiles (a lane per page and slab, so that small pages are issued side by side), warp 1 issues the products,
-// warp 2 works out the CTA's segments and loads their queries, warp 3 clears values behind a sequence's end, warps 4-7 and
-// 8-11 are the streams' softmax; with an 8-bit cache warps 12-15 turn codes into 16-bit tiles.
+// Roles: warp 0 loads tiles (a lane per page and slab, so that small pages are issued side by side), warps 1 and 3 issue the
+// products of a stream each, warp 2 works out the CTA's segments and loads their queries, warps 4-11 and 12-19 are the streams'
+// softmax; with an 8-bit cache warps 20-23 turn codes into 16-bit tiles.
 //
 // The chain scores -> weights -> second product -> next scores of a stream is what bounds a long call (its S, P and O fill
-// TMEM, so a stream has one tile in the works), hence: the maximum in independent chains of three-input maxima, taken
-// while the second half of the scores is still on its way; the maximum only raised when a score passes it by 2^8, so that O
-// is rarely rescaled (by then the stream's products have ended, its next S is issued behind them); every fourth
-// exponential on the FMA pipes (the MUFU unit takes 8 cycles a warp); and the second product begins when half of
-// the weights are stored.
+// TMEM, so a stream has one tile in the works), hence: two threads to a row, an issuing warp to a stream; the maximum only
+// raised when a score passes it by 2^8, so that O is rarely rescaled (by then the stream's products have ended, its next S is
+// issued behind them); the streams' products issued in turn, so that one stream's exponentials fall into the
+// other's products; some exponentials on the FMA pipes (the MUFU unit takes 8 cycles a warp).
+//
+// 8-bit caches are multiplied in fp16, whatever the type of the queries, because the hardware turns E4M3 codes into fp16
+// numbers (exactly) in one instruction per two.  A tile's rows are held relative to its largest exponent, which the
+// scores (keys) or the weights (values) are multiplied by; bf16 queries are brought into fp16's range by a power of two a row.
 //
 // 0 x NaN is NaN, so what a row does not see must not reach the second product as a non-finite number.  Places behind the
 // sequence's end are cleared in shared memory.  Values of the chunk itself are not looked at unless a sum comes out
@@ -39,6 +42,7 @@ namespace {
 constexpr int kTile = 128;                                 // rows of a row tile, positions of a tile
 constexpr int kSlabBytes = kTile * 128;                    // 64 elements of every row of a tile
 constexpr float kSlack = 8.f;
+constexpr int kEveryFma = 16;                              // two of so many exponentials are taken on the FMA pipes
 constexpr int kFixed = 2;                                  // queries and join of a segment take about as long as two tiles
 
 template <bool Q8, int D>
@@ -46,11 +50,10 @@ struct Geometry {
     static constexpr int kSlabs = D / 64;
     static constexpr int kTileBytes = kSlabs * kSlabBytes;
     static constexpr int kStages = (D == 128 ? 1 : 2) * (Q8 ? 3 : 5);     // 16-bit tiles
-    static constexpr int kRaw = Q8 ? (D == 128 ? 4 : 8) : 0;              // 8-bit tiles
+    static constexpr int kRaw = Q8 ? (D == 128 ? 3 : 6) : 0;              // 8-bit tiles
     static constexpr int kRawBytes = kTile * D;
-    static constexpr int kThreads = Q8 ? 512 : 384;
+    static constexpr int kThreads = Q8 ? 768 : 640;
     static constexpr int kBig = 2 * kTileBytes + kStages * kTileBytes + kRaw * kRawBytes;
-    static constexpr int kSmall = 2048 + (D == 64 ? 2048 : 1024);             // maxima and sums of both streams; barriers, plan, exponents
 };
 constexpr int kSmemBytes = 232448;                         // all of an SM's shared memory (one CTA per SM, by TMEM too)
 
@@ -106,25 +109,28 @@ struct Job {
         }
     }
     __device__ __forceinline__ int tile(int j) const { return t0 + (one ? (j >> 1) * step + (j & 1) : j); }
-    // Place of value tile j in the order in which tiles are loaded and consumed: K0 V0 K1 V1 ... for two row tiles,
-    // K0 K1 V0 K2 V1 K3 ... for one.
+    // Places of key tile j and value tile j in the order in which tiles are loaded and consumed: K0 V0 K1 V1 ... for two
+    // row tiles, K0 K1 V0 K2 V1 K3 ... for one.
+    __device__ __forceinline__ int k_place(int j) const { return one ? (j < 2 ? j : 2 * j - 1) : 2 * j; }
     __device__ __forceinline__ int v_place(int j) const { return one ? (j == nt - 1 ? 2 * nt - 1 : 2 + 2 * j) : 2 * j + 1; }
-    // the last value tile holds places behind the end
-    __device__ __forceinline__ bool ragged() const { return nt > 0 && (tile(nt - 1) + 1) * kTile > c.total; }
 };
 
 template <int kStages, int kRaw>
 struct Shared {
+    float m[2][kTile], l[2][kTile];                        // of the streams' rows; l also passes maxima between a row's threads
     uint64_t full[kStages], empty[kStages];
     uint64_t raw_full[kRaw ? kRaw : 1], raw_empty[kRaw ? kRaw : 1];
-    uint64_t q_full[2], q_empty[2], s_full[2], p_half[2], p_full[2], o_full[2];
-    uint64_t cleared[2];                                   // ragged value tile of this segment, of the next
+    uint64_t q_full[2], q_ready[2], q_empty[2], s_full[2], p_full[2], o_full[2];
     uint64_t job_full[2], job_empty[2];
     uint64_t ready, taken;                                 // cluster: every CTA's sums are in place / have been read
-    alignas(16) uint8_t exps[kRaw ? kRaw : 1][kTile];      // exponents of the 8-bit tiles (bulk copies: 16-byte aligned)
+    alignas(16) uint8_t exps[kRaw ? kRaw : 1][kRaw ? kTile : 16];      // exponents of the 8-bit tiles (bulk copies: 16-byte aligned)
+    float q_scale[2][kRaw ? kTile : 1];                    // 8-bit: 1 / power of two that a query row was multiplied by
+    int tile_exp[16];                                      // 8-bit: largest exponent of the last tiles, by place
+    int v_exp[2];                                          // 8-bit: the streams' sums are relative to 2^v_exp
     Job job[2];
     uint32_t tmem;
     unsigned ticket;
+    unsigned tensor;                                       // 1: a stream's products are being issued
 };
 
 __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, int x, int y, int z, uint64_t *bar)
@@ -169,6 +175,13 @@ __device__ __forceinline__ void tmem_ld_wait_for(uint32_t *r)
                    "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
                  :: "memory");
 }
+__device__ __forceinline__ void tmem_ld_wait16(uint32_t *r)
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :: "memory");
+}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
 {
     asm volatile(
@@ -178,22 +191,22 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
         : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// A warpgroup's registers per thread.  The warpgroups' shares together are what the CTA was launched with: 512 x 128
-// (8-bit: 64 + 192 + 192 + 64 a thread of each) or 384 x 168 (88 + 208 + 208).
+// A warpgroup's registers per thread.  The warpgroups' shares together are what the CTA was launched with: 640 x 96
+// (64 + 4 x 104 a thread of each), with an 8-bit cache 768 x 80 (64 + 4 x 88 + 64).
 template <bool kMore, int kCount>
 __device__ __forceinline__ void set_registers()
 {
     if constexpr (kMore) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCount));
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCount));
 }
-// Barrier and "all of them".
-__device__ __forceinline__ bool bar_and(int id, int threads, bool x)
+// Barrier and "any of them".
+__device__ __forceinline__ bool bar_or(int id, int threads, bool x)
 {
     int r;
     asm volatile(
         "{\n\t.reg .pred p, q;\n\t"
         "setp.ne.s32 q, %3, 0;\n\t"
-        "bar.red.and.pred p, %1, %2, q;\n\t"
+        "bar.red.or.pred p, %1, %2, q;\n\t"
         "selp.s32 %0, 1, 0, p;\n\t}"
         : "=r"(r)
         : "r"(id), "r"(threads), "r"((int)x)
@@ -269,7 +282,7 @@ __device__ __forceinline__ uint64_t ex2_fma(uint64_t x)
     return mul2(p, pair(__uint_as_float(__float_as_uint(lo) << 23), __uint_as_float(__float_as_uint(hi) << 23)));
 }
 
-// Sums of stream `st` for row `row` and elements d .. d + 31 of a segment, added up one position after the other without what the
+// Sums of stream `st` for row `row` and elements d .. d + 15 of a segment, added up one position after the other without what the
 // row does not see -- called when the tensor cores' sum is not finite.  Leaves `x` alone if the chunk's own values are
 // finite (then the non-finite ones are seen by every row).
 template <typename T, int D>
@@ -283,7 +296,7 @@ __device__ __noinline__ void repair(const AttendArgs &a, const Job &job, int st,
         const int page = a.kv.table[(long long)job.seg.b * a.kv.width + (p >> a.kv.page_shift)];
         return kv_row(a.kv, a.kv.layer, page < 0 || page >= a.kv.num_pages ? 0 : page, head, p & in_page);
     };
-    float y[32] = {};
+    float y[16] = {};
     bool odd = false;
     for (int pass = 0; pass < 2; ++pass) {
         for (int j = 0; j < job.n[st]; ++j) {
@@ -292,7 +305,7 @@ __device__ __noinline__ void repair(const AttendArgs &a, const Job &job, int st,
                 const long long r = row_of(p);
                 const T *k = static_cast<const T *>(a.kv.k) + r * D, *v = static_cast<const T *>(a.kv.v) + r * D + d;
                 if (pass == 0) {
-                    for (int e = 0; e < 32; ++e) odd |= !isfinite(unpack2<T>(reinterpret_cast<const uint16_t *>(v)[e]).x);
+                    for (int e = 0; e < 16; ++e) odd |= !isfinite(unpack2<T>(reinterpret_cast<const uint16_t *>(v)[e]).x);
                     continue;
                 }
                 const int t = p - c.ctx;
@@ -303,13 +316,13 @@ __device__ __noinline__ void repair(const AttendArgs &a, const Job &job, int st,
                     s = fmaf(kk.x, qq.x, s);
                     s = fmaf(kk.y, qq.y, s);
                 }
-                const float w = unpack2<T>(pack2<T>(ex2((s - m) * a.scale_log2), 0.f)).x;
-                for (int e = 0; e < 32; ++e) y[e] += w * unpack2<T>(reinterpret_cast<const uint16_t *>(v)[e]).x;
+                const float w = unpack2<T>(pack2<T>(ex2(s * a.scale_log2 - m), 0.f)).x;
+                for (int e = 0; e < 16; ++e) y[e] += w * unpack2<T>(reinterpret_cast<const uint16_t *>(v)[e]).x;
             }
         }
         if (pass == 0 && !odd) return;
     }
-    for (int e = 0; e < 32; ++e) x[e] = y[e];
+    for (int e = 0; e < 16; ++e) x[e] = y[e];
 }
 
 template <typename T, bool Q8, int D>
@@ -319,17 +332,16 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 {
     using Geo = Geometry<Q8, D>;
     using Sh = Shared<Geo::kStages, Geo::kRaw>;
-    static_assert(2048 + sizeof(Sh) <= Geo::kSmall, "shared memory");
+    using M = std::conditional_t<Q8, __half, T>;            // type of the products
+    constexpr bool kTurnQ = Q8 && std::is_same<T, __nv_bfloat16>::value;
     constexpr int kStages = Geo::kStages, kSlabs = Geo::kSlabs, kTileBytes = Geo::kTileBytes;
+    static_assert(Geo::kBig + sizeof(Sh) <= kSmemBytes, "shared memory");
     extern __shared__ uint8_t smem_raw[];
-    const int pad = (int)(-smem_u32(smem_raw) & 1023u);
-    uint8_t *q_s = smem_raw + pad;
+    uint8_t *q_s = smem_raw;
     uint8_t *stages = q_s + 2 * kTileBytes;
     uint8_t *raws = stages + kStages * kTileBytes;
-    float *s_m = reinterpret_cast<float *>(raws + Geo::kRaw * Geo::kRawBytes);       // [2][128]
-    float *s_l = s_m + 2 * kTile;                                                     // [2][128]
-    Sh &sh = *reinterpret_cast<Sh *>(s_l + 2 * kTile);
-    if (pad + Geo::kBig + Geo::kSmall > kSmemBytes) {       // shared memory never starts there
+    Sh &sh = *reinterpret_cast<Sh *>(raws + Geo::kRaw * Geo::kRawBytes);
+    if (smem_u32(smem_raw) & 1023u) {                       // shared memory never starts there
         if (threadIdx.x == 0) report_timeout(a.kv.status);
         return;
     }
@@ -340,7 +352,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
             mbar_init(&sh.full[s], Q8 ? 4 : 1);
-            mbar_init(&sh.empty[s], 1);
+            mbar_init(&sh.empty[s], 2);                     // both streams
         }
         for (int s = 0; s < Geo::kRaw; ++s) {
             mbar_init(&sh.raw_full[s], 1);
@@ -348,17 +360,17 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         }
         for (int w = 0; w < 2; ++w) {
             mbar_init(&sh.q_full[w], 1);
-            mbar_init(&sh.q_empty[w], w == 0 && a.ctas > 1 ? 2 : 1);      // cluster: the sums pass through its place
+            mbar_init(&sh.q_ready[w], 4);
+            mbar_init(&sh.q_empty[w], w == 0 && a.ctas > 1 ? 3 : 2);      // both streams; in a cluster the sums pass through place 0
             mbar_init(&sh.s_full[w], 1);
-            mbar_init(&sh.p_half[w], 4);
-            mbar_init(&sh.p_full[w], 4);
+            mbar_init(&sh.p_full[w], 8);
             mbar_init(&sh.o_full[w], 1);
-            mbar_init(&sh.cleared[w], 1);
             mbar_init(&sh.job_full[w], 1);
-            mbar_init(&sh.job_empty[w], Q8 ? 2 + 8 + 4 : 3 + 8);          // a warp each: loads, products, (clearing,) softmax, (conversion)
+            mbar_init(&sh.job_empty[w], 3 + 16 + (Q8 ? 4 : 0));           // a warp each: loads, products, softmax, conversion
         }
         mbar_init(&sh.ready, a.ctas);
         mbar_init(&sh.taken, a.ctas);
+        sh.tensor = 0;
         mbar_fence_init();
         tma_prefetch_desc(&q_map);
         tma_prefetch_desc(&k_map);
@@ -377,8 +389,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     pdl_wait();                                             // what follows reads what earlier kernels wrote
     pdl_launch_dependents();
 
-    // Segment number `i` of this CTA, when warp 2 has worked it out; false = a wait ran out.
-    auto job_of = [&](int i) { return mbar_wait(&sh.job_full[i & 1], (i >> 1) & 1, wl); };
+    // Segment number `i` of this CTA, when warp 2 has worked it out; false = a wait ran out.  For whole warps.
+    auto job_of = [&](int i) { return __all_sync(0xFFFFFFFFu, mbar_wait(&sh.job_full[i & 1], (i >> 1) & 1, wl)); };
     // The calling warp is done with it.
     auto job_done = [&](int i) {
         __syncwarp();
@@ -389,7 +401,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         KvPlan<ManyRows> plan;
         bool more = false;
         if (warp == 2) more = plan.start(a, lane, blockIdx.x / a.ctas, gridDim.x / a.ctas);     // the same for the whole cluster
-        set_registers<false, Q8 ? 64 : 88>();
+        set_registers<false, 64>();
         if (warp == 0) {
             // ---- tiles of keys and values: 16-bit ones straight into the stages, 8-bit ones into the raw ring
             constexpr int kRing = Q8 ? Geo::kRaw : kStages;
@@ -454,27 +466,29 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     if (lane == 0) report_timeout(a.kv.status);
                     break;
                 }
-        } else if (warp == 1) {
-            // ---- products.  The whole warp walks through the loop and one lane issues: what the instructions take must be known
-            // to be the same for all lanes (hence the shuffles), or every operand is moved to the uniform registers by itself,
-            // at 100 cycles and more an instruction against the 64 that it runs.
-            constexpr uint32_t kFmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+        } else if (warp != 2) {
+            // ---- products of stream st.  The whole warp walks through the loop and one lane issues: what the instructions take
+            // must be known to be the same for all lanes (hence the shuffles), or every operand is moved to the uniform registers
+            // by itself, at 100 cycles and more an instruction against the 64 that it runs.
+            constexpr uint32_t kFmt = std::is_same<M, __nv_bfloat16>::value ? 1u : 0u;
             constexpr uint32_t kCommon = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((uint32_t)(kTile >> 4) << 24);
             constexpr uint32_t kIdescS = kCommon | ((uint32_t)(kTile >> 3) << 17);
             constexpr uint32_t kIdescO = kCommon | ((uint32_t)(D >> 3) << 17) | (1u << 16);       // second operand MN-major
             auto uniform = [](int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); };
-            const uint32_t t0 = uniform(tmem);
+            const int st = uniform(warp == 3);
+            const uint32_t t0 = uniform(tmem), s_at = t0 + st * kTile, o_at = t0 + 256 + st * D;
             const uint64_t q_desc = make_desc(smem_u32(q_s)), k_desc = make_desc(smem_u32(stages)), v_desc = make_desc_mn(smem_u32(stages));
+            uint64_t *q_bar = kTurnQ ? sh.q_ready : sh.q_full, *q_empty = sh.q_empty;
             const bool issuer = elect_one();
-            int base = 0;                                    // tiles consumed by earlier segments
-            int steps0 = 0, steps1 = 0, uses0 = 0, uses1 = 0, clears0 = 0, clears1 = 0;
+            int base = 0, at = 0;                            // tiles of earlier segments; tiles gone through
+            int steps = 0, uses0 = 0, uses1 = 0;
             bool ok = true;
             for (int i = 0; ok; ++i) {
-                if (!__all_sync(0xFFFFFFFFu, job_of(i))) { ok = false; break; }
+                if (!job_of(i)) { ok = false; break; }
                 const Job &w = sh.job[i & 1];
                 if (!uniform(w.more)) break;
-                const bool one = uniform(w.one) != 0, ragged = !Q8 && uniform(w.ragged()) != 0;
-                const int nt = uniform(w.nt), n0 = uniform(w.n[0]), n1 = uniform(w.n[1]);
+                const bool one = uniform(w.one) != 0;
+                const int nt = uniform(w.nt), n = uniform(w.n[st]);
                 auto wait = [&](uint64_t *bar, int parity) {
                     ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity & 1, wl));
                     tc_fence_after();
@@ -482,72 +496,85 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 };
                 auto k_place = [&](int j) { return one ? (j < 2 ? j : 2 * j - 1) : 2 * j; };
                 auto v_place = [&](int j) { return one ? (j == nt - 1 ? 2 * nt - 1 : 2 + 2 * j) : 2 * j + 1; };
-                auto scores = [&](auto st_, int j) {
-                    constexpr int st = decltype(st_)::value;
-                    const int x = base + k_place(one ? 2 * j + st : j), s = x % kStages;
-                    if (!wait(&sh.full[s], x / kStages)) return;
+                // Tile x of the line.  Both streams go through ALL tiles in order and both free each of them, the other stream's
+                // too: a barrier's parity tells two neighbouring rounds of the ring apart and no more, so neither stream may
+                // get a round ahead of a tile that the other one has not seen arrive.
+                auto reach = [&](int x) {
+                    for (; at < x; ++at) {
+                        if (!wait(&sh.full[at % kStages], at / kStages)) return false;
+                        if (lane == 0) mbar_arrive(&sh.empty[at % kStages]);
+                    }
+                    ++at;
+                    return wait(&sh.full[x % kStages], x / kStages);
+                };
+                // A stream's products are issued in one go: side by side, both streams would wait for the tensor cores and
+                // then for the exponentials together, instead of in turn.  (Nothing waits while it holds the lock.)
+                auto lock = [&] {
+                    bool got = true;
+                    if (lane == 0) {
+                        const long long t = clock64();
+                        while (got && atomicExch(&sh.tensor, 1u) != 0) got = clock64() - t < wl;
+                    }
+                    ok = __all_sync(0xFFFFFFFFu, got);
+                    return ok;
+                };
+                auto unlock = [&] {
+                    __syncwarp();
+                    if (lane == 0) atomicExch(&sh.tensor, 0u);
+                };
+                auto issue_scores = [&](int j, int s) {
                     const uint64_t qd = q_desc + (one ? 0 : st * (kTileBytes >> 4)), kd = k_desc + s * (kTileBytes >> 4);
-                    const bool last = one ? 2 * j + st == nt - 1 : j == nt - 1;
-                    if (issuer) {
 #pragma unroll
-                        for (int k = 0; k < D / 16; ++k)
-                            umma_f16(t0 + st * kTile, qd + ((k >> 2) * (kSlabBytes >> 4) + 2 * (k & 3)), kd + ((k >> 2) * (kSlabBytes >> 4) + 2 * (k & 3)),
-                                     kIdescS, k != 0);
-                        tc_commit(&sh.s_full[st]);
-                        if (one || st == 1) tc_commit(&sh.empty[s]);
-                        if (last) tc_commit(&sh.q_empty[one ? 0 : st]);
+                    for (int k = 0; k < D / 16; ++k)
+                        umma_f16(s_at, qd + ((k >> 2) * (kSlabBytes >> 4) + 2 * (k & 3)), kd + ((k >> 2) * (kSlabBytes >> 4) + 2 * (k & 3)),
+                                 kIdescS, k != 0);
+                    tc_commit(&sh.s_full[st]);
+                    tc_commit(&sh.empty[s]);
+                    if (j == n - 1) {
+                        tc_commit(&q_empty[0]);
+                        if (!one) tc_commit(&q_empty[1]);
                     }
-                    __syncwarp();
                 };
-                auto sums = [&](auto st_, int j, int &steps) {
-                    constexpr int st = decltype(st_)::value;
-                    const int vj = one ? 2 * j + st : j, x = base + v_place(vj), s = x % kStages;
-                    if (!wait(&sh.full[s], x / kStages)) return;
-                    if (ragged && vj == nt - 1 && (one || st == 0)) {
-                        if (!wait(&sh.cleared[i & 1], i & 1 ? clears1 : clears0)) return;
-                        if (i & 1) ++clears1;
-                        else ++clears0;
+                // the queries: both streams wait for and free all row tiles, for the same reason
+                wait(&q_bar[0], uses0++);
+                if (ok && !one) wait(&q_bar[1], uses1++);
+                if (ok && n > 0) {
+                    const int x = base + k_place(one ? st : 0);
+                    if (reach(x) && lock()) {
+                        if (issuer) issue_scores(0, x % kStages);
+                        unlock();
                     }
-                    const uint64_t vd = v_desc + s * (kTileBytes >> 4);
-                    const uint32_t o = t0 + 256 + st * D, p = t0 + st * kTile;
-                    if (!wait(&sh.p_half[st], steps)) return;
-                    if (issuer) {
-                        if (j == 0) umma_f16_ta(o, p, vd, kIdescO, 0);
-                        else umma_f16_ta(o, p, vd, kIdescO, 1);
-#pragma unroll
-                        for (int k = 1; k < kTile / 32; ++k) umma_f16_ta(o, p + 8 * k, vd + 128 * k, kIdescO, 1);
-                    }
-                    __syncwarp();
-                    if (!wait(&sh.p_full[st], steps)) return;
-                    ++steps;
-                    if (issuer) {
-#pragma unroll
-                        for (int k = kTile / 32; k < kTile / 16; ++k) umma_f16_ta(o, p + 8 * k, vd + 128 * k, kIdescO, 1);
-                        if (one || st == 1) tc_commit(&sh.empty[s]);
-                        if (j == (st ? n1 : n0) - 1) tc_commit(&sh.o_full[st]);
-                    }
-                    __syncwarp();
-                };
-                const std::integral_constant<int, 0> s0{};
-                const std::integral_constant<int, 1> s1{};
-                wait(&sh.q_full[0], uses0++);
-                if (ok && !one) wait(&sh.q_full[1], uses1++);
-                if (nt == 0 && ok && issuer) tc_commit(&sh.q_empty[0]);        // a cluster with fewer tiles than streams
-                if (ok && n0 > 0) scores(s0, 0);
-                if (ok && n1 > 0) scores(s1, 0);
+                } else if (ok && issuer) {
+                    tc_commit(&q_empty[0]);                  // a cluster with fewer tiles than streams
+                }
 #pragma unroll 1
-                for (int j = 0; j < n0 && ok; ++j) {
-                    sums(s0, j, steps0);
-                    if (ok && j + 1 < n0) scores(s0, j + 1);
-                    if (!ok || j >= n1) continue;
-                    sums(s1, j, steps1);
-                    if (ok && j + 1 < n1) scores(s1, j + 1);
+                for (int j = 0; j < n && ok; ++j) {
+                    const int vj = one ? 2 * j + st : j, x = base + v_place(vj), s = x % kStages;
+                    const bool more = j + 1 < n;
+                    const int y = more ? base + k_place(one ? vj + 2 : j + 1) : 0;
+                    if (!reach(x) || (more && !reach(y)) || !wait(&sh.p_full[st], steps) || !lock()) break;
+                    ++steps;
+                    const uint64_t vd = v_desc + s * (kTileBytes >> 4);
+                    if (issuer) {
+                        if (j == 0) umma_f16_ta(o_at, s_at, vd, kIdescO, 0);
+                        else umma_f16_ta(o_at, s_at, vd, kIdescO, 1);
+#pragma unroll
+                        for (int k = 1; k < kTile / 16; ++k) umma_f16_ta(o_at, s_at + 8 * k, vd + 128 * k, kIdescO, 1);
+                        tc_commit(&sh.empty[s]);
+                        if (more) issue_scores(j + 1, y % kStages);
+                        else tc_commit(&sh.o_full[st]);
+                    }
+                    unlock();
                 }
                 base += 2 * nt;
+                if (ok && at < base) {                       // the other stream's last tiles
+                    reach(base - 1);
+                    if (ok && lane == 0) mbar_arrive(&sh.empty[(base - 1) % kStages]);
+                }
                 job_done(i);
             }
             if (!ok && lane == 0) report_timeout(a.kv.status);
-        } else if (warp == 2) {
+        } else {
             // ---- the plan, and queries
             if (lane == 0) {
                 const int tokens = ManyRows::per_tile(a);
@@ -564,7 +591,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         w.c = plan.c;
                         w.set(a, rank);
                     }
-                    mbar_arrive(&sh.job_full[i & 1]);
+    mbar_arrive(&sh.job_full[i & 1]);
                     if (!more) break;
                     const int tiles = w.one ? 1 : 2, y = w.seg.head * a.group, z = plan.c.row0 + 2 * w.seg.rt * tokens;
             #pragma unroll 1
@@ -584,48 +611,20 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 if (uses0 > 0 && !mbar_wait(&sh.q_full[0], (uses0 - 1) & 1, wl)) report_timeout(a.kv.status);
                 if (uses1 > 0 && !mbar_wait(&sh.q_full[1], (uses1 - 1) & 1, wl)) report_timeout(a.kv.status);
             }
-        } else {
-            // ---- values behind the end (16-bit cache; the conversion does it for codes)
-            if constexpr (!Q8) {
-                int base = 0;
-                bool ok = true;
-                for (int i = 0; ok; ++i) {
-                    if (!job_of(i)) { ok = false; break; }
-                    const Job &w = sh.job[i & 1];
-                    if (!w.more) break;
-                    if (w.ragged()) {
-                        const int x = base + w.v_place(w.nt - 1), s = x % kStages;
-                        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&sh.full[s], (x / kStages) & 1, wl));
-                        if (!ok) break;
-                        const int end = max(w.c.total - w.tile(w.nt - 1) * kTile, 0), rows = kTile - end;
-                        uint8_t *tile = stages + (size_t)s * kTileBytes + end * 128;
-#pragma unroll 1
-                        for (int y = lane; y < rows * 8; y += 32)
-#pragma unroll
-                            for (int p = 0; p < kSlabs; ++p) *reinterpret_cast<uint4 *>(tile + p * kSlabBytes + y * 16) = make_uint4(0, 0, 0, 0);
-                        fence_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&sh.cleared[i & 1]);
-                    }
-                    base += 2 * w.nt;
-                    job_done(i);
-                }
-                if (!ok && lane == 0) report_timeout(a.kv.status);
-            }
         }
-    } else if (warp < 12) {
-        set_registers<true, Q8 ? 192 : 208>();
-        // ---- softmax of stream st; a thread owns a row
-        const int st = warp >= 8 ? 1 : 0;
+    } else if (warp < 20) {
+        set_registers<true, Q8 ? 88 : 104>();
+        // ---- softmax of stream st; a thread has positions 64 half .. of a tile of its row
+        const int st = warp >= 12 ? 1 : 0, half = (warp >> 2) & 1 ? 0 : 1;      // warps 4-7, 12-15: the first half
         const int row = tid & 127;                           // TMEM lane
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;    // (warp % 4) x 32 lanes, in the address's upper half
-        const uint32_t ts = tmem + lanes + st * kTile, to = tmem + lanes + 256 + st * D;
+        const uint32_t ts = tmem + lanes + st * kTile + 64 * half, tp = tmem + lanes + st * kTile + 32 * half;
+        const uint32_t to = tmem + lanes + 256 + st * D;
         const int row_tok = a.by_group.div(row);
-        const float scale = a.scale_log2;
-        int steps = 0, items0 = 0, items1 = 0, joins = 0;
+        int steps = 0, items0 = 0, items1 = 0, joins = 0, base = 0;
         bool dead = false;
         for (int i = 0;; ++i) {
-            if (!bar_and(1, 256, job_of(i))) {               // all softmax warps go on, or none (they meet at barriers)
+            if (bar_or(1, 512, !job_of(i))) {                // all softmax warps go on, or none (they meet at barriers)
                 report_timeout(a.kv.status);
                 break;
             }
@@ -638,86 +637,113 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             const int tok = first_tok + row_tok;              // of this row; may lie behind the chunk
             const int limit = a.mask ? c.total : min(c.total, c.ctx + min(tok, c.len - 1) + 1);
             const int all_seen = min(c.total, a.mask ? c.ctx : c.ctx + min(first_tok, c.len - 1) + 1);    // by every row
-            float m = -INFINITY, l = 0.f;
+            float m = -INFINITY, l = 0.f, scale = a.scale_log2;      // m in powers of two
+            int v_exp = -127;
 #pragma unroll 1
             for (int j = 0; j < n_mine; ++j) {
-                const int p0 = w.tile(w.one ? 2 * j + st : j) * kTile;
+                const int vj = w.one ? 2 * j + st : j, p0 = w.tile(vj) * kTile, v_at = base + w.v_place(vj);
                 if (!dead && !mbar_wait(&sh.s_full[st], steps & 1, wl)) {
                     report_timeout(a.kv.status);
                     dead = true;
                 }
+                const bool ragged = !Q8 && vj == w.nt - 1 && p0 + kTile > c.total;
+                if (Q8 || ragged)                             // the values' exponent, or their places behind the end
+                    if (!dead && !mbar_wait(&sh.full[v_at % kStages], (v_at / kStages) & 1, wl)) {
+                        report_timeout(a.kv.status);
+                        dead = true;
+                    }
                 dead = __any_sync(0xFFFFFFFFu, dead);
                 ++steps;
                 tc_fence_after();
-                float s[kTile];
+                float s[64];
                 uint32_t *su = reinterpret_cast<uint32_t *>(s);
                 const bool masked = p0 + kTile > all_seen;
                 tmem_ld32(ts, su);
                 tmem_ld32(ts + 32, su + 32);
+                int dv = 0;                                   // 8-bit: weights are multiplied by 2^dv
+                bool over = false;
+                if constexpr (Q8) {
+                    scale = a.scale_log2 * (kTurnQ ? sh.q_scale[w.one ? 0 : st][row] : 1.f) * pow2f(max(sh.tile_exp[(base + w.k_place(vj)) & 15], -100));
+                    scale = fmaxf(scale, 1e-37f);             // -infinity times it stays one
+                    dv = sh.tile_exp[v_at & 15];
+                    over = dv > v_exp;
+                }
                 tmem_ld_wait_for(su);
                 tmem_ld_wait_for(su + 32);
-                tmem_ld32(ts + 64, su + 64);
-                tmem_ld32(ts + 96, su + 96);
+                if (masked) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int p = p0 + 64 * half + 32 * k;
+                        const int n = min(max(limit - p, 0), 32);
+                        uint32_t see = n == 32 ? 0xFFFFFFFFu : (1u << n) - 1u;
+                        if (a.mask && p + 32 > c.ctx) {
+                            const uint32_t *mask = a.mask + (long long)(c.row0 + min(tok, c.len - 1)) * a.mask_words;
+                            const int j0 = p - c.ctx;         // place in the chunk of bit 0; context below 0
+                            const int w0 = j0 >> 5;           // floor; -1 at the least
+                            const uint32_t lo = w0 < 0 ? 0xFFFFFFFFu : w0 < a.mask_words ? mask[w0] : 0u;
+                            const uint32_t hi = w0 + 1 < a.mask_words ? mask[w0 + 1] : 0u;
+                            see &= __funnelshift_r(lo, hi, j0 & 31);
+                        }
+#pragma unroll
+                        for (int x = 0; x < 32; ++x)
+                            if (!(see >> x & 1)) s[32 * k + x] = -INFINITY;
+                    }
+                }
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (h == 1) {
-                        tmem_ld_wait_for(su + 64);
-                        tmem_ld_wait_for(su + 96);
-                    }
-                    if (masked) {
+                for (int k = 0; k < 64; k += 8)
 #pragma unroll
-                        for (int k = 2 * h; k < 2 * h + 2; ++k) {
-                            const int p = p0 + 32 * k;
-                            const int n = min(max(limit - p, 0), 32);
-                            uint32_t see = n == 32 ? 0xFFFFFFFFu : (1u << n) - 1u;
-                            if (a.mask && p + 32 > c.ctx) {
-                                const uint32_t *mask = a.mask + (long long)(c.row0 + min(tok, c.len - 1)) * a.mask_words;
-                                const int j0 = p - c.ctx;         // place in the chunk of bit 0; context below 0
-                                const int w0 = j0 >> 5;           // floor; -1 at the least
-                                const uint32_t lo = w0 < 0 ? 0xFFFFFFFFu : w0 < a.mask_words ? mask[w0] : 0u;
-                                const uint32_t hi = w0 + 1 < a.mask_words ? mask[w0 + 1] : 0u;
-                                see &= __funnelshift_r(lo, hi, j0 & 31);
-                            }
-#pragma unroll
-                            for (int x = 0; x < 32; ++x)
-                                if (!(see >> x & 1)) s[32 * k + x] = -INFINITY;
+                    for (int x = 0; x < 4; ++x) mx[x] = fmaxf(fmaxf(mx[x], s[k + 2 * x]), s[k + 2 * x + 1]);
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+                over |= top - m > kSlack;                     // -inf - -inf is NaN: no
+                tc_fence_before();
+                const bool raise = bar_or(2 + st, 256, over); // also: both halves have been read, weights may take their place
+                tc_fence_after();
+                if (raise) {
+                    float *pass = &sh.l[st][row];
+                    if (half) *pass = top;
+                    bar_sync(2 + st, 256);
+                    float mn;
+                    if (!half) *pass = mn = fmaxf(fmaxf(m, top), *pass);
+                    bar_sync(2 + st, 256);
+                    if (half) mn = *pass;
+                    float f = mn > -INFINITY ? ex2(m - mn) : 1.f;
+                    l *= f;
+                    m = mn;
+                    if constexpr (Q8) {
+                        if (dv > v_exp) {
+                            f *= pow2f(max(v_exp - dv, -126));
+                            v_exp = dv;
                         }
                     }
-#pragma unroll
-                    for (int k = 64 * h; k < 64 * h + 64; k += 8)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) mx[x] = fmaxf(fmaxf(mx[x], s[k + 2 * x]), s[k + 2 * x + 1]);
-                }
-                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-                if (__any_sync(0xFFFFFFFFu, (top - m) * scale > kSlack)) {     // -inf - -inf is NaN: no
-                    const float mn = fmaxf(m, top);
                     if (j > 0) {
-                        const float f = mn > -INFINITY ? ex2((m - mn) * scale) : 1.f;
-                        l *= f;
 #pragma unroll 1
-                        for (int k = 0; k < D; k += 16) {
+                        for (int k = half * (D / 2); k < half * (D / 2) + D / 2; k += 16) {
                             uint32_t r[16];
                             tmem_ld16(to + k, r);
-                            tmem_ld_wait();
+                            tmem_ld_wait16(r);
 #pragma unroll
                             for (int x = 0; x < 16; ++x) r[x] = __float_as_uint(__uint_as_float(r[x]) * f);
                             tmem_st16(to + k, r);
                         }
+                        tmem_st_wait();
                     }
-                    m = mn;
+                    tc_fence_before();
+                    bar_sync(2 + st, 256);                    // the second product begins when one half has its weights
+                    tc_fence_after();
                 }
-                const float base = m > -INFINITY ? m * scale : 0.f;
-                const uint64_t scale2 = pair(scale, scale), base2 = pair(-base, -base);
+                if constexpr (Q8) dv = max(dv - v_exp, -126);
+                const float off = (m > -INFINITY ? m : 0.f) - (Q8 ? (float)dv : 0.f);
+                const uint64_t scale2 = pair(scale, scale), off2 = pair(-off, -off);
                 uint64_t sum0 = 0, sum1 = 0;
                 // weights of 32 scores at a time, packed and stored over scores that have been read
                 auto weights = [&](int c0, bool fma) {
                     uint32_t p[16];
 #pragma unroll
                     for (int k = 0; k < 32; k += 2) {
-                        uint64_t x = fma2(pair(s[c0 + k], s[c0 + k + 1]), scale2, base2);
+                        uint64_t x = fma2(pair(s[c0 + k], s[c0 + k + 1]), scale2, off2);
                         float lo, hi;
-                        if (fma && (k & 6) == 6) {
+                        if (fma && k % kEveryFma == kEveryFma - 2) {
                             x = ex2_fma(x);
                             unpair(x, lo, hi);
                         } else {
@@ -728,39 +754,45 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         }
                         if (k & 2) sum1 = add2(sum1, x);
                         else sum0 = add2(sum0, x);
-                        p[k / 2] = pack2<T>(lo, hi);
+                        p[k / 2] = pack2<M>(lo, hi);
                     }
-                    tmem_st16(ts + c0 / 2, p);
-                };
-                auto stored = [&](uint64_t *bar) {
-                    tmem_st_wait();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar);
+                    tmem_st16(tp + c0 / 2, p);
                 };
                 if (masked) {                                 // -infinity has to give 0 exactly
                     weights(0, false);
                     weights(32, false);
-                    stored(&sh.p_half[st]);
-                    weights(64, false);
-                    weights(96, false);
                 } else {
                     weights(0, true);
                     weights(32, true);
-                    stored(&sh.p_half[st]);
-                    weights(64, true);
-                    weights(96, true);
                 }
                 float a0, a1;
                 unpair(add2(sum0, sum1), a0, a1);
-                l += a0 + a1;
-                stored(&sh.p_full[st]);
+                l += Q8 ? (a0 + a1) * pow2f(-dv) : a0 + a1;
+                if (ragged) {                                 // the places behind the end among this half's positions
+                    const int end = min(max(c.total - p0, 64 * half), 64 * half + 64), rows = 64 * half + 64 - end;
+                    uint8_t *tile = stages + (size_t)(v_at % kStages) * kTileBytes + end * 128;
+#pragma unroll 1
+                    for (int y = row; y < rows * 8; y += kTile)
+#pragma unroll
+                        for (int p = 0; p < kSlabs; ++p) *reinterpret_cast<uint4 *>(tile + p * kSlabBytes + y * 16) = make_uint4(0, 0, 0, 0);
+                    fence_async_smem();
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.p_full[st]);
             }
             // ---- the segment's result
+            base += 2 * w.nt;
             const bool valid = row < ManyRows::per_tile(a) * a.group && tok < c.len;
             const int heads = a.kv.heads * a.group;
-            s_m[st * kTile + row] = m;
-            s_l[st * kTile + row] = l;
+            if (half) sh.l[st][row] = l;
+            bar_sync(2 + st, 256);
+            if (!half) {
+                sh.l[st][row] += l;
+                sh.m[st][row] = m;
+                if (Q8 && row == 0) sh.v_exp[st] = v_exp;
+            }
             if (w.n[0] > 0) {
                 if ((w.one || st == 0) && !dead && !mbar_wait(&sh.o_full[0], items0 & 1, wl)) {
                     report_timeout(a.kv.status);
@@ -776,21 +808,28 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 ++items1;
             }
             dead = __any_sync(0xFFFFFFFFu, dead);
+            bar_sync(1, 512);
             tc_fence_after();
-            bar_sync(1, 256);
             // A thread has a row and some OCTETS of its elements, o0, o0 + o_step, ...: with two row tiles its stream's row and
-            // all octets; with one, half of the octets from both streams, or in a cluster its CTA's share of them.
+            // half of the octets; with one, a quarter of the octets from both streams, or in a cluster its CTA's share of them.
             const bool joined = w.one && a.ctas > 1;
-            const int prow = w.one ? row : st * kTile + row;
-            const int o0 = joined ? 2 * rank + st : w.one ? st * (D / 16) : 0;
-            const int o_step = joined ? 2 * a.ctas : 1, o_end = w.one && !joined ? o0 + D / 16 : D / 8;
+            const int prow = w.one ? row : st * kTile + row, quarter = 2 * st + half;
+            const int d0 = w.one ? quarter * (D / 4) : half * (D / 2), d1 = w.one ? d0 + D / 4 : d0 + D / 2;
+            const int o0 = joined ? 4 * rank + quarter : d0 / 8;
+            const int o_step = joined ? 4 * a.ctas : 1, o_end = joined ? D / 8 : d1 / 8;
             float f0 = 1.f, f1 = 0.f;
+            l = sh.l[w.one ? 0 : st][row];
             if (w.one) {
-                const float ma = s_m[row], mb = s_m[kTile + row];
+                const float ma = sh.m[0][row], mb = sh.m[1][row];
                 m = fmaxf(ma, mb);
-                f0 = m > -INFINITY ? ex2((ma - m) * scale) : 0.f;
-                f1 = m > -INFINITY ? ex2((mb - m) * scale) : 0.f;
-                l = f0 * s_l[row] + f1 * s_l[kTile + row];
+                f0 = m > -INFINITY ? ex2(ma - m) : 0.f;
+                f1 = m > -INFINITY ? ex2(mb - m) : 0.f;
+                l = f0 * l + f1 * sh.l[1][row];
+            }
+            float e0 = 1.f, e1 = 1.f;                          // 8-bit: what the sums are relative to
+            if constexpr (Q8) {
+                e0 = pow2f(max(sh.v_exp[w.one ? 0 : st], -126));
+                e1 = pow2f(max(sh.v_exp[1], -126));
             }
             const bool split = seg.c0 != seg.c1;
             const long long at = (long long)(c.row0 + tok) * heads + seg.head * a.group + row - row_tok * a.group;
@@ -809,49 +848,51 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 __stcg(dst, make_float4(x[0], x[1], x[2], x[3]));
                 __stcg(dst + kPartRows, make_float4(x[4], x[5], x[6], x[7]));
             };
-            // sums of this CTA: 32 elements at a time from TMEM to the result, the part, or (cluster) shared memory
+            // sums of this CTA: 16 elements at a time from TMEM to the result, the part, or (cluster) shared memory
             float4 *sums = reinterpret_cast<float4 *>(q_s);    // [D / 4][128 rows], where the queries were
-            const int d0 = w.one ? st * (D / 2) : 0, d1 = w.one ? d0 + D / 2 : D;
-#pragma unroll 1
-            for (int d = d0; d < d1; d += 32) {
-                uint32_t r[32];
-                float x[32];
-                tmem_ld32(w.one ? tmem + lanes + 256 + d : to + d, r);
-                tmem_ld_wait();
+            auto take = [&](int of, uint32_t addr, int d, float e, float *x) {         // sums of stream `of`
+                uint32_t r[16];
+                tmem_ld16(addr, r);
+                tmem_ld_wait16(r);
+                float odd = 0.f;
 #pragma unroll
-                for (int k = 0; k < 32; ++k) x[k] = __uint_as_float(r[k]);
-                auto check = [&](int of, float *x) {           // sums of stream `of`
-                    if constexpr (!Q8) {
-                        float odd = 0.f;
+                for (int k = 0; k < 16; ++k) {
+                    x[k] = __uint_as_float(r[k]);
+                    odd = fmaf(x[k], 0.f, odd);
+                    if (Q8) x[k] *= e;
+                }
+                if constexpr (!Q8) {
+                    if (own && valid && odd != 0.f) {          // NaN
+                        float y[16];
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) odd = fmaf(x[k], 0.f, odd);
-                        if (own && valid && odd != 0.f) {      // NaN
-                            float y[32];
+                        for (int k = 0; k < 16; ++k) y[k] = x[k];
+                        repair<T, D>(a, w, of, row, tok, sh.m[of][row], d, y);
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) y[k] = x[k];
-                            repair<T, D>(a, w, of, row, tok, s_m[of * kTile + row], d, y);
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) x[k] = y[k];
-                        }
+                        for (int k = 0; k < 16; ++k) x[k] = y[k];
                     }
-                };
-                if (w.n[w.one ? 0 : st] > 0) check(w.one ? 0 : st, x);
+                }
+            };
+#pragma unroll 1
+            for (int d = d0; d < d1; d += 16) {
+                float x[16];
+                if (w.n[w.one ? 0 : st] > 0) {
+                    take(w.one ? 0 : st, w.one ? tmem + lanes + 256 + d : to + d, d, e0, x);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) x[k] = 0.f;
+                }
                 if (w.one) {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) x[k] = f0 > 0.f || f0 != f0 ? f0 * x[k] : 0.f;
+                    for (int k = 0; k < 16; ++k) x[k] = f0 > 0.f || f0 != f0 ? f0 * x[k] : 0.f;
                     if (w.n[1] > 0) {
-                        tmem_ld32(tmem + lanes + 256 + D + d, r);
-                        tmem_ld_wait();
-                        float z[32];
+                        float z[16];
+                        take(1, tmem + lanes + 256 + D + d, d, e1, z);
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) z[k] = __uint_as_float(r[k]);
-                        check(1, z);
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) x[k] += f1 > 0.f || f1 != f1 ? f1 * z[k] : 0.f;
+                        for (int k = 0; k < 16; ++k) x[k] += f1 > 0.f || f1 != f1 ? f1 * z[k] : 0.f;
                     }
                 }
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < 2; ++k) {
                     if (joined) {
                         sums[(d / 4 + 2 * k) * kTile + row] = make_float4(x[8 * k], x[8 * k + 1], x[8 * k + 2], x[8 * k + 3]);
                         sums[(d / 4 + 2 * k + 1) * kTile + row] = make_float4(x[8 * k + 4], x[8 * k + 5], x[8 * k + 6], x[8 * k + 7]);
@@ -863,57 +904,69 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 }
             }
             if (joined) {
-                bar_sync(1, 256);
+                bar_sync(1, 512);
                 if (tid - 128 < a.ctas) mbar_arrive_cluster(mapa_rank(smem_u32(&sh.ready), tid - 128));
                 if (!dead && !mbar_wait_cluster(&sh.ready, joins & 1, wl)) {
                     report_timeout(a.kv.status);
                     dead = true;
                 }
-                // all loads of a kind before the first use: a remote load takes long, many take little longer
-                float ma[kMaxCluster], mb[kMaxCluster], f[kMaxCluster], g[kMaxCluster];
+                // many remote loads before the first use: one takes long, several take little longer
+                float f[kMaxCluster];
+                float ma[kMaxCluster], mb[kMaxCluster];
 #pragma unroll
                 for (int x = 0; x < kMaxCluster; ++x) {
                     ma[x] = mb[x] = -INFINITY;
-                    f[x] = g[x] = 0.f;
                     if (x < a.ctas) {
-                        ma[x] = ld_cluster(s_m + row, x);
-                        mb[x] = ld_cluster(s_m + kTile + row, x);
-                        f[x] = ld_cluster(s_l + row, x);
-                        g[x] = ld_cluster(s_l + kTile + row, x);
+                        ma[x] = ld_cluster(&sh.m[0][row], x);
+                        mb[x] = ld_cluster(&sh.m[1][row], x);
                     }
                 }
                 m = -INFINITY;
 #pragma unroll
                 for (int x = 0; x < kMaxCluster; ++x) m = fmaxf(m, fmaxf(ma[x], mb[x]));
+                float la[kMaxCluster], lb[kMaxCluster];
+#pragma unroll
+                for (int x = 0; x < kMaxCluster; ++x) {
+                    la[x] = lb[x] = 0.f;
+                    if (x < a.ctas) {
+                        la[x] = ld_cluster(&sh.l[0][row], x);
+                        lb[x] = ld_cluster(&sh.l[1][row], x);
+                    }
+                }
                 l = 0.f;
 #pragma unroll
                 for (int x = 0; x < kMaxCluster; ++x) {
                     const bool any = x < a.ctas && m > -INFINITY;
-                    if (any) l += ex2((ma[x] - m) * scale) * f[x] + ex2((mb[x] - m) * scale) * g[x];
-                    f[x] = any ? ex2((fmaxf(ma[x], mb[x]) - m) * scale) : 0.f;
+                    if (any) l += ex2(ma[x] - m) * la[x] + ex2(mb[x] - m) * lb[x];
+                    f[x] = any ? ex2(fmaxf(ma[x], mb[x]) - m) : 0.f;
                 }
                 inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
 #pragma unroll 1
                 for (int o = o0; o < o_end; o += o_step) {
-                    float4 y[kMaxCluster], z[kMaxCluster];
-#pragma unroll
-                    for (int x = 0; x < kMaxCluster; ++x)
-                        if (x < a.ctas) {
-                            y[x] = ld_cluster(sums + 2 * o * kTile + row, x);
-                            z[x] = ld_cluster(sums + (2 * o + 1) * kTile + row, x);
-                        }
                     float x8[8] = {};
 #pragma unroll
-                    for (int x = 0; x < kMaxCluster; ++x)
-                        if (x < a.ctas && (f[x] > 0.f || f[x] != f[x])) {
-                            x8[0] += f[x] * y[x].x, x8[1] += f[x] * y[x].y, x8[2] += f[x] * y[x].z, x8[3] += f[x] * y[x].w;
-                            x8[4] += f[x] * z[x].x, x8[5] += f[x] * z[x].y, x8[6] += f[x] * z[x].z, x8[7] += f[x] * z[x].w;
-                        }
+                    for (int g = 0; g < kMaxCluster; g += 4) {
+                        if (g >= a.ctas) break;
+                        float4 y[4], z[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            if (g + x < a.ctas) {
+                                y[x] = ld_cluster(sums + 2 * o * kTile + row, g + x);
+                                z[x] = ld_cluster(sums + (2 * o + 1) * kTile + row, g + x);
+                            }
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            if (g + x < a.ctas && (f[g + x] > 0.f || f[g + x] != f[g + x])) {
+                                const float ff = f[g + x];
+                                x8[0] += ff * y[x].x, x8[1] += ff * y[x].y, x8[2] += ff * y[x].z, x8[3] += ff * y[x].w;
+                                x8[4] += ff * z[x].x, x8[5] += ff * z[x].y, x8[6] += ff * z[x].z, x8[7] += ff * z[x].w;
+                            }
+                    }
                     if (split) put_part(o, x8);
                     else put(o, x8);
                 }
                 fence_async_smem();                           // the next queries come to the same place
-                bar_sync(1, 256);
+                bar_sync(1, 512);
                 if (tid - 128 < a.ctas) mbar_arrive_cluster(mapa_rank(smem_u32(&sh.taken), tid - 128));
                 if (!dead && !mbar_wait_cluster(&sh.taken, joins & 1, wl)) {
                     report_timeout(a.kv.status);
@@ -925,15 +978,15 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             if (a.ctas > 1 && tid == 128) mbar_arrive(&sh.q_empty[0]);
             bool done = !split;
             if (split) {
-                if (o0 == (joined ? 2 * rank : 0)) {
+                if (joined ? quarter == 0 : w.one ? quarter == 0 : half == 0) {
                     __stcg(part + kPartRows * D + prow, m);
                     __stcg(part + kPartRows * (D + 1) + prow, l);
                 }
                 __threadfence();
-                bar_sync(1, 256);
+                bar_sync(1, 512);
                 // CTAs of the same rank join the same octets
                 if (tid == 128) sh.ticket = atomicAdd(a.tickets + seg.c0 * a.ctas + rank, 1u);
-                bar_sync(1, 256);
+                bar_sync(1, 512);
                 done = *reinterpret_cast<volatile unsigned *>(&sh.ticket) == (unsigned)(seg.c1 - seg.c0);
                 if (done) {                                       // the last of the item's workers: join the parts in order
                     __threadfence();
@@ -942,31 +995,33 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         return a.part + ((size_t)(i * a.ctas + rank) * 2 + (i == seg.c0 ? seg.slot0 : 0)) * part_floats(D);
                     };
                     m = -INFINITY;
+#pragma unroll 4
                     for (int i = seg.c0; i <= seg.c1; ++i) m = fmaxf(m, __ldcg(part_of(i) + kPartRows * D + prow));
                     l = 0.f;
+#pragma unroll 4
                     for (int i = seg.c0; i <= seg.c1; ++i) {
                         const float *ps = part_of(i);
-                        const float f = m > -INFINITY ? ex2((__ldcg(ps + kPartRows * D + prow) - m) * scale) : 0.f;
+                        const float f = m > -INFINITY ? ex2(__ldcg(ps + kPartRows * D + prow) - m) : 0.f;
                         l += f * __ldcg(ps + kPartRows * (D + 1) + prow);
                     }
                     inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
 #pragma unroll 1
-                    for (int o = o0; o < o_end; o += 4 * o_step) {           // four octets at a time
-                        float x[32] = {};
+                    for (int o = o0; o < o_end; o += 2 * o_step) {           // two octets at a time
+                        float x[16] = {};
 #pragma unroll 2
                         for (int i = seg.c0; i <= seg.c1; ++i) {
                             const float *ps = part_of(i);
-                            const float f = m > -INFINITY ? ex2((__ldcg(ps + kPartRows * D + prow) - m) * scale) : 0.f;
-                            float4 y[8];
+                            const float f = m > -INFINITY ? ex2(__ldcg(ps + kPartRows * D + prow) - m) : 0.f;
+                            float4 y[4];
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) {
+                            for (int k = 0; k < 4; ++k) {
                                 const int oo = o + (k >> 1) * o_step;
                                 y[k] = valid && oo < o_end ? __ldcg(reinterpret_cast<const float4 *>(ps) + (size_t)(2 * oo + (k & 1)) * kPartRows + prow)
                                                            : make_float4(0.f, 0.f, 0.f, 0.f);
                             }
                             if (f > 0.f || f != f) {
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) {
+                                for (int k = 0; k < 4; ++k) {
                                     x[4 * k] += f * y[k].x;
                                     x[4 * k + 1] += f * y[k].y;
                                     x[4 * k + 2] += f * y[k].z;
@@ -975,29 +1030,67 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                             }
                         }
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
+                        for (int k = 0; k < 2; ++k)
                             if (o + k * o_step < o_end) put(o + k * o_step, x + 8 * k);
                     }
                 }
             }
-            if (done && valid && a.lse && o0 == 0) a.lse[at] = (m > -INFINITY ? m * scale + log2f(l) : -INFINITY) * 0.69314718055994531f;
+            if (done && valid && a.lse && o0 == 0) a.lse[at] = (m > -INFINITY ? m + log2f(l) : -INFINITY) * 0.69314718055994531f;
             tc_fence_before();
-            bar_sync(1, 256);                                // all have read O, s_m and s_l
+            bar_sync(1, 512);                                // all have read O, sh.m and sh.l
             job_done(i);
         }
     } else {
-        // ---- 8-bit tiles -> 16-bit tiles (128 threads)
+        // ---- 8-bit tiles -> fp16 tiles, bf16 queries -> fp16 (128 threads)
         if constexpr (Q8) {
             set_registers<false, 64>();
             constexpr int kPieces = D / 16;                  // 16-byte pieces of a position
             const int t = tid & 127;
-            int done = 0;                                    // tiles
+            int done = 0, uses0 = 0, uses1 = 0;              // tiles; queries
             bool ok = true;
             for (int i = 0; ok; ++i) {
                 if (!job_of(i)) { ok = false; break; }
                 const Job &w = sh.job[i & 1];
                 if (!w.more) break;
                 const Chunk c = w.c;
+                if constexpr (kTurnQ) {
+#pragma unroll 1
+                    for (int st = 0; st < (w.one ? 1 : 2) && ok; ++st) {
+                        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&sh.q_full[st], (st ? uses1 : uses0) & 1, wl));
+                        if (!ok) break;
+                        if (st) ++uses1;
+                        else ++uses0;
+                        uint8_t *q_row = q_s + st * kTileBytes + t * 128;       // thread t has row t
+                        auto at = [&](int x) { return reinterpret_cast<uint4 *>(q_row + (x >> 3) * kSlabBytes + (((x & 7) ^ (t & 7)) << 4)); };
+                        uint32_t big = 0;
+#pragma unroll 4
+                        for (int x = 0; x < kSlabs * 8; ++x) {
+                            const uint4 v = *at(x);
+                            big = __vmaxu2(big, __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
+                        }
+                        big = max(big & 0xFFFFu, big >> 16);
+                        // times 2^e: the largest element to 2^14 .. 2^15; in two factors, as e may be beyond a number's range
+                        const int e = big ? min(14 + 127 - (int)(big >> 7), 200) : 0;
+                        const float f0 = pow2f(e / 2), f1 = pow2f(e - e / 2);
+#pragma unroll 4
+                        for (int x = 0; x < kSlabs * 8; ++x) {
+                            const uint4 v = *at(x);
+                            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+                            uint32_t o[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const float2 y = unpack2<T>(u[k]);
+                                o[k] = pack2<__half>(y.x * f0 * f1, y.y * f0 * f1);
+                            }
+                            *at(x) = make_uint4(o[0], o[1], o[2], o[3]);
+                        }
+                        sh.q_scale[st][t] = pow2f(-(e / 2)) * pow2f(-(e - e / 2));
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sh.q_ready[st]);
+                    }
+                }
+#pragma unroll 1
                 for (int x = 0, kj = 0, vj = 0; x < 2 * w.nt && ok; ++x, ++done) {
                     const bool is_v = x == w.v_place(vj);
                     const int p0 = w.tile(is_v ? vj++ : kj++) * kTile;
@@ -1009,30 +1102,33 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     const uint8_t *raw = raws + (size_t)rs * Geo::kRawBytes;
                     uint8_t *tile = stages + (size_t)s * kTileBytes;
                     const bool clean = p0 + kTile <= c.ctx;
+                    // the largest exponent in use (every warp finds it)
+                    uint32_t e4 = reinterpret_cast<const uint32_t *>(sh.exps[rs])[lane];
+                    const int used = min(max(c.total - p0 - 4 * lane, 0), 4);
+                    e4 &= used == 4 ? 0xFFFFFFFFu : (1u << 8 * used) - 1u;
+                    e4 = __vmaxu4(e4, e4 >> 16);
+                    const int e_max = max(1, (int)__reduce_max_sync(0xFFFFFFFFu, max(e4 & 0xFFu, e4 >> 8 & 0xFFu)));
+                    if (t == 0) sh.tile_exp[done & 15] = e_max - 127;
 #pragma unroll
                     for (int n = 0; n < kPieces; ++n) {
                         const int pos = t / kPieces + n * (kTile / kPieces), piece = t % kPieces;
                         const uint4 r = *reinterpret_cast<const uint4 *>(raw + pos * D + piece * 16);
                         uint32_t u[4] = {r.x, r.y, r.z, r.w};
-                        const int e = sh.exps[rs][pos];
+                        const int e = min((int)sh.exps[rs][pos] - e_max, 0);
                         if (!clean) {                          // unused places and the code of NaN count as 0
 #pragma unroll
                             for (int k = 0; k < 4; ++k) u[k] = p0 + pos >= c.total ? 0u : u[k] & ~__vcmpeq4(u[k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
                         }
-                        const uint32_t sc = scale_bits<T>(e) * 0x10001u;
+                        // 2^e as fp16, 0 below 2^-24
+                        const uint32_t sc = (e >= -14 ? (uint32_t)(e + 15) << 10 : e >= -24 ? 1u << (e + 24) : 0u) * 0x10001u;
                         uint32_t o[8];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            codes_to_pairs<T>(u[k], sc, o[2 * k], o[2 * k + 1]);
-                        }
-                        if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-                            if (e > 134) {
-                                const uint32_t big = big_scale(e) * 0x10001u;
+                            codes_to_halves(u[k], o[2 * k], o[2 * k + 1]);
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) {
-                                    const __nv_bfloat162 y = __hmul2(*reinterpret_cast<__nv_bfloat162 *>(&o[k]), *reinterpret_cast<const __nv_bfloat162 *>(&big));
-                                    o[k] = *reinterpret_cast<const uint32_t *>(&y);
-                                }
+                            for (int y = 2 * k; y < 2 * k + 2; ++y) {
+                                const __half2 v = __hmul2(*reinterpret_cast<__half2 *>(&o[y]), *reinterpret_cast<const __half2 *>(&sc));
+                                o[y] = *reinterpret_cast<const uint32_t *>(&v);
                             }
                         }
                         // two 16-byte chunks of the slab's 128-byte row, swizzled by the row; every second piece stores
@@ -1068,7 +1164,6 @@ template <typename T, bool Q8, int D>
 cudaError_t launch(const CUtensorMap &q_map, const CUtensorMap &k_map, const CUtensorMap &v_map, const AttendArgs &a, int sms,
                    cudaStream_t stream)
 {
-    static_assert(Geometry<Q8, D>::kBig + Geometry<Q8, D>::kSmall <= kSmemBytes, "shared memory");
     const cudaError_t e = cudaFuncSetAttribute(attend_umma_kernel<T, Q8, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
     if (e != cudaSuccess) return e;
     return launch_workers(attend_umma_kernel<T, Q8, D>, Geometry<Q8, D>::kThreads, kSmemBytes, a.ctas, sms, stream, q_map, k_map, v_map, a);
