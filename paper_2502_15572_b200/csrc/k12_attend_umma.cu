@@ -42,7 +42,7 @@ namespace {
 constexpr int kTile = 128;                                 // rows of a row tile, positions of a tile
 constexpr int kSlabBytes = kTile * 128;                    // 64 elements of every row of a tile
 constexpr float kSlack = 8.f;
-constexpr int kEveryFma = 16;                              // two of so many exponentials are taken on the FMA pipes
+constexpr int kEveryFma = 8;                               // two of so many exponentials are taken on the FMA pipes
 constexpr int kFixed = 2;                                  // queries and join of a segment take about as long as two tiles
 
 template <bool Q8, int D>
@@ -1109,12 +1109,21 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     e4 = __vmaxu4(e4, e4 >> 16);
                     const int e_max = max(1, (int)__reduce_max_sync(0xFFFFFFFFu, max(e4 & 0xFFu, e4 >> 8 & 0xFFu)));
                     if (t == 0) sh.tile_exp[done & 15] = e_max - 127;
+                    // all of a thread's pieces before the first store, which the compiler would not move a load across
+                    const int piece = t % kPieces;
+                    uint4 codes[kPieces];
+                    int exps[kPieces];
 #pragma unroll
                     for (int n = 0; n < kPieces; ++n) {
-                        const int pos = t / kPieces + n * (kTile / kPieces), piece = t % kPieces;
-                        const uint4 r = *reinterpret_cast<const uint4 *>(raw + pos * D + piece * 16);
-                        uint32_t u[4] = {r.x, r.y, r.z, r.w};
-                        const int e = min((int)sh.exps[rs][pos] - e_max, 0);
+                        const int pos = t / kPieces + n * (kTile / kPieces);
+                        codes[n] = *reinterpret_cast<const uint4 *>(raw + pos * D + piece * 16);
+                        exps[n] = sh.exps[rs][pos];
+                    }
+#pragma unroll
+                    for (int n = 0; n < kPieces; ++n) {
+                        const int pos = t / kPieces + n * (kTile / kPieces);
+                        uint32_t u[4] = {codes[n].x, codes[n].y, codes[n].z, codes[n].w};
+                        const int e = min(exps[n] - e_max, 0);
                         if (!clean) {                          // unused places and the code of NaN count as 0
 #pragma unroll
                             for (int k = 0; k < 4; ++k) u[k] = p0 + pos >= c.total ? 0u : u[k] & ~__vcmpeq4(u[k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
