@@ -228,6 +228,7 @@ struct AttendArgs {
     FastDiv by_rows;            // rows (few rows) or tokens (many) of a row tile
     FastDiv by_unit;            // positions (few rows) or 128-position tiles (many) of a unit of work
     int ctas;                   // CTAs of a worker: 1, or a cluster (see kv_plan.cuh)
+    int tile_tokens;            // tokens of a 128-row tile (many rows)
     int groups;                 // workers of a CTA (few rows; then ctas is 1)
     int fixed;                  // what an item costs besides its units, in units
     int small;                  // the plan's numbers fit 32 bits

@@ -10,8 +10,8 @@
 //     P_w = 2^(scale S_w - m)        two threads own a row, 64 positions each: no shuffles; 16 bits, back to TMEM
 //     O_w += P_w V         P from TMEM, V as stored ([position][d] is the MN-major operand)
 //
-// When there are fewer items than CTAs, clusters of up to eight CTAs share an item: the 2 x ctas streams take every
-// (2 x ctas)-th tile, and each CTA adds up its share of the sums over distributed shared memory.
+// When there are fewer items than CTAs, clusters of two or four CTAs share an item: the 2 x ctas streams take every
+// (2 x ctas)-th tile and send their sums through distributed shared memory, each CTA adding up its share of them.
 //
 // Items of more than 128 rows give the streams two row tiles and every loaded tile of positions to both; items of
 // up to 128 rows give both streams the same rows and every second tile each, and join them at the end.  Rows of a group of heads are
@@ -42,6 +42,7 @@ namespace {
 constexpr int kTile = 128;                                 // rows of a row tile, positions of a tile
 constexpr int kSlabBytes = kTile * 128;                    // 64 elements of every row of a tile
 constexpr float kSlack = 8.f;
+constexpr int kMaxCtas = 4;                                // of a cluster
 constexpr int kEveryFma = 8;                               // two of so many exponentials are taken on the FMA pipes
 constexpr int kFixed = 2;                                  // queries and join of a segment take about as long as two tiles
 
@@ -49,17 +50,22 @@ template <bool Q8, int D>
 struct Geometry {
     static constexpr int kSlabs = D / 64;
     static constexpr int kTileBytes = kSlabs * kSlabBytes;
-    static constexpr int kStages = (D == 128 ? 1 : 2) * (Q8 ? 3 : 5);     // 16-bit tiles
-    static constexpr int kRaw = Q8 ? (D == 128 ? 3 : 6) : 0;              // 8-bit tiles
+    static constexpr int kStages = (D == 128 ? 1 : 2) * (Q8 ? 3 : 4);     // 16-bit tiles
+    static constexpr int kRaw = Q8 ? (D == 128 ? 1 : 2) * 2 : 0;          // 8-bit tiles
     static constexpr int kRawBytes = kTile * D;
     static constexpr int kThreads = Q8 ? 768 : 640;
-    static constexpr int kBig = 2 * kTileBytes + kStages * kTileBytes + kRaw * kRawBytes;
+    // Two tiles of queries -- or one, and in a cluster what its CTAs send: sums (of all but a CTA itself, at most 3/4 of
+    // 128 rows in fp32), maxima and weight sums -- then the rings.
+    static constexpr int kMl = kMaxCtas * kTile * 8;
+    static constexpr int kFront = kTileBytes + kTile * D * 4 / kMaxCtas * (kMaxCtas - 1) + kMl;
+    static_assert(kFront >= 2 * kTileBytes && kFront % 1024 == 0, "room for the queries, tiles aligned");
+    static constexpr int kBig = kFront + kStages * kTileBytes + kRaw * kRawBytes;
 };
 constexpr int kSmemBytes = 232448;                         // all of an SM's shared memory (one CTA per SM, by TMEM too)
 
-// Row tiles of one or two streams.
+// Row tiles of one or two streams (of one in a cluster).
 struct ManyRows {
-    static __device__ __forceinline__ int per_tile(const AttendArgs &a) { return (int)a.by_rows.d >> 1; }     // tokens of a stream
+    static __device__ __forceinline__ int per_tile(const AttendArgs &a) { return a.tile_tokens; }     // tokens of a stream
     static __device__ __forceinline__ int row_tiles(const AttendArgs &a, const Chunk &k) { return a.by_rows.ceil(k.len); }
     static __device__ __forceinline__ int tokens(const AttendArgs &a, const Chunk &k, int r)
     {
@@ -122,7 +128,7 @@ struct Shared {
     uint64_t raw_full[kRaw ? kRaw : 1], raw_empty[kRaw ? kRaw : 1];
     uint64_t q_full[2], q_ready[2], q_empty[2], s_full[2], p_full[2], o_full[2];
     uint64_t job_full[2], job_empty[2];
-    uint64_t ready, taken;                                 // cluster: every CTA's sums are in place / have been read
+    uint64_t ready, taken;                                 // cluster: all sums have come / every CTA has read its share
     alignas(16) uint8_t exps[kRaw ? kRaw : 1][kRaw ? kTile : 16];      // exponents of the 8-bit tiles (bulk copies: 16-byte aligned)
     float q_scale[2][kRaw ? kTile : 1];                    // 8-bit: 1 / power of two that a query row was multiplied by
     int tile_exp[16];                                      // 8-bit: largest exponent of the last tiles, by place
@@ -338,7 +344,10 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     static_assert(Geo::kBig + sizeof(Sh) <= kSmemBytes, "shared memory");
     extern __shared__ uint8_t smem_raw[];
     uint8_t *q_s = smem_raw;
-    uint8_t *stages = q_s + 2 * kTileBytes;
+    float4 *sent = reinterpret_cast<float4 *>(q_s + kTileBytes);       // [other CTA][octet / CTAs][2][128 rows]
+    float4 *kept = reinterpret_cast<float4 *>(q_s);        // this CTA's own share, where its queries were
+    float2 *sent_ml = reinterpret_cast<float2 *>(q_s + Geo::kFront - Geo::kMl);        // [CTA][128 rows]
+    uint8_t *stages = q_s + Geo::kFront;
     uint8_t *raws = stages + kStages * kTileBytes;
     Sh &sh = *reinterpret_cast<Sh *>(raws + Geo::kRaw * Geo::kRawBytes);
     if (smem_u32(smem_raw) & 1023u) {                       // shared memory never starts there
@@ -349,45 +358,56 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     const long long wl = a.wait_cycles > 0 ? a.wait_cycles : kWaitCycles;
     const int rank = a.ctas > 1 ? (int)cluster_ctarank() : 0;
 
-    if (tid == 0) {
-        for (int s = 0; s < kStages; ++s) {
-            mbar_init(&sh.full[s], Q8 ? 4 : 1);
-            mbar_init(&sh.empty[s], 2);                     // both streams
+    KvPlan<ManyRows> plan;
+    bool more = false;
+    if (warp == 0) {
+        if (lane < kStages) {
+            mbar_init(&sh.full[lane], Q8 ? 4 : 1);
+            mbar_init(&sh.empty[lane], 2);                  // both streams
         }
-        for (int s = 0; s < Geo::kRaw; ++s) {
-            mbar_init(&sh.raw_full[s], 1);
-            mbar_init(&sh.raw_empty[s], 4);
+        if (lane < Geo::kRaw) {
+            mbar_init(&sh.raw_full[lane], 1);
+            mbar_init(&sh.raw_empty[lane], 4);
         }
-        for (int w = 0; w < 2; ++w) {
-            mbar_init(&sh.q_full[w], 1);
-            mbar_init(&sh.q_ready[w], 4);
-            mbar_init(&sh.q_empty[w], w == 0 && a.ctas > 1 ? 3 : 2);      // both streams; in a cluster the sums pass through place 0
-            mbar_init(&sh.s_full[w], 1);
-            mbar_init(&sh.p_full[w], 8);
-            mbar_init(&sh.o_full[w], 1);
-            mbar_init(&sh.job_full[w], 1);
-            mbar_init(&sh.job_empty[w], 3 + 16 + (Q8 ? 4 : 0));           // a warp each: loads, products, softmax, conversion
+        if (lane < 2) {
+            mbar_init(&sh.q_full[lane], 1);
+            mbar_init(&sh.q_ready[lane], 4);
+            mbar_init(&sh.q_empty[lane], lane == 0 && a.ctas > 1 ? 3 : 2);    // both streams; in a cluster sums are kept in place 0
+            mbar_init(&sh.s_full[lane], 1);
+            mbar_init(&sh.p_full[lane], 8);
+            mbar_init(&sh.o_full[lane], 1);
+            mbar_init(&sh.job_full[lane], 1);
+            mbar_init(&sh.job_empty[lane], 3 + 16 + (Q8 ? 4 : 0));        // a warp each: loads, products, softmax, conversion
         }
-        mbar_init(&sh.ready, a.ctas);
-        mbar_init(&sh.taken, a.ctas);
-        sh.tensor = 0;
+        if (lane == 2) {
+            mbar_init(&sh.ready, 1);
+            mbar_init(&sh.taken, a.ctas);
+            sh.tensor = 0;
+        }
         mbar_fence_init();
-        tma_prefetch_desc(&q_map);
-        tma_prefetch_desc(&k_map);
-        tma_prefetch_desc(&v_map);
-    }
-    if (warp == 3) {
+        if (lane == 3) {
+            tma_prefetch_desc(&q_map);
+            tma_prefetch_desc(&k_map);
+            tma_prefetch_desc(&v_map);
+        }
+    } else if (warp == 3) {
         tmem_alloc(&sh.tmem, 512);
         tmem_relinquish();
     }
-    tc_fence_before();
-    __syncwarp();
-    if (a.ctas > 1) cluster_sync_all();                     // the neighbours' barriers are set up
-    else __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem = sh.tmem;                          // S0, S1 at 0, 128; O0, O1 at 256, 256 + D
     pdl_wait();                                             // what follows reads what earlier kernels wrote
     pdl_launch_dependents();
+    if (warp == 2) more = plan.start(a, lane, blockIdx.x / a.ctas, gridDim.x / a.ctas);     // the same for the whole cluster
+    tc_fence_before();
+    __syncwarp();
+    if (a.ctas > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // this CTA's barriers are set up
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;                          // S0, S1 at 0, 128; O0, O1 at 256, 256 + D
+    bool cluster_up = a.ctas == 1;                          // the neighbours' barriers are, as far as this warp knows
+    auto cluster_wait = [&] {
+        if (!cluster_up) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        cluster_up = true;
+    };
 
     // Segment number `i` of this CTA, when warp 2 has worked it out; false = a wait ran out.  For whole warps.
     auto job_of = [&](int i) { return __all_sync(0xFFFFFFFFu, mbar_wait(&sh.job_full[i & 1], (i >> 1) & 1, wl)); };
@@ -398,9 +418,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     };
 
     if (warp < 4) {
-        KvPlan<ManyRows> plan;
-        bool more = false;
-        if (warp == 2) more = plan.start(a, lane, blockIdx.x / a.ctas, gridDim.x / a.ctas);     // the same for the whole cluster
         set_registers<false, 64>();
         if (warp == 0) {
             // ---- tiles of keys and values: 16-bit ones straight into the stages, 8-bit ones into the raw ring
@@ -593,7 +610,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     }
     mbar_arrive(&sh.job_full[i & 1]);
                     if (!more) break;
-                    const int tiles = w.one ? 1 : 2, y = w.seg.head * a.group, z = plan.c.row0 + 2 * w.seg.rt * tokens;
+                    const int tiles = w.one ? 1 : 2, y = w.seg.head * a.group, z = plan.c.row0 + w.seg.rt * (int)a.by_rows.d;
             #pragma unroll 1
                     for (int st = 0; st < tiles && ok; ++st) {
                         int &uses = st ? uses1 : uses0;
@@ -633,7 +650,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             const Chunk &c = w.c;
             const Segment &seg = w.seg;
             const int n_mine = w.n[st];
-            const int first_tok = (2 * seg.rt + (w.one ? 0 : st)) * ManyRows::per_tile(a);
+            const int first_tok = seg.rt * (int)a.by_rows.d + (w.one ? 0 : st * ManyRows::per_tile(a));
             const int tok = first_tok + row_tok;              // of this row; may lie behind the chunk
             const int limit = a.mask ? c.total : min(c.total, c.ctx + min(tok, c.len - 1) + 1);
             const int all_seen = min(c.total, a.mask ? c.ctx : c.ctx + min(first_tok, c.len - 1) + 1);    // by every row
@@ -812,10 +829,10 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             tc_fence_after();
             // A thread has a row and some OCTETS of its elements, o0, o0 + o_step, ...: with two row tiles its stream's row and
             // half of the octets; with one, a quarter of the octets from both streams, or in a cluster its CTA's share of them.
-            const bool joined = w.one && a.ctas > 1;
+            const bool joined = a.ctas > 1;
             const int prow = w.one ? row : st * kTile + row, quarter = 2 * st + half;
             const int d0 = w.one ? quarter * (D / 4) : half * (D / 2), d1 = w.one ? d0 + D / 4 : d0 + D / 2;
-            const int o0 = joined ? 4 * rank + quarter : d0 / 8;
+            const int o0 = joined ? quarter * a.ctas + rank : d0 / 8;      // in a cluster octet o is with CTA o % ctas
             const int o_step = joined ? 4 * a.ctas : 1, o_end = joined ? D / 8 : d1 / 8;
             float f0 = 1.f, f1 = 0.f;
             l = sh.l[w.one ? 0 : st][row];
@@ -848,8 +865,19 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 __stcg(dst, make_float4(x[0], x[1], x[2], x[3]));
                 __stcg(dst + kPartRows, make_float4(x[4], x[5], x[6], x[7]));
             };
-            // sums of this CTA: 16 elements at a time from TMEM to the result, the part, or (cluster) shared memory
-            float4 *sums = reinterpret_cast<float4 *>(q_s);    // [D / 4][128 rows], where the queries were
+            const int per = D / 8 / a.ctas;                    // octets of a CTA of a cluster
+            if (joined) {
+                cluster_wait();
+                if (tid == 128) mbar_arrive_expect_tx(&sh.ready, (uint32_t)(kTile * ((a.ctas - 1) * per * 32 + a.ctas * 8)));
+                // what was sent the last time has been read
+                if (joins > 0 && !dead && !mbar_wait_cluster(&sh.taken, (joins - 1) & 1, wl)) {
+                    report_timeout(a.kv.status);
+                    dead = true;
+                }
+                if (quarter == 0)
+                    for (int x = 0; x < a.ctas; ++x) st_async(&sent_ml[rank * kTile + row], make_float2(m, l), &sh.ready, x);
+            }
+            // sums of this CTA: 16 elements at a time from TMEM to the result, the part, or the octet's CTA
             auto take = [&](int of, uint32_t addr, int d, float e, float *x) {         // sums of stream `of`
                 uint32_t r[16];
                 tmem_ld16(addr, r);
@@ -894,8 +922,17 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     if (joined) {
-                        sums[(d / 4 + 2 * k) * kTile + row] = make_float4(x[8 * k], x[8 * k + 1], x[8 * k + 2], x[8 * k + 3]);
-                        sums[(d / 4 + 2 * k + 1) * kTile + row] = make_float4(x[8 * k + 4], x[8 * k + 5], x[8 * k + 6], x[8 * k + 7]);
+                        const int o = d / 8 + k, to = o & (a.ctas - 1), n = o / a.ctas;
+                        const float4 y = make_float4(x[8 * k], x[8 * k + 1], x[8 * k + 2], x[8 * k + 3]);
+                        const float4 z = make_float4(x[8 * k + 4], x[8 * k + 5], x[8 * k + 6], x[8 * k + 7]);
+                        if (to == rank) {
+                            kept[2 * n * kTile + row] = y;
+                            kept[(2 * n + 1) * kTile + row] = z;
+                        } else {                               // its place there: 0 for the next CTA in the ring
+                            float4 *at = sent + (((rank - to - 1) & (a.ctas - 1)) * per + n) * 2 * kTile + row;
+                            st_async(at, y, &sh.ready, to);
+                            st_async(at + kTile, z, &sh.ready, to);
+                        }
                     } else if (split) {
                         put_part(d / 8 + k, x + 8 * k);
                     } else {
@@ -904,63 +941,30 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 }
             }
             if (joined) {
-                bar_sync(1, 512);
-                if (tid - 128 < a.ctas) mbar_arrive_cluster(mapa_rank(smem_u32(&sh.ready), tid - 128));
                 if (!dead && !mbar_wait_cluster(&sh.ready, joins & 1, wl)) {
                     report_timeout(a.kv.status);
                     dead = true;
                 }
-                // many remote loads before the first use: one takes long, several take little longer
-                float f[kMaxCluster];
-                float ma[kMaxCluster], mb[kMaxCluster];
-#pragma unroll
-                for (int x = 0; x < kMaxCluster; ++x) {
-                    ma[x] = mb[x] = -INFINITY;
-                    if (x < a.ctas) {
-                        ma[x] = ld_cluster(&sh.m[0][row], x);
-                        mb[x] = ld_cluster(&sh.m[1][row], x);
-                    }
-                }
+                bar_sync(1, 512);                             // what is kept is in place
                 m = -INFINITY;
-#pragma unroll
-                for (int x = 0; x < kMaxCluster; ++x) m = fmaxf(m, fmaxf(ma[x], mb[x]));
-                float la[kMaxCluster], lb[kMaxCluster];
-#pragma unroll
-                for (int x = 0; x < kMaxCluster; ++x) {
-                    la[x] = lb[x] = 0.f;
-                    if (x < a.ctas) {
-                        la[x] = ld_cluster(&sh.l[0][row], x);
-                        lb[x] = ld_cluster(&sh.l[1][row], x);
-                    }
-                }
+                for (int x = 0; x < a.ctas; ++x) m = fmaxf(m, sent_ml[x * kTile + row].x);
                 l = 0.f;
-#pragma unroll
-                for (int x = 0; x < kMaxCluster; ++x) {
-                    const bool any = x < a.ctas && m > -INFINITY;
-                    if (any) l += ex2(ma[x] - m) * la[x] + ex2(mb[x] - m) * lb[x];
-                    f[x] = any ? ex2(fmaxf(ma[x], mb[x]) - m) : 0.f;
+                for (int x = 0; x < a.ctas; ++x) {
+                    const float2 p = sent_ml[x * kTile + row];
+                    l += m > -INFINITY ? ex2(p.x - m) * p.y : 0.f;
                 }
                 inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
 #pragma unroll 1
                 for (int o = o0; o < o_end; o += o_step) {
                     float x8[8] = {};
-#pragma unroll
-                    for (int g = 0; g < kMaxCluster; g += 4) {
-                        if (g >= a.ctas) break;
-                        float4 y[4], z[4];
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            if (g + x < a.ctas) {
-                                y[x] = ld_cluster(sums + 2 * o * kTile + row, g + x);
-                                z[x] = ld_cluster(sums + (2 * o + 1) * kTile + row, g + x);
-                            }
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            if (g + x < a.ctas && (f[g + x] > 0.f || f[g + x] != f[g + x])) {
-                                const float ff = f[g + x];
-                                x8[0] += ff * y[x].x, x8[1] += ff * y[x].y, x8[2] += ff * y[x].z, x8[3] += ff * y[x].w;
-                                x8[4] += ff * z[x].x, x8[5] += ff * z[x].y, x8[6] += ff * z[x].z, x8[7] += ff * z[x].w;
-                            }
+                    for (int x = 0; x < a.ctas; ++x) {
+                        const float f = m > -INFINITY ? ex2(sent_ml[x * kTile + row].x - m) : 0.f;
+                        const float4 *at = (x == rank ? kept : sent + ((x - rank - 1) & (a.ctas - 1)) * per * 2 * kTile) + o / a.ctas * 2 * kTile + row;
+                        const float4 y = at[0], z = at[kTile];
+                        if (f > 0.f || f != f) {
+                            x8[0] += f * y.x, x8[1] += f * y.y, x8[2] += f * y.z, x8[3] += f * y.w;
+                            x8[4] += f * z.x, x8[5] += f * z.y, x8[6] += f * z.z, x8[7] += f * z.w;
+                        }
                     }
                     if (split) put_part(o, x8);
                     else put(o, x8);
@@ -968,14 +972,10 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 fence_async_smem();                           // the next queries come to the same place
                 bar_sync(1, 512);
                 if (tid - 128 < a.ctas) mbar_arrive_cluster(mapa_rank(smem_u32(&sh.taken), tid - 128));
-                if (!dead && !mbar_wait_cluster(&sh.taken, joins & 1, wl)) {
-                    report_timeout(a.kv.status);
-                    dead = true;
-                }
+                if (tid == 128) mbar_arrive(&sh.q_empty[0]);
                 dead = __any_sync(0xFFFFFFFFu, dead);
                 ++joins;
             }
-            if (a.ctas > 1 && tid == 128) mbar_arrive(&sh.q_empty[0]);
             bool done = !split;
             if (split) {
                 if (joined ? quarter == 0 : w.one ? quarter == 0 : half == 0) {
@@ -1161,7 +1161,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     }
     tc_fence_before();
     __syncwarp();
-    if (a.ctas > 1) cluster_sync_all();                     // nobody leaves while a neighbour may read its shared memory
+    cluster_wait();
+    if (a.ctas > 1) cluster_sync_all();                     // nobody leaves while a neighbour may write to its shared memory
     else __syncthreads();
     if (warp == 3) {
         tc_fence_after();
@@ -1186,13 +1187,14 @@ cudaError_t launch_attend_umma(const CUtensorMap &q_map, const CUtensorMap &k_ma
                                const AttendArgs &args, int sms, cudaStream_t stream)
 {
     AttendArgs a = args;
-    // One row tile per sequence and head, and fewer of them than half the SMs: clusters share them.  No more CTAs than give
+    // One row tile per sequence and head (the hint says), and no more of them than half the SMs: clusters share them.  No more CTAs than give
     // every stream a tile of the longest sequence that the table can hold.
     const long long items = (long long)a.kv.B * a.kv.heads, tiles = (((long long)a.kv.width << a.kv.page_shift) + kTile - 1) / kTile;
     long long ctas = a.max_chunk <= kTile / a.group ? sms / items : 1;
     if (ctas > (tiles + 1) / 2) ctas = (tiles + 1) / 2;
-    a.ctas = (int)(ctas < 1 ? 1 : ctas > kMaxCluster ? kMaxCluster : ctas);
-    a.by_rows = FastDiv(2 * (kTile / a.group));
+    a.ctas = ctas >= 4 ? 4 : ctas >= 2 ? 2 : 1;       // (a power of two divides the octets of a row)
+    a.tile_tokens = kTile / a.group;
+    a.by_rows = FastDiv(a.ctas > 1 ? a.tile_tokens : 2 * a.tile_tokens);
     a.by_unit = FastDiv(2 * a.ctas);
     a.groups = 1;
     a.fixed = kFixed;
