@@ -159,6 +159,7 @@ dresd_status dresd_kv_create(void *k_pages, void *v_pages, uint8_t *k_exps, uint
     if ((k_exps == nullptr) != (v_exps == nullptr)) return fail(DRESD_ERR_INVALID, "k_exps and v_exps go together");
     if (dtype != DRESD_F32 && dtype != DRESD_F16 && dtype != DRESD_BF16) return fail(DRESD_ERR_INVALID, "unknown dtype %d", (int)dtype);
     if (dtype == DRESD_F32) return fail(DRESD_ERR_UNSUPPORTED, "the cache holds fp16, bf16 or 8-bit rows");
+    if ((long long)layers * kv_heads > 1 << 24) return fail(DRESD_ERR_UNSUPPORTED, "layers x kv_heads exceed 2^24");
     if (layers < 1 || num_pages < 1 || kv_heads < 1 || page_size < 1 || head_dim < 1)
         return fail(DRESD_ERR_INVALID, "layers = %d, num_pages = %lld, kv_heads = %d, page_size = %d, head_dim = %d", layers,
                     (long long)num_pages, kv_heads, page_size, head_dim);
@@ -327,8 +328,6 @@ dresd_status dresd_kv_keep_draft(dresd_kv *kv, const dresd_kv_batch *batch, cons
     if (n < 1 || L < 1) return fail(DRESD_ERR_INVALID, "bad n/L");
     if (n > DRESD_MAX_TOP_N) return fail(DRESD_ERR_UNSUPPORTED, "n = %d exceeds DRESD_MAX_TOP_N", n);
     if (L > 65536) return fail(DRESD_ERR_UNSUPPORTED, "L = %d exceeds 65536", L);
-    if ((long long)L * a.heads * a.layers * a.d / 8 > 2147483647LL)
-        return fail(DRESD_ERR_UNSUPPORTED, "L = %d drafts' rows of %d layers exceed 2^31 - 1 pieces", L, a.layers);
     kv->last_launches = 0;
     if (a.B == 0) return DRESD_OK;
     if (!is_device_ptr(best) || !is_device_ptr(length)) return fail(DRESD_ERR_INVALID, "best/length must be device pointers");
