@@ -172,7 +172,7 @@ keep_kernel(const KvArgs a, const int32_t *__restrict__ best, const int32_t *__r
     pdl_launch_dependents();
     const int b = blockIdx.y, r = best[b], kept = min(length[b] - 1, L);
     if (r < 1 || r >= n || kept < 1) return;
-    const int lh = (blockIdx.x * kThreads + threadIdx.x) >> 5;
+    const int lh = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     if (lh >= a.layers * a.heads) return;
     const int layer = lh / a.heads, head = lh - layer * a.heads;
     const int lane = threadIdx.x & 31, rows = 32 >> lanes_shift, sub = lane >> lanes_shift, piece = lane & ((1 << lanes_shift) - 1);

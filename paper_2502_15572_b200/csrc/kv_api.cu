@@ -159,7 +159,6 @@ dresd_status dresd_kv_create(void *k_pages, void *v_pages, uint8_t *k_exps, uint
     if ((k_exps == nullptr) != (v_exps == nullptr)) return fail(DRESD_ERR_INVALID, "k_exps and v_exps go together");
     if (dtype != DRESD_F32 && dtype != DRESD_F16 && dtype != DRESD_BF16) return fail(DRESD_ERR_INVALID, "unknown dtype %d", (int)dtype);
     if (dtype == DRESD_F32) return fail(DRESD_ERR_UNSUPPORTED, "the cache holds fp16, bf16 or 8-bit rows");
-    if ((long long)layers * kv_heads > 1 << 24) return fail(DRESD_ERR_UNSUPPORTED, "layers x kv_heads exceed 2^24");
     if (layers < 1 || num_pages < 1 || kv_heads < 1 || page_size < 1 || head_dim < 1)
         return fail(DRESD_ERR_INVALID, "layers = %d, num_pages = %lld, kv_heads = %d, page_size = %d, head_dim = %d", layers,
                     (long long)num_pages, kv_heads, page_size, head_dim);
