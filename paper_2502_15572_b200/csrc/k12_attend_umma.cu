@@ -19,7 +19,7 @@
 //
 // Roles: warp 0 loads tiles (a lane per page and slab, so that small pages are issued side by side), warps 1 and 3 issue the
 // products of a stream each, warp 2 works out the CTA's segments and loads their queries, warps 4-11 and 12-19 are the streams'
-// softmax; with an 8-bit cache warps 20-23 turn codes into 16-bit tiles.
+// softmax; with an 8-bit cache warps 20-27 turn codes into 16-bit tiles.
 //
 // The chain scores -> weights -> second product -> next scores of a stream is what bounds a long call (its S, P and O fill
 // TMEM, so a stream has one tile in the works), hence: two threads to a row, an issuing warp to a stream; the maximum only
@@ -43,6 +43,7 @@ constexpr int kTile = 128;                                 // rows of a row tile
 constexpr int kSlabBytes = kTile * 128;                    // 64 elements of every row of a tile
 constexpr float kSlack = 8.f;
 constexpr int kMaxCtas = 4;                                // of a cluster
+constexpr int kConvert = 8;                                // warps that convert 8-bit tiles
 constexpr int kEveryFma = 8;                               // two of so many exponentials are taken on the FMA pipes
 constexpr int kFixed = 2;                                  // queries and join of a segment take about as long as two tiles
 
@@ -53,7 +54,7 @@ struct Geometry {
     static constexpr int kStages = (D == 128 ? 1 : 2) * (Q8 ? 3 : 4);     // 16-bit tiles
     static constexpr int kRaw = Q8 ? (D == 128 ? 1 : 2) * 2 : 0;          // 8-bit tiles
     static constexpr int kRawBytes = kTile * D;
-    static constexpr int kThreads = Q8 ? 768 : 640;
+    static constexpr int kThreads = Q8 ? 896 : 640;
     // Two tiles of queries -- or one, and in a cluster what its CTAs send: sums (of all but a CTA itself, at most 3/4 of
     // 128 rows in fp32), maxima and weight sums -- then the rings.
     static constexpr int kMl = kMaxCtas * kTile * 8;
@@ -196,9 +197,15 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // A warpgroup's registers per thread.  The warpgroups' shares together are what the CTA was launched with: 640 x 96
-// (64 + 4 x 104 a thread of each), with an 8-bit cache 768 x 80 (64 + 4 x 88 + 64).
+// (64 + 4 x 104 a thread of each), with an 8-bit cache 896 x 72 (56 + 4 x 96 + 2 x 32).
 template <bool kMore, int kCount>
 __device__ __forceinline__ void set_registers()
 {
@@ -355,19 +362,19 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         return;
     }
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const long long wl = a.wait_cycles > 0 ? a.wait_cycles : kWaitCycles;
+    const long long wl = a.wait_cycles;
     const int rank = a.ctas > 1 ? (int)cluster_ctarank() : 0;
 
     KvPlan<ManyRows> plan;
     bool more = false;
     if (warp == 0) {
         if (lane < kStages) {
-            mbar_init(&sh.full[lane], Q8 ? 4 : 1);
+            mbar_init(&sh.full[lane], Q8 ? kConvert : 1);
             mbar_init(&sh.empty[lane], 2);                  // both streams
         }
         if (lane < Geo::kRaw) {
             mbar_init(&sh.raw_full[lane], 1);
-            mbar_init(&sh.raw_empty[lane], 4);
+            mbar_init(&sh.raw_empty[lane], kConvert);
         }
         if (lane < 2) {
             mbar_init(&sh.q_full[lane], 1);
@@ -377,7 +384,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             mbar_init(&sh.p_full[lane], 8);
             mbar_init(&sh.o_full[lane], 1);
             mbar_init(&sh.job_full[lane], 1);
-            mbar_init(&sh.job_empty[lane], 3 + 16 + (Q8 ? 4 : 0));        // a warp each: loads, products, softmax, conversion
+            mbar_init(&sh.job_empty[lane], 3 + 16 + (Q8 ? kConvert : 0));        // a warp each: loads, products, softmax, conversion
         }
         if (lane == 2) {
             mbar_init(&sh.ready, 1);
@@ -418,7 +425,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     };
 
     if (warp < 4) {
-        set_registers<false, 64>();
+        set_registers<false, Q8 ? 56 : 64>();
         if (warp == 0) {
             // ---- tiles of keys and values: 16-bit ones straight into the stages, 8-bit ones into the raw ring
             constexpr int kRing = Q8 ? Geo::kRaw : kStages;
@@ -493,7 +500,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             constexpr uint32_t kIdescO = kCommon | ((uint32_t)(D >> 3) << 17) | (1u << 16);       // second operand MN-major
             auto uniform = [](int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); };
             const int st = uniform(warp == 3);
-            const uint32_t t0 = uniform(tmem), s_at = t0 + st * kTile, o_at = t0 + 256 + st * D;
+            const uint32_t t0 = uniform(tmem), s_at = t0 + st * kTile, p_at = s_at + (Q8 ? 32 : 0), o_at = t0 + 256 + st * D;
             const uint64_t q_desc = make_desc(smem_u32(q_s)), k_desc = make_desc(smem_u32(stages)), v_desc = make_desc_mn(smem_u32(stages));
             uint64_t *q_bar = kTurnQ ? sh.q_ready : sh.q_full, *q_empty = sh.q_empty;
             const bool issuer = elect_one();
@@ -573,10 +580,10 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     ++steps;
                     const uint64_t vd = v_desc + s * (kTileBytes >> 4);
                     if (issuer) {
-                        if (j == 0) umma_f16_ta(o_at, s_at, vd, kIdescO, 0);
-                        else umma_f16_ta(o_at, s_at, vd, kIdescO, 1);
+                        if (j == 0) umma_f16_ta(o_at, p_at, vd, kIdescO, 0);
+                        else umma_f16_ta(o_at, p_at, vd, kIdescO, 1);
 #pragma unroll
-                        for (int k = 1; k < kTile / 16; ++k) umma_f16_ta(o_at, s_at + 8 * k, vd + 128 * k, kIdescO, 1);
+                        for (int k = 1; k < kTile / 16; ++k) umma_f16_ta(o_at, p_at + 8 * k + (Q8 && k >= kTile / 32 ? 32 : 0), vd + 128 * k, kIdescO, 1);
                         tc_commit(&sh.empty[s]);
                         if (more) issue_scores(j + 1, y % kStages);
                         else tc_commit(&sh.o_full[st]);
@@ -608,10 +615,10 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         w.c = plan.c;
                         w.set(a, rank);
                     }
-    mbar_arrive(&sh.job_full[i & 1]);
+                    mbar_arrive(&sh.job_full[i & 1]);
                     if (!more) break;
                     const int tiles = w.one ? 1 : 2, y = w.seg.head * a.group, z = plan.c.row0 + w.seg.rt * (int)a.by_rows.d;
-            #pragma unroll 1
+#pragma unroll 1
                     for (int st = 0; st < tiles && ok; ++st) {
                         int &uses = st ? uses1 : uses0;
                         if (uses > 0) ok = mbar_wait(&sh.q_empty[st], (uses - 1) & 1, wl);
@@ -630,12 +637,12 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             }
         }
     } else if (warp < 20) {
-        set_registers<true, Q8 ? 88 : 104>();
+        set_registers<true, Q8 ? 96 : 104>();
         // ---- softmax of stream st; a thread has positions 64 half .. of a tile of its row
         const int st = warp >= 12 ? 1 : 0, half = (warp >> 2) & 1 ? 0 : 1;      // warps 4-7, 12-15: the first half
         const int row = tid & 127;                           // TMEM lane
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;    // (warp % 4) x 32 lanes, in the address's upper half
-        const uint32_t ts = tmem + lanes + st * kTile + 64 * half, tp = tmem + lanes + st * kTile + 32 * half;
+        const uint32_t ts = tmem + lanes + st * kTile + 64 * half, tp = Q8 ? ts + 32 : tmem + lanes + st * kTile + 32 * half;
         const uint32_t to = tmem + lanes + 256 + st * D;
         const int row_tok = a.by_group.div(row);
         int steps = 0, items0 = 0, items1 = 0, joins = 0, base = 0;
@@ -672,11 +679,15 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 dead = __any_sync(0xFFFFFFFFu, dead);
                 ++steps;
                 tc_fence_after();
+                // With a 16-bit cache a thread holds its 64 scores, and weights go to the first half of the tile's columns: 61 rows x 4
+                // heads of 64 behind 8000 positions in 148 items take 125 us.  With an 8-bit cache there are fewer registers (the
+                // converting warps have the rest): 32 scores at a time, the first 32 read twice, weights to the place of
+                // the second 32, 152 us; held and spilled, 207.  (The 16-bit kernel in this form: 130 us.)
                 float s[64];
                 uint32_t *su = reinterpret_cast<uint32_t *>(s);
                 const bool masked = p0 + kTile > all_seen;
                 tmem_ld32(ts, su);
-                tmem_ld32(ts + 32, su + 32);
+                if constexpr (!Q8) tmem_ld32(ts + 32, su + 32);
                 int dv = 0;                                   // 8-bit: weights are multiplied by 2^dv
                 bool over = false;
                 if constexpr (Q8) {
@@ -685,36 +696,48 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     dv = sh.tile_exp[v_at & 15];
                     over = dv > v_exp;
                 }
-                tmem_ld_wait_for(su);
-                tmem_ld_wait_for(su + 32);
-                if (masked) {
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int p = p0 + 64 * half + 32 * k;
-                        const int n = min(max(limit - p, 0), 32);
-                        uint32_t see = n == 32 ? 0xFFFFFFFFu : (1u << n) - 1u;
-                        if (a.mask && p + 32 > c.ctx) {
-                            const uint32_t *mask = a.mask + (long long)(c.row0 + min(tok, c.len - 1)) * a.mask_words;
-                            const int j0 = p - c.ctx;         // place in the chunk of bit 0; context below 0
-                            const int w0 = j0 >> 5;           // floor; -1 at the least
-                            const uint32_t lo = w0 < 0 ? 0xFFFFFFFFu : w0 < a.mask_words ? mask[w0] : 0u;
-                            const uint32_t hi = w0 + 1 < a.mask_words ? mask[w0 + 1] : 0u;
-                            see &= __funnelshift_r(lo, hi, j0 & 31);
-                        }
-#pragma unroll
-                        for (int x = 0; x < 32; ++x)
-                            if (!(see >> x & 1)) s[32 * k + x] = -INFINITY;
+                // What a row sees of 32 positions, and the largest score.
+                auto seen = [&](int p) {
+                    const int n = min(max(limit - p, 0), 32);
+                    uint32_t see = n == 32 ? 0xFFFFFFFFu : (1u << n) - 1u;
+                    if (a.mask && p + 32 > c.ctx) {
+                        const uint32_t *mask = a.mask + (long long)(c.row0 + min(tok, c.len - 1)) * a.mask_words;
+                        const int j0 = p - c.ctx;             // place in the chunk of bit 0; context below 0
+                        const int w0 = j0 >> 5;               // floor; -1 at the least
+                        const uint32_t lo = w0 < 0 ? 0xFFFFFFFFu : w0 < a.mask_words ? mask[w0] : 0u;
+                        const uint32_t hi = w0 + 1 < a.mask_words ? mask[w0 + 1] : 0u;
+                        see &= __funnelshift_r(lo, hi, j0 & 31);
                     }
-                }
+                    return see;
+                };
+                auto hide = [&](float *x, uint32_t see) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (!(see >> k & 1)) x[k] = -INFINITY;
+                };
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                auto largest = [&](const float *x, int n) {
 #pragma unroll
-                for (int k = 0; k < 64; k += 8)
+                    for (int k = 0; k < n; k += 8)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) mx[x] = fmaxf(fmaxf(mx[x], s[k + 2 * x]), s[k + 2 * x + 1]);
+                        for (int y = 0; y < 4; ++y) mx[y] = fmaxf(fmaxf(mx[y], x[k + 2 * y]), x[k + 2 * y + 1]);
+                };
+                uint32_t see = 0xFFFFFFFFu;                   // of the first 32
+                tmem_ld_wait_for(su);
+                if constexpr (Q8) tmem_ld32(ts + 32, su + 32);
+                else tmem_ld_wait_for(su + 32);
+                if (masked) hide(s, see = seen(p0 + 64 * half));
+                if constexpr (Q8) {
+                    largest(s, 32);
+                    tmem_ld_wait_for(su + 32);
+                }
+                if (masked) hide(s + 32, seen(p0 + 64 * half + 32));
+                if constexpr (Q8) largest(s + 32, 32);
+                else largest(s, 64);
                 const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
                 over |= top - m > kSlack;                     // -inf - -inf is NaN: no
                 tc_fence_before();
-                const bool raise = bar_or(2 + st, 256, over); // also: both halves have been read, weights may take their place
+                const bool raise = bar_or(2 + st, 256, over); // one maximum for both halves of a row; both have been read, weights may take their place
                 tc_fence_after();
                 if (raise) {
                     float *pass = &sh.l[st][row];
@@ -753,12 +776,13 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 const float off = (m > -INFINITY ? m : 0.f) - (Q8 ? (float)dv : 0.f);
                 const uint64_t scale2 = pair(scale, scale), off2 = pair(-off, -off);
                 uint64_t sum0 = 0, sum1 = 0;
-                // weights of 32 scores at a time, packed and stored over scores that have been read
-                auto weights = [&](int c0, bool fma) {
-                    uint32_t p[16];
+                // weights of some scores, packed and stored at column c0
+                constexpr int kAtOnce = Q8 ? 16 : 32;
+                auto weights = [&](const float *of, int c0, bool fma) {
+                    uint32_t p[kAtOnce / 2];
 #pragma unroll
-                    for (int k = 0; k < 32; k += 2) {
-                        uint64_t x = fma2(pair(s[c0 + k], s[c0 + k + 1]), scale2, off2);
+                    for (int k = 0; k < kAtOnce; k += 2) {
+                        uint64_t x = fma2(pair(of[k], of[k + 1]), scale2, off2);
                         float lo, hi;
                         if (fma && k % kEveryFma == kEveryFma - 2) {
                             x = ex2_fma(x);
@@ -773,15 +797,27 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         else sum0 = add2(sum0, x);
                         p[k / 2] = pack2<M>(lo, hi);
                     }
-                    tmem_st16(tp + c0 / 2, p);
+                    if constexpr (Q8) tmem_st8(tp + c0, p);
+                    else tmem_st16(tp + c0, p);
                 };
-                if (masked) {                                 // -infinity has to give 0 exactly
-                    weights(0, false);
-                    weights(32, false);
-                } else {
-                    weights(0, true);
-                    weights(32, true);
-                }
+                auto all_weights = [&](bool fma) {            // (masked: -infinity has to give 0 exactly)
+                    if constexpr (Q8) {
+                        tmem_ld16(ts, su);
+                        weights(s + 32, 16, fma);
+                        tmem_ld16(ts + 16, su + 16);
+                        weights(s + 48, 24, fma);
+                        tmem_ld_wait16(su);
+                        tmem_ld_wait16(su + 16);
+                        if (!fma) hide(s, see);
+                        weights(s, 0, fma);
+                        weights(s + 16, 8, fma);
+                    } else {
+                        weights(s, 0, fma);
+                        weights(s + 32, 16, fma);
+                    }
+                };
+                if (masked) all_weights(false);
+                else all_weights(true);
                 float a0, a1;
                 unpair(add2(sum0, sum1), a0, a1);
                 l += Q8 ? (a0 + a1) * pow2f(-dv) : a0 + a1;
@@ -1041,12 +1077,12 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             job_done(i);
         }
     } else {
-        // ---- 8-bit tiles -> fp16 tiles, bf16 queries -> fp16 (128 threads)
+        // ---- 8-bit tiles -> fp16 tiles, bf16 queries -> fp16 
         if constexpr (Q8) {
-            set_registers<false, 64>();
+            set_registers<false, 32>();
             constexpr int kPieces = D / 16;                  // 16-byte pieces of a position
-            const int t = tid & 127;
-            int done = 0, uses0 = 0, uses1 = 0;              // tiles; queries
+            const int t = tid - 640, q_st = t >> 7, q_at = t & 127;      // queries: thread q_at has row q_at of tile q_st
+            int done = 0, uses = 0;                          // tiles; queries
             bool ok = true;
             for (int i = 0; ok; ++i) {
                 if (!job_of(i)) { ok = false; break; }
@@ -1054,14 +1090,11 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 if (!w.more) break;
                 const Chunk c = w.c;
                 if constexpr (kTurnQ) {
-#pragma unroll 1
-                    for (int st = 0; st < (w.one ? 1 : 2) && ok; ++st) {
-                        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&sh.q_full[st], (st ? uses1 : uses0) & 1, wl));
+                    if (q_st == 0 || !w.one) {
+                        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&sh.q_full[q_st], uses++ & 1, wl));
                         if (!ok) break;
-                        if (st) ++uses1;
-                        else ++uses0;
-                        uint8_t *q_row = q_s + st * kTileBytes + t * 128;       // thread t has row t
-                        auto at = [&](int x) { return reinterpret_cast<uint4 *>(q_row + (x >> 3) * kSlabBytes + (((x & 7) ^ (t & 7)) << 4)); };
+                        uint8_t *q_row = q_s + q_st * kTileBytes + q_at * 128;
+                        auto at = [&](int x) { return reinterpret_cast<uint4 *>(q_row + (x >> 3) * kSlabBytes + (((x & 7) ^ (q_at & 7)) << 4)); };
                         uint32_t big = 0;
 #pragma unroll 4
                         for (int x = 0; x < kSlabs * 8; ++x) {
@@ -1084,10 +1117,10 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                             }
                             *at(x) = make_uint4(o[0], o[1], o[2], o[3]);
                         }
-                        sh.q_scale[st][t] = pow2f(-(e / 2)) * pow2f(-(e - e / 2));
+                        sh.q_scale[q_st][q_at] = pow2f(-(e / 2)) * pow2f(-(e - e / 2));
                         fence_async_smem();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&sh.q_ready[st]);
+                        if (lane == 0) mbar_arrive(&sh.q_ready[q_st]);
                     }
                 }
 #pragma unroll 1
@@ -1101,7 +1134,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     if (!ok) break;
                     const uint8_t *raw = raws + (size_t)rs * Geo::kRawBytes;
                     uint8_t *tile = stages + (size_t)s * kTileBytes;
-                    const bool clean = p0 + kTile <= c.ctx;
                     // the largest exponent in use (every warp finds it)
                     uint32_t e4 = reinterpret_cast<const uint32_t *>(sh.exps[rs])[lane];
                     const int used = min(max(c.total - p0 - 4 * lane, 0), 4);
@@ -1109,25 +1141,33 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     e4 = __vmaxu4(e4, e4 >> 16);
                     const int e_max = max(1, (int)__reduce_max_sync(0xFFFFFFFFu, max(e4 & 0xFFu, e4 >> 8 & 0xFFu)));
                     if (t == 0) sh.tile_exp[done & 15] = e_max - 127;
-                    // all of a thread's pieces before the first store, which the compiler would not move a load across
-                    const int piece = t % kPieces;
-                    uint4 codes[kPieces];
-                    int exps[kPieces];
+                    // A thread has piece `piece` of every (32 x kConvert / kPieces)-th position: all loads before the first store, which
+                    // the compiler would not move a load across.  Pieces of the second slab go by the neighbouring
+                    // position, whose swizzle spreads the slabs over the banks.
+                    constexpr int kMine = kTile * kPieces / (32 * kConvert);
+                    const int piece = t % kPieces, pos0 = (t / kPieces) ^ (piece >> 2 & 1);
+                    uint4 codes[kMine];
+                    int exps[kMine];
 #pragma unroll
-                    for (int n = 0; n < kPieces; ++n) {
-                        const int pos = t / kPieces + n * (kTile / kPieces);
+                    for (int n = 0; n < kMine; ++n) {
+                        const int pos = pos0 + n * (kTile / kMine);
                         codes[n] = *reinterpret_cast<const uint4 *>(raw + pos * D + piece * 16);
                         exps[n] = sh.exps[rs][pos];
                     }
+                    if (p0 + kTile > c.ctx) {                  // unused places and the code of NaN count as 0
 #pragma unroll
-                    for (int n = 0; n < kPieces; ++n) {
-                        const int pos = t / kPieces + n * (kTile / kPieces);
-                        uint32_t u[4] = {codes[n].x, codes[n].y, codes[n].z, codes[n].w};
-                        const int e = min(exps[n] - e_max, 0);
-                        if (!clean) {                          // unused places and the code of NaN count as 0
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) u[k] = p0 + pos >= c.total ? 0u : u[k] & ~__vcmpeq4(u[k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                        for (int n = 0; n < kMine; ++n) {
+                            const bool use = p0 + pos0 + n * (kTile / kMine) < c.total;
+                            auto plain = [&](uint32_t u) { return use ? u & ~__vcmpeq4(u & 0x7F7F7F7Fu, 0x7F7F7F7Fu) : 0u; };
+                            codes[n] = make_uint4(plain(codes[n].x), plain(codes[n].y), plain(codes[n].z), plain(codes[n].w));
                         }
+                    }
+                    uint8_t *dst = tile + (piece >> 2) * kSlabBytes + pos0 * 128;
+                    const int ch = ((piece & 3) * 2 ^ (pos0 & 7)) << 4;      // two chunks of the slab's 128-byte row, swizzled by the row
+#pragma unroll
+                    for (int n = 0; n < kMine; ++n) {
+                        const uint32_t u[4] = {codes[n].x, codes[n].y, codes[n].z, codes[n].w};
+                        const int e = min(exps[n] - e_max, 0);
                         // 2^e as fp16, 0 below 2^-24
                         const uint32_t sc = (e >= -14 ? (uint32_t)(e + 15) << 10 : e >= -24 ? 1u << (e + 24) : 0u) * 0x10001u;
                         uint32_t o[8];
@@ -1140,12 +1180,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                                 o[y] = *reinterpret_cast<const uint32_t *>(&v);
                             }
                         }
-                        // two 16-byte chunks of the slab's 128-byte row, swizzled by the row; every second piece stores
-                        // its second chunk first, which spreads the slabs over the banks
-                        uint8_t *dst = tile + (piece >> 2) * kSlabBytes + pos * 128;
-                        const int ch = (piece & 3) * 2, sw = pos & 7, flip = piece >> 2 & 1;
-                        *reinterpret_cast<uint4 *>(dst + (((ch + flip) ^ sw) << 4)) = flip ? make_uint4(o[4], o[5], o[6], o[7]) : make_uint4(o[0], o[1], o[2], o[3]);
-                        *reinterpret_cast<uint4 *>(dst + (((ch + 1 - flip) ^ sw) << 4)) = flip ? make_uint4(o[0], o[1], o[2], o[3]) : make_uint4(o[4], o[5], o[6], o[7]);
+                        static_assert(kTile / kMine % 8 == 0, "a thread's positions are swizzled alike");
+                        *reinterpret_cast<uint4 *>(dst + n * (kTile / kMine) * 128 + ch) = make_uint4(o[0], o[1], o[2], o[3]);
+                        *reinterpret_cast<uint4 *>(dst + n * (kTile / kMine) * 128 + (ch ^ 16)) = make_uint4(o[4], o[5], o[6], o[7]);
                     }
                     fence_async_smem();
                     __syncwarp();
@@ -1187,6 +1224,7 @@ cudaError_t launch_attend_umma(const CUtensorMap &q_map, const CUtensorMap &k_ma
                                const AttendArgs &args, int sms, cudaStream_t stream)
 {
     AttendArgs a = args;
+    if (a.wait_cycles <= 0) a.wait_cycles = kWaitCycles;
     // One row tile per sequence and head (the hint says), and no more of them than half the SMs: clusters share them.  No more CTAs than give
     // every stream a tile of the longest sequence that the table can hold.
     const long long items = (long long)a.kv.B * a.kv.heads, tiles = (((long long)a.kv.width << a.kv.page_shift) + kTile - 1) / kTile;
