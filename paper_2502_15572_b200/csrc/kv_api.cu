@@ -211,9 +211,13 @@ dresd_status dresd_kv_create(void *k_pages, void *v_pages, uint8_t *k_exps, uint
         free_kv(kv);
         return fail(DRESD_ERR_ALLOC, "workspace allocation failed");
     }
-    e = cudaMemset(kv->tickets, 0, tickets);
-    if (e == cudaSuccess) e = cudaMemset(a.status, 0, sizeof(int));
-    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);        // other streams may follow at once
+    // On a stream of its own: any stream may follow at once, and what others have queued is not waited for.
+    cudaStream_t own = nullptr;
+    e = cudaStreamCreateWithFlags(&own, cudaStreamNonBlocking);
+    if (e == cudaSuccess) e = cudaMemsetAsync(kv->tickets, 0, tickets, own);
+    if (e == cudaSuccess) e = cudaMemsetAsync(a.status, 0, sizeof(int), own);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(own);
+    if (own) cudaStreamDestroy(own);
     if (e != cudaSuccess) {
         free_kv(kv);
         return fail_cuda(e, "workspace reset");
