@@ -540,7 +540,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     return wait(&sh.full[x % kStages], x / kStages);
                 };
                 // A stream's products are issued in one go: side by side, both streams would wait for the tensor cores and
-                // then for the exponentials together, instead of in turn.  (Nothing waits while it holds the lock.)
+                // then for the exponentials together, instead of in turn.
                 auto lock = [&] {
                     bool got = true;
                     if (lane == 0) {
@@ -584,7 +584,14 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     const int vj = one ? 2 * j + st : j, x = base + v_place(vj), s = x % kStages;
                     const bool more = j + 1 < n;
                     const int y = more ? base + k_place(one ? vj + 2 : j + 1) : 0;
-                    if (!reach(x) || (more && !reach(y)) || !wait(&sh.p_full[st], steps) || !lock()) break;
+                    if (!reach(x) || (more && !reach(y))) break;
+                    // The turn is taken before the weights are there, to have its cost behind us -- but not for a segment's first tile,
+                    // whose weights may wait for the other stream's last products of the segment before.
+                    if (j == 0 ? !wait(&sh.p_full[st], steps) || !lock() : !lock()) break;
+                    if (j > 0 && !wait(&sh.p_full[st], steps)) {
+                        unlock();
+                        break;
+                    }
                     ++steps;
                     const uint64_t vd = v_desc + s * (kTileBytes >> 4);
                     if (issuer) {
@@ -649,6 +656,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         // ---- softmax of stream st; a thread has positions 64 half .. of a tile of its row
         const int st = warp >= 12 ? 1 : 0, half = (warp >> 2) & 1 ? 0 : 1;      // warps 4-7, 12-15: the first half
         const int row = tid & 127;                           // TMEM lane
+        const int pair_bar = 4 + 4 * st + (warp & 3);        // barrier of the two warps that have the same rows
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;    // (warp % 4) x 32 lanes, in the address's upper half
         const uint32_t ts = tmem + lanes + st * kTile + 64 * half, tp = Q8 ? ts + 32 : tmem + lanes + st * kTile + 32 * half;
         const uint32_t to = tmem + lanes + 256 + st * D;
@@ -745,15 +753,17 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
                 over |= top - m > kSlack;                     // -inf - -inf is NaN: no
                 tc_fence_before();
-                const bool raise = bar_or(2 + st, 256, over); // one maximum for both halves of a row; both have been read, weights may take their place
+                // Both halves of a row have one maximum; both have been read, weights may take their place.  The two warps that have
+                // these 32 rows meet, nobody else has to.
+                const bool raise = bar_or(pair_bar, 64, over);
                 tc_fence_after();
                 if (raise) {
                     float *pass = &sh.l[st][row];
                     if (half) *pass = top;
-                    bar_sync(2 + st, 256);
+                    bar_sync(pair_bar, 64);
                     float mn;
                     if (!half) *pass = mn = fmaxf(fmaxf(m, top), *pass);
-                    bar_sync(2 + st, 256);
+                    bar_sync(pair_bar, 64);
                     if (half) mn = *pass;
                     float f = mn > -INFINITY ? ex2(m - mn) : 1.f;
                     l *= f;
@@ -777,7 +787,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         tmem_st_wait();
                     }
                     tc_fence_before();
-                    bar_sync(2 + st, 256);                    // the second product begins when one half has its weights
+                    bar_sync(pair_bar, 64);                   // the second product begins when one half has its weights
                     tc_fence_after();
                 }
                 if constexpr (Q8) dv = max(dv - v_exp, -126);
