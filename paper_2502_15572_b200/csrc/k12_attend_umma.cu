@@ -25,12 +25,14 @@
 // TMEM, so a stream has one tile in the works), hence: two threads to a row, an issuing warp to a stream; the maximum only
 // raised when a score passes it by 2^8, so that O is rarely rescaled (by then the stream's products have ended, its next S is
 // issued behind them); the streams' products issued in turn, so that one stream's exponentials fall into the
-// other's products; some exponentials on the FMA pipes (the MUFU unit takes 8 cycles a warp).
+// other's products.
 //
-// Measured (148 SMs): 2047 rows x 4 heads of 128 at 12345 positions, bf16, 400 to 460 us = 1.0 to 1.1 PFLOP/s (the power limit
-// moves it: the tensor cores are busy half of the time, the exponentials' pipe 37 %); the same work of 1024 rows in 8 bits takes 1.38
-// times as long, the converting and the softmax warps' instructions together (60 % of the issue slots); three drafts of
-// twenty tokens of 16 sequences, 8 bits, 63 us; ten of ten of one sequence 23 us, of which 10 are fixed (plan, first scores, join).
+// Measured (148 SMs): 2047 rows x 4 heads of 128 at 12345 positions, bf16, 390 to 450 us = 1.0 to 1.15 PFLOP/s (the power limit
+// moves it; the tensor cores are busy half of the time); 148 items of 256 rows at 8000 positions, heads of 64, 117 us, with an 8-bit cache
+// 134, the converting warps' instructions between those of the softmax; three drafts of twenty tokens of 16 sequences, 8
+// bits, 57 us; ten of ten of one sequence 23 us, of which 10 are fixed (plan, first scores, join).  Taking a quarter of the
+// exponentials on the FMA pipes changes the first by nothing and costs 7 us of the second and 10 of the third: the chain's
+// instructions and its four handovers a tile bound it, not the exponentials' unit.
 //
 // 8-bit caches are multiplied in fp16, whatever the type of the queries, because the hardware turns E4M3 codes into fp16
 // numbers (exactly) in one instruction per two.  A tile's rows are held relative to its largest exponent, which the
@@ -49,11 +51,8 @@ constexpr int kSlabBytes = kTile * 128;                    // 64 elements of eve
 constexpr float kSlack = 8.f;
 constexpr int kMaxCtas = 4;                                // of a cluster
 constexpr int kConvert = 8;                                // warps that convert 8-bit tiles
-// Two of so many exponentials are taken on the FMA pipes: 148 items of 256 rows at 8000 positions, heads of 64, 123 us with 8, 127
-// with 16, 130 with none, 149 with 4.
-constexpr int kEveryFma = 8;
-// Queries and join of a segment take about as long as two tiles: 160 ragged items of 244 rows 63 us, 67 with 1, 64 with 4, 73 with 8.
-constexpr int kFixed = 2;
+// Queries and join of a segment take about as long as three tiles: 160 ragged items of 244 rows 57 us, 64 with 1, 59 with 2, 64 with 8.
+constexpr int kFixed = 3;
 
 template <bool Q8, int D>
 struct Geometry {
@@ -269,40 +268,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ float max_nan(float a, float b)
-{
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
-// 2^x of a pair on the FMA pipes: x = n + f with n the nearest whole number (x + 1.5 x 2^23 holds n in its low bits), 2^f by a
-// polynomial of degree 5 on [-1/2, 1/2] (least squares at Chebyshev points, reweighted towards the smallest largest relative
-// error; 2^-22.1 in fp32 arithmetic over the interval), 2^n from n's bits.  NaN stays NaN; below 2^-126 the result
-// stays at about 2^-126.
-__device__ __forceinline__ uint64_t ex2_fma(uint64_t x)
-{
-    float lo, hi;
-    unpair(x, lo, hi);
-    x = pair(max_nan(lo, -126.f), max_nan(hi, -126.f));
-    const float kRound = 12582912.f + 127.f;               // low bits of the sum: n + 127
-    const uint64_t t = add2(x, pair(kRound, kRound));
-    const uint64_t f = add2(x, mul2(add2(t, pair(-kRound, -kRound)), pair(-1.f, -1.f)));
-    uint64_t p = pair(0.0013276466634124517f, 0.0013276466634124517f);
-    p = fma2(p, f, pair(0.009675540961325169f, 0.009675540961325169f));
-    p = fma2(p, f, pair(0.05550713464617729f, 0.05550713464617729f));
-    p = fma2(p, f, pair(0.24022120237350464f, 0.24022120237350464f));
-    p = fma2(p, f, pair(0.6931469440460205f, 0.6931469440460205f));
-    p = fma2(p, f, pair(1.0000001192092896f, 1.0000001192092896f));
-    unpair(t, lo, hi);
-    return mul2(p, pair(__uint_as_float(__float_as_uint(lo) << 23), __uint_as_float(__float_as_uint(hi) << 23)));
-}
-
 // Sums of stream `st` for row `row` and elements d .. d + 15 of a segment, added up one position after the other without what the
 // row does not see -- called when the tensor cores' sum is not finite.  Leaves `x` alone if the chunk's own values are
 // finite (then the non-finite ones are seen by every row).
@@ -695,10 +660,10 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 dead = __any_sync(0xFFFFFFFFu, dead);
                 ++steps;
                 tc_fence_after();
-                // With a 16-bit cache a thread holds its 64 scores, and weights go to the first half of the tile's columns: 61 rows x 4
-                // heads of 64 behind 8000 positions in 148 items take 125 us.  With an 8-bit cache there are fewer registers (the
-                // converting warps have the rest): 32 scores at a time, the first 32 read twice, weights to the place of
-                // the second 32, 152 us; held and spilled, 207.  (The 16-bit kernel in this form: 130 us.)
+                // With a 16-bit cache a thread holds its 64 scores, and weights go to the first half of the tile's columns.  With an
+                // 8-bit cache there are fewer registers (the converting warps have the rest): 32 scores at a time, the
+                // first 32 read twice, weights to the place of the second 32.  61 rows x 4 heads of 64 behind 8000 positions in 148
+                // items took 161 us so and 207 with 64 held and spilled; the 16-bit kernel 130 so and 123 with 64 held.
                 float s[64];
                 uint32_t *su = reinterpret_cast<uint32_t *>(s);
                 const bool masked = p0 + kTile > all_seen;
@@ -796,21 +761,16 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 uint64_t sum0 = 0, sum1 = 0;
                 // weights of some scores, packed and stored at column c0
                 constexpr int kAtOnce = Q8 ? 16 : 32;
-                auto weights = [&](const float *of, int c0, bool fma) {
+                auto weights = [&](const float *of, int c0) {
                     uint32_t p[kAtOnce / 2];
 #pragma unroll
                     for (int k = 0; k < kAtOnce; k += 2) {
                         uint64_t x = fma2(pair(of[k], of[k + 1]), scale2, off2);
                         float lo, hi;
-                        if (fma && k % kEveryFma == kEveryFma - 2) {
-                            x = ex2_fma(x);
-                            unpair(x, lo, hi);
-                        } else {
-                            unpair(x, lo, hi);
-                            lo = ex2(lo);
-                            hi = ex2(hi);
-                            x = pair(lo, hi);
-                        }
+                        unpair(x, lo, hi);
+                        lo = ex2(lo);
+                        hi = ex2(hi);
+                        x = pair(lo, hi);
                         if (k & 2) sum1 = add2(sum1, x);
                         else sum0 = add2(sum0, x);
                         p[k / 2] = pack2<M>(lo, hi);
@@ -818,24 +778,20 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     if constexpr (Q8) tmem_st8(tp + c0, p);
                     else tmem_st16(tp + c0, p);
                 };
-                auto all_weights = [&](bool fma) {            // (masked: -infinity has to give 0 exactly)
-                    if constexpr (Q8) {
-                        tmem_ld16(ts, su);
-                        weights(s + 32, 16, fma);
-                        tmem_ld16(ts + 16, su + 16);
-                        weights(s + 48, 24, fma);
-                        tmem_ld_wait16(su);
-                        tmem_ld_wait16(su + 16);
-                        if (!fma) hide(s, see);
-                        weights(s, 0, fma);
-                        weights(s + 16, 8, fma);
-                    } else {
-                        weights(s, 0, fma);
-                        weights(s + 32, 16, fma);
-                    }
-                };
-                if (masked) all_weights(false);
-                else all_weights(true);
+                if constexpr (Q8) {
+                    tmem_ld16(ts, su);
+                    weights(s + 32, 16);
+                    tmem_ld16(ts + 16, su + 16);
+                    weights(s + 48, 24);
+                    tmem_ld_wait16(su);
+                    tmem_ld_wait16(su + 16);
+                    if (masked) hide(s, see);
+                    weights(s, 0);
+                    weights(s + 16, 8);
+                } else {
+                    weights(s, 0);
+                    weights(s + 32, 16);
+                }
                 float a0, a1;
                 unpair(add2(sum0, sum1), a0, a1);
                 l += Q8 ? (a0 + a1) * pow2f(-dv) : a0 + a1;
