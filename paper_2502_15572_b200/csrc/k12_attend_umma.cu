@@ -1115,48 +1115,51 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     e4 = __vmaxu4(e4, e4 >> 16);
                     const int e_max = max(1, (int)__reduce_max_sync(0xFFFFFFFFu, max(e4 & 0xFFu, e4 >> 8 & 0xFFu)));
                     if (t == 0) sh.tile_exp[done & 15] = e_max - 127;
-                    // A thread has piece `piece` of every (32 x kConvert / kPieces)-th position: all loads before the first store, which
+                    // A thread has piece `piece` of every (32 x kConvert / kPieces)-th position, two at a time: both loads before the first store, which
                     // the compiler would not move a load across.  Pieces of the second slab go by the neighbouring
                     // position, whose swizzle spreads the slabs over the banks.
                     constexpr int kMine = kTile * kPieces / (32 * kConvert);
                     const int piece = t % kPieces, pos0 = (t / kPieces) ^ (piece >> 2 & 1);
-                    uint4 codes[kMine];
-                    int exps[kMine];
-#pragma unroll
-                    for (int n = 0; n < kMine; ++n) {
-                        const int pos = pos0 + n * (kTile / kMine);
-                        codes[n] = *reinterpret_cast<const uint4 *>(raw + pos * D + piece * 16);
-                        exps[n] = sh.exps[rs][pos];
-                    }
-                    if (p0 + kTile > c.ctx) {                  // unused places and the code of NaN count as 0
-#pragma unroll
-                        for (int n = 0; n < kMine; ++n) {
-                            const bool use = p0 + pos0 + n * (kTile / kMine) < c.total;
-                            auto plain = [&](uint32_t u) { return use ? u & ~__vcmpeq4(u & 0x7F7F7F7Fu, 0x7F7F7F7Fu) : 0u; };
-                            codes[n] = make_uint4(plain(codes[n].x), plain(codes[n].y), plain(codes[n].z), plain(codes[n].w));
-                        }
-                    }
                     uint8_t *dst = tile + (piece >> 2) * kSlabBytes + pos0 * 128;
                     const int ch = ((piece & 3) * 2 ^ (pos0 & 7)) << 4;      // two chunks of the slab's 128-byte row, swizzled by the row
+#pragma unroll 1
+                    for (int n0 = 0; n0 < kMine; n0 += 2) {
+                        uint4 codes[2];
+                        int exps[2];
 #pragma unroll
-                    for (int n = 0; n < kMine; ++n) {
-                        const uint32_t u[4] = {codes[n].x, codes[n].y, codes[n].z, codes[n].w};
-                        const int e = min(exps[n] - e_max, 0);
-                        // 2^e as fp16, 0 below 2^-24
-                        const uint32_t sc = (e >= -14 ? (uint32_t)(e + 15) << 10 : e >= -24 ? 1u << (e + 24) : 0u) * 0x10001u;
-                        uint32_t o[8];
+                        for (int n = 0; n < 2; ++n) {
+                            const int pos = pos0 + (n0 + n) * (kTile / kMine);
+                            codes[n] = *reinterpret_cast<const uint4 *>(raw + pos * D + piece * 16);
+                            exps[n] = sh.exps[rs][pos];
+                        }
+                        if (p0 + kTile > c.ctx) {                  // unused places and the code of NaN count as 0
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            codes_to_halves(u[k], o[2 * k], o[2 * k + 1]);
-#pragma unroll
-                            for (int y = 2 * k; y < 2 * k + 2; ++y) {
-                                const __half2 v = __hmul2(*reinterpret_cast<__half2 *>(&o[y]), *reinterpret_cast<const __half2 *>(&sc));
-                                o[y] = *reinterpret_cast<const uint32_t *>(&v);
+                            for (int n = 0; n < 2; ++n) {
+                                const bool use = p0 + pos0 + (n0 + n) * (kTile / kMine) < c.total;
+                                auto plain = [&](uint32_t u) { return use ? u & ~__vcmpeq4(u & 0x7F7F7F7Fu, 0x7F7F7F7Fu) : 0u; };
+                                codes[n] = make_uint4(plain(codes[n].x), plain(codes[n].y), plain(codes[n].z), plain(codes[n].w));
                             }
                         }
-                        static_assert(kTile / kMine % 8 == 0, "a thread's positions are swizzled alike");
-                        *reinterpret_cast<uint4 *>(dst + n * (kTile / kMine) * 128 + ch) = make_uint4(o[0], o[1], o[2], o[3]);
-                        *reinterpret_cast<uint4 *>(dst + n * (kTile / kMine) * 128 + (ch ^ 16)) = make_uint4(o[4], o[5], o[6], o[7]);
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) {
+                            const uint32_t u[4] = {codes[n].x, codes[n].y, codes[n].z, codes[n].w};
+                            const int e = min(exps[n] - e_max, 0);
+                            // 2^e as fp16, 0 below 2^-24
+                            const uint32_t sc = (e >= -14 ? (uint32_t)(e + 15) << 10 : e >= -24 ? 1u << (e + 24) : 0u) * 0x10001u;
+                            uint32_t o[8];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                codes_to_halves(u[k], o[2 * k], o[2 * k + 1]);
+#pragma unroll
+                                for (int y = 2 * k; y < 2 * k + 2; ++y) {
+                                    const __half2 v = __hmul2(*reinterpret_cast<__half2 *>(&o[y]), *reinterpret_cast<const __half2 *>(&sc));
+                                    o[y] = *reinterpret_cast<const uint32_t *>(&v);
+                                }
+                            }
+                            static_assert(kTile / kMine % 8 == 0, "a thread's positions are swizzled alike");
+                            *reinterpret_cast<uint4 *>(dst + (n0 + n) * (kTile / kMine) * 128 + ch) = make_uint4(o[0], o[1], o[2], o[3]);
+                            *reinterpret_cast<uint4 *>(dst + (n0 + n) * (kTile / kMine) * 128 + (ch ^ 16)) = make_uint4(o[4], o[5], o[6], o[7]);
+                        }
                     }
                     fence_async_smem();
                     __syncwarp();
