@@ -31,7 +31,7 @@
 // moves it; the tensor cores are busy half of the time); 148 items of 256 rows at 8000 positions, heads of 64, 117 us, with an 8-bit cache
 // 134, the converting warps' instructions between those of the softmax; three drafts of twenty tokens of 16 sequences, 8
 // bits, 57 us; ten of ten of one sequence 23 us, of which 10 are fixed (plan, first scores, join).  Taking a quarter of the
-// exponentials on the FMA pipes changes the first by nothing and costs 7 us of the second and 10 of the third: the chain's
+// exponentials on the FMA pipes changed the first by nothing and cost 2 us of the second (8 bits: 16) and 5 of the third: the chain's
 // instructions and its four handovers a tile bound it, not the exponentials' unit.
 //
 // 8-bit caches are multiplied in fp16, whatever the type of the queries, because the hardware turns E4M3 codes into fp16
@@ -1115,8 +1115,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     e4 = __vmaxu4(e4, e4 >> 16);
                     const int e_max = max(1, (int)__reduce_max_sync(0xFFFFFFFFu, max(e4 & 0xFFu, e4 >> 8 & 0xFFu)));
                     if (t == 0) sh.tile_exp[done & 15] = e_max - 127;
-                    // A thread has piece `piece` of every (32 x kConvert / kPieces)-th position, two at a time: both loads before the first store, which
-                    // the compiler would not move a load across.  Pieces of the second slab go by the neighbouring
+                    // A thread has piece `piece` of every (32 x kConvert / kPieces)-th position, two at a time (four spill): both
+                    // loads before the first store, which the compiler would not move a load across.  Pieces of the second slab go by the neighbouring
                     // position, whose swizzle spreads the slabs over the banks.
                     constexpr int kMine = kTile * kPieces / (32 * kConvert);
                     const int piece = t % kPieces, pos0 = (t / kPieces) ^ (piece >> 2 & 1);
