@@ -138,7 +138,9 @@ struct Shared {
     uint64_t job_full[2], job_empty[2];
     uint64_t ready, taken;                                 // cluster: all sums have come / every CTA has read its share
     alignas(16) uint8_t exps[kRaw ? kRaw : 1][kRaw ? kTile : 16];      // exponents of the 8-bit tiles (bulk copies: 16-byte aligned)
-    float q_scale[2][kRaw ? kTile : 1];                    // 8-bit: 1 / power of two that a query row was multiplied by
+    // 8-bit: 1 / power of two that a query row was multiplied by.  By the segment's parity: the next segment's queries are
+    // turned while the softmax warps still read this one's; those of two segments on wait for job_empty.
+    float q_scale[2][2][kRaw ? kTile : 1];
     int tile_exp[16];                                      // 8-bit: largest exponent of the last tiles, by place
     int v_exp[2];                                          // 8-bit: the streams' sums are relative to 2^v_exp
     Job job[2];
@@ -672,7 +674,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 int dv = 0;                                   // 8-bit: weights are multiplied by 2^dv
                 bool over = false;
                 if constexpr (Q8) {
-                    scale = a.scale_log2 * (kTurnQ ? sh.q_scale[w.one ? 0 : st][row] : 1.f) * pow2f(max(sh.tile_exp[(base + w.k_place(vj)) & 15], -100));
+                    scale = a.scale_log2 * (kTurnQ ? sh.q_scale[i & 1][w.one ? 0 : st][row] : 1.f) * pow2f(max(sh.tile_exp[(base + w.k_place(vj)) & 15], -100));
                     scale = fmaxf(scale, 1e-37f);             // -infinity times it stays one
                     dv = sh.tile_exp[v_at & 15];
                     over = dv > v_exp;
@@ -1091,7 +1093,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                             }
                             *at(x) = make_uint4(o[0], o[1], o[2], o[3]);
                         }
-                        sh.q_scale[q_st][q_at] = pow2f(-(e / 2)) * pow2f(-(e - e / 2));
+                        sh.q_scale[i & 1][q_st][q_at] = pow2f(-(e / 2)) * pow2f(-(e - e / 2));
                         fence_async_smem();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&sh.q_ready[q_st]);

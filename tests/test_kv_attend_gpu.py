@@ -1,0 +1,125 @@
+"""Attention over the paged cache where a worker goes through several segments, where 8-bit rows differ in size by
+powers of two, and where masked rows hold anything: against float64 on the GPU, vectorised (the definitions and the
+derivation of the tolerance are those of test_kv_cache_gpu).
+"""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2502_15572_b200 import binding
+from tests.test_kv_cache_gpu import DT, U, Case, bits_of
+
+pytestmark = pytest.mark.gpu
+
+
+def held_rows(case, name, b, upto):
+    """float64 [upto][Hkv][d] of a sequence, on the GPU."""
+    p = np.arange(upto)
+    page, off = torch.from_numpy(case.table_np[b, p // case.page].astype(np.int64)).cuda(), torch.from_numpy(p % case.page).cuda()
+    x = case.t[name][case.layer][page, :, off]
+    if not case.q8:
+        return x.double()
+    c = x.long()
+    man, ex = (c & 7).double(), (c >> 3) & 15
+    mag = torch.where(ex > 0, (8 + man) * torch.pow(2.0, (ex - 10).double()), man * 2.0 ** -9)
+    e = case.t[name + "_exp"][case.layer][page, :, off].double() - 127
+    return torch.where(c >= 128, -mag, mag) * torch.pow(2.0, e)[..., None]
+
+
+def expected(case, q, b, see, scale):
+    """One sequence: out [n][Hq][d], lse, the largest |v| seen, the largest sum |q k| scale seen; see: bool [n][S]."""
+    s, e, S = case.start_np[b], case.start_np[b + 1], see.shape[1]
+    n, Hq, G = int(e - s), q.shape[1], q.shape[1] // case.Hkv
+    k, v, x = held_rows(case, "k", b, S), held_rows(case, "v", b, S), q[s:e].double().view(n, case.Hkv, G, case.d)
+    sc = (torch.einsum("ihgd,jhd->ihgj", x, k) * scale).masked_fill(~see[:, None, None], -np.inf)
+    m = sc.amax(-1, keepdim=True)
+    p = torch.exp(sc - torch.where(m > -np.inf, m, torch.zeros_like(m)))
+    l = p.sum(-1, keepdim=True)
+    out = torch.einsum("ihgj,jhd->ihgd", p, v) / torch.where(l > 0, l, torch.ones_like(l))
+    lse = (m + l.log()).squeeze(-1)
+    big = torch.where(see[:, None], v.abs().amax(-1).T[None], 0.0).amax(-1)                      # [n][Hkv]
+    ds = torch.einsum("ihgd,jhd->ihgj", x.abs(), k.abs()).mul(abs(scale)).masked_fill(~see[:, None, None], 0).amax(-1)
+    shape = lambda t: t.reshape(n, Hq, *t.shape[3:])
+    return shape(out), shape(lse), shape(big[:, :, None].expand(n, case.Hkv, G)), shape(ds)
+
+
+def causal_of(c, n):
+    return torch.arange(c + n, device="cuda")[None] <= c + torch.arange(n, device="cuda")[:, None]
+
+
+def check(case, q, seen=None, mask=None, scale=None):
+    d, u = case.d, U[case.dtype]
+    scale = d ** -0.5 if scale is None else scale
+    lse = torch.full((case.rows, q.shape[1]), 7.0, device="cuda")
+    got = case.cache.attend(case.layer, q, case.batch, scale=scale, mask=mask, lse=lse)
+    torch.cuda.synchronize()
+    case.cache.status()
+    for b in range(case.B):
+        c, n = case.ctx[b], case.chunk[b]
+        if n == 0:
+            continue
+        s, e = case.start_np[b], case.start_np[b + 1]
+        want, wlse, V, ds = expected(case, q, b, causal_of(c, n) if seen is None else seen[b], scale)
+        ds = (d + 4) * 2.0 ** -24 * ds
+        tol = u * V[..., None] + u * want.abs() + ((2 * (ds + 2.0 ** -21) + (c + n) * 2.0 ** -24) * V)[..., None]
+        if case.dtype == "f16":
+            tol = tol + 2.0 ** -24                            # the type's step below its normal numbers
+        err = (got[s:e].double() - want).abs()
+        assert torch.isfinite(got[s:e]).all(), f"sequence {b}: not finite"
+        assert (err <= tol).all(), f"sequence {b}: {(err / tol).max().item()} tolerances"
+        off = (lse[s:e].double() - wlse).abs() <= ds + 2.0 ** -20 + 2.0 ** -23 * wlse.abs()
+        assert (off | (lse[s:e].double() == wlse)).all(), f"sequence {b}: lse"
+    return got
+
+
+def ragged(seed, B, lo, hi):
+    rng = np.random.default_rng(seed)
+    return [int(x) for x in rng.integers(lo, hi + 1, B)]
+
+
+# ---- several segments a worker ---------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,d,quantised", [("bf16", 64, True), ("bf16", 128, True), ("f16", 64, True), ("bf16", 128, False),
+                                               ("f16", 64, False)])
+@pytest.mark.parametrize("tree", [False, True])
+def test_many_row_items_of_ragged_batches(dtype, d, quantised, tree):
+    """More items than SMs, lengths that share no cut: a CTA has the tail of one item, whole ones and the head of another.
+    The queries of every sequence have a size of their own."""
+    B, Hkv, G = 30, 4, 3
+    ctx, chunk = ragged(1, B, 0, 2500), ragged(2, B, 40, 200)
+    ctx[3], chunk[5], chunk[6] = 0, 0, 1
+    case = Case(dtype, d, 64, Hkv, ctx, chunk, quantised, seed=70)
+    q = case.queries(Hkv * G)
+    for b in range(B):
+        q[case.start_np[b]:case.start_np[b + 1]] *= 2.0 ** (b % 7 - 4)
+    seen = mask = None
+    if tree:                                                  # random bits, but every token sees itself
+        g = torch.Generator(device="cuda").manual_seed(3)
+        bits = torch.rand((case.rows, max(chunk)), device="cuda", generator=g) < 0.5
+        for b in range(B):
+            i = torch.arange(chunk[b], device="cuda")
+            bits[int(case.start_np[b]) + i, i] = True
+        mask = bits_of(bits.cpu().numpy())
+        seen = [torch.cat([torch.ones((chunk[b], ctx[b]), dtype=torch.bool, device="cuda"),
+                           bits[int(case.start_np[b]):int(case.start_np[b + 1]), :chunk[b]]], 1) for b in range(B)]
+    check(case, q, seen, mask)
+
+
+@pytest.mark.parametrize("dtype,d,quantised", [("f16", 128, False), ("bf16", 128, True), ("bf16", 64, False), ("f16", 64, True)])
+@pytest.mark.parametrize("B,Hkv,G,hi,longest", [(70, 4, 4, 800, 9000), (160, 8, 7, 150, 3000), (300, 8, 1, 60, 1000), (60, 4, 12, 500, 5000)])
+def test_single_tokens_of_large_ragged_batches(dtype, d, quantised, B, Hkv, G, hi, longest):
+    """Groups of four, two and one warps with tiles of 8 rows, and of four with tiles of 16; several segments each."""
+    ctx = ragged(B, B, 0, hi)
+    ctx[0], ctx[B // 2] = 0, longest
+    case = Case(dtype, d, 32, Hkv, ctx, [1] * B, quantised, seed=71)
+    q = case.queries(Hkv * G)
+    check(case, q)
+
+
+@pytest.mark.parametrize("dtype,quantised", [("f16", False), ("bf16", False), ("bf16", True)])
+@pytest.mark.parametrize("chunk,path", [(1, 0), (33, 0), (2, 2), (33, 1)])
+def test_long_contexts(dtype, quantised, chunk, path):
+    """Parts of a long item joined through clusters and global memory."""
+    case = Case(dtype, 128, 128, 2, [40000, 9999], [chunk] * 2, quantised, seed=72)
+    case.cache.set_option("attend_path", path)
+    check(case, case.queries(8))
