@@ -642,6 +642,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             const int n_mine = w.n[st];
             const int first_tok = seg.rt * (int)a.by_rows.d + (w.one ? 0 : st * ManyRows::per_tile(a));
             const int tok = first_tok + row_tok;              // of this row; may lie behind the chunk
+            // A row of the result.  The others hold the queries of other tokens, or (behind 128 / group x group) whatever was in shared
+            // memory: they take part in nothing.
+            const bool valid = row < ManyRows::per_tile(a) * a.group && tok < c.len;
             const int limit = a.mask ? c.total : min(c.total, c.ctx + min(tok, c.len - 1) + 1);
             const int all_seen = min(c.total, a.mask ? c.ctx : c.ctx + min(first_tok, c.len - 1) + 1);    // by every row
             float m = -INFINITY, l = 0.f, scale = a.scale_log2;      // m in powers of two
@@ -718,7 +721,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 if constexpr (Q8) largest(s + 32, 32);
                 else largest(s, 64);
                 const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-                over |= top - m > kSlack;                     // -inf - -inf is NaN: no
+                over |= valid && top - m > kSlack;            // -inf - -inf is NaN: no
                 tc_fence_before();
                 // Both halves of a row have one maximum; both have been read, weights may take their place.  The two warps that have
                 // these 32 rows meet, nobody else has to.
@@ -813,7 +816,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             }
             // ---- the segment's result
             base += 2 * w.nt;
-            const bool valid = row < ManyRows::per_tile(a) * a.group && tok < c.len;
             const int heads = a.kv.heads * a.group;
             if (half) sh.l[st][row] = l;
             bar_sync(2 + st, 256);

@@ -123,3 +123,19 @@ def test_long_contexts(dtype, quantised, chunk, path):
     case = Case(dtype, 128, 128, 2, [40000, 9999], [chunk] * 2, quantised, seed=72)
     case.cache.set_option("attend_path", path)
     check(case, case.queries(8))
+
+
+# ---- the same call, the same bits -------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,quantised", [("f16", False), ("bf16", False), ("f16", True), ("bf16", True)])
+@pytest.mark.parametrize("G,chunk,path", [(3, 50, 2), (7, 20, 2), (12, 200, 2), (3, 1, 1), (5, 4, 1), (7, 30, 1)])
+def test_repeatable_whatever_ran_before(dtype, quantised, G, chunk, path):
+    """Groups that do not divide a row tile, and other calls in between whose queries are very large or very small."""
+    case = Case(dtype, 64, 16, 3, [700, 90, 2100, 0], [chunk, 1, chunk, chunk // 2 + 1], quantised, seed=73)
+    other = Case(dtype, 64, 16, 2, [600] * 80, [8 * chunk // G + 1] * 80, quantised, seed=74)
+    case.cache.set_option("attend_path", path)
+    other.cache.set_option("attend_path", path)
+    q = case.queries(3 * G)
+    first = check(case, q)
+    for amp in (1e-3, 8.0, 200.0):
+        other.cache.attend(0, other.queries(2 * 8, amp=amp), other.batch)
+        assert torch.equal(case.cache.attend(0, q, case.batch), first)
