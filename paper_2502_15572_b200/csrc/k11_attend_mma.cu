@@ -21,8 +21,10 @@
 // 8-bit caches are multiplied in fp16, whatever the type of the queries, because the hardware turns E4M3 codes into fp16
 // numbers (exactly) in one instruction per two.  A bf16 query row is multiplied by the power of two that brings its
 // largest element to 2^14 .. 2^15: every element down to 2^-31 of it stays exact, the rest is off by 2^-40 of it.  The keys'
-// scale is applied to the score; the values' to the weight, relative to the largest exponent so far, and the
-// sums are brought back at the end.
+// scale 2^k is applied to the score.  The values' 2^e is part of the weight of the second product, 2^(s + e - n), with a
+// running maximum n of s + e for every row beside that of s: so fp16's range is counted from the largest product that the row
+// has seen, whatever the exponents of other rows and of positions that it does not see.  (Rows of zeros have an exponent of
+// no meaning; they are found when it would raise a maximum.)  The sums are brought from 2^n to 2^m at the end.
 //
 // Which position is which row of the instruction is free as well: row g is position g ^ (g odd ? 4 : 0), which together
 // with the 128-byte swizzle of the copies makes the reads of keys and of values free of bank conflicts.
@@ -309,11 +311,10 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 q_scale[nt][x] = a.scale_log2 * pow2f(-(er / 2)) * pow2f(-(er - er / 2));
             }
         }
-        int v_exp = -127;                                   // 8-bit: the sums are held relative to 2^v_exp
         float o[NT][kSteps][4] = {};
-        float m[NT][2], l[NT][2];
+        float m[NT][2], l[NT][2], mv[NT][2];                // mv: 8-bit: the sums are held relative to 2^mv
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) m[nt][0] = m[nt][1] = -INFINITY, l[nt][0] = l[nt][1] = 0.f;
+        for (int nt = 0; nt < NT; ++nt) m[nt][0] = m[nt][1] = mv[nt][0] = mv[nt][1] = -INFINITY, l[nt][0] = l[nt][1] = 0.f;
 
 #pragma unroll 1
         for (int t = w.t0 + mine; t < w.t1; t += step) {
@@ -384,15 +385,8 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             // ---- scale, mask.  sc[nt][2 j + x]: key place(g) + 8 j, row 2 c + x
             const bool all_seen = p0 + kTile <= ch.ctx && p0 + kTile <= ch.total;
             const float sk[2] = {pow2f(ke[0] - 127), pow2f(ke[1] - 127)};
+            float vf[2] = {(float)(ve[0] - 127), (float)(ve[1] - 127)};       // exponents of the values
             bool over = false;
-            if constexpr (Q8) {
-                if (!all_seen) {                           // places that are not in use have any exponent
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        if (p0 + 8 * j + place(g) >= ch.total) ve[j] = 1;
-                }
-                over = max(ve[0], ve[1]) - 127 > v_exp;
-            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -412,13 +406,26 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         }
                         sc[nt][2 * j + x] = y;
                         over |= y > m[nt][x] + kSlack;
+                        if constexpr (Q8) over |= y + vf[j] > mv[nt][x] + kSlack;
                     }
             if (__any_sync(0xFFFFFFFFu, over)) {
-                float fe = 1.f;
-                if constexpr (Q8) {
-                    const int e = max(v_exp, __reduce_max_sync(0xFFFFFFFFu, max(ve[0], ve[1])) - 127);
-                    fe = pow2f(max(v_exp - e, -126));
-                    v_exp = e;
+                if constexpr (Q8) {                        // values that are all zeros raise nothing
+                    uint32_t some = 0;                     // bit j: position j of this lane's four has a code other than 0
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t any = 0;
+#pragma unroll
+                        for (int x = 0; x < kValPieces; ++x)
+#pragma unroll
+                            for (int k = 0; k < kValBytes / 4; ++k) any |= word(vx[j][x], k);
+                        some |= (any & 0x7F7F7F7Fu) ? 1u << j : 0u;
+                    }
+#pragma unroll
+                    for (int sh_ = 4; sh_ < 32; sh_ <<= 1) some |= __shfl_xor_sync(0xFFFFFFFFu, some, sh_);
+                    some = __shfl_sync(0xFFFFFFFFu, some, g >> 1) >> (g & 1);        // rows g, 8 + g: bits 0 and 2
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        if (!(some >> (2 * j) & 1)) vf[j] = -INFINITY;
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -427,13 +434,20 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         float y = fmaxf(fmaxf(sc[nt][x], sc[nt][2 + x]), m[nt][x]);
 #pragma unroll
                         for (int sh_ = 4; sh_ < 32; sh_ <<= 1) y = fmaxf(y, __shfl_xor_sync(0xFFFFFFFFu, y, sh_));
-                        const float f = y > -INFINITY ? ex2(m[nt][x] - y) : 1.f;
+                        float f = y > -INFINITY ? ex2(m[nt][x] - y) : 1.f;
                         m[nt][x] = y;
                         l[nt][x] *= f;
+                        if constexpr (Q8) {
+                            float z = fmaxf(fmaxf(sc[nt][x] + vf[0], sc[nt][2 + x] + vf[1]), mv[nt][x]);
+#pragma unroll
+                            for (int sh_ = 4; sh_ < 32; sh_ <<= 1) z = fmaxf(z, __shfl_xor_sync(0xFFFFFFFFu, z, sh_));
+                            f = z > -INFINITY ? ex2(mv[nt][x] - z) : 1.f;
+                            mv[nt][x] = z;
+                        }
 #pragma unroll
                         for (int st = 0; st < kSteps; ++st) {
-                            o[nt][st][x] *= f * fe;
-                            o[nt][st][2 + x] *= f * fe;
+                            o[nt][st][x] *= f;
+                            o[nt][st][2 + x] *= f;
                         }
                     }
             }
@@ -441,18 +455,20 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             uint32_t p[NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
+                float wv[4];                               // 8-bit: weights with the values' scale
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const float base = m[nt][x] > -INFINITY ? m[nt][x] : 0.f;
+                    const float base = m[nt][x] > -INFINITY ? m[nt][x] : 0.f, base_v = mv[nt][x] > -INFINITY ? mv[nt][x] : 0.f;
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) sc[nt][2 * j + x] = ex2(sc[nt][2 * j + x] - base);
+                    for (int j = 0; j < 2; ++j) {
+                        if constexpr (Q8) wv[2 * j + x] = ex2(sc[nt][2 * j + x] + (vf[j] - base_v));
+                        sc[nt][2 * j + x] = ex2(sc[nt][2 * j + x] - base);
+                    }
                     l[nt][x] += sc[nt][x] + sc[nt][2 + x];
                 }
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float f = Q8 ? pow2f(max(ve[j] - 127 - v_exp, -126)) : 1.f;
-                    p[nt][j] = turn8x8(Q8 ? pack2<M>(sc[nt][2 * j] * f, sc[nt][2 * j + 1] * f) : pack2<M>(sc[nt][2 * j], sc[nt][2 * j + 1]));
-                }
+                for (int j = 0; j < 2; ++j)
+                    p[nt][j] = turn8x8(Q8 ? pack2<M>(wv[2 * j], wv[2 * j + 1]) : pack2<M>(sc[nt][2 * j], sc[nt][2 * j + 1]));
             }
             // ---- O^T += V^T P^T
             if (!all_seen) {
@@ -560,10 +576,10 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     sh.m[warp][r] = m[nt][x];
                     sh.l[warp][r] = l[nt][x];
                 }
+                const float f = !Q8 ? 1.f : mv[nt][x] > -INFINITY ? ex2(mv[nt][x] - m[nt][x]) : 0.f;
 #pragma unroll
                 for (int st = 0; st < kSteps; st += 2) {   // elements 2 st .. 2 st + 3 of the lane's piece are neighbours
                     const int e = 2 * st;
-                    const float f = Q8 ? pow2f(max(v_exp, -126)) : 1.f;
                     *reinterpret_cast<float4 *>(&sh.o[warp][r][e / kValElems * 8 * kValElems + g * kValElems + e % kValElems]) =
                         make_float4(o[nt][st][x] * f, o[nt][st][2 + x] * f, o[nt][st + 1][x] * f, o[nt][st + 1][2 + x] * f);
                 }
