@@ -34,9 +34,8 @@
 // exponentials on the FMA pipes changed the first by nothing and cost 2 us of the second (8 bits: 16) and 5 of the third: the chain's
 // instructions and its four handovers a tile bound it, not the exponentials' unit.
 //
-// 8-bit caches are multiplied in fp16, whatever the type of the queries, because the hardware turns E4M3 codes into fp16
-// numbers (exactly) in one instruction per two.  A tile's rows are held relative to its largest exponent, which the
-// scores (keys) or the weights (values) are multiplied by; bf16 queries are brought into fp16's range by a power of two a row.
+// 8-bit tiles become tiles of the queries' type, which holds every code x 2^e exactly: behind the conversion an 8-bit cache is a 16-bit
+// one, and no row's size matters to another.
 //
 // 0 x NaN is NaN, so what a row does not see must not reach the second product as a non-finite number.  Places behind the
 // sequence's end are cleared in shared memory.  Values of the chunk itself are not looked at unless a sum comes out
@@ -134,15 +133,10 @@ struct Shared {
     float m[2][kTile], l[2][kTile];                        // of the streams' rows; l also passes maxima between a row's threads
     uint64_t full[kStages], empty[kStages];
     uint64_t raw_full[kRaw ? kRaw : 1], raw_empty[kRaw ? kRaw : 1];
-    uint64_t q_full[2], q_ready[2], q_empty[2], s_full[2], p_full[2], o_full[2];
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2];
     uint64_t job_full[2], job_empty[2];
     uint64_t ready, taken;                                 // cluster: all sums have come / every CTA has read its share
     alignas(16) uint8_t exps[kRaw ? kRaw : 1][kRaw ? kTile : 16];      // exponents of the 8-bit tiles (bulk copies: 16-byte aligned)
-    // 8-bit: 1 / power of two that a query row was multiplied by.  By the segment's parity: the next segment's queries are
-    // turned while the softmax warps still read this one's; those of two segments on wait for job_empty.
-    float q_scale[2][2][kRaw ? kTile : 1];
-    int tile_exp[16];                                      // 8-bit: largest exponent of the last tiles, by place
-    int v_exp[2];                                          // 8-bit: the streams' sums are relative to 2^v_exp
     Job job[2];
     uint32_t tmem;
     unsigned ticket;
@@ -320,8 +314,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 {
     using Geo = Geometry<Q8, D>;
     using Sh = Shared<Geo::kStages, Geo::kRaw>;
-    using M = std::conditional_t<Q8, __half, T>;            // type of the products
-    constexpr bool kTurnQ = Q8 && std::is_same<T, __nv_bfloat16>::value;
     constexpr int kStages = Geo::kStages, kSlabs = Geo::kSlabs, kTileBytes = Geo::kTileBytes;
     static_assert(Geo::kBig + sizeof(Sh) <= kSmemBytes, "shared memory");
     extern __shared__ uint8_t smem_raw[];
@@ -353,7 +345,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         }
         if (lane < 2) {
             mbar_init(&sh.q_full[lane], 1);
-            mbar_init(&sh.q_ready[lane], 4);
             mbar_init(&sh.q_empty[lane], lane == 0 && a.ctas > 1 ? 3 : 2);    // both streams; in a cluster sums are kept in place 0
             mbar_init(&sh.s_full[lane], 1);
             mbar_init(&sh.p_full[lane], 8);
@@ -469,7 +460,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             // ---- products of stream st.  The whole warp walks through the loop and one lane issues: what the instructions take
             // must be known to be the same for all lanes (hence the shuffles), or every operand is moved to the uniform registers
             // by itself, at 100 cycles and more an instruction against the 64 that it runs.
-            constexpr uint32_t kFmt = std::is_same<M, __nv_bfloat16>::value ? 1u : 0u;
+            constexpr uint32_t kFmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
             constexpr uint32_t kCommon = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((uint32_t)(kTile >> 4) << 24);
             constexpr uint32_t kIdescS = kCommon | ((uint32_t)(kTile >> 3) << 17);
             constexpr uint32_t kIdescO = kCommon | ((uint32_t)(D >> 3) << 17) | (1u << 16);       // second operand MN-major
@@ -477,7 +468,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             const int st = uniform(warp == 3);
             const uint32_t t0 = uniform(tmem), s_at = t0 + st * kTile, p_at = s_at + (Q8 ? 32 : 0), o_at = t0 + 256 + st * D;
             const uint64_t q_desc = make_desc(smem_u32(q_s)), k_desc = make_desc(smem_u32(stages)), v_desc = make_desc_mn(smem_u32(stages));
-            uint64_t *q_bar = kTurnQ ? sh.q_ready : sh.q_full, *q_empty = sh.q_empty;
+            uint64_t *q_full = sh.q_full, *q_empty = sh.q_empty;
             const bool issuer = elect_one();
             int base = 0, at = 0;                            // tiles of earlier segments; tiles gone through
             int steps = 0, uses0 = 0, uses1 = 0;
@@ -535,8 +526,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     }
                 };
                 // the queries: both streams wait for and free all row tiles, for the same reason
-                wait(&q_bar[0], uses0++);
-                if (ok && !one) wait(&q_bar[1], uses1++);
+                wait(&q_full[0], uses0++);
+                if (ok && !one) wait(&q_full[1], uses1++);
                 if (ok && n > 0) {
                     const int x = base + k_place(one ? st : 0);
                     if (reach(x) && lock()) {
@@ -647,8 +638,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             const bool valid = row < ManyRows::per_tile(a) * a.group && tok < c.len;
             const int limit = a.mask ? c.total : min(c.total, c.ctx + min(tok, c.len - 1) + 1);
             const int all_seen = min(c.total, a.mask ? c.ctx : c.ctx + min(first_tok, c.len - 1) + 1);    // by every row
-            float m = -INFINITY, l = 0.f, scale = a.scale_log2;      // m in powers of two
-            int v_exp = -127;
+            float m = -INFINITY, l = 0.f;                     // m in powers of two
+            const float scale = a.scale_log2;
 #pragma unroll 1
             for (int j = 0; j < n_mine; ++j) {
                 const int vj = w.one ? 2 * j + st : j, p0 = w.tile(vj) * kTile, v_at = base + w.v_place(vj);
@@ -657,7 +648,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     dead = true;
                 }
                 const bool ragged = !Q8 && vj == w.nt - 1 && p0 + kTile > c.total;
-                if (Q8 || ragged)                             // the values' exponent, or their places behind the end
+                if (ragged)                                   // the values: their places behind the end are cleared
                     if (!dead && !mbar_wait(&sh.full[v_at % kStages], (v_at / kStages) & 1, wl)) {
                         report_timeout(a.kv.status);
                         dead = true;
@@ -674,14 +665,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 const bool masked = p0 + kTile > all_seen;
                 tmem_ld32(ts, su);
                 if constexpr (!Q8) tmem_ld32(ts + 32, su + 32);
-                int dv = 0;                                   // 8-bit: weights are multiplied by 2^dv
-                bool over = false;
-                if constexpr (Q8) {
-                    scale = a.scale_log2 * (kTurnQ ? sh.q_scale[i & 1][w.one ? 0 : st][row] : 1.f) * pow2f(max(sh.tile_exp[(base + w.k_place(vj)) & 15], -100));
-                    scale = fmaxf(scale, 1e-37f);             // -infinity times it stays one
-                    dv = sh.tile_exp[v_at & 15];
-                    over = dv > v_exp;
-                }
                 // What a row sees of 32 positions, and the largest score.
                 auto seen = [&](int p) {
                     const int n = min(max(limit - p, 0), 32);
@@ -721,7 +704,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 if constexpr (Q8) largest(s + 32, 32);
                 else largest(s, 64);
                 const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-                over |= valid && top - m > kSlack;            // -inf - -inf is NaN: no
+                const bool over = valid && top - m > kSlack;  // -inf - -inf is NaN: no
                 tc_fence_before();
                 // Both halves of a row have one maximum; both have been read, weights may take their place.  The two warps that have
                 // these 32 rows meet, nobody else has to.
@@ -735,15 +718,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     if (!half) *pass = mn = fmaxf(fmaxf(m, top), *pass);
                     bar_sync(pair_bar, 64);
                     if (half) mn = *pass;
-                    float f = mn > -INFINITY ? ex2(m - mn) : 1.f;
+                    const float f = mn > -INFINITY ? ex2(m - mn) : 1.f;
                     l *= f;
                     m = mn;
-                    if constexpr (Q8) {
-                        if (dv > v_exp) {
-                            f *= pow2f(max(v_exp - dv, -126));
-                            v_exp = dv;
-                        }
-                    }
                     if (j > 0) {
 #pragma unroll 1
                         for (int k = half * (D / 2); k < half * (D / 2) + D / 2; k += 16) {
@@ -760,8 +737,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     bar_sync(pair_bar, 64);                   // the second product begins when one half has its weights
                     tc_fence_after();
                 }
-                if constexpr (Q8) dv = max(dv - v_exp, -126);
-                const float off = (m > -INFINITY ? m : 0.f) - (Q8 ? (float)dv : 0.f);
+                const float off = m > -INFINITY ? m : 0.f;
                 const uint64_t scale2 = pair(scale, scale), off2 = pair(-off, -off);
                 uint64_t sum0 = 0, sum1 = 0;
                 // weights of some scores, packed and stored at column c0
@@ -778,7 +754,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         x = pair(lo, hi);
                         if (k & 2) sum1 = add2(sum1, x);
                         else sum0 = add2(sum0, x);
-                        p[k / 2] = pack2<M>(lo, hi);
+                        p[k / 2] = pack2<T>(lo, hi);
                     }
                     if constexpr (Q8) tmem_st8(tp + c0, p);
                     else tmem_st16(tp + c0, p);
@@ -799,7 +775,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 }
                 float a0, a1;
                 unpair(add2(sum0, sum1), a0, a1);
-                l += Q8 ? (a0 + a1) * pow2f(-dv) : a0 + a1;
+                l += a0 + a1;
                 if (ragged) {                                 // the places behind the end among this half's positions
                     const int end = min(max(c.total - p0, 64 * half), 64 * half + 64), rows = 64 * half + 64 - end;
                     uint8_t *tile = stages + (size_t)(v_at % kStages) * kTileBytes + end * 128;
@@ -822,7 +798,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             if (!half) {
                 sh.l[st][row] += l;
                 sh.m[st][row] = m;
-                if (Q8 && row == 0) sh.v_exp[st] = v_exp;
             }
             if (w.n[0] > 0) {
                 if ((w.one || st == 0) && !dead && !mbar_wait(&sh.o_full[0], items0 & 1, wl)) {
@@ -857,11 +832,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 f1 = m > -INFINITY ? ex2(mb - m) : 0.f;
                 l = f0 * l + f1 * sh.l[1][row];
             }
-            float e0 = 1.f, e1 = 1.f;                          // 8-bit: what the sums are relative to
-            if constexpr (Q8) {
-                e0 = pow2f(max(sh.v_exp[w.one ? 0 : st], -126));
-                e1 = pow2f(max(sh.v_exp[1], -126));
-            }
             const bool split = seg.c0 != seg.c1;
             const long long at = (long long)(c.row0 + tok) * heads + seg.head * a.group + row - row_tok * a.group;
             const bool own = (w.tile(max(w.nt - 1, 0)) + 1) * kTile > c.ctx;      // the chunk's own tokens are among the positions
@@ -892,7 +862,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     for (int x = 0; x < a.ctas; ++x) st_async(&sent_ml[rank * kTile + row], make_float2(m, l), &sh.ready, x);
             }
             // sums of this CTA: 16 elements at a time from TMEM to the result, the part, or the octet's CTA
-            auto take = [&](int of, uint32_t addr, int d, float e, float *x) {         // sums of stream `of`
+            auto take = [&](int of, uint32_t addr, int d, float *x) {         // sums of stream `of`
                 uint32_t r[16];
                 tmem_ld16(addr, r);
                 tmem_ld_wait16(r);
@@ -901,7 +871,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 for (int k = 0; k < 16; ++k) {
                     x[k] = __uint_as_float(r[k]);
                     odd = fmaf(x[k], 0.f, odd);
-                    if (Q8) x[k] *= e;
                 }
                 if constexpr (!Q8) {
                     if (own && valid && odd != 0.f) {          // NaN
@@ -918,7 +887,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             for (int d = d0; d < d1; d += 16) {
                 float x[16];
                 if (w.n[w.one ? 0 : st] > 0) {
-                    take(w.one ? 0 : st, w.one ? tmem + lanes + 256 + d : to + d, d, e0, x);
+                    take(w.one ? 0 : st, w.one ? tmem + lanes + 256 + d : to + d, d, x);
                 } else {
 #pragma unroll
                     for (int k = 0; k < 16; ++k) x[k] = 0.f;
@@ -928,7 +897,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     for (int k = 0; k < 16; ++k) x[k] = f0 > 0.f || f0 != f0 ? f0 * x[k] : 0.f;
                     if (w.n[1] > 0) {
                         float z[16];
-                        take(1, tmem + lanes + 256 + D + d, d, e1, z);
+                        take(1, tmem + lanes + 256 + D + d, d, z);
 #pragma unroll
                         for (int k = 0; k < 16; ++k) x[k] += f1 > 0.f || f1 != f1 ? f1 * z[k] : 0.f;
                     }
@@ -1055,52 +1024,18 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             job_done(i);
         }
     } else {
-        // ---- 8-bit tiles -> fp16 tiles, bf16 queries -> fp16 
+        // ---- 8-bit tiles -> 16-bit tiles
         if constexpr (Q8) {
             set_registers<false, 32>();
             constexpr int kPieces = D / 16;                  // 16-byte pieces of a position
-            const int t = tid - 640, q_st = t >> 7, q_at = t & 127;      // queries: thread q_at has row q_at of tile q_st
-            int done = 0, uses = 0;                          // tiles; queries
+            const int t = tid - 640;
+            int done = 0;                                    // tiles
             bool ok = true;
             for (int i = 0; ok; ++i) {
                 if (!job_of(i)) { ok = false; break; }
                 const Job &w = sh.job[i & 1];
                 if (!w.more) break;
                 const Chunk c = w.c;
-                if constexpr (kTurnQ) {
-                    if (q_st == 0 || !w.one) {
-                        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&sh.q_full[q_st], uses++ & 1, wl));
-                        if (!ok) break;
-                        uint8_t *q_row = q_s + q_st * kTileBytes + q_at * 128;
-                        auto at = [&](int x) { return reinterpret_cast<uint4 *>(q_row + (x >> 3) * kSlabBytes + (((x & 7) ^ (q_at & 7)) << 4)); };
-                        uint32_t big = 0;
-#pragma unroll 4
-                        for (int x = 0; x < kSlabs * 8; ++x) {
-                            const uint4 v = *at(x);
-                            big = __vmaxu2(big, __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
-                        }
-                        big = max(big & 0xFFFFu, big >> 16);
-                        // times 2^e: the largest element to 2^14 .. 2^15; in two factors, as e may be beyond a number's range
-                        const int e = big ? min(14 + 127 - (int)(big >> 7), 200) : 0;
-                        const float f0 = pow2f(e / 2), f1 = pow2f(e - e / 2);
-#pragma unroll 4
-                        for (int x = 0; x < kSlabs * 8; ++x) {
-                            const uint4 v = *at(x);
-                            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-                            uint32_t o[4];
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const float2 y = unpack2<T>(u[k]);
-                                o[k] = pack2<__half>(y.x * f0 * f1, y.y * f0 * f1);
-                            }
-                            *at(x) = make_uint4(o[0], o[1], o[2], o[3]);
-                        }
-                        sh.q_scale[i & 1][q_st][q_at] = pow2f(-(e / 2)) * pow2f(-(e - e / 2));
-                        fence_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&sh.q_ready[q_st]);
-                    }
-                }
 #pragma unroll 1
                 for (int x = 0, kj = 0, vj = 0; x < 2 * w.nt && ok; ++x, ++done) {
                     const bool is_v = x == w.v_place(vj);
@@ -1112,13 +1047,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     if (!ok) break;
                     const uint8_t *raw = raws + (size_t)rs * Geo::kRawBytes;
                     uint8_t *tile = stages + (size_t)s * kTileBytes;
-                    // the largest exponent in use (every warp finds it)
-                    uint32_t e4 = reinterpret_cast<const uint32_t *>(sh.exps[rs])[lane];
-                    const int used = min(max(c.total - p0 - 4 * lane, 0), 4);
-                    e4 &= used == 4 ? 0xFFFFFFFFu : (1u << 8 * used) - 1u;
-                    e4 = __vmaxu4(e4, e4 >> 16);
-                    const int e_max = max(1, (int)__reduce_max_sync(0xFFFFFFFFu, max(e4 & 0xFFu, e4 >> 8 & 0xFFu)));
-                    if (t == 0) sh.tile_exp[done & 15] = e_max - 127;
                     // A thread has piece `piece` of every (32 x kConvert / kPieces)-th position, two at a time (four spill): both
                     // loads before the first store, which the compiler would not move a load across.  Pieces of the second slab go by the neighbouring
                     // position, whose swizzle spreads the slabs over the banks.
@@ -1147,17 +1075,15 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 #pragma unroll
                         for (int n = 0; n < 2; ++n) {
                             const uint32_t u[4] = {codes[n].x, codes[n].y, codes[n].z, codes[n].w};
-                            const int e = min(exps[n] - e_max, 0);
-                            // 2^e as fp16, 0 below 2^-24
-                            const uint32_t sc = (e >= -14 ? (uint32_t)(e + 15) << 10 : e >= -24 ? 1u << (e + 24) : 0u) * 0x10001u;
+                            const uint32_t sc = scale_bits<T>(exps[n]) * 0x10001u;
                             uint32_t o[8];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                codes_to_halves(u[k], o[2 * k], o[2 * k + 1]);
+                            for (int k = 0; k < 4; ++k) codes_to_pairs<T>(u[k], sc, o[2 * k], o[2 * k + 1]);
+                            if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+                                if (exps[n] > kBigExp) {          // values beyond 57344
+                                    const uint32_t more = big_scale(exps[n]) * 0x10001u;
 #pragma unroll
-                                for (int y = 2 * k; y < 2 * k + 2; ++y) {
-                                    const __half2 v = __hmul2(*reinterpret_cast<__half2 *>(&o[y]), *reinterpret_cast<const __half2 *>(&sc));
-                                    o[y] = *reinterpret_cast<const uint32_t *>(&v);
+                                    for (int k = 0; k < 8; ++k) o[k] = times_pair(o[k], more);
                                 }
                             }
                             static_assert(kTile / kMine % 8 == 0, "a thread's positions are swizzled alike");

@@ -48,22 +48,6 @@ template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, f
     return *reinterpret_cast<uint32_t *>(&h);
 }
 
-// Two E4M3 codes in bytes 1 and 3 of `w` (the others 0) as a pair of T, times the pair `scale`.  fp16: the hardware
-// conversion.  bf16: the code's bits moved to bf16's exponent and mantissa are its value x 2^-120 (the biases
-// differ by 120, E4M3's subnormals fall among the normal numbers' steps), so `scale` carries 2^120.
-template <typename T> __device__ __forceinline__ uint32_t codes_to_pair(uint32_t w, uint32_t scale);
-template <> __device__ __forceinline__ uint32_t codes_to_pair<__half>(uint32_t w, uint32_t scale)
-{
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)__byte_perm(w, 0, 0x0031), __NV_E4M3);
-    const __half2 r = __hmul2(*reinterpret_cast<const __half2 *>(&h), *reinterpret_cast<const __half2 *>(&scale));
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
-template <> __device__ __forceinline__ uint32_t codes_to_pair<__nv_bfloat16>(uint32_t w, uint32_t scale)
-{
-    const uint32_t b = (w & 0x80008000u) | ((w >> 4) & 0x07F007F0u);
-    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&b), *reinterpret_cast<const __nv_bfloat162 *>(&scale));
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
 // The four codes of a word as two pairs of fp16.
 __device__ __forceinline__ void codes_to_halves(uint32_t w, uint32_t &lo, uint32_t &hi)
 {
@@ -72,24 +56,36 @@ __device__ __forceinline__ void codes_to_halves(uint32_t w, uint32_t &lo, uint32
     lo = *reinterpret_cast<const uint32_t *>(&x);
     hi = *reinterpret_cast<const uint32_t *>(&y);
 }
-// The four codes of a word as two pairs, scaled.
+__device__ __forceinline__ uint32_t times_halves(uint32_t x, uint32_t y)
+{
+    const __half2 r = __hmul2(*reinterpret_cast<const __half2 *>(&x), *reinterpret_cast<const __half2 *>(&y));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+// The same of bf16.
+__device__ __forceinline__ uint32_t times_pair(uint32_t x, uint32_t y)
+{
+    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&y));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+// The four codes of a word as two pairs of T, times the pair `scale` = scale_bits() twice: the values, exactly.  fp16: the hardware
+// conversion.  bf16: the code's bits moved to bf16's exponent and mantissa are its value x 2^-120 (the biases
+// differ by 120, E4M3's subnormals become bf16's), so `scale` carries 2^120.
 template <typename T>
 __device__ __forceinline__ void codes_to_pairs(uint32_t w, uint32_t scale, uint32_t &lo, uint32_t &hi)
 {
     if constexpr (std::is_same<T, __half>::value) {
-        const __half2 s = *reinterpret_cast<const __half2 *>(&scale);
-        const __half2_raw x = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3);
-        const __half2_raw y = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
-        const __half2 p = __hmul2(*reinterpret_cast<const __half2 *>(&x), s), q = __hmul2(*reinterpret_cast<const __half2 *>(&y), s);
-        lo = *reinterpret_cast<const uint32_t *>(&p);
-        hi = *reinterpret_cast<const uint32_t *>(&q);
+        codes_to_halves(w, lo, hi);
+        lo = times_halves(lo, scale);
+        hi = times_halves(hi, scale);
     } else {
-        lo = codes_to_pair<T>(__byte_perm(w, 0, 0x1404), scale);
-        hi = codes_to_pair<T>(__byte_perm(w, 0, 0x3424), scale);
+        auto moved = [](uint32_t two) { return (two & 0x80008000u) | ((two >> 4) & 0x07F007F0u); };      // codes in bytes 1 and 3
+        lo = times_pair(moved(__byte_perm(w, 0, 0x1404)), scale);
+        hi = times_pair(moved(__byte_perm(w, 0, 0x3424)), scale);
     }
 }
-// What codes_to_pair() multiplies by for exponent byte `eb`, as the bits of one T.  bf16: 2^(e + 120) is representable up
-// to e = 7; larger ones (values beyond 57344) are finished by a second product with big_scale().
+// What codes_to_pairs() multiplies by for exponent byte `eb`, as the bits of one T; finite for any byte.  bf16: 2^(e + 120) is
+// representable up to e = 7 (kBigExp); larger ones (values beyond 57344) are finished by a second product with big_scale().
+constexpr int kBigExp = 134;
 template <typename T> __device__ __forceinline__ uint32_t scale_bits(int eb);
 template <> __device__ __forceinline__ uint32_t scale_bits<__half>(int eb)
 {
@@ -98,10 +94,9 @@ template <> __device__ __forceinline__ uint32_t scale_bits<__half>(int eb)
 }
 template <> __device__ __forceinline__ uint32_t scale_bits<__nv_bfloat16>(int eb)
 {
-    return (uint32_t)(min(eb, 134) + 120) << 7;
+    return (uint32_t)(min(eb, kBigExp) + 120) << 7;
 }
-__device__ __forceinline__ uint32_t big_scale(int eb) { return (uint32_t)(127 + max(eb - 134, 0)) << 7; }
-
+__device__ __forceinline__ uint32_t big_scale(int eb) { return (uint32_t)(127 + max(eb - kBigExp, 0)) << 7; }
 
 // ---- a batch of chunks -------------------------------------------------------------------------
 struct Chunk {
@@ -134,19 +129,6 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t b
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
                  "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar))
                  : "memory");
-}
-// Distributed shared memory: the same place in CTA `rank` of the cluster.
-__device__ __forceinline__ float ld_cluster(const float *p, uint32_t rank)
-{
-    float x;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(mapa_rank(smem_u32(p), rank)) : "memory");
-    return x;
-}
-__device__ __forceinline__ float4 ld_cluster(const float4 *p, uint32_t rank)
-{
-    float4 x;
-    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(mapa_rank(smem_u32(p), rank)) : "memory");
-    return x;
 }
 // Sends to CTA `rank` of the cluster; its barrier (at the same place as `bar` here) counts the bytes when they have arrived.
 __device__ __forceinline__ void st_async(float4 *p, const float4 &x, uint64_t *bar, uint32_t rank)

@@ -147,7 +147,7 @@ def pathed(path, *args, **kw):
     return case
 
 
-@pytest.mark.parametrize("path", [1])
+@pytest.mark.parametrize("path", [1, 2])
 @pytest.mark.parametrize("dtype,d", BOTH)
 @pytest.mark.parametrize("chunk,G,peak", [(1, 4, 1.0), (30, 2, 6.0), (150, 1, 1.0), (1, 12, 6.0)])
 def test_zero_rows_among_small_values(path, dtype, d, chunk, G, peak):
@@ -163,7 +163,7 @@ def test_zero_rows_among_small_values(path, dtype, d, chunk, G, peak):
     check(case, case.queries(2 * G, amp=peak), scale=d ** -0.5 / amp)
 
 
-@pytest.mark.parametrize("path", [1])
+@pytest.mark.parametrize("path", [1, 2])
 @pytest.mark.parametrize("dtype,d", BOTH)
 @pytest.mark.parametrize("chunk,G", [(5, 1), (30, 2), (100, 1), (90, 4)])
 @pytest.mark.parametrize("what", ["k", "v", "kv"])
@@ -183,7 +183,7 @@ def test_tokens_that_are_not_seen_may_have_any_size(path, dtype, d, chunk, G, wh
     check(case, q, seen=seen, mask=bits_of(np.concatenate([tree, tree])))
 
 
-@pytest.mark.parametrize("path", [1])
+@pytest.mark.parametrize("path", [1, 2])
 @pytest.mark.parametrize("dtype,d", BOTH)
 @pytest.mark.parametrize("chunk,G", [(1, 4), (40, 3)])
 def test_rows_of_very_different_sizes(path, dtype, d, chunk, G):
