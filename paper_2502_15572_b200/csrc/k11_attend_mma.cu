@@ -133,6 +133,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     constexpr int kValPieces = kRowBytes / 8 / kValBytes;
     constexpr int kValElems = kValBytes / (Q8 ? 1 : 2);   // elements in it
     using M = std::conditional_t<Q8, __half, T>;            // type of the products
+    constexpr float kLift = Lift<M>::value;                 // 2^kLift x weights; of an 8-bit cache those of the values alone
     using VPiece = typename Piece<kValBytes>::type;
     using Sh = Shared<Q8, D, NT>;
 
@@ -461,8 +462,8 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     const float base = m[nt][x] > -INFINITY ? m[nt][x] : 0.f, base_v = mv[nt][x] > -INFINITY ? mv[nt][x] : 0.f;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        if constexpr (Q8) wv[2 * j + x] = ex2(sc[nt][2 * j + x] + (vf[j] - base_v));
-                        sc[nt][2 * j + x] = ex2(sc[nt][2 * j + x] - base);
+                        if constexpr (Q8) wv[2 * j + x] = ex2(sc[nt][2 * j + x] + (vf[j] - base_v + kLift));
+                        sc[nt][2 * j + x] = ex2(sc[nt][2 * j + x] - (Q8 ? base : base - kLift));
                     }
                     l[nt][x] += sc[nt][x] + sc[nt][2 + x];
                 }
@@ -576,7 +577,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     sh.m[warp][r] = m[nt][x];
                     sh.l[warp][r] = l[nt][x];
                 }
-                const float f = !Q8 ? 1.f : mv[nt][x] > -INFINITY ? ex2(mv[nt][x] - m[nt][x]) : 0.f;
+                const float f = !Q8 ? 1.f : mv[nt][x] > -INFINITY ? ex2(mv[nt][x] - m[nt][x] - kLift) : 0.f;
 #pragma unroll
                 for (int st = 0; st < kSteps; st += 2) {   // elements 2 st .. 2 st + 3 of the lane's piece are neighbours
                     const int e = 2 * st;
@@ -595,7 +596,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             const long long at = (long long)(ch.row0 + tok) * heads + seg.head * a.group + rr - tok * a.group;
             *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + at * D + e) =
                 make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
-            if (a.lse && e == 0) a.lse[at] = ((mm > -INFINITY ? mm : 0.f) + log2f(ll)) * 0.69314718055994531f;
+            if (a.lse && e == 0) a.lse[at] = ((mm > -INFINITY ? mm - (Q8 ? 0.f : kLift) : 0.f) + log2f(ll)) * 0.69314718055994531f;
         };
         auto add = [](float4 &acc, float f, const float4 &y) {                         // what has no weight may be anything
             if (f > 0.f || f != f) acc.x += f * y.x, acc.y += f * y.y, acc.z += f * y.z, acc.w += f * y.w;

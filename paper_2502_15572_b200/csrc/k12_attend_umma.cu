@@ -298,7 +298,7 @@ __device__ __noinline__ void repair(const AttendArgs &a, const Job &job, int st,
                     s = fmaf(kk.x, qq.x, s);
                     s = fmaf(kk.y, qq.y, s);
                 }
-                const float w = unpack2<T>(pack2<T>(ex2(s * a.scale_log2 - m), 0.f)).x;
+                const float w = unpack2<T>(pack2<T>(ex2(s * a.scale_log2 - m + Lift<T>::value), 0.f)).x;
                 for (int e = 0; e < 16; ++e) y[e] += w * unpack2<T>(reinterpret_cast<const uint16_t *>(v)[e]).x;
             }
         }
@@ -737,7 +737,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     bar_sync(pair_bar, 64);                   // the second product begins when one half has its weights
                     tc_fence_after();
                 }
-                const float off = m > -INFINITY ? m : 0.f;
+                const float off = (m > -INFINITY ? m : 0.f) - Lift<T>::value;
                 const uint64_t scale2 = pair(scale, scale), off2 = pair(-off, -off);
                 uint64_t sum0 = 0, sum1 = 0;
                 // weights of some scores, packed and stored at column c0
@@ -1018,7 +1018,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     }
                 }
             }
-            if (done && valid && a.lse && o0 == 0) a.lse[at] = (m > -INFINITY ? m + log2f(l) : -INFINITY) * 0.69314718055994531f;
+            if (done && valid && a.lse && o0 == 0) a.lse[at] = (m > -INFINITY ? m - Lift<T>::value + log2f(l) : -INFINITY) * 0.69314718055994531f;
             tc_fence_before();
             bar_sync(1, 512);                                // all have read O, sh.m and sh.l
             job_done(i);

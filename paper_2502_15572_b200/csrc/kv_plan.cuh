@@ -18,6 +18,11 @@ template <> struct KvType<__nv_bfloat16> {
     static constexpr uint32_t kBoundBits = 0x7F70u;      // 1.875 x 2^127
 };
 
+// fp16 ends at 2^-24, and a long tail of weights below that is still a part of the result: weights are held as 2^7 times what
+// they are, up to 2^8 of slack over a late maximum so up to 2^15, and down to 2^-31 of the largest.  (bf16 has fp32's range.)
+template <typename T> struct Lift { static constexpr float value = 0.f; };
+template <> struct Lift<__half> { static constexpr float value = 7.f; };
+
 // Least e with amax <= 448 2^e (448 = 1.75 x 2^8), from the bits of amax; 0 for amax = 0.
 __device__ __forceinline__ int kv_exponent(float amax, int min_exp)
 {

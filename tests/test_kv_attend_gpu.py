@@ -201,6 +201,41 @@ def test_rows_of_very_different_sizes(path, dtype, d, chunk, G):
     check(case, q)
 
 
+# ---- a long tail of small weights -------------------------------------------------------------------------------
+@pytest.mark.parametrize("path,chunk", [(1, 1), (1, 9), (2, 40)])
+@pytest.mark.parametrize("dtype,quantised", [("f16", False), ("f16", True), ("bf16", True), ("bf16", False)])
+def test_tails_below_the_types_last_bit(dtype, quantised, path, chunk):
+    """One position in 64 has e^18 = 2^26 times the weight of the others, whose values are large: what the tail adds up
+    to is all that most elements of the result have.  Weights are off by u of themselves or by 2^-32 of the largest:
+    |out - o| <= u sum p |v| / l + 2^-32 sum |v| / l + u |o| + fp32 terms, the weights p and their sum l relative to the largest;
+    sum p |v| / l is |o|, as every element's values have one sign."""
+    S, d = 8000, 64
+    case = Case(dtype, d, 64, 1, [S], [chunk], quantised, seed=79)
+    case.cache.set_option("attend_path", path)
+    k, v = np.zeros((S + chunk, 1, d)), np.full((S + chunk, 1, d), 28672.0)
+    k[::64, :, 0], v[::64, :, 1:], v[:, :, 0] = 18, 0, 0
+    v[::64, :, 0] = 1
+    for name, x in (("k", k), ("v", v)):
+        page, off = zip(*(case.place(0, p) for p in range(S + chunk)))
+        if quantised:
+            codes, exps = ref_quantise(x, dtype)
+            case.t[name][0, page, :, off] = torch.from_numpy(codes).cuda()
+            case.t[name + "_exp"][0, page, :, off] = torch.from_numpy(exps).cuda()
+        else:
+            case.t[name][0, page, :, off] = torch.from_numpy(x).to(DT[dtype]).cuda()
+    q = torch.zeros((chunk, 2, d), dtype=DT[dtype], device="cuda")
+    q[:, :, 0] = 8
+    lse = torch.empty((chunk, 2), device="cuda")
+    got = case.cache.attend(0, q, case.batch, lse=lse).double()
+    want, wlse, V, ds = expected(case, q, 0, causal_of(S, chunk), d ** -0.5)
+    u, ds, l = U[dtype], (d + 4) * 2.0 ** -24 * ds[..., None], torch.exp(wlse - 18)[..., None]
+    step = 0 if dtype == "bf16" and not quantised else 2.0 ** -32 * (S + chunk) * V[..., None] / l
+    tol = (2 * u + 2 * (ds + 2.0 ** -21) + (S + chunk) * 2.0 ** -24) * want.abs() + step + 2.0 ** -24
+    assert want[0, 0, 1] > 20 * tol[0, 0, 1] or dtype == "bf16"
+    assert ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).max()
+    assert ((lse - wlse).abs() <= ds[..., 0] + 2.0 ** -20 + 2.0 ** -23 * wlse.abs()).all()
+
+
 # ---- the same call, the same bits -------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype,quantised", [("f16", False), ("bf16", False), ("f16", True), ("bf16", True)])
 @pytest.mark.parametrize("G,chunk,path", [(3, 50, 2), (7, 20, 2), (12, 200, 2), (3, 1, 1), (5, 4, 1), (7, 30, 1)])
