@@ -374,8 +374,8 @@ dresd_status dresd_kv_status(dresd_kv *kv);
  *   "attend_path"  0 = automatic (by rows per key/value head), 1 = the mma.sync kernel, 2 = the tcgen05 kernel
  *                  (which a scale that is not positive never takes)
  *   "wait_ms"      bound of the device-side waits in milliseconds (0 = default, about 2 s)
- *   "debug_lose_stage"  test hook: in the next calls the first CTA of the tcgen05 kernel never receives its
- *                  tile (value-1), so its waits run out and dresd_kv_status() reports DRESD_ERR_TIMEOUT; 0 = off
+ *   "debug_lose_stage"  test hook: in the next calls the first CTA (of the mma.sync kernel its first warp) never receives
+ *                  its tile (value-1), so its waits run out and dresd_kv_status() reports DRESD_ERR_TIMEOUT; 0 = off
  * Unknown names return DRESD_ERR_INVALID.
  */
 dresd_status dresd_kv_set_option(dresd_kv *kv, const char *name, int value);

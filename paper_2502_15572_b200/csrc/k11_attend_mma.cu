@@ -103,6 +103,7 @@ struct Shared {
     uint64_t full[Geo::kWarps][Geo::kStages];
     uint64_t ready, taken;
     Job job[Geo::kWarps][4];                                         // of a worker
+    int dead[Geo::kWarps][2];                                        // a wait of the worker ran out, by the segment's parity
     unsigned ticket[Geo::kWarps];
 };
 
@@ -160,6 +161,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 
     if (lane == 0) {
         for (int s = 0; s < kStages; ++s) mbar_init(&sh.full[warp][s], 1);
+        sh.dead[warp][0] = sh.dead[warp][1] = 0;
         if (warp == 0) {
             mbar_init(&sh.ready, 1);
             mbar_init(&sh.taken, a.ctas);
@@ -259,7 +261,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         const Segment &seg = w.seg;
         const Chunk ch = w.c;
         if (!pending) look_ahead(i);                        // the segment after this one has become known
-        while (fetched - used < kStages && pending) {
+        while (fetched - used < kStages && pending && !dead) {
             if (lane == 0) fetch();
             ++fetched;
             look_ahead(i);
@@ -318,13 +320,16 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         for (int nt = 0; nt < NT; ++nt) m[nt][0] = m[nt][1] = mv[nt][0] = mv[nt][1] = -INFINITY, l[nt][0] = l[nt][1] = 0.f;
 
 #pragma unroll 1
-        for (int t = w.t0 + mine; t < w.t1; t += step) {
+        for (int t = w.t0 + mine; t < w.t1 && !dead; t += step) {
             const int p0 = t * kTile, s = used % kStages;
-            if (!dead && !mbar_wait(&sh.full[warp][s], (used / kStages) & 1, wl)) {
+            if (!mbar_wait(&sh.full[warp][s], (used / kStages) & 1, wl)) {
                 report_timeout(a.kv.status);
                 dead = true;
             }
+            // A warp that gave up asks for nothing more (its barriers' phases are not over) and leaves with its worker at the
+            // segment's end.
             dead = __any_sync(0xFFFFFFFFu, dead);
+            if (dead) break;
             const uint8_t *ks = sh.ring[warp][s], *vs_ = ks + Geo::kHalf;
             // ---- S^T = K Q^T; lane (g, c): keys place(g) (+ 8)
             float sc[NT][4] = {};
@@ -585,6 +590,10 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         make_float4(o[nt][st][x] * f, o[nt][st][2 + x] * f, o[nt][st + 1][x] * f, o[nt][st + 1][2 + x] * f);
                 }
             }
+        auto give_up = [&] {
+            if (dead) *const_cast<volatile int *>(&sh.dead[group][i & 1]) = 1;
+        };
+        give_up();
         sync();
         if (g_tid == 0) publish(i + 2);
         const int heads = a.kv.heads * a.group;
@@ -663,9 +672,9 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 }
                 put(y * a.ctas + rank, acc, mm, ll);
             }
+            give_up();
             __syncthreads();
             if (tid < a.ctas) mbar_arrive_cluster(mapa_rank(smem_u32(&sh.taken), tid));
-            dead = __any_sync(0xFFFFFFFFu, dead);
             ++joins;
         }
         if (split) {
@@ -698,13 +707,11 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             }
         }
         sync();                                             // the join's buffers are written again; job i + 2 is known
+        if (*const_cast<volatile int *>(&sh.dead[group][i & 1])) break;      // all of the worker's warps, or none
     }
     // no copy may be in flight when the CTA ends: all fetched tiles have been used unless a wait ran out
     for (; used < fetched; ++used)
-        if (!mbar_wait(&sh.full[warp][used % kStages], (used / kStages) & 1, wl)) {
-            if (lane == 0) report_timeout(a.kv.status);
-            break;
-        }
+        if (!mbar_wait(&sh.full[warp][used % kStages], (used / kStages) & 1, wl) && lane == 0) report_timeout(a.kv.status);
     __syncwarp();
     if (a.ctas > 1) cluster_sync_all();                     // nobody leaves while a neighbour may read its shared memory
 }

@@ -133,7 +133,7 @@ struct Shared {
     float m[2][kTile], l[2][kTile];                        // of the streams' rows; l also passes maxima between a row's threads
     uint64_t full[kStages], empty[kStages];
     uint64_t raw_full[kRaw ? kRaw : 1], raw_empty[kRaw ? kRaw : 1];
-    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2];
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], drained[2];
     uint64_t job_full[2], job_empty[2];
     uint64_t ready, taken;                                 // cluster: all sums have come / every CTA has read its share
     alignas(16) uint8_t exps[kRaw ? kRaw : 1][kRaw ? kTile : 16];      // exponents of the 8-bit tiles (bulk copies: 16-byte aligned)
@@ -349,6 +349,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             mbar_init(&sh.s_full[lane], 1);
             mbar_init(&sh.p_full[lane], 8);
             mbar_init(&sh.o_full[lane], 1);
+            mbar_init(&sh.drained[lane], 1);
             mbar_init(&sh.job_full[lane], 1);
             mbar_init(&sh.job_empty[lane], 3 + 16 + (Q8 ? kConvert : 0));        // a warp each: loads, products, softmax, conversion
         }
@@ -452,10 +453,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             if (!ok && lane == 0) report_timeout(a.kv.status);
             // no copy may be in flight when the CTA ends
             for (int x = max(0, issued - kRing); x < issued; ++x)
-                if (!mbar_wait(&full[x % kRing], (x / kRing) & 1, wl)) {
-                    if (lane == 0) report_timeout(a.kv.status);
-                    break;
-                }
+                if (!mbar_wait(&full[x % kRing], (x / kRing) & 1, wl) && lane == 0) report_timeout(a.kv.status);
         } else if (warp != 2) {
             // ---- products of stream st.  The whole warp walks through the loop and one lane issues: what the instructions take
             // must be known to be the same for all lanes (hence the shuffles), or every operand is moved to the uniform registers
@@ -570,6 +568,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 }
                 job_done(i);
             }
+            // no product may be running when the CTA ends, nor when TMEM is given back
+            if (issuer) tc_commit(&sh.drained[st]);
+            if (!mbar_wait(&sh.drained[st], 0, wl)) ok = false;
             if (!ok && lane == 0) report_timeout(a.kv.status);
         } else {
             // ---- the plan, and queries
@@ -622,7 +623,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         int steps = 0, items0 = 0, items1 = 0, joins = 0, base = 0;
         bool dead = false;
         for (int i = 0;; ++i) {
-            if (bar_or(1, 512, !job_of(i))) {                // all softmax warps go on, or none (they meet at barriers)
+            if (bar_or(1, 512, dead || !job_of(i))) {        // all softmax warps go on, or none (they meet at barriers)
                 report_timeout(a.kv.status);
                 break;
             }

@@ -250,3 +250,29 @@ def test_repeatable_whatever_ran_before(dtype, quantised, G, chunk, path):
     for amp in (1e-3, 8.0, 200.0):
         other.cache.attend(0, other.queries(2 * 8, amp=amp), other.batch)
         assert torch.equal(case.cache.attend(0, q, case.batch), first)
+
+
+# ---- waits that run out -------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("quantised", [False, True])
+@pytest.mark.parametrize("B,chunk,path,stage", [(2, 1, 1, 1), (2, 1, 1, 3), (60, 1, 1, 1), (60, 1, 1, 3)] +
+                         [(b, c, p, s) for b, c, p in ((2, 50, 1), (2, 30, 2), (12, 90, 2)) for s in (1, 3, 11)])
+def test_waits_that_run_out_in_either_kernel(B, chunk, path, stage, quantised):
+    """A warp (K11) or CTA (K12) never receives one of its tiles -- alone, in a cluster, in one group of several --: the call ends,
+    the status says so once, and the next call is right again."""
+    ctx = [30000] + [600] * (B - 1)
+    case = Case("bf16", 128, 32, 4, ctx, [chunk] * B, quantised, seed=80)
+    case.cache.set_option("attend_path", path)
+    q = case.queries(8)
+    first = case.cache.attend(0, q, case.batch)
+    case.cache.status()
+    case.cache.set_option("wait_ms", 20)
+    case.cache.set_option("debug_lose_stage", stage)
+    case.cache.attend(0, q, case.batch)
+    with pytest.raises(binding.DresdError) as e:
+        case.cache.status()
+    assert e.value.status == -5
+    case.cache.set_option("debug_lose_stage", 0)
+    case.cache.set_option("wait_ms", 0)
+    for _ in range(2):
+        assert torch.equal(case.cache.attend(0, q, case.batch), first)
+        case.cache.status()
