@@ -82,8 +82,7 @@ struct ManyRows {
     // position tiles that the item's rows see
     static __device__ __forceinline__ int tiles(const AttendArgs &a, const Chunk &k, int r)
     {
-        int seen = k.total;
-        if (!a.mask) seen = min(seen, k.ctx + r * (int)a.by_rows.d + tokens(a, k, r));
+        const int seen = a.mask ? k.total : k.upto(r * (int)a.by_rows.d + tokens(a, k, r) - 1);
         return max(1, (seen + kTile - 1) / kTile);
     }
     // a unit keeps all streams busy for one tile: one tile of positions for two row tiles, one for each stream for one
@@ -637,8 +636,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             // A row of the result.  The others hold the queries of other tokens, or (behind 128 / group x group) whatever was in shared
             // memory: they take part in nothing.
             const bool valid = row < ManyRows::per_tile(a) * a.group && tok < c.len;
-            const int limit = a.mask ? c.total : min(c.total, c.ctx + min(tok, c.len - 1) + 1);
-            const int all_seen = min(c.total, a.mask ? c.ctx : c.ctx + min(first_tok, c.len - 1) + 1);    // by every row
+            const int limit = a.mask ? c.total : c.upto(min(tok, c.len - 1));
+            const int all_seen = a.mask ? c.ctx : c.upto(min(first_tok, c.len - 1));    // by every row
             float m = -INFINITY, l = 0.f;                     // m in powers of two
             const float scale = a.scale_log2;
 #pragma unroll 1

@@ -106,15 +106,18 @@ __device__ __forceinline__ uint32_t big_scale(int eb) { return (uint32_t)(127 + 
 // ---- a batch of chunks -------------------------------------------------------------------------
 struct Chunk {
     int row0, len;      // rows of the dense tensors
-    int ctx, total;     // positions before the chunk; positions in all that the table reaches
+    int ctx, total;     // positions before the chunk; positions in all; both no more than the table reaches
+    // Positions that token `tok` sees in causal order.  (ctx + tok may be beyond 31 bits, what the table reaches is not.)
+    __device__ __forceinline__ int upto(int tok) const { return ctx + min(tok + 1, total - ctx); }
 };
 __device__ __forceinline__ Chunk kv_chunk(const KvArgs &a, int b)
 {
     Chunk c;
     c.row0 = min(max(a.start[b], 0), a.rows);
     c.len = min(max(a.start[b + 1], c.row0), a.rows) - c.row0;
-    c.ctx = max(a.ctx[b], 0);
-    c.total = (int)min((long long)c.ctx + c.len, (long long)a.width << a.page_shift);
+    const int reach = (int)((long long)a.width << a.page_shift);      // the host has checked that it fits
+    c.ctx = min(max(a.ctx[b], 0), reach);
+    c.total = c.ctx + min(c.len, reach - c.ctx);
     return c;
 }
 // Row of (layer, page, head, offset) in the cache arrays; page numbers outside the pool count as `bad`.
@@ -201,7 +204,7 @@ struct FewRows {
     static __device__ __forceinline__ int row_tiles(const AttendArgs &a, const Chunk &k) { return a.by_rows.ceil(k.len * a.group); }
     static __device__ __forceinline__ int seen(const AttendArgs &a, const Chunk &k, int r)         // positions
     {
-        return a.mask ? k.total : min(k.total, k.ctx + min(k.len - 1, a.by_group.div((r + 1) * (int)a.by_rows.d - 1)) + 1);
+        return a.mask ? k.total : k.upto(min(k.len - 1, a.by_group.div((r + 1) * (int)a.by_rows.d - 1)));
     }
     static __device__ __forceinline__ int units(const AttendArgs &a, const Chunk &k, int r) { return max(1, a.by_unit.ceil(seen(a, k, r))); }
 };

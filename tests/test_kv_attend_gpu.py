@@ -276,3 +276,32 @@ def test_waits_that_run_out_in_either_kernel(B, chunk, path, stage, quantised):
     for _ in range(2):
         assert torch.equal(case.cache.attend(0, q, case.batch), first)
         case.cache.status()
+
+
+# ---- lengths that cannot be --------------------------------------------------------------------------------------
+@pytest.mark.parametrize("path,chunk", [(1, 1), (1, 40), (2, 40), (2, 200)])
+@pytest.mark.parametrize("ctx", [2 ** 31 - 1, 2 ** 31 - 64, 2 ** 31 - 4097, 10 ** 6])
+@pytest.mark.parametrize("quantised,masked", [(False, False), (False, True), (True, False)])
+def test_contexts_beyond_the_table(path, chunk, ctx, quantised, masked):
+    """A sequence whose ctx is far beyond its table, as far as 31 bits go: its own result is unspecified, the
+    other sequences' are what they are, nothing is written to the cache."""
+    case = Case("f16", 64, 16, 2, [37, 500, 90], [chunk] * 3, quantised, seed=81)
+    case.cache.set_option("attend_path", path)
+    q = case.queries(6)
+    mask = bits_of(np.concatenate([np.tri(chunk, dtype=bool)] * 3)) if masked else None
+    want = case.cache.attend(0, q, case.batch, mask=mask)
+    case.batch.ctx[1] = ctx
+    held = {x: t.clone() for x, t in case.t.items() if t is not None}
+    got = case.cache.attend(0, q, case.batch, mask=mask)
+    good = torch.ones(case.rows, dtype=torch.bool, device="cuda")
+    good[chunk:2 * chunk] = False
+    # the work is divided otherwise, so the sums may be in another order: two roundings, and the weights'
+    most = held_rows(case, "v", 0, 37 + chunk).abs().max(), held_rows(case, "v", 2, 90 + chunk).abs().max()
+    assert ((got[good].double() - want[good].double()).abs() <= 4 * U["f16"] * max(most)).all()
+    k = torch.zeros((case.rows, 2, 64), dtype=torch.float16, device="cuda")
+    case.batch.ctx.fill_(ctx)
+    case.cache.append(0, k, k, case.batch)
+    case.cache.keep_draft(case.batch, torch.ones(3, dtype=torch.int32, device="cuda"), torch.full((3,), 3, dtype=torch.int32, device="cuda"), 2, 2)
+    assert not case.cache.read(0, case.batch)[0].any()
+    assert all(torch.equal(case.t[x], t) for x, t in held.items())
+    case.cache.status()
