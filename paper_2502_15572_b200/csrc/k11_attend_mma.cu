@@ -747,7 +747,7 @@ cudaError_t launch(const CUtensorMap &k_map, const CUtensorMap &v_map, const Att
     a.by_unit = FastDiv(unit);
     // Queries and join of a segment take about as long as four tiles of a warp: 48 ragged sequences 37 us, 66 with 0, 40 with 8.
     a.fixed = kFixed;
-    a.small = a.kv.heads * (a.kv.B + (long long)a.kv.rows * a.group / Geo::kRows + 1) * (positions / unit + 1 + a.fixed) < 1LL << 30;
+    a.small = plan_is_small(a, Geo::kRows, positions / unit + 1);
     auto kernel = attend_mma_kernel<T, Q8, D, NT>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;

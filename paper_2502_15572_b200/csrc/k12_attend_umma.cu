@@ -1144,7 +1144,7 @@ cudaError_t launch_attend_umma(const CUtensorMap &q_map, const CUtensorMap &k_ma
     a.by_unit = FastDiv(2 * a.ctas);
     a.groups = 1;
     a.fixed = kFixed;
-    a.small = a.kv.heads * (a.kv.B + (long long)a.kv.rows * a.group / kTile + 1) * (tiles + 1 + a.fixed) < 1LL << 30;
+    a.small = plan_is_small(a, kTile / a.group * a.group, tiles + 1);
     const bool q8 = a.kv.k_exps != nullptr;
     if (a.kv.dtype == kF16) {
         if (a.kv.d == 64) return q8 ? launch<__half, true, 64>(q_map, k_map, v_map, a, sms, stream) : launch<__half, false, 64>(q_map, k_map, v_map, a, sms, stream);

@@ -222,10 +222,12 @@ struct KvPlan {
     Chunk c;
 
     // Units of a sequence for one head in pieces of at most L, its largest item, its row tiles.
-    static __device__ __forceinline__ unsigned pieces_of(const AttendArgs &a, const Chunk &k, unsigned L, unsigned *most, unsigned *items)
+    template <typename Int>
+    static __device__ __forceinline__ Int pieces_of(const AttendArgs &a, const Chunk &k, unsigned L, unsigned *most, unsigned *items)
     {
         const int nr = Shape::row_tiles(a, k);
-        unsigned p = 0, m = 0;
+        Int p = 0;
+        unsigned m = 0;
 #pragma unroll 1
         for (int r = 0; r < nr; ++r) {
             const unsigned u = Shape::units(a, k, r);
@@ -265,17 +267,17 @@ struct KvPlan {
     {
         // a lane adds up B / 32 sequences in a row
         const int per = (a.kv.B + 31) >> 5, H = a.kv.heads, b0 = lane * per, b1 = min(b0 + per, a.kv.B);
-        unsigned most = 0, nr = 0;
-        Int own = 0;
+        unsigned most = 0;
+        Int own = 0, nr = 0;
 #pragma unroll 1
         for (int bb = b0; bb < b1; ++bb) {
             unsigned m, i;
-            own += pieces_of(a, kv_chunk(a.kv, bb), 1, &m, &i);
+            own += pieces_of<Int>(a, kv_chunk(a.kv, bb), 1, &m, &i);
             most = max(most, m);
             nr += i;
         }
         most = __reduce_max_sync(0xFFFFFFFFu, most);
-        const Int items = (Int)__reduce_add_sync(0xFFFFFFFFu, nr) * H, W = add_lanes(own) * H;
+        const Int items = add_lanes(nr) * H, W = add_lanes(own) * H;
         first = true;
         if (W == 0) return false;
         Int find = me;
@@ -291,12 +293,12 @@ struct KvPlan {
 #pragma unroll 1
                 for (int bb = b0; bb < b1; ++bb) {
                     unsigned m, i;
-                    own += pieces_of(a, kv_chunk(a.kv, bb), L, &m, &i);
+                    own += pieces_of<Int>(a, kv_chunk(a.kv, bb), L, &m, &i);
                 }
             }
         } else {
             L = 1;
-            own += (Int)nr * a.fixed;
+            own += nr * a.fixed;
             const Int line = W + items * a.fixed;
             n = (int)min((Int)count, line);
             if (me >= n) return false;
@@ -390,6 +392,14 @@ struct KvPlan {
         return false;
     }
 };
+
+// Do the plan's numbers fit 32 bits, for tiles of `rows` rows and items of at most `units` units?  start[] may contradict itself, up to
+// every sequence with all rows.
+inline bool plan_is_small(const AttendArgs &a, int rows, long long units)
+{
+    const double tiles = (double)a.kv.rows * a.group / rows + 1;
+    return (double)a.kv.heads * a.kv.B * tiles * (double)(units + a.fixed) < (double)(1 << 30);
+}
 
 // A persistent kernel of one CTA per SM, as clusters of `ctas`, no more of them than the device holds at once (its SMs
 // come in groups, which a cluster does not cross).

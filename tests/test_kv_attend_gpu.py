@@ -305,3 +305,31 @@ def test_contexts_beyond_the_table(path, chunk, ctx, quantised, masked):
     assert not case.cache.read(0, case.batch)[0].any()
     assert all(torch.equal(case.t[x], t) for x, t in held.items())
     case.cache.status()
+
+
+@pytest.mark.parametrize("path,chunk", [(1, 1), (1, 20), (2, 50)])
+def test_tables_so_wide_that_the_plan_counts_in_64_bits(path, chunk):
+    B, Hkv = 200, 4
+    ctx = ragged(82, B, 0, 200)
+    case = Case("f16", 64, 16, Hkv, ctx, [chunk] * B, seed=82)
+    case.cache.set_option("attend_path", path)
+    q = case.queries(2 * Hkv)
+    check(case, q)
+    table = torch.full((B, 1 << 18), -1, dtype=torch.int32, device="cuda")
+    table[:, :case.batch.page_table.shape[1]] = case.batch.page_table
+    case.batch = binding.KvBatch(table, case.batch.ctx, case.batch.start, rows=case.rows, max_chunk=chunk)
+    check(case, q)
+
+
+@pytest.mark.parametrize("path", [1, 2])
+def test_starts_that_contradict_each_other(path):
+    """Every second sequence has all rows: unspecified results, but an end, and nothing written beside them."""
+    B, rows = 41, 60
+    case = Case("bf16", 64, 32, 2, [100] * B, [rows] * B, seed=83)
+    case.cache.set_option("attend_path", path)
+    start = torch.tensor([rows * (b % 2) for b in range(B + 1)], dtype=torch.int32, device="cuda")
+    batch = binding.KvBatch(case.batch.page_table, case.batch.ctx, start, rows=rows, max_chunk=0)
+    out = torch.full((3 * rows, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    case.cache.attend(0, case.queries(4)[:rows], batch, out=out[rows:2 * rows])
+    case.cache.status()
+    assert (out[:rows] == 7).all() and (out[2 * rows:] == 7).all()
