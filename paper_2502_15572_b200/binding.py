@@ -9,6 +9,7 @@ them for torch tensors (used for device memory and streams only).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -369,6 +370,12 @@ def _torch():
     return _torch_module
 
 
+def _allocated_on(stream):
+    """Results are allocated on the stream that writes them: memory of the current stream's pool may still be in use by
+    what is queued there, and is given out there again while `stream` writes it."""
+    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
+
+
 def to_device(array, dtype: str, device="cuda"):
     """Upload a numpy array holding store-dtype values (bit patterns for 16-bit)."""
     import numpy as np
@@ -418,9 +425,10 @@ class Store:
         B = queries.shape[0]
         if out is None:
             dev = queries.device
-            out = (torch.empty((B, top_n), dtype=torch.int32, device=dev),
-                   torch.empty((B, top_n), dtype=torch.float32, device=dev),
-                   torch.empty((B, top_n, draft_len), dtype=torch.int32, device=dev))
+            with _allocated_on(stream):
+                out = (torch.empty((B, top_n), dtype=torch.int32, device=dev),
+                       torch.empty((B, top_n), dtype=torch.float32, device=dev),
+                       torch.empty((B, top_n, draft_len), dtype=torch.int32, device=dev))
         ids, scores, tokens = out
         s = (stream or torch.cuda.current_stream()).cuda_stream
         dresd_retrieve(self.handle, queries.data_ptr(), B, top_n, draft_len, ids.data_ptr(),
@@ -443,9 +451,10 @@ class Store:
         B = queries.shape[0]
         if out is None:
             dev = queries.device
-            out = (torch.empty((B, top_n), dtype=torch.int32, device=dev),
-                   torch.empty((B, top_n), dtype=torch.float32, device=dev),
-                   torch.empty((B, top_n, draft_len), dtype=torch.int32, device=dev))
+            with _allocated_on(stream):
+                out = (torch.empty((B, top_n), dtype=torch.int32, device=dev),
+                       torch.empty((B, top_n), dtype=torch.float32, device=dev),
+                       torch.empty((B, top_n, draft_len), dtype=torch.int32, device=dev))
         ids, scores, tokens = out
         s = (stream or torch.cuda.current_stream()).cuda_stream
         dresd_retrieve_filtered(self.handle, queries.data_ptr(),
@@ -457,7 +466,8 @@ class Store:
         """Build the 8-bit (E4M3) copy of the keys on the device and attach it; returns the copy."""
         torch = _torch()
         s = (stream or torch.cuda.current_stream()).cuda_stream
-        q8 = torch.empty((self.N, self.d), dtype=torch.uint8, device=self.keys.device)
+        with _allocated_on(stream):
+            q8 = torch.empty((self.N, self.d), dtype=torch.uint8, device=self.keys.device)
         dresd_quantise_keys(self.keys.data_ptr(), self.N, self.d, DTYPE_CODE[self.dtype], q8.data_ptr(), s)
         dresd_store_attach_quantised(self.handle, q8.data_ptr())
         self.keys_q8 = q8                                # keep the borrowed buffer alive
@@ -471,9 +481,10 @@ class Store:
         B = queries.shape[0]
         if out is None:
             dev = queries.device
-            out = (torch.empty((B, top_n), dtype=torch.int32, device=dev),
-                   torch.empty((B, top_n), dtype=torch.float32, device=dev),
-                   torch.empty((B, top_n, draft_len), dtype=torch.int32, device=dev))
+            with _allocated_on(stream):
+                out = (torch.empty((B, top_n), dtype=torch.int32, device=dev),
+                       torch.empty((B, top_n), dtype=torch.float32, device=dev),
+                       torch.empty((B, top_n, draft_len), dtype=torch.int32, device=dev))
         ids, scores, tokens = out
         s = (stream or torch.cuda.current_stream()).cuda_stream
         dresd_retrieve_quantised(self.handle, queries.data_ptr(),
@@ -493,7 +504,8 @@ class Store:
     def preprocess(self, queries, stream=None):
         torch = _torch()
         B = queries.shape[0]
-        out = torch.empty((B, self.d), dtype=torch.float32, device=queries.device)
+        with _allocated_on(stream):
+            out = torch.empty((B, self.d), dtype=torch.float32, device=queries.device)
         s = (stream or torch.cuda.current_stream()).cuda_stream
         dresd_preprocess(self.handle, queries.data_ptr(), B, out.data_ptr(), s)
         return out
@@ -614,7 +626,8 @@ class KvCache:
         torch = _torch()
         shape = (batch.rows, self.kv_heads, self.head_dim)
         if out is None:
-            k, v = torch.empty((2, *shape), dtype=self.torch_dtype, device=self.k_pages.device).unbind(0)
+            with _allocated_on(stream):
+                k, v = torch.empty((2, *shape), dtype=self.torch_dtype, device=self.k_pages.device).unbind(0)
         else:
             k, v = out
             for name, t in (("out k", k), ("out v", v)):
@@ -631,7 +644,8 @@ class KvCache:
         q_row, q_head = self._rows("q", q, batch)
         rows, heads, d = q.shape
         if out is None:
-            out = torch.empty((rows, heads, d), dtype=self.torch_dtype, device=self.k_pages.device)
+            with _allocated_on(stream):
+                out = torch.empty((rows, heads, d), dtype=self.torch_dtype, device=self.k_pages.device)
         elif out.shape != q.shape or out.dtype != q.dtype or not out.is_cuda or not out.is_contiguous():
             raise DresdError(-1, f"out must be a contiguous {q.dtype} CUDA tensor of shape {tuple(q.shape)}")
         if lse is not None and (lse.shape != (rows, heads) or lse.dtype != torch.float32 or not lse.is_cuda or
