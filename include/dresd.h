@@ -285,8 +285,8 @@ dresd_status dresd_retrieve_quantised(dresd_store *store, const void *queries, c
  * A row that holds a NaN gives unspecified values.
  *
  * All arrays are BORROWED.  dresd_kv_create() allocates the workspace of the attention on the
- * current device (about 50 MB) and launches nothing.  A cache is bound to its device and may be used
- * from one stream at a time; the calls below are asynchronous on `stream`, allocate nothing
+ * current device (about 50 MB) and launches nothing.  A cache is bound to its device (memory of another one is
+ * refused, here and in every call) and may be used from one stream at a time; the calls below are asynchronous on `stream`, allocate nothing
  * and can be captured into a CUDA graph.
  */
 typedef struct dresd_kv dresd_kv; /* opaque handle */

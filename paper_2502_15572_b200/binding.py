@@ -556,11 +556,15 @@ def draft_mask(n: int, L: int, device="cuda"):
 
 
 class KvBatch:
-    """A batch of chunks (``dresd_kv_batch``): int32 CUDA tensors, borrowed; their contents are read when a call runs."""
+    """A batch of chunks (``dresd_kv_batch``): int32 CUDA tensors of one device, borrowed; their contents are read when a
+    call runs."""
 
     def __init__(self, page_table, ctx, start, rows: int, max_chunk: int = 0):
         torch = _torch()
+        self.device_index = page_table.get_device()           # -1: not a CUDA tensor
         for name, t, dims in (("page_table", page_table, 2), ("ctx", ctx, 1), ("start", start, 1)):
+            if t.get_device() != self.device_index:
+                raise DresdError(-1, f"{name} is on another device than page_table")
             if not t.is_cuda or t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous():
                 raise DresdError(-1, f"{name} must be a contiguous int32 CUDA tensor with {dims} dimension(s)")
         B, width = page_table.shape
@@ -572,7 +576,8 @@ class KvBatch:
 
 
 class KvCache:
-    """A paged key/value cache on the current CUDA device; tensors passed in are borrowed.
+    """A paged key/value cache on the current CUDA device; tensors passed in are borrowed.  All tensors, the batches' too, are
+    of that device, which has to be the current one in every call.
 
     k_pages, v_pages: [layers][num_pages][kv_heads][page_size][head_dim] in `dtype`, or uint8 with
     k_exps, v_exps: uint8 [layers][num_pages][kv_heads][page_size] (8-bit rows)."""
@@ -594,19 +599,27 @@ class KvCache:
             if t is not None and (not t.is_cuda or t.dtype != torch.uint8 or t.shape != k_pages.shape[:4] or
                                   not t.is_contiguous()):
                 raise DresdError(-1, f"{name} must be a contiguous uint8 CUDA tensor of shape {tuple(k_pages.shape[:4])}")
+        self.device_index = k_pages.get_device()
+        for name, t in (("v_pages", v_pages), ("k_exps", k_exps), ("v_exps", v_exps)):
+            if t is not None and t.get_device() != self.device_index:
+                raise DresdError(-1, f"{name} is on another device than k_pages")
         self.dtype = dtype
         self.k_pages, self.v_pages, self.k_exps, self.v_exps = k_pages, v_pages, k_exps, v_exps   # keep alive
         self.layers, self.num_pages, self.kv_heads, self.page_size, self.head_dim = k_pages.shape
-        self.device_index = k_pages.device.index
         ptr = lambda t: None if t is None else t.data_ptr()
         self.handle = dresd_kv_create(k_pages.data_ptr(), v_pages.data_ptr(), ptr(k_exps), ptr(v_exps), self.layers,
                                       self.num_pages, self.kv_heads, self.page_size, self.head_dim, DTYPE_CODE[dtype])
 
+    def _batch(self, batch):
+        if batch.device_index != self.device_index:
+            raise DresdError(-1, f"the batch is on cuda:{batch.device_index}, the cache on cuda:{self.device_index}")
+
     def _rows(self, name, t, batch, heads=None):
         """Distances of rows and heads of a [rows][heads][head_dim] tensor."""
+        self._batch(batch)
         shape = t.shape
-        if t.dtype != self.torch_dtype or not t.is_cuda or len(shape) != 3:
-            raise DresdError(-1, f"{name} must be a {self.torch_dtype} CUDA tensor with 3 dimensions")
+        if t.dtype != self.torch_dtype or t.get_device() != self.device_index or len(shape) != 3:
+            raise DresdError(-1, f"{name} must be a {self.torch_dtype} tensor with 3 dimensions on cuda:{self.device_index}")
         if shape[0] != batch.rows or shape[2] != self.head_dim or (heads is not None and shape[1] != heads):
             raise DresdError(-1, f"{name} has shape {tuple(shape)}")
         row, head, last = t.stride()
@@ -624,6 +637,7 @@ class KvCache:
     def read(self, layer: int, batch: KvBatch, out=None, stream=None):
         """Returns ``(k, v)``, dense [rows][kv_heads][head_dim], of the positions ctx[b] .. of every sequence."""
         torch = _torch()
+        self._batch(batch)
         shape = (batch.rows, self.kv_heads, self.head_dim)
         if out is None:
             with _allocated_on(stream):
@@ -631,8 +645,8 @@ class KvCache:
         else:
             k, v = out
             for name, t in (("out k", k), ("out v", v)):
-                if t.shape != shape or t.dtype != self.torch_dtype or not t.is_cuda or not t.is_contiguous():
-                    raise DresdError(-1, f"{name} must be a contiguous {self.torch_dtype} CUDA tensor of shape {shape}")
+                if t.shape != shape or t.dtype != self.torch_dtype or t.get_device() != self.device_index or not t.is_contiguous():
+                    raise DresdError(-1, f"{name} must be a contiguous {self.torch_dtype} tensor of shape {shape} on cuda:{self.device_index}")
         dresd_kv_read(self.handle, layer, batch.c, k.data_ptr(), v.data_ptr(), _raw_stream(self.device_index, stream))
         return k, v
 
@@ -646,15 +660,16 @@ class KvCache:
         if out is None:
             with _allocated_on(stream):
                 out = torch.empty((rows, heads, d), dtype=self.torch_dtype, device=self.k_pages.device)
-        elif out.shape != q.shape or out.dtype != q.dtype or not out.is_cuda or not out.is_contiguous():
-            raise DresdError(-1, f"out must be a contiguous {q.dtype} CUDA tensor of shape {tuple(q.shape)}")
-        if lse is not None and (lse.shape != (rows, heads) or lse.dtype != torch.float32 or not lse.is_cuda or
+        elif out.shape != q.shape or out.dtype != q.dtype or out.get_device() != self.device_index or not out.is_contiguous():
+            raise DresdError(-1, f"out must be a contiguous {q.dtype} tensor of shape {tuple(q.shape)} on cuda:{self.device_index}")
+        if lse is not None and (lse.shape != (rows, heads) or lse.dtype != torch.float32 or lse.get_device() != self.device_index or
                                 not lse.is_contiguous()):
-            raise DresdError(-1, f"lse must be a contiguous float32 CUDA tensor of shape {(rows, heads)}")
+            raise DresdError(-1, f"lse must be a contiguous float32 tensor of shape {(rows, heads)} on cuda:{self.device_index}")
         mask_ptr, words = None, 0
         if mask is not None:
-            if mask.dtype != torch.int32 or not mask.is_cuda or mask.dim() != 2 or mask.shape[0] != rows or not mask.is_contiguous():
-                raise DresdError(-1, f"mask must be a contiguous int32 CUDA tensor of {rows} rows")
+            if mask.dtype != torch.int32 or mask.get_device() != self.device_index or mask.dim() != 2 or mask.shape[0] != rows or \
+                    not mask.is_contiguous():
+                raise DresdError(-1, f"mask must be a contiguous int32 tensor of {rows} rows on cuda:{self.device_index}")
             mask_ptr, words = mask.data_ptr(), mask.shape[1]
         dresd_kv_attend(self.handle, layer, batch.c, q.data_ptr(), q_row, q_head, heads,
                         d ** -0.5 if scale is None else scale, mask_ptr, words, out.data_ptr(),
@@ -664,9 +679,10 @@ class KvCache:
     def keep_draft(self, batch: KvBatch, best, length, n: int, L: int, stream=None):
         """Moves the accepted drafts' tokens into place in every layer (best, length: of dresd_drafts_accept)."""
         int32 = _torch().int32
+        self._batch(batch)
         for name, t in (("best", best), ("length", length)):
-            if t.dtype != int32 or not t.is_cuda or t.shape != (batch.B,) or not t.is_contiguous():
-                raise DresdError(-1, f"{name} must be a contiguous int32 CUDA tensor of {batch.B} entries")
+            if t.dtype != int32 or t.get_device() != self.device_index or t.shape != (batch.B,) or not t.is_contiguous():
+                raise DresdError(-1, f"{name} must be a contiguous int32 tensor of {batch.B} entries on cuda:{self.device_index}")
         dresd_kv_keep_draft(self.handle, batch.c, best.data_ptr(), length.data_ptr(), n, L,
                             _raw_stream(self.device_index, stream))
 

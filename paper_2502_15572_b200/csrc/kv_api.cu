@@ -32,7 +32,8 @@ constexpr uint32_t kKvMagic = 0xD2E5D0C4u;
 constexpr int kMaxKvBatch = 65535;
 constexpr int kMaxGroup = 64;
 
-bool is_device_ptr(const void *p)
+// Memory of `device` (a cache's kernels must not be given another GPU's), or managed memory.
+bool is_device_ptr(const void *p, int device)
 {
     if (!p) return false;
     cudaPointerAttributes at;
@@ -40,7 +41,7 @@ bool is_device_ptr(const void *p)
         cudaGetLastError();
         return false;
     }
-    return at.type == cudaMemoryTypeDevice || at.type == cudaMemoryTypeManaged;
+    return (at.type == cudaMemoryTypeDevice && at.device == device) || at.type == cudaMemoryTypeManaged;
 }
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
@@ -129,15 +130,17 @@ dresd_status check_call(dresd_kv *kv, int layer, const dresd_kv_batch *b, bool w
     out->width = b->table_width;
     out->rows = b->rows;
     if (b->B == 0 || (whole && b->rows == 0)) return DRESD_OK;
-    if (!is_device_ptr(b->page_table) || !is_device_ptr(b->ctx) || (whole && !is_device_ptr(b->start)))
-        return fail(DRESD_ERR_INVALID, "page_table/ctx/start must be device pointers");
+    if (!is_device_ptr(b->page_table, dev) || !is_device_ptr(b->ctx, dev) || (whole && !is_device_ptr(b->start, dev)))
+        return fail(DRESD_ERR_INVALID, "page_table/ctx/start must be pointers of the cache's device");
     return DRESD_OK;
 }
 
 // Rows of `heads` heads at the given distances: 16-byte loads.
-dresd_status check_rows(const char *name, const void *p, int rows, long long row, long long head, int heads, int d)
+dresd_status check_rows(const dresd_kv *kv, const char *name, const void *p, int rows, long long row, long long head, int heads)
 {
-    if (!is_device_ptr(p) || !aligned16(p)) return fail(DRESD_ERR_INVALID, "%s must be a 16-byte aligned device pointer", name);
+    const int d = kv->args.d;
+    if (!is_device_ptr(p, kv->device) || !aligned16(p))
+        return fail(DRESD_ERR_INVALID, "%s must be a 16-byte aligned pointer of the cache's device", name);
     if (row < 0 || head < 0 || row % 8 != 0 || head % 8 != 0)
         return fail(DRESD_ERR_INVALID, "%s: the distances of rows and heads must be multiples of 8 elements", name);
     if ((heads > 1 && (head < d || head >= 1LL << 38)) || (rows > 1 && (row < d || row >= 1LL << 38)))
@@ -169,8 +172,10 @@ dresd_status dresd_kv_create(void *k_pages, void *v_pages, uint8_t *k_exps, uint
         return fail(DRESD_ERR_UNSUPPORTED, "the cache has more than 2^31 - 1 rows");
     if (!aligned16(k_pages) || !aligned16(v_pages)) return fail(DRESD_ERR_INVALID, "pages not 16-byte aligned");
     if (k_exps && (!aligned16(k_exps) || !aligned16(v_exps))) return fail(DRESD_ERR_INVALID, "exponents not 16-byte aligned");
-    if (!is_device_ptr(k_pages) || !is_device_ptr(v_pages) || (k_exps && (!is_device_ptr(k_exps) || !is_device_ptr(v_exps))))
-        return fail(DRESD_ERR_INVALID, "k_pages/v_pages/k_exps/v_exps must be device pointers");
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) cudaGetLastError();       // then no pointer is one of it
+    if (!is_device_ptr(k_pages, dev) || !is_device_ptr(v_pages, dev) || (k_exps && (!is_device_ptr(k_exps, dev) || !is_device_ptr(v_exps, dev))))
+        return fail(DRESD_ERR_INVALID, "k_pages/v_pages/k_exps/v_exps must be pointers of the current device");
     dresd_kv *kv = new (std::nothrow) dresd_kv();
     if (!kv) return fail(DRESD_ERR_ALLOC, "host allocation failed");
     kv->magic = kKvMagic;
@@ -185,8 +190,8 @@ dresd_status dresd_kv_create(void *k_pages, void *v_pages, uint8_t *k_exps, uint
     a.d = head_dim;
     a.dtype = (int)dtype;
     a.num_pages = (int)num_pages;
-    cudaError_t e = cudaGetDevice(&kv->device);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&kv->sms, cudaDevAttrMultiProcessorCount, kv->device);
+    kv->device = dev;
+    cudaError_t e = cudaDeviceGetAttribute(&kv->sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) {
         free_kv(kv);
         return fail_cuda(e, "device query");
@@ -239,8 +244,8 @@ dresd_status dresd_kv_append(dresd_kv *kv, int layer, const dresd_kv_batch *batc
     if (st != DRESD_OK) return st;
     kv->last_launches = 0;
     if (a.B == 0 || a.rows == 0) return DRESD_OK;
-    if ((st = check_rows("k", k, a.rows, k_row, k_head, a.heads, a.d)) != DRESD_OK) return st;
-    if ((st = check_rows("v", v, a.rows, v_row, v_head, a.heads, a.d)) != DRESD_OK) return st;
+    if ((st = check_rows(kv, "k", k, a.rows, k_row, k_head, a.heads)) != DRESD_OK) return st;
+    if ((st = check_rows(kv, "v", v, a.rows, v_row, v_head, a.heads)) != DRESD_OK) return st;
     kv->last_stream = static_cast<cudaStream_t>(stream);
     const cudaError_t e = launch_kv_append(a, k, k_row, k_head, v, v_row, v_head, kv->last_stream);
     if (e != cudaSuccess) return fail_cuda(e, "kv_append launch");
@@ -255,8 +260,8 @@ dresd_status dresd_kv_read(dresd_kv *kv, int layer, const dresd_kv_batch *batch,
     if (st != DRESD_OK) return st;
     kv->last_launches = 0;
     if (a.B == 0 || a.rows == 0) return DRESD_OK;
-    if (!is_device_ptr(out_k) || !is_device_ptr(out_v) || !aligned16(out_k) || !aligned16(out_v))
-        return fail(DRESD_ERR_INVALID, "out_k/out_v must be 16-byte aligned device pointers");
+    if (!is_device_ptr(out_k, kv->device) || !is_device_ptr(out_v, kv->device) || !aligned16(out_k) || !aligned16(out_v))
+        return fail(DRESD_ERR_INVALID, "out_k/out_v must be 16-byte aligned pointers of the cache's device");
     kv->last_stream = static_cast<cudaStream_t>(stream);
     const cudaError_t e = launch_kv_read(a, out_k, out_v, kv->last_stream);
     if (e != cudaSuccess) return fail_cuda(e, "kv_read launch");
@@ -281,10 +286,10 @@ dresd_status dresd_kv_attend(dresd_kv *kv, int layer, const dresd_kv_batch *batc
         return fail(DRESD_ERR_UNSUPPORTED, "rows x heads per key/value head exceed 2^31 - 1025");
     kv->last_launches = 0;
     if (a.kv.B == 0 || a.kv.rows == 0) return DRESD_OK;
-    if ((st = check_rows("q", q, a.kv.rows, q_row, q_head, heads, a.kv.d)) != DRESD_OK) return st;
-    if (!is_device_ptr(out) || !aligned16(out) || (out_lse && !is_device_ptr(out_lse)))
-        return fail(DRESD_ERR_INVALID, "out must be a 16-byte aligned device pointer, out_lse a device pointer or NULL");
-    if (mask && !is_device_ptr(mask)) return fail(DRESD_ERR_INVALID, "mask must be a device pointer");
+    if ((st = check_rows(kv, "q", q, a.kv.rows, q_row, q_head, heads)) != DRESD_OK) return st;
+    if (!is_device_ptr(out, kv->device) || !aligned16(out) || (out_lse && !is_device_ptr(out_lse, kv->device)))
+        return fail(DRESD_ERR_INVALID, "out must be a 16-byte aligned pointer of the cache's device, out_lse one of it or NULL");
+    if (mask && !is_device_ptr(mask, kv->device)) return fail(DRESD_ERR_INVALID, "mask must be a pointer of the cache's device");
     a.q = q;
     a.q_row = q_row;
     a.q_head = q_head;
@@ -334,7 +339,8 @@ dresd_status dresd_kv_keep_draft(dresd_kv *kv, const dresd_kv_batch *batch, cons
     if (L > 65536) return fail(DRESD_ERR_UNSUPPORTED, "L = %d exceeds 65536", L);
     kv->last_launches = 0;
     if (a.B == 0) return DRESD_OK;
-    if (!is_device_ptr(best) || !is_device_ptr(length)) return fail(DRESD_ERR_INVALID, "best/length must be device pointers");
+    if (!is_device_ptr(best, kv->device) || !is_device_ptr(length, kv->device))
+        return fail(DRESD_ERR_INVALID, "best/length must be pointers of the cache's device");
     kv->last_stream = static_cast<cudaStream_t>(stream);
     const cudaError_t e = launch_kv_keep_draft(a, best, length, n, L, kv->last_stream);
     if (e != cudaSuccess) return fail_cuda(e, "kv_keep_draft launch");

@@ -420,14 +420,19 @@ cudaError_t launch_workers(void (*kernel)(KArgs...), int threads, int smem, int 
     cfg.attrs = attr;
     cfg.numAttrs = ctas > 1 ? 2 : 1;
     if (ctas > 1) {
-        static int held[kMaxCluster + 1] = {};              // per kernel type; every kernel of a type fills an SM
-        if (held[ctas] == 0) {
-            int n = 0;
-            const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+        // by device and kernel type; every kernel of a type fills an SM
+        constexpr int kDevices = 16;                        // of more than these it is asked every time
+        static int held[kDevices][kMaxCluster + 1] = {};
+        int device = 0;
+        cudaError_t e = cudaGetDevice(&device);
+        int n = e == cudaSuccess && device < kDevices ? held[device][ctas] : 0;
+        if (n == 0) {
+            if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
             if (e != cudaSuccess) return e;
-            held[ctas] = n > 0 ? n : 1;
+            if (n < 1) n = 1;
+            if (device < kDevices) held[device][ctas] = n;
         }
-        if ((int)cfg.gridDim.x > held[ctas] * ctas) cfg.gridDim.x = held[ctas] * ctas;
+        if ((int)cfg.gridDim.x > n * ctas) cfg.gridDim.x = n * ctas;
     }
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }

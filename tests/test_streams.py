@@ -78,3 +78,56 @@ def test_results_on_another_stream_while_the_current_one_is_busy():
         torch.cuda.synchronize()
         assert torch.equal(got, right)
     case.cache.status()
+
+
+class Tensor:
+    """Stands for a CUDA tensor of device `at`."""
+    is_cuda = True
+
+    def __init__(self, at, dtype, *shape):
+        self.at, self.dtype, self.shape = at, dtype, torch.Size(shape)
+        self.device = torch.device("cuda", at)
+
+    def get_device(self):
+        return self.at
+
+    def is_contiguous(self):
+        return True
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self):
+        return tuple(torch.empty(self.shape, device="meta").stride())
+
+    def data_ptr(self):
+        return 4096
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    for name in ("dresd_kv_attend", "dresd_kv_read", "dresd_kv_append", "dresd_kv_keep_draft", "_raw_stream"):
+        monkeypatch.setattr(binding, name, lambda *a: 0)
+    monkeypatch.setattr(binding, "dresd_kv_create", lambda *a: 0)
+    i32, f16, u8, f32 = torch.int32, torch.float16, torch.uint8, torch.float32
+    batch = lambda *at: binding.KvBatch(Tensor(at[0], i32, 2, 4), Tensor(at[1], i32, 2), Tensor(at[2], i32, 3), 5)
+    pages = lambda at, dtype=f16: Tensor(at, dtype, 1, 9, 2, 16, 64)
+    cache = binding.KvCache(pages(0), pages(0), "f16")
+    here, there = batch(0, 0, 0), batch(1, 1, 1)
+    k, q, best = (lambda at: Tensor(at, f16, 5, 2, 64)), (lambda at: Tensor(at, f16, 5, 4, 64)), (lambda at: Tensor(at, i32, 2))
+    good = [lambda: cache.append(0, k(0), k(0), here), lambda: cache.read(0, here, out=(k(0), k(0))),
+            lambda: cache.attend(0, q(0), here, out=q(0), lse=Tensor(0, f32, 5, 4), mask=Tensor(0, i32, 5, 1)),
+            lambda: cache.keep_draft(here, best(0), best(0), 2, 2)]
+    bad = [lambda: batch(0, 1, 0), lambda: batch(0, 0, 1), lambda: binding.KvCache(pages(0), pages(1), "f16"),
+           lambda: binding.KvCache(pages(0, u8), pages(0, u8), "f16", Tensor(1, u8, 1, 9, 2, 16), Tensor(0, u8, 1, 9, 2, 16)),
+           lambda: cache.append(0, k(1), k(0), here), lambda: cache.append(0, k(0), k(1), here), lambda: cache.append(0, k(0), k(0), there),
+           lambda: cache.read(0, there, out=(k(0), k(0))), lambda: cache.read(0, here, out=(k(0), k(1))),
+           lambda: cache.attend(0, q(1), here, out=q(0)), lambda: cache.attend(0, q(0), there, out=q(0)), lambda: cache.attend(0, q(0), here, out=q(1)),
+           lambda: cache.attend(0, q(0), here, out=q(0), lse=Tensor(1, f32, 5, 4)),
+           lambda: cache.attend(0, q(0), here, out=q(0), mask=Tensor(1, i32, 5, 1)),
+           lambda: cache.keep_draft(there, best(0), best(0), 2, 2), lambda: cache.keep_draft(here, best(1), best(0), 2, 2)]
+    for call in good:
+        call()
+    for i, call in enumerate(bad):
+        with pytest.raises(binding.DresdError) as e:
+            call()
+        assert e.value.status == -1, i
