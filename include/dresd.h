@@ -464,18 +464,21 @@ dresd_status dresd_store_status(dresd_store *store);
  * -DDRESD_DEBUG_BOUNDS (the Python binding loads it when the environment variable
  * DRESD_DEBUG is 1): every global index and pipeline-ring slot that the kernels form -- stage
  * slots and tile coordinates of the loaders, rows of the first-token column, entries of the
- * window table, positions in the candidate array, the row ids of candidates and winners -- is
- * checked where it is formed; a violation skips the access and records its site in the status
- * word, and dresd_store_status() then returns DRESD_ERR_INTERNAL with the site number in the
+ * window table, positions in the candidate array, the row ids of candidates and winners; of the
+ * paged cache the entries of the page table and of the lengths, rows of the pool, of queries, masks and results, places of
+ * the parts -- is checked where it is formed; a violation skips the access and records its site in the status
+ * word, and dresd_store_status() (dresd_kv_status()) then returns DRESD_ERR_INTERNAL with the site number in the
  * message.  It stands in for a memory checker on systems where none can be run; it is a few per
  * cent slower and otherwise computes the same results.
  *   dresd_debug_build()            1 in the debug build, 0 in the release build.
  *   dresd_store_debug_selftest()   debug build: one thread fails check 7 on purpose (no access is
  *                                  attempted), so that the reporting path can be seen to work;
  *                                  release build: DRESD_ERR_UNSUPPORTED.
+ *   dresd_kv_debug_selftest()      the same for a cache.
  */
 int dresd_debug_build(void);
 dresd_status dresd_store_debug_selftest(dresd_store *store, void *stream);
+dresd_status dresd_kv_debug_selftest(dresd_kv *kv, void *stream);
 
 /*
  * Kernel-selection knobs for tests and measurements (set between calls).

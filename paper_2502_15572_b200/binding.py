@@ -36,7 +36,7 @@ EXPORTS = (
     "dresd_retrieve_quantised", "dresd_store_index_first_tokens", "dresd_merge_shards_packed",
     "dresd_noalloc_status", "dresd_debug_build", "dresd_store_debug_selftest",
     "dresd_kv_create", "dresd_kv_destroy", "dresd_kv_append", "dresd_kv_read", "dresd_kv_attend",
-    "dresd_kv_keep_draft", "dresd_kv_status", "dresd_kv_set_option", "dresd_kv_last_launches",
+    "dresd_kv_keep_draft", "dresd_kv_status", "dresd_kv_set_option", "dresd_kv_last_launches", "dresd_kv_debug_selftest",
 )
 
 
@@ -144,6 +144,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.dresd_kv_status.argtypes = [vp]
     lib.dresd_kv_set_option.restype = i32
     lib.dresd_kv_set_option.argtypes = [vp, c.c_char_p, i32]
+    lib.dresd_kv_debug_selftest.restype = i32
+    lib.dresd_kv_debug_selftest.argtypes = [vp, vp]
     lib.dresd_kv_last_launches.restype = i32
     lib.dresd_kv_last_launches.argtypes = [vp]
     if path is None:
@@ -348,6 +350,10 @@ def dresd_kv_status(kv: int) -> None:
 
 def dresd_kv_set_option(kv: int, name: str, value: int) -> None:
     _check(load().dresd_kv_set_option(kv, name.encode(), value))
+
+
+def dresd_kv_debug_selftest(kv: int, stream: int = 0) -> None:
+    _check(load().dresd_kv_debug_selftest(kv, stream))
 
 
 def dresd_kv_last_launches(kv: int) -> int:

@@ -31,7 +31,7 @@ __device__ __forceinline__ bool place_of(const KvArgs &a, int row, int &page, in
     if (row < first || row >= __ldg(a.start + lo + 1)) return false;
     const long long p = (long long)max(__ldg(a.ctx + lo), 0) + (row - first);
     const long long i = p >> a.page_shift;
-    if (i >= a.width) return false;
+    if (i >= a.width || !debug_check(lo < a.B && i >= 0, a.status, 51)) return false;
     page = __ldg(a.table + (long long)lo * a.width + i);
     off = (int)(p & ((1 << a.page_shift) - 1));
     return page >= 0 && page < a.num_pages;
@@ -76,6 +76,7 @@ append_kernel(const KvArgs a, const T *__restrict__ k, long long k_row, long lon
     for (int i = 0; i < kHeads; ++i) {
         if (h0 + i >= a.heads) break;
         const long long r = kv_row(a, a.layer, page, h0 + i, off);
+        if (!debug_check(r >= 0 && r < kv_rows(a), a.status, 52)) break;       // the same for every lane of the row
         if constexpr (!Q8) {
             reinterpret_cast<uint4 *>(is_v ? a.v : a.k)[r * kLanes + piece] = x[i];
         } else {
@@ -120,7 +121,8 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const KvArgs a, T *__res
     const bool is_v = blockIdx.y != 0;
     uint4 *dst = reinterpret_cast<uint4 *>(is_v ? out_v : out_k) + ((long long)row * a.heads + h0) * kLanes + piece;
     int page = 0, off = 0;
-    const bool there = place_of(a, row, page, off);
+    const bool there = place_of(a, row, page, off) &&
+                       debug_check(kv_row(a, a.layer, page, min(h0 + kHeads, a.heads) - 1, off) < kv_rows(a), a.status, 53);
     const void *cache = is_v ? a.v : a.k;
     if constexpr (!Q8) {
         uint4 x[kHeads];
@@ -190,6 +192,7 @@ keep_kernel(const KvArgs a, const int32_t *__restrict__ best, const int32_t *__r
         const int pf = __ldg(table + (q >> a.page_shift)), pt = __ldg(table + (p >> a.page_shift));
         if (pf < 0 || pf >= a.num_pages || pt < 0 || pt >= a.num_pages) continue;
         const long long from = kv_row(a, layer, pf, head, (int)(q & in_page)), to = kv_row(a, layer, pt, head, (int)(p & in_page));
+        if (!debug_check(from >= 0 && from < kv_rows(a) && to >= 0 && to < kv_rows(a) && pt >= 0, a.status, 54)) continue;
         cache[(to << lanes_shift) + piece] = cache[(from << lanes_shift) + piece];
         if (exps && piece == 0) exps[to] = exps[from];
     }

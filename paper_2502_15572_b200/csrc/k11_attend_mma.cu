@@ -111,6 +111,7 @@ struct Shared {
 // rows' weight sums.
 __device__ __forceinline__ float *part_slot(const AttendArgs &a, int worker, int slot, int rows)
 {
+    if (!debug_check(worker >= 0 && worker < gridDim.x * a.groups && (unsigned)slot < 2, a.kv.status, 66)) worker = slot = 0;
     return a.part + ((size_t)worker * 2 + slot) * rows * (a.kv.d + 2);
 }
 
@@ -199,7 +200,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 
     // ---- the ring.  The fetching side is up to kStages tiles ahead of the using side, in the next segment if need be.
     const int beyond = (int)min((long long)a.kv.layers * a.kv.num_pages * a.kv.heads << a.kv.page_shift, 2147483647LL);
-    int fetched = 0, f_job = -1, f_tile = -step;           // the last tile that was looked up, of segment f_job
+    int fetched = 0, used = 0, f_job = -1, f_tile = -step;           // the last tile that was looked up, of segment f_job
     // The next tile: its place in the pool but for the page, whose number (loaded here, used when the copy is issued) may be
     // anything.  pending = false: none known yet (up to the segment after `i`).
     bool pending = false;
@@ -225,12 +226,13 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         pending = true;
         off = p & in_page;
         page = -1;
-        if (p < f_total) page = __ldg(f_table + (p >> a.kv.page_shift));
+        if (p < f_total && debug_check(p >= 0 && (p >> a.kv.page_shift) < a.kv.width, a.kv.status, 61)) page = __ldg(f_table + (p >> a.kv.page_shift));
     };
     auto fetch = [&] {                                      // lane 0
         const int s = fetched % kStages;
         // beyond the end or outside the pool: zeros are loaded.  (The pool has fewer than 2^31 rows.)
-        const int row = (unsigned)page < (unsigned)a.kv.num_pages ? (((layer_pages + page) * a.kv.heads + f_head) << a.kv.page_shift) + off : beyond;
+        int row = (unsigned)page < (unsigned)a.kv.num_pages ? (((layer_pages + page) * a.kv.heads + f_head) << a.kv.page_shift) + off : beyond;
+        if (!debug_check(row >= 0 && row <= beyond && (row == beyond || row % kTile == 0) && fetched - used < kStages, a.kv.status, 62)) row = beyond;
         uint64_t *bar = &sh.full[warp][s];
         uint8_t *dst = sh.ring[warp][s];
         mbar_arrive_expect_tx(bar, (uint32_t)(Geo::kStage + (Q8 ? 2 * kTile : 0)));
@@ -253,7 +255,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         look_ahead(0);
     }
 
-    int used = 0, joins = 0;
+    int joins = 0;
     bool dead = false;
     for (int i = 0;; ++i) {
         const Job &w = jobs[i & 3];
@@ -272,7 +274,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int r = seg.rt * kRows + nt * 8 + g, tok = a.by_group.div(r);
-            const bool ok = nt * 8 + g < rows;
+            const bool ok = nt * 8 + g < rows && debug_check(ch.row0 + tok < a.kv.rows && seg.head < a.kv.heads, a.kv.status, 63);
             const T *src = static_cast<const T *>(a.q) + (long long)(ch.row0 + (ok ? tok : 0)) * a.q_row +
                            (seg.head * a.group + (ok ? r - tok * a.group : 0)) * a.q_head;
 #pragma unroll
@@ -406,7 +408,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                             const int p = p0 + 8 * j + place(g), e = p - ch.ctx;
                             bool seen = p < ch.total;
                             if (seen && e >= 0)
-                                seen = a.mask ? (e >> 5) < a.mask_words && (a.mask[(long long)(ch.row0 + tok) * a.mask_words + (e >> 5)] >> (e & 31) & 1)
+                                seen = a.mask ? (e >> 5) < a.mask_words && debug_check(ch.row0 + tok < a.kv.rows, a.kv.status, 64) && (a.mask[(long long)(ch.row0 + tok) * a.mask_words + (e >> 5)] >> (e & 31) & 1)
                                               : e <= tok;
                             if (!seen) y = -INFINITY;
                         }
@@ -603,6 +605,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             const float inv = ll > 0.f ? 1.f / ll : ll == 0.f ? 0.f : ll;              // a NaN sum stays one
             const int rr = seg.rt * kRows + r, tok = a.by_group.div(rr);
             const long long at = (long long)(ch.row0 + tok) * heads + seg.head * a.group + rr - tok * a.group;
+            if (!debug_check(at >= 0 && at < (long long)a.kv.rows * heads, a.kv.status, 65)) return;
             *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + at * D + e) =
                 make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
             if (a.lse && e == 0) a.lse[at] = ((mm > -INFINITY ? mm - (Q8 ? 0.f : kLift) : 0.f) + log2f(ll)) * 0.69314718055994531f;
@@ -680,7 +683,8 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         if (split) {
             __threadfence();
             sync();
-            if (g_tid == 0) sh.ticket[group] = atomicAdd(a.tickets + seg.c0 * a.ctas + rank, 1u);
+            if (g_tid == 0 && debug_check(seg.c0 >= 0 && seg.c0 * a.ctas + rank < gridDim.x * a.groups, a.kv.status, 67))
+                sh.ticket[group] = atomicAdd(a.tickets + seg.c0 * a.ctas + rank, 1u);
             sync();
             if (sh.ticket[group] == (unsigned)(seg.c1 - seg.c0)) {                      // the last of them: join the parts in order
                 __threadfence();

@@ -121,9 +121,8 @@ struct Job {
         }
     }
     __device__ __forceinline__ int tile(int j) const { return t0 + (one ? (j >> 1) * step + (j & 1) : j); }
-    // Places of key tile j and value tile j in the order in which tiles are loaded and consumed: K0 V0 K1 V1 ... for two
-    // row tiles, K0 K1 V0 K2 V1 K3 ... for one.
-    __device__ __forceinline__ int k_place(int j) const { return one ? (j < 2 ? j : 2 * j - 1) : 2 * j; }
+    // Place of value tile j in the order in which tiles are loaded and consumed: K0 V0 K1 V1 ... for two row tiles, K0 K1 V0
+    // K2 V1 K3 ... for one.
     __device__ __forceinline__ int v_place(int j) const { return one ? (j == nt - 1 ? 2 * nt - 1 : 2 + 2 * j) : 2 * j + 1; }
 };
 
@@ -274,6 +273,7 @@ __device__ __noinline__ void repair(const AttendArgs &a, const Job &job, int st,
     const int head = job.seg.head, heads = a.group, in_page = (1 << a.kv.page_shift) - 1;
     const T *q = static_cast<const T *>(a.q) + (long long)(c.row0 + tok) * a.q_row + (long long)(head * heads + row - a.by_group.div(row) * heads) * a.q_head;
     auto row_of = [&](int p) {
+        if (!debug_check(p >= 0 && (p >> a.kv.page_shift) < a.kv.width, a.kv.status, 78)) p = 0;
         const int page = a.kv.table[(long long)job.seg.b * a.kv.width + (p >> a.kv.page_shift)];
         return kv_row(a.kv, a.kv.layer, page < 0 || page >= a.kv.num_pages ? 0 : page, head, p & in_page);
     };
@@ -414,12 +414,13 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 auto row_of = [&](int j) {
                     const int p = w.tile(j) * kTile + (pg << a.kv.page_shift);
                     int page = -1;
-                    if (j < w.nt && pg < per && p < total) page = __ldg(table + (p >> a.kv.page_shift));
+                    if (j < w.nt && pg < per && p < total && debug_check(p >= 0 && (p >> a.kv.page_shift) < a.kv.width, a.kv.status, 71)) page = __ldg(table + (p >> a.kv.page_shift));
                     if (page < 0 || page >= a.kv.num_pages) return beyond;
                     return (int)kv_row(a.kv, a.kv.layer, page, head, 0);
                 };
                 auto load = [&](bool is_v, int row) {
                     const int s = issued % kRing;
+                    if (!debug_check(row >= 0 && row <= beyond && (row == beyond || (row & ((1 << a.kv.page_shift) - 1)) == 0), a.kv.status, 72)) row = beyond;
                     if (issued >= kRing && !mbar_wait(&empty[s], ((issued / kRing) - 1) & 1, wl)) ok = false;
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     if (!ok) return;
@@ -590,7 +591,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                     }
                     mbar_arrive(&sh.job_full[i & 1]);
                     if (!more) break;
-                    const int tiles = w.one ? 1 : 2, y = w.seg.head * a.group, z = plan.c.row0 + w.seg.rt * (int)a.by_rows.d;
+                    const int tiles = w.one ? 1 : 2, y = w.seg.head * a.group;
+                    int z = plan.c.row0 + w.seg.rt * (int)a.by_rows.d;
+                    if (!debug_check(z >= 0 && z < a.kv.rows && w.seg.head < a.kv.heads, a.kv.status, 73)) z = 0;
 #pragma unroll 1
                     for (int st = 0; st < tiles && ok; ++st) {
                         int &uses = st ? uses1 : uses0;
@@ -669,7 +672,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 auto seen = [&](int p) {
                     const int n = min(max(limit - p, 0), 32);
                     uint32_t see = n == 32 ? 0xFFFFFFFFu : (1u << n) - 1u;
-                    if (a.mask && p + 32 > c.ctx) {
+                    if (a.mask && p + 32 > c.ctx && debug_check(c.row0 + min(tok, c.len - 1) < a.kv.rows && p - c.ctx > -32, a.kv.status, 74)) {
                         const uint32_t *mask = a.mask + (long long)(c.row0 + min(tok, c.len - 1)) * a.mask_words;
                         const int j0 = p - c.ctx;             // place in the chunk of bit 0; context below 0
                         const int w0 = j0 >> 5;               // floor; -1 at the least
@@ -838,13 +841,13 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             float *part = a.part + ((size_t)blockIdx.x * 2 + seg.slot) * part_floats(D);
             float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;       // a NaN sum stays one
             auto put = [&](int o, const float *x) {            // an octet of the result
-                if (valid)
+                if (valid && debug_check(at >= 0 && at < (long long)a.kv.rows * heads && o < D / 8, a.kv.status, 75))
                     reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + at * D)[o] =
                         make_uint4(pack2<T>(x[0] * inv, x[1] * inv), pack2<T>(x[2] * inv, x[3] * inv), pack2<T>(x[4] * inv, x[5] * inv),
                                    pack2<T>(x[6] * inv, x[7] * inv));
             };
             auto put_part = [&](int o, const float *x) {
-                if (!valid) return;
+                if (!valid || !debug_check((unsigned)seg.slot < 2 && o < D / 8, a.kv.status, 76)) return;
                 float4 *dst = reinterpret_cast<float4 *>(part) + (size_t)(2 * o) * kPartRows + prow;
                 __stcg(dst, make_float4(x[0], x[1], x[2], x[3]));
                 __stcg(dst + kPartRows, make_float4(x[4], x[5], x[6], x[7]));
@@ -912,7 +915,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                             kept[2 * n * kTile + row] = y;
                             kept[(2 * n + 1) * kTile + row] = z;
                         } else {                               // its place there: 0 for the next CTA in the ring
-                            float4 *at = sent + (((rank - to - 1) & (a.ctas - 1)) * per + n) * 2 * kTile + row;
+                            const int place = (((rank - to - 1) & (a.ctas - 1)) * per + n) * 2 * kTile + row;
+                            if (!debug_check(place >= 0 && place + kTile < kTile * D / 4 / kMaxCtas * (kMaxCtas - 1), a.kv.status, 79)) continue;
+                            float4 *at = sent + place;
                             st_async(at, y, &sh.ready, to);
                             st_async(at + kTile, z, &sh.ready, to);
                         }
@@ -968,7 +973,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 __threadfence();
                 bar_sync(1, 512);
                 // CTAs of the same rank join the same octets
-                if (tid == 128) sh.ticket = atomicAdd(a.tickets + seg.c0 * a.ctas + rank, 1u);
+                if (tid == 128 && debug_check(seg.c0 >= 0 && (seg.c1 + 1) * a.ctas <= (int)gridDim.x, a.kv.status, 77))
+                    sh.ticket = atomicAdd(a.tickets + seg.c0 * a.ctas + rank, 1u);
                 bar_sync(1, 512);
                 done = *reinterpret_cast<volatile unsigned *>(&sh.ticket) == (unsigned)(seg.c1 - seg.c0);
                 if (done) {                                       // the last of the item's workers: join the parts in order

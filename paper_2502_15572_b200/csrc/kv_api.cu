@@ -362,7 +362,7 @@ dresd_status dresd_kv_status(dresd_kv *kv)
     if (e == cudaSuccess) e = cudaMemset(kv->tickets, 0, sizeof(unsigned int) * attend_mma_workers(kv->sms));
     if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
     if (e != cudaSuccess) return fail_cuda(e, "status reset");
-    if (word <= -1000) return fail(DRESD_ERR_INTERNAL, "bounds check %d failed inside a kernel", -1000 - word);
+    if (word <= -1000) return fail(DRESD_ERR_INTERNAL, "debug build: bounds check %d failed (an index or ring slot out of range)", -1000 - word);
     return fail(DRESD_ERR_TIMEOUT, "a device-side wait expired");
 }
 
@@ -385,6 +385,19 @@ dresd_status dresd_kv_set_option(dresd_kv *kv, const char *name, int value)
         return DRESD_OK;
     }
     return fail(DRESD_ERR_INVALID, "unknown option '%s'", name);
+}
+
+dresd_status dresd_kv_debug_selftest(dresd_kv *kv, void *stream)
+{
+    if (!valid(kv)) return fail(DRESD_ERR_INVALID, "cache handle is NULL or destroyed");
+#ifdef DRESD_DEBUG_BOUNDS
+    kv->last_stream = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = launch_debug_selftest(kv->args.status, kv->last_stream);
+    return e == cudaSuccess ? DRESD_OK : fail_cuda(e, "selftest launch");
+#else
+    (void)stream;
+    return fail(DRESD_ERR_UNSUPPORTED, "this is the release build: no bounds checks are compiled in");
+#endif
 }
 
 int dresd_kv_last_launches(const dresd_kv *kv) { return valid(kv) ? kv->last_launches : 0; }

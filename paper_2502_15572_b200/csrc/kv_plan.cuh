@@ -112,6 +112,7 @@ struct Chunk {
 };
 __device__ __forceinline__ Chunk kv_chunk(const KvArgs &a, int b)
 {
+    if (!debug_check(b >= 0 && b < a.B, a.status, 60)) b = 0;
     Chunk c;
     c.row0 = min(max(a.start[b], 0), a.rows);
     c.len = min(max(a.start[b + 1], c.row0), a.rows) - c.row0;
@@ -120,11 +121,13 @@ __device__ __forceinline__ Chunk kv_chunk(const KvArgs &a, int b)
     c.total = c.ctx + min(c.len, reach - c.ctx);
     return c;
 }
-// Row of (layer, page, head, offset) in the cache arrays; page numbers outside the pool count as `bad`.
+// Row of (layer, page, head, offset) in the cache arrays.
 __device__ __forceinline__ long long kv_row(const KvArgs &a, int layer, int page, int head, int off)
 {
     return (((((long long)layer * a.num_pages + page) * a.heads + head) << a.page_shift) + off);
 }
+// Rows of the cache arrays.
+__device__ __forceinline__ long long kv_rows(const KvArgs &a) { return (long long)a.layers * a.num_pages * a.heads << a.page_shift; }
 
 // ---- shared memory of the CTA and its cluster ------------------------------------------------------
 constexpr int kMaxCluster = 8;
