@@ -3,8 +3,8 @@
 // One pass with the running maximum, as in K11, but every key and value meets 128 or 256 rows, so the bound is the
 // tensor cores together with the exponentials (a 128 x 128 tile of scores is 512 cycles of each product at d = 128 and
 // 1024 cycles of the 16 exponentials per cycle that an SM has).  A CTA (one per SM) runs TWO STREAMS of tiles, each
-// with scores S, weights P and sums O of its own in TMEM (S 128 columns, P in S's place, O d columns), so that the
-// tensor cores work on one stream while the other's warps take exponentials:
+// with scores S, weights P and sums O of its own in TMEM (S 128 columns, O d columns; P 64 columns, which at d = 128
+// are S's, as TMEM is full), so that the tensor cores work on one stream while the other's warps take exponentials:
 //
 //     S_w = Q_w K^T        128 rows x 128 positions, operands in shared memory (128-byte swizzle, K-major)
 //     P_w = 2^(scale S_w - m)        two threads own a row, 64 positions each: no shuffles; 16 bits, back to TMEM
@@ -314,6 +314,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     using Geo = Geometry<Q8, D>;
     using Sh = Shared<Geo::kStages, Geo::kRaw>;
     constexpr int kStages = Geo::kStages, kSlabs = Geo::kSlabs, kTileBytes = Geo::kTileBytes;
+    constexpr bool kOwnP = D == 64;                         // weights have columns of their own
+    constexpr int kPAt = 384;                               // then: there
     static_assert(Geo::kBig + sizeof(Sh) <= kSmemBytes, "shared memory");
     extern __shared__ uint8_t smem_raw[];
     uint8_t *q_s = smem_raw;
@@ -375,7 +377,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     if (a.ctas > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // this CTA's barriers are set up
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = sh.tmem;                          // S0, S1 at 0, 128; O0, O1 at 256, 256 + D
+    const uint32_t tmem = sh.tmem;                          // S0, S1 at 0, 128; O0, O1 at 256, 256 + D; of heads of 64 P0, P1 at 384, 448
     bool cluster_up = a.ctas == 1;                          // the neighbours' barriers are, as far as this warp knows
     auto cluster_wait = [&] {
         if (!cluster_up) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -464,7 +466,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             constexpr uint32_t kIdescO = kCommon | ((uint32_t)(D >> 3) << 17) | (1u << 16);       // second operand MN-major
             auto uniform = [](int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); };
             const int st = uniform(warp == 3);
-            const uint32_t t0 = uniform(tmem), s_at = t0 + st * kTile, p_at = s_at + (Q8 ? 32 : 0), o_at = t0 + 256 + st * D;
+            const uint32_t t0 = uniform(tmem), s_at = t0 + st * kTile, o_at = t0 + 256 + st * D;
+            const uint32_t p_at = kOwnP ? t0 + kPAt + st * (kTile / 2) : s_at + (Q8 ? 32 : 0);
             const uint64_t q_desc = make_desc(smem_u32(q_s)), k_desc = make_desc(smem_u32(stages)), v_desc = make_desc_mn(smem_u32(stages));
             uint64_t *q_full = sh.q_full, *q_empty = sh.q_empty;
             const bool issuer = elect_one();
@@ -554,8 +557,13 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                         if (j == 0) umma_f16_ta(o_at, p_at, vd, kIdescO, 0);
                         else umma_f16_ta(o_at, p_at, vd, kIdescO, 1);
 #pragma unroll
-                        for (int k = 1; k < kTile / 16; ++k) umma_f16_ta(o_at, p_at + 8 * k + (Q8 && k >= kTile / 32 ? 32 : 0), vd + 128 * k, kIdescO, 1);
+                        for (int k = 1; k < kTile / 16; ++k) umma_f16_ta(o_at, p_at + 8 * k + (Q8 && !kOwnP && k >= kTile / 32 ? 32 : 0), vd + 128 * k, kIdescO, 1);
                         tc_commit(&sh.empty[s]);
+                        // At d = 128 the next scores go to the columns that hold the weights of the product just issued, with no wait
+                        // between: this relies on the tensor core running the products of a CTA in the order in which one thread
+                        // issues them, also where their sums lie in different columns.  (A wait there changes no bit of any result and
+                        // costs 6 % of a long prompt and 10 % of 1024 rows at 6000.)  What else reads or writes these columns, or O, is
+                        // behind the commit of the next scores, which counts all products issued before it.
                         if (more) issue_scores(j + 1, y % kStages);
                         else tc_commit(&sh.o_full[st]);
                     }
@@ -619,8 +627,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         const int row = tid & 127;                           // TMEM lane
         const int pair_bar = 4 + 4 * st + (warp & 3);        // barrier of the two warps that have the same rows
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;    // (warp % 4) x 32 lanes, in the address's upper half
-        const uint32_t ts = tmem + lanes + st * kTile + 64 * half, tp = Q8 ? ts + 32 : tmem + lanes + st * kTile + 32 * half;
-        const uint32_t to = tmem + lanes + 256 + st * D;
+        const uint32_t ts = tmem + lanes + st * kTile + 64 * half, to = tmem + lanes + 256 + st * D;
+        const uint32_t tp = kOwnP ? tmem + lanes + kPAt + st * (kTile / 2) + 32 * half : Q8 ? ts + 32 : tmem + lanes + st * kTile + 32 * half;
         const int row_tok = a.by_group.div(row);
         int steps = 0, items0 = 0, items1 = 0, joins = 0, base = 0;
         bool dead = false;
@@ -659,9 +667,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 dead = __any_sync(0xFFFFFFFFu, dead);
                 ++steps;
                 tc_fence_after();
-                // With a 16-bit cache a thread holds its 64 scores, and weights go to the first half of the tile's columns.  With an
-                // 8-bit cache there are fewer registers (the converting warps have the rest): 32 scores at a time, the
-                // first 32 read twice, weights to the place of the second 32.  61 rows x 4 heads of 64 behind 8000 positions in 148
+                // With a 16-bit cache a thread holds its 64 scores, and weights (where they have no columns of their own) go to the first
+                // half of the tile's columns.  With an 8-bit cache there are fewer registers (the converting warps have the rest): 32
+                // scores at a time, the first 32 read twice, weights to the place of the second 32.  61 rows x 4 heads of 64 behind 8000 positions in 148
                 // items took 161 us so and 207 with 64 held and spilled; the 16-bit kernel 130 so and 123 with 64 held.
                 float s[64];
                 uint32_t *su = reinterpret_cast<uint32_t *>(s);
