@@ -13,6 +13,36 @@ from tests.test_kv_cache_gpu import DT, U, Case, bits_of, ref_quantise
 pytestmark = pytest.mark.gpu
 
 
+class Large(Case):
+    """A case whose pool is made on the GPU (random rows; quantised by the definition, in torch)."""
+
+    def __init__(self, dtype, d, page, Hkv, ctx, chunk, quantised=False, seed=0):
+        super().__init__(dtype, d, page, 1, [0] * len(ctx), [0] * len(ctx), quantised, seed=seed)      # handles of an empty pool
+        self.cache.close()
+        rng, gen = np.random.default_rng(seed), torch.Generator(device="cuda").manual_seed(seed)
+        self.Hkv, self.ctx, self.chunk = Hkv, list(ctx), list(chunk)
+        need = [-(-(c + n) // page) for c, n in zip(ctx, chunk)]
+        self.pages, at = sum(need) + 3, 0
+        order = rng.permutation(self.pages)
+        self.table_np = np.full((self.B, max(need)), -1, dtype=np.int32)
+        for b, m in enumerate(need):
+            self.table_np[b, :m] = order[at:at + m]
+            at += m
+        self.start_np = np.concatenate([[0], np.cumsum(chunk)]).astype(np.int32)
+        self.rows = int(self.start_np[-1])
+        for name in ("k", "v"):
+            x = torch.randn((1, self.pages, Hkv, page, d), device="cuda", generator=gen).to(DT[dtype])
+            self.t[name], self.t[name + "_exp"] = x, None
+            if quantised:
+                m, e = torch.frexp(x.float().abs().amax(-1))          # 448 = 0.875 2^9
+                e = torch.where(m <= 0.875, e - 9, e - 8)
+                self.t[name] = torch.ldexp(x.float(), -e[..., None]).to(torch.float8_e4m3fn).view(torch.uint8)
+                self.t[name + "_exp"] = (e + 127).to(torch.uint8)
+        self.cache = binding.KvCache(self.t["k"], self.t["v"], dtype, k_exps=self.t["k_exp"], v_exps=self.t["v_exp"])
+        dev = lambda a: torch.from_numpy(np.asarray(a, dtype=np.int32)).cuda()
+        self.batch = binding.KvBatch(dev(self.table_np), dev(ctx), dev(self.start_np), rows=self.rows, max_chunk=max(chunk))
+
+
 def held_rows(case, name, b, upto):
     """float64 [upto][Hkv][d] of a sequence, on the GPU."""
     p = np.arange(upto)
@@ -37,6 +67,7 @@ def expected(case, q, b, see, scale):
     m = sc.amax(-1, keepdim=True)
     p = torch.exp(sc - torch.where(m > -np.inf, m, torch.zeros_like(m)))
     l = p.sum(-1, keepdim=True)
+    v = torch.where(torch.isfinite(v), v, torch.zeros_like(v))        # rows that see them are not compared
     out = torch.einsum("ihgj,jhd->ihgd", p, v) / torch.where(l > 0, l, torch.ones_like(l))
     lse = (m + l.log()).squeeze(-1)
     big = torch.where(see[:, None], v.abs().amax(-1).T[None], 0.0).amax(-1)                      # [n][Hkv]
@@ -92,7 +123,7 @@ def test_many_row_items_of_ragged_batches(dtype, d, quantised, tree):
     B, Hkv, G = 30, 4, 3
     ctx, chunk = ragged(1, B, 0, 2500), ragged(2, B, 40, 200)
     ctx[3], chunk[5], chunk[6] = 0, 0, 1
-    case = Case(dtype, d, 64, Hkv, ctx, chunk, quantised, seed=70)
+    case = Large(dtype, d, 64, Hkv, ctx, chunk, quantised, seed=70)
     q = case.queries(Hkv * G)
     for b in range(B):
         q[case.start_np[b]:case.start_np[b + 1]] *= 2.0 ** (b % 7 - 4)
@@ -106,7 +137,9 @@ def test_many_row_items_of_ragged_batches(dtype, d, quantised, tree):
         mask = bits_of(bits.cpu().numpy())
         seen = [torch.cat([torch.ones((chunk[b], ctx[b]), dtype=torch.bool, device="cuda"),
                            bits[int(case.start_np[b]):int(case.start_np[b + 1]), :chunk[b]]], 1) for b in range(B)]
-    check(case, q, seen, mask)
+    first = check(case, q, seen, mask)
+    for _ in range(3):
+        assert torch.equal(case.cache.attend(0, q, case.batch, mask=mask), first)
 
 
 @pytest.mark.parametrize("dtype,d,quantised", [("f16", 128, False), ("bf16", 128, True), ("bf16", 64, False), ("f16", 64, True)])
@@ -115,7 +148,7 @@ def test_single_tokens_of_large_ragged_batches(dtype, d, quantised, B, Hkv, G, h
     """Groups of four, two and one warps with tiles of 8 rows, and of four with tiles of 16; several segments each."""
     ctx = ragged(B, B, 0, hi)
     ctx[0], ctx[B // 2] = 0, longest
-    case = Case(dtype, d, 32, Hkv, ctx, [1] * B, quantised, seed=71)
+    case = Large(dtype, d, 32, Hkv, ctx, [1] * B, quantised, seed=71)
     q = case.queries(Hkv * G)
     check(case, q)
 
@@ -124,9 +157,26 @@ def test_single_tokens_of_large_ragged_batches(dtype, d, quantised, B, Hkv, G, h
 @pytest.mark.parametrize("chunk,path", [(1, 0), (33, 0), (2, 2), (33, 1)])
 def test_long_contexts(dtype, quantised, chunk, path):
     """Parts of a long item joined through clusters and global memory."""
-    case = Case(dtype, 128, 128, 2, [40000, 9999], [chunk] * 2, quantised, seed=72)
+    case = Large(dtype, 128, 128, 2, [40000, 9999], [chunk] * 2, quantised, seed=72)
     case.cache.set_option("attend_path", path)
     check(case, case.queries(8))
+
+
+@pytest.mark.parametrize("dtype,d", [("f16", 64), ("f16", 128), ("bf16", 64), ("bf16", 128)])
+@pytest.mark.parametrize("path,B,lo,hi", [(1, 30, 2, 30), (2, 30, 40, 150), (2, 3, 20, 60)])
+def test_bad_values_in_several_segments(dtype, d, path, B, lo, hi):
+    """16-bit values that are not finite, in the middle of every second chunk: tokens before them are untouched, through clusters,
+    several segments and parts."""
+    Hkv, ctx, chunk = 4, ragged(4, B, 0, 1500), ragged(5, B, lo, hi)
+    case = Large(dtype, d, 32, Hkv, ctx, chunk, seed=84)
+    case.cache.set_option("attend_path", path)
+    leave = set()
+    for b in range(0, B, 2):
+        bad = chunk[b] // 2
+        pg, off = case.place(b, ctx[b] + bad)
+        case.t["v"][0, pg, :, off, ::7] = float("nan") if b % 4 else float("inf")
+        leave |= {int(case.start_np[b]) + i for i in range(bad, chunk[b])}
+    check(case, case.queries(3 * Hkv), leave=leave)
 
 
 # ---- 8-bit rows of very different sizes -----------------------------------------------------------------------
@@ -241,8 +291,8 @@ def test_tails_below_the_types_last_bit(dtype, quantised, path, chunk):
 @pytest.mark.parametrize("G,chunk,path", [(3, 50, 2), (7, 20, 2), (12, 200, 2), (3, 1, 1), (5, 4, 1), (7, 30, 1)])
 def test_repeatable_whatever_ran_before(dtype, quantised, G, chunk, path):
     """Groups that do not divide a row tile, and other calls in between whose queries are very large or very small."""
-    case = Case(dtype, 64, 16, 3, [700, 90, 2100, 0], [chunk, 1, chunk, chunk // 2 + 1], quantised, seed=73)
-    other = Case(dtype, 64, 16, 2, [600] * 80, [8 * chunk // G + 1] * 80, quantised, seed=74)
+    case = Large(dtype, 64, 16, 3, [700, 90, 2100, 0], [chunk, 1, chunk, chunk // 2 + 1], quantised, seed=73)
+    other = Large(dtype, 64, 16, 2, [600] * 80, [8 * chunk // G + 1] * 80, quantised, seed=74)
     case.cache.set_option("attend_path", path)
     other.cache.set_option("attend_path", path)
     q = case.queries(3 * G)
@@ -260,7 +310,7 @@ def test_waits_that_run_out_in_either_kernel(B, chunk, path, stage, quantised):
     """A warp (K11) or CTA (K12) never receives one of its tiles -- alone, in a cluster, in one group of several --: the call ends,
     the status says so once, and the next call is right again."""
     ctx = [30000] + [600] * (B - 1)
-    case = Case("bf16", 128, 32, 4, ctx, [chunk] * B, quantised, seed=80)
+    case = Large("bf16", 128, 32, 4, ctx, [chunk] * B, quantised, seed=80)
     case.cache.set_option("attend_path", path)
     q = case.queries(8)
     first = case.cache.attend(0, q, case.batch)
