@@ -71,6 +71,8 @@ class Speculator:
     def __init__(self, model, prompts, room: int, store=None, n: int = 4, L: int = 8, eos_id: int = -1,
                  page_size: int = 64, quantised: bool = False):
         import torch
+        if not prompts or not all(prompts):
+            raise ValueError("every sequence needs a prompt of at least one token")
         device = model.embed.device
         self.model, self.store, self.n, self.L, self.eos_id = model, store, n if store else 0, L if store else 0, eos_id
         self.B, self.chunk = len(prompts), 1 + self.n * self.L
