@@ -344,11 +344,14 @@ dresd_status dresd_kv_read(dresd_kv *kv, int layer, const dresd_kv_batch *batch,
  *   out        device, dense [rows][heads][head_dim] in `dtype`
  *   out_lse    device, fp32 [rows][heads], or NULL: ln sum_j exp(scale q.k_j)
  *
- * Products of 16-bit numbers, sums, maxima and exponentials in fp32; the weights of the second
- * product are rounded to `dtype` once.  A token that sees nothing gets zeros and -infinity.
- * Keys and values that a token does not see take no part whatever they hold, NaN included;
- * so do the unused places of a page.  Non-finite values that it does see give
- * non-finite results.  The order of summation depends on the lengths only.
+ * Products of 16-bit numbers, sums, maxima and exponentials in fp32.  The weights of the second
+ * product are rounded once, to `dtype` -- fp16 weights reach down to 2^-32 of the largest --, and up to 16 rows per key/value head on an
+ * 8-bit cache to fp16 whatever `dtype` is (with the value's scale, counted from the row's largest product); bf16 queries
+ * are then multiplied in fp16 as well, scaled by a power of two a row: exact down to 2^-31 of the row's largest element, off
+ * by 2^-40 of it below.  A token that sees nothing gets zeros and -infinity.
+ * Keys and values that a token does not see take no part whatever they hold, NaN included (of an 8-bit cache: whatever
+ * dresd_kv_append() has written); nor do the unused places of a page.  Non-finite values that it does see give
+ * non-finite results.  The order of summation depends on the lengths and on the kernel only.
  */
 dresd_status dresd_kv_attend(dresd_kv *kv, int layer, const dresd_kv_batch *batch, const void *q, int64_t q_row,
                              int64_t q_head, int heads, float scale, const uint32_t *mask, int mask_words, void *out,

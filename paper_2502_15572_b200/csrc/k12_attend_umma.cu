@@ -27,12 +27,12 @@
 // issued behind them); the streams' products issued in turn, so that one stream's exponentials fall into the
 // other's products.
 //
-// Measured (148 SMs): 2047 rows x 4 heads of 128 at 12345 positions, bf16, 390 to 450 us = 1.0 to 1.15 PFLOP/s (the power limit
-// moves it; the tensor cores are busy half of the time); 148 items of 256 rows at 8000 positions, heads of 64, 117 us, with an 8-bit cache
-// 134, the converting warps' instructions between those of the softmax; three drafts of twenty tokens of 16 sequences, 8
-// bits, 57 us; ten of ten of one sequence 23 us, of which 10 are fixed (plan, first scores, join).  Taking a quarter of the
-// exponentials on the FMA pipes changed the first by nothing and cost 2 us of the second (8 bits: 16) and 5 of the third: the chain's
-// instructions and its four handovers a tile bound it, not the exponentials' unit.
+// Measured (148 SMs; medians): 2047 rows x 4 heads of 128 at 12345 positions, bf16, 455 us = 0.98 PFLOP/s (the power limit moves it,
+// single runs take 400 to 470; the tensor cores are busy half of the time), with an 8-bit cache 531 (fp16 478); 148 items of 244 rows
+// at 8000 positions, heads of 64, 118 us, with an 8-bit cache 124, the converting warps' instructions between those of the
+// softmax; three drafts of twenty tokens of 16 sequences, 8 bits, 53 us; ten of ten of one sequence 23.6 us, of which at most
+// three tiles a stream, some 5 us, are the chain.  Taking a quarter of the exponentials on the FMA pipes changed the first by nothing
+// and cost 2 us of the second: the chain's instructions and its four handovers a tile bound it, not the exponentials' unit.
 //
 // 8-bit tiles become tiles of the queries' type, which holds every code x 2^e exactly: behind the conversion an 8-bit cache is a 16-bit
 // one, and no row's size matters to another.
@@ -50,7 +50,7 @@ constexpr int kSlabBytes = kTile * 128;                    // 64 elements of eve
 constexpr float kSlack = 8.f;
 constexpr int kMaxCtas = 4;                                // of a cluster
 constexpr int kConvert = 8;                                // warps that convert 8-bit tiles
-// Queries and join of a segment take about as long as three tiles: 160 ragged items of 244 rows 57 us, 64 with 1, 59 with 2, 64 with 8.
+// Queries and join of a segment take about as long as three tiles: 160 ragged items of 244 rows 53 us, 59 with 1, 55 with 2, 61 with 8.
 constexpr int kFixed = 3;
 
 template <bool Q8, int D>
@@ -669,8 +669,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
                 tc_fence_after();
                 // With a 16-bit cache a thread holds its 64 scores, and weights (where they have no columns of their own) go to the first
                 // half of the tile's columns.  With an 8-bit cache there are fewer registers (the converting warps have the rest): 32
-                // scores at a time, the first 32 read twice, weights to the place of the second 32.  61 rows x 4 heads of 64 behind 8000 positions in 148
-                // items took 161 us so and 207 with 64 held and spilled; the 16-bit kernel 130 so and 123 with 64 held.
+                // scores at a time, the first 32 read twice, weights to the place of the second 32.  1024 rows x 4 heads of 128 at 6000 positions, 8 bits,
+                // 167 us so and 170 with 64 held (fp16 145 and 157; 148 items of 244 rows, heads of 64, 124 and 123); the 16-bit
+                // kernel, heads of 64, 124 so and 118 with 64 held.
                 float s[64];
                 uint32_t *su = reinterpret_cast<uint32_t *>(s);
                 const bool masked = p0 + kTile > all_seen;
@@ -1147,7 +1148,7 @@ cudaError_t launch_attend_umma(const CUtensorMap &q_map, const CUtensorMap &k_ma
     AttendArgs a = args;
     if (a.wait_cycles <= 0) a.wait_cycles = kWaitCycles;
     // One row tile per sequence and head (the hint says), and no more of them than half the SMs: clusters share them (101 rows of 32
-    // heads at 1999 positions 23.4 us, without clusters 28.6).  No more CTAs than give every stream a tile of the longest sequence that
+    // heads at 1999 positions 23.6 us, without clusters 29.0).  No more CTAs than give every stream a tile of the longest sequence that
     // the table can hold.
     const long long items = (long long)a.kv.B * a.kv.heads, tiles = (((long long)a.kv.width << a.kv.page_shift) + kTile - 1) / kTile;
     long long ctas = a.max_chunk <= kTile / a.group ? sms / items : 1;
