@@ -230,6 +230,7 @@ struct AttendArgs {
     int ctas;                   // CTAs of a worker: 1, or a cluster (see kv_plan.cuh)
     int tile_tokens;            // tokens of a 128-row tile (many rows)
     int groups;                 // workers of a CTA (few rows; then ctas is 1)
+    int group_shift;            // log2 of a worker's warps (few rows)
     int fixed;                  // what an item costs besides its units, in units
     int small;                  // the plan's numbers fit 32 bits
     long long wait_cycles;      // bound of every device-side wait in cycles, 0 = default

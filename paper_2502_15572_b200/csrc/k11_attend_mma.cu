@@ -104,6 +104,7 @@ struct Shared {
     uint64_t ready, taken;
     Job job[Geo::kWarps][4];                                         // of a worker
     int dead[Geo::kWarps][2];                                        // a wait of the worker ran out, by the segment's parity
+    KvPlan<FewRows> plan[Geo::kWarps];                               // of a worker; one thread goes on with it
     unsigned ticket[Geo::kWarps];
 };
 
@@ -149,7 +150,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     const long long wl = a.wait_cycles > 0 ? a.wait_cycles : kWaitCycles;
     const int rank = a.ctas > 1 ? (int)cluster_ctarank() : 0;
     const bool grouped = a.groups > 1;                     // then not in clusters
-    const int g_warps = kWarps / a.groups, group = warp / g_warps, first_warp = group * g_warps;
+    const int g_warps = 1 << a.group_shift, group = warp >> a.group_shift, first_warp = group << a.group_shift;
     const int g_tid = tid - first_warp * 32, g_threads = g_warps * 32;
     const int worker = grouped ? blockIdx.x * a.groups + group : blockIdx.x;       // of a cluster each CTA has its own parts
     const int step = g_warps * a.ctas;                     // a warp takes every step-th tile
@@ -174,25 +175,26 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     pdl_wait();                                             // what follows reads what earlier kernels wrote
     pdl_launch_dependents();
 
-    // The worker's first warp works out the segments, one ahead of the present one.
-    KvPlan<FewRows> plan;
-    bool more = false;
-    auto publish = [&](int i) {
+    // The worker's first warp works out the segments, one ahead of the present one.  (The plan lies in shared memory: in registers
+    // it made the 8-bit kernel spill, 16 sequences of 8000 59 us instead of 53.)
+    auto publish = [&](KvPlan<FewRows> &plan, int i) {
         Job &w = jobs[i & 3];
-        if (more) more = plan.next(a, w.seg);
-        w.more = more;
-        if (!more) return;
+        w.more = plan.next(a, w.seg);
+        if (!w.more) return;
         w.c = plan.c;
         const int seen = FewRows::seen(a, plan.c, w.seg.rt);
         w.t0 = w.seg.kt0 * step;
         w.t1 = min(w.seg.kt1 * step, (seen + kTile - 1) / kTile);
     };
     if (warp == first_warp) {
-        more = grouped ? plan.start(a, lane, worker, gridDim.x * a.groups)
-                       : plan.start(a, lane, blockIdx.x / a.ctas, gridDim.x / a.ctas);         // the same for the whole cluster
+        KvPlan<FewRows> plan;
+        const bool more = grouped ? plan.start(a, lane, worker, gridDim.x * a.groups)
+                                  : plan.start(a, lane, blockIdx.x / a.ctas, gridDim.x / a.ctas);         // the same for the whole cluster
         if (lane == 0) {
-            publish(0);
-            publish(1);
+            if (!more) plan.none();
+            publish(plan, 0);
+            publish(plan, 1);
+            sh.plan[group] = plan;
         }
     }
     if (a.ctas > 1) cluster_sync_all();                     // the neighbours' barriers are set up
@@ -597,7 +599,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         };
         give_up();
         sync();
-        if (g_tid == 0) publish(i + 2);
+        if (g_tid == 0) publish(sh.plan[group], i + 2);
         const int heads = a.kv.heads * a.group;
         const bool split = seg.c0 != seg.c1;
         float *part = part_slot(a, worker, seg.slot, kRows);
@@ -638,16 +640,23 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll 1
         for (int x = g_tid; x < Geo::kSums; x += g_threads) {
             const int r = x / (D / 4), e = x % (D / 4) * 4;
-            float mm = -INFINITY;
-#pragma unroll 4
-            for (int y = first_warp; y < first_warp + g_warps; ++y) mm = fmaxf(mm, sh.m[y][r]);
-            float ll = 0.f;
+            float mm = -INFINITY, ll = 0.f;
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-            for (int y = first_warp; y < first_warp + g_warps; ++y) {
+            auto add_warp = [&](int y) {
                 const float f = mm > -INFINITY ? ex2(sh.m[y][r] - mm) : 0.f;
                 ll += f * sh.l[y][r];
                 add(acc, f, *reinterpret_cast<const float4 *>(&sh.o[y][r][e]));
+            };
+            if (!grouped) {                                // all loads at once
+#pragma unroll
+                for (int y = 0; y < kWarps; ++y) mm = fmaxf(mm, sh.m[y][r]);
+#pragma unroll
+                for (int y = 0; y < kWarps; ++y) add_warp(y);
+            } else {
+#pragma unroll 4
+                for (int y = first_warp; y < first_warp + g_warps; ++y) mm = fmaxf(mm, sh.m[y][r]);
+#pragma unroll 4
+                for (int y = first_warp; y < first_warp + g_warps; ++y) add_warp(y);
             }
             if (a.ctas == 1) {
                 put(x, acc, mm, ll);
@@ -748,6 +757,7 @@ cudaError_t launch(const CUtensorMap &k_map, const CUtensorMap &v_map, const Att
                       : items >= (long long)sms * Geo::kWarps / 2 && positions <= 8192 ? 2
                                                                                        : 4;
     a.groups = items > sms ? Geo::kWarps / group : 1;
+    a.group_shift = items > sms ? group / 2 : Geo::kWarps == 8 ? 3 : 4;      // 1, 2, 4: 0, 1, 2
     const int unit = (int)tile * a.ctas / a.groups;
     a.by_unit = FastDiv(unit);
     // Queries and join of a segment take about as long as four tiles of a warp: 48 ragged sequences 39 us, 70 with 0, 41 with 8.

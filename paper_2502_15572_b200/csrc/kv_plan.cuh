@@ -346,7 +346,13 @@ struct KvPlan {
         return true;
     }
 
-    // The next segment; false when the worker has done its share.  Uniform over the worker.
+    // A worker with nothing to do.
+    __device__ __forceinline__ void none()
+    {
+        n = 0;
+        first = false;
+    }
+    // The next segment; false when the worker has done its share (also when asked again).  Uniform over the worker.
     __device__ bool next(const AttendArgs &a, Segment &s)
     {
         if (n == 0) {
