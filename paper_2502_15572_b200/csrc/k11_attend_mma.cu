@@ -30,9 +30,9 @@
 // with the 128-byte swizzle of the copies makes the reads of keys and of values free of bank conflicts.
 //
 // Measured (148 SMs, 8 heads of 128, 4 rows each): 2 sequences of 131071 positions in bf16 166 us = 6.46 TB/s, 98 % of what a copy
-// reaches; 16 of 8000 81 us = 6.4 TB/s; the same in 8 bits 59 us = 4.5 TB/s, where a warp's instructions (440 a tile) are what
-// is left; 48 of 0 to 8191 in 8 bits 39 us = 2.5 TB/s, bound by queries and joins of the many short segments; one of 700 with 32
-// heads 9.6 us, the chain of launch, plan, first tile and join.
+// reaches; 16 of 8000 81 us = 6.4 TB/s; the same in 8 bits 53 us = 5.0 TB/s, where a warp's instructions (425 a tile) are what
+// is left; 48 of 0 to 8191 in 8 bits 34.5 us = 2.8 TB/s, bound by queries and joins of the many short segments; one of 700 with 32
+// heads 9.4 us, the chain of launch, plan, first tile and join.
 //
 // Work is divided as kv_plan.cuh says.  With few items a worker is a CTA or a cluster; with more items than SMs it is a group of
 // four warps or fewer, so that what a segment costs besides its tiles (queries, join) is hidden behind the tiles of the
@@ -76,7 +76,7 @@ struct Geometry {
     static constexpr int kHalf = kTile * kRowBytes;       // keys (or values) of a tile
     static constexpr int kStage = 2 * kHalf;
     // A tile takes a warp about as long whatever its bytes: smaller tiles need more warps to keep HBM busy (2048 items of 1000
-    // positions of 64 in 8 bits: 88 us with 16 warps, 117 with 8).
+    // positions of 64 in 8 bits: 83 us with 16 warps, 117 with 8).
     static constexpr int kWarps = kStage <= 4096 && NT == 1 ? 16 : 8;
     static constexpr int kThreads = kWarps * 32;
     static constexpr int kStages = 131072 / (kWarps * kStage);       // 128 KB in flight an SM
@@ -745,14 +745,14 @@ cudaError_t launch(const CUtensorMap &k_map, const CUtensorMap &v_map, const Att
     // Clusters leave SMs idle (of 148, clusters of 7 use 112 or so) but save joins through global memory.  Where a CTA's share
     // of the cache takes long (1 MB, some 20 us) the SMs matter more, unless an item has so many parts that their join does:
     // 131071 positions of 128 in 16 bits, 3 items 43 us with clusters and 61 without, 10 items 109 and 112, 16 items 167 and 167;
-    // 60000 in 8 bits, 20 items 95 and 68, 50 items 144 and 137.  (700 positions, 32 items: 9.6 and 10.2.)
+    // 60000 in 8 bits, 20 items 85 and 62, 50 items 130 and 126.  (700 positions, 32 items: 9.4 and 10.2.)
     if (sms / items <= kMaxCluster && items * positions * 2 * Geo::kRowBytes / sms > 1 << 20) ctas = 1;
     a.ctas = (int)(ctas < 1 ? 1 : ctas > kMaxCluster ? kMaxCluster : ctas);
-    // More items than SMs: a CTA's groups work on items of their own (48 ragged sequences in 384 items 39 us, with the whole CTA on an
-    // item 47; 2048 items of 1000 positions of 64 in 8 bits 88 and 133).  Small groups only where no sequence is long, because the
-    // last worker on an item joins its parts alone: in 8 bits, heads of 64, 3200 items of 300 positions 55 us with groups of one
-    // warp, 59 of two, 66 of four, 2048 of 1000 88 us with two, 91 with one and with four; the 384 ragged ones (up to 8191) 99
-    // us with one, 51 with two.
+    // More items than SMs: a CTA's groups work on items of their own (48 ragged sequences in 384 items 35 us, with the whole CTA on an
+    // item 42; 2048 items of 1000 positions of 64 in 8 bits 83 and 126).  Small groups only where no sequence is long, because the
+    // last worker on an item joins its parts alone: in 8 bits, heads of 64, 3200 items of 300 positions 54 us with groups of one
+    // warp, 58 of two, 64 of four, 2048 of 1000 83 us with two, 84 with one, 87 with four; the 384 ragged ones (up to 8191) 97
+    // us with one, 47 with two.
     const int group = items >= (long long)sms * Geo::kWarps && positions <= 2048       ? 1
                       : items >= (long long)sms * Geo::kWarps / 2 && positions <= 8192 ? 2
                                                                                        : 4;
@@ -760,7 +760,7 @@ cudaError_t launch(const CUtensorMap &k_map, const CUtensorMap &v_map, const Att
     a.group_shift = items > sms ? group / 2 : Geo::kWarps == 8 ? 3 : 4;      // 1, 2, 4: 0, 1, 2
     const int unit = (int)tile * a.ctas / a.groups;
     a.by_unit = FastDiv(unit);
-    // Queries and join of a segment take about as long as four tiles of a warp: 48 ragged sequences 39 us, 70 with 0, 41 with 8.
+    // Queries and join of a segment take about as long as four tiles of a warp: 48 ragged sequences 34.5 us, 60 with 0, 36.3 with 8.
     a.fixed = kFixed;
     a.small = plan_is_small(a, Geo::kRows, positions / unit + 1);
     auto kernel = attend_mma_kernel<T, Q8, D, NT>;

@@ -307,9 +307,9 @@ dresd_status dresd_kv_attend(dresd_kv *kv, int layer, const dresd_kv_batch *batc
     a.lose_stage = kv->opt_lose_stage;
     kv->last_stream = static_cast<cudaStream_t>(stream);
     cudaError_t e;
-    // Up to 16 rows per key/value head the registers of mma.sync hold them: 16 sequences of 8000, 8 heads of 128, 16 rows 84 us
-    // with that kernel and 93 with the other (8 bits: 93 and 128), 32 rows 159 and 94 (177 and 130); one of 2000, 32
-    // heads, 16 rows 15.1 and 21.0, 17 rows 19.7 and 21.1.  The other kernel masks before it scales, which needs a positive scale.
+    // Up to 16 rows per key/value head the registers of mma.sync hold them: 16 sequences of 8000, 8 heads of 128, 16 rows 88 us
+    // with that kernel and 93 with the other (8 bits: 90 and 128), 32 rows 167 and 94 (171 and 131); one of 2000, 32
+    // heads, 16 rows 14.5 and 20.9, 17 rows 19.5 and 21.1.  The other kernel masks before it scales, which needs a positive scale.
     const bool many = kv->opt_path == 0 ? (long long)a.max_chunk * a.group > 16 : kv->opt_path == 2;
     if (many && scale > 0.f) {
         CUtensorMap q_map;

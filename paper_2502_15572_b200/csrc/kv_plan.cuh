@@ -187,8 +187,8 @@ __device__ __forceinline__ float ex2(float x)
 //   few items: a piece of ONE item.  With n / items workers for each, items are cut into pieces of at most L units, if L is
 //       within an eighth and five units of an even share W / n: nobody starts a second item, whose queries and join cost
 //       several units, and up to an eighth of the workers may idle for it (HBM is as busy without them, and an 8-bit cache,
-//       which is bound by instructions, still loses more by second items).  One token at 700 positions 9.6 us, 10.6 on the
-//       line; 16 at 8000, 8 heads of 128, 81 and 88, 8 bits 59 and 63 (heads of 64 47 and 48); two at 131071 167 and 167; 101 rows
+//       which is bound by instructions, still loses more by second items).  One token at 700 positions 9.4 us, 10.4 on the
+//       line; 16 at 8000, 8 heads of 128, 81 and 88, 8 bits 53 and 55 (heads of 64 43 and 45); two at 131071 166 and 165; 101 rows
 //       at 1999 23.6 and 33.7.
 //   otherwise: an even share of a line of all items in the order (sequence, row tile, head), so that the workers finish
 //       together however ragged the batch is; a worker has the tail of one item, some whole items and the head of another.
