@@ -37,7 +37,7 @@
 // Work is divided as kv_plan.cuh says.  With few items a worker is a CTA or a cluster; with more items than SMs it is a group of
 // four warps or fewer, so that what a segment costs besides its tiles (queries, join) is hidden behind the tiles of the
 // other groups.  The warps of a worker take every (warps)-th tile of a segment and are joined at its end.  The maximum is only raised when a score passes it by 2^8
-// (weights stay far inside the range of either type), which saves the shuffles of the maximum on most tiles.
+// (weights stay inside the range of either type, lifted ones of fp16 below 2^15), which saves the shuffles of the maximum on most tiles.
 #include "kv_plan.cuh"
 
 namespace dresd {
