@@ -258,6 +258,72 @@ dresd_status dresd_retrieve_quantised(dresd_store *store, const void *queries, c
                                       int32_t *out_tokens, void *stream);
 
 /*
+ * Verification by SAMPLING (Section 4: nucleus sampling with T = 0.7, p = 0.95): the counterpart of dresd_drafts_accept() for a
+ * language model that draws its tokens.  A retrieved draft proposes its token with certainty, so to accept token x with
+ * the model's probability p(x) and to draw from the rest of p otherwise is to draw y from p and to accept x if y is x: one
+ * random number a depth, and a text that does not depend on the drafts.
+ *
+ * Sequence b has a row of V logits behind its last token and one behind every token of its n drafts, in the order of the
+ * verification chunk (dresd_kv_attend): row 0, and row 1 + r L + t behind token t of draft r.  Drafts that are not valid take no part.  At depth t = 0, 1, ..
+ * one token y_t is drawn with uniform[b][t] from the row behind token t - 1 (t = 0: row 0) of the best-ranked (lowest) draft that begins
+ * with y_0 .. y_{t-1}; the sequence ends when no draft begins with y_0 .. y_t, or t = L.  Only the rows on this path are
+ * read.  n = L = 0: one token from the sequence's one row (drafts, valid may be NULL).
+ *
+ * A row's distribution, from x_i = its logits (NaN counts as -infinity, which is never drawn; -0 as 0):
+ *   temperature[b] > 0      w_i = round(2^42 exp((x_i - max x) / temperature)), a whole number: sums are exact, do not depend on
+ *                           their order, and the tokens not on the batch.  (exp in float64.)
+ *   otherwise (0, < 0, NaN) the largest logit, the lowest index of equal ones (uniform is not used); log-probability 0
+ *   top_k[b] > 0            only the top_k largest logits, the lowest indices of equal ones
+ *   top_p[b] < 1            of these, in descending order and then by index, the fewest whose sum of w is at least top_p times all of
+ *                           theirs, one at least (NaN: off)
+ *   y                       the lowest index whose running sum of remaining w, by index, exceeds floor(u S), S = their sum,
+ *                           u = uniform[b][t] brought into 0 .. 1 - 2^-24 (NaN: 0)
+ *   log-probability         (x_y - max x) / temperature - ln(S / 2^42)
+ * A row that holds no logit above -infinity gives token -1 with log-probability 0, and ends its sequence.
+ *
+ *   logits        device, `dtype` (all three), at any element's address; chunk_stride (between sequences) and row_stride
+ *                 (between rows of one) in elements, at least V.  V <= 2^20.
+ *   drafts, valid device, int32 [B][n][L], [B][n]: out_drafts, out_valid of dresd_drafts_prepare()
+ *   uniform       device, fp32 [B][L + 1], in [0, 1)
+ *   temperature, top_k, top_p   device, fp32 / int32 / fp32 [B], each may be NULL: 1, off, off
+ *   out_best, out_len, out_tokens   as for dresd_drafts_accept(): the lowest draft that begins with all of the accepted tokens (-1: none is
+ *                 valid); accepted tokens and the model's own, together 1 .. L + 1; [B][L + 1], -1 behind them
+ *   out_logprobs  device, fp32 [B][L + 1], 0 behind them; may be NULL
+ * Asynchronous on `stream`, on the current device; no workspace.
+ */
+dresd_status dresd_drafts_sample(const void *logits, dresd_dtype dtype, int64_t chunk_stride, int64_t row_stride, int V,
+                                 const int32_t *drafts, const int32_t *valid, const float *uniform, const float *temperature,
+                                 const int32_t *top_k, const float *top_p, int B, int n, int L, int32_t *out_best,
+                                 int32_t *out_len, int32_t *out_tokens, float *out_logprobs, void *stream);
+
+/*
+ * Products with 4-bit weights, for the projections of the language model that verifies the drafts: a step has few
+ * rows (a token, or a chunk of drafts, for every sequence) and is bound by the weights' bytes.
+ *
+ *   codes   device, uint8 [outputs][inputs / 2], 16-byte aligned: the low half of byte j of row o is c[o][2 j], the high one
+ *           c[o][2 j + 1], each 0 .. 15
+ *   scales  device, [outputs][inputs / group] in `dtype` (fp16 or bf16)
+ *   weight  w[o][i] = s[o][i / group] (c[o][i] - 8)
+ * group 32, 64 or 128; inputs a multiple of it; sizes up to DRESD_MAX_W4_SIZE.
+ *
+ * dresd_w4_quantise  from weights in `dtype`, w[i w_in + o w_out]: s = dtype(max |w| / 7) over the group, c = 8 + w / s rounded to
+ *                    nearest even and kept in 0 .. 15; 8 where s is 0.  Groups that hold NaN or infinity: unspecified.
+ * dresd_w4_matmul    out[t][o] = f(sum_i w[o][i] x[t][i]) + residual[t][o],  f(y) = max(y, 0) if relu != 0, otherwise y
+ *     x              [rows][inputs], 16-byte aligned, rows x_row elements apart (a multiple of 8)
+ *     residual       [rows][outputs], residual_row apart, or NULL; may be `out` itself
+ *     out            [rows][outputs], out_row apart
+ *   Products of (c - 8) and x are exact, their sums and the scales' products in fp32; one rounding, to `dtype`.  The order of
+ *   summation depends on the sizes only.
+ * Asynchronous on `stream`, on the current device; no workspace.
+ */
+enum { DRESD_MAX_W4_SIZE = 1 << 20 };
+dresd_status dresd_w4_quantise(const void *w, int64_t w_in, int64_t w_out, int inputs, int outputs, dresd_dtype dtype, int group,
+                               uint8_t *out_codes, void *out_scales, void *stream);
+dresd_status dresd_w4_matmul(const void *x, int64_t x_row, int rows, const uint8_t *codes, const void *scales, int inputs, int outputs,
+                             dresd_dtype dtype, int group, int relu, const void *residual, int64_t residual_row, void *out,
+                             int64_t out_row, void *stream);
+
+/*
  * Paged key/value cache of the language model that verifies the drafts, and its attention.
  * Batch verification (Section 3.6) runs the language model on the n x L draft matrix behind
  * the tokens it has already read; the keys and values of those tokens are kept here, so that
@@ -368,6 +434,42 @@ dresd_status dresd_kv_attend(dresd_kv *kv, int layer, const dresd_kv_batch *batc
  */
 dresd_status dresd_kv_keep_draft(dresd_kv *kv, const dresd_kv_batch *batch, const int32_t *best, const int32_t *length,
                                  int n, int L, void *stream);
+
+/*
+ * Pages that come and go, and that sequences share.  refs[p] is the number of table rows that hold page p (a row holds the pages
+ * of its entries within 0 .. num_pages - 1); a page with refs <= 0 is free.  The calls below keep the counts right as long as every row
+ * that holds pages of the cache is written by them alone; contradictory counts give unspecified tables and counts, but no access outside the
+ * arrays.  Results do not depend on timing.  They WRITE batch->page_table (dresd_kv_fork also batch->ctx), which the
+ * batch names as an input of the other calls.
+ *
+ * dresd_kv_attach_pages  refs: device, int32 [num_pages], 4-byte aligned, borrowed until destroy or the next attach.  A set-up
+ *                   call: the first one allocates 28 bytes per page and 256 KB.
+ * dresd_kv_fork     row b becomes a copy of row parent[b]: the pages of its first ctx[parent[b]] tokens are
+ *                   shared (refs + 1), the other entries are -1, ctx[b] = ctx[parent[b]].  No key or value
+ *                   moves.  parent[b] < 0 leaves row b alone; so does one of B or more, or a parent that is itself to become a copy
+ *                   (parent[parent[b]] >= 0; a row that is its own parent).  What row b held before is NOT released: that is the caller's.
+ *     parent        device, int32 [B];  ctx: batch->ctx, once more, as what is written
+ * dresd_kv_reserve  makes the places ctx[b] .. ctx[b] + (start[b+1] - start[b]) - 1 of every row its own, so that dresd_kv_append() of
+ *                   the same batch writes pages that no other row sees.  An entry that names no page gets a free one; one whose
+ *                   page is shared gets a free one too, into which all layers' keys and values are copied if the page
+ *                   holds tokens before ctx[b]; of several rows that wish for one page the last one keeps it if no other row holds it.
+ *                   Free pages are taken in ascending order, wishes served in the order (row, place).
+ *     out_missing   device, int32: 0, or the number of pages that the pool lacks (places beyond the table included, at most 16384 of a
+ *                   row); then nothing else has changed
+ * dresd_kv_release  row b gives back the pages behind its first keep[b] tokens: refs - 1, entries -1.  keep[b] <= 0: all.
+ *     keep          device, int32 [B]
+ * dresd_kv_compact  moves the used pages behind the first out_used ones, in ascending order and in all layers, to the free ones before
+ *                   them, and changes refs and the rows of the table.  Every row that holds pages of the
+ *                   cache has to be in `batch`; entries of free pages are left as they are.
+ *     out_used      device, int32: used pages, which are now pages 0 .. out_used - 1
+ *
+ * batch: fork, release and compact use page_table, ctx, B and table_width alone.
+ */
+dresd_status dresd_kv_attach_pages(dresd_kv *kv, int32_t *refs);
+dresd_status dresd_kv_fork(dresd_kv *kv, const dresd_kv_batch *batch, int32_t *ctx, const int32_t *parent, void *stream);
+dresd_status dresd_kv_reserve(dresd_kv *kv, const dresd_kv_batch *batch, int32_t *out_missing, void *stream);
+dresd_status dresd_kv_release(dresd_kv *kv, const dresd_kv_batch *batch, const int32_t *keep, void *stream);
+dresd_status dresd_kv_compact(dresd_kv *kv, const dresd_kv_batch *batch, int32_t *out_used, void *stream);
 
 /* dresd_store_status() for a cache: waits for its last stream, reports and clears its status word. */
 dresd_status dresd_kv_status(dresd_kv *kv);

@@ -36,6 +36,8 @@ EXPORTS = (
     "dresd_retrieve_quantised", "dresd_store_index_first_tokens", "dresd_merge_shards_packed",
     "dresd_noalloc_status", "dresd_debug_build", "dresd_store_debug_selftest",
     "dresd_kv_create", "dresd_kv_destroy", "dresd_kv_append", "dresd_kv_read", "dresd_kv_attend",
+    "dresd_drafts_sample", "dresd_w4_quantise", "dresd_w4_matmul",
+    "dresd_kv_attach_pages", "dresd_kv_fork", "dresd_kv_reserve", "dresd_kv_release", "dresd_kv_compact",
     "dresd_kv_keep_draft", "dresd_kv_status", "dresd_kv_set_option", "dresd_kv_last_launches", "dresd_kv_debug_selftest",
 )
 
@@ -140,6 +142,19 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.dresd_kv_attend.argtypes = [vp, i32, batch, vp, i64, i64, i32, f32, vp, i32, vp, vp, vp]
     lib.dresd_kv_keep_draft.restype = i32
     lib.dresd_kv_keep_draft.argtypes = [vp, batch, vp, vp, i32, i32, vp]
+    lib.dresd_drafts_sample.restype = i32
+    lib.dresd_drafts_sample.argtypes = [vp, i32, i64, i64, i32, vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.dresd_w4_quantise.restype = i32
+    lib.dresd_w4_quantise.argtypes = [vp, i64, i64, i32, i32, i32, i32, vp, vp, vp]
+    lib.dresd_w4_matmul.restype = i32
+    lib.dresd_w4_matmul.argtypes = [vp, i64, i32, vp, vp, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp]
+    lib.dresd_kv_attach_pages.restype = i32
+    lib.dresd_kv_attach_pages.argtypes = [vp, vp]
+    lib.dresd_kv_fork.restype = i32
+    lib.dresd_kv_fork.argtypes = [vp, batch, vp, vp, vp]
+    for name in ("dresd_kv_reserve", "dresd_kv_release", "dresd_kv_compact"):
+        getattr(lib, name).restype = i32
+        getattr(lib, name).argtypes = [vp, batch, vp, vp]
     lib.dresd_kv_status.restype = i32
     lib.dresd_kv_status.argtypes = [vp]
     lib.dresd_kv_set_option.restype = i32
@@ -204,6 +219,25 @@ def dresd_drafts_accept(drafts_ptr: int, valid_ptr: int, llm_ptr: int, B: int, n
                         out_best_ptr: int, out_len_ptr: int, out_tokens_ptr: int, stream: int = 0) -> None:
     _check(load().dresd_drafts_accept(drafts_ptr, valid_ptr, llm_ptr, B, n, L, out_best_ptr, out_len_ptr,
                                       out_tokens_ptr, stream))
+
+
+def dresd_drafts_sample(logits_ptr: int, dtype: int, chunk_stride: int, row_stride: int, V: int, drafts_ptr, valid_ptr,
+                        uniform_ptr: int, temperature_ptr, top_k_ptr, top_p_ptr, B: int, n: int, L: int, out_best_ptr: int,
+                        out_len_ptr: int, out_tokens_ptr: int, out_logprobs_ptr, stream: int = 0) -> None:
+    _check(load().dresd_drafts_sample(logits_ptr, dtype, chunk_stride, row_stride, V, drafts_ptr, valid_ptr, uniform_ptr,
+                                      temperature_ptr, top_k_ptr, top_p_ptr, B, n, L, out_best_ptr, out_len_ptr,
+                                      out_tokens_ptr, out_logprobs_ptr, stream))
+
+
+def dresd_w4_quantise(w_ptr: int, w_in: int, w_out: int, inputs: int, outputs: int, dtype: int, group: int,
+                      out_codes_ptr: int, out_scales_ptr: int, stream: int = 0) -> None:
+    _check(load().dresd_w4_quantise(w_ptr, w_in, w_out, inputs, outputs, dtype, group, out_codes_ptr, out_scales_ptr, stream))
+
+
+def dresd_w4_matmul(x_ptr: int, x_row: int, rows: int, codes_ptr: int, scales_ptr: int, inputs: int, outputs: int, dtype: int,
+                    group: int, relu: int, residual_ptr, residual_row: int, out_ptr: int, out_row: int, stream: int = 0) -> None:
+    _check(load().dresd_w4_matmul(x_ptr, x_row, rows, codes_ptr, scales_ptr, inputs, outputs, dtype, group, relu, residual_ptr,
+                                  residual_row, out_ptr, out_row, stream))
 
 
 def dresd_merge_shards_packed(packed_ptr: int, offsets_ptr: int, P: int, B: int, top_n: int, draft_len: int,
@@ -342,6 +376,26 @@ def dresd_kv_attend(kv: int, layer: int, batch: dresd_kv_batch, q_ptr: int, q_ro
 def dresd_kv_keep_draft(kv: int, batch: dresd_kv_batch, best_ptr: int, length_ptr: int, n: int, L: int,
                         stream: int = 0) -> None:
     _check(load().dresd_kv_keep_draft(kv, batch, best_ptr, length_ptr, n, L, stream))
+
+
+def dresd_kv_attach_pages(kv: int, refs_ptr: int) -> None:
+    _check(load().dresd_kv_attach_pages(kv, refs_ptr))
+
+
+def dresd_kv_fork(kv: int, batch: dresd_kv_batch, ctx_ptr: int, parent_ptr: int, stream: int = 0) -> None:
+    _check(load().dresd_kv_fork(kv, batch, ctx_ptr, parent_ptr, stream))
+
+
+def dresd_kv_reserve(kv: int, batch: dresd_kv_batch, out_missing_ptr: int, stream: int = 0) -> None:
+    _check(load().dresd_kv_reserve(kv, batch, out_missing_ptr, stream))
+
+
+def dresd_kv_release(kv: int, batch: dresd_kv_batch, keep_ptr: int, stream: int = 0) -> None:
+    _check(load().dresd_kv_release(kv, batch, keep_ptr, stream))
+
+
+def dresd_kv_compact(kv: int, batch: dresd_kv_batch, out_used_ptr: int, stream: int = 0) -> None:
+    _check(load().dresd_kv_compact(kv, batch, out_used_ptr, stream))
 
 
 def dresd_kv_status(kv: int) -> None:
@@ -711,3 +765,175 @@ class KvCache:
             self.close()
         except Exception:
             pass
+
+
+class KvPages:
+    """The pages of a cache as rows of a table hold them (``dresd_kv_fork`` and the calls after it).  Borrowed int32 CUDA tensors of the
+    cache's device: page_table [rows][places], an entry outside the pool names no page; refs [num_pages], the rows that hold a page."""
+
+    def __init__(self, cache: KvCache, page_table, refs):
+        torch = _torch()
+        self.cache, self.page_table, self.refs = cache, page_table, refs      # keep alive
+        for name, t, dims in (("page_table", page_table, 2), ("refs", refs, 1)):
+            if t.get_device() != cache.device_index or t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous():
+                raise DresdError(-1, f"{name} must be a contiguous int32 tensor with {dims} dimension(s) on cuda:{cache.device_index}")
+        if refs.shape[0] != cache.num_pages:
+            raise DresdError(-1, f"refs has {refs.shape[0]} entries for {cache.num_pages} pages")
+        self.rows, self._width = page_table.shape
+        # what release and compact read of a batch is the table; in the place of ctx, which is checked but not read, it stands again
+        self._c = dresd_kv_batch(page_table.data_ptr(), page_table.data_ptr(), None, self.rows, self._width, 0, 0)
+        self._attach()
+
+    def _attach(self):
+        """A cache counts in one array at a time: that of the KvPages whose call it is."""
+        if getattr(self.cache, "_counted_in", None) is not self.refs:
+            dresd_kv_attach_pages(self.cache.handle, self.refs.data_ptr())
+            self.cache._counted_in = self.refs
+
+    def _vector(self, name, t):
+        if t.dtype != _torch().int32 or t.get_device() != self.cache.device_index or t.shape != (self.rows,) or not t.is_contiguous():
+            raise DresdError(-1, f"{name} must be a contiguous int32 tensor of {self.rows} entries on cuda:{self.cache.device_index}")
+
+    def _word(self, stream):
+        with _allocated_on(stream):
+            return _torch().empty(1, dtype=_torch().int32, device=self.refs.device)
+
+    def fork(self, ctx, parent, stream=None):
+        """Row b becomes a copy of row parent[b] (-1: stays) that shares its pages; ctx[b] = ctx[parent[b]]."""
+        self._vector("ctx", ctx)
+        self._vector("parent", parent)
+        c = dresd_kv_batch(self.page_table.data_ptr(), ctx.data_ptr(), None, self.rows, self._width, 0, 0)
+        self._attach()
+        dresd_kv_fork(self.cache.handle, c, ctx.data_ptr(), parent.data_ptr(), _raw_stream(self.cache.device_index, stream))
+
+    def reserve(self, batch: KvBatch, stream=None):
+        """Makes the places that the batch's chunks will be written to the rows' own; returns int32 [1], 0 or the number of
+        pages that are missing (then nothing has changed)."""
+        if batch.page_table.data_ptr() != self.page_table.data_ptr() or batch.page_table.shape != self.page_table.shape:
+            raise DresdError(-1, "the batch has another page_table")
+        self.cache._batch(batch)
+        self._attach()
+        missing = self._word(stream)
+        dresd_kv_reserve(self.cache.handle, batch.c, missing.data_ptr(), _raw_stream(self.cache.device_index, stream))
+        return missing
+
+    def release(self, keep, stream=None):
+        """Row b gives back the pages behind its first keep[b] tokens."""
+        self._vector("keep", keep)
+        self._attach()
+        dresd_kv_release(self.cache.handle, self._c, keep.data_ptr(), _raw_stream(self.cache.device_index, stream))
+
+    def compact(self, stream=None):
+        """Moves the used pages to the lowest numbers; returns their count, int32 [1].  The table has to hold every row of the cache."""
+        self._attach()
+        used = self._word(stream)
+        dresd_kv_compact(self.cache.handle, self._c, used.data_ptr(), _raw_stream(self.cache.device_index, stream))
+        return used
+
+
+def drafts_sample(logits, uniform, drafts=None, valid=None, temperature=None, top_k=None, top_p=None, stream=None):
+    """Verification by sampling (``dresd_drafts_sample``).  logits [B][1 + n L][V] (f32, f16, bf16; rows may lie further apart than V):
+    of every sequence's chunk [last token, n drafts of L tokens]; uniform fp32 [B][L + 1]; drafts int32 [B][n][L], valid int32
+    [B][n], or neither (one row a sequence); temperature, top_p fp32 [B], top_k int32 [B], or None (1, off, off).
+    Returns ``(best [B], length [B], tokens [B][L + 1], logprobs [B][L + 1])``."""
+    torch = _torch()
+    code = {torch.float32: DRESD_F32, torch.float16: DRESD_F16, torch.bfloat16: DRESD_BF16}.get(logits.dtype)
+    dev = logits.get_device()
+    if code is None or dev < 0 or logits.dim() != 3:
+        raise DresdError(-1, "logits must be a CUDA tensor of f32, f16 or bf16 with 3 dimensions")
+    B, rows, V = logits.shape
+    if (drafts is None) != (valid is None):
+        raise DresdError(-1, "drafts and valid go together")
+    n, L = (0, 0) if drafts is None else drafts.shape[1:] if drafts.dim() == 3 else (-1, -1)
+    if n == 0 or L == 0:
+        n = L = 0
+    if rows != 1 + n * L:
+        raise DresdError(-1, f"logits have {rows} rows a sequence for {n} drafts of {L} tokens")
+    if V > 1 and logits.stride(2) != 1:
+        raise DresdError(-1, "the logits of a row must be adjacent")
+    for name, t, dtype, shape in (("uniform", uniform, torch.float32, (B, L + 1)), ("drafts", drafts, torch.int32, (B, n, L)),
+                                  ("valid", valid, torch.int32, (B, n)), ("temperature", temperature, torch.float32, (B,)),
+                                  ("top_k", top_k, torch.int32, (B,)), ("top_p", top_p, torch.float32, (B,))):
+        if t is None and name != "uniform" or n == 0 and name in ("drafts", "valid"):
+            continue
+        if t is None or t.dtype != dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+            raise DresdError(-1, f"{name} must be a contiguous {dtype} tensor of shape {shape} on cuda:{dev}")
+    with _allocated_on(stream):
+        words = torch.empty((2 + 2 * (L + 1), B), dtype=torch.int32, device=logits.device)
+    best, length = words[0], words[1]
+    tokens = words[2:3 + L].view(B, L + 1)
+    logs = words[3 + L:].view(torch.float32).view(B, L + 1)
+    ptr = lambda t: None if t is None else t.data_ptr()
+    if B:
+        dresd_drafts_sample(logits.data_ptr(), code, logits.stride(0), logits.stride(1), V, ptr(drafts) if n else None,
+                            ptr(valid) if n else None, uniform.data_ptr(), ptr(temperature), ptr(top_k), ptr(top_p), B, n, L, best.data_ptr(),
+                            length.data_ptr(), tokens.data_ptr(), logs.data_ptr(), _raw_stream(dev, stream))
+    return best, length, tokens, logs
+
+
+class W4:
+    """Weights of 4 bits with group scales (``dresd_w4_matmul``); tensors passed in are borrowed.
+
+    codes: uint8 [outputs][inputs / 2], scales: `dtype` [outputs][inputs / group]."""
+
+    def __init__(self, codes, scales, dtype: str):
+        torch = _torch()
+        if dtype not in ("f16", "bf16"):
+            raise DresdError(-2, f"4-bit weights go with f16 or bf16, not {dtype}")
+        self.torch_dtype = {"f16": torch.float16, "bf16": torch.bfloat16}[dtype]
+        for name, t, held in (("codes", codes, torch.uint8), ("scales", scales, self.torch_dtype)):
+            if not t.is_cuda or t.dtype != held or t.dim() != 2 or not t.is_contiguous():
+                raise DresdError(-1, f"{name} must be a contiguous {held} CUDA tensor with 2 dimensions")
+        if scales.get_device() != codes.get_device():
+            raise DresdError(-1, "scales are on another device than codes")
+        self.outputs, self.inputs = codes.shape[0], 2 * codes.shape[1]
+        if scales.shape[0] != self.outputs or scales.shape[1] < 1 or self.inputs % scales.shape[1]:
+            raise DresdError(-1, f"scales have shape {tuple(scales.shape)} for {self.outputs} outputs and {self.inputs} inputs")
+        self.dtype, self.group = dtype, self.inputs // scales.shape[1]
+        if self.group not in (32, 64, 128):
+            raise DresdError(-2, f"group = {self.group} is not 32, 64 or 128")
+        self.codes, self.scales, self.device_index = codes, scales, codes.get_device()       # keep alive
+
+    @classmethod
+    def quantise(cls, w, group: int = 128, stream=None):
+        """From weights [inputs][outputs] (as in ``x @ w``; a transposed view is fine)."""
+        torch = _torch()
+        dtype = {torch.float16: "f16", torch.bfloat16: "bf16"}.get(w.dtype)
+        if not w.is_cuda or dtype is None or w.dim() != 2:
+            raise DresdError(-1, "w must be an f16 or bf16 CUDA tensor with 2 dimensions")
+        inputs, outputs = w.shape
+        if group not in (32, 64, 128):
+            raise DresdError(-2, f"group = {group} is not 32, 64 or 128")
+        if inputs < 1 or outputs < 1 or inputs % group:
+            raise DresdError(-1, f"w has {inputs} inputs (a multiple of {group} is needed) and {outputs} outputs")
+        with _allocated_on(stream):
+            codes = torch.empty((outputs, inputs // 2), dtype=torch.uint8, device=w.device)
+            scales = torch.empty((outputs, inputs // group), dtype=w.dtype, device=w.device)
+        # the distance of a dimension with one entry is never used
+        dresd_w4_quantise(w.data_ptr(), w.stride(0), w.stride(1) if outputs > 1 else 1, inputs, outputs, DTYPE_CODE[dtype], group, codes.data_ptr(), scales.data_ptr(),
+                          _raw_stream(w.get_device(), stream))
+        return cls(codes, scales, dtype)
+
+    def _rows(self, name, t, rows, columns):
+        if t.dtype != self.torch_dtype or t.get_device() != self.device_index or t.shape != (rows, columns):
+            raise DresdError(-1, f"{name} must be a {self.torch_dtype} tensor of shape {(rows, columns)} on cuda:{self.device_index}")
+        if columns > 1 and t.stride(1) != 1:
+            raise DresdError(-1, f"{name}: the elements of a row must be adjacent")
+        return t.data_ptr(), t.stride(0)
+
+    def matmul(self, x, residual=None, relu: bool = False, out=None, stream=None):
+        """f(x w) + residual for x [rows][inputs]; f is max(., 0) with `relu`.  out: [rows][outputs], may be `residual` itself."""
+        if x.dim() != 2:
+            raise DresdError(-1, "x must have 2 dimensions")
+        rows = x.shape[0]
+        x_ptr, x_row = self._rows("x", x, rows, self.inputs)
+        res_ptr, res_row = (None, 0) if residual is None else self._rows("residual", residual, rows, self.outputs)
+        if out is None:
+            with _allocated_on(stream):
+                out = _torch().empty((rows, self.outputs), dtype=self.torch_dtype, device=x.device)
+        out_ptr, out_row = self._rows("out", out, rows, self.outputs)
+        if rows:
+            dresd_w4_matmul(x_ptr, x_row, rows, self.codes.data_ptr(), self.scales.data_ptr(), self.inputs, self.outputs,
+                            DTYPE_CODE[self.dtype], self.group, int(relu), res_ptr, res_row, out_ptr, out_row,
+                            _raw_stream(self.device_index, stream))
+        return out

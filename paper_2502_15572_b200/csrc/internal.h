@@ -196,6 +196,52 @@ cudaError_t launch_kv_read(const KvArgs &a, void *out_k, void *out_v, cudaStream
 cudaError_t launch_kv_keep_draft(const KvArgs &a, const int32_t *best, const int32_t *length, int n, int L,
                                  cudaStream_t stream);
 
+// ---- K13: verification of drafts by sampling ----
+struct SampleArgs {
+    const void *logits;         // [B][1 + n L][V] at the distances below, in elements
+    long long chunk_stride, row_stride;
+    const int32_t *drafts, *valid;        // [B][n][L], [B][n]
+    const float *uniform;       // [B][L + 1]
+    const float *temperature, *top_p;     // [B] or null
+    const int32_t *top_k;
+    int B, n, L, V, ctas;
+    int32_t *out_best, *out_len, *out_tokens;
+    float *out_logs;            // or null
+};
+cudaError_t launch_sample(const SampleArgs &a, int dtype, int sms, cudaStream_t stream);
+
+// ---- K15: products with 4-bit weights ----
+struct W4Args {
+    const void *x;              // [rows][inputs]
+    long long x_row;
+    const uint8_t *codes;       // [outputs][inputs / 2]
+    const void *scales;         // [outputs][inputs / group]
+    const void *residual;       // [rows][outputs] or null
+    long long residual_row;
+    void *out;                  // [rows][outputs]
+    long long out_row;
+    int rows, inputs, outputs, groups;
+    int relu;
+};
+cudaError_t launch_w4_quantise(const void *w, long long w_in, long long w_out, int inputs, int outputs, int dtype, int group,
+                               uint8_t *codes, void *scales, cudaStream_t stream);
+cudaError_t launch_w4_matmul(const W4Args &a, int dtype, int group, int sms, cudaStream_t stream);
+
+// ---- K14: pages of the cache ----
+enum { kPageMoves, kPageShared, kPageUsed, kPageCounts };
+struct PageArgs {
+    int32_t *refs;              // [num_pages] rows that hold a page; the caller's
+    unsigned long long *last;   // [num_pages] workspace, zero between calls: the last wish for a shared page
+    int32_t *holders;           // [num_pages] likewise: how many wish for it
+    int32_t *map, *list, *from, *to;      // [num_pages] each
+    int32_t *row_first;         // [kMaxKvBatch]
+    int32_t *counts;            // [kPageCounts]
+};
+cudaError_t launch_kv_fork(const KvArgs &a, int32_t *refs, int32_t *table, int32_t *ctx, const int32_t *parent, cudaStream_t stream);
+cudaError_t launch_kv_release(const KvArgs &a, int32_t *refs, int32_t *table, const int32_t *keep, cudaStream_t stream);
+cudaError_t launch_kv_reserve(const KvArgs &a, const PageArgs &w, int32_t *table, int32_t *out_missing, int sms, cudaStream_t stream);
+cudaError_t launch_kv_compact(const KvArgs &a, const PageArgs &w, int32_t *table, int32_t *out_used, int sms, cudaStream_t stream);
+
 // Division by a number that the host knows: q = (umulhi(n, m) + n) >> s for n < 2^31 (Granlund and Montgomery 1994).
 struct FastDiv {
     uint32_t d, m, s;

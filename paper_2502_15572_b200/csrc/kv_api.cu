@@ -1,48 +1,19 @@
 // C ABI of the paged key/value cache (the dresd_kv_* calls of include/dresd.h): handle, argument
-// validation, tensor maps, workspace.  The kernels are in k10_kv_cache.cu, k11_attend_mma.cu and
-// k12_attend_umma.cu.
-#include <cstdarg>
-#include <cstdio>
+// validation, tensor maps, workspace.  The kernels are in k10_kv_cache.cu, k11_attend_mma.cu,
+// k12_attend_umma.cu and k14_kv_pages.cu.
 #include <cstring>
 #include <new>
 
-#include "../../include/dresd.h"
-#include "internal.h"
+#include "api_util.h"
 
 using namespace dresd;
 
 namespace {
 
-dresd_status fail(dresd_status st, const char *fmt, ...)
-{
-    char msg[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(msg, sizeof msg, fmt, ap);
-    va_end(ap);
-    set_last_error(msg);
-    return st;
-}
-dresd_status fail_cuda(cudaError_t e, const char *what)
-{
-    return fail(DRESD_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
-}
-
 constexpr uint32_t kKvMagic = 0xD2E5D0C4u;
 constexpr int kMaxKvBatch = 65535;
 constexpr int kMaxGroup = 64;
 
-// Memory of `device` (a cache's kernels must not be given another GPU's), or managed memory.
-bool is_device_ptr(const void *p, int device)
-{
-    if (!p) return false;
-    cudaPointerAttributes at;
-    if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
-        cudaGetLastError();
-        return false;
-    }
-    return (at.type == cudaMemoryTypeDevice && at.device == device) || at.type == cudaMemoryTypeManaged;
-}
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -74,7 +45,7 @@ bool encode(CUtensorMap *map, const void *base, int dtype, int rank, const cuuin
                     swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+bool aligned16(const void *p) { return aligned(p, 16); }
 
 }  // namespace
 
@@ -86,6 +57,7 @@ struct dresd_kv {
     KvArgs args;                 // arrays and geometry; the batch's part is filled in per call
     float *part;                 // parts of shared items (see kv_plan.cuh)
     unsigned int *tickets;
+    PageArgs pages;              // refs is null until dresd_kv_attach_pages()
     int opt_path, opt_wait_ms, opt_lose_stage;
     cudaStream_t last_stream;
     int last_launches;
@@ -99,6 +71,7 @@ void free_kv(dresd_kv *kv)
 {
     cudaFree(kv->part);
     cudaFree(kv->tickets);
+    cudaFree(kv->pages.last);     // all of the pages' workspace
     cudaFree(kv->args.status);
     kv->magic = 0;
     delete kv;
@@ -132,6 +105,15 @@ dresd_status check_call(dresd_kv *kv, int layer, const dresd_kv_batch *b, bool w
     if (b->B == 0 || (whole && b->rows == 0)) return DRESD_OK;
     if (!is_device_ptr(b->page_table, dev) || !is_device_ptr(b->ctx, dev) || (whole && !is_device_ptr(b->start, dev)))
         return fail(DRESD_ERR_INVALID, "page_table/ctx/start must be pointers of the cache's device");
+    return DRESD_OK;
+}
+
+// The same for a call that counts pages and writes the table.
+dresd_status check_pages(dresd_kv *kv, const dresd_kv_batch *b, bool whole, KvArgs *out)
+{
+    const dresd_status st = check_call(kv, 0, b, whole, out);
+    if (st != DRESD_OK) return st;
+    if (!kv->pages.refs) return fail(DRESD_ERR_INVALID, "the cache has no page counts: dresd_kv_attach_pages() comes first");
     return DRESD_OK;
 }
 
@@ -345,6 +327,107 @@ dresd_status dresd_kv_keep_draft(dresd_kv *kv, const dresd_kv_batch *batch, cons
     const cudaError_t e = launch_kv_keep_draft(a, best, length, n, L, kv->last_stream);
     if (e != cudaSuccess) return fail_cuda(e, "kv_keep_draft launch");
     kv->last_launches = 1;
+    return DRESD_OK;
+}
+
+dresd_status dresd_kv_attach_pages(dresd_kv *kv, int32_t *refs)
+{
+    if (!valid(kv)) return fail(DRESD_ERR_INVALID, "cache handle is NULL or destroyed");
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev != kv->device)
+        return fail(DRESD_ERR_INVALID, "the cache belongs to device %d; the current device is %d", kv->device, dev);
+    if (!is_device_ptr(refs, dev) || !aligned(refs, 4))
+        return fail(DRESD_ERR_INVALID, "refs must be an aligned pointer of the cache's device");
+    if (!kv->pages.last) {
+        const size_t n = (size_t)kv->args.num_pages, words = 7 * n + kMaxKvBatch + kPageCounts;
+        PageArgs w{};
+        if (cudaMalloc(&w.last, 4 * words) != cudaSuccess) {
+            cudaGetLastError();
+            return fail(DRESD_ERR_ALLOC, "workspace allocation failed");
+        }
+        w.holders = reinterpret_cast<int32_t *>(w.last + n);
+        w.map = w.holders + n;
+        w.list = w.map + n;
+        w.from = w.list + n;
+        w.to = w.from + n;
+        w.row_first = w.to + n;
+        w.counts = w.row_first + kMaxKvBatch;
+        // on a stream of its own, as in dresd_kv_create()
+        cudaStream_t own = nullptr;
+        cudaError_t e = cudaStreamCreateWithFlags(&own, cudaStreamNonBlocking);
+        if (e == cudaSuccess) e = cudaMemsetAsync(w.last, 0, 4 * words, own);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(own);
+        if (own) cudaStreamDestroy(own);
+        if (e != cudaSuccess) {
+            cudaFree(w.last);
+            return fail_cuda(e, "workspace reset");
+        }
+        kv->pages = w;
+    }
+    kv->pages.refs = refs;
+    return DRESD_OK;
+}
+
+dresd_status dresd_kv_fork(dresd_kv *kv, const dresd_kv_batch *batch, int32_t *ctx, const int32_t *parent, void *stream)
+{
+    KvArgs a;
+    dresd_status st = check_pages(kv, batch, false, &a);
+    if (st != DRESD_OK) return st;
+    kv->last_launches = 0;
+    if (a.B == 0) return DRESD_OK;
+    if (ctx != a.ctx) return fail(DRESD_ERR_INVALID, "ctx must be the batch's");
+    if (!is_device_ptr(parent, kv->device)) return fail(DRESD_ERR_INVALID, "parent must be a pointer of the cache's device");
+    kv->last_stream = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = launch_kv_fork(a, kv->pages.refs, const_cast<int32_t *>(a.table), ctx, parent, kv->last_stream);
+    if (e != cudaSuccess) return fail_cuda(e, "kv_fork launch");
+    kv->last_launches = 1;
+    return DRESD_OK;
+}
+
+dresd_status dresd_kv_reserve(dresd_kv *kv, const dresd_kv_batch *batch, int32_t *out_missing, void *stream)
+{
+    KvArgs a;
+    dresd_status st = check_pages(kv, batch, true, &a);
+    if (st != DRESD_OK) return st;
+    kv->last_launches = 0;
+    if (!is_device_ptr(out_missing, kv->device)) return fail(DRESD_ERR_INVALID, "out_missing must be a pointer of the cache's device");
+    kv->last_stream = static_cast<cudaStream_t>(stream);
+    if (a.B == 0 || a.rows == 0) {
+        const cudaError_t e = cudaMemsetAsync(out_missing, 0, sizeof(int32_t), kv->last_stream);
+        return e == cudaSuccess ? DRESD_OK : fail_cuda(e, "kv_reserve");
+    }
+    const cudaError_t e = launch_kv_reserve(a, kv->pages, const_cast<int32_t *>(a.table), out_missing, kv->sms, kv->last_stream);
+    if (e != cudaSuccess) return fail_cuda(e, "kv_reserve launch");
+    kv->last_launches = 2;
+    return DRESD_OK;
+}
+
+dresd_status dresd_kv_release(dresd_kv *kv, const dresd_kv_batch *batch, const int32_t *keep, void *stream)
+{
+    KvArgs a;
+    dresd_status st = check_pages(kv, batch, false, &a);
+    if (st != DRESD_OK) return st;
+    kv->last_launches = 0;
+    if (a.B == 0) return DRESD_OK;
+    if (!is_device_ptr(keep, kv->device)) return fail(DRESD_ERR_INVALID, "keep must be a pointer of the cache's device");
+    kv->last_stream = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = launch_kv_release(a, kv->pages.refs, const_cast<int32_t *>(a.table), keep, kv->last_stream);
+    if (e != cudaSuccess) return fail_cuda(e, "kv_release launch");
+    kv->last_launches = 1;
+    return DRESD_OK;
+}
+
+dresd_status dresd_kv_compact(dresd_kv *kv, const dresd_kv_batch *batch, int32_t *out_used, void *stream)
+{
+    KvArgs a;
+    dresd_status st = check_pages(kv, batch, false, &a);
+    if (st != DRESD_OK) return st;
+    kv->last_launches = 0;
+    if (!is_device_ptr(out_used, kv->device)) return fail(DRESD_ERR_INVALID, "out_used must be a pointer of the cache's device");
+    kv->last_stream = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = launch_kv_compact(a, kv->pages, const_cast<int32_t *>(a.table), out_used, kv->sms, kv->last_stream);
+    if (e != cudaSuccess) return fail_cuda(e, "kv_compact launch");
+    kv->last_launches = 2;
     return DRESD_OK;
 }
 
