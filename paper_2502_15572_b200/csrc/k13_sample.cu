@@ -1,27 +1,52 @@
 // K13 -- verification of drafts against the model's distribution, from given random numbers (no drafts: sampling).
 //
 // A sequence is a chain: the token drawn at depth t decides which row of logits is read at depth t + 1, so that only the rows on
-// the path are read, at most L + 1 of the 1 + n L.  One cluster follows a sequence; its CTAs share a row by contiguous pieces.
-// Per row: the maximum; the cuts of top_k and top_p (radix selection by histograms of 2048 bins, summed over the cluster);
-// the weights' sums piece by piece; and the piece, warp, lane and element where the running sum passes u times the whole.
+// the path are read, at most L + 1 of the 1 + n L.  One cluster follows a sequence; its CTAs share a row by contiguous pieces, which
+// they keep in shared memory as far as it goes.  Per row: the maximum; the cuts of top_k and top_p; the weights' sums piece by piece; and
+// the piece, warp, lane and element where the running sum passes u times the whole.  Every step ends in an exchange through the cluster, a
+// barrier (some 700 cycles) and loads from the other CTAs' shared memory (some 500): latency, not bytes, is what a row costs.  Instructions
+// come from far at the first depth, so loops are not unrolled where that multiplies long code (32000 logits, top_p: 22.0 us a row so, 18.8 us without).
 //
 // A weight is rint(2^42 e^((x - max) / T)), a whole number: sums are exact, so they depend neither on their order nor on how
 // many CTAs share a row, and a token is the same whatever the batch.
+//
+// Cuts are found from the largest logit down with histograms of 2048 bins.  The first one has bins of equal width in (max - x) / T, over the 44 octaves in
+// which weights are not 0: logits spread over many of them, while bits of a float's exponent would put most into a few, whose
+// atomic additions then wait for one another.  Further ones divide the range of keys of the bin that was hit, until a bin is one key; the
+// second one is the last for 16-bit logits as a rule, and looks at one group of 32 bins.
+#include <atomic>
+#include <cfloat>
+
 #include "common.cuh"
 #include "internal.h"
 
 namespace dresd {
 namespace {
 
-constexpr int kThreads = 1024, kWarps = kThreads / 32, kMaxCtas = 8;
-constexpr int kBins = 2048, kEntries = 2048;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCtas = 16;
+constexpr int kBins = 2048, kGroups = kBins / 32, kSteps = 64;
 constexpr double kOne = 4398046511104.0;                       // 2^42, the largest weight
+constexpr float kOctaves = 44.f;                               // a weight 2^-44 of the largest rounds to 0
+constexpr int kTable = 64;                                     // 2^(-j / 64)
 
 typedef unsigned long long u64;
 
-template <typename T> __device__ __forceinline__ float to_float(T x) { return x; }
-template <> __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
-template <> __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T> struct Logit;
+template <> struct Logit<float> {
+    static constexpr uint32_t kLowest = 0xFF800000u;           // -infinity
+    static constexpr int kGrain = 0;                           // low bits of float_to_ordered() that are the same for all
+    static __device__ __forceinline__ float value(float x) { return x; }
+};
+template <> struct Logit<__half> {
+    static constexpr uint32_t kLowest = 0xFC00FC00u;
+    static constexpr int kGrain = 13;
+    static __device__ __forceinline__ float value(__half x) { return __half2float(x); }
+};
+template <> struct Logit<__nv_bfloat16> {
+    static constexpr uint32_t kLowest = 0xFF80FF80u;
+    static constexpr int kGrain = 16;
+    static __device__ __forceinline__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
+};
 
 // A row of logits at any address, as blocks of 16 bytes from the boundary at or before its first element.
 template <typename T> struct Row {
@@ -35,60 +60,53 @@ template <typename T> struct Row {
         last = first + V;
         blocks = (last + kVec - 1) / kVec;
     }
-    // Elements of block q; what is not the row's, and NaN, as -infinity; -0 as 0.
-    __device__ __forceinline__ void load(int q, float (&x)[kVec]) const
+    // Block q; what is not the row's is -infinity.
+    __device__ __forceinline__ uint4 load(int q) const
     {
         const int j = q * kVec;
-        if (j >= first && j + kVec <= last) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(base + j);
-            const T *e = reinterpret_cast<const T *>(&w);
+        if (j >= first && j + kVec <= last) return __ldg(reinterpret_cast<const uint4 *>(base + j));
+        constexpr uint32_t low = Logit<T>::kLowest;
+        uint4 w = make_uint4(low, low, low, low);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) x[i] = to_float(e[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) x[i] = j + i >= first && j + i < last ? to_float(base[j + i]) : -INFINITY;
-        }
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) x[i] = x[i] == x[i] ? x[i] + 0.f : -INFINITY;
+        for (int i = 0; i < kVec; ++i)
+            if (j + i >= first && j + i < last) reinterpret_cast<T *>(&w)[i] = base[j + i];
+        return w;
     }
 };
+template <typename T> __device__ __forceinline__ void values(const uint4 &w, float (&x)[16 / sizeof(T)])
+{
+#pragma unroll
+    for (int i = 0; i < (int)(16 / sizeof(T)); ++i) x[i] = Logit<T>::value(reinterpret_cast<const T *>(&w)[i]);
+}
 
-// Order of logits as whole numbers.  16-bit types leave the low 13 bits of a float alike, so that 22 bits tell them apart.
-template <typename T> struct Order {
-    static constexpr int kBits = sizeof(T) == 2 ? 22 : 32, kPasses = sizeof(T) == 2 ? 2 : 3;
-    static __device__ __forceinline__ uint32_t key(float x) { return float_to_ordered(x) >> (32 - kBits); }
-    static __device__ __forceinline__ int shift(int pass) { return max(kBits - 11 * (pass + 1), 0); }
-    static __device__ __forceinline__ int width(int pass) { return kBits - 11 * pass - shift(pass); }
-};
-
-// What remains of a row: elements whose key is larger, and the first `ties` of those whose key is equal.
+// What remains of a row: logits that are larger than x, and the first `ties` of those that are equal.  NaN is neither.
 struct Cut {
-    uint32_t key;
+    float x;
     int ties;
 };
 
-struct Shared {
-    union {
-        struct {
-            u64 bins[kBins];             // this CTA's elements
-            u64 sums[kBins];             // the cluster's, for this CTA's part of the bins
-        };
-        struct {
-            u64 weight[kEntries];        // of a warp's consecutive blocks
-            int ties[kEntries];
-        };
-    };
-    u64 warp_u64[kWarps];
-    int warp_int[kWarps];
-    u64 total;                           // of this CTA, for the others to read
-    int count;                           // of logits above -infinity
-    int tied;                            // of those that the cut ties
-    float top;
-    u64 found_above;                     // written by the CTA that finds it, in every CTA
-    int found_bin;
-    int token;
-    float log;
+struct alignas(16) Shared {                     // the cache of 16-byte blocks lies behind it
+    u64 bins[2][kBins];                        // the halves are added to apart.  Two: the one before is read by the other CTAs until the next barrier
+    u64 group[2][kMaxCtas][kGroups];           // of 32 bins each, of every CTA of the cluster
+    u64 weight[kWarps][kSteps];                // of a warp's consecutive blocks, and its logits that are tied
+    int ties[kWarps][kSteps];
+    long long table[kTable];                   // 2^62 2^(-j / 64)
+    double rate;                               // log2(e) / T, the sequence's, and what follows from it
+    float rate_high, rate_low, span, bin_rate;
+    double log_whole;
+    u64 warp_weight[kWarps];
+    int warp_ties[kWarps], warp_count[kWarps];
+    uint32_t warp_top[kWarps];
+    u64 total[kMaxCtas];                       // of every CTA; likewise the next three
+    int tied[kMaxCtas];
+    int count[kMaxCtas];                       // of logits above -infinity
+    uint32_t top[kMaxCtas];
+    u64 above, target;                         // found by warp 0
+    int position;
+    int token;                                 // written by the CTA that finds it, in every CTA
+    float logit;
 };
+static_assert(sizeof(Shared) % 16 == 0, "blocks behind it are aligned");
 
 template <typename V> __device__ __forceinline__ V *in_cta(V *p, uint32_t rank)
 {
@@ -97,361 +115,503 @@ template <typename V> __device__ __forceinline__ V *in_cta(V *p, uint32_t rank)
     return reinterpret_cast<V *>(r);
 }
 
-__device__ __forceinline__ u64 shfl_up64(u64 x, int o) { return __shfl_up_sync(0xFFFFFFFFu, x, o); }
-
-// Exclusive sums over the CTA's threads, of a weight and a count.
-__device__ __forceinline__ void scan_cta(u64 x, int n, Shared &s, u64 &x_before, int &n_before, u64 &x_total, int &n_total)
+__device__ __forceinline__ u64 sum_warp(u64 x)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    u64 xi = x;
-    int ni = n;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const u64 y = shfl_up64(xi, o);
-        const int m = __shfl_up_sync(0xFFFFFFFFu, ni, o);
-        if (lane >= o) {
-            xi += y;
-            ni += m;
-        }
-    }
-    __syncthreads();
-    if (lane == 31) {
-        s.warp_u64[warp] = xi;
-        s.warp_int[warp] = ni;
-    }
-    __syncthreads();
-    u64 xs = s.warp_u64[lane];
-    int ns = s.warp_int[lane];
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const u64 y = shfl_up64(xs, o);
-        const int m = __shfl_up_sync(0xFFFFFFFFu, ns, o);
-        if (lane >= o) {
-            xs += y;
-            ns += m;
-        }
-    }
-    x_total = __shfl_sync(0xFFFFFFFFu, xs, 31);
-    n_total = __shfl_sync(0xFFFFFFFFu, ns, 31);
-    const u64 xb = __shfl_sync(0xFFFFFFFFu, xs, max(warp - 1, 0));
-    const int nb = __shfl_sync(0xFFFFFFFFu, ns, max(warp - 1, 0));
-    x_before = (warp ? xb : 0) + xi - x;
-    n_before = (warp ? nb : 0) + ni - n;
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+    return x;
 }
-static_assert(kWarps == 32, "scan_cta: one sum a lane");
+// Inclusive sums over the lanes.
+template <typename V> __device__ __forceinline__ V scan_warp(V x)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const V y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        if (lane >= o) x += y;
+    }
+    return x;
+}
 
 template <typename T>
 struct Sampler {
     static constexpr int kVec = Row<T>::kVec;
     Shared &s;
+    uint4 *const cache;          // this CTA's first blocks in shared memory
+    const int cached;
     const uint32_t rank, ctas;
     const Row<T> row;
     int q0, q1;                  // this CTA's blocks
-    float top;                   // the row's largest logit
-    double rate;                 // 1 / T
-    __device__ __forceinline__ Sampler(Shared &s_, uint32_t rank_, uint32_t ctas_, const T *p, int V)
-        : s(s_), rank(rank_), ctas(ctas_), row(p, V), top(0.f), rate(1.)
+    float top, least;            // the row's largest logit; a logit that is not above `least` has no weight
+    float rate, rate_low;        // log2(e) / T
+    float top_high, top_low;     // top log2(e) / T, the first part a multiple of 1/64 and not less
+    float bin_rate;              // half logits to bins
+    int buffer;                  // histogram that is free
+    __device__ __forceinline__ Sampler(Shared &s_, uint4 *cache_, int cached_, uint32_t rank_, uint32_t ctas_, const T *p, int V)
+        : s(s_), cache(cache_), cached(cached_), rank(rank_), ctas(ctas_), row(p, V), buffer(0)
     {
         const int per = (row.blocks + ctas - 1) / ctas;
         q0 = min((int)rank * per, row.blocks);
         q1 = min(q0 + per, row.blocks);
     }
-    __device__ __forceinline__ u64 weight(float x) const
-    {
-        if (x == top) return (u64)kOne;
-        const double below = (double)x - (double)top;
-        return below > -INFINITY ? (u64)__double2ll_rn(exp(below * rate) * kOne) : 0;
-    }
-    __device__ __forceinline__ bool above(float x, const Cut &c) const { return x > -INFINITY && Order<T>::key(x) > c.key; }
-    __device__ __forceinline__ bool tied(float x, const Cut &c) const { return x > -INFINITY && Order<T>::key(x) == c.key; }
+    __device__ __forceinline__ void block(int q, float (&x)[kVec]) const { values<T>(q - q0 < cached ? cache[q - q0] : row.load(q), x); }
 
-    // The row's largest logit and how many logits there are above -infinity.
-    __device__ __forceinline__ int maximum()
+    // What weight() and bin() need of the temperature (one thread, once: fp64) and of the maximum.
+    static __device__ __forceinline__ void set_rate(Shared &s, double r)
     {
+        s.rate = r;
+        s.rate_high = (float)r;
+        s.rate_low = (float)(r - (double)s.rate_high);
+        s.span = (float)((double)kOctaves / r);
+        s.bin_rate = fminf((float)(2. * r * (kBins / (double)kOctaves)), 1e38f);
+    }
+    __device__ __forceinline__ void scales()
+    {
+        rate = s.rate_high;
+        rate_low = s.rate_low;
+        bin_rate = s.bin_rate;
+        const float t = __fmul_rn(top, rate);
+        top_high = ceilf(t * (float)kTable) * (1.f / kTable);
+        top_low = __fadd_rn(__fsub_rn(t, top_high), __fmaf_rn(top, rate_low, __fmaf_rn(top, rate, -t)));
+        least = fmaxf(top - s.span, -FLT_MAX);
+        if (!(least < top)) least = nextafterf(top, -INFINITY);
+    }
+    // 2^42 2^-y, y = (top - x) log2(e) / T, as a whole number: k = rint(64 y), 2^(-k / 64) is a power of two times a table's entry (Tang 1989),
+    // and 2^-r, r = y - k / 64, five terms of its series.  fp64 has an eighth of fp32's rate here, so r is computed as
+    // (top_high - k / 64 - x rate) + (top_low - x rate_low), whose first difference is exact and whose fma is rounded when what
+    // is large has gone: off by 2^-28 at most, relative to the weight.  That needs |top| log2(e) / T < 2^12; beyond (kWide), x - top comes first, as a sum of two
+    // floats (Knuth).  No branch: the chain is long, and a thread has several logits to do at once.
+    template <bool kWide> __device__ __forceinline__ u64 weight_by(float x) const
+    {
+        constexpr float kRound = 12582912.f;                                // 1.5 2^23: the sum's low bits are the nearest whole number
+        float near, r;
+        if constexpr (!kWide) {
+            near = __fmaf_rn(x, -(float)kTable * rate, __fmaf_rn(top_high, (float)kTable, kRound));
+            const float rest = __fmaf_rn(__fsub_rn(near, kRound), -1.f / kTable, top_high);       // exact
+            r = __fadd_rn(__fmaf_rn(-x, rate, rest), __fmaf_rn(-x, rate_low, top_low));
+        } else {
+            const float d = __fsub_rn(top, x), back = __fsub_rn(d, top);
+            const float d_low = __fsub_rn(__fsub_rn(top, __fsub_rn(d, back)), __fadd_rn(x, back));
+            const float y = __fmul_rn(d, rate);
+            near = __fmaf_rn(y, (float)kTable, kRound);
+            const float low = __fmaf_rn(d_low, rate, __fmaf_rn(d, rate_low, __fmaf_rn(d, rate, -y)));
+            r = __fadd_rn(__fmaf_rn(__fsub_rn(near, kRound), -1.f / kTable, y), low);
+        }
+        const int k = __float_as_int(near) - 0x4B400000;
+        constexpr float a = 0.6931471805599453f;
+        // (2^-r - 1) 2^32
+        const float e = __fmul_rn(r, __fmaf_rn(r, __fmaf_rn(r, __fmaf_rn(r, a * a * a * a / 24.f * 0x1p32f, a * a * a / -6.f * 0x1p32f), a * a / 2.f * 0x1p32f), -a * 0x1p32f));
+        const long long entry = s.table[k & (kTable - 1)];
+        const u64 w = (u64)(entry + (long long)(int)(entry >> 32) * __float2int_rn(e));
+        const u64 v = ((w >> 19 >> (k >> 6 & 63)) + 1) >> 1;
+        return x == top ? (u64)kOne : x > least ? v : 0;
+    }
+    __device__ __forceinline__ bool wide() const { return fabsf(top_high) >= 4096.f; }
+    __device__ __forceinline__ u64 weight(float x) const { return wide() ? weight_by<true>(x) : weight_by<false>(x); }
+    __device__ __forceinline__ void weights(const float (&x)[kVec], u64 (&w)[kVec]) const
+    {
+        if (!wide()) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) w[i] = weight_by<false>(x[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) w[i] = weight_by<true>(x[i]);
+        }
+    }
+    // Weights above the cut and logits at it, of a block; all lanes of a warp together.
+    __device__ __forceinline__ void sums(const float (&x)[kVec], const Cut &cut, u64 &w, int &n) const
+    {
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            any |= x[i] > cut.x && x[i] > least;
+            n += x[i] == cut.x;
+        }
+        if (!__any_sync(0xFFFFFFFFu, any)) return;
+        u64 v[kVec];
+        weights(x, v);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) w += x[i] > cut.x ? v[i] : 0;
+    }
+    // Bin of equal widths, from the largest logit down; it does not fall where x falls.  (Halves: no overflow.)
+    __device__ __forceinline__ int bin(float x) const
+    {
+        return x == top ? 0 : (int)fminf((0.5f * top - 0.5f * x) * bin_rate, (float)(kBins - 1));
+    }
+    // A number that no logit of bins 0 .. b is below, but few of the others: the edge, moved by more than the roundings of bin().
+    __device__ __forceinline__ float edge(int b) const
+    {
+        if (b >= kBins - 1 || !(bin_rate > 0.f) || !(top < INFINITY)) return -FLT_MAX;
+        return fmaxf(__double2float_rd((double)top - (b + 1) * (2. / (double)bin_rate * (1. + 0x1p-20))), -FLT_MAX);
+    }
+    static __device__ __forceinline__ uint32_t key(float x) { return float_to_ordered(x + 0.f) >> Logit<T>::kGrain; }
+    static __device__ __forceinline__ float of_key(uint32_t k)
+    {
+        constexpr int low = Logit<T>::kGrain;
+        const uint32_t u = k << low;
+        return ordered_to_float(u & 0x80000000u ? u : u | ((1u << low) - 1));
+    }
+
+    // The row's largest logit and how many logits there are above -infinity.  Fills the cache; `mine`: the thread's largest.
+    __device__ __forceinline__ int maximum(float &mine)
+    {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         float m = -INFINITY;
         int n = 0;
+#pragma unroll 4
         for (int q = q0 + threadIdx.x; q < q1; q += kThreads) {
+            const uint4 w = row.load(q);
+            if (q - q0 < cached) cache[q - q0] = w;
             float x[kVec];
-            row.load(q, x);
+            values<T>(w, x);
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
                 m = fmaxf(m, x[i]);
                 n += x[i] > -INFINITY;
             }
         }
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        mine = m;
         n = __reduce_add_sync(0xFFFFFFFFu, n);
-        uint32_t k = __reduce_max_sync(0xFFFFFFFFu, float_to_ordered(m));
-        __syncthreads();
+        uint32_t k = __reduce_max_sync(0xFFFFFFFFu, float_to_ordered(m + 0.f));
         if (lane == 0) {
-            s.warp_int[warp] = n;
-            s.warp_u64[warp] = k;
+            s.warp_count[warp] = n;
+            s.warp_top[warp] = k;
         }
         __syncthreads();
         if (warp == 0) {
-            n = __reduce_add_sync(0xFFFFFFFFu, s.warp_int[lane]);
-            k = __reduce_max_sync(0xFFFFFFFFu, (uint32_t)s.warp_u64[lane]);
-            if (lane == 0) {
-                s.count = n;
-                s.top = ordered_to_float(k);
+            n = __reduce_add_sync(0xFFFFFFFFu, lane < kWarps ? s.warp_count[lane] : 0);
+            k = __reduce_max_sync(0xFFFFFFFFu, lane < kWarps ? s.warp_top[lane] : 0u);
+            if (lane < (int)ctas) {
+                *in_cta(&s.count[rank], lane) = n;
+                *in_cta(&s.top[rank], lane) = k;
             }
         }
         cluster_sync_all();
-        top = -INFINITY;
-        n = 0;
-        for (uint32_t c = 0; c < ctas; ++c) {
-            top = fmaxf(top, *in_cta(&s.top, c));
-            n += *in_cta(&s.count, c);
-        }
+        const bool there = lane < (int)ctas;
+        n = __reduce_add_sync(0xFFFFFFFFu, there ? s.count[lane] : 0);
+        top = ordered_to_float(__reduce_max_sync(0xFFFFFFFFu, there ? s.top[lane] : 0u));
         return n;
     }
 
-    // Sum over the cluster of what remains behind `cut`.
-    __device__ __forceinline__ u64 sum(const Cut &cut)
+    // Frees a histogram; by the threads from `from` on.
+    __device__ __forceinline__ void clear(int which, int from)
     {
-        u64 w = 0;
-        for (int q = q0 + threadIdx.x; q < q1; q += kThreads) {
-            float x[kVec];
-            row.load(q, x);
+        uint4 *bins = reinterpret_cast<uint4 *>(s.bins[which]);
+        for (int i = (int)threadIdx.x - from; i < kBins / 2; i += kThreads - from) bins[i] = make_uint4(0, 0, 0, 0);
+    }
+    // Adds `v` to positions at[i] >= 0 of the free histogram.  The low halves first, all of them on their way before a carry is looked at.
+    template <bool by_weight, int kCount> __device__ __forceinline__ void add(const int (&at)[kCount], const u64 (&v)[kCount])
+    {
+        uint32_t old[kCount];
 #pragma unroll
-            for (int i = 0; i < kVec; ++i)
-                if (above(x[i], cut)) w += weight(x[i]);
+        for (int i = 0; i < kCount; ++i)
+            if (at[i] >= 0) old[i] = atomicAdd(reinterpret_cast<uint32_t *>(s.bins[buffer] + at[i]), (uint32_t)v[i]);
+        if (by_weight) {
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) {
+                const uint32_t hi = (uint32_t)(v[i] >> 32) + (old[i] + (uint32_t)v[i] < old[i] ? 1u : 0u);
+                if (at[i] >= 0 && hi) atomicAdd(reinterpret_cast<uint32_t *>(s.bins[buffer] + at[i]) + 1, hi);
+            }
         }
-        u64 xb, xt;
-        int nb, nt;
-        scan_cta(w, 0, s, xb, nb, xt, nt);
-        if (threadIdx.x == 0) s.total = xt;
-        cluster_sync_all();
-        w = 0;
-        for (uint32_t c = 0; c < ctas; ++c) w += *in_cta(&s.total, c);
-        cluster_sync_all();
-        return w + (u64)cut.ties * weight_of(cut.key);
     }
-    __device__ __forceinline__ u64 weight_of(uint32_t key) const       // of the logit with this key
+    template <bool by_weight> __device__ __forceinline__ void add_one(int at, u64 v)
     {
-        constexpr int low = 32 - Order<T>::kBits;
-        const uint32_t u = key << low;
-        return weight(ordered_to_float(u & 0x80000000u ? u : u | ((1u << low) - 1)));
+        const int where[1] = {at};
+        const u64 what[1] = {v};
+        add<by_weight, 1>(where, what);
     }
-
-    // The shortest part of `cut`, in descending order and then by index, whose elements' weights (counts) reach `target`, which is
-    // positive and not more than they have in all.
-    template <bool by_weight>
-    __device__ __forceinline__ Cut select(const Cut &cut, u64 target)
+    // The first position of the cluster's histogram whose running sum, `before` included, reaches `target`; what lies before it replaces `before`.
+    // positions: a multiple of 32.  share >= 0: the target is that share of all.  Frees the other histogram.
+    __device__ __forceinline__ int find(int positions, u64 &before, u64 &target, float share)
     {
-        uint32_t prefix = 0;
-        u64 before = 0;
-        for (int pass = 0; pass < Order<T>::kPasses; ++pass) {
-            const int shift = Order<T>::shift(pass), width = Order<T>::width(pass), bins = 1 << width;
-            const bool all = pass == 0;
-            for (int i = threadIdx.x; i < kBins; i += kThreads) s.bins[i] = 0;
-            __syncthreads();
-            for (int q = q0 + threadIdx.x; q < q1; q += kThreads) {
-                float x[kVec];
-                row.load(q, x);
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        __syncthreads();
+        if (positions > 32) {
+            // four threads a group; each has the sum and sends it to a quarter of the cluster
+            static_assert(kThreads == 4 * kGroups, "four threads a group");
+            const ulonglong2 *mine = reinterpret_cast<const ulonglong2 *>(s.bins[buffer] + threadIdx.x * 8);
+            u64 v = 0;
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    const uint32_t k = Order<T>::key(x[i]);
-                    if (above(x[i], cut) && (all || k >> (shift + width) == prefix))
-                        atomicAdd(s.bins + (k >> shift & (bins - 1)), by_weight ? weight(x[i]) : 1ull);
-                }
-            }
-            if (rank == 0 && threadIdx.x == 0 && cut.ties > 0 && (all || cut.key >> (shift + width) == prefix))
-                atomicAdd(s.bins + (cut.key >> shift & (bins - 1)), (u64)cut.ties * (by_weight ? weight_of(cut.key) : 1ull));
-            cluster_sync_all();
-            // bins are summed over the cluster by the CTA whose part they are, and searched from the largest key down:
-            // position i stands for bin bins - 1 - i
-            const int part = bins / ctas, first = (int)rank * part;
-            u64 mine = 0;
-            const int each = (part + kThreads - 1) / kThreads;
-            for (int j = 0; j < each; ++j) {
-                const int i = threadIdx.x * each + j;
-                if (i >= part) break;
-                u64 v = 0;
-                for (uint32_t c = 0; c < ctas; ++c) v += *in_cta(s.bins + (bins - 1 - first - i), c);
-                s.sums[i] = v;
-                mine += v;
-            }
-            u64 mine_before, total;
-            int nb, nt;
-            scan_cta(mine, 0, s, mine_before, nb, total, nt);
-            if (threadIdx.x == 0) s.total = total;
-            cluster_sync_all();
+            for (int i = 0; i < 4; ++i) v += mine[i].x + mine[i].y;
+            v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+            v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+            for (uint32_t c = threadIdx.x & 3; c < ctas; c += 4) *in_cta(&s.group[buffer][rank][threadIdx.x >> 2], c) = v;
+        }
+        cluster_sync_all();
+        if (warp == 0) {                                  // of every CTA, alike
             u64 at = before;
-            for (uint32_t c = 0; c < rank; ++c) at += *in_cta(&s.total, c);
-            at += mine_before;
-            if (at < target && at + mine >= target) {           // one thread of the cluster
-                for (int j = 0; j < each; ++j) {
-                    const u64 v = s.sums[threadIdx.x * each + j];
-                    if (at + v >= target) {
-                        for (uint32_t c = 0; c < ctas; ++c) {
-                            *in_cta(&s.found_bin, c) = bins - 1 - first - (threadIdx.x * each + j);
-                            *in_cta(&s.found_above, c) = at;
-                        }
-                        break;
-                    }
-                    at += v;
+            int g = 0;
+            if (positions > 32) {
+                u64 a = 0, b = 0;
+#pragma unroll
+                for (uint32_t c = 0; c < kMaxCtas; ++c) {
+                    const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(&s.group[buffer][c][2 * lane]);
+                    a += c < ctas ? v.x : 0;
+                    b += c < ctas ? v.y : 0;
+                }
+                const u64 up_to = scan_warp(a + b);
+                if (share >= 0.f) {
+                    const u64 all = __shfl_sync(0xFFFFFFFFu, up_to, 31);
+                    target = max((u64)__double2ll_ru((double)share * (double)all), 1ull);
+                }
+                const unsigned m = __ballot_sync(0xFFFFFFFFu, at + up_to >= target);
+                const int l = m ? __ffs(m) - 1 : 31;
+                at += __shfl_sync(0xFFFFFFFFu, up_to - a - b, l);
+                const u64 one = __shfl_sync(0xFFFFFFFFu, a, l);
+                g = 2 * l;
+                if (at + one < target) {
+                    at += one;
+                    ++g;
                 }
             }
-            cluster_sync_all();
-            prefix = prefix << width | (uint32_t)s.found_bin;
-            before = s.found_above;
+            u64 v = 0, y[kMaxCtas];
+#pragma unroll
+            for (uint32_t c = 0; c < kMaxCtas; ++c) y[c] = *in_cta(&s.bins[buffer][g * 32 + lane], min(c, ctas - 1));   // all on their way at once
+#pragma unroll
+            for (uint32_t c = 0; c < kMaxCtas; ++c) v += c < ctas ? y[c] : 0;
+            const u64 run = scan_warp(v);
+            const unsigned m = __ballot_sync(0xFFFFFFFFu, at + run >= target);
+            const int l = m ? __ffs(m) - 1 : 31;
+            at += __shfl_sync(0xFFFFFFFFu, run - v, l);
+            if (lane == 0) {
+                s.position = g * 32 + l;
+                s.above = at;
+                s.target = target;
+            }
+        } else {
+            clear(buffer ^ 1, 32);                        // nobody reads the last one any more
         }
-        const u64 one = by_weight ? weight_of(prefix) : 1ull;
-        return Cut{prefix, (int)((target - before + one - 1) / one)};
+        __syncthreads();
+        before = s.above;
+        target = s.target;
+        buffer ^= 1;
+        return s.position;
+    }
+    // f(x) for blocks from .. to - 1 in turn, `stride` at a time, the next load ahead; f is called by whole warps (what is not there is
+    // -infinity).  One copy of f: at depth 0 its instructions come from far.
+    template <typename F> __device__ __forceinline__ void each_block(int from, int to, int stride, F &&f) const
+    {
+        const int me = stride == 32 ? threadIdx.x & 31 : threadIdx.x;
+        auto load = [&](int q) {
+            constexpr uint32_t low = Logit<T>::kLowest;
+            return q >= to ? make_uint4(low, low, low, low) : q - q0 < cached ? cache[q - q0] : row.load(q);
+        };
+        uint4 next = load(from + me);
+#pragma unroll 1
+        for (int base = from, j = 0; base < to; base += stride, ++j) {
+            float x[kVec];
+            values<T>(next, x);
+            next = load(base + stride + me);
+            f(x, j);
+        }
     }
 
-    // Draws from what remains behind `cut` (greedy: the first of the largest); returns the token, -1 if nothing remains.
-    __device__ __forceinline__ int draw(const Cut &cut, float u, bool greedy, float &log)
+    // The shortest part of `cut`, in descending order and then by index, whose weights reach the share `p` of all its weights (by weight), or that
+    // has `k` logits (otherwise; it has more in all).  mine: the thread's largest logit.
+    template <bool by_weight>
+    __device__ __forceinline__ Cut select(const Cut &cut, float p, u64 k, float mine)
+    {
+        u64 before = 0, target = k;
+        float low = by_weight ? least : -FLT_MAX;             // logits below are not looked at
+        if (!by_weight && row.blocks > 4 * kThreads * (int)ctas && k <= kThreads / 2) {
+            // The k-th largest of the threads' largest logits is not above the k-th largest of all: few are left to be counted.
+            if (mine > cut.x) add_one<false>(bin(mine), 1);
+            u64 none = 0, aim = k;
+            low = edge(find(kBins, none, aim, -1.f));
+        }
+        // the first histogram
+        each_block(q0, q1, kThreads, [&](const float (&x)[kVec], int) {
+            bool any = false;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) any |= x[i] > cut.x && x[i] >= low;
+            if (!__any_sync(0xFFFFFFFFu, any)) return;
+            u64 v[kVec];
+            int at[kVec];
+            if (by_weight) weights(x, v);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                if (!by_weight) v[i] = 1;
+                at[i] = x[i] > cut.x && x[i] >= low && v[i] > 0 ? bin(x[i]) : -1;
+            }
+            add<by_weight, kVec>(at, v);
+        });
+        const bool first = rank == 0 && threadIdx.x == 0;
+        if (first && cut.ties > 0) add_one<by_weight>(bin(cut.x), (u64)cut.ties * (by_weight ? weight(cut.x) : 1));
+        const int hit = find(kBins, before, target, by_weight ? p : -1.f);
+        // keys that the bin can have, and a few more
+        float most = top, bottom = edge(hit);
+        if (hit > 0 && bin_rate > 0.f && top < INFINITY)
+            most = fminf(top, __double2float_ru((double)top - hit * (2. / (double)bin_rate * (1. - 0x1p-20))));
+        while (true) {
+            const uint32_t hi = key(most), lo = key(bottom);
+            const int shift = max(32 - __clz(hi - lo) - 11, 0);
+            each_block(q0, q1, kThreads, [&](const float (&x)[kVec], int) {
+                bool any = false;
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) any |= x[i] > cut.x && x[i] >= bottom && x[i] <= most;
+                if (!__any_sync(0xFFFFFFFFu, any)) return;
+                unsigned few = 0;
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) few |= x[i] > cut.x && x[i] >= bottom && x[i] <= most ? 1u << i : 0u;
+#pragma unroll 1
+                for (; few; few &= few - 1) {
+                    float one = x[0];
+#pragma unroll
+                    for (int i = 1; i < kVec; ++i) one = few >> i & 1 && !(few & ((1u << i) - 1)) ? x[i] : one;
+                    if (bin(one) != hit) continue;
+                    const u64 v = by_weight ? weight(one) : 1;
+                    if (v > 0) add_one<by_weight>((int)((hi - key(one)) >> shift), v);
+                }
+            });
+            if (first && cut.ties > 0 && cut.x >= bottom && cut.x <= most && bin(cut.x) == hit)
+                add_one<by_weight>((int)((hi - key(cut.x)) >> shift), (u64)cut.ties * (by_weight ? weight(cut.x) : 1));
+            const uint32_t at = (uint32_t)find(((int)((hi - lo) >> shift) | 31) + 1, before, target, -1.f);
+            const uint32_t key_hi = hi - (at << shift);
+            most = of_key(key_hi);
+            if (shift == 0) break;
+            bottom = of_key(max(lo, key_hi - ((1u << shift) - 1)));
+        }
+        const u64 one = by_weight ? weight(most) : 1;
+        return Cut{most, (int)((target - before + one - 1) / one)};
+    }
+
+    // Draws from what remains behind `cut` (greedy: the first of the largest); returns the token.
+    __device__ __forceinline__ int draw(const Cut &cut, float u, bool greedy, float &logit)
     {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         // a warp has `per` consecutive blocks, 32 at a time; an entry sums up 1 << fold of these steps
         const int per = (q1 - q0 + kWarps - 1) / kWarps, w0 = min(q0 + warp * per, q1), w1 = min(w0 + per, q1);
         const int steps = (per + 31) / 32;
         int fold = 0;
-        while (((steps + (1 << fold) - 1) >> fold) * kWarps > kEntries) ++fold;
-        const int entries = (steps + (1 << fold) - 1) >> fold;      // of a warp
-        for (int e = 0; e < entries; ++e) {
-            u64 w = 0;
-            int n = 0;
-            for (int j = e << fold; j < min(steps, (e + 1) << fold); ++j) {
-                const int q = w0 + j * 32 + lane;
-                if (q >= w1) continue;
-                float x[kVec];
-                row.load(q, x);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    if (above(x[i], cut)) w += weight(x[i]);
-                    n += tied(x[i], cut);
-                }
+        while (((steps + (1 << fold) - 1) >> fold) > kSteps) ++fold;
+        u64 w_warp = 0, w = 0;
+        int n_warp = 0, n = 0;
+        each_block(w0, w1, 32, [&](const float (&x)[kVec], int j) {
+            sums(x, cut, w, n);
+            if ((j + 1) % (1 << fold) != 0 && j + 1 < (w1 - w0 + 31) / 32) return;
+            const bool some = __any_sync(0xFFFFFFFFu, w != 0 || n != 0);
+            if (some) {
+                w = sum_warp(w);
+                n = __reduce_add_sync(0xFFFFFFFFu, n);
             }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xFFFFFFFFu, w, o);
-            n = __reduce_add_sync(0xFFFFFFFFu, n);
             if (lane == 0) {
-                s.weight[warp * entries + e] = w;
-                s.ties[warp * entries + e] = n;
+                s.weight[warp][j >> fold] = w;
+                s.ties[warp][j >> fold] = n;
             }
+            w_warp += w;
+            n_warp += n;
+            w = 0;
+            n = 0;
+        });
+        const int mine_entries = ((w1 - w0 + 31) / 32 + (1 << fold) - 1) >> fold;
+        if (lane == 0) {
+            s.warp_weight[warp] = w_warp;
+            s.warp_ties[warp] = n_warp;
         }
         __syncthreads();
-        const int each = (kWarps * entries + kThreads - 1) / kThreads;
-        u64 w = 0, w_before, w_total;
-        int n = 0, n_before, n_total;
-        for (int j = 0; j < each; ++j) {
-            const int e = threadIdx.x * each + j;
-            if (e < kWarps * entries) {
-                w += s.weight[e];
-                n += s.ties[e];
+        // every warp: sums before it in the CTA
+        const u64 w_lane = lane < kWarps ? s.warp_weight[lane] : 0;
+        const int n_lane = lane < kWarps ? s.warp_ties[lane] : 0;
+        const u64 w_scan = scan_warp(w_lane);
+        const int n_scan = scan_warp(n_lane);
+        if (threadIdx.x == 0) s.token = -1;
+        if (warp == 0) {
+            const u64 w_sum = __shfl_sync(0xFFFFFFFFu, w_scan, 31);
+            const int n_sum = __shfl_sync(0xFFFFFFFFu, n_scan, 31);
+            if (lane < (int)ctas) {
+                *in_cta(&s.total[rank], lane) = w_sum;
+                *in_cta(&s.tied[rank], lane) = n_sum;
             }
         }
-        scan_cta(w, n, s, w_before, n_before, w_total, n_total);
-        if (threadIdx.x == 0) {
-            s.total = w_total;
-            s.tied = n_total;
-            s.token = -1;
-            s.log = 0.f;
-        }
+        const u64 tie = cut.ties > 0 ? weight(cut.x) : 0;
         cluster_sync_all();
-        const u64 tie = weight_of(cut.key);
-        u64 whole = 0;
-        for (uint32_t c = 0; c < ctas; ++c) {
-            const u64 wc = *in_cta(&s.total, c);
-            const int nc = *in_cta(&s.tied, c);
-            if (c < rank) {
-                w_before += wc;
-                n_before += nc;
-            }
-            whole += wc;
+        u64 whole = (u64)cut.ties * tie, w_before = __shfl_sync(0xFFFFFFFFu, w_scan - w_lane, warp);
+        int n_before = __shfl_sync(0xFFFFFFFFu, n_scan - n_lane, warp);
+#pragma unroll
+        for (uint32_t c = 0; c < kMaxCtas; ++c) {
+            const u64 v = s.total[c];
+            whole += c < ctas ? v : 0;
+            w_before += c < rank ? v : 0;
+            n_before += c < rank ? s.tied[c] : 0;
         }
-        whole += (u64)cut.ties * tie;
         // the first element whose running sum passes `aim`
         const u64 aim = greedy ? 0 : (u64)__double2ll_rz((double)fminf(fmaxf(u, 0.f), 1.f - 0x1p-24f) * (double)whole);
         auto running = [&](u64 weight_before, int ties_before) { return weight_before + (u64)min(ties_before, cut.ties) * tie; };
-        if (running(w_before, n_before) <= aim && running(w_before + w, n_before + n) > aim) {    // one thread of the cluster
-            for (int j = 0; j < each; ++j) {
-                const int e = threadIdx.x * each + j;
-                if (running(w_before + s.weight[e], n_before + s.ties[e]) > aim) {
-                    s.found_bin = e;
-                    s.found_above = w_before;
-                    s.warp_int[0] = n_before;
-                    break;
+        if (running(w_before, n_before) <= aim && running(w_before + w_warp, n_before + n_warp) > aim) {     // one warp of the cluster
+            // the entry
+            int e = 0;
+            if (mine_entries > 1)
+                while (true) {
+                    const u64 w = e + lane < mine_entries ? s.weight[warp][e + lane] : 0;
+                    const int n = e + lane < mine_entries ? s.ties[warp][e + lane] : 0;
+                    const u64 ws = scan_warp(w);
+                    const int ns = scan_warp(n);
+                    const unsigned m = __ballot_sync(0xFFFFFFFFu, running(w_before + ws, n_before + ns) > aim);
+                    const int l = m ? __ffs(m) - 1 : 31;
+                    w_before += __shfl_sync(0xFFFFFFFFu, m ? ws - w : ws, l);
+                    n_before += __shfl_sync(0xFFFFFFFFu, m ? ns - n : ns, l);
+                    if (m || e + 32 >= mine_entries) {
+                        e = min(e + l, mine_entries - 1);
+                        break;
+                    }
+                    e += 32;
                 }
-                w_before += s.weight[e];
-                n_before += s.ties[e];
-            }
-        } else {
-            n_before = -1;
-        }
-        const bool here = __syncthreads_or(n_before >= 0);
-        if (here && warp == 0) {
-            const int e = s.found_bin, of = e / entries, j0 = (e % entries) << fold;
-            const int v0 = min(q0 + of * per, q1), v1 = min(v0 + per, q1);
-            u64 sum = s.found_above;
-            int ties = s.warp_int[0];
-            for (int j = j0; j < min(steps, j0 + (1 << fold)); ++j) {
-                const int q = v0 + j * 32 + lane;
+            // its step, lane and element
+            for (int j = e << fold; j < steps; ++j) {
                 float x[kVec];
-                u64 mine = 0;
-                int count = 0;
-                if (q < v1) {
-                    row.load(q, x);
+                u64 w = 0;
+                int n = 0;
+                const int q = w0 + j * 32 + lane;
 #pragma unroll
-                    for (int i = 0; i < kVec; ++i) {
-                        if (above(x[i], cut)) mine += weight(x[i]);
-                        count += tied(x[i], cut);
-                    }
-                }
-                u64 mine_inc = mine;
-                int count_inc = count;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const u64 y = shfl_up64(mine_inc, o);
-                    const int m = __shfl_up_sync(0xFFFFFFFFu, count_inc, o);
-                    if (lane >= o) {
-                        mine_inc += y;
-                        count_inc += m;
-                    }
-                }
-                const bool in = running(sum + mine_inc, ties + count_inc) > aim;
-                const unsigned m = __ballot_sync(0xFFFFFFFFu, in);
+                for (int i = 0; i < kVec; ++i) x[i] = -INFINITY;
+                if (q < w1) block(q, x);
+                sums(x, cut, w, n);
+                const u64 ws = scan_warp(w);
+                const int ns = scan_warp(n);
+                const unsigned m = __ballot_sync(0xFFFFFFFFu, running(w_before + ws, n_before + ns) > aim);
                 if (m == 0) {
-                    sum += __shfl_sync(0xFFFFFFFFu, mine_inc, 31);
-                    ties += __shfl_sync(0xFFFFFFFFu, count_inc, 31);
+                    w_before += __shfl_sync(0xFFFFFFFFu, ws, 31);
+                    n_before += __shfl_sync(0xFFFFFFFFu, ns, 31);
                     continue;
                 }
-                if (lane == __ffs(m) - 1) {
-                    sum += mine_inc - mine;
-                    ties += count_inc - count;
-                    bool done = false;
+                // element i of that lane's block is looked at by lane i
+                const int l = __ffs(m) - 1;
+                w_before += __shfl_sync(0xFFFFFFFFu, ws - w, l);
+                n_before += __shfl_sync(0xFFFFFFFFu, ns - n, l);
+                float mine = -INFINITY;
 #pragma unroll
-                    for (int i = 0; i < kVec; ++i) {
-                        if (above(x[i], cut)) sum += weight(x[i]);
-                        ties += tied(x[i], cut);
-                        if (!done && running(sum, ties) > aim) {
-                            done = true;
-                            const float l = greedy ? 0.f : (float)((x[i] == top ? 0. : ((double)x[i] - (double)top) * rate) - ::log((double)whole / kOne));
-                            for (uint32_t c = 0; c < ctas; ++c) {
-                                *in_cta(&s.token, c) = q * kVec + i - row.first;
-                                *in_cta(&s.log, c) = l;
-                            }
-                        }
-                    }
+                for (int i = 0; i < kVec; ++i) {
+                    const float y = __shfl_sync(0xFFFFFFFFu, x[i], l);
+                    if (lane == i) mine = y;
+                }
+                const u64 one = weight(mine), we = scan_warp(mine > cut.x ? one : 0);
+                const int ne = scan_warp((int)(mine == cut.x));
+                const int i = __ffs(__ballot_sync(0xFFFFFFFFu, running(w_before + we, n_before + ne) > aim)) - 1;
+                const int token = (w0 + j * 32 + l) * kVec + i - row.first;
+                mine = __shfl_sync(0xFFFFFFFFu, mine, i);
+                if (lane < (int)ctas) {
+                    *in_cta(&s.token, lane) = token;
+                    *in_cta(&s.logit, lane) = mine;
                 }
                 break;
             }
         }
+        if (threadIdx.x == 32 && rank == 0) s.log_whole = ::log((double)whole / kOne);      // meanwhile
         cluster_sync_all();
-        log = s.log;
+        logit = s.logit;
         return s.token;
     }
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a)
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a, int cached)
 {
-    __shared__ Shared s;
+    extern __shared__ __align__(16) uint8_t smem[];
+    Shared &s = *reinterpret_cast<Shared *>(smem);
+    uint4 *cache = reinterpret_cast<uint4 *>(smem + sizeof(Shared));
     const uint32_t rank = cluster_ctarank(), ctas = a.ctas;
     const int b = blockIdx.x / ctas;
+    if (threadIdx.x < kTable) s.table[threadIdx.x] = __double2ll_rn(exp2(62. - (double)threadIdx.x / kTable));
     pdl_wait();
     pdl_launch_dependents();
     const int n = a.n, L = a.L;
@@ -465,26 +625,29 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a)
     unsigned live = 0;
     for (int r = 0; r < n; ++r) live |= (a.valid[(long long)b * n + r] != 0 ? 1u : 0u) << r;
     int best = __ffs(live) - 1, t = 0;
+    // an infinite temperature times infinitely small a logit would be no number
+    if (threadIdx.x == 64) Sampler<T>::set_rate(s, greedy ? 1. : 1.4426950408889634 / (double)fminf(temperature, 1e36f));
     while (true) {
         const int at = t == 0 ? 0 : 1 + best * L + t - 1;
-        Sampler<T> one(s, rank, ctas, logits + (long long)at * a.row_stride, a.V);
-        const int valid = one.maximum();
-        one.rate = greedy ? 1. : 1. / (double)temperature;
-        Cut cut{0, 0};                                        // all: no logit has key 0
-        if (greedy) cut = Cut{Order<T>::key(one.top), 1};
+        Sampler<T> one(s, cache, cached, rank, ctas, logits + (long long)at * a.row_stride, a.V);
+        const float u = a.uniform[(long long)b * (L + 1) + t];
+        one.clear(0, 0);
+        float mine;
+        const int valid = one.maximum(mine);
+        one.scales();
+        Cut cut{-INFINITY, 0};
+        if (greedy) cut = Cut{one.top, 1};
         else if (valid > 0) {
-            if (top_k > 0 && top_k < valid) cut = one.template select<false>(cut, top_k);
-            if (top_p < 1.f) {
-                const u64 all = one.sum(cut);
-                const u64 target = (u64)__double2ll_ru((double)fmaxf(top_p, 0.f) * (double)all);
-                cut = one.template select<true>(cut, max(target, 1ull));
-            }
+            if (top_k > 0 && top_k < valid) cut = one.template select<false>(cut, 0.f, top_k, mine);
+            if (top_p < 1.f) cut = one.template select<true>(cut, fmaxf(top_p, 0.f), 0, mine);
         }
-        float log = 0.f;
-        const int token = valid > 0 ? one.draw(cut, a.uniform[(long long)b * (L + 1) + t], greedy, log) : -1;
+        float logit = 0.f;
+        const int token = valid > 0 ? one.draw(cut, u, greedy, logit) : -1;
         if (rank == 0 && threadIdx.x == 0) {
             a.out_tokens[(long long)b * (L + 1) + t] = token;
-            if (a.out_logs) a.out_logs[(long long)b * (L + 1) + t] = log;
+            if (a.out_logs)
+                a.out_logs[(long long)b * (L + 1) + t] =
+                    greedy || token < 0 ? 0.f : (float)((logit == one.top ? 0. : ((double)logit - (double)one.top) * (s.rate * 0.6931471805599453)) - s.log_whole);
         }
         ++t;
         unsigned next = 0;
@@ -496,7 +659,6 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a)
         if (next == 0) break;
         live = next;
         best = __ffs(live) - 1;
-        cluster_sync_all();                                   // the shared words are read no more
     }
     if (rank == 0) {
         if (threadIdx.x == 0) {
@@ -508,17 +670,27 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a)
             if (a.out_logs) a.out_logs[(long long)b * (L + 1) + i] = 0.f;
         }
     }
-    cluster_sync_all();
+    cluster_sync_all();                                       // a row without logits leaves the others' words unread until here
 }
 
-}  // namespace
-
-cudaError_t launch_sample(const SampleArgs &args, int dtype, int sms, cudaStream_t stream)
+template <typename T> cudaError_t launch(SampleArgs a, int sms, cudaStream_t stream)
 {
-    SampleArgs a = args;
-    // CTAs of a cluster: as many as the sequences leave SMs for, each with 2048 logits at least
+    // CTAs of a cluster: as many as are resident at once, two a SM, each with 1024 logits at least
     a.ctas = 1;
-    while (a.ctas < kMaxCtas && a.B * a.ctas * 2 <= sms && a.V / (a.ctas * 2) >= 2048) a.ctas *= 2;
+    while (a.ctas < kMaxCtas && a.B * a.ctas * 2 <= 2 * sms && a.V / (a.ctas * 2) >= 1024) a.ctas *= 2;
+    // a row's piece is kept in shared memory as far as it goes
+    const int vec = 16 / (int)sizeof(T), blocks = (a.V + 2 * vec - 2) / vec, per = (blocks + a.ctas - 1) / a.ctas;
+    const int room = (int)(((a.B * a.ctas <= sms ? 225 : 112) * 1024 - sizeof(Shared)) / 16), cached = per < room ? per : room;
+    const size_t smem = sizeof(Shared) + 16 * (size_t)cached;
+    static std::atomic<bool> ready[64];                       // by device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && (dev >= 64 || !ready[dev])) {
+        e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e == cudaSuccess && dev < 64) ready[dev] = true;
+    }
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -528,12 +700,18 @@ cudaError_t launch_sample(const SampleArgs &args, int dtype, int sms, cudaStream
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.gridDim = dim3(a.B * a.ctas);
     cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return dtype == kF16    ? cudaLaunchKernelEx(&cfg, sample_kernel<__half>, a)
-           : dtype == kBF16 ? cudaLaunchKernelEx(&cfg, sample_kernel<__nv_bfloat16>, a)
-                            : cudaLaunchKernelEx(&cfg, sample_kernel<float>, a);
+    return cudaLaunchKernelEx(&cfg, sample_kernel<T>, a, cached);
+}
+
+}  // namespace
+
+cudaError_t launch_sample(const SampleArgs &a, int dtype, int sms, cudaStream_t stream)
+{
+    return dtype == kF16 ? launch<__half>(a, sms, stream) : dtype == kBF16 ? launch<__nv_bfloat16>(a, sms, stream) : launch<float>(a, sms, stream);
 }
 
 }  // namespace dresd
