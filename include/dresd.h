@@ -315,7 +315,8 @@ dresd_status dresd_drafts_sample(const void *logits, dresd_dtype dtype, int64_t 
  *     out            [rows][outputs], out_row apart
  *   Products of (c - 8) and x are exact, their sums and the scales' products in fp32; one rounding, to `dtype`.  The order of
  *   summation depends on the sizes only.
- * Asynchronous on `stream`, on the current device; no workspace.
+ * Both are asynchronous on `stream`, on the current device; no workspace.
+ * dresd_w4_status    dresd_store_status() for these calls: waits for `stream`, reports and clears the current device's status word.
  */
 enum { DRESD_MAX_W4_SIZE = 1 << 20 };
 dresd_status dresd_w4_quantise(const void *w, int64_t w_in, int64_t w_out, int inputs, int outputs, dresd_dtype dtype, int group,
@@ -323,6 +324,7 @@ dresd_status dresd_w4_quantise(const void *w, int64_t w_in, int64_t w_out, int i
 dresd_status dresd_w4_matmul(const void *x, int64_t x_row, int rows, const uint8_t *codes, const void *scales, int inputs, int outputs,
                              dresd_dtype dtype, int group, int relu, const void *residual, int64_t residual_row, void *out,
                              int64_t out_row, void *stream);
+dresd_status dresd_w4_status(void *stream);
 
 /*
  * Paged key/value cache of the language model that verifies the drafts, and its attention.
@@ -500,6 +502,10 @@ int dresd_kv_last_launches(const dresd_kv *kv);
  *                       leader of the first pair) never receives the copies of pipeline stage
  *                       (value-1), so its waits run out: the kernel returns in an orderly way and
  *                       the call returns DRESD_ERR_TIMEOUT.  0 = off.
+ *   "w4_path"           dresd_w4_matmul: 0 = automatic (by rows), 1 = the mma.sync kernel, 2 = the tcgen05 kernel
+ *   "w4_wait_ms"        bound of its device-side waits in milliseconds (0 = default, about 2 s)
+ *   "w4_debug_lose_stage"  test hook: in the next calls the first CTA of the tcgen05 kernel never receives the copies of its stage
+ *                       (value-1), so its waits run out and dresd_w4_status() reports DRESD_ERR_TIMEOUT.  0 = off.
  * Unknown names and values outside the stated set return DRESD_ERR_INVALID.
  */
 dresd_status dresd_set_global_option(const char *name, int value);

@@ -36,7 +36,7 @@ EXPORTS = (
     "dresd_retrieve_quantised", "dresd_store_index_first_tokens", "dresd_merge_shards_packed",
     "dresd_noalloc_status", "dresd_debug_build", "dresd_store_debug_selftest",
     "dresd_kv_create", "dresd_kv_destroy", "dresd_kv_append", "dresd_kv_read", "dresd_kv_attend",
-    "dresd_drafts_sample", "dresd_w4_quantise", "dresd_w4_matmul",
+    "dresd_drafts_sample", "dresd_w4_quantise", "dresd_w4_matmul", "dresd_w4_status",
     "dresd_kv_attach_pages", "dresd_kv_fork", "dresd_kv_reserve", "dresd_kv_release", "dresd_kv_compact",
     "dresd_kv_keep_draft", "dresd_kv_status", "dresd_kv_set_option", "dresd_kv_last_launches", "dresd_kv_debug_selftest",
 )
@@ -148,6 +148,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.dresd_w4_quantise.argtypes = [vp, i64, i64, i32, i32, i32, i32, vp, vp, vp]
     lib.dresd_w4_matmul.restype = i32
     lib.dresd_w4_matmul.argtypes = [vp, i64, i32, vp, vp, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp]
+    lib.dresd_w4_status.restype = i32
+    lib.dresd_w4_status.argtypes = [vp]
     lib.dresd_kv_attach_pages.restype = i32
     lib.dresd_kv_attach_pages.argtypes = [vp, vp]
     lib.dresd_kv_fork.restype = i32
@@ -238,6 +240,10 @@ def dresd_w4_matmul(x_ptr: int, x_row: int, rows: int, codes_ptr: int, scales_pt
                     group: int, relu: int, residual_ptr, residual_row: int, out_ptr: int, out_row: int, stream: int = 0) -> None:
     _check(load().dresd_w4_matmul(x_ptr, x_row, rows, codes_ptr, scales_ptr, inputs, outputs, dtype, group, relu, residual_ptr,
                                   residual_row, out_ptr, out_row, stream))
+
+
+def dresd_w4_status(stream: int = 0) -> None:
+    _check(load().dresd_w4_status(stream))
 
 
 def dresd_merge_shards_packed(packed_ptr: int, offsets_ptr: int, P: int, B: int, top_n: int, draft_len: int,

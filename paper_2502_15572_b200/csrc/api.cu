@@ -1108,6 +1108,7 @@ dresd_status dresd_set_global_option(const char *name, int value)
         g_build_lose_stage.store(value);
         return DRESD_OK;
     }
+    if (std::strncmp(name, "w4_", 3) == 0) return (dresd_status)set_w4_option(name, value);
     return fail(DRESD_ERR_INVALID, "unknown global option '%s'", name);
 }
 

@@ -1,4 +1,4 @@
-// What the C entry points share: messages of failing calls and checks of addresses.
+// What the C entry points share: messages of failing calls, checks of addresses, tensor maps.
 #pragma once
 
 #include <cstdarg>
@@ -37,5 +37,36 @@ inline bool is_device_ptr(const void *p, int device)
 }
 
 inline bool aligned(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+inline EncodeTiledFn encode_tiled_fn()
+{
+    static EncodeTiledFn fn = nullptr;
+    if (!fn) {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(p);
+    }
+    return fn;
+}
+
+// Zeros beyond the ends.
+inline bool encode(CUtensorMap *map, const void *base, int dtype, int rank, const cuuint64_t *dims, const cuuint64_t *strides,
+            const cuuint32_t *box, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B)
+{
+    const cuuint32_t ones[3] = {1, 1, 1};
+    EncodeTiledFn fn = encode_tiled_fn();
+    return fn && fn(map,
+                    dtype == kE4M3  ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                    : dtype == kF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                    : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                    rank, const_cast<void *>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 }  // namespace dresd

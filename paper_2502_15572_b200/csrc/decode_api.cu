@@ -1,5 +1,8 @@
 // C ABI of the decoding step's operators that need no handle: dresd_drafts_sample (k13_sample.cu) and the products with 4-bit
 // weights (k15_w4.cu).  Argument validation only.
+#include <atomic>
+#include <cstring>
+
 #include "api_util.h"
 
 using namespace dresd;
@@ -8,6 +11,9 @@ namespace {
 
 constexpr int kMaxVocab = 1 << 20;
 constexpr long long kMaxDistance = 1LL << 38;
+
+// process-wide, for tests (dresd_set_global_option)
+std::atomic<int> g_w4_path{0}, g_w4_wait_ms{0}, g_w4_lose_stage{0};
 
 dresd_status current_device(int *dev, int *sms)
 {
@@ -133,8 +139,53 @@ dresd_status dresd_w4_matmul(const void *x, int64_t x_row, int rows, const uint8
     a.outputs = outputs;
     a.groups = inputs / group;
     a.relu = relu != 0;
-    const cudaError_t e = launch_w4_matmul(a, (int)dtype, group, sms, static_cast<cudaStream_t>(stream));
+    cudaError_t e;
+    const int path = g_w4_path.load();
+    if (path == 2 || (path == 0 && rows > 16)) {
+        CUtensorMap code_map, x_map;
+        const cuuint64_t code_dims[2] = {(cuuint64_t)inputs / 2, (cuuint64_t)outputs}, code_strides[1] = {(cuuint64_t)inputs / 2};
+        // the distance of a single row is never used, but has to be a valid one
+        const cuuint64_t x_dims[2] = {(cuuint64_t)inputs, (cuuint64_t)rows}, x_strides[1] = {(cuuint64_t)(rows > 1 ? x_row : inputs) * 2};
+        const cuuint32_t code_box[2] = {64, 256}, x_box[2] = {64, (cuuint32_t)w4_umma_rows(rows)};
+        if (!encode(&code_map, codes, kE4M3, 2, code_dims, code_strides, code_box, CU_TENSOR_MAP_SWIZZLE_64B) ||
+            !encode(&x_map, x, (int)dtype, 2, x_dims, x_strides, x_box))
+            return fail(DRESD_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+        const int ms = g_w4_wait_ms.load();
+        e = launch_w4_umma(code_map, x_map, a, (int)dtype, group, ms > 0 ? ms * 2000000LL : 4000000000LL, g_w4_lose_stage.load(), sms,
+                           static_cast<cudaStream_t>(stream));
+    } else {
+        e = launch_w4_matmul(a, (int)dtype, group, sms, static_cast<cudaStream_t>(stream));
+    }
     return e == cudaSuccess ? DRESD_OK : fail_cuda(e, "w4_matmul launch");
 }
 
+dresd_status dresd_w4_status(void *stream)
+{
+    int word = 0;
+    const cudaError_t e = w4_status(&word, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return fail_cuda(e, "status read");
+    return word == 0 ? DRESD_OK : fail(DRESD_ERR_TIMEOUT, "a device-side wait expired");
+}
+
 }  // extern "C"
+
+namespace dresd {
+
+int set_w4_option(const char *name, int value)
+{
+    if (std::strcmp(name, "w4_path") == 0) {
+        if (value < 0 || value > 2) return fail(DRESD_ERR_INVALID, "w4_path = %d outside 0..2", value);
+        g_w4_path.store(value);
+    } else if (std::strcmp(name, "w4_wait_ms") == 0) {
+        if (value < 0 || value > 60000) return fail(DRESD_ERR_INVALID, "w4_wait_ms = %d outside 0..60000", value);
+        g_w4_wait_ms.store(value);
+    } else if (std::strcmp(name, "w4_debug_lose_stage") == 0) {
+        if (value < 0) return fail(DRESD_ERR_INVALID, "w4_debug_lose_stage = %d is negative", value);
+        g_w4_lose_stage.store(value);
+    } else {
+        return fail(DRESD_ERR_INVALID, "unknown global option '%s'", name);
+    }
+    return DRESD_OK;
+}
+
+}  // namespace dresd

@@ -226,6 +226,12 @@ struct W4Args {
 cudaError_t launch_w4_quantise(const void *w, long long w_in, long long w_out, int inputs, int outputs, int dtype, int group,
                                uint8_t *codes, void *scales, cudaStream_t stream);
 cudaError_t launch_w4_matmul(const W4Args &a, int dtype, int group, int sms, cudaStream_t stream);
+// K16, many rows.  Tensor maps: codes as bytes [outputs][inputs / 2] (boxes of 64 x 256, 64-byte swizzle), x [rows][inputs] (boxes of
+// 64 x w4_umma_rows(rows), 128-byte swizzle).
+int w4_umma_rows(int rows);
+cudaError_t launch_w4_umma(const CUtensorMap &code_map, const CUtensorMap &x_map, const W4Args &w, int dtype, int group, long long wait_cycles,
+                           int lose_stage, int sms, cudaStream_t stream);
+cudaError_t w4_status(int *word, cudaStream_t stream);        // waits for `stream`; reads and clears the current device's word
 
 // ---- K14: pages of the cache ----
 enum { kPageMoves, kPageShared, kPageUsed, kPageCounts };
@@ -295,6 +301,9 @@ cudaError_t launch_attend_umma(const CUtensorMap &q_map, const CUtensorMap &k_ma
 
 // Debug build only: one thread fails check 7 on purpose (no access is attempted), to show the reporting path.
 cudaError_t launch_debug_selftest(int *status, cudaStream_t stream);
+
+// The options of dresd_set_global_option() that begin with "w4_"; a dresd_status.
+int set_w4_option(const char *name, int value);
 
 // Stores `msg` as the calling thread's dresd_last_error() text.
 void set_last_error(const char *msg);

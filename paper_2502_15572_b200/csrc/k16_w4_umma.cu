@@ -1,0 +1,496 @@
+// K16 -- products with 4-bit weights for many rows (a chunk of drafts, a piece of a prompt), on tcgen05.
+//
+// What K15 computes, with the same arithmetic: codes minus 8 and activations are multiplied as they are, exact in the activations' type, and the
+// scale meets a group's sum in fp32.  A CTA has 256 outputs (two halves of 128, the M of the instruction) and up to 128 rows (its N):
+//
+//     A   codes minus 8 in TMEM, written by the warps that unpack them: a thread owns an output, 128 inputs at a time, two slots (one a half)
+//     B   activations in shared memory as TMA lays them (128-byte swizzle, K-major), used by both halves
+//     D   three blocks of 128 columns in turn; a block is the sum of ONE group, which other warps take out, scale and add to the
+//         sums in their registers (an output a thread, up to 128 rows) while the tensor core works on the next two
+//
+// Weights rounded to 16 bits with their scales would need no second step, but add an error as large as the result's own rounding; that step's
+// instructions (32 packed fmas of a warp for 64 columns of a group) fit beside the unpacking as long as groups are not small.
+//
+// Roles: warp 0 loads (lane 0: codes and activations of 128 inputs a stage), warp 1 issues the products, warps 4-11 unpack, warps 12-19 scale and add.
+// With few tiles the CTAs of a cluster split the inputs and add their parts up in the order of their ranks; with many, CTAs are persistent.
+#include <atomic>
+#include <type_traits>
+
+#include "kv_plan.cuh"
+
+namespace dresd {
+namespace {
+
+constexpr int kThreads = 640, kOutputs = 256, kTileRows = 128, kBlock = 128;     // inputs of a stage
+constexpr int kCodeBytes = kOutputs * kBlock / 2;
+constexpr int kMaxStages = 8, kMaxSplit = 8;
+constexpr int kSmemBytes = 232448;
+constexpr uint32_t kColumnsA = 384;                            // of the first slot; D at 0, 128, 256
+
+__device__ int g_status;                                       // a wait ran out; see w4_status()
+
+struct UmmaArgs {
+    W4Args w;
+    int n;                      // rows of a tile, a multiple of 16
+    int row_tiles, tiles;
+    int blocks;                 // of 128 inputs
+    int split, stages;
+    long long wait_cycles;
+    int lose_stage;             // test hook: the first CTA never receives its stage (value - 1)
+};
+
+struct Shared {
+    uint64_t full[kMaxStages], empty[kMaxStages];
+    uint64_t a_full[2], a_empty[2], d_empty[3], drained;
+    uint64_t d_full[2][3];      // of a half's own sums in turn: a warp that waits has seen the one three before
+    uint32_t tmem;
+};
+
+__device__ __forceinline__ void umma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr));
+}
+// Waits for the loads, and tells the compiler that these registers come with it.
+__device__ __forceinline__ void tmem_ld_wait16(uint32_t *r)
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :: "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// A warpgroup's registers per thread; together what the CTA was launched with, 640 x 96: 32 + 2 x 64 + 2 x 160 of each.
+template <bool kMore, int kCount> __device__ __forceinline__ void set_registers()
+{
+    if constexpr (kMore) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCount));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCount));
+}
+__device__ __forceinline__ uint64_t pair(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// Codes 2 p and 2 p + 1 of `w`, minus 8, as a pair of T: nibbles in the low bits of the mantissas of 1024 (fp16) or 128 (bf16).  high = w >> 4.
+template <typename T> __device__ __forceinline__ uint32_t code_pair(uint32_t w, uint32_t high, int p);
+template <> __device__ __forceinline__ uint32_t code_pair<__half>(uint32_t w, uint32_t high, int p)
+{
+    const uint32_t two = (__byte_perm(w, high, p | p << 4 | (4 + p) << 8 | (4 + p) << 12) & 0x000F000Fu) | 0x64006400u, c = 0x64086408u;
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&two), *reinterpret_cast<const __half2 *>(&c));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+template <> __device__ __forceinline__ uint32_t code_pair<__nv_bfloat16>(uint32_t w, uint32_t high, int p)
+{
+    const uint32_t two = (__byte_perm(w, high, p | p << 4 | (4 + p) << 8 | (4 + p) << 12) & 0x000F000Fu) | 0x43004300u, c = 0x43084308u;
+    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&two), *reinterpret_cast<const __nv_bfloat162 *>(&c));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+
+template <typename T, int kGroup>
+__global__ void __launch_bounds__(kThreads, 1)
+matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ UmmaArgs a)
+{
+    constexpr int kGroups = kBlock / kGroup;                    // of a block
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ Shared sh;
+    const int slab = a.n * 128, stage_bytes = kCodeBytes + 2 * slab;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const long long wl = a.wait_cycles;
+    const int rank = a.split > 1 ? (int)cluster_ctarank() : 0;
+    const int tile0 = blockIdx.x / a.split, tile_step = gridDim.x / a.split;
+    const int b0 = (int)((long long)a.blocks * rank / a.split), b1 = (int)((long long)a.blocks * (rank + 1) / a.split);
+    const int groups = min(b1 * kGroups, a.w.groups) - b0 * kGroups;       // of this CTA
+    uint8_t *stages = smem_raw + (-smem_u32(smem_raw) & 1023u);
+
+    if (warp == 0) {
+        if (lane < a.stages) {
+            mbar_init(&sh.full[lane], 1);
+            mbar_init(&sh.empty[lane], 8 + 1);                  // the unpacking warps, the products
+        }
+        if (lane < 2) {
+            mbar_init(&sh.a_full[lane], 4);
+            mbar_init(&sh.a_empty[lane], 1);
+        }
+        if (lane < 3) {
+            mbar_init(&sh.d_full[0][lane], 1);
+            mbar_init(&sh.d_full[1][lane], 1);
+            mbar_init(&sh.d_empty[lane], 4);
+        }
+        if (lane == 3) mbar_init(&sh.drained, 1);
+        mbar_fence_init();
+        if (lane == 4) {
+            tma_prefetch_desc(&code_map);
+            tma_prefetch_desc(&x_map);
+        }
+    } else if (warp == 1) {
+        tmem_alloc(&sh.tmem, 512);
+        tmem_relinquish();
+    }
+    pdl_wait();
+    pdl_launch_dependents();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+
+    if (warp < 4) {
+        set_registers<false, 32>();
+        if (warp == 0 && lane == 0) {
+            int it = 0;
+            bool ok = true;
+#pragma unroll 1
+            for (int tile = tile0; tile < a.tiles && ok; tile += tile_step) {
+                const int o = tile / a.row_tiles * kOutputs, t = tile % a.row_tiles * a.n;
+#pragma unroll 1
+                for (int b = b0; b < b1; ++b, ++it) {
+                    const int s = it % a.stages;
+                    if (it >= a.stages && !mbar_wait(&sh.empty[s], (it / a.stages - 1) & 1, wl)) {
+                        ok = false;
+                        break;
+                    }
+                    uint8_t *dst = stages + s * stage_bytes;
+                    mbar_arrive_expect_tx(&sh.full[s], (uint32_t)stage_bytes);
+                    if (a.lose_stage > 0 && blockIdx.x == 0 && it == a.lose_stage - 1) continue;
+                    tma_load_2d(dst, &code_map, b * (kBlock / 2), o, &sh.full[s]);
+                    tma_load_2d(dst + kCodeBytes, &x_map, b * kBlock, t, &sh.full[s]);
+                    tma_load_2d(dst + kCodeBytes + slab, &x_map, b * kBlock + 64, t, &sh.full[s]);
+                }
+            }
+            // what is on its way arrives before the CTA ends
+            for (int i = max(0, it - a.stages); i < it; ++i)
+                if (!mbar_wait(&sh.full[i % a.stages], (i / a.stages) & 1, wl)) ok = false;
+            if (!ok) report_timeout(&g_status);
+        } else if (warp == 1 && lane == 0) {
+            constexpr uint32_t kFmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+            const uint32_t idesc = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((uint32_t)(a.n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+            int it = 0, u = 0, v0 = 0, v1 = 0;                  // stages, sums, the halves' sums
+            bool ok = true;
+#pragma unroll 1
+            for (int tile = tile0; tile < a.tiles && ok; tile += tile_step)
+#pragma unroll 1
+                for (int b = b0; b < b1 && ok; ++b, ++it) {
+                    const int s = it % a.stages, here = min(kGroups, groups - (b - b0) * kGroups);
+                    const uint64_t x_desc = make_desc(smem_u32(stages + s * stage_bytes + kCodeBytes));
+                    ok = mbar_wait(&sh.full[s], (it / a.stages) & 1, wl);
+#pragma unroll 1
+                    for (int half = 0; half < 2 && ok; ++half) {
+                        if (!mbar_wait(&sh.a_full[half], it & 1, wl)) { ok = false; break; }
+#pragma unroll 1
+                        for (int g = 0; g < here; ++g, ++u) {
+                            const int d = u % 3;
+                            if (u >= 3 && !mbar_wait(&sh.d_empty[d], (u / 3 - 1) & 1, wl)) { ok = false; break; }
+                            tc_fence_after();
+#pragma unroll
+                            for (int k = 0; k < kGroup / 16; ++k) {
+                                const int kk = g * (kGroup / 16) + k;
+                                umma_f16_ta(tmem + d * 128, tmem + kColumnsA + half * 64 + kk * 8, x_desc + (uint64_t)((kk >> 2) * (slab >> 4) + 2 * (kk & 3)),
+                                            idesc, k != 0);
+                            }
+                            tc_commit(&sh.d_full[half][(half ? v1 : v0) % 3]);
+                            ++(half ? v1 : v0);
+                        }
+                        if (!ok) break;
+                        tc_commit(&sh.a_empty[half]);
+                    }
+                    if (ok) tc_commit(&sh.empty[s]);
+                }
+            // no product may be running when TMEM is given back
+            tc_commit(&sh.drained);
+            if (!mbar_wait(&sh.drained, 0, wl)) ok = false;
+            if (!ok) report_timeout(&g_status);
+        }
+    } else if (warp < 12) {
+        set_registers<false, 64>();
+        const int half = (warp - 4) >> 2, quarter = warp & 3, r = half * 128 + quarter * 32 + lane;
+        const uint32_t to = tmem + kColumnsA + half * 64 + ((uint32_t)(quarter * 32) << 16);
+        int it = 0;
+        bool ok = true;
+#pragma unroll 1
+        for (int tile = tile0; tile < a.tiles && ok; tile += tile_step)
+#pragma unroll 1
+            for (int b = b0; b < b1; ++b, ++it) {
+                const int s = it % a.stages;
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&sh.full[s], (it / a.stages) & 1, wl))) { ok = false; break; }
+                // 64 bytes of a row, which TMA has swizzled by 64 bytes
+                const uint8_t *row = stages + s * stage_bytes + r * 64;
+                uint4 w[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) w[c] = *reinterpret_cast<const uint4 *>(row + 16 * (c ^ ((r >> 1) & 3)));
+                if (it > 0 && !__all_sync(0xFFFFFFFFu, mbar_wait(&sh.a_empty[half], (it - 1) & 1, wl))) { ok = false; break; }
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t word = j == 0 ? w[c].x : j == 1 ? w[c].y : j == 2 ? w[c].z : w[c].w, high = word >> 4;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) p[4 * j + k] = code_pair<T>(word, high, k);
+                    }
+                    tmem_st16(to + 16 * c, p);
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&sh.a_full[half]);
+                    mbar_arrive(&sh.empty[s]);
+                }
+            }
+        if (!ok && lane == 0) report_timeout(&g_status);
+    } else {
+        set_registers<true, 160>();
+        const int half = (warp - 12) >> 2, quarter = warp & 3, r = half * 128 + quarter * 32 + lane;
+        const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16);
+        int base = 0, own = 0;                                  // sums of the tiles before, this half's
+        bool ok = true;
+#pragma unroll 1
+        for (int tile = tile0; tile < a.tiles && ok; tile += tile_step) {
+            const int o = tile / a.row_tiles * kOutputs + r, t0 = tile % a.row_tiles * a.n;
+            const T *scales = static_cast<const T *>(a.w.scales) + (long long)min(o, a.w.outputs - 1) * a.w.groups + b0 * kGroups;
+            uint64_t sum[kTileRows / 2];
+#pragma unroll
+            for (int i = 0; i < kTileRows / 2; ++i) sum[i] = 0;
+            float next = (float)__ldg(scales);
+#pragma unroll 1
+            for (int g = 0; g < groups; ++g, ++own) {
+                const int block = g / kGroups, here = min(kGroups, groups - block * kGroups);
+                const int u = base + block * 2 * kGroups + half * here + g % kGroups, d = u % 3;
+                const float scale = next;
+                if (g + 1 < groups) next = (float)__ldg(scales + g + 1);
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&sh.d_full[half][own % 3], (own / 3) & 1, wl))) { ok = false; break; }
+                tc_fence_after();
+                const uint64_t two = pair(scale, scale);
+                uint32_t x[2][16];
+                tmem_ld16(from + d * 128, x[0]);
+#pragma unroll
+                for (int c = 0; c < kTileRows / 16; ++c) {
+                    if (c * 16 >= a.n) break;
+                    tmem_ld_wait16(x[c & 1]);
+                    if (c + 1 < kTileRows / 16 && (c + 1) * 16 < a.n) tmem_ld16(from + d * 128 + 16 * (c + 1), x[(c + 1) & 1]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        sum[8 * c + i] = fma2(pair(__uint_as_float(x[c & 1][2 * i]), __uint_as_float(x[c & 1][2 * i + 1])), two, sum[8 * c + i]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.d_empty[d]);
+            }
+            base += 2 * groups;
+            if (!ok) break;
+            if (a.split > 1) {
+                // [row][output], where the stages were: when all products are done, the other half's too
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&sh.drained, 0, wl))) { ok = false; break; }
+                float *part = reinterpret_cast<float *>(stages);
+#pragma unroll
+                for (int i = 0; i < kTileRows / 2; ++i) {
+                    if (2 * i >= a.n) break;
+                    const float2 y = unpair(sum[i]);
+                    part[(2 * i) * kOutputs + r] = y.x;
+                    part[(2 * i + 1) * kOutputs + r] = y.y;
+                }
+            } else if (o < a.w.outputs) {
+                T *out = static_cast<T *>(a.w.out) + o;
+                const T *residual = a.w.residual ? static_cast<const T *>(a.w.residual) + o : nullptr;
+#pragma unroll
+                for (int i = 0; i < kTileRows; ++i) {
+                    const int t = t0 + i;
+                    if (i >= a.n || t >= a.w.rows) break;
+                    const float2 both = unpair(sum[i / 2]);
+                    float y = i & 1 ? both.y : both.x;
+                    if (a.w.relu && y < 0.f) y = 0.f;
+                    if (residual) y += (float)residual[t * a.w.residual_row];
+                    out[t * a.w.out_row] = (T)y;
+                }
+            }
+        }
+        if (!ok && lane == 0) report_timeout(&g_status);
+    }
+    __syncwarp();
+    if (a.split > 1) {
+        // one tile a cluster: its parts, each CTA a share of the rows
+        cluster_sync_all();
+        const int o0 = tile0 / a.row_tiles * kOutputs, t0 = tile0 % a.row_tiles * a.n;
+        const float *part = reinterpret_cast<const float *>(stages);
+#pragma unroll 1
+        for (int i = rank * kThreads + tid; i < a.n * (kOutputs / 4); i += a.split * kThreads) {
+            const int t = t0 + i / (kOutputs / 4), o = o0 + i % (kOutputs / 4) * 4;
+            if (t >= a.w.rows || o >= a.w.outputs) continue;
+            float4 v[kMaxSplit];
+#pragma unroll
+            for (int c = 0; c < kMaxSplit; ++c)
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(v[c].x), "=f"(v[c].y), "=f"(v[c].z), "=f"(v[c].w)
+                             : "r"(mapa_rank(smem_u32(part + 4 * i), min(c, a.split - 1))) : "memory");
+            float y[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+            for (int c = 1; c < kMaxSplit; ++c) {
+                if (c >= a.split) break;
+                y[0] += v[c].x;
+                y[1] += v[c].y;
+                y[2] += v[c].z;
+                y[3] += v[c].w;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (o + j >= a.w.outputs) break;
+                if (a.w.relu && y[j] < 0.f) y[j] = 0.f;
+                if (a.w.residual) y[j] += (float)static_cast<const T *>(a.w.residual)[t * a.w.residual_row + o + j];
+                static_cast<T *>(a.w.out)[t * a.w.out_row + o + j] = (T)y[j];
+            }
+        }
+        cluster_sync_all();                                     // the others may still read this CTA's part
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// CTAs (clusters of `split`) that are resident at once.
+template <typename T, int kGroup> cudaError_t resident(int split, int smem, int sms, int *clusters)
+{
+    static std::atomic<int> known[64][kMaxSplit + 1];           // by device; + 1
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    *clusters = dev < 64 ? known[dev][split].load() - 1 : -1;
+    if (*clusters >= 0) return cudaSuccess;
+    e = cudaFuncSetAttribute(matmul_umma_kernel<T, kGroup>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    if (split == 1) {
+        *clusters = sms;
+    } else {
+        cudaLaunchConfig_t cfg{};
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = split;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.gridDim = dim3(split);
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        e = cudaOccupancyMaxActiveClusters(clusters, matmul_umma_kernel<T, kGroup>, &cfg);
+        if (e != cudaSuccess) return e;
+    }
+    if (dev < 64) known[dev][split].store(*clusters + 1);
+    return cudaSuccess;
+}
+
+template <typename T, int kGroup>
+cudaError_t launch(const CUtensorMap &code_map, const CUtensorMap &x_map, UmmaArgs a, int sms, cudaStream_t stream)
+{
+    constexpr int kRing = kSmemBytes - 1024 - (int)sizeof(Shared) - 64;
+    const int stage = kCodeBytes + a.n * 256, smem = kRing + 1024;
+    a.stages = min(kRing / stage, kMaxStages);
+    // Inputs are split over a cluster when tiles are few: the split with the least work in a row, where a join counts as four blocks.
+    long long best = -1;
+    int clusters = 0;
+    for (int split = 1; split <= min(kMaxSplit, a.blocks); ++split) {
+        int room = 0;
+        const cudaError_t e = resident<T, kGroup>(split, smem, sms, &room);
+        if (e != cudaSuccess) return e;
+        if (room < 1) continue;
+        const long long rounds = (a.tiles + room - 1) / room, cost = rounds * ((a.blocks + split - 1) / split + (split > 1 ? 4 : 0));
+        if (best < 0 || cost < best) {
+            best = cost;
+            a.split = split;
+            clusters = room;
+        }
+        if (a.tiles >= sms) break;
+    }
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = a.split;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(a.split > 1 ? a.tiles * a.split : min(a.tiles, clusters));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.split > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, matmul_umma_kernel<T, kGroup>, code_map, x_map, a);
+}
+
+template <typename T>
+cudaError_t by_group(int group, const CUtensorMap &code_map, const CUtensorMap &x_map, const UmmaArgs &a, int sms, cudaStream_t stream)
+{
+    return group == 32   ? launch<T, 32>(code_map, x_map, a, sms, stream)
+           : group == 64 ? launch<T, 64>(code_map, x_map, a, sms, stream)
+                         : launch<T, 128>(code_map, x_map, a, sms, stream);
+}
+
+}  // namespace
+
+int w4_umma_rows(int rows)
+{
+    const int tiles = (rows + kTileRows - 1) / kTileRows;
+    return ((rows + tiles - 1) / tiles + 15) / 16 * 16;
+}
+
+cudaError_t launch_w4_umma(const CUtensorMap &code_map, const CUtensorMap &x_map, const W4Args &w, int dtype, int group, long long wait_cycles,
+                           int lose_stage, int sms, cudaStream_t stream)
+{
+    UmmaArgs a{};
+    a.w = w;
+    a.n = w4_umma_rows(w.rows);
+    a.row_tiles = (w.rows + a.n - 1) / a.n;
+    a.tiles = (w.outputs + kOutputs - 1) / kOutputs * a.row_tiles;
+    a.blocks = (w.inputs + kBlock - 1) / kBlock;
+    a.wait_cycles = wait_cycles;
+    a.lose_stage = lose_stage;
+    return dtype == kF16 ? by_group<__half>(group, code_map, x_map, a, sms, stream) : by_group<__nv_bfloat16>(group, code_map, x_map, a, sms, stream);
+}
+
+cudaError_t w4_status(int *word, cudaStream_t stream)
+{
+    *word = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(word, g_status, sizeof(int), 0, cudaMemcpyDeviceToHost, stream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+    if (e != cudaSuccess || *word == 0) return e;
+    const int zero = 0;
+    e = cudaMemcpyToSymbolAsync(g_status, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, stream);
+    return e == cudaSuccess ? cudaStreamSynchronize(stream) : e;
+}
+
+}  // namespace dresd

@@ -50,6 +50,56 @@ def test_whole_numbers_are_exact(rows, inputs, outputs, group, dtype):
     assert torch.equal(got.cpu(), (want.clamp(min=0) + residual.double()).to(DT[dtype]))
 
 
+@pytest.fixture
+def option():
+    def set_option(name, value):
+        binding.dresd_set_global_option(name, value)
+    yield set_option
+    for name in ("w4_path", "w4_wait_ms", "w4_debug_lose_stage"):
+        binding.dresd_set_global_option(name, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("path", [1, 2])
+@pytest.mark.parametrize("rows,inputs,outputs,group", SIZES + [(1, 4096, 4096, 128), (16, 11008, 4096, 64), (112, 4096, 11008, 32), (700, 1024, 3000, 128)])
+def test_either_kernel_at_every_size(option, path, rows, inputs, outputs, group):
+    dtype = "f16" if (rows + inputs) % 3 else "bf16"
+    x, codes, scales = exact_inputs(rows, inputs, outputs, group, dtype, rows)
+    option("w4_path", path)
+    got = binding.W4(codes, scales, dtype).matmul(x)
+    assert torch.equal(got.cpu(), (x.cpu().double() @ weights64(codes, scales, group).T).to(DT[dtype]))
+    binding.dresd_w4_status(torch.cuda.current_stream().cuda_stream)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,stage", [(40, 1), (40, 4), (300, 3)])      # a CTA has at least four stages here: 32 blocks, split by up to 8
+def test_a_wait_that_runs_out_is_reported(option, rows, stage):
+    """The first CTA never receives a stage: the call comes back, says so, and the next one is right."""
+    x, codes, scales = exact_inputs(rows, 4096, 600, 128, "f16", 4)
+    w, stream = binding.W4(codes, scales, "f16"), torch.cuda.current_stream().cuda_stream
+    want = w.matmul(x)
+    binding.dresd_w4_status(stream)
+    option("w4_wait_ms", 20)
+    option("w4_debug_lose_stage", stage)
+    w.matmul(x)
+    with pytest.raises(binding.DresdError) as e:
+        binding.dresd_w4_status(stream)
+    assert e.value.status == -5
+    option("w4_debug_lose_stage", 0)
+    binding.dresd_w4_status(stream)
+    assert torch.equal(w.matmul(x), want)
+    binding.dresd_w4_status(stream)
+
+
+@pytest.mark.parametrize("name,value", [("w4_path", 3), ("w4_path", -1), ("w4_wait_ms", -1), ("w4_wait_ms", 60001), ("w4_debug_lose_stage", -1), ("w4_other", 0)])
+def test_options_outside_their_range(name, value):
+    from paper_2502_15572_b200 import build
+    build.build()
+    with pytest.raises(binding.DresdError) as e:
+        binding.dresd_set_global_option(name, value)
+    assert e.value.status == -1
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("rows,inputs,outputs,group", SIZES)
