@@ -3,7 +3,7 @@
 // What K15 computes, with the same arithmetic: codes minus 8 and activations are multiplied as they are, exact in the activations' type, and the
 // scale meets a group's sum in fp32.  A CTA has 256 outputs (two halves of 128, the M of the instruction) and up to 128 rows (its N):
 //
-//     A   codes minus 8 in TMEM, written by the warps that unpack them: a thread owns an output, 128 inputs at a time, two slots (one a half)
+//     A   codes minus 8 in TMEM, written by the warps that unpack them: a thread owns an output; four slots of 64 inputs, two a half
 //     B   activations in shared memory as TMA lays them (128-byte swizzle, K-major), used by both halves
 //     D   three blocks of 128 columns in turn; a block is the sum of ONE group, which other warps take out, scale and add to the
 //         sums in their registers (an output a thread, up to 128 rows) while the tensor core works on the next two
@@ -41,7 +41,7 @@ struct UmmaArgs {
 
 struct Shared {
     uint64_t full[kMaxStages], empty[kMaxStages];
-    uint64_t a_full[2], a_empty[2], d_empty[3], drained;
+    uint64_t a_full[4], a_empty[4], d_empty[3], drained;      // a: [half][64 inputs]
     uint64_t d_full[2][3];      // of a half's own sums in turn: a warp that waits has seen the one three before
     uint32_t tmem;
 };
@@ -55,20 +55,14 @@ __device__ __forceinline__ void umma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, ui
         ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t *r)
-{
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr));
-}
 // Waits for the loads, and tells the compiler that these registers come with it.
-__device__ __forceinline__ void tmem_ld_wait16(uint32_t *r)
+__device__ __forceinline__ void tmem_ld_wait32(uint32_t *r)
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
-                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+                   "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+                   "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
                  :: "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
@@ -80,11 +74,21 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
         : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// A warpgroup's registers per thread; together what the CTA was launched with, 640 x 96: 32 + 2 x 64 + 2 x 160 of each.
+// A warpgroup's registers per thread; together no more than the CTA was launched with, 640 x 96: 24 + 2 x 56 + 2 x 168 of each.
 template <bool kMore, int kCount> __device__ __forceinline__ void set_registers()
 {
     if constexpr (kMore) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCount));
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCount));
+}
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xFFFFFFFF;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r != 0;
 }
 __device__ __forceinline__ uint64_t pair(float lo, float hi)
 {
@@ -141,7 +145,7 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
             mbar_init(&sh.full[lane], 1);
             mbar_init(&sh.empty[lane], 8 + 1);                  // the unpacking warps, the products
         }
-        if (lane < 2) {
+        if (lane < 4) {
             mbar_init(&sh.a_full[lane], 4);
             mbar_init(&sh.a_empty[lane], 1);
         }
@@ -168,7 +172,7 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
     const uint32_t tmem = sh.tmem;
 
     if (warp < 4) {
-        set_registers<false, 32>();
+        set_registers<false, 24>();
         if (warp == 0 && lane == 0) {
             int it = 0;
             bool ok = true;
@@ -194,47 +198,60 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
             for (int i = max(0, it - a.stages); i < it; ++i)
                 if (!mbar_wait(&sh.full[i % a.stages], (i / a.stages) & 1, wl)) ok = false;
             if (!ok) report_timeout(&g_status);
-        } else if (warp == 1 && lane == 0) {
+        } else if (warp == 1) {
+            // One thread issues, the warp goes along: code that only one thread reaches takes 90 cycles an instruction, a product of 128 rows 64.
             constexpr uint32_t kFmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
             const uint32_t idesc = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((uint32_t)(a.n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-            int it = 0, u = 0, v0 = 0, v1 = 0;                  // stages, sums, the halves' sums
+            const bool issuer = elect_one();
+            const uint32_t slab_step = slab >> 4;
+            int u = 0, v[2] = {0, 0}, s = 0, s_phase = 0;       // sums, the halves' sums, stage
+            uint32_t a_phase = 0;
             bool ok = true;
+            auto wait = [&](uint64_t *bar, uint32_t phase) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, phase, wl)); };
 #pragma unroll 1
             for (int tile = tile0; tile < a.tiles && ok; tile += tile_step)
 #pragma unroll 1
-                for (int b = b0; b < b1 && ok; ++b, ++it) {
-                    const int s = it % a.stages, here = min(kGroups, groups - (b - b0) * kGroups);
+                for (int b = b0; b < b1 && ok; ++b) {
+                    const int here = min(kGroups, groups - (b - b0) * kGroups);
                     const uint64_t x_desc = make_desc(smem_u32(stages + s * stage_bytes + kCodeBytes));
-                    ok = mbar_wait(&sh.full[s], (it / a.stages) & 1, wl);
-#pragma unroll 1
-                    for (int half = 0; half < 2 && ok; ++half) {
-                        if (!mbar_wait(&sh.a_full[half], it & 1, wl)) { ok = false; break; }
-#pragma unroll 1
-                        for (int g = 0; g < here; ++g, ++u) {
-                            const int d = u % 3;
-                            if (u >= 3 && !mbar_wait(&sh.d_empty[d], (u / 3 - 1) & 1, wl)) { ok = false; break; }
-                            tc_fence_after();
+                    ok = wait(&sh.full[s], s_phase);
 #pragma unroll
-                            for (int k = 0; k < kGroup / 16; ++k) {
-                                const int kk = g * (kGroup / 16) + k;
-                                umma_f16_ta(tmem + d * 128, tmem + kColumnsA + half * 64 + kk * 8, x_desc + (uint64_t)((kk >> 2) * (slab >> 4) + 2 * (kk & 3)),
-                                            idesc, k != 0);
+                    for (int half = 0; half < 2; ++half) {
+                        int d = 0;
+#pragma unroll
+                        for (int k = 0; k < kBlock / 16; ++k) {
+                            if (k % 4 == 0 && ok) ok = wait(&sh.a_full[half * 2 + k / 4], a_phase);
+                            const bool there = k / (kGroup / 16) < here;
+                            if (k % (kGroup / 16) == 0 && there) {
+                                d = u % 3;
+                                if (u >= 3 && ok) ok = wait(&sh.d_empty[d], (u / 3 - 1) & 1);
                             }
-                            tc_commit(&sh.d_full[half][(half ? v1 : v0) % 3]);
-                            ++(half ? v1 : v0);
+                            if (k % 4 == 0 || k % (kGroup / 16) == 0) tc_fence_after();
+                            if (issuer && ok && there)
+                                umma_f16_ta(tmem + d * 128, tmem + kColumnsA + half * 64 + k * 8, x_desc + (k / 4 * slab_step + 2 * (k & 3)), idesc,
+                                            k % (kGroup / 16) != 0);
+                            if (k % 4 == 3 && issuer && ok) tc_commit(&sh.a_empty[half * 2 + k / 4]);
+                            if ((k + 1) % (kGroup / 16) == 0 && there) {
+                                if (issuer && ok) tc_commit(&sh.d_full[half][v[half] % 3]);
+                                ++u;
+                                ++v[half];
+                            }
                         }
-                        if (!ok) break;
-                        tc_commit(&sh.a_empty[half]);
                     }
-                    if (ok) tc_commit(&sh.empty[s]);
+                    if (issuer && ok) tc_commit(&sh.empty[s]);
+                    a_phase ^= 1;
+                    if (++s == a.stages) {
+                        s = 0;
+                        s_phase ^= 1;
+                    }
                 }
             // no product may be running when TMEM is given back
-            tc_commit(&sh.drained);
-            if (!mbar_wait(&sh.drained, 0, wl)) ok = false;
-            if (!ok) report_timeout(&g_status);
+            if (issuer) tc_commit(&sh.drained);
+            if (!wait(&sh.drained, 0)) ok = false;
+            if (!ok && lane == 0) report_timeout(&g_status);
         }
     } else if (warp < 12) {
-        set_registers<false, 64>();
+        set_registers<false, 56>();
         const int half = (warp - 4) >> 2, quarter = warp & 3, r = half * 128 + quarter * 32 + lane;
         const uint32_t to = tmem + kColumnsA + half * 64 + ((uint32_t)(quarter * 32) << 16);
         int it = 0;
@@ -250,30 +267,33 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
                 uint4 w[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) w[c] = *reinterpret_cast<const uint4 *>(row + 16 * (c ^ ((r >> 1) & 3)));
-                if (it > 0 && !__all_sync(0xFFFFFFFFu, mbar_wait(&sh.a_empty[half], (it - 1) & 1, wl))) { ok = false; break; }
-                tc_fence_after();
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t p[16];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t word = j == 0 ? w[c].x : j == 1 ? w[c].y : j == 2 ? w[c].z : w[c].w, high = word >> 4;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) p[4 * j + k] = code_pair<T>(word, high, k);
-                    }
-                    tmem_st16(to + 16 * c, p);
-                }
-                tmem_st_wait();
-                tc_fence_before();
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(&sh.a_full[half]);
-                    mbar_arrive(&sh.empty[s]);
+                if (lane == 0) mbar_arrive(&sh.empty[s]);
+#pragma unroll
+                for (int q = 0; q < 2 && ok; ++q) {
+                    if (it > 0 && !__all_sync(0xFFFFFFFFu, mbar_wait(&sh.a_empty[half * 2 + q], (it - 1) & 1, wl))) { ok = false; break; }
+                    tc_fence_after();
+#pragma unroll
+                    for (int c = 2 * q; c < 2 * q + 2; ++c) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t word = j == 0 ? w[c].x : j == 1 ? w[c].y : j == 2 ? w[c].z : w[c].w, high = word >> 4;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) p[4 * j + k] = code_pair<T>(word, high, k);
+                        }
+                        tmem_st16(to + 16 * c, p);
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.a_full[half * 2 + q]);
                 }
+                if (!ok) break;
             }
         if (!ok && lane == 0) report_timeout(&g_status);
     } else {
-        set_registers<true, 160>();
+        set_registers<true, 168>();
         const int half = (warp - 12) >> 2, quarter = warp & 3, r = half * 128 + quarter * 32 + lane;
         const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16);
         int base = 0, own = 0;                                  // sums of the tiles before, this half's
@@ -285,26 +305,25 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
             uint64_t sum[kTileRows / 2];
 #pragma unroll
             for (int i = 0; i < kTileRows / 2; ++i) sum[i] = 0;
-            float next = (float)__ldg(scales);
+            T next = __ldg(scales);
 #pragma unroll 1
             for (int g = 0; g < groups; ++g, ++own) {
                 const int block = g / kGroups, here = min(kGroups, groups - block * kGroups);
                 const int u = base + block * 2 * kGroups + half * here + g % kGroups, d = u % 3;
-                const float scale = next;
-                if (g + 1 < groups) next = (float)__ldg(scales + g + 1);
+                const float scale = (float)next;
+                if (g + 1 < groups) next = __ldg(scales + g + 1);
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait(&sh.d_full[half][own % 3], (own / 3) & 1, wl))) { ok = false; break; }
                 tc_fence_after();
                 const uint64_t two = pair(scale, scale);
-                uint32_t x[2][16];
-                tmem_ld16(from + d * 128, x[0]);
 #pragma unroll
-                for (int c = 0; c < kTileRows / 16; ++c) {
-                    if (c * 16 >= a.n) break;
-                    tmem_ld_wait16(x[c & 1]);
-                    if (c + 1 < kTileRows / 16 && (c + 1) * 16 < a.n) tmem_ld16(from + d * 128 + 16 * (c + 1), x[(c + 1) & 1]);
+                for (int c = 0; c < kTileRows / 32; ++c) {
+                    if (c * 32 >= a.n) break;
+                    uint32_t x[32];
+                    tmem_ld32(from + d * 128 + 32 * c, x);      // (columns behind the last row hold something, and are not looked at again)
+                    tmem_ld_wait32(x);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        sum[8 * c + i] = fma2(pair(__uint_as_float(x[c & 1][2 * i]), __uint_as_float(x[c & 1][2 * i + 1])), two, sum[8 * c + i]);
+                    for (int i = 0; i < 16; ++i)
+                        sum[16 * c + i] = fma2(pair(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), two, sum[16 * c + i]);
                 }
                 tc_fence_before();
                 __syncwarp();
