@@ -11,7 +11,8 @@
 // Weights rounded to 16 bits with their scales would need no second step, but add an error as large as the result's own rounding; that step's
 // instructions (32 packed fmas of a warp for 64 columns of a group) fit beside the unpacking as long as groups are not small.
 //
-// Roles: warp 0 loads (lane 0: codes and activations of 128 inputs a stage), warp 1 issues the products, warps 4-11 unpack, warps 12-19 scale and add.
+// Roles: warp 0 loads (lane 0: codes and activations of 128 inputs a stage), warps 1 and 2 issue the products of a half each, warps 4-11 unpack,
+// warps 12-19 scale and add.
 // With few tiles the CTAs of a cluster split the inputs and add their parts up in the order of their ranks; with many, CTAs are persistent.
 #include <atomic>
 #include <type_traits>
@@ -26,6 +27,8 @@ constexpr int kCodeBytes = kOutputs * kBlock / 2;
 constexpr int kMaxStages = 8, kMaxSplit = 8;
 constexpr int kSmemBytes = 232448;
 constexpr uint32_t kColumnsA = 384;                            // of the first slot; D at 0, 128, 256
+constexpr int kControl = 40, kUnpack = 56, kAdd = 160;         // registers of the roles' warps
+static_assert(kControl + 2 * kUnpack + 2 * kAdd <= 5 * 96, "what a CTA is launched with: 5 warpgroups of 96 a thread");
 
 __device__ int g_status;                                       // a wait ran out; see w4_status()
 
@@ -41,8 +44,9 @@ struct UmmaArgs {
 
 struct Shared {
     uint64_t full[kMaxStages], empty[kMaxStages];
-    uint64_t a_full[4], a_empty[4], d_empty[3], drained;      // a: [half][64 inputs]
-    uint64_t d_full[2][3];      // of a half's own sums in turn: a warp that waits has seen the one three before
+    uint64_t a_full[2][2], a_empty[2][2], drained;            // of a half's slots of 64 inputs
+    // Of a half's own sums in turn, so that a warp that waits has seen the one three before; sum v of half h lies in block (2 v + h) % 3.
+    uint64_t d_full[2][3], d_empty[2][3];
     uint32_t tmem;
 };
 
@@ -55,15 +59,15 @@ __device__ __forceinline__ void umma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, ui
         ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-// Waits for the loads, and tells the compiler that these registers come with it.
-__device__ __forceinline__ void tmem_ld_wait32(uint32_t *r)
+// Sixteen columns, waited for (in one piece: apart, every register is moved once more).
+__device__ __forceinline__ void tmem_load16(uint32_t taddr, uint32_t *r)
 {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
-                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
-                   "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
-                   "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-                 :: "memory");
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
 {
@@ -74,7 +78,7 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
         : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// A warpgroup's registers per thread; together no more than the CTA was launched with, 640 x 96: 24 + 2 x 56 + 2 x 168 of each.
+// A warpgroup's registers per thread.
 template <bool kMore, int kCount> __device__ __forceinline__ void set_registers()
 {
     if constexpr (kMore) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCount));
@@ -90,38 +94,29 @@ __device__ __forceinline__ bool elect_one()
         : "=r"(r));
     return r != 0;
 }
-__device__ __forceinline__ uint64_t pair(float lo, float hi)
+// The eight codes of a word, minus 8, as pairs of T: nibbles become bits of the mantissas of powers of two, the lower one of a byte the lowest bits
+// (fp16 2048 + 2 c, bf16 256 + 2 c), the upper one those above them (fp16 128 + 2 c; bf16, which has fewer, moved down by one: 32 + 2 c).  Half of
+// that minus 1032, 136, 72, 24 is exact, and an fma: additions of halves go to the unit that permutes bytes, and that is the busiest one here.
+template <typename T> __device__ __forceinline__ void unpack(uint32_t w, uint32_t *p);
+template <> __device__ __forceinline__ void unpack<__half>(uint32_t w, uint32_t *p)
 {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t two = (__byte_perm(w, w, 0x1111 * k) & 0x00F0000Fu) | 0x58006800u, half = 0x38003800u, less = 0xD480E408u;
+        const __half2 r = __hfma2(*reinterpret_cast<const __half2 *>(&two), *reinterpret_cast<const __half2 *>(&half), *reinterpret_cast<const __half2 *>(&less));
+        p[k] = *reinterpret_cast<const uint32_t *>(&r);
+    }
 }
-__device__ __forceinline__ float2 unpair(uint64_t v)
+template <> __device__ __forceinline__ void unpack<__nv_bfloat16>(uint32_t w, uint32_t *p)
 {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-
-// Codes 2 p and 2 p + 1 of `w`, minus 8, as a pair of T: nibbles in the low bits of the mantissas of 1024 (fp16) or 128 (bf16).  high = w >> 4.
-template <typename T> __device__ __forceinline__ uint32_t code_pair(uint32_t w, uint32_t high, int p);
-template <> __device__ __forceinline__ uint32_t code_pair<__half>(uint32_t w, uint32_t high, int p)
-{
-    const uint32_t two = (__byte_perm(w, high, p | p << 4 | (4 + p) << 8 | (4 + p) << 12) & 0x000F000Fu) | 0x64006400u, c = 0x64086408u;
-    const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&two), *reinterpret_cast<const __half2 *>(&c));
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
-template <> __device__ __forceinline__ uint32_t code_pair<__nv_bfloat16>(uint32_t w, uint32_t high, int p)
-{
-    const uint32_t two = (__byte_perm(w, high, p | p << 4 | (4 + p) << 8 | (4 + p) << 12) & 0x000F000Fu) | 0x43004300u, c = 0x43084308u;
-    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&two), *reinterpret_cast<const __nv_bfloat162 *>(&c));
-    return *reinterpret_cast<const uint32_t *>(&r);
+    const uint32_t down = w >> 1;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t two = (__byte_perm(w, down, 0x4400 + 0x1111 * k) & 0x0078000Fu) | 0x42004380u, half = 0x3F003F00u, less = 0xC1C0C308u;
+        const __nv_bfloat162 r = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&two), *reinterpret_cast<const __nv_bfloat162 *>(&half),
+                                         *reinterpret_cast<const __nv_bfloat162 *>(&less));
+        p[k] = *reinterpret_cast<const uint32_t *>(&r);
+    }
 }
 
 template <typename T, int kGroup>
@@ -143,24 +138,27 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
     if (warp == 0) {
         if (lane < a.stages) {
             mbar_init(&sh.full[lane], 1);
-            mbar_init(&sh.empty[lane], 8 + 1);                  // the unpacking warps, the products
+            mbar_init(&sh.empty[lane], 8 + 2);                  // the unpacking warps, the halves' products
         }
-        if (lane < 4) {
-            mbar_init(&sh.a_full[lane], 4);
-            mbar_init(&sh.a_empty[lane], 1);
+        if (lane < 2) {
+            mbar_init(&sh.a_full[0][lane], 4);
+            mbar_init(&sh.a_full[1][lane], 4);
+            mbar_init(&sh.a_empty[0][lane], 1);
+            mbar_init(&sh.a_empty[1][lane], 1);
         }
         if (lane < 3) {
             mbar_init(&sh.d_full[0][lane], 1);
             mbar_init(&sh.d_full[1][lane], 1);
-            mbar_init(&sh.d_empty[lane], 4);
+            mbar_init(&sh.d_empty[0][lane], 4);
+            mbar_init(&sh.d_empty[1][lane], 4);
         }
-        if (lane == 3) mbar_init(&sh.drained, 1);
+        if (lane == 3) mbar_init(&sh.drained, 2);
         mbar_fence_init();
         if (lane == 4) {
             tma_prefetch_desc(&code_map);
             tma_prefetch_desc(&x_map);
         }
-    } else if (warp == 1) {
+    } else if (warp == 3) {
         tmem_alloc(&sh.tmem, 512);
         tmem_relinquish();
     }
@@ -172,7 +170,7 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
     const uint32_t tmem = sh.tmem;
 
     if (warp < 4) {
-        set_registers<false, 24>();
+        set_registers<false, kControl>();
         if (warp == 0 && lane == 0) {
             int it = 0;
             bool ok = true;
@@ -198,48 +196,49 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
             for (int i = max(0, it - a.stages); i < it; ++i)
                 if (!mbar_wait(&sh.full[i % a.stages], (i / a.stages) & 1, wl)) ok = false;
             if (!ok) report_timeout(&g_status);
-        } else if (warp == 1) {
-            // One thread issues, the warp goes along: code that only one thread reaches takes 90 cycles an instruction, a product of 128 rows 64.
+        } else if (warp == 1 || warp == 2) {
+            // One thread issues, the warp goes along: code that only one thread reaches takes 90 cycles an instruction, a product of 128 rows 64.  A
+            // warp to each half: the waits and commits of a block take one warp 2000 cycles, its products 1024.
             constexpr uint32_t kFmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
             const uint32_t idesc = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((uint32_t)(a.n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
             const bool issuer = elect_one();
             const uint32_t slab_step = slab >> 4;
-            int u = 0, v[2] = {0, 0}, s = 0, s_phase = 0;       // sums, the halves' sums, stage
-            uint32_t a_phase = 0;
+            const int half = warp - 1;
+            const uint32_t a_at = tmem + kColumnsA + half * 64;
+            int v = 0, d = half, s = 0, s_phase = 0, a_phase = 0;        // the half's sums, block of the next one, stage
             bool ok = true;
             auto wait = [&](uint64_t *bar, uint32_t phase) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, phase, wl)); };
 #pragma unroll 1
             for (int tile = tile0; tile < a.tiles && ok; tile += tile_step)
 #pragma unroll 1
-                for (int b = b0; b < b1 && ok; ++b) {
+                for (int b = b0; b < b1; ++b) {
                     const int here = min(kGroups, groups - (b - b0) * kGroups);
                     const uint64_t x_desc = make_desc(smem_u32(stages + s * stage_bytes + kCodeBytes));
-                    ok = wait(&sh.full[s], s_phase);
+                    if (!(ok = wait(&sh.full[s], s_phase))) break;
+                    uint32_t d_at = 0;
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        int d = 0;
-#pragma unroll
-                        for (int k = 0; k < kBlock / 16; ++k) {
-                            if (k % 4 == 0 && ok) ok = wait(&sh.a_full[half * 2 + k / 4], a_phase);
-                            const bool there = k / (kGroup / 16) < here;
-                            if (k % (kGroup / 16) == 0 && there) {
-                                d = u % 3;
-                                if (u >= 3 && ok) ok = wait(&sh.d_empty[d], (u / 3 - 1) & 1);
-                            }
-                            if (k % 4 == 0 || k % (kGroup / 16) == 0) tc_fence_after();
-                            if (issuer && ok && there)
-                                umma_f16_ta(tmem + d * 128, tmem + kColumnsA + half * 64 + k * 8, x_desc + (k / 4 * slab_step + 2 * (k & 3)), idesc,
-                                            k % (kGroup / 16) != 0);
-                            if (k % 4 == 3 && issuer && ok) tc_commit(&sh.a_empty[half * 2 + k / 4]);
-                            if ((k + 1) % (kGroup / 16) == 0 && there) {
-                                if (issuer && ok) tc_commit(&sh.d_full[half][v[half] % 3]);
-                                ++u;
-                                ++v[half];
-                            }
+                    for (int k = 0; k < kBlock / 16; ++k) {
+                        const bool there = k / (kGroup / 16) < here;
+                        if (k % (kGroup / 16) == 0 && there) {
+                            d_at = tmem + (uint32_t)d * kTileRows;
+                            // the sum three before in all: of the other half
+                            const int e = v - 2 + half;
+                            if (e >= 0 && ok) ok = wait(&sh.d_empty[half ^ 1][e % 3], (e / 3) & 1);
+                        }
+                        if (k % 4 == 0 && ok) ok = wait(&sh.a_full[half][k / 4], a_phase);
+                        if (k % 4 == 0 || k % (kGroup / 16) == 0) tc_fence_after();
+                        if (issuer && ok && there)
+                            umma_f16_ta(d_at, a_at + k * 8, x_desc + (k / 4 * slab_step + 2 * (k & 3)), idesc, k % (kGroup / 16) != 0);
+                        if (k % 4 == 3 && issuer && ok) tc_commit(&sh.a_empty[half][k / 4]);
+                        if ((k + 1) % (kGroup / 16) == 0 && there) {
+                            if (issuer && ok) tc_commit(&sh.d_full[half][v % 3]);
+                            ++v;
+                            d = d == 0 ? 2 : d - 1;             // (2 v + half) % 3
                         }
                     }
-                    if (issuer && ok) tc_commit(&sh.empty[s]);
                     a_phase ^= 1;
+                    if (!ok) break;
+                    if (issuer) tc_commit(&sh.empty[s]);
                     if (++s == a.stages) {
                         s = 0;
                         s_phase ^= 1;
@@ -251,109 +250,112 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
             if (!ok && lane == 0) report_timeout(&g_status);
         }
     } else if (warp < 12) {
-        set_registers<false, 56>();
+        set_registers<false, kUnpack>();
         const int half = (warp - 4) >> 2, quarter = warp & 3, r = half * 128 + quarter * 32 + lane;
         const uint32_t to = tmem + kColumnsA + half * 64 + ((uint32_t)(quarter * 32) << 16);
-        int it = 0;
+        // 64 bytes of a row, which TMA has swizzled by 64 bytes
+        const uint8_t *row = stages + r * 64;
+        const int swizzle = ((r >> 1) & 3) * 16;
+        int s = 0, s_phase = 0, a_phase = 1;                    // (the phase before the first one counts as complete)
         bool ok = true;
 #pragma unroll 1
         for (int tile = tile0; tile < a.tiles && ok; tile += tile_step)
 #pragma unroll 1
-            for (int b = b0; b < b1; ++b, ++it) {
-                const int s = it % a.stages;
-                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&sh.full[s], (it / a.stages) & 1, wl))) { ok = false; break; }
-                // 64 bytes of a row, which TMA has swizzled by 64 bytes
-                const uint8_t *row = stages + s * stage_bytes + r * 64;
+            for (int b = b0; b < b1; ++b) {
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&sh.full[s], s_phase, wl))) { ok = false; break; }
                 uint4 w[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) w[c] = *reinterpret_cast<const uint4 *>(row + 16 * (c ^ ((r >> 1) & 3)));
+                for (int c = 0; c < 4; ++c) w[c] = *reinterpret_cast<const uint4 *>(row + s * stage_bytes + (16 * c ^ swizzle));
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.empty[s]);
+                if (++s == a.stages) {
+                    s = 0;
+                    s_phase ^= 1;
+                }
 #pragma unroll
-                for (int q = 0; q < 2 && ok; ++q) {
-                    if (it > 0 && !__all_sync(0xFFFFFFFFu, mbar_wait(&sh.a_empty[half * 2 + q], (it - 1) & 1, wl))) { ok = false; break; }
+                for (int q = 0; q < 2; ++q) {
+                    if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&sh.a_empty[half][q], a_phase, wl));
                     tc_fence_after();
 #pragma unroll
                     for (int c = 2 * q; c < 2 * q + 2; ++c) {
                         uint32_t p[16];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint32_t word = j == 0 ? w[c].x : j == 1 ? w[c].y : j == 2 ? w[c].z : w[c].w, high = word >> 4;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) p[4 * j + k] = code_pair<T>(word, high, k);
-                        }
-                        tmem_st16(to + 16 * c, p);
+                        for (int i = 0; i < 4; ++i)
+                            unpack<T>(i == 0 ? w[c].x : i == 1 ? w[c].y : i == 2 ? w[c].z : w[c].w, p + 4 * i);
+                        if (ok) tmem_st16(to + 16 * c, p);
                     }
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.a_full[half * 2 + q]);
+                    if (ok && lane == 0) mbar_arrive(&sh.a_full[half][q]);
                 }
+                a_phase ^= 1;
                 if (!ok) break;
             }
         if (!ok && lane == 0) report_timeout(&g_status);
     } else {
-        set_registers<true, 168>();
+        set_registers<true, kAdd>();
         const int half = (warp - 12) >> 2, quarter = warp & 3, r = half * 128 + quarter * 32 + lane;
         const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16);
-        int base = 0, own = 0;                                  // sums of the tiles before, this half's
+        int i_full = 0, full_phase = 0, d = half;               // this half's sums: of three barriers in turn, block
         bool ok = true;
 #pragma unroll 1
         for (int tile = tile0; tile < a.tiles && ok; tile += tile_step) {
             const int o = tile / a.row_tiles * kOutputs + r, t0 = tile % a.row_tiles * a.n;
             const T *scales = static_cast<const T *>(a.w.scales) + (long long)min(o, a.w.outputs - 1) * a.w.groups + b0 * kGroups;
-            uint64_t sum[kTileRows / 2];
+            float sum[kTileRows];
 #pragma unroll
-            for (int i = 0; i < kTileRows / 2; ++i) sum[i] = 0;
+            for (int i = 0; i < kTileRows; ++i) sum[i] = 0.f;
             T next = __ldg(scales);
 #pragma unroll 1
-            for (int g = 0; g < groups; ++g, ++own) {
-                const int block = g / kGroups, here = min(kGroups, groups - block * kGroups);
-                const int u = base + block * 2 * kGroups + half * here + g % kGroups, d = u % 3;
+            for (int g = 0; g < groups; ++g) {
                 const float scale = (float)next;
                 if (g + 1 < groups) next = __ldg(scales + g + 1);
-                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&sh.d_full[half][own % 3], (own / 3) & 1, wl))) { ok = false; break; }
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&sh.d_full[half][i_full], full_phase, wl))) { ok = false; break; }
                 tc_fence_after();
-                const uint64_t two = pair(scale, scale);
 #pragma unroll
-                for (int c = 0; c < kTileRows / 32; ++c) {
-                    if (c * 32 >= a.n) break;
-                    uint32_t x[32];
-                    tmem_ld32(from + d * 128 + 32 * c, x);      // (columns behind the last row hold something, and are not looked at again)
-                    tmem_ld_wait32(x);
+                for (int c = 0; c < kTileRows / 16; ++c) {
+                    if (c * 16 >= a.n) break;
+                    uint32_t x[16];
+                    tmem_load16(from + d * kTileRows + 16 * c, x);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        sum[16 * c + i] = fma2(pair(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), two, sum[16 * c + i]);
+                    for (int i = 0; i < 16; ++i) sum[16 * c + i] = fmaf(scale, __uint_as_float(x[i]), sum[16 * c + i]);
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.d_empty[d]);
+                if (lane == 0) mbar_arrive(&sh.d_empty[half][i_full]);
+                d = d == 0 ? 2 : d - 1;
+                if (++i_full == 3) {
+                    i_full = 0;
+                    full_phase ^= 1;
+                }
             }
-            base += 2 * groups;
             if (!ok) break;
             if (a.split > 1) {
                 // [row][output], where the stages were: when all products are done, the other half's too
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait(&sh.drained, 0, wl))) { ok = false; break; }
                 float *part = reinterpret_cast<float *>(stages);
 #pragma unroll
-                for (int i = 0; i < kTileRows / 2; ++i) {
-                    if (2 * i >= a.n) break;
-                    const float2 y = unpair(sum[i]);
-                    part[(2 * i) * kOutputs + r] = y.x;
-                    part[(2 * i + 1) * kOutputs + r] = y.y;
+                for (int c = 0; c < kTileRows / 16; ++c) {
+                    if (c * 16 >= a.n) break;
+#pragma unroll
+                    for (int i = 16 * c; i < 16 * c + 16; ++i) part[i * kOutputs + r] = sum[i];
                 }
             } else if (o < a.w.outputs) {
                 T *out = static_cast<T *>(a.w.out) + o;
                 const T *residual = a.w.residual ? static_cast<const T *>(a.w.residual) + o : nullptr;
 #pragma unroll
-                for (int i = 0; i < kTileRows; ++i) {
-                    const int t = t0 + i;
-                    if (i >= a.n || t >= a.w.rows) break;
-                    const float2 both = unpair(sum[i / 2]);
-                    float y = i & 1 ? both.y : both.x;
-                    if (a.w.relu && y < 0.f) y = 0.f;
-                    if (residual) y += (float)residual[t * a.w.residual_row];
-                    out[t * a.w.out_row] = (T)y;
+                for (int c = 0; c < kTileRows / 16; ++c) {
+                    if (c * 16 >= a.n) break;
+#pragma unroll
+                    for (int i = 16 * c; i < 16 * c + 16; ++i) {
+                        const int t = t0 + i;
+                        if (t >= a.w.rows) continue;
+                        float y = sum[i];
+                        if (a.w.relu && y < 0.f) y = 0.f;
+                        if (residual) y += (float)residual[t * a.w.residual_row];
+                        out[t * a.w.out_row] = (T)y;
+                    }
                 }
             }
         }
@@ -361,12 +363,12 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
     }
     __syncwarp();
     if (a.split > 1) {
-        // one tile a cluster: its parts, each CTA a share of the rows
+        // one tile a cluster: its parts, each CTA a share of the rows, by the warps with registers for it
         cluster_sync_all();
         const int o0 = tile0 / a.row_tiles * kOutputs, t0 = tile0 % a.row_tiles * a.n;
         const float *part = reinterpret_cast<const float *>(stages);
 #pragma unroll 1
-        for (int i = rank * kThreads + tid; i < a.n * (kOutputs / 4); i += a.split * kThreads) {
+        for (int i = warp < 12 ? a.n * (kOutputs / 4) : rank * 256 + tid - 384; i < a.n * (kOutputs / 4); i += a.split * 256) {
             const int t = t0 + i / (kOutputs / 4), o = o0 + i % (kOutputs / 4) * 4;
             if (t >= a.w.rows || o >= a.w.outputs) continue;
             float4 v[kMaxSplit];
@@ -396,7 +398,7 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 1) {
+    if (warp == 3) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
