@@ -802,7 +802,7 @@ class KvPages:
 
     def _word(self, stream):
         with _allocated_on(stream):
-            return _torch().empty(1, dtype=_torch().int32, device=self.refs.device)
+            return self.refs.new_empty(1)
 
     def fork(self, ctx, parent, stream=None):
         """Row b becomes a copy of row parent[b] (-1: stays) that shares its pages; ctx[b] = ctx[parent[b]]."""
@@ -843,37 +843,46 @@ def drafts_sample(logits, uniform, drafts=None, valid=None, temperature=None, to
     [B][n], or neither (one row a sequence); temperature, top_p fp32 [B], top_k int32 [B], or None (1, off, off).
     Returns ``(best [B], length [B], tokens [B][L + 1], logprobs [B][L + 1])``."""
     torch = _torch()
-    code = {torch.float32: DRESD_F32, torch.float16: DRESD_F16, torch.bfloat16: DRESD_BF16}.get(logits.dtype)
+    f32, i32 = torch.float32, torch.int32
+    code = {f32: DRESD_F32, torch.float16: DRESD_F16, torch.bfloat16: DRESD_BF16}.get(logits.dtype)
     dev = logits.get_device()
     if code is None or dev < 0 or logits.dim() != 3:
         raise DresdError(-1, "logits must be a CUDA tensor of f32, f16 or bf16 with 3 dimensions")
     B, rows, V = logits.shape
+    chunk_stride, row_stride, last = logits.stride()
+    if last != 1 and V > 1:
+        raise DresdError(-1, "the logits of a row must be adjacent")
+
+    def ptr(name, t, dtype, shape):
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+            raise DresdError(-1, f"{name} must be a contiguous {dtype} tensor of shape {shape} on cuda:{dev}")
+        return t.data_ptr()
+
     if (drafts is None) != (valid is None):
         raise DresdError(-1, "drafts and valid go together")
-    n, L = (0, 0) if drafts is None else drafts.shape[1:] if drafts.dim() == 3 else (-1, -1)
-    if n == 0 or L == 0:
-        n = L = 0
+    n = L = 0
+    d_ptr = v_ptr = None
+    if drafts is not None:
+        n, L = drafts.shape[1:] if drafts.dim() == 3 else (-1, -1)
+        if n and L:
+            d_ptr, v_ptr = ptr("drafts", drafts, i32, (B, n, L)), ptr("valid", valid, i32, (B, n))
+        else:
+            n = L = 0
     if rows != 1 + n * L:
         raise DresdError(-1, f"logits have {rows} rows a sequence for {n} drafts of {L} tokens")
-    if V > 1 and logits.stride(2) != 1:
-        raise DresdError(-1, "the logits of a row must be adjacent")
-    for name, t, dtype, shape in (("uniform", uniform, torch.float32, (B, L + 1)), ("drafts", drafts, torch.int32, (B, n, L)),
-                                  ("valid", valid, torch.int32, (B, n)), ("temperature", temperature, torch.float32, (B,)),
-                                  ("top_k", top_k, torch.int32, (B,)), ("top_p", top_p, torch.float32, (B,))):
-        if t is None and name != "uniform" or n == 0 and name in ("drafts", "valid"):
-            continue
-        if t is None or t.dtype != dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
-            raise DresdError(-1, f"{name} must be a contiguous {dtype} tensor of shape {shape} on cuda:{dev}")
+    if uniform is None:
+        raise DresdError(-1, "uniform is missing")
+    u_ptr = ptr("uniform", uniform, f32, (B, L + 1))
+    t_ptr, k_ptr, p_ptr = ptr("temperature", temperature, f32, (B,)), ptr("top_k", top_k, i32, (B,)), ptr("top_p", top_p, f32, (B,))
     with _allocated_on(stream):
-        words = torch.empty((2 + 2 * (L + 1), B), dtype=torch.int32, device=logits.device)
-    best, length = words[0], words[1]
-    tokens = words[2:3 + L].view(B, L + 1)
-    logs = words[3 + L:].view(torch.float32).view(B, L + 1)
-    ptr = lambda t: None if t is None else t.data_ptr()
+        logs = torch.empty_like(uniform)
+        tokens = torch.empty_like(uniform, dtype=i32)
+        best, length = tokens.new_empty((2, B)).unbind(0)
     if B:
-        dresd_drafts_sample(logits.data_ptr(), code, logits.stride(0), logits.stride(1), V, ptr(drafts) if n else None,
-                            ptr(valid) if n else None, uniform.data_ptr(), ptr(temperature), ptr(top_k), ptr(top_p), B, n, L, best.data_ptr(),
-                            length.data_ptr(), tokens.data_ptr(), logs.data_ptr(), _raw_stream(dev, stream))
+        dresd_drafts_sample(logits.data_ptr(), code, chunk_stride, row_stride, V, d_ptr, v_ptr, u_ptr, t_ptr, k_ptr, p_ptr, B, n, L,
+                            best.data_ptr(), length.data_ptr(), tokens.data_ptr(), logs.data_ptr(), _raw_stream(dev, stream))
     return best, length, tokens, logs
 
 
@@ -899,6 +908,7 @@ class W4:
         if self.group not in (32, 64, 128):
             raise DresdError(-2, f"group = {self.group} is not 32, 64 or 128")
         self.codes, self.scales, self.device_index = codes, scales, codes.get_device()       # keep alive
+        self._codes_ptr, self._scales_ptr, self._code = codes.data_ptr(), scales.data_ptr(), DTYPE_CODE[dtype]
 
     @classmethod
     def quantise(cls, w, group: int = 128, stream=None):
@@ -921,11 +931,13 @@ class W4:
         return cls(codes, scales, dtype)
 
     def _rows(self, name, t, rows, columns):
-        if t.dtype != self.torch_dtype or t.get_device() != self.device_index or t.shape != (rows, columns):
+        """Address of a [rows][columns] tensor and the distance of its rows."""
+        if t.dtype is not self.torch_dtype or t.get_device() != self.device_index or t.shape != (rows, columns):
             raise DresdError(-1, f"{name} must be a {self.torch_dtype} tensor of shape {(rows, columns)} on cuda:{self.device_index}")
-        if columns > 1 and t.stride(1) != 1:
+        row, last = t.stride()
+        if last != 1 and columns > 1:
             raise DresdError(-1, f"{name}: the elements of a row must be adjacent")
-        return t.data_ptr(), t.stride(0)
+        return t.data_ptr(), row
 
     def matmul(self, x, residual=None, relu: bool = False, out=None, stream=None):
         """f(x w) + residual for x [rows][inputs]; f is max(., 0) with `relu`.  out: [rows][outputs], may be `residual` itself."""
@@ -936,10 +948,11 @@ class W4:
         res_ptr, res_row = (None, 0) if residual is None else self._rows("residual", residual, rows, self.outputs)
         if out is None:
             with _allocated_on(stream):
-                out = _torch().empty((rows, self.outputs), dtype=self.torch_dtype, device=x.device)
-        out_ptr, out_row = self._rows("out", out, rows, self.outputs)
+                out = x.new_empty((rows, self.outputs))
+            out_ptr, out_row = out.data_ptr(), self.outputs
+        else:
+            out_ptr, out_row = self._rows("out", out, rows, self.outputs)
         if rows:
-            dresd_w4_matmul(x_ptr, x_row, rows, self.codes.data_ptr(), self.scales.data_ptr(), self.inputs, self.outputs,
-                            DTYPE_CODE[self.dtype], self.group, int(relu), res_ptr, res_row, out_ptr, out_row,
-                            _raw_stream(self.device_index, stream))
+            dresd_w4_matmul(x_ptr, x_row, rows, self._codes_ptr, self._scales_ptr, self.inputs, self.outputs, self._code, self.group,
+                            1 if relu else 0, res_ptr, res_row, out_ptr, out_row, _raw_stream(self.device_index, stream))
         return out
