@@ -1,12 +1,16 @@
-// K15 -- products with 4-bit weights and one scale for a group of inputs:
+// K15 -- products with 4-bit weights and one scale for a group of inputs, for few rows (a token or a few for every sequence):
 //     y[t][o] = sum_g s[o][g] sum_{i in g} (c[o][i] - 8) x[t][i]
 // The inner sums multiply whole numbers -8 .. 7 and the activations, both exact in the activations' type, and are kept in fp32; the scale meets
 // them there.  So a weight is never rounded, and a result is rounded once.
 //
+// Bound: the weights' bytes, and on small matrices the latency of fetching them once.  A CTA has 128 outputs and 512 inputs at a time; the CTAs of a
+// cluster split the inputs until all are resident at once, so that (almost) every byte is on its way from the start -- codes and
+// activations by cp.async, scales through registers --, and add their parts up in the order of their ranks.
+//
 // A warp computes 32 outputs for up to 8 kBlocks rows with mma.sync, weights as the 16-row operand.  The order of inputs within an
-// instruction is free, as long as both operands agree: a lane takes G / 4 consecutive codes of a row, as they lie in
-// memory (4 lanes a row, 8 rows a load), and the same inputs of its row of activations.  No shared memory is involved until the
-// end, when the CTAs of a cluster, which split the inputs, add their parts up in the order of their ranks.
+// instruction is free, as long as both operands agree: a lane takes 8 or 16 consecutive codes of a row (4 lanes a row, 8 rows
+// a load) and the same inputs of its row of activations.  Rows in shared memory are padded so that neither load meets a bank twice.
+#include <atomic>
 #include <type_traits>
 
 #include "kv_plan.cuh"
@@ -15,28 +19,34 @@ namespace dresd {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kTile = 32 * kWarps;      // outputs of a CTA
+constexpr int kChunk = 512;                                                 // inputs at a time
 constexpr int kMaxSplit = 8;
+static_assert(kThreads == kTile, "a thread fetches the scales of an output");
 
-// Codes of nibbles j and j + 4 of `w` (already moved to j = 0), minus 8, as a pair of T: the nibble in the low bits of the mantissa of 1024
-// (fp16) or 128 (bf16) is that number plus the code.
-template <typename T> __device__ __forceinline__ uint32_t code_pair(uint32_t w);
-template <> __device__ __forceinline__ uint32_t code_pair<__half>(uint32_t w)
+// The eight codes of a word, minus 8, as the pairs (0, 4), (1, 5), (2, 6), (3, 7) of T.  Nibbles become bits of the mantissas of powers of two, at the
+// bottom (fp16 2048 + 2 c, bf16 256 + 2 c) or above that (fp16 128 + 2 c; bf16, which has fewer, moved down by one: 32 + 2 c); half of that less 1032,
+// 136, 72, 24 is exact, and an fma: additions of halves share a unit with shifts and logic, of which there are more.
+template <typename T> __device__ __forceinline__ void unpack(uint32_t w, uint32_t (&p)[4]);
+template <> __device__ __forceinline__ void unpack<__half>(uint32_t w, uint32_t (&p)[4])
 {
-    const uint32_t u = (w & 0x000F000Fu) | 0x64006400u, c = 0x64086408u;      // 1024 + 8
-    const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&u), *reinterpret_cast<const __half2 *>(&c));
-    return *reinterpret_cast<const uint32_t *>(&r);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t at = k < 2 ? w : w >> 8, two = k % 2 ? (at & 0x00F000F0u) | 0x58005800u : (at & 0x000F000Fu) | 0x68006800u;
+        const uint32_t half = 0x38003800u, less = k % 2 ? 0xD480D480u : 0xE408E408u;
+        const __half2 r = __hfma2(*reinterpret_cast<const __half2 *>(&two), *reinterpret_cast<const __half2 *>(&half), *reinterpret_cast<const __half2 *>(&less));
+        p[k] = *reinterpret_cast<const uint32_t *>(&r);
+    }
 }
-template <> __device__ __forceinline__ uint32_t code_pair<__nv_bfloat16>(uint32_t w)
+template <> __device__ __forceinline__ void unpack<__nv_bfloat16>(uint32_t w, uint32_t (&p)[4])
 {
-    const uint32_t u = (w & 0x000F000Fu) | 0x43004300u, c = 0x43084308u;      // 128 + 8
-    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&u), *reinterpret_cast<const __nv_bfloat162 *>(&c));
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
-template <typename T> __device__ __forceinline__ float scale_of(const void *scales, long long i)
-{
-    const T v = __ldg(static_cast<const T *>(scales) + i);
-    if constexpr (std::is_same<T, __half>::value) return __half2float(v);
-    else return __bfloat162float(v);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t at = w >> (k / 2 * 8 + k % 2), two = k % 2 ? (at & 0x00780078u) | 0x42004200u : (at & 0x000F000Fu) | 0x43804380u;
+        const uint32_t half = 0x3F003F00u, less = k % 2 ? 0xC1C0C1C0u : 0xC308C308u;
+        const __nv_bfloat162 r = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&two), *reinterpret_cast<const __nv_bfloat162 *>(&half),
+                                         *reinterpret_cast<const __nv_bfloat162 *>(&less));
+        p[k] = *reinterpret_cast<const uint32_t *>(&r);
+    }
 }
 template <typename T> __device__ __forceinline__ T from_float(float x)
 {
@@ -46,45 +56,99 @@ template <typename T> __device__ __forceinline__ T from_float(float x)
 template <typename T> __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     if constexpr (std::is_same<T, __half>::value)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Eight codes a word: words of a lane's share of a group of one row, as one load.
-template <int kWords> struct Words;
-template <> struct Words<4> { typedef uint4 type; };
-template <> struct Words<2> { typedef uint2 type; };
-template <> struct Words<1> { typedef uint32_t type; };
+__device__ __forceinline__ void copy_async(void *dst, const void *src, bool there)      // 16 bytes, or zeros
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(__cvta_generic_to_global(src)), "r"(there ? 16 : 0) : "memory");
+}
+
+// Waits for all but the last kLast - done groups of copies.
+template <int kLast> __device__ __forceinline__ void wait_copies(int done)
+{
+    if (done == 0) asm volatile("cp.async.wait_group %0;" ::"n"(kLast) : "memory");
+    else if (done == 1) asm volatile("cp.async.wait_group %0;" ::"n"(kLast - 1) : "memory");
+    else if (done == 2) asm volatile("cp.async.wait_group %0;" ::"n"(kLast - 2) : "memory");
+    else asm volatile("cp.async.wait_group %0;" ::"n"(kLast - 3) : "memory");
+}
+
+template <int kGroup, int kBlocks> struct Stage {
+    static constexpr int kWords = kGroup == 32 ? 1 : 2;                     // of eight codes, of a lane and row at a time
+    static constexpr int kSub = 32 * kWords;                                // inputs of four lanes at a time
+    static constexpr int kCodeRow = kChunk / 2 + kSub / 2, kXRow = kChunk * 2 + (kWords == 1 ? 64 : 16);      // bytes; padded
+    static constexpr int kGroups = kChunk / kGroup;
+    static constexpr int kX = kTile * kCodeRow, kScales = kX + 8 * kBlocks * kXRow, kBytes = kScales + kGroups * kTile * 4;
+};
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// Chunks that the CTA with the most groups has.
+__host__ __device__ constexpr int chunks_of(int groups, int split, int per_chunk) { return ((groups + split - 1) / split + per_chunk - 1) / per_chunk; }
 
 template <typename T, int kGroup, int kBlocks>
 __global__ void __launch_bounds__(kThreads) matmul_mma_kernel(const W4Args a)
 {
-    constexpr int kWords = kGroup / 32, kAhead = 512 / kGroup;      // groups whose codes are loaded together
-    typedef typename Words<kWords>::type Load;
-    extern __shared__ float part[];                                 // [8 kBlocks rows][kTile outputs]
+    using S = Stage<kGroup, kBlocks>;
+    extern __shared__ __align__(16) uint8_t smem[];
     const uint32_t rank = cluster_ctarank(), split = gridDim.x;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane & 3, row = lane >> 2;
-    const int o0 = blockIdx.y * kTile + warp * 32, t0 = blockIdx.z * 8 * kBlocks;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane & 3, row = lane >> 2;
+    const int o0 = blockIdx.y * kTile, t0 = blockIdx.z * 8 * kBlocks;
     const int g0 = (int)((long long)a.groups * rank / split), g1 = (int)((long long)a.groups * (rank + 1) / split);
+    const int chunks = (g1 - g0 + S::kGroups - 1) / S::kGroups;
+    cluster_arrive();
     pdl_wait();
     pdl_launch_dependents();
     // rows and outputs beyond the end are computed like the last ones and not written
-    const uint8_t *codes[4];
-    long long scale_row[4];
+    const T *scales = static_cast<const T *>(a.scales) + (long long)min(o0 + tid, a.outputs - 1) * a.groups + g0;
+    const uint8_t *code_row[4];
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-        const long long o = min(o0 + m * 8 + row, a.outputs - 1);
-        codes[m] = a.codes + o * (a.inputs / 2) + quad * (kGroup / 8);
-        scale_row[m] = o * a.groups;
-    }
-    const T *x[kBlocks];
+    for (int i = 0; i < 4; ++i) code_row[i] = a.codes + (long long)min(o0 + warp * 32 + i * 8 + row, a.outputs - 1) * (a.inputs / 2);
+    auto fetch = [&](int c) {                                               // activations of chunk c, then its codes
+        uint8_t *stage = smem + (c & 1) * S::kBytes;
+        const int i0 = (g0 + c * S::kGroups) * kGroup, n = min(kChunk, (g1 - g0 - c * S::kGroups) * kGroup);
+#pragma unroll 4
+        for (int i = tid; i < 8 * kBlocks * (kChunk / 8); i += kThreads) {
+            const int r = i / (kChunk / 8), piece = i % (kChunk / 8);
+            copy_async(stage + S::kX + r * S::kXRow + piece * 16,
+                       static_cast<const T *>(a.x) + (long long)min(t0 + r, a.rows - 1) * a.x_row + i0 + (piece * 8 < n ? piece * 8 : 0), piece * 8 < n);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        // a warp's own rows, 128 inputs after the other
 #pragma unroll
-    for (int n = 0; n < kBlocks; ++n) x[n] = static_cast<const T *>(a.x) + (long long)min(t0 + n * 8 + row, a.rows - 1) * a.x_row + quad * (kGroup / 4);
+        for (int q = 0; q < 4; ++q) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int piece = 4 * q + quad;
+                copy_async(stage + (warp * 32 + i * 8 + row) * S::kCodeRow + piece * 16, code_row[i] + i0 / 2 + (piece * 32 < n ? piece * 16 : 0), piece * 32 < n);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    };
+    // An output's scales of a chunk: one load of 8 or 16 bytes (two of group 32) where rows of scales allow it; else as many as there are groups, each of
+    // which meets 32 lines (7 x 4096 x 11008: 2.5 us of 15).
+    constexpr int kWide = S::kGroups < 8 ? S::kGroups : 8;
+    typedef std::conditional_t<kWide == 8, uint4, uint2> Wide;
+    alignas(16) T scale[S::kGroups];
+    const bool wide = a.groups % kWide == 0 && g0 % kWide == 0 && reinterpret_cast<uintptr_t>(a.scales) % sizeof(Wide) == 0;
+    auto fetch_scales = [&](int c) {
+        const int left = g1 - g0 - c * S::kGroups;
+        if (wide && left >= S::kGroups) {
+#pragma unroll
+            for (int g = 0; g < S::kGroups; g += kWide)
+                *reinterpret_cast<Wide *>(scale + g) = __ldg(reinterpret_cast<const Wide *>(scales + c * S::kGroups + g));
+            return;
+        }
+#pragma unroll
+        for (int g = 0; g < S::kGroups; ++g)
+            if (g < left) scale[g] = __ldg(scales + c * S::kGroups + g);
+    };
     float sum[2][kBlocks][4];
 #pragma unroll
     for (int m = 0; m < 2; ++m)
@@ -93,19 +157,33 @@ __global__ void __launch_bounds__(kThreads) matmul_mma_kernel(const W4Args a)
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[m][n][i] = 0.f;
 
-    for (int g = g0; g < g1; g += kAhead) {
-        Load w[kAhead][4];
+    fetch(0);
+    fetch_scales(0);
+#pragma unroll 1
+    for (int c = 0; c < chunks; ++c) {
+        uint8_t *stage = smem + (c & 1) * S::kBytes;
+        float *held = reinterpret_cast<float *>(stage + S::kScales);        // [group][output]
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j)
+        for (int g = 0; g < S::kGroups; ++g) held[g * kTile + tid] = (float)scale[g];
+        asm volatile("cp.async.wait_group 4;" ::: "memory");               // the activations
+        __syncthreads();
+        const bool more = c + 1 < chunks;
+        if (more) {
+            fetch(c + 1);
+            fetch_scales(c + 1);
+        }
+        const int groups = min(S::kGroups, g1 - g0 - c * S::kGroups);
+        const uint8_t *codes = stage + (warp * 32 + row) * S::kCodeRow + quad * (S::kWords * 4);
+        const uint8_t *x = stage + S::kX + row * S::kXRow + quad * (S::kWords * 16);
 #pragma unroll
-            for (int m = 0; m < 4; ++m)
-                if (g + j < g1) w[j][m] = __ldg(reinterpret_cast<const Load *>(codes[m] + (long long)(g + j) * (kGroup / 2)));
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (g + j >= g1) break;
-            float s[4], acc[2][kBlocks][4];
-#pragma unroll
-            for (int m = 0; m < 4; ++m) s[m] = scale_of<T>(a.scales, scale_row[m] + g + j);
+        for (int g = 0; g < S::kGroups; ++g) {                              // unrolled: a group's chain is long, and they overlap
+            if (g >= groups) break;
+            if (g * kGroup % 128 == 0) {                                    // the next 128 inputs of this warp's codes
+                if (more) wait_copies<8>(g * kGroup / 128);
+                else wait_copies<3>(g * kGroup / 128);
+                __syncwarp();
+            }
+            float acc[2][kBlocks][4];
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -113,34 +191,49 @@ __global__ void __launch_bounds__(kThreads) matmul_mma_kernel(const W4Args a)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.f;
 #pragma unroll
-            for (int k = 0; k < kWords; ++k) {
-                uint32_t b[kBlocks][4];
-#pragma unroll
-                for (int n = 0; n < kBlocks; ++n) {
-                    // the pairs (0, 4), (1, 5), (2, 6), (3, 7) of eight inputs, as the codes come
-                    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(x[n] + (long long)(g + j) * kGroup + k * 8));
-                    b[n][0] = __byte_perm(v.x, v.z, 0x5410);
-                    b[n][1] = __byte_perm(v.x, v.z, 0x7632);
-                    b[n][2] = __byte_perm(v.y, v.w, 0x5410);
-                    b[n][3] = __byte_perm(v.y, v.w, 0x7632);
-                }
-                uint32_t c[4][4];
+            for (int j = 0; j < kGroup / S::kSub; ++j) {
+                const int at = g * kGroup + j * S::kSub;
+                uint32_t w[4][S::kWords];
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
-                    const uint32_t word = reinterpret_cast<const uint32_t *>(&w[j][m])[k];
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) c[m][p] = code_pair<T>(word >> (4 * p));
+                    const uint8_t *p = codes + m * 8 * S::kCodeRow + at / 2;
+                    if constexpr (S::kWords == 2) {
+                        const uint2 v = *reinterpret_cast<const uint2 *>(p);
+                        w[m][0] = v.x;
+                        w[m][1] = v.y;
+                    } else {
+                        w[m][0] = *reinterpret_cast<const uint32_t *>(p);
+                    }
                 }
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+                for (int k = 0; k < S::kWords; ++k) {
+                    uint32_t b[kBlocks][4];
 #pragma unroll
                     for (int n = 0; n < kBlocks; ++n) {
-                        const uint32_t lo[4] = {c[2 * m][0], c[2 * m + 1][0], c[2 * m][1], c[2 * m + 1][1]};
-                        const uint32_t hi[4] = {c[2 * m][2], c[2 * m + 1][2], c[2 * m][3], c[2 * m + 1][3]};
-                        mma16816<T>(acc[m][n], lo, b[n][0], b[n][1]);
-                        mma16816<T>(acc[m][n], hi, b[n][2], b[n][3]);
+                        // the pairs (0, 4), (1, 5), (2, 6), (3, 7) of eight inputs, as the codes come
+                        const uint4 v = *reinterpret_cast<const uint4 *>(x + n * 8 * S::kXRow + at * 2 + k * 16);
+                        b[n][0] = __byte_perm(v.x, v.z, 0x5410);
+                        b[n][1] = __byte_perm(v.x, v.z, 0x7632);
+                        b[n][2] = __byte_perm(v.y, v.w, 0x5410);
+                        b[n][3] = __byte_perm(v.y, v.w, 0x7632);
                     }
+                    uint32_t p[4][4];
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) unpack<T>(w[m][k], p[m]);
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int n = 0; n < kBlocks; ++n) {
+                            const uint32_t lo[4] = {p[2 * m][0], p[2 * m + 1][0], p[2 * m][1], p[2 * m + 1][1]};
+                            const uint32_t hi[4] = {p[2 * m][2], p[2 * m + 1][2], p[2 * m][3], p[2 * m + 1][3]};
+                            mma16816<T>(acc[m][n], lo, b[n][0], b[n][1]);
+                            mma16816<T>(acc[m][n], hi, b[n][2], b[n][3]);
+                        }
+                }
             }
+            float s[4];
+#pragma unroll
+            for (int m = 0; m < 4; ++m) s[m] = held[g * kTile + warp * 32 + m * 8 + row];
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -149,29 +242,32 @@ __global__ void __launch_bounds__(kThreads) matmul_mma_kernel(const W4Args a)
                     for (int i = 0; i < 4; ++i) sum[m][n][i] = fmaf(s[2 * m + (i >> 1)], acc[m][n][i], sum[m][n][i]);
         }
     }
+    // An output's parts go to the CTA whose share of the tile it is, [rank][row][output of the share]: a barrier less than fetching them there.
+    const int share = kTile / split;
+    float *part = reinterpret_cast<float *>(smem + (chunks_of(a.groups, split, S::kGroups) > 1 ? 2 : 1) * S::kBytes);
+    cluster_wait();                                                 // every CTA has begun
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < 2; ++m) {
+        const int o = warp * 32 + m * 16;                           // the 16 outputs from here are of one share
+        const uint32_t there = mapa_rank(smem_u32(part + rank * (8 * kBlocks) * share + o % share + row), o / share);
 #pragma unroll
         for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                part[(n * 8 + quad * 2 + (i & 1)) * kTile + warp * 32 + m * 16 + (i >> 1) * 8 + row] = sum[m][n][i];
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there + 4 * ((n * 8 + quad * 2 + (i & 1)) * share + (i >> 1) * 8)), "f"(sum[m][n][i]) : "memory");
+    }
     cluster_sync_all();
-    // results are shared out over the cluster; neighbours in a warp are neighbours in memory
-    for (int i = rank * kThreads + threadIdx.x; i < 8 * kBlocks * kTile; i += split * kThreads) {
-        const int t = t0 + i / kTile, o = blockIdx.y * kTile + i % kTile;
-        if (t >= a.rows || o >= a.outputs) continue;
-        float y = 0.f;
-        for (uint32_t c = 0; c < split; ++c) {
-            float v;
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(mapa_rank(smem_u32(part + i), c)) : "memory");
-            y += v;
-        }
+    const int rows = min(8 * kBlocks, a.rows - t0);
+    for (int i = tid; i < rows * share; i += kThreads) {
+        const int t = t0 + i / share, o = o0 + rank * share + i % share;
+        float y = part[i];
+#pragma unroll
+        for (uint32_t c = 1; c < kMaxSplit; ++c) y = c < split ? y + part[c * (8 * kBlocks) * share + i] : y;
+        if (o >= a.outputs) continue;
         if (a.relu && y < 0.f) y = 0.f;
         if (a.residual) y += (float)static_cast<const T *>(a.residual)[t * a.residual_row + o];
         static_cast<T *>(a.out)[t * a.out_row + o] = from_float<T>(y);
     }
-    cluster_sync_all();                                             // the others may still read this CTA's part
 }
 
 // ---- quantisation --------------------------------------------------------------------------------------------------
@@ -210,11 +306,21 @@ template <typename F> cudaError_t by_group(int group, F &&f)
 
 template <typename T, int kGroup, int kBlocks> cudaError_t launch_mma(const W4Args &a, int sms, cudaStream_t stream)
 {
+    using S = Stage<kGroup, kBlocks>;
     const int tiles = (a.outputs + kTile - 1) / kTile, steps = (a.rows + 8 * kBlocks - 1) / (8 * kBlocks);
     // CTAs that share a tile's inputs: until there are four a SM, each with 512 inputs at least
     int split = 1;
-    while (split < kMaxSplit && (long long)tiles * steps * split < 4LL * sms && a.inputs / (split * 2) >= 512) split *= 2;
-    const size_t smem = sizeof(float) * 8 * kBlocks * kTile;
+    while (split < kMaxSplit && (long long)tiles * steps * split < 4LL * sms && a.inputs / (split * 2) >= kChunk) split *= 2;
+    const size_t smem = (chunks_of(a.groups, split, S::kGroups) > 1 ? 2 : 1) * (size_t)S::kBytes + 8 * kBlocks * kTile * sizeof(float);
+    static std::atomic<bool> ready[64];                             // by device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && (dev >= 64 || !ready[dev])) {
+        e = cudaFuncSetAttribute(matmul_mma_kernel<T, kGroup, kBlocks>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 2 * S::kBytes + 8 * kBlocks * kTile * (int)sizeof(float));
+        if (e == cudaSuccess && dev < 64) ready[dev] = true;
+    }
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

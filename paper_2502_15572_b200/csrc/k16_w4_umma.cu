@@ -119,6 +119,14 @@ template <> __device__ __forceinline__ void unpack<__nv_bfloat16>(uint32_t w, ui
     }
 }
 
+template <typename T> __device__ __forceinline__ void unpack(const uint4 &w, uint32_t *p)
+{
+    unpack<T>(w.x, p);
+    unpack<T>(w.y, p + 4);
+    unpack<T>(w.z, p + 8);
+    unpack<T>(w.w, p + 12);
+}
+
 template <typename T, int kGroup>
 __global__ void __launch_bounds__(kThreads, 1)
 matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ UmmaArgs a)
@@ -274,16 +282,13 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
                 }
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
+                    uint32_t p[16];
+                    unpack<T>(w[2 * q], p);                     // before the slot is free
                     if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&sh.a_empty[half][q], a_phase, wl));
                     tc_fence_after();
-#pragma unroll
-                    for (int c = 2 * q; c < 2 * q + 2; ++c) {
-                        uint32_t p[16];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            unpack<T>(i == 0 ? w[c].x : i == 1 ? w[c].y : i == 2 ? w[c].z : w[c].w, p + 4 * i);
-                        if (ok) tmem_st16(to + 16 * c, p);
-                    }
+                    if (ok) tmem_st16(to + 32 * q, p);
+                    unpack<T>(w[2 * q + 1], p);
+                    if (ok) tmem_st16(to + 32 * q + 16, p);
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
@@ -342,19 +347,28 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
                     for (int i = 16 * c; i < 16 * c + 16; ++i) part[i * kOutputs + r] = sum[i];
                 }
             } else if (o < a.w.outputs) {
-                T *out = static_cast<T *>(a.w.out) + o;
-                const T *residual = a.w.residual ? static_cast<const T *>(a.w.residual) + o : nullptr;
+                T *out = static_cast<T *>(a.w.out) + t0 * a.w.out_row + o;
+                const T *residual = a.w.residual ? static_cast<const T *>(a.w.residual) + t0 * a.w.residual_row + o : nullptr;
+                const int rows = min(a.n, a.w.rows - t0);
+                if (a.w.relu) {
+#pragma unroll
+                    for (int i = 0; i < kTileRows; ++i) sum[i] = sum[i] < 0.f ? 0.f : sum[i];
+                }
+                // (checks and products of a row's address, all in one loop: a tenth of a long call)
 #pragma unroll
                 for (int c = 0; c < kTileRows / 16; ++c) {
-                    if (c * 16 >= a.n) break;
+                    if (c * 16 >= rows) break;
+                    if (residual) {
 #pragma unroll
-                    for (int i = 16 * c; i < 16 * c + 16; ++i) {
-                        const int t = t0 + i;
-                        if (t >= a.w.rows) continue;
-                        float y = sum[i];
-                        if (a.w.relu && y < 0.f) y = 0.f;
-                        if (residual) y += (float)residual[t * a.w.residual_row];
-                        out[t * a.w.out_row] = (T)y;
+                        for (int i = 0; i < 16; ++i) {
+                            if (c * 16 + i < rows) sum[16 * c + i] += (float)*residual;
+                            residual += a.w.residual_row;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        if (c * 16 + i < rows) *out = (T)sum[16 * c + i];
+                        out += a.w.out_row;
                     }
                 }
             }
