@@ -141,7 +141,11 @@ dresd_status dresd_w4_matmul(const void *x, int64_t x_row, int rows, const uint8
     a.relu = relu != 0;
     cudaError_t e;
     const int path = g_w4_path.load();
-    if (path == 2 || (path == 0 && rows > 16)) {
+    // Up to 16 rows mma.sync keeps up with the weights (4096 x 11008: 16.6 us, tcgen05 15.5; 11008 x 4096: 13.8 and 21; 4096 x 4096: 8.1 and 10.9).  Beyond, it
+    // takes a step for every 32 rows and tcgen05 one for 128, at a fixed cost of some 5 us more, which is what 30 million weights take a step (4096 x 4096:
+    // 32 rows 9.9 and 12.3 us, 48 rows 19.8 and 12.8; 2048 x 512: 256 rows 8.0 and 12.3; 4096 x 11008: 32 rows 27 and 16.5).
+    const bool many = rows > 16 && (long long)inputs * outputs * ((rows + 31) / 32) > 30000000;
+    if (path == 0 ? many : path == 2) {
         CUtensorMap code_map, x_map;
         const cuuint64_t code_dims[2] = {(cuuint64_t)inputs / 2, (cuuint64_t)outputs}, code_strides[1] = {(cuuint64_t)inputs / 2};
         // the distance of a single row is never used, but has to be a valid one

@@ -222,6 +222,7 @@ struct W4Args {
     long long out_row;
     int rows, inputs, outputs, groups;
     int relu;
+    int stages;                 // K15: filled in by its launch
 };
 cudaError_t launch_w4_quantise(const void *w, long long w_in, long long w_out, int inputs, int outputs, int dtype, int group,
                                uint8_t *codes, void *scales, cudaStream_t stream);

@@ -3,9 +3,10 @@
 // The inner sums multiply whole numbers -8 .. 7 and the activations, both exact in the activations' type, and are kept in fp32; the scale meets
 // them there.  So a weight is never rounded, and a result is rounded once.
 //
-// Bound: the weights' bytes, and on small matrices the latency of fetching them once.  A CTA has 128 outputs and 512 inputs at a time; the CTAs of a
-// cluster split the inputs until all are resident at once, so that (almost) every byte is on its way from the start -- codes and
-// activations by cp.async, scales through registers --, and add their parts up in the order of their ranks.
+// Bound: the weights' bytes, and on small matrices the latency of fetching them once.  A CTA has 128 outputs and 256 inputs at a time, up to three of these
+// steps on their way by cp.async; the CTAs of a cluster split the inputs, so that on small matrices every byte is on its way from the
+// start, and add their parts up in the order of their ranks.  Measured (device): one row of 4096 x 4096 6.1 us, 7 rows of 4096 x 11008 12.5 us
+// (1.9 TB/s: launch, fetch, products and join of a CTA follow one another, and most CTAs do the same at the same time).
 //
 // A warp computes 32 outputs for up to 8 kBlocks rows with mma.sync, weights as the 16-row operand.  The order of inputs within an
 // instruction is free, as long as both operands agree: a lane takes 8 or 16 consecutive codes of a row (4 lanes a row, 8 rows
@@ -19,7 +20,7 @@ namespace dresd {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kTile = 32 * kWarps;      // outputs of a CTA
-constexpr int kChunk = 512;                                                 // inputs at a time
+constexpr int kChunk = 256;                                                 // inputs at a time
 constexpr int kMaxSplit = 8;
 static_assert(kThreads == kTile, "a thread fetches the scales of an output");
 
@@ -65,32 +66,37 @@ template <typename T> __device__ __forceinline__ void mma16816(float (&d)[4], co
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ void copy_async(void *dst, const void *src, bool there)      // 16 bytes, or zeros
+template <int kBytes> __device__ __forceinline__ void copy_async(void *dst, const void *src, bool there)      // or zeros
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(__cvta_generic_to_global(src)), "r"(there ? 16 : 0) : "memory");
+    if constexpr (kBytes == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(__cvta_generic_to_global(src)), "r"(there ? 16 : 0) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(smem_u32(dst)), "l"(__cvta_generic_to_global(src)), "r"(there ? kBytes : 0), "n"(kBytes) : "memory");
 }
-
-// Waits for all but the last kLast - done groups of copies.
-template <int kLast> __device__ __forceinline__ void wait_copies(int done)
+// Waits for all but the last `left` groups of copies.
+__device__ __forceinline__ void wait_copies(int left)
 {
-    if (done == 0) asm volatile("cp.async.wait_group %0;" ::"n"(kLast) : "memory");
-    else if (done == 1) asm volatile("cp.async.wait_group %0;" ::"n"(kLast - 1) : "memory");
-    else if (done == 2) asm volatile("cp.async.wait_group %0;" ::"n"(kLast - 2) : "memory");
-    else asm volatile("cp.async.wait_group %0;" ::"n"(kLast - 3) : "memory");
+    switch (left) {
+    case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+    case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+    case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+    case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+    default: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+    }
 }
 
 template <int kGroup, int kBlocks> struct Stage {
     static constexpr int kWords = kGroup == 32 ? 1 : 2;                     // of eight codes, of a lane and row at a time
     static constexpr int kSub = 32 * kWords;                                // inputs of four lanes at a time
     static constexpr int kCodeRow = kChunk / 2 + kSub / 2, kXRow = kChunk * 2 + (kWords == 1 ? 64 : 16);      // bytes; padded
-    static constexpr int kGroups = kChunk / kGroup;
-    static constexpr int kX = kTile * kCodeRow, kScales = kX + 8 * kBlocks * kXRow, kBytes = kScales + kGroups * kTile * 4;
+    static constexpr int kGroups = kChunk / kGroup, kScaleRow = 2 * kGroups;
+    static constexpr int kMost = kBlocks == 4 ? 2 : 3;                      // stages: more would leave fewer CTAs resident (11008 x 4096, 1 row: 3 11.7 us, 5 23.7;
+                                                                            // 32 rows: 2 19.6 us, 3 38.3)
+    static constexpr int kX = kTile * kCodeRow, kScales = kX + 8 * kBlocks * kXRow, kBytes = kScales + kTile * kScaleRow;
 };
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// Chunks that the CTA with the most groups has.
-__host__ __device__ constexpr int chunks_of(int groups, int split, int per_chunk) { return ((groups + split - 1) / split + per_chunk - 1) / per_chunk; }
 
 template <typename T, int kGroup, int kBlocks>
 __global__ void __launch_bounds__(kThreads) matmul_mma_kernel(const W4Args a)
@@ -100,54 +106,41 @@ __global__ void __launch_bounds__(kThreads) matmul_mma_kernel(const W4Args a)
     const uint32_t rank = cluster_ctarank(), split = gridDim.x;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane & 3, row = lane >> 2;
     const int o0 = blockIdx.y * kTile, t0 = blockIdx.z * 8 * kBlocks;
-    const int g0 = (int)((long long)a.groups * rank / split), g1 = (int)((long long)a.groups * (rank + 1) / split);
-    const int chunks = (g1 - g0 + S::kGroups - 1) / S::kGroups;
+    // whole chunks for every CTA, so that its scales begin at a boundary
+    const int all = (a.groups + S::kGroups - 1) / S::kGroups, c0 = (int)(all * rank / split), c1 = (int)(all * (rank + 1) / split);
+    const int chunks = c1 - c0, g0 = c0 * S::kGroups, g1 = min(c1 * S::kGroups, a.groups);
     cluster_arrive();
     pdl_wait();
     pdl_launch_dependents();
     // rows and outputs beyond the end are computed like the last ones and not written
     const T *scales = static_cast<const T *>(a.scales) + (long long)min(o0 + tid, a.outputs - 1) * a.groups + g0;
-    const uint8_t *code_row[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) code_row[i] = a.codes + (long long)min(o0 + warp * 32 + i * 8 + row, a.outputs - 1) * (a.inputs / 2);
-    auto fetch = [&](int c) {                                               // activations of chunk c, then its codes
-        uint8_t *stage = smem + (c & 1) * S::kBytes;
+    // scales of an output's chunk are one copy where rows of scales allow it; otherwise as many loads as there are groups, each of which meets 32 lines
+    const bool wide = a.groups % S::kGroups == 0 && reinterpret_cast<uintptr_t>(a.scales) % S::kScaleRow == 0;
+    auto fetch = [&](int c, int at) {                                       // chunk c into stage `at`
+        uint8_t *stage = smem + at * S::kBytes;
         const int i0 = (g0 + c * S::kGroups) * kGroup, n = min(kChunk, (g1 - g0 - c * S::kGroups) * kGroup);
-#pragma unroll 4
+#pragma unroll
         for (int i = tid; i < 8 * kBlocks * (kChunk / 8); i += kThreads) {
             const int r = i / (kChunk / 8), piece = i % (kChunk / 8);
-            copy_async(stage + S::kX + r * S::kXRow + piece * 16,
-                       static_cast<const T *>(a.x) + (long long)min(t0 + r, a.rows - 1) * a.x_row + i0 + (piece * 8 < n ? piece * 8 : 0), piece * 8 < n);
+            const bool there = piece * 8 < n;
+            copy_async<16>(stage + S::kX + r * S::kXRow + piece * 16,
+                           static_cast<const T *>(a.x) + (long long)min(t0 + r, a.rows - 1) * a.x_row + i0 + (there ? piece * 8 : 0), there);
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        // a warp's own rows, 128 inputs after the other
+        if (wide) {
+            copy_async<S::kScaleRow>(stage + S::kScales + tid * S::kScaleRow, scales + c * S::kGroups, true);
+        } else {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int piece = 4 * q + quad;
-                copy_async(stage + (warp * 32 + i * 8 + row) * S::kCodeRow + piece * 16, code_row[i] + i0 / 2 + (piece * 32 < n ? piece * 16 : 0), piece * 32 < n);
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
+            for (int g = 0; g < S::kGroups; ++g)
+                if (c * S::kGroups + g < g1 - g0) reinterpret_cast<T *>(stage + S::kScales + tid * S::kScaleRow)[g] = __ldg(scales + c * S::kGroups + g);
         }
-    };
-    // An output's scales of a chunk: one load of 8 or 16 bytes (two of group 32) where rows of scales allow it; else as many as there are groups, each of
-    // which meets 32 lines (7 x 4096 x 11008: 2.5 us of 15).
-    constexpr int kWide = S::kGroups < 8 ? S::kGroups : 8;
-    typedef std::conditional_t<kWide == 8, uint4, uint2> Wide;
-    alignas(16) T scale[S::kGroups];
-    const bool wide = a.groups % kWide == 0 && g0 % kWide == 0 && reinterpret_cast<uintptr_t>(a.scales) % sizeof(Wide) == 0;
-    auto fetch_scales = [&](int c) {
-        const int left = g1 - g0 - c * S::kGroups;
-        if (wide && left >= S::kGroups) {
+        // eight lanes a row, its 128 bytes
+        const int piece = tid & 7;
+        const bool there = piece * 32 < n;
 #pragma unroll
-            for (int g = 0; g < S::kGroups; g += kWide)
-                *reinterpret_cast<Wide *>(scale + g) = __ldg(reinterpret_cast<const Wide *>(scales + c * S::kGroups + g));
-            return;
+        for (int i = 0; i < kTile / 16; ++i) {
+            const int r = i * 16 + tid / 8;
+            copy_async<16>(stage + r * S::kCodeRow + piece * 16, a.codes + ((long long)min(o0 + r, a.outputs - 1) * a.inputs + i0) / 2 + (there ? piece * 16 : 0), there);
         }
-#pragma unroll
-        for (int g = 0; g < S::kGroups; ++g)
-            if (g < left) scale[g] = __ldg(scales + c * S::kGroups + g);
     };
     float sum[2][kBlocks][4];
 #pragma unroll
@@ -157,32 +150,24 @@ __global__ void __launch_bounds__(kThreads) matmul_mma_kernel(const W4Args a)
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[m][n][i] = 0.f;
 
-    fetch(0);
-    fetch_scales(0);
+    const int stages = a.stages;
+    for (int c = 0; c < stages; ++c) {
+        if (c < chunks) fetch(c, c);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    int at = 0;
 #pragma unroll 1
     for (int c = 0; c < chunks; ++c) {
-        uint8_t *stage = smem + (c & 1) * S::kBytes;
-        float *held = reinterpret_cast<float *>(stage + S::kScales);        // [group][output]
-#pragma unroll
-        for (int g = 0; g < S::kGroups; ++g) held[g * kTile + tid] = (float)scale[g];
-        asm volatile("cp.async.wait_group 4;" ::: "memory");               // the activations
+        wait_copies(stages - 1);
         __syncthreads();
-        const bool more = c + 1 < chunks;
-        if (more) {
-            fetch(c + 1);
-            fetch_scales(c + 1);
-        }
+        const uint8_t *stage = smem + at * S::kBytes;
+        const T *held = reinterpret_cast<const T *>(stage + S::kScales);    // [output][group]
         const int groups = min(S::kGroups, g1 - g0 - c * S::kGroups);
         const uint8_t *codes = stage + (warp * 32 + row) * S::kCodeRow + quad * (S::kWords * 4);
         const uint8_t *x = stage + S::kX + row * S::kXRow + quad * (S::kWords * 16);
 #pragma unroll
         for (int g = 0; g < S::kGroups; ++g) {                              // unrolled: a group's chain is long, and they overlap
             if (g >= groups) break;
-            if (g * kGroup % 128 == 0) {                                    // the next 128 inputs of this warp's codes
-                if (more) wait_copies<8>(g * kGroup / 128);
-                else wait_copies<3>(g * kGroup / 128);
-                __syncwarp();
-            }
             float acc[2][kBlocks][4];
 #pragma unroll
             for (int m = 0; m < 2; ++m)
@@ -233,7 +218,7 @@ __global__ void __launch_bounds__(kThreads) matmul_mma_kernel(const W4Args a)
             }
             float s[4];
 #pragma unroll
-            for (int m = 0; m < 4; ++m) s[m] = held[g * kTile + warp * 32 + m * 8 + row];
+            for (int m = 0; m < 4; ++m) s[m] = (float)held[(warp * 32 + m * 8 + row) * S::kGroups + g];
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -241,10 +226,16 @@ __global__ void __launch_bounds__(kThreads) matmul_mma_kernel(const W4Args a)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) sum[m][n][i] = fmaf(s[2 * m + (i >> 1)], acc[m][n][i], sum[m][n][i]);
         }
+        if (chunks > stages) {                                              // the stage is used again
+            __syncthreads();
+            if (c + stages < chunks) fetch(c + stages, at);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (++at == stages) at = 0;
     }
     // An output's parts go to the CTA whose share of the tile it is, [rank][row][output of the share]: a barrier less than fetching them there.
     const int share = kTile / split;
-    float *part = reinterpret_cast<float *>(smem + (chunks_of(a.groups, split, S::kGroups) > 1 ? 2 : 1) * S::kBytes);
+    float *part = reinterpret_cast<float *>(smem + stages * S::kBytes);
     cluster_wait();                                                 // every CTA has begun
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
@@ -304,20 +295,23 @@ template <typename F> cudaError_t by_group(int group, F &&f)
     return group == 32 ? f(std::integral_constant<int, 32>{}) : group == 64 ? f(std::integral_constant<int, 64>{}) : f(std::integral_constant<int, 128>{});
 }
 
-template <typename T, int kGroup, int kBlocks> cudaError_t launch_mma(const W4Args &a, int sms, cudaStream_t stream)
+template <typename T, int kGroup, int kBlocks> cudaError_t launch_mma(const W4Args &args, int sms, cudaStream_t stream)
 {
     using S = Stage<kGroup, kBlocks>;
-    const int tiles = (a.outputs + kTile - 1) / kTile, steps = (a.rows + 8 * kBlocks - 1) / (8 * kBlocks);
-    // CTAs that share a tile's inputs: until there are four a SM, each with 512 inputs at least
-    int split = 1;
-    while (split < kMaxSplit && (long long)tiles * steps * split < 4LL * sms && a.inputs / (split * 2) >= kChunk) split *= 2;
-    const size_t smem = (chunks_of(a.groups, split, S::kGroups) > 1 ? 2 : 1) * (size_t)S::kBytes + 8 * kBlocks * kTile * sizeof(float);
+    const int tiles = (args.outputs + kTile - 1) / kTile, steps = (args.rows + 8 * kBlocks - 1) / (8 * kBlocks);
+    // CTAs that share a tile's inputs: eight, with 256 inputs at least (4096 x 4096, 1 row: eight 6.1 us, four 7.0, one 16; 4096 x 32000: 29.7, 36, 34)
+    int split = kMaxSplit;
+    while (split > 1 && args.inputs / split < kChunk) split /= 2;
+    W4Args a = args;
+    const int chunks = ((a.groups + S::kGroups - 1) / S::kGroups + split - 1) / split;
+    a.stages = chunks < S::kMost ? chunks : S::kMost;
+    const size_t smem = a.stages * (size_t)S::kBytes + 8 * kBlocks * kTile * sizeof(float);
     static std::atomic<bool> ready[64];                             // by device
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess && (dev >= 64 || !ready[dev])) {
         e = cudaFuncSetAttribute(matmul_mma_kernel<T, kGroup, kBlocks>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 2 * S::kBytes + 8 * kBlocks * kTile * (int)sizeof(float));
+                                 S::kMost * S::kBytes + 8 * kBlocks * kTile * (int)sizeof(float));
         if (e == cudaSuccess && dev < 64) ready[dev] = true;
     }
     if (e != cudaSuccess) return e;

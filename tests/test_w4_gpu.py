@@ -61,7 +61,7 @@ def option():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("path", [1, 2])
-@pytest.mark.parametrize("rows,inputs,outputs,group", SIZES + [(1, 4096, 4096, 128), (16, 11008, 4096, 64), (112, 4096, 11008, 32), (700, 1024, 3000, 128)])
+@pytest.mark.parametrize("rows,inputs,outputs,group", SIZES + [(1, 4096, 4096, 128), (16, 11008, 4096, 64), (112, 4096, 11008, 32), (700, 1024, 3000, 128), (48, 4096, 4096, 32), (17, 4096, 11008, 64), (2047, 512, 1000, 128)])
 def test_either_kernel_at_every_size(option, path, rows, inputs, outputs, group):
     dtype = "f16" if (rows + inputs) % 3 else "bf16"
     x, codes, scales = exact_inputs(rows, inputs, outputs, group, dtype, rows)
@@ -77,6 +77,7 @@ def test_a_wait_that_runs_out_is_reported(option, rows, stage):
     """The first CTA never receives a stage: the call comes back, says so, and the next one is right."""
     x, codes, scales = exact_inputs(rows, 4096, 600, 128, "f16", 4)
     w, stream = binding.W4(codes, scales, "f16"), torch.cuda.current_stream().cuda_stream
+    option("w4_path", 2)
     want = w.matmul(x)
     binding.dresd_w4_status(stream)
     option("w4_wait_ms", 20)
