@@ -24,7 +24,7 @@ namespace dresd {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCtas = 16;
-constexpr int kBins = 2048, kGroups = kBins / 32, kSteps = 64;
+constexpr int kBins = 2048, kGroups = kBins / 32, kSteps = 64, kList = 64;
 constexpr double kOne = 4398046511104.0;                       // 2^42, the largest weight
 constexpr float kOctaves = 44.f;                               // a weight 2^-44 of the largest rounds to 0
 constexpr int kTable = 64;                                     // 2^(-j / 64)
@@ -101,6 +101,9 @@ struct alignas(16) Shared {                     // the cache of 16-byte blocks l
     int tied[kMaxCtas];
     int count[kMaxCtas];                       // of logits above -infinity
     uint32_t top[kMaxCtas];
+    float list_x[kWarps][kList];               // logits that are left, by index, and where they lie
+    int list_at[kWarps][kList];
+    int spilled[kMaxCtas];                     // of every CTA: a warp has more than that
     u64 above, target;                         // found by warp 0
     int position;
     int token;                                 // written by the CTA that finds it, in every CTA
@@ -147,12 +150,17 @@ struct Sampler {
     float top_high, top_low;     // top log2(e) / T, the first part a multiple of 1/64 and not less
     float bin_rate;              // half logits to bins
     int buffer;                  // histogram that is free
+    int w0, w1;                  // this warp's blocks
+    int listed;                  // logits in this warp's list; -1: none is kept
     __device__ __forceinline__ Sampler(Shared &s_, uint4 *cache_, int cached_, uint32_t rank_, uint32_t ctas_, const T *p, int V)
-        : s(s_), cache(cache_), cached(cached_), rank(rank_), ctas(ctas_), row(p, V), buffer(0)
+        : s(s_), cache(cache_), cached(cached_), rank(rank_), ctas(ctas_), row(p, V), buffer(0), listed(-1)
     {
         const int per = (row.blocks + ctas - 1) / ctas;
         q0 = min((int)rank * per, row.blocks);
         q1 = min(q0 + per, row.blocks);
+        const int each = (q1 - q0 + kWarps - 1) / kWarps;
+        w0 = min(q0 + (int)(threadIdx.x >> 5) * each, q1);
+        w1 = min(w0 + each, q1);
     }
     __device__ __forceinline__ void block(int q, float (&x)[kVec]) const { values<T>(q - q0 < cached ? cache[q - q0] : row.load(q), x); }
 
@@ -387,23 +395,58 @@ struct Sampler {
         buffer ^= 1;
         return s.position;
     }
-    // f(x) for blocks from .. to - 1 in turn, `stride` at a time, the next load ahead; f is called by whole warps (what is not there is
-    // -infinity).  One copy of f: at depth 0 its instructions come from far.
+    // f(x) for blocks from .. to - 1 in turn, `stride` at a time, the next load ahead, or for what is in the warp's list; f is called by
+    // whole warps (what is not there is -infinity).  One copy of f: at depth 0 its instructions come from far.
     template <typename F> __device__ __forceinline__ void each_block(int from, int to, int stride, F &&f) const
     {
         const int me = stride == 32 ? threadIdx.x & 31 : threadIdx.x;
         auto load = [&](int q) {
             constexpr uint32_t low = Logit<T>::kLowest;
-            return q >= to ? make_uint4(low, low, low, low) : q - q0 < cached ? cache[q - q0] : row.load(q);
+            return listed >= 0 || q >= to ? make_uint4(low, low, low, low) : q - q0 < cached ? cache[q - q0] : row.load(q);
         };
+        const int steps = listed >= 0 ? (listed + 31) / 32 : to > from ? (to - from + stride - 1) / stride : 0;
         uint4 next = load(from + me);
 #pragma unroll 1
-        for (int base = from, j = 0; base < to; base += stride, ++j) {
+        for (int j = 0; j < steps; ++j) {
             float x[kVec];
             values<T>(next, x);
-            next = load(base + stride + me);
+            if (listed >= 0) x[0] = of_list(j);
+            next = load(from + (j + 1) * stride + me);
             f(x, j);
         }
+    }
+    __device__ __forceinline__ float of_list(int j) const      // this lane's logit of step j
+    {
+        const int i = j * 32 + (threadIdx.x & 31);
+        return i < listed ? s.list_x[threadIdx.x >> 5][i] : -INFINITY;
+    }
+    // Keeps the logits that are not below `low` in lists, if every warp of the cluster has room for its own: further passes look at these alone.
+    __device__ __forceinline__ void gather(float low)
+    {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        int held = 0;
+        each_block(w0, w1, 32, [&](const float (&x)[kVec], int j) {
+            unsigned few = 0;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) few |= x[i] >= low ? 1u << i : 0u;
+            if (!__any_sync(0xFFFFFFFFu, few != 0)) return;
+            const int mine = __popc(few), up_to = scan_warp(mine);
+            int at = held + up_to - mine;
+            held += __shfl_sync(0xFFFFFFFFu, up_to, 31);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                if (few >> i & 1) {
+                    if (at < kList) {
+                        s.list_x[warp][at] = x[i];
+                        s.list_at[warp][at] = (w0 + j * 32 + lane) * kVec + i - row.first;
+                    }
+                    ++at;
+                }
+        });
+        const int spills = __syncthreads_or(held > kList);
+        if (warp == 0 && lane < (int)ctas) *in_cta(&s.spilled[rank], lane) = spills;
+        cluster_sync_all();
+        if (!__any_sync(0xFFFFFFFFu, lane < (int)ctas && s.spilled[lane])) listed = held;
     }
 
     // The shortest part of `cut`, in descending order and then by index, whose weights reach the share `p` of all its weights (by weight), or that
@@ -418,6 +461,7 @@ struct Sampler {
             if (mine > cut.x) add_one<false>(bin(mine), 1);
             u64 none = 0, aim = k;
             low = edge(find(kBins, none, aim, -1.f));
+            gather(low);
         }
         // the first histogram
         each_block(q0, q1, kThreads, [&](const float (&x)[kVec], int) {
@@ -479,16 +523,15 @@ struct Sampler {
     __device__ __forceinline__ int draw(const Cut &cut, float u, bool greedy, float &logit)
     {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        // a warp has `per` consecutive blocks, 32 at a time; an entry sums up 1 << fold of these steps
-        const int per = (q1 - q0 + kWarps - 1) / kWarps, w0 = min(q0 + warp * per, q1), w1 = min(w0 + per, q1);
-        const int steps = (per + 31) / 32;
+        // a warp has consecutive blocks, 32 at a time; an entry sums up 1 << fold of these steps
+        const int steps = ((q1 - q0 + kWarps - 1) / kWarps + 31) / 32, own = listed >= 0 ? (listed + 31) / 32 : (w1 - w0 + 31) / 32;
         int fold = 0;
         while (((steps + (1 << fold) - 1) >> fold) > kSteps) ++fold;
         u64 w_warp = 0, w = 0;
         int n_warp = 0, n = 0;
         each_block(w0, w1, 32, [&](const float (&x)[kVec], int j) {
             sums(x, cut, w, n);
-            if ((j + 1) % (1 << fold) != 0 && j + 1 < (w1 - w0 + 31) / 32) return;
+            if ((j + 1) % (1 << fold) != 0 && j + 1 < own) return;
             const bool some = __any_sync(0xFFFFFFFFu, w != 0 || n != 0);
             if (some) {
                 w = sum_warp(w);
@@ -503,7 +546,7 @@ struct Sampler {
             w = 0;
             n = 0;
         });
-        const int mine_entries = ((w1 - w0 + 31) / 32 + (1 << fold) - 1) >> fold;
+        const int mine_entries = (own + (1 << fold) - 1) >> fold;
         if (lane == 0) {
             s.warp_weight[warp] = w_warp;
             s.warp_ties[warp] = n_warp;
@@ -557,14 +600,15 @@ struct Sampler {
                     e += 32;
                 }
             // its step, lane and element
-            for (int j = e << fold; j < steps; ++j) {
+            for (int j = e << fold; j < own; ++j) {
                 float x[kVec];
                 u64 w = 0;
                 int n = 0;
                 const int q = w0 + j * 32 + lane;
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) x[i] = -INFINITY;
-                if (q < w1) block(q, x);
+                if (listed >= 0) x[0] = of_list(j);
+                else if (q < w1) block(q, x);
                 sums(x, cut, w, n);
                 const u64 ws = scan_warp(w);
                 const int ns = scan_warp(n);
@@ -587,7 +631,7 @@ struct Sampler {
                 const u64 one = weight(mine), we = scan_warp(mine > cut.x ? one : 0);
                 const int ne = scan_warp((int)(mine == cut.x));
                 const int i = __ffs(__ballot_sync(0xFFFFFFFFu, running(w_before + we, n_before + ne) > aim)) - 1;
-                const int token = (w0 + j * 32 + l) * kVec + i - row.first;
+                const int token = listed >= 0 ? s.list_at[warp][j * 32 + l] : (w0 + j * 32 + l) * kVec + i - row.first;
                 mine = __shfl_sync(0xFFFFFFFFu, mine, i);
                 if (lane < (int)ctas) {
                     *in_cta(&s.token, lane) = token;

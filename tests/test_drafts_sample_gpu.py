@@ -131,6 +131,28 @@ def test_large_vocabularies(V, B, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("order", ["mixed", "falling", "rising", "few values", "one value", "few left"])
+def test_the_largest_few_of_long_rows(dtype, order):
+    """Short lists of what is left, and rows whose largest logits all lie in one place, or are too many of a kind, for them."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    B, V = 40, 70003
+    x = torch.randn((B, 1, V), device="cuda", generator=g) * 2
+    if order in ("falling", "rising"):
+        x = x.sort(-1, descending=order == "falling").values
+    elif order == "few values":
+        x = (x * 2).round()
+    elif order == "one value":
+        x = torch.ones_like(x)
+    elif order == "few left":
+        x[:, :, 37:] = -float("inf")
+    u = np.random.default_rng(7).random((B, 1))
+    k = np.array([1, 2, 7, 40, 100, 127, 128, 129, 300, 5000] * 4)
+    check(x.to(DT[dtype]), u, temperature=0.9, top_k=k)
+    check(x.to(DT[dtype]), u, temperature=0.9, top_k=k, top_p=0.7)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 def test_any_address_and_distance(dtype):
     """Rows that begin at every element of a 16-byte block, with strangers between them that would win."""
