@@ -312,7 +312,7 @@ dresd_status dresd_drafts_sample(const void *logits, dresd_dtype dtype, int64_t 
  * dresd_w4_matmul    out[t][o] = f(sum_i w[o][i] x[t][i]) + residual[t][o],  f(y) = max(y, 0) if relu != 0, otherwise y
  *     x              [rows][inputs], 16-byte aligned, rows x_row elements apart (a multiple of 8)
  *     residual       [rows][outputs], residual_row apart, or NULL; may be `out` itself
- *     out            [rows][outputs], out_row apart
+ *     out            [rows][outputs], out_row apart; shares no memory with x, codes, scales or a residual that is not `out` itself
  *   Products of (c - 8) and x are exact, their sums and the scales' products in fp32; one rounding, to `dtype`.  The order of
  *   summation depends on the sizes only.
  * Both are asynchronous on `stream`, on the current device; no workspace.

@@ -37,6 +37,8 @@ inline bool is_device_ptr(const void *p, int device)
 }
 
 inline bool aligned(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+// The same for int32 and fp32 arrays.
+inline bool is_word_ptr(const void *p, int device) { return aligned(p, 4) && is_device_ptr(p, device); }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,

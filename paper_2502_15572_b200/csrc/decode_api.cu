@@ -59,14 +59,14 @@ dresd_status dresd_drafts_sample(const void *logits, dresd_dtype dtype, int64_t 
     if (st != DRESD_OK) return st;
     if (!is_device_ptr(logits, dev) || !aligned(logits, dtype == DRESD_F32 ? 4 : 2))
         return fail(DRESD_ERR_INVALID, "logits must be an aligned pointer of the current device");
-    if (n > 0 && (!is_device_ptr(drafts, dev) || !is_device_ptr(valid, dev)))
-        return fail(DRESD_ERR_INVALID, "drafts/valid must be pointers of the current device");
-    if (!is_device_ptr(uniform, dev) || (temperature && !is_device_ptr(temperature, dev)) || (top_k && !is_device_ptr(top_k, dev)) ||
-        (top_p && !is_device_ptr(top_p, dev)))
-        return fail(DRESD_ERR_INVALID, "uniform/temperature/top_k/top_p must be pointers of the current device (the last three may be NULL)");
-    if (!is_device_ptr(out_best, dev) || !is_device_ptr(out_len, dev) || !is_device_ptr(out_tokens, dev) ||
-        (out_logprobs && !is_device_ptr(out_logprobs, dev)))
-        return fail(DRESD_ERR_INVALID, "out_* must be pointers of the current device (out_logprobs may be NULL)");
+    if (n > 0 && (!is_word_ptr(drafts, dev) || !is_word_ptr(valid, dev)))
+        return fail(DRESD_ERR_INVALID, "drafts/valid must be 4-byte aligned pointers of the current device");
+    if (!is_word_ptr(uniform, dev) || (temperature && !is_word_ptr(temperature, dev)) || (top_k && !is_word_ptr(top_k, dev)) ||
+        (top_p && !is_word_ptr(top_p, dev)))
+        return fail(DRESD_ERR_INVALID, "uniform/temperature/top_k/top_p must be 4-byte aligned pointers of the current device (the last three may be NULL)");
+    if (!is_word_ptr(out_best, dev) || !is_word_ptr(out_len, dev) || !is_word_ptr(out_tokens, dev) ||
+        (out_logprobs && !is_word_ptr(out_logprobs, dev)))
+        return fail(DRESD_ERR_INVALID, "out_* must be 4-byte aligned pointers of the current device (out_logprobs may be NULL)");
     SampleArgs a{};
     a.logits = logits;
     a.chunk_stride = chunk_stride;
@@ -158,7 +158,7 @@ dresd_status dresd_w4_matmul(const void *x, int64_t x_row, int rows, const uint8
         e = launch_w4_umma(code_map, x_map, a, (int)dtype, group, ms > 0 ? ms * 2000000LL : 4000000000LL, g_w4_lose_stage.load(), sms,
                            static_cast<cudaStream_t>(stream));
     } else {
-        e = launch_w4_matmul(a, (int)dtype, group, sms, static_cast<cudaStream_t>(stream));
+        e = launch_w4_matmul(a, (int)dtype, group, static_cast<cudaStream_t>(stream));
     }
     return e == cudaSuccess ? DRESD_OK : fail_cuda(e, "w4_matmul launch");
 }

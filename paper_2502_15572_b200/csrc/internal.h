@@ -226,7 +226,7 @@ struct W4Args {
 };
 cudaError_t launch_w4_quantise(const void *w, long long w_in, long long w_out, int inputs, int outputs, int dtype, int group,
                                uint8_t *codes, void *scales, cudaStream_t stream);
-cudaError_t launch_w4_matmul(const W4Args &a, int dtype, int group, int sms, cudaStream_t stream);
+cudaError_t launch_w4_matmul(const W4Args &a, int dtype, int group, cudaStream_t stream);
 // K16, many rows.  Tensor maps: codes as bytes [outputs][inputs / 2] (boxes of 64 x 256, 64-byte swizzle), x [rows][inputs] (boxes of
 // 64 x w4_umma_rows(rows), 128-byte swizzle).
 int w4_umma_rows(int rows);

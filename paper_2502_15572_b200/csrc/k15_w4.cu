@@ -79,9 +79,7 @@ __device__ __forceinline__ void wait_copies(int left)
     switch (left) {
     case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
     case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
-    case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
-    case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
-    default: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+    default: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
     }
 }
 
@@ -295,7 +293,7 @@ template <typename F> cudaError_t by_group(int group, F &&f)
     return group == 32 ? f(std::integral_constant<int, 32>{}) : group == 64 ? f(std::integral_constant<int, 64>{}) : f(std::integral_constant<int, 128>{});
 }
 
-template <typename T, int kGroup, int kBlocks> cudaError_t launch_mma(const W4Args &args, int sms, cudaStream_t stream)
+template <typename T, int kGroup, int kBlocks> cudaError_t launch_mma(const W4Args &args, cudaStream_t stream)
 {
     using S = Stage<kGroup, kBlocks>;
     const int tiles = (args.outputs + kTile - 1) / kTile, steps = (args.rows + 8 * kBlocks - 1) / (8 * kBlocks);
@@ -331,21 +329,21 @@ template <typename T, int kGroup, int kBlocks> cudaError_t launch_mma(const W4Ar
     return cudaLaunchKernelEx(&cfg, matmul_mma_kernel<T, kGroup, kBlocks>, a);
 }
 
-template <typename T> cudaError_t launch_type(const W4Args &a, int group, int sms, cudaStream_t stream)
+template <typename T> cudaError_t launch_type(const W4Args &a, int group, cudaStream_t stream)
 {
     return by_group(group, [&](auto g) {
         constexpr int kGroup = decltype(g)::value;
-        return a.rows <= 8    ? launch_mma<T, kGroup, 1>(a, sms, stream)
-               : a.rows <= 16 ? launch_mma<T, kGroup, 2>(a, sms, stream)
-                              : launch_mma<T, kGroup, 4>(a, sms, stream);
+        return a.rows <= 8    ? launch_mma<T, kGroup, 1>(a, stream)
+               : a.rows <= 16 ? launch_mma<T, kGroup, 2>(a, stream)
+                              : launch_mma<T, kGroup, 4>(a, stream);
     });
 }
 
 }  // namespace
 
-cudaError_t launch_w4_matmul(const W4Args &a, int dtype, int group, int sms, cudaStream_t stream)
+cudaError_t launch_w4_matmul(const W4Args &a, int dtype, int group, cudaStream_t stream)
 {
-    return dtype == kF16 ? launch_type<__half>(a, group, sms, stream) : launch_type<__nv_bfloat16>(a, group, sms, stream);
+    return dtype == kF16 ? launch_type<__half>(a, group, stream) : launch_type<__nv_bfloat16>(a, group, stream);
 }
 
 cudaError_t launch_w4_quantise(const void *w, long long w_in, long long w_out, int inputs, int outputs, int dtype, int group,

@@ -83,6 +83,8 @@ dresd_status check_pages(dresd_kv *kv, const dresd_kv_batch *b, bool whole, KvAr
     const dresd_status st = check_call(kv, 0, b, whole, out);
     if (st != DRESD_OK) return st;
     if (!kv->pages.refs) return fail(DRESD_ERR_INVALID, "the cache has no page counts: dresd_kv_attach_pages() comes first");
+    if (!aligned(b->page_table, 4) || !aligned(b->ctx, 4) || (whole && !aligned(b->start, 4)))
+        return fail(DRESD_ERR_INVALID, "page_table/ctx/start must be 4-byte aligned");
     return DRESD_OK;
 }
 
@@ -305,7 +307,7 @@ dresd_status dresd_kv_attach_pages(dresd_kv *kv, int32_t *refs)
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev != kv->device)
         return fail(DRESD_ERR_INVALID, "the cache belongs to device %d; the current device is %d", kv->device, dev);
-    if (!is_device_ptr(refs, dev) || !aligned(refs, 4))
+    if (!is_word_ptr(refs, dev))
         return fail(DRESD_ERR_INVALID, "refs must be an aligned pointer of the cache's device");
     if (!kv->pages.last) {
         const size_t n = (size_t)kv->args.num_pages, words = 7 * n + kMaxKvBatch + kPageCounts;
@@ -345,7 +347,7 @@ dresd_status dresd_kv_fork(dresd_kv *kv, const dresd_kv_batch *batch, int32_t *c
     kv->last_launches = 0;
     if (a.B == 0) return DRESD_OK;
     if (ctx != a.ctx) return fail(DRESD_ERR_INVALID, "ctx must be the batch's");
-    if (!is_device_ptr(parent, kv->device)) return fail(DRESD_ERR_INVALID, "parent must be a pointer of the cache's device");
+    if (!is_word_ptr(parent, kv->device)) return fail(DRESD_ERR_INVALID, "parent must be an aligned pointer of the cache's device");
     kv->last_stream = static_cast<cudaStream_t>(stream);
     const cudaError_t e = launch_kv_fork(a, kv->pages.refs, const_cast<int32_t *>(a.table), ctx, parent, kv->last_stream);
     if (e != cudaSuccess) return fail_cuda(e, "kv_fork launch");
@@ -359,7 +361,7 @@ dresd_status dresd_kv_reserve(dresd_kv *kv, const dresd_kv_batch *batch, int32_t
     dresd_status st = check_pages(kv, batch, true, &a);
     if (st != DRESD_OK) return st;
     kv->last_launches = 0;
-    if (!is_device_ptr(out_missing, kv->device)) return fail(DRESD_ERR_INVALID, "out_missing must be a pointer of the cache's device");
+    if (!is_word_ptr(out_missing, kv->device)) return fail(DRESD_ERR_INVALID, "out_missing must be an aligned pointer of the cache's device");
     kv->last_stream = static_cast<cudaStream_t>(stream);
     if (a.B == 0 || a.rows == 0) {
         const cudaError_t e = cudaMemsetAsync(out_missing, 0, sizeof(int32_t), kv->last_stream);
@@ -378,7 +380,7 @@ dresd_status dresd_kv_release(dresd_kv *kv, const dresd_kv_batch *batch, const i
     if (st != DRESD_OK) return st;
     kv->last_launches = 0;
     if (a.B == 0) return DRESD_OK;
-    if (!is_device_ptr(keep, kv->device)) return fail(DRESD_ERR_INVALID, "keep must be a pointer of the cache's device");
+    if (!is_word_ptr(keep, kv->device)) return fail(DRESD_ERR_INVALID, "keep must be an aligned pointer of the cache's device");
     kv->last_stream = static_cast<cudaStream_t>(stream);
     const cudaError_t e = launch_kv_release(a, kv->pages.refs, const_cast<int32_t *>(a.table), keep, kv->last_stream);
     if (e != cudaSuccess) return fail_cuda(e, "kv_release launch");
@@ -392,7 +394,7 @@ dresd_status dresd_kv_compact(dresd_kv *kv, const dresd_kv_batch *batch, int32_t
     dresd_status st = check_pages(kv, batch, false, &a);
     if (st != DRESD_OK) return st;
     kv->last_launches = 0;
-    if (!is_device_ptr(out_used, kv->device)) return fail(DRESD_ERR_INVALID, "out_used must be a pointer of the cache's device");
+    if (!is_word_ptr(out_used, kv->device)) return fail(DRESD_ERR_INVALID, "out_used must be an aligned pointer of the cache's device");
     kv->last_stream = static_cast<cudaStream_t>(stream);
     const cudaError_t e = launch_kv_compact(a, kv->pages, const_cast<int32_t *>(a.table), out_used, kv->sms, kv->last_stream);
     if (e != cudaSuccess) return fail_cuda(e, "kv_compact launch");

@@ -211,6 +211,7 @@ class Speculator:
     def run(self, count: int):
         """At least `count` tokens for every sequence: lists of tokens, and the steps that it took.  ``score``: the logarithms of
         their probabilities, where tokens are drawn."""
+        import torch
         texts, logs, steps = [[int(t)] for t in self.last.tolist()], [row[:1] for row in self.logs.tolist()], 0
         while min(map(len, texts)) < count:
             out, length = self.step()
@@ -221,6 +222,8 @@ class Speculator:
                 for log, row, m in zip(logs, self.logs.tolist(), length.tolist()):
                     log += row[:m]
         self.cache.status()
+        if isinstance(self.model.w_vocab, binding.W4):
+            binding.dresd_w4_status(torch.cuda.current_stream().cuda_stream)
         if int(self.missing):
             raise RuntimeError(f"the pool had {int(self.missing)} pages too few")
         self.score = [sum(log[:count]) for log in logs]
