@@ -13,7 +13,10 @@
 // Cuts are found from the largest logit down with histograms of 2048 bins.  The first one has bins of equal width in (max - x) / T, over the 44 octaves in
 // which weights are not 0: logits spread over many of them, while bits of a float's exponent would put most into a few, whose
 // atomic additions then wait for one another.  Further ones divide the range of keys of the bin that was hit, until a bin is one key; the
-// second one is the last for 16-bit logits as a rule, and looks at one group of 32 bins.
+// second one is the last for 16-bit logits as a rule, and looks at one group of 32 bins.  A small top_k needs none of this: see few().
+//
+// Measured (device): one row of 32000 with top_p 18 us, with top_k 50 12.5; ten drafts of ten of 32000 29.6; 16 sequences of 3 x 20 of 100003 77 (some 8600
+// cycles a row); 64 rows of 151001 in fp32 with top_k 40 25.5 (1.5 TB/s: the row is read at 4 TB/s or so, and five exchanges follow), top_k 200 103.
 #include <atomic>
 #include <cfloat>
 
@@ -24,7 +27,8 @@ namespace dresd {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCtas = 16;
-constexpr int kBins = 2048, kGroups = kBins / 32, kSteps = 64, kList = 64;
+constexpr int kBins = 2048, kGroups = kBins / 32, kSteps = 64;
+constexpr int kFew = 512, kFewKept = 128;                     // see few()
 constexpr double kOne = 4398046511104.0;                       // 2^42, the largest weight
 constexpr float kOctaves = 44.f;                               // a weight 2^-44 of the largest rounds to 0
 constexpr int kTable = 64;                                     // 2^(-j / 64)
@@ -101,9 +105,10 @@ struct alignas(16) Shared {                     // the cache of 16-byte blocks l
     int tied[kMaxCtas];
     int count[kMaxCtas];                       // of logits above -infinity
     uint32_t top[kMaxCtas];
-    float list_x[kWarps][kList];               // logits that are left, by index, and where they lie
-    int list_at[kWarps][kList];
-    int spilled[kMaxCtas];                     // of every CTA: a warp has more than that
+    float2 few[kFew];                          // of the cluster's first CTA: logits that are left, with the bits of their indices, in any order
+    float2 kept[kFewKept];                     // the largest of them, in order
+    u64 kept_weight[2][kFewKept];              // without and with top_p
+    int few_count;
     u64 above, target;                         // found by warp 0
     int position;
     int token;                                 // written by the CTA that finds it, in every CTA
@@ -151,9 +156,8 @@ struct Sampler {
     float bin_rate;              // half logits to bins
     int buffer;                  // histogram that is free
     int w0, w1;                  // this warp's blocks
-    int listed;                  // logits in this warp's list; -1: none is kept
     __device__ __forceinline__ Sampler(Shared &s_, uint4 *cache_, int cached_, uint32_t rank_, uint32_t ctas_, const T *p, int V)
-        : s(s_), cache(cache_), cached(cached_), rank(rank_), ctas(ctas_), row(p, V), buffer(0), listed(-1)
+        : s(s_), cache(cache_), cached(cached_), rank(rank_), ctas(ctas_), row(p, V), buffer(0)
     {
         const int per = (row.blocks + ctas - 1) / ctas;
         q0 = min((int)rank * per, row.blocks);
@@ -395,74 +399,123 @@ struct Sampler {
         buffer ^= 1;
         return s.position;
     }
-    // f(x) for blocks from .. to - 1 in turn, `stride` at a time, the next load ahead, or for what is in the warp's list; f is called by
-    // whole warps (what is not there is -infinity).  One copy of f: at depth 0 its instructions come from far.
+    // f(x) for blocks from .. to - 1 in turn, `stride` at a time, the next load ahead; f is called by whole warps (what is not there is
+    // -infinity).  One copy of f: at depth 0 its instructions come from far.
     template <typename F> __device__ __forceinline__ void each_block(int from, int to, int stride, F &&f) const
     {
         const int me = stride == 32 ? threadIdx.x & 31 : threadIdx.x;
         auto load = [&](int q) {
             constexpr uint32_t low = Logit<T>::kLowest;
-            return listed >= 0 || q >= to ? make_uint4(low, low, low, low) : q - q0 < cached ? cache[q - q0] : row.load(q);
+            return q >= to ? make_uint4(low, low, low, low) : q - q0 < cached ? cache[q - q0] : row.load(q);
         };
-        const int steps = listed >= 0 ? (listed + 31) / 32 : to > from ? (to - from + stride - 1) / stride : 0;
+        const int steps = to > from ? (to - from + stride - 1) / stride : 0;
         uint4 next = load(from + me);
 #pragma unroll 1
         for (int j = 0; j < steps; ++j) {
             float x[kVec];
             values<T>(next, x);
-            if (listed >= 0) x[0] = of_list(j);
             next = load(from + (j + 1) * stride + me);
             f(x, j);
         }
     }
-    __device__ __forceinline__ float of_list(int j) const      // this lane's logit of step j
-    {
-        const int i = j * 32 + (threadIdx.x & 31);
-        return i < listed ? s.list_x[threadIdx.x >> 5][i] : -INFINITY;
-    }
-    // Keeps the logits that are not below `low` in lists, if every warp of the cluster has room for its own: further passes look at these alone.
-    __device__ __forceinline__ void gather(float low)
+
+    // A small top_k (of fewer logits than there are): the token from the k largest logits themselves.  The k-th largest of the threads' largest logits
+    // is not above the k-th largest of all, so only threads whose largest (`mine`) is not below it have to look at theirs again; what they
+    // find is brought to the first CTA.  There a logit's place in the order, and its running sums, are counted against each of the others.
+    // Nothing depends on the order in which they came.  false: more than kFew of them, nothing is drawn.
+    // (64 rows of 151001, top_k 40, top_p: 25.5 us; with histograms of what is left in lists 48.7, of whole rows 103.)
+    __device__ __forceinline__ bool few(int k, float p, float u, float mine, float &logit, int &token)
     {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        int held = 0;
-        each_block(w0, w1, 32, [&](const float (&x)[kVec], int j) {
-            unsigned few = 0;
+        if (mine > -INFINITY) add_one<false>(bin(mine), 1);
+        u64 none = 0, aim = k;
+        const float low = edge(find(kBins, none, aim, -1.f));
+        int *const count = in_cta(&s.few_count, 0);
+        float2 *const found = in_cta(s.few, 0);
+        for (unsigned m = __ballot_sync(0xFFFFFFFFu, mine >= low); m; m &= m - 1) {
+            // the warp looks at that thread's blocks
+            const int first = q0 + warp * 32 + __ffs(m) - 1;
+            for (int q = first + lane * kThreads; q < q1; q += 32 * kThreads) {
+                float x[kVec];
+                block(q, x);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) few |= x[i] >= low ? 1u << i : 0u;
-            if (!__any_sync(0xFFFFFFFFu, few != 0)) return;
-            const int mine = __popc(few), up_to = scan_warp(mine);
-            int at = held + up_to - mine;
-            held += __shfl_sync(0xFFFFFFFFu, up_to, 31);
-#pragma unroll
-            for (int i = 0; i < kVec; ++i)
-                if (few >> i & 1) {
-                    if (at < kList) {
-                        s.list_x[warp][at] = x[i];
-                        s.list_at[warp][at] = (w0 + j * 32 + lane) * kVec + i - row.first;
+                for (int i = 0; i < kVec; ++i)
+                    if (x[i] >= low) {
+                        const int at = atomicAdd(count, 1);
+                        if (at < kFew) found[at] = make_float2(x[i], __int_as_float(q * kVec + i - row.first));
                     }
-                    ++at;
-                }
-        });
-        const int spills = __syncthreads_or(held > kList);
-        if (warp == 0 && lane < (int)ctas) *in_cta(&s.spilled[rank], lane) = spills;
+            }
+        }
         cluster_sync_all();
-        if (!__any_sync(0xFFFFFFFFu, lane < (int)ctas && s.spilled[lane])) listed = held;
+        const int all = *count;
+        if (all > kFew) {
+            cluster_sync_all();                                   // before the count is set back
+            return false;
+        }
+        if (rank == 0) {
+            for (int i = threadIdx.x; i < all; i += kThreads) {
+                const float2 me = s.few[i];
+                int before = 0;
+                for (int j = 0; j < all; ++j) {
+                    const float2 other = s.few[j];
+                    before += other.x > me.x || (other.x == me.x && __float_as_int(other.y) < __float_as_int(me.y));
+                }
+                if (before < k) {
+                    s.kept[before] = me;
+                    s.kept_weight[0][before] = weight(me.x);
+                }
+            }
+            __syncthreads();
+            const int r = threadIdx.x;
+            if (r < k) {
+                u64 before = 0, whole = 0;
+                for (int j = 0; j < k; ++j) {
+                    const u64 w = s.kept_weight[0][j];
+                    whole += w;
+                    before += j < r ? w : 0;
+                }
+                const u64 target = p < 1.f ? max((u64)__double2ll_ru((double)fmaxf(p, 0.f) * (double)whole), 1ull) : ~0ull;
+                s.kept_weight[1][r] = before < target ? s.kept_weight[0][r] : 0;
+            }
+            __syncthreads();
+            if (r < k || r == kFewKept) {
+                const int me = r < k ? __float_as_int(s.kept[r].y) : 0;
+                u64 before = 0, whole = 0;
+                for (int j = 0; j < k; ++j) {
+                    const u64 w = s.kept_weight[1][j];
+                    whole += w;
+                    before += __float_as_int(s.kept[j].y) < me ? w : 0;
+                }
+                if (r == kFewKept) {
+                    s.log_whole = ::log((double)whole / kOne);    // by a warp of its own
+                } else {
+                    const u64 at = target_of(u, whole);
+                    if (before <= at && at < before + s.kept_weight[1][r])
+                        for (uint32_t c = 0; c < ctas; ++c) {
+                            *in_cta(&s.token, c) = me;
+                            *in_cta(&s.logit, c) = s.kept[r].x;
+                        }
+                }
+            }
+        }
+        cluster_sync_all();
+        logit = s.logit;
+        token = s.token;
+        return true;
+    }
+    // floor(u S)
+    static __device__ __forceinline__ u64 target_of(float u, u64 whole)
+    {
+        return (u64)__double2ll_rz((double)fminf(fmaxf(u, 0.f), 1.f - 0x1p-24f) * (double)whole);
     }
 
     // The shortest part of `cut`, in descending order and then by index, whose weights reach the share `p` of all its weights (by weight), or that
-    // has `k` logits (otherwise; it has more in all).  mine: the thread's largest logit.
+    // has `k` logits (otherwise; it has more in all).
     template <bool by_weight>
-    __device__ __forceinline__ Cut select(const Cut &cut, float p, u64 k, float mine)
+    __device__ __forceinline__ Cut select(const Cut &cut, float p, u64 k)
     {
         u64 before = 0, target = k;
-        float low = by_weight ? least : -FLT_MAX;             // logits below are not looked at
-        if (!by_weight && row.blocks > 4 * kThreads * (int)ctas && k <= kThreads / 2) {
-            // The k-th largest of the threads' largest logits is not above the k-th largest of all: few are left to be counted.
-            if (mine > cut.x) add_one<false>(bin(mine), 1);
-            u64 none = 0, aim = k;
-            low = edge(find(kBins, none, aim, -1.f));
-            gather(low);
-        }
+        const float low = by_weight ? least : -FLT_MAX;       // logits below are not looked at
         // the first histogram
         each_block(q0, q1, kThreads, [&](const float (&x)[kVec], int) {
             bool any = false;
@@ -524,7 +577,7 @@ struct Sampler {
     {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         // a warp has consecutive blocks, 32 at a time; an entry sums up 1 << fold of these steps
-        const int steps = ((q1 - q0 + kWarps - 1) / kWarps + 31) / 32, own = listed >= 0 ? (listed + 31) / 32 : (w1 - w0 + 31) / 32;
+        const int steps = ((q1 - q0 + kWarps - 1) / kWarps + 31) / 32, own = (w1 - w0 + 31) / 32;
         int fold = 0;
         while (((steps + (1 << fold) - 1) >> fold) > kSteps) ++fold;
         u64 w_warp = 0, w = 0;
@@ -578,7 +631,7 @@ struct Sampler {
             n_before += c < rank ? s.tied[c] : 0;
         }
         // the first element whose running sum passes `aim`
-        const u64 aim = greedy ? 0 : (u64)__double2ll_rz((double)fminf(fmaxf(u, 0.f), 1.f - 0x1p-24f) * (double)whole);
+        const u64 aim = greedy ? 0 : target_of(u, whole);
         auto running = [&](u64 weight_before, int ties_before) { return weight_before + (u64)min(ties_before, cut.ties) * tie; };
         if (running(w_before, n_before) <= aim && running(w_before + w_warp, n_before + n_warp) > aim) {     // one warp of the cluster
             // the entry
@@ -607,8 +660,7 @@ struct Sampler {
                 const int q = w0 + j * 32 + lane;
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) x[i] = -INFINITY;
-                if (listed >= 0) x[0] = of_list(j);
-                else if (q < w1) block(q, x);
+                if (q < w1) block(q, x);
                 sums(x, cut, w, n);
                 const u64 ws = scan_warp(w);
                 const int ns = scan_warp(n);
@@ -631,7 +683,7 @@ struct Sampler {
                 const u64 one = weight(mine), we = scan_warp(mine > cut.x ? one : 0);
                 const int ne = scan_warp((int)(mine == cut.x));
                 const int i = __ffs(__ballot_sync(0xFFFFFFFFu, running(w_before + we, n_before + ne) > aim)) - 1;
-                const int token = listed >= 0 ? s.list_at[warp][j * 32 + l] : (w0 + j * 32 + l) * kVec + i - row.first;
+                const int token = (w0 + j * 32 + l) * kVec + i - row.first;
                 mine = __shfl_sync(0xFFFFFFFFu, mine, i);
                 if (lane < (int)ctas) {
                     *in_cta(&s.token, lane) = token;
@@ -676,17 +728,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         Sampler<T> one(s, cache, cached, rank, ctas, logits + (long long)at * a.row_stride, a.V);
         const float u = a.uniform[(long long)b * (L + 1) + t];
         one.clear(0, 0);
+        if (threadIdx.x == 0) s.few_count = 0;
         float mine;
         const int valid = one.maximum(mine);
         one.scales();
-        Cut cut{-INFINITY, 0};
-        if (greedy) cut = Cut{one.top, 1};
-        else if (valid > 0) {
-            if (top_k > 0 && top_k < valid) cut = one.template select<false>(cut, 0.f, top_k, mine);
-            if (top_p < 1.f) cut = one.template select<true>(cut, fmaxf(top_p, 0.f), 0, mine);
-        }
         float logit = 0.f;
-        const int token = valid > 0 ? one.draw(cut, u, greedy, logit) : -1;
+        int token = -1;
+        const bool cut_k = !greedy && top_k > 0 && top_k < valid;
+        if (valid > 0 && !(cut_k && top_k <= kFewKept && one.row.blocks >= 4 * top_k && one.few(top_k, top_p, u, mine, logit, token))) {
+            Cut cut{-INFINITY, 0};
+            if (greedy) cut = Cut{one.top, 1};
+            if (cut_k) cut = one.template select<false>(cut, 0.f, top_k);
+            if (!greedy && top_p < 1.f) cut = one.template select<true>(cut, fmaxf(top_p, 0.f), 0);
+            token = one.draw(cut, u, greedy, logit);
+        }
         if (rank == 0 && threadIdx.x == 0) {
             a.out_tokens[(long long)b * (L + 1) + t] = token;
             if (a.out_logs)
@@ -717,24 +772,59 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     cluster_sync_all();                                       // a row without logits leaves the others' words unread until here
 }
 
+constexpr int kRoom[2] = {112 * 1024, 225 * 1024};            // shared memory of a CTA: two a SM, or one
+
+// Clusters of `ctas` that are resident at once, with kRoom[which].  A cluster lies in one GPC, and some have fewer SMs than others (of 16 CTAs, two a
+// SM: 14 clusters, not 18).
+template <typename T> cudaError_t resident(int dev, int ctas, int which, int sms, int *clusters)
+{
+    static std::atomic<int> known[64][kMaxCtas + 1][2];       // by device; + 1
+    *clusters = ctas == 1 ? (2 - which) * sms : dev < 64 ? known[dev][ctas][which].load() - 1 : -1;
+    if (*clusters >= 0) return cudaSuccess;
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kRoom[which];
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaOccupancyMaxActiveClusters(clusters, sample_kernel<T>, &cfg);
+    if (e == cudaSuccess && dev < 64) known[dev][ctas][which].store(*clusters + 1);
+    return e;
+}
+
 template <typename T> cudaError_t launch(SampleArgs a, int sms, cudaStream_t stream)
 {
-    // CTAs of a cluster: as many as are resident at once, two a SM, each with 1024 logits at least
-    a.ctas = 1;
-    while (a.ctas < kMaxCtas && a.B * a.ctas * 2 <= 2 * sms && a.V / (a.ctas * 2) >= 1024) a.ctas *= 2;
-    // a row's piece is kept in shared memory as far as it goes
-    const int vec = 16 / (int)sizeof(T), blocks = (a.V + 2 * vec - 2) / vec, per = (blocks + a.ctas - 1) / a.ctas;
-    const int room = (int)(((a.B * a.ctas <= sms ? 225 : 112) * 1024 - sizeof(Shared)) / 16), cached = per < room ? per : room;
-    const size_t smem = sizeof(Shared) + 16 * (size_t)cached;
     static std::atomic<bool> ready[64];                       // by device
-    int dev = 0;
+    int dev = 0, clusters = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess && (dev >= 64 || !ready[dev])) {
-        e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024);
+        e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom[1]);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e == cudaSuccess && dev < 64) ready[dev] = true;
     }
     if (e != cudaSuccess) return e;
+    // CTAs of a cluster: as many as there is room for at two a SM, each with 1024 logits at least.  Without drafts all rows take the same time, and those
+    // that wait double the call's (16 rows of 32000, top_k: clusters of 16 23.3 us, of 8 12.5); with drafts sequences
+    // end one by one, and a few may wait (16 sequences, 3 x 20 of 100003: 77 us, 88).
+    a.ctas = 1;
+    while (a.ctas < kMaxCtas && a.B * a.ctas * 2 <= 2 * sms && a.V / (a.ctas * 2) >= 1024) a.ctas *= 2;
+    for (; a.n == 0 && a.ctas > 1; a.ctas /= 2) {
+        if ((e = resident<T>(dev, a.ctas, 0, sms, &clusters)) != cudaSuccess) return e;
+        if (clusters >= a.B) break;
+    }
+    // a row's piece is kept in shared memory as far as it goes; with one CTA a SM if all clusters find room so
+    const int vec = 16 / (int)sizeof(T), blocks = (a.V + 2 * vec - 2) / vec, per = (blocks + a.ctas - 1) / a.ctas;
+    int room = (int)((kRoom[0] - sizeof(Shared)) / 16);
+    if (per > room) {
+        if ((e = resident<T>(dev, a.ctas, 1, sms, &clusters)) != cudaSuccess) return e;
+        if (clusters >= a.B) room = (int)((kRoom[1] - sizeof(Shared)) / 16);
+    }
+    const int cached = per < room ? per : room;
+    const size_t smem = sizeof(Shared) + 16 * (size_t)cached;
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

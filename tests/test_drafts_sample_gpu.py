@@ -27,7 +27,7 @@ def ref_row(x, u, temperature=1.0, top_k=0, top_p=1.0):
     if not temperature > 0:
         return int(np.argmax(x)), 0.0
     with np.errstate(invalid="ignore", over="ignore"):
-        below = np.where(x == top, 0.0, (x - top) / np.float64(temperature))
+        below = np.where(x == top, 0.0, (x - top) / np.float64(min(temperature, 1e36)))
         below = np.where(x == -np.inf, -np.inf, below)
     w = np.rint(ONE * np.exp(below)).astype(np.int64)
     order = np.lexsort((np.arange(len(x)), -x))                # descending, then by index
@@ -150,6 +150,27 @@ def test_the_largest_few_of_long_rows(dtype, order):
     k = np.array([1, 2, 7, 40, 100, 127, 128, 129, 300, 5000] * 4)
     check(x.to(DT[dtype]), u, temperature=0.9, top_k=k)
     check(x.to(DT[dtype]), u, temperature=0.9, top_k=k, top_p=0.7)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("top", [0.0, 2.0, np.inf])
+@pytest.mark.parametrize("equal", [1, 59, 60, 61, 511, 512, 513, 1500])
+def test_equal_logits_around_top_k(dtype, top, equal):
+    """More or fewer of the largest than top_k takes, and than are looked at together; zeros of both signs, NaN among them."""
+    g = np.random.default_rng(equal)
+    B, V, k = 6, 9001, np.array([60, 60, 128, 1, 100, 60])
+    x = -1 - np.abs(g.standard_normal((B, 1, V)))
+    for b in range(B):
+        at = g.permutation(V)
+        x[b, 0, at[:equal]] = top
+        x[b, 0, at[:equal:2]] = top if top else -0.0
+        x[b, 0, at[equal:equal + 50]] = np.nan
+        x[b, 0, at[equal + 50:equal + 90]] = -np.inf
+    logits = torch.from_numpy(x).float().to(DT[dtype]).cuda()
+    for u in (g.random((B, 1)), np.zeros((B, 1)), np.full((B, 1), 1 - 2.0 ** -24)):
+        check(logits, u, temperature=0.8, top_k=k)
+        check(logits, u, temperature=[0.8, 2.0, 1e-3, 1.0, 50.0, np.inf], top_k=k, top_p=[0.5, 0.99, 0.9, 0.1, 0.7, 1e-9])
 
 
 @pytest.mark.gpu
