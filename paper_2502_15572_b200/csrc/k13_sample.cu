@@ -16,7 +16,7 @@
 // second one is the last for 16-bit logits as a rule, and looks at one group of 32 bins.  A small top_k needs none of this: see few().
 //
 // Measured (device): one row of 32000 with top_p 18 us, with top_k 50 12.5; ten drafts of ten of 32000 29.6; 16 sequences of 3 x 20 of 100003 77 (some 8600
-// cycles a row); 64 rows of 151001 in fp32 with top_k 40 25.5 (1.5 TB/s: the row is read at 4 TB/s or so, and five exchanges follow), top_k 200 103.
+// cycles a row); 64 rows of 151001 in fp32 with top_k 40 25.5 (1.5 TB/s: reading, then one exchange after the other), top_k 200 103.
 #include <atomic>
 #include <cfloat>
 
