@@ -264,8 +264,9 @@ struct Sampler {
         return ordered_to_float(u & 0x80000000u ? u : u | ((1u << low) - 1));
     }
 
-    // The row's largest logit and how many logits there are above -infinity.  Fills the cache; `mine`: the thread's largest.
-    __device__ __forceinline__ int maximum(float &mine)
+    // The row's largest logit and how many logits there are above -infinity.  Fills the cache; `mine`: the thread's largest.  first: the
+    // sequence's first row, nothing has been sent to another CTA yet.
+    __device__ __forceinline__ int maximum(float &mine, bool first)
     {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         float m = -INFINITY;
@@ -290,6 +291,7 @@ struct Sampler {
             s.warp_top[warp] = k;
         }
         __syncthreads();
+        if (first) cluster_wait();                            // every CTA has begun: its shared memory may be written
         if (warp == 0) {
             n = __reduce_add_sync(0xFFFFFFFFu, lane < kWarps ? s.warp_count[lane] : 0);
             k = __reduce_max_sync(0xFFFFFFFFu, lane < kWarps ? s.warp_top[lane] : 0u);
@@ -707,6 +709,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     uint4 *cache = reinterpret_cast<uint4 *>(smem + sizeof(Shared));
     const uint32_t rank = cluster_ctarank(), ctas = a.ctas;
     const int b = blockIdx.x / ctas;
+    cluster_arrive();                                         // waited for in the first row's maximum()
     if (threadIdx.x < kTable) s.table[threadIdx.x] = __double2ll_rn(exp2(62. - (double)threadIdx.x / kTable));
     pdl_wait();
     pdl_launch_dependents();
@@ -730,7 +733,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
         one.clear(0, 0);
         if (threadIdx.x == 0) s.few_count = 0;
         float mine;
-        const int valid = one.maximum(mine);
+        const int valid = one.maximum(mine, t == 0);
         one.scales();
         float logit = 0.f;
         int token = -1;

@@ -93,9 +93,6 @@ template <int kGroup, int kBlocks> struct Stage {
     static constexpr int kX = kTile * kCodeRow, kScales = kX + 8 * kBlocks * kXRow, kBytes = kScales + kTile * kScaleRow;
 };
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
 template <typename T, int kGroup, int kBlocks>
 __global__ void __launch_bounds__(kThreads) matmul_mma_kernel(const W4Args a)
 {
