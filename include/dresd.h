@@ -316,7 +316,9 @@ dresd_status dresd_drafts_sample(const void *logits, dresd_dtype dtype, int64_t 
  *   Products of (c - 8) and x are exact, their sums and the scales' products in fp32; one rounding, to `dtype`.  The order of
  *   summation depends on the sizes only.
  * Both are asynchronous on `stream`, on the current device; no workspace.
- * dresd_w4_status    dresd_store_status() for these calls: waits for `stream`, reports and clears the current device's status word.
+ * dresd_w4_status    dresd_store_status() for these calls: waits for `stream`, and returns DRESD_ERR_TIMEOUT if a wait ran out on the current device, on
+ *                    any stream, since the calling thread was last told (the first time: since the process began).  No thread's call takes a
+ *                    report from another thread.
  */
 enum { DRESD_MAX_W4_SIZE = 1 << 20 };
 dresd_status dresd_w4_quantise(const void *w, int64_t w_in, int64_t w_out, int inputs, int outputs, dresd_dtype dtype, int group,

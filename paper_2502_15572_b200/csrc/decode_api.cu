@@ -2,6 +2,8 @@
 // weights (k15_w4.cu).  Argument validation only.
 #include <atomic>
 #include <cstring>
+#include <map>
+#include <new>
 
 #include "api_util.h"
 
@@ -165,10 +167,22 @@ dresd_status dresd_w4_matmul(const void *x, int64_t x_row, int rows, const uint8
 
 dresd_status dresd_w4_status(void *stream)
 {
-    int word = 0;
-    const cudaError_t e = w4_status(&word, static_cast<cudaStream_t>(stream));
+    // The device counts and never forgets; every thread has its own mark, by device.  (A word that is read and cleared would lose what
+    // another stream reports between the two, and a report taken by one thread would be missing for the next.)
+    static thread_local std::map<int, unsigned int> told;
+    unsigned int count = 0;
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = w4_expired(&count, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return fail_cuda(e, "status read");
-    return word == 0 ? DRESD_OK : fail(DRESD_ERR_TIMEOUT, "a device-side wait expired");
+    try {
+        unsigned int &mark = told[dev];
+        if (mark == count) return DRESD_OK;
+        mark = count;
+    } catch (const std::bad_alloc &) {
+        return fail(DRESD_ERR_ALLOC, "host allocation failed");
+    }
+    return fail(DRESD_ERR_TIMEOUT, "a device-side wait expired");
 }
 
 }  // extern "C"

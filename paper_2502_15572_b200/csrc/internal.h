@@ -232,7 +232,7 @@ cudaError_t launch_w4_matmul(const W4Args &a, int dtype, int group, cudaStream_t
 int w4_umma_rows(int rows);
 cudaError_t launch_w4_umma(const CUtensorMap &code_map, const CUtensorMap &x_map, const W4Args &w, int dtype, int group, long long wait_cycles,
                            int lose_stage, int sms, cudaStream_t stream);
-cudaError_t w4_status(int *word, cudaStream_t stream);        // waits for `stream`; reads and clears the current device's word
+cudaError_t w4_expired(unsigned int *count, cudaStream_t stream);      // waits for `stream`; waits that ran out on the current device so far
 
 // ---- K14: pages of the cache ----
 enum { kPageMoves, kPageShared, kPageUsed, kPageCounts };

@@ -35,7 +35,7 @@ constexpr uint32_t kColumnsA = 384;                            // of the first s
 constexpr int kControl = 40, kUnpack = 56, kAdd = 160;         // registers of the roles' warps
 static_assert(kControl + 2 * kUnpack + 2 * kAdd <= 5 * 96, "what a CTA is launched with: 5 warpgroups of 96 a thread");
 
-__device__ int g_status;                                       // a wait ran out; see w4_status()
+__device__ unsigned int g_expired;                             // waits that ran out; see w4_expired()
 
 struct UmmaArgs {
     W4Args w;
@@ -208,7 +208,7 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
             // what is on its way arrives before the CTA ends
             for (int i = max(0, it - a.stages); i < it; ++i)
                 if (!mbar_wait(&sh.full[i % a.stages], (i / a.stages) & 1, wl)) ok = false;
-            if (!ok) report_timeout(&g_status);
+            if (!ok) atomicAdd(&g_expired, 1u);
         } else if (warp == 1 || warp == 2) {
             // One thread issues, the warp goes along: code that only one thread reaches takes 90 cycles an instruction, a product of 128 rows 64.  A
             // warp to each half: the waits and commits of a block take one warp 2000 cycles, its products 1024.
@@ -260,7 +260,7 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
             // no product may be running when TMEM is given back
             if (issuer) tc_commit(&sh.drained);
             if (!wait(&sh.drained, 0)) ok = false;
-            if (!ok && lane == 0) report_timeout(&g_status);
+            if (!ok && lane == 0) atomicAdd(&g_expired, 1u);
         }
     } else if (warp < 12) {
         set_registers<false, kUnpack>();
@@ -302,7 +302,7 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
                 a_phase ^= 1;
                 if (!ok) break;
             }
-        if (!ok && lane == 0) report_timeout(&g_status);
+        if (!ok && lane == 0) atomicAdd(&g_expired, 1u);
     } else {
         set_registers<true, kAdd>();
         const int half = (warp - 12) >> 2, quarter = warp & 3, r = half * 128 + quarter * 32 + lane;
@@ -378,7 +378,7 @@ matmul_umma_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_co
                 }
             }
         }
-        if (!ok && lane == 0) report_timeout(&g_status);
+        if (!ok && lane == 0) atomicAdd(&g_expired, 1u);
     }
     __syncwarp();
     if (a.split > 1) {
@@ -522,14 +522,10 @@ cudaError_t launch_w4_umma(const CUtensorMap &code_map, const CUtensorMap &x_map
     return dtype == kF16 ? by_group<__half>(group, code_map, x_map, a, sms, stream) : by_group<__nv_bfloat16>(group, code_map, x_map, a, sms, stream);
 }
 
-cudaError_t w4_status(int *word, cudaStream_t stream)
+cudaError_t w4_expired(unsigned int *count, cudaStream_t stream)
 {
-    *word = 0;
-    cudaError_t e = cudaMemcpyFromSymbolAsync(word, g_status, sizeof(int), 0, cudaMemcpyDeviceToHost, stream);
-    if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
-    if (e != cudaSuccess || *word == 0) return e;
-    const int zero = 0;
-    e = cudaMemcpyToSymbolAsync(g_status, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, stream);
+    *count = 0;
+    const cudaError_t e = cudaMemcpyFromSymbolAsync(count, g_expired, sizeof *count, 0, cudaMemcpyDeviceToHost, stream);
     return e == cudaSuccess ? cudaStreamSynchronize(stream) : e;
 }
 
