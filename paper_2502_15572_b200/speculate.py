@@ -85,6 +85,8 @@ class Decoder:
 class Speculator:
     """Continues prompts with drafts of a datastore (or without, n = 0): a cache, its pages and the sequences' state.
 
+    room: places behind a prompt, so texts of up to room + 1 tokens (the last one needs no place).  A sequence whose drafts are accepted may be ahead of the
+    others: what ``step`` returns of it beyond its room is not part of its text.
     samples: sequences of every prompt, one after the other (sequence b * samples + s); the prompt is read once.  temperature > 0: tokens are drawn
     (top_k, top_p as in dresd_drafts_sample), the token at place p of sequence q with the random number random[q][p] that
     `seed` gives, so that a text does not depend on its drafts; 0: the largest logit, and samples are alike."""
@@ -125,6 +127,7 @@ class Speculator:
             self.random = torch.rand((most, self.B), generator=torch.Generator().manual_seed(seed)).t().contiguous().to(device)
         # a sequence may be ahead of the others when they are done: what it writes beyond its room takes the same places again
         self.limit = torch.tensor([len(p) + room for p in prompts], dtype=torch.int32, device=device).repeat_interleave(samples)
+        self.steps_left = room                                 # a step writes a token at least: then every sequence is at its limit
         self.logs = torch.zeros((self.B, 1), device=device)        # of the last tokens' probabilities, where tokens are drawn
         # places of a step's chunk: of its first token on, in the sequence
         self.offset = torch.tensor([0] + [1 + t for _ in range(self.n) for t in range(self.L)], device=device).repeat(self.B)
@@ -170,6 +173,9 @@ class Speculator:
         import torch
         if self.pages is None:
             raise ValueError("the sequences have ended")
+        if self.steps_left < 1:
+            raise ValueError("no sequence has room for another token")
+        self.steps_left -= 1
         B, n, L = self.B, self.n, self.L
         chunk, drafts, valid = self.last[:, None], None, None
         if n:
@@ -209,9 +215,12 @@ class Speculator:
         return out, length
 
     def run(self, count: int):
-        """At least `count` tokens for every sequence: lists of tokens, and the steps that it took.  ``score``: the logarithms of
-        their probabilities, where tokens are drawn."""
+        """At least `count` tokens for every sequence, from its last one on: lists of tokens, and the steps that it took.  ``score``: the
+        logarithms of their probabilities, where tokens are drawn."""
         import torch
+        left = int((self.limit - self.ctx).min())
+        if count > left + 1:
+            raise ValueError(f"{count} tokens for sequences with room for {left + 1}")
         texts, logs, steps = [[int(t)] for t in self.last.tolist()], [row[:1] for row in self.logs.tolist()], 0
         while min(map(len, texts)) < count:
             out, length = self.step()
