@@ -1,6 +1,7 @@
 // What the C entry points share: messages of failing calls, checks of addresses, tensor maps.
 #pragma once
 
+#include <atomic>
 #include <cstdarg>
 #include <cstdio>
 
@@ -46,13 +47,14 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
 
 inline EncodeTiledFn encode_tiled_fn()
 {
-    static EncodeTiledFn fn = nullptr;
+    static std::atomic<EncodeTiledFn> known{nullptr};      // several host threads may come here first
+    EncodeTiledFn fn = known.load();
     if (!fn) {
         void *p = nullptr;
         cudaDriverEntryPointQueryResult q;
         if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
             q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<EncodeTiledFn>(p);
+            known.store(fn = reinterpret_cast<EncodeTiledFn>(p));
     }
     return fn;
 }

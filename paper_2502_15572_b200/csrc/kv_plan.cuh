@@ -2,6 +2,8 @@
 // division of the attention's work over the CTAs.
 #pragma once
 
+#include <atomic>
+
 #include "common.cuh"
 #include "internal.h"
 
@@ -433,15 +435,15 @@ cudaError_t launch_workers(void (*kernel)(KArgs...), int threads, int smem, int 
     if (ctas > 1) {
         // by device and kernel type; every kernel of a type fills an SM
         constexpr int kDevices = 16;                        // of more than these it is asked every time
-        static int held[kDevices][kMaxCluster + 1] = {};
+        static std::atomic<int> held[kDevices][kMaxCluster + 1];
         int device = 0;
         cudaError_t e = cudaGetDevice(&device);
-        int n = e == cudaSuccess && device < kDevices ? held[device][ctas] : 0;
+        int n = e == cudaSuccess && device < kDevices ? held[device][ctas].load() : 0;
         if (n == 0) {
             if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
             if (e != cudaSuccess) return e;
             if (n < 1) n = 1;
-            if (device < kDevices) held[device][ctas] = n;
+            if (device < kDevices) held[device][ctas].store(n);
         }
         if ((int)cfg.gridDim.x > n * ctas) cfg.gridDim.x = n * ctas;
     }

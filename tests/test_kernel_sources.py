@@ -42,3 +42,11 @@ def test_a_cluster_barrier_comes_before_the_first_access(name, kernel, reach):
     text = body(read(name), kernel)
     before = text[:text.index(reach)]
     assert "cluster_sync_all()" in before or "cluster_wait()" in before
+
+
+@pytest.mark.parametrize("name", sorted(n for n in os.listdir(CSRC) if n.endswith((".cu", ".cuh", ".h"))))
+def test_what_calls_remember_is_atomic(name):
+    """Calls of several host threads may be the first ones together: what a function keeps for the process is an atomic, a thread's own, or constant."""
+    text = re.sub(r"//[^\n]*", "", read(name))
+    kept = re.findall(r"^ +static (?!const|__device__|cudaError_t|inline)([^;=({]+)[;={]", text, re.M)
+    assert all(k.startswith(("std::atomic<", "thread_local ")) for k in kept), kept
