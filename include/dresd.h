@@ -272,7 +272,7 @@ dresd_status dresd_retrieve_quantised(dresd_store *store, const void *queries, c
  * A row's distribution, from x_i = its logits (NaN counts as -infinity, which is never drawn; -0 as 0):
  *   temperature[b] > 0      w_i = round(2^42 exp((x_i - max x) / temperature)), a whole number: sums are exact, do not depend on
  *                           their order, and the tokens not on the batch.  The exponential is off by less than 2^-28 of itself (the
- *                           largest logits' by nothing); temperatures above 10^36 count as that.
+ *                           largest logits' by nothing); temperatures below 10^-36 and above 10^33 count as those.
  *   otherwise (0, < 0, NaN) the largest logit, the lowest index of equal ones (uniform is not used); log-probability 0
  *   top_k[b] > 0            only the top_k largest logits, the lowest indices of equal ones
  *   top_p[b] < 1            of these, in descending order and then by index, the fewest whose sum of w is at least top_p times all of

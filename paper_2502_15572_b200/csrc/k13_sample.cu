@@ -565,7 +565,7 @@ struct Sampler {
             if (first && cut.ties > 0 && cut.x >= bottom && cut.x <= most && bin(cut.x) == hit)
                 add_one<by_weight>((int)((hi - key(cut.x)) >> shift), (u64)cut.ties * (by_weight ? weight(cut.x) : 1));
             const uint32_t at = (uint32_t)find(((int)((hi - lo) >> shift) | 31) + 1, before, target, -1.f);
-            const uint32_t key_hi = hi - (at << shift);
+            const uint32_t key_hi = hi - min(at << shift, hi - lo);            // not below lo: the range shrinks whatever the sums are, and the search ends
             most = of_key(key_hi);
             if (shift == 0) break;
             bottom = of_key(max(lo, key_hi - ((1u << shift) - 1)));
@@ -724,8 +724,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a,
     unsigned live = 0;
     for (int r = 0; r < n; ++r) live |= (a.valid[(long long)b * n + r] != 0 ? 1u : 0u) << r;
     int best = __ffs(live) - 1, t = 0;
-    // an infinite temperature times infinitely small a logit would be no number
-    if (threadIdx.x == 64) Sampler<T>::set_rate(s, greedy ? 1. : 1.4426950408889634 / (double)fminf(temperature, 1e36f));
+    // 64 log2(e) / T has to be finite (from 10^-37 down it is not, and weights were no numbers), and the low part of log2(e) / T needs its bits (at
+    // 10^36 it is a subnormal number with six, and weights were off by 2^-27)
+    if (threadIdx.x == 64) Sampler<T>::set_rate(s, greedy ? 1. : 1.4426950408889634 / (double)fminf(fmaxf(temperature, 1e-36f), 1e33f));
     while (true) {
         const int at = t == 0 ? 0 : 1 + best * L + t - 1;
         Sampler<T> one(s, cache, cached, rank, ctas, logits + (long long)at * a.row_stride, a.V);

@@ -1,12 +1,11 @@
-"""Verification by sampling where few calls go: CTAs that begin late, rows so long that an entry stands for several steps, temperatures at
-their ends, and the weights themselves."""
+"""Verification by sampling where few calls go: CTAs that begin late, temperatures at their ends."""
 import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 
 from paper_2502_15572_b200 import binding
-from tests.test_drafts_sample_gpu import DT, ONE, check, chunk, ref_row
+from tests.test_drafts_sample_gpu import DT, chunk, ref_row
 
 pytestmark = pytest.mark.gpu
 
@@ -36,3 +35,47 @@ def test_clusters_of_a_busy_gpu():
     torch.cuda.synchronize()
     for i, outs in got:
         assert all(torch.equal(a, b) for a, b in zip(outs, want[i]))
+
+
+# ---- temperatures at their ends ------------------------------------------------------------------------------------
+def check_clipped(logits, uniform, temperature, top_k=0, top_p=1.0):
+    """check() with temperatures brought into 10^-36 .. 10^33; a weight is off by 2^-28, so the logarithm of their sum by less than 2^-27."""
+    B = logits.shape[0]
+    new = lambda x, dtype: torch.full((B,), x, dtype=dtype, device="cuda")
+    got = binding.drafts_sample(logits, torch.from_numpy(uniform.astype(np.float32)).cuda(), temperature=torch.from_numpy(temperature).cuda(),
+                                top_k=new(top_k, torch.int32), top_p=new(top_p, torch.float32))
+    x = logits.double().cpu().numpy()
+    for b in range(B):
+        T = min(max(np.float64(temperature[b]), np.float64(np.float32(1e-36))), np.float64(np.float32(1e33)))
+        token, log = ref_row(x[b, 0], np.float32(uniform[b, 0]), T, top_k, np.float32(top_p))
+        assert int(got[2][b, 0]) == token, (b, T, int(got[2][b, 0]), token)
+        assert abs(float(got[3][b, 0]) - log) <= 2.0 ** -24 * abs(log) + 2.0 ** -27, (b, T, float(got[3][b, 0]), log)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top_k,top_p", [(0, 1.0), (7, 1.0), (300, 0.8), (0, 0.7)])
+@pytest.mark.parametrize("temperature", [2.0 ** -149, 1e-45, 1e-42, 1e-40, 1e-38, 1e-37, 1e-36, 1e-35])
+def test_small_temperatures(temperature, top_k, top_p, dtype):
+    """Logits within a few hundred temperatures of each other, subnormal numbers among them, around zero and away from it.  (Of 1000 borders one
+    is next to a random number, within 2^-28 of the whole, with a probability of 2^-18.)"""
+    g = np.random.default_rng(11)
+    T = np.float32(temperature)
+    x = -np.abs(g.standard_normal((6, 1, 1000))) * 20 * max(np.float64(T), 2e-44)
+    x[1] += 5 * np.float64(T)
+    x[2, 0, ::3] = 0
+    x[3] = np.float32(-2.0 ** -149) * g.integers(0, 9, 1000)
+    x[4, 0, 500:] = -np.inf
+    x[5] *= 1e8
+    check_clipped(torch.from_numpy(x).to(DT[dtype]).cuda(), g.random((6, 1)), np.full(6, T), top_k, top_p)
+
+
+@pytest.mark.parametrize("top_k,top_p", [(0, 1.0), (7, 1.0), (0, 0.7)])
+@pytest.mark.parametrize("temperature", [1e30, 1e33, 1e34, 1e35, 1e36, 1e38, np.inf])
+def test_large_temperatures(temperature, top_k, top_p):
+    g = np.random.default_rng(12)
+    T = np.float32(temperature)
+    x = g.standard_normal((4, 1, 1000)) * 5 * min(np.float64(T), 1e33)
+    x[1] *= 100
+    x[2] = np.where(g.random((1, 1000)) < 0.5, 3e38, -3e38)
+    x[3] = x[3] / 1e20
+    check_clipped(torch.from_numpy(x).float().cuda(), g.random((4, 1)), np.full(4, T), top_k, top_p)
