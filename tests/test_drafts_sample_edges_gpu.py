@@ -1,4 +1,5 @@
-"""Verification by sampling where few calls go: CTAs that begin late, temperatures at their ends."""
+"""Verification by sampling where few calls go: CTAs that begin late, rows so long that an entry stands for several steps, temperatures at
+their ends."""
 import numpy as np
 import pytest
 
@@ -79,3 +80,51 @@ def test_large_temperatures(temperature, top_k, top_p):
     x[2] = np.where(g.random((1, 1000)) < 0.5, 3e38, -3e38)
     x[3] = x[3] / 1e20
     check_clipped(torch.from_numpy(x).float().cuda(), g.random((4, 1)), np.full(4, T), top_k, top_p)
+
+
+# ---- rows so long that an entry of a warp's sums stands for several of its steps -----------------------------------
+def alone(logits, u, settings, size):
+    """The same rows, `size` at a time: more CTAs a row, and fewer steps of each."""
+    parts = [binding.drafts_sample(logits[b:b + size], u[b:b + size], **{k: v[b:b + size] for k, v in settings.items()}) for b in range(0, logits.shape[0], size)]
+    return [torch.cat(p) for p in zip(*parts)]
+
+
+@pytest.mark.parametrize("dtype,V", [("bf16", 151937), ("f16", 262147), ("f32", 70001), ("f32", 200003)])
+@pytest.mark.parametrize("values", ["many", "few"])
+def test_one_cta_for_a_long_row(dtype, V, values):
+    """One CTA has more than 16384 blocks of 16 bytes: entries of 2 or 4 steps."""
+    B = 152
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn((B, 1, V), device="cuda", generator=g) * 2
+    logits = (x.round() if values == "few" else x).to(DT[dtype])
+    del x
+    random = np.random.default_rng(V)
+    u = random.random((B, 1)).astype(np.float32)
+    u[:4, 0] = 0, 1 - 2.0 ** -24, 2.0 ** -24, 0.5
+    kind = np.arange(B) % 4                                   # all tokens, top_p, top_k and top_p, the largest
+    t, k, p = np.where(kind == 3, 0, 0.9).astype(np.float32), np.where(kind == 2, 1000, 0).astype(np.int32), np.where(kind % 3 == 0, 1, 0.9).astype(np.float32)
+    settings = dict(temperature=torch.from_numpy(t).cuda(), top_k=torch.from_numpy(k).cuda(), top_p=torch.from_numpy(p).cuda())
+    ud = torch.from_numpy(u).cuda()
+    got = binding.drafts_sample(logits, ud, **settings)
+    for a, b in zip(got, alone(logits, ud, settings, 8)):
+        assert torch.equal(a, b)
+    for b in list(range(12)) + [B - 1]:
+        token, log = ref_row(logits[b, 0].double().cpu().numpy(), u[b, 0], np.float64(t[b]), k[b], p[b])
+        assert int(got[2][b, 0]) == token
+        assert abs(float(got[3][b, 0]) - log) <= 2.0 ** -24 * abs(log) + 2.0 ** -27
+
+
+def test_one_cta_for_the_longest_row():
+    """2^20 logits in fp32: entries of 16 steps or 32.  The last token with weight lies at the very end, in a step that is not full."""
+    B, V = 150, 1 << 20
+    wide = torch.randn((B, 1, V + 1), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    logits = wide[:, :, 1:] if wide.data_ptr() % 16 == 0 else wide[:, :, :V]        # rows begin anywhere in a block
+    u = torch.rand((B, 1), device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    u[0], u[1] = 0, 1 - 2.0 ** -24
+    logits[2, 0, :-1] = -float("inf")
+    for p in (1.0, 0.5):
+        settings = dict(top_p=torch.full((B,), p, device="cuda"))
+        got = binding.drafts_sample(logits, u, **settings)
+        for a, b in zip(got, alone(logits, u, settings, 6)):
+            assert torch.equal(a, b)
+        assert int(got[2][2, 0]) == V - 1
