@@ -1,12 +1,12 @@
 """Verification by sampling where few calls go: CTAs that begin late, rows so long that an entry stands for several steps, temperatures at
-their ends."""
+their ends, and the weights themselves."""
 import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 
 from paper_2502_15572_b200 import binding
-from tests.test_drafts_sample_gpu import DT, chunk, ref_row
+from tests.test_drafts_sample_gpu import DT, ONE, chunk, ref_row
 
 pytestmark = pytest.mark.gpu
 
@@ -128,3 +128,58 @@ def test_one_cta_for_the_longest_row():
         for a, b in zip(got, alone(logits, u, settings, 6)):
             assert torch.equal(a, b)
         assert int(got[2][2, 0]) == V - 1
+
+
+# ---- the weights -----------------------------------------------------------------------------------------------------
+def brackets(w, N, M, g, below):
+    """(u, j) for a row of N logits of weight W, w or nearly, and M of 2^42 behind them: u S >= j W exactly if W <= theta = u M 2^42 / (j - u N).  theta
+    lies beyond what W may be, w (1 +- 2^-28) and half a unit: by 2^-29 at most (or 1/4)."""
+    edge = w * (1 - 2.0 ** -28) - 0.5 if below else w * (1 + 2.0 ** -28) + 0.5
+    room = max(w * 2.0 ** -29, 0.25)
+    q = M * 2.0 ** 42 / (edge + (-0.5 if below else 0.5) * room)      # j - u N over u
+    scale = 2.0 ** -np.ceil(max(0.0, np.log2((N + q) / N)))
+    for _ in range(4):
+        u = g.integers(1 << 23, 1 << 24, 1 << 20) * 2.0 ** -24 * scale
+        j = np.rint(u * (N + q))
+        with np.errstate(divide="ignore"):
+            theta = u * M * 2.0 ** 42 / (j - u * N)           # j, u N: exact in 53 bits; relative error 2^-51
+        off = (edge - theta if below else theta - edge)
+        fits = np.flatnonzero((off > room * 2.0 ** -6) & (off < room) & (j >= 1) & (j <= N))
+        if len(fits):
+            return u[fits[0]], int(j[fits[0]])
+    return None
+
+
+@pytest.mark.parametrize("temperature,top", [(1.0, 0.0), (0.7, 3.25), (0.05, -11.5), (1.3, 100.0), (0.7, 5000.0), (0.1, -900.0), (1e-36, 7e-36), (1e33, 2e34), (1e-30, 1e-26)])
+def test_a_weight_is_off_by_less_than_its_bound(temperature, top):
+    """The documented bound, 2^-28 of the weight and the rounding to a whole number, from both sides: a random number that draws a
+    token for every weight within the bound, and one that does not.  (log_probabilities in fp32 are too coarse to show it.)  |top| / T above
+    2^12 ln 2 takes another form of the difference."""
+    g = np.random.default_rng(3)
+    T, rows = np.float64(np.float32(temperature)), []
+    N, top = 1 << 14, np.float32(top)
+    gaps = np.concatenate((np.geomspace(1e-3, 26, 24), np.arange(1, 9) * np.log(2) / 64 * 7.5))
+    for gap in gaps:
+        x = np.float32(np.float64(top) - gap * T)
+        if x == top:
+            continue
+        w = ONE * np.exp((np.float64(x) - np.float64(top)) / T)
+        for below in (False, True):
+            M, found = 0, None
+            while found is None:                              # (some M have few random numbers that come near)
+                M = int(max(1, g.uniform(0.7, 1.3) * 2.0 ** 13 * w / ONE))
+                found = brackets(w, N, M, g, below)
+            rows.append((x, M, below, *found))
+    most = N + max(r[1] for r in rows)
+    logits = np.full((len(rows), 1, most), -np.inf, dtype=np.float32)
+    for i, (x, M, _, _, _) in enumerate(rows):
+        logits[i, 0, :N] = x
+        logits[i, 0, N:N + M] = top
+    u = np.array([r[3] for r in rows])
+    assert (u == u.astype(np.float32)).all()
+    got = binding.drafts_sample(torch.from_numpy(logits).cuda(), torch.from_numpy(u.astype(np.float32)[:, None]).cuda(),
+                                temperature=torch.full((len(rows),), float(T), device="cuda"))[2][:, 0].tolist()
+    assert len(rows) > 20
+    for y, (x, M, below, _, j) in zip(got, rows):
+        # the token is the first one whose running sum exceeds floor(u S): j or later exactly if j W <= u S
+        assert (y >= j) is (not below), (x, y, j, below)

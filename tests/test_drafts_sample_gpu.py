@@ -1,10 +1,14 @@
 """Verification by sampling: the definition in numpy (weights as whole numbers, sums exact) on the CPU.
 
-Tokens, lengths and drafts have to be equal.  A weight is a rounded 2^42 exp(.), float64 on both sides, so two computations may differ by one
-unit where exp falls next to a half; a border between tokens then moves by at most V units in V 2^42 or more, 2^-42 of
-the whole, and one of the few thousand random numbers here lies that near to one of at most 2^20 borders with a probability below 2^-10.
-Log-probabilities: one rounding to fp32 (2^-24 of the value) of a float64 value, whose own error (exp, log, sums: a few 2^-52, and a
-unit in the sum) is below 2^-40.
+Tokens, lengths and drafts have to be equal.  A weight is 2^42 exp(.) rounded to a whole number; here exp is float64's, the kernel's is off by up to 2^-28 of
+itself.  At a border R between tokens, u S against R then moves by at most 2 u (1 - u) 2^-28 S, and a random number lies between the two places with
+a probability of no more than that; over V borders, and u anywhere, V 2^-28 / 3.  That is for errors of one sign.  They change sign from logit to logit, and these
+rows have their weight on N > 2^10 of V logits, so the sums' errors are sqrt(N) times smaller: V 2^-34 or so, 2^-14 for the longest rows here
+(2^20), of which there are four random numbers, and 2^-17 for the few hundred of some 10^5.  Inputs are fixed, so equality that holds stays.
+Log-probabilities, x - ln S in units of the temperature: one rounding to fp32, 2^-24 of the value, and ln S is off by at most 2^-28 of itself (the largest logit's
+weight is exact: S = 1 + R, off by 2^-28 R, and ln(1 + R) >= R / (1 + R)), so by at most 2^-28 of the value, which is not smaller.  The tolerance
+leaves 2^-40 for that in place of 2^-28 of the value, again since errors of both signs meet in a sum; tests/test_drafts_sample_edges_gpu.py has the full
+bound, and the weights' own.
 """
 import numpy as np
 import pytest
