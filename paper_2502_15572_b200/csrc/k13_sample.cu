@@ -3,9 +3,12 @@
 // A sequence is a chain: the token drawn at depth t decides which row of logits is read at depth t + 1, so that only the rows on
 // the path are read, at most L + 1 of the 1 + n L.  One cluster follows a sequence; its CTAs share a row by contiguous pieces, which
 // they keep in shared memory as far as it goes.  Per row: the maximum; the cuts of top_k and top_p; the weights' sums piece by piece; and
-// the piece, warp, lane and element where the running sum passes u times the whole.  Every step ends in an exchange through the cluster, a
-// barrier (some 700 cycles) and loads from the other CTAs' shared memory (some 500): latency, not bytes, is what a row costs.  Instructions
-// come from far at the first depth, so loops are not unrolled where that multiplies long code (32000 logits, top_p: 22.0 us a row so, 18.8 us without).
+// the piece, warp, lane and element where the running sum passes u times the whole.  Bytes are not what a row costs.  32000 16-bit logits in 16 CTAs, top_p, the second row
+// of a sequence and later ones, cycles by the SM's clock at one thread (24600 in all; each step's wait for slower warps and CTAs is part of the next one):
+//     reading and the CTA's maximum 1000, its exchange 1400; first histogram 4300, its search 6400 (with the wait for the slowest
+//     CTA's histogram); second one 1400, 2500; pass for the running sums 1900, their sums in the CTA 900, exchange 1400; search for the token 1000, last exchange 2000;
+//     the next row's choice 400.  Without top_p 11400.
+// Instructions come from far at the first depth (30000 cycles; 45000 in a process's first call), so loops are not unrolled where that multiplies long code (32000 logits, top_p: 22.0 us a row so, 18.8 us without).
 //
 // A weight is rint(2^42 e^((x - max) / T)), a whole number: sums are exact, so they depend neither on their order nor on how
 // many CTAs share a row, and a token is the same whatever the batch.
@@ -16,7 +19,8 @@
 // second one is the last for 16-bit logits as a rule, and looks at one group of 32 bins.  A small top_k needs none of this: see few().
 //
 // Measured (device): one row of 32000 with top_p 18 us, with top_k 50 12.5; ten drafts of ten of 32000 29.6; 16 sequences of 3 x 20 of 100003 77 (some 8600
-// cycles a row); 64 rows of 151001 in fp32 with top_k 40 25.5 (1.5 TB/s: reading, then one exchange after the other), top_k 200 103.
+// cycles a row); 64 rows of 151001 in fp32, normal logits: greedy 27.8, temperature alone 49, top_k 40 25.5 (1.5 TB/s: reading, then one exchange after the other), top_k 200 70, with
+// top_p 110, top_p alone 103 (spread 4, temperature 0.7) to 120 (2, 1): whole rows are gone through three times, their weights computed twice.
 #include <atomic>
 #include <cfloat>
 

@@ -5,8 +5,9 @@
 //
 // Bound: the weights' bytes, and on small matrices the latency of fetching them once.  A CTA has 128 outputs and 256 inputs at a time, up to three of these
 // steps on their way by cp.async; the CTAs of a cluster split the inputs, so that on small matrices every byte is on its way from the
-// start, and add their parts up in the order of their ranks.  Measured (device): one row of 4096 x 4096 6.1 us, 7 rows of 4096 x 11008 12.5 us
-// (1.9 TB/s: launch, fetch, products and join of a CTA follow one another, and most CTAs do the same at the same time).
+// start, and add their parts up in the order of their ranks.  Measured (device): one row of 4096 x 4096 6.2 us, 7 rows of 4096 x 11008 12.5 us, one row of
+// 4096 x 32000 27 us: 1.9 to 2.5 TB/s, so neither bytes nor a small matrix's latency bounds the larger ones.  A CTA goes through two steps, joins and
+// ends, nothing is on its way from one tile to the next, and 11008 outputs are a wave and a part (688 CTAs, 592 resident).
 //
 // A warp computes 32 outputs for up to 8 kBlocks rows with mma.sync, weights as the 16-row operand.  The order of inputs within an
 // instruction is free, as long as both operands agree: a lane takes 8 or 16 consecutive codes of a row (4 lanes a row, 8 rows
@@ -257,7 +258,8 @@ __global__ void __launch_bounds__(kThreads) matmul_mma_kernel(const W4Args a)
 }
 
 // ---- quantisation --------------------------------------------------------------------------------------------------
-// One thread a group of an output; neighbours take neighbouring outputs (or, of weights that lie by outputs, groups).
+// One thread a group of an output; neighbours take neighbouring outputs (or, of weights that lie by outputs, groups).  Done once for a matrix, and not
+// made fast: 4096 x 11008 with adjacent outputs 99 us, with adjacent inputs 397 (90 MB in: 14 us).
 template <typename T, int kGroup>
 __global__ void __launch_bounds__(128)
 quantise_kernel(const T *__restrict__ w, long long w_in, long long w_out, int groups, int outputs, uint8_t *__restrict__ codes,
